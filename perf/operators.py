@@ -141,7 +141,8 @@ def _quantise(x, bits):
     """x [..., D] -> codes as floats in [-M, M] and scales [..., D / 32] in bf16."""
     most = 127.0 if bits == 8 else 7.0
     g = x.float().reshape(*x.shape[:-1], -1, GROUP)
-    scale = (g.abs().amax(-1) / most).to(torch.bfloat16)
+    # (a Python number as divisor would become a product with its reciprocal)
+    scale = (g.abs().amax(-1) / torch.full((), most, device=x.device)).to(torch.bfloat16)
     s = scale.float().unsqueeze(-1)
     code = torch.where(s > 0, torch.round(g / s), torch.zeros_like(g)).clamp(-most, most)
     return code.reshape(x.shape), scale
@@ -498,7 +499,8 @@ def _unit64(x, bits):
     """What rows x stand for after they were stored."""
     top = 127 if bits == 8 else 7
     x = x.double()
-    s = (x.unflatten(-1, (-1, 32)).abs().max(-1, keepdim=True).values.float() / top).bfloat16().double()
+    a = x.unflatten(-1, (-1, 32)).abs().max(-1, keepdim=True).values.float()
+    s = (a / torch.tensor(float(top), device=x.device)).bfloat16().double()
     c = torch.round(x.unflatten(-1, (-1, 32)) / torch.where(s == 0, torch.ones_like(s), s))
     return (c.clip(-top, top) * s).flatten(-2)
 
