@@ -1,4 +1,4 @@
-"""Builds libheadkv.so (the C-ABI of include/hkv.h) and the synthetic-input
+"""Builds libheadkv.so (the C-ABI of include/hkv.h and include/hkv_serve.h) and the synthetic-input
 generator library for sm_103a with nvcc, in tree.
 
 Translation units compile in parallel; objects go to the package's _build/
@@ -23,7 +23,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
-SOURCES = ["hkv_api.cu", "hkv_attention.cu", "hkv_step.cu", "hkv_update.cu", "hkv_noalloc.cu"]
+SOURCES = ["hkv_api.cu", "hkv_attention.cu", "hkv_step.cu", "hkv_update.cu", "hkv_noalloc.cu",
+           "hkv_serve_api.cu", "hkv_quant.cu", "hkv_quant_attn.cu", "hkv_prefix.cu"]
 
 
 def nvcc() -> str:
@@ -63,7 +64,7 @@ def build(force: bool = False, extra_flags=(), lib_path: str | None = None,
     os.makedirs(bdir, exist_ok=True)
     cc = nvcc()
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    headers.append(os.path.join(ROOT, "include", "hkv.h"))
+    headers += [os.path.join(ROOT, "include", h) for h in ("hkv.h", "hkv_serve.h")]
     objs, cmds = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

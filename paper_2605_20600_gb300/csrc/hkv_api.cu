@@ -13,14 +13,12 @@
 #include <vector>
 
 #include "hkv.h"
+#include "hkv_host.h"
 #include "hkv_kernels.h"
 
 namespace {
 
 using namespace hkv;
-
-constexpr int kMaxDevices = 64;
-constexpr size_t kMaxSmem = 227 * 1024;
 
 // Per-device launch setup, filled on first use. Every field is written at
 // most once (under g_mu) and read lock-free: atomics with acquire/release
@@ -36,20 +34,8 @@ struct DeviceState {
 DeviceState g_dev[kMaxDevices];
 std::mutex g_mu;
 
-hkv_status injected(const char *name) {
-  const char *s = getenv("HKV_FAULT_INJECT");
-  if (!s) return HKV_OK;
-  const size_t n = strlen(name);
-  if (strncmp(s, name, n) == 0 && s[n] == ':') return (hkv_status)atoi(s + n + 1);
-  return HKV_OK;
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int dt_index(int dtype) { return dtype == HKV_BF16 ? 1 : 0; }
 int d_index(int D) { return D == 128 ? 1 : 0; }
-
-hkv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? HKV_OK : HKV_ERR_CUDA; }
 
 // Per-device, per-(D, dtype) launch setup (shared memory limits, occupancy);
 // done on the first call that needs it, outside any stream capture.
@@ -100,66 +86,6 @@ hkv_status update_ready(DeviceState *st, int D, int dtype, size_t smem) {
   }
   return HKV_OK;
 }
-
-hkv_status check_cache(const hkv_cache *c) {
-  if (!c || !c->k || !c->v || !c->pos || !c->off || !c->cap || !c->len || !c->nbuf || !c->ntok ||
-      !c->label || !c->qbuf || !c->err)
-    return HKV_ERR_INVALID_ARG;
-  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->qbuf)) return HKV_ERR_ALIGN;
-  if (c->capacity_tokens <= 0) return HKV_ERR_CAPACITY;
-  return HKV_OK;
-}
-
-CacheArgs cache_args(const hkv_cache *c) {
-  CacheArgs a;
-  a.K = c->k;
-  a.V = c->v;
-  a.pos = c->pos;
-  a.off = c->off;
-  a.cap = c->cap;
-  a.len = c->len;
-  a.nbuf = c->nbuf;
-  a.ntok = c->ntok;
-  a.label = c->label;
-  a.qbuf = c->qbuf;
-  a.err = c->err;
-  a.arena_tokens = c->capacity_tokens;
-  return a;
-}
-
-MethodArgs method_args(const hkv_config *cfg) {
-  MethodArgs m;
-  m.C = cfg->n_cond;
-  m.w = cfg->recent_w;
-  m.w_loc = cfg->local_w;
-  m.P = cfg->period;
-  m.r_s = cfg->r_s;
-  m.tau = (float)cfg->tau;
-  m.grid2d = cfg->distance_mode == HKV_DIST_GRID2D ? 1 : 0;
-  m.row_len = cfg->row_len;
-  return m;
-}
-
-int heads_per_layer(const hkv_config *c) { return c->n_seqs * c->n_heads; }
-
-// longest segment any call may see: a dense head (C + E) or a compressed
-// global head right before its update (C + B_g + P)
-// the longest segment the config allows: the dense cache at grouping, or a
-// global head's C + budget + P tokens (never more than C + N); a
-// redistributed budget reaches B_g + (H - 1)(B_g - w) for a group of one
-// global head
-int max_segment(const hkv_config *c) {
-  const int a = c->n_cond + c->group_at;
-  long long bud = c->global_budget;
-  if (c->budget_mode == HKV_BUDGET_REDISTRIBUTE)
-    bud += (long long)(c->n_heads - 1) * (c->global_budget - c->recent_w);
-  long long kept = bud + c->period;
-  if (kept > c->n_image) kept = c->n_image;
-  const int b = c->n_cond + (int)kept;
-  return a > b ? a : b;
-}
-
-size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 constexpr size_t kCtlBytes = 256;  // AttnCtl, padded
 
@@ -285,12 +211,6 @@ bool one_launch_step(const hkv_config *cfg, int grid) {
   if (chunk < 2) chunk = 2;
   return chunk + 1 <= kStepTable;
 }
-
-#define HKV_TRY(x)                 \
-  do {                             \
-    hkv_status s_ = (x);           \
-    if (s_ != HKV_OK) return s_;   \
-  } while (0)
 
 }  // namespace
 

@@ -1,0 +1,288 @@
+// The quantised cache outside its attention: rows written from a plain cache
+// (pack), read back into one (unpack), and the periodic head-aware update.
+#include "hkv_quant.cuh"
+#include "hkv_quant.h"
+#include "hkv_select.cuh"
+
+namespace hkv {
+namespace {
+
+// rows per CTA of pack and unpack: 8 values a thread, D / 8 threads a row
+constexpr int kRowThreads = 256;
+constexpr int kRowsPerCta = 64;
+
+__device__ __forceinline__ bool segment_ok(long long off, int cap, int len, long long arena) {
+  return off >= 0 && cap >= 0 && off + cap <= arena && len >= 0 && len <= cap;
+}
+
+// One CTA: up to kRowsPerCta rows of one head. Block 0 of a head also sets
+// its counters.
+template <int D, typename T, int BITS>
+__global__ void __launch_bounds__(kRowThreads)
+    pack_kernel(const CacheArgs src, const QCacheArgs dst, int first, int blocks, int skip,
+                int max_len) {
+  using R = QRow<D, BITS>;
+  constexpr int TPR = D / 8;  // threads per row
+  // no early launch of the next kernel: a decode step that prefetches this
+  // cache before its own wait must start after the rows are written
+  pdl_wait();
+  const int i = first + (int)(blockIdx.x / blocks), b = (int)(blockIdx.x % blocks);
+  const int tid = threadIdx.x;
+  const int len = src.len[i], scap = src.cap[i], dcap = dst.c.cap[i];
+  const long long soff = src.off[i], doff = dst.c.off[i];
+  const int n = len - skip;
+  uint32_t bad = 0;
+  if (!segment_ok(soff, scap, len, src.arena_tokens) ||
+      !segment_ok(doff, dcap, 0, dst.c.arena_tokens))
+    bad = HKV_ERR_BOUNDS;
+  else if (n < 0)
+    bad = HKV_ERR_STATE;
+  else if (n > dcap || len > max_len)
+    bad = HKV_ERR_CAPACITY;
+  if (bad) {
+    if (tid == 0 && b == 0) set_err(dst.c.err, bad);
+    return;
+  }
+  if (b == 0 && tid == 0) {
+    dst.c.len[i] = n;
+    dst.c.nbuf[i] = src.nbuf[i];
+    dst.c.ntok[i] = src.ntok[i];
+  }
+  const int r_end = min(n, (b + 1) * kRowsPerCta);
+  const int col = tid % TPR;
+  for (int r = b * kRowsPerCta + tid / TPR; r < r_end; r += kRowThreads / TPR) {
+    const long long so = soff + skip + r, dof = doff + r;
+    const uint32_t mask = 0xFu << (threadIdx.x & 28);  // the four lanes of a group
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[8];
+      const T *row = static_cast<const T *>(kv ? src.V : src.K) + so * D;
+      load8<T>(row + col * 8, x);
+      uint32_t lo, hi;
+      const uint32_t sb = quant_group<BITS>(x, mask, lo, hi);
+      unsigned char *out = static_cast<unsigned char *>(kv ? dst.c.V : dst.c.K) + dof * R::kBytes;
+      if (BITS == 8) reinterpret_cast<uint2 *>(out)[col] = make_uint2(lo, hi);
+      else reinterpret_cast<uint32_t *>(out)[col] = lo;
+      if ((col & 3) == 0)
+        static_cast<uint16_t *>(kv ? dst.vs : dst.ks)[dof * R::kGroups + col / 4] = (uint16_t)sb;
+    }
+    if (col == 0) dst.c.pos[dof] = src.pos[so] - skip;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float *x);
+template <>
+__device__ __forceinline__ void store8<float>(float *p, const float *x) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+template <>
+__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, const float *x) {
+  __nv_bfloat162 h[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+  *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(h);
+}
+
+template <int D, typename T, int BITS>
+__global__ void __launch_bounds__(kRowThreads)
+    unpack_kernel(const QCacheArgs src, const CacheArgs dst, int first, int blocks, int max_len) {
+  using R = QRow<D, BITS>;
+  constexpr int TPR = D / 8;
+  pdl_wait();  // no early launch of the next kernel, as in pack_kernel
+  const int i = first + (int)(blockIdx.x / blocks), b = (int)(blockIdx.x % blocks);
+  const int tid = threadIdx.x;
+  const int n = src.c.len[i], scap = src.c.cap[i], dcap = dst.cap[i];
+  const long long soff = src.c.off[i], doff = dst.off[i];
+  uint32_t bad = 0;
+  if (!segment_ok(soff, scap, n, src.c.arena_tokens) ||
+      !segment_ok(doff, dcap, 0, dst.arena_tokens))
+    bad = HKV_ERR_BOUNDS;
+  else if (n > dcap || n > max_len)
+    bad = HKV_ERR_CAPACITY;
+  if (bad) {
+    if (tid == 0 && b == 0) set_err(dst.err, bad);
+    return;
+  }
+  if (b == 0 && tid == 0) {
+    dst.len[i] = n;
+    dst.nbuf[i] = src.c.nbuf[i];
+    dst.ntok[i] = src.c.ntok[i];
+  }
+  const int r_end = min(n, (b + 1) * kRowsPerCta);
+  const int col = tid % TPR;
+  for (int r = b * kRowsPerCta + tid / TPR; r < r_end; r += kRowThreads / TPR) {
+    const long long so = soff + r, dof = doff + r;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const unsigned char *row =
+          static_cast<const unsigned char *>(kv ? src.c.V : src.c.K) + so * R::kBytes;
+      const float s = bf16_bits_to_float(
+          static_cast<const uint16_t *>(kv ? src.vs : src.ks)[so * R::kGroups + col / 4]);
+      uint32_t lo, hi = 0;
+      if (BITS == 8) {
+        const uint2 u = reinterpret_cast<const uint2 *>(row)[col];
+        lo = u.x;
+        hi = u.y;
+      } else {
+        lo = reinterpret_cast<const uint32_t *>(row)[col];
+      }
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = BITS == 4 ? (int)((lo >> (4 * j)) & 15u)
+                                : (int)(((j < 4 ? lo : hi) >> (8 * (j & 3))) & 255u);
+        x[j] = s * (float)(c - R::kBias);
+      }
+      store8<T>(static_cast<T *>(kv ? dst.V : dst.K) + dof * D + col * 8, x);
+    }
+    if (col == 0) dst.pos[dof] = src.c.pos[so];
+  }
+}
+
+// Key rows as codes: the score of Eq. 6 takes what the row stands for, s c in
+// fp32 (exact: 8 by 8 bits), in the channels' order with every product and
+// sum rounded to fp32 by itself.
+template <int D, int BITS>
+struct CodeRows {
+  static constexpr int kBytes = QRow<D, BITS>::kBytes;
+  const uint16_t *scale;  // the segment's first row
+  __device__ __forceinline__ float dot(const unsigned char *krow, const float *qbar, int r) const {
+    constexpr int G = QRow<D, BITS>::kGroups, BIAS = QRow<D, BITS>::kBias;
+    constexpr int WPG = BITS;  // 32-bit words per group of 32 codes
+    float s = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float sc = bf16_bits_to_float(scale[(size_t)r * G + g]);
+#pragma unroll
+      for (int w = 0; w < WPG; ++w) {
+        const uint32_t u = reinterpret_cast<const uint32_t *>(krow)[g * WPG + w];
+#pragma unroll
+        for (int j = 0; j < 32 / BITS; ++j) {
+          const float c = (float)((int)((u >> (BITS * j)) & (BITS == 8 ? 255u : 15u)) - BIAS);
+          s = __fadd_rn(s, __fmul_rn(qbar[g * 32 + w * (32 / BITS) + j], __fmul_rn(sc, c)));
+        }
+      }
+    }
+    return s;
+  }
+};
+
+constexpr int kQuantUpdCtasPerSm = 5;
+
+template <int D, typename T, int BITS>
+__global__ void __launch_bounds__(NT, kQuantUpdCtasPerSm)
+    quant_evict_kernel(const QCacheArgs q, const MethodArgs m, int first, int max_len) {
+  using R = QRow<D, BITS>;
+  constexpr int KB = R::kBytes, SB = R::kScaleBytes, PPR = KB / 16;
+  extern __shared__ __align__(16) unsigned char dyn[];
+  __shared__ UpdShared sh;
+  // no early launch of the next kernel: a decode step that prefetches this
+  // layer's cache before its own wait must start after the update is done
+  pdl_wait();
+  const CacheArgs &c = q.c;
+  const int tid = threadIdx.x, i = first + blockIdx.x;
+  const uint8_t lab = c.label[i];
+  if (lab == HKV_DENSE || c.nbuf[i] < m.P) return;  // not due
+  const int len = c.len[i], cp = c.cap[i], ntok = c.ntok[i];
+  const long long off = c.off[i];
+  if (!segment_ok(off, cp, len, c.arena_tokens)) {
+    if (tid == 0) set_err(c.err, HKV_ERR_BOUNDS);
+    return;
+  }
+  if (len > max_len) {
+    if (tid == 0) set_err(c.err, HKV_ERR_CAPACITY);
+    return;
+  }
+  unsigned char *K = static_cast<unsigned char *>(c.K) + off * KB;
+  unsigned char *V = static_cast<unsigned char *>(c.V) + off * KB;
+  unsigned char *KS = static_cast<unsigned char *>(q.ks) + off * SB;
+  unsigned char *VS = static_cast<unsigned char *>(q.vs) + off * SB;
+  int32_t *pos = c.pos + off;
+  const unsigned char *ring =
+      static_cast<const unsigned char *>(c.qbuf) + (size_t)i * m.P * D * sizeof(T);
+  const UpdSmem u = carve(dyn, max_len, D, m.P, (int)sizeof(T));
+  SegRef sg{K, V, pos, K, V, pos, len, cp, true, c.err};
+  const CodeRows<D, BITS> rows{reinterpret_cast<const uint16_t *>(KS)};
+  const int M = select_evictions<D, T>(sg, lab, m, ring, ntok, u, sh, rows);
+  if (M > 0) {
+    int *hole, *fill;
+    const int k = pair_holes(len, M, u, sh, &hole, &fill);
+    for (int w = tid; w < k * PPR; w += NT) {
+      const size_t src = (size_t)fill[w / PPR] * KB + (w % PPR) * 16;
+      const size_t dst = (size_t)hole[w / PPR] * KB + (w % PPR) * 16;
+      const uint4 a = __ldcg(reinterpret_cast<const uint4 *>(K + src));
+      const uint4 b = __ldcg(reinterpret_cast<const uint4 *>(V + src));
+      *reinterpret_cast<uint4 *>(K + dst) = a;
+      *reinterpret_cast<uint4 *>(V + dst) = b;
+    }
+    for (int w = tid; w < k * (SB / 4); w += NT) {
+      const size_t src = (size_t)fill[w / (SB / 4)] * SB + (w % (SB / 4)) * 4;
+      const size_t dst = (size_t)hole[w / (SB / 4)] * SB + (w % (SB / 4)) * 4;
+      *reinterpret_cast<uint32_t *>(KS + dst) = *reinterpret_cast<const uint32_t *>(KS + src);
+      *reinterpret_cast<uint32_t *>(VS + dst) = *reinterpret_cast<const uint32_t *>(VS + src);
+    }
+    for (int j = tid; j < k; j += NT) pos[hole[j]] = u.ps[fill[j]];
+  }
+  if (tid == 0) {
+    c.len[i] = len - M;
+    c.nbuf[i] = 0;
+  }
+}
+
+}  // namespace
+
+#define HKV_QDISPATCH(D_, DT_, BITS_, ...)            \
+  do {                                                \
+    if ((BITS_) == HKV_Q8) {                          \
+      constexpr int kBits = 8;                        \
+      HKV_DISPATCH(D_, DT_, __VA_ARGS__);             \
+    } else {                                          \
+      constexpr int kBits = 4;                        \
+      HKV_DISPATCH(D_, DT_, __VA_ARGS__);             \
+    }                                                 \
+  } while (0)
+
+cudaError_t launch_quant_pack(const CacheArgs &src, const QCacheArgs &dst, int first, int count,
+                              int skip, int max_len, int D, int dtype, int bits, cudaStream_t s) {
+  const int blocks = (max_len + kRowsPerCta - 1) / kRowsPerCta;
+  if ((long long)blocks * count > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  HKV_QDISPATCH(D, dtype, bits,
+                return pdl_launch(pack_kernel<kD, kT, kBits>, blocks * count, kRowThreads, 0, s,
+                                  src, dst, first, blocks, skip, max_len));
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_quant_unpack(const QCacheArgs &src, const CacheArgs &dst, int first, int count,
+                                int max_len, int D, int dtype, int bits, cudaStream_t s) {
+  const int blocks = (max_len + kRowsPerCta - 1) / kRowsPerCta;
+  if ((long long)blocks * count > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  HKV_QDISPATCH(D, dtype, bits,
+                return pdl_launch(unpack_kernel<kD, kT, kBits>, blocks * count, kRowThreads, 0, s,
+                                  src, dst, first, blocks, max_len));
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t quant_evict_prepare(int D, int dtype, int bits, size_t smem) {
+  HKV_QDISPATCH(D, dtype, bits, {
+    cudaError_t e = cudaFuncSetAttribute(quant_evict_kernel<kD, kT, kBits>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(quant_evict_kernel<kD, kT, kBits>,
+                               cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+    return e;
+  });
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_quant_evict(const QCacheArgs &c, const MethodArgs &m, int first, int count,
+                               int D, int dtype, int bits, size_t smem, cudaStream_t s) {
+  const int max_len = update_max_len(smem, D, m.P, dtype == HKV_BF16 ? 2 : 4);
+  HKV_QDISPATCH(D, dtype, bits,
+                return pdl_launch(quant_evict_kernel<kD, kT, kBits>, count, NT, smem, s, c, m,
+                                  first, max_len));
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace hkv

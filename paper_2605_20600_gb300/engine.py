@@ -4,10 +4,15 @@ Owns the device buffers (allocated with torch, which serves only as the
 memory and stream provider) and sequences the calls of one image generation
 (Sec. 4): Step 1 cache prefilling into an uncompressed cache, Step 2 head
 grouping at image token E-1, Step 3 head-aware compression (budgets, arena
-allocation, repack), then decode steps of append/evict + attention. All
-compute runs in libheadkv.so kernels.
+allocation, repack), then decode steps of append/evict + attention. After
+compression the cache may be quantised (Engine.quantise): the decode steps
+and updates then run on codes, and conditioning tokens that all sequences
+share may be kept once, outside the cache. All compute runs in libheadkv.so
+kernels.
 """
 from __future__ import annotations
+
+import copy
 
 import torch
 
@@ -46,6 +51,30 @@ class CacheBuffers:
                              self.qbuf.data_ptr(), self.err.data_ptr(), capacity_tokens)
 
 
+class QuantCacheBuffers:
+    """Device buffers behind one hkv_qcache (layout documented in hkv_serve.h)."""
+
+    def __init__(self, cfg: H.hkv_config, fmt: int, capacity_tokens: int, device, *, qbuf, label,
+                 off, cap):
+        n = cfg.n_layers * cfg.n_seqs * cfg.n_heads
+        D, rows = cfg.head_dim, max(capacity_tokens, 1)
+
+        def arena(width, dt):
+            return torch.empty(rows, width, dtype=dt, device=device)
+
+        self.k, self.v = arena(D * fmt // 8, torch.uint8), arena(D * fmt // 8, torch.uint8)
+        self.ks, self.vs = arena(D // 32, torch.bfloat16), arena(D // 32, torch.bfloat16)
+        self.pos = torch.full((rows,), -1, dtype=torch.int32, device=device)
+        self.off, self.cap, self.label, self.qbuf = off, cap, label, qbuf
+        self.len, self.nbuf, self.ntok = (torch.zeros(n, dtype=torch.int32, device=device)
+                                          for _ in range(3))
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self.capacity_tokens = capacity_tokens
+        self.c = H.make_qcache(fmt, self.k, self.v, self.ks, self.vs, self.pos, self.off, self.cap,
+                               self.len, self.nbuf, self.ntok, self.label, self.qbuf, self.err,
+                               capacity_tokens)
+
+
 class Engine:
     """One batch of sequences through the HeadKV decode path."""
 
@@ -63,6 +92,8 @@ class Engine:
         self.ragged: CacheBuffers | None = None
         self.budget = self.cap = self.off = None
         self.total_tokens = 0
+        self.quant: QuantCacheBuffers | None = None
+        self.prompt = None            # shared prompts: one hkv_prefix per layer
         H.hkv_init_dense(cfg, self.dense.c, self.stream())
         self.cache = self.dense
 
@@ -84,10 +115,16 @@ class Engine:
 
     # fused path: the update when due, then append + attention in one launch
     def evict(self, layer: int) -> None:
+        if self.quant is not None:
+            H.hkv_quant_evict(self.quant_cfg, self.quant.c, layer, self.stream())
+            return
         H.hkv_evict(self.cfg, self.cache.c, layer, self.stream())
 
     def evict_all(self) -> None:
         """The periodic update of every layer in one launch."""
+        if self.quant is not None:
+            H.hkv_quant_evict_all(self.quant_cfg, self.quant.c, self.stream())
+            return
         H.hkv_evict_all(self.cfg, self.cache.c, self.stream())
 
     def step(self, layer: int, q, k, v, out) -> None:
@@ -95,6 +132,9 @@ class Engine:
         # decode step belongs to another layer (or is hkv_evict, which never
         # lets its successor start early): the step may prefetch
         flags = H.HKV_STEP_PREFETCH if self.cfg.n_layers >= 2 else 0
+        if self.quant is not None:
+            self._quant_step(layer, q, k, v, out, flags)
+            return
         H.hkv_decode_step(self.cfg, self.cache.c, layer, q, k, v, out, self.ws, self.ws_bytes,
                           flags, self.stream())
 
@@ -135,11 +175,66 @@ class Engine:
             H.hkv_repack(self.cfg, self.dense.c, self.ragged.c, layer, self.stream())
         self.cache = self.ragged
 
+    # the serving cache
+    def quantise(self, fmt: int, prompt=None) -> None:
+        """Puts the compressed cache into 8 or 4 bits (HKV_Q8 or HKV_Q4) and
+        frees its plain rows; decode steps and updates run on the codes from
+        here on. prompt: None, or (k, v), [L][groups][H][C][head_dim] tensors
+        of the conditioning tokens that each of `groups` equal runs of
+        sequences shares; they then stay plain and are kept once instead of
+        in every sequence's segments."""
+        if self.ragged is None or self.quant is not None:
+            raise H.HkvError("quantise", H.HKV_ERR_STATE)
+        cfg, dev = self.cfg, self.device
+        off, cap, total = self.off, self.cap, self.total_tokens
+        flags = 0
+        self.quant_cfg = copy.copy(cfg)
+        if prompt is not None:
+            k, v = prompt
+            if k.shape[0] != cfg.n_layers or k.shape[2:] != (cfg.n_heads, cfg.n_cond, cfg.head_dim) \
+                    or k.shape != v.shape or cfg.n_cond < 1:
+                raise H.HkvError("quantise", H.HKV_ERR_SHAPE)
+            self.quant_cfg.n_cond = 0
+            off, cap = torch.empty_like(off), torch.empty_like(cap)
+            total = H.hkv_allocate_budgets(self.quant_cfg, self.labels, torch.empty_like(self.budget),
+                                           cap, off, self.stream())
+            flags = H.HKV_PACK_SKIP_COND
+        quant = QuantCacheBuffers(cfg, fmt, total, dev, qbuf=self.ragged.qbuf, label=self.labels,
+                                  off=off, cap=cap)
+        H.hkv_quant_pack(cfg, self.ragged.c, quant.c, H.HKV_ALL_LAYERS, flags, self.stream())
+        if prompt is not None:
+            groups = k.shape[1]
+            self.prompt_len = torch.full((groups,), cfg.n_cond, dtype=torch.int32, device=dev)
+            self.prompt_rows = (k, v)
+            self.prompt = [H.make_prefix(k[layer], v[layer], self.prompt_len, quant.err)
+                           for layer in range(cfg.n_layers)]
+            self.prompt_ws_bytes = H.hkv_prefix_workspace_size(cfg, self.prompt[0])
+            self.prompt_ws = torch.zeros(self.prompt_ws_bytes, dtype=torch.uint8, device=dev)
+            shape = (cfg.n_seqs, cfg.n_heads)
+            self.prior = (torch.empty(*shape, cfg.head_dim, dtype=torch.float32, device=dev),
+                          torch.empty(*shape, dtype=torch.float32, device=dev))
+        self.quant_ws_bytes = H.hkv_quant_workspace_size(self.quant_cfg)
+        self.quant_ws = torch.zeros(self.quant_ws_bytes, dtype=torch.uint8, device=dev)
+        self.off, self.cap, self.total_tokens = off, cap, total
+        self.cache = self.quant = quant
+        self.ragged.k = self.ragged.v = self.ragged.pos = None
+
+    def _quant_step(self, layer: int, q, k, v, out, flags: int) -> None:
+        prior = None
+        if self.prompt is not None:
+            prior = self.prior
+            H.hkv_prefix_attention(self.cfg, self.prompt[layer], q, prior[0], prior[1],
+                                   self.prompt_ws, self.prompt_ws_bytes, self.stream())
+        H.hkv_quant_step(self.quant_cfg, self.quant.c, layer, q, k, v, out, self.quant_ws,
+                         self.quant_ws_bytes, prior=prior, flags=flags, stream=self.stream())
+
     def release_dense(self) -> None:
         """Frees the uncompressed arena once the ragged cache holds everything."""
         self.dense.k = self.dense.v = self.dense.pos = None
 
     def check(self) -> None:
-        H.hkv_check(self.cache.c, self.stream())
-        if self.cache is not self.dense:
-            H.hkv_check(self.dense.c, self.stream())
+        if self.quant is not None:
+            H.hkv_quant_check(self.quant.c, self.stream())
+        if self.ragged is not None:
+            H.hkv_check(self.ragged.c, self.stream())
+        H.hkv_check(self.dense.c, self.stream())

@@ -1,4 +1,4 @@
-"""ctypes binding of the HeadKV C-ABI (include/hkv.h).
+"""ctypes binding of the HeadKV C-ABI (include/hkv.h, include/hkv_serve.h).
 
 Argument marshalling only: every function has the name of the C entry point
 it forwards to, accepts integers (device addresses) or objects with a
@@ -31,6 +31,9 @@ HKV_STEP_PREFETCH = 1
 HKV_LOCAL, HKV_GLOBAL, HKV_DENSE = 0, 1, 255
 HKV_BUDGET_PAPER, HKV_BUDGET_REDISTRIBUTE = 0, 1
 HKV_DIST_RASTER, HKV_DIST_GRID2D = 0, 1
+HKV_Q8, HKV_Q4 = 8, 4
+HKV_ALL_LAYERS = -1
+HKV_PACK_SKIP_COND = 1
 
 
 class hkv_config(Structure):
@@ -48,6 +51,23 @@ class hkv_cache(Structure):
         ("k", c_void_p), ("v", c_void_p), ("pos", c_void_p), ("off", c_void_p), ("cap", c_void_p),
         ("len", c_void_p), ("nbuf", c_void_p), ("ntok", c_void_p), ("label", c_void_p),
         ("qbuf", c_void_p), ("err", c_void_p), ("capacity_tokens", c_int64),
+    ]
+
+
+class hkv_qcache(Structure):
+    _fields_ = [
+        ("k", c_void_p), ("v", c_void_p), ("ks", c_void_p), ("vs", c_void_p), ("pos", c_void_p),
+        ("off", c_void_p), ("cap", c_void_p), ("len", c_void_p), ("nbuf", c_void_p),
+        ("ntok", c_void_p), ("label", c_void_p), ("qbuf", c_void_p), ("err", c_void_p),
+        ("capacity_tokens", c_int64), ("format", c_int32), ("reserved", c_int32),
+    ]
+
+
+class hkv_prefix(Structure):
+    _fields_ = [
+        ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
+        ("group_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
+        ("n_groups", c_int32), ("max_len", c_int32),
     ]
 
 
@@ -90,6 +110,22 @@ _SIGNATURES = {
     "hkv_check": ([POINTER(hkv_cache), c_void_p], c_int),
     "hkv_export_state": ([POINTER(hkv_config), POINTER(hkv_cache), c_int, c_void_p, c_void_p, c_void_p,
                           c_void_p, c_void_p, c_int64, POINTER(c_int64), c_void_p], c_int),
+    "hkv_quant_pack": ([POINTER(hkv_config), POINTER(hkv_cache), POINTER(hkv_qcache), c_int, c_int,
+                        c_void_p], c_int),
+    "hkv_quant_unpack": ([POINTER(hkv_config), POINTER(hkv_qcache), POINTER(hkv_cache), c_int,
+                          c_void_p], c_int),
+    "hkv_quant_workspace_size": ([POINTER(hkv_config)], c_size_t),
+    "hkv_quant_attention": ([POINTER(hkv_config), POINTER(hkv_qcache), c_int, c_void_p, c_void_p,
+                             c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p], c_int),
+    "hkv_quant_step": ([POINTER(hkv_config), POINTER(hkv_qcache), c_int, c_void_p, c_void_p, c_void_p,
+                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_int, c_void_p],
+                       c_int),
+    "hkv_quant_evict": ([POINTER(hkv_config), POINTER(hkv_qcache), c_int, c_void_p], c_int),
+    "hkv_quant_evict_all": ([POINTER(hkv_config), POINTER(hkv_qcache), c_void_p], c_int),
+    "hkv_quant_check": ([POINTER(hkv_qcache), c_void_p], c_int),
+    "hkv_prefix_workspace_size": ([POINTER(hkv_config), POINTER(hkv_prefix)], c_size_t),
+    "hkv_prefix_attention": ([POINTER(hkv_config), POINTER(hkv_prefix), c_void_p, c_void_p, c_void_p,
+                              c_void_p, c_size_t, c_void_p], c_int),
 }
 
 
@@ -254,3 +290,78 @@ def hkv_export_state(cfg, cache, layer, stream=0):
     split = np.cumsum(ln)[:-1]
     return {"label": label, "len": ln, "nbuf": nbuf, "ntok": ntok,
             "pos": np.split(pos[:int(count.value)], split)}
+
+
+# ---------------------------------------------------------------------------
+# the serving cache (include/hkv_serve.h)
+# ---------------------------------------------------------------------------
+def make_qcache(fmt, k, v, ks, vs, pos, off, cap, length, nbuf, ntok, label, qbuf, err,
+                capacity_tokens) -> hkv_qcache:
+    """An hkv_qcache over the caller's buffers (kept alive with it); fmt is
+    HKV_Q8 or HKV_Q4."""
+    arrays = (k, v, ks, vs, pos, off, cap, length, nbuf, ntok, label, qbuf, err)
+    c = hkv_qcache(*(_p(x) for x in arrays), int(capacity_tokens), int(fmt), 0)
+    c.arrays = arrays
+    return c
+
+
+def make_prefix(k, v, length, err=None) -> hkv_prefix:
+    """An hkv_prefix from tensors k and v of [groups][heads][tokens][head_dim]
+    (any strides whose last is 1, the same in both) and the prompts' lengths,
+    int32 on the device; keeps them alive."""
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+        raise HkvError("make_prefix", HKV_ERR_SHAPE)
+    if length.numel() != k.shape[0]:
+        raise HkvError("make_prefix", HKV_ERR_SHAPE)
+    p = hkv_prefix(k.data_ptr(), v.data_ptr(), length.data_ptr(), _p(err), k.stride(0),
+                   k.stride(1), k.stride(2), k.shape[0], k.shape[2])
+    p.arrays = (k, v, length, err)
+    return p
+
+
+def hkv_quant_pack(cfg, src, dst, layer, flags=0, stream=0) -> None:
+    _call("quant_pack", ctypes.byref(cfg), ctypes.byref(src), ctypes.byref(dst), layer, flags, stream)
+
+
+def hkv_quant_unpack(cfg, src, dst, layer, stream=0) -> None:
+    _call("quant_unpack", ctypes.byref(cfg), ctypes.byref(src), ctypes.byref(dst), layer, stream)
+
+
+def hkv_quant_workspace_size(cfg) -> int:
+    return int(lib().hkv_quant_workspace_size(ctypes.byref(cfg)))
+
+
+def hkv_quant_attention(cfg, cache, layer, q, out, workspace, ws_bytes, prior=None, lse=None,
+                        stream=0) -> None:
+    """prior: None or (out, lse) of the same queries over other keys."""
+    po, pl = prior or (None, None)
+    _call("quant_attention", ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q), _p(po), _p(pl),
+          _p(out), _p(lse), _p(workspace), ws_bytes, stream)
+
+
+def hkv_quant_step(cfg, cache, layer, q, k, v, out, workspace, ws_bytes, prior=None, lse=None,
+                   flags=0, stream=0) -> None:
+    po, pl = prior or (None, None)
+    _call("quant_step", ctypes.byref(cfg), ctypes.byref(cache), layer, _p(q), _p(k), _p(v), _p(po),
+          _p(pl), _p(out), _p(lse), _p(workspace), ws_bytes, flags, stream)
+
+
+def hkv_quant_evict(cfg, cache, layer, stream=0) -> None:
+    _call("quant_evict", ctypes.byref(cfg), ctypes.byref(cache), layer, stream)
+
+
+def hkv_quant_evict_all(cfg, cache, stream=0) -> None:
+    _call("quant_evict_all", ctypes.byref(cfg), ctypes.byref(cache), stream)
+
+
+def hkv_quant_check(cache, stream=0) -> None:
+    _call("quant_check", ctypes.byref(cache), stream)
+
+
+def hkv_prefix_workspace_size(cfg, prefix) -> int:
+    return int(lib().hkv_prefix_workspace_size(ctypes.byref(cfg), ctypes.byref(prefix)))
+
+
+def hkv_prefix_attention(cfg, prefix, q, out, lse, workspace, ws_bytes, stream=0) -> None:
+    _call("prefix_attention", ctypes.byref(cfg), ctypes.byref(prefix), _p(q), _p(out), _p(lse),
+          _p(workspace), ws_bytes, stream)

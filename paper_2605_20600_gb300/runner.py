@@ -15,7 +15,8 @@ from .engine import Engine, torch_dtype
 
 def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=None,
              before_compress=None, fused: bool = True, first_step: int = 0,
-             identify: str | None = None) -> None:
+             identify: str | None = None, cache_format: int | None = None,
+             shared_prompt: bool = False) -> None:
     """Runs image tokens first_step..last_step (default N-1) for every layer.
 
     fused: hkv_evict_all (every layer in one launch) when the update is due,
@@ -30,7 +31,15 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
     hkv_identify_heads_multi after it (the recent queries' averaged
     attention; labels and n_h). Default: fused when the path is fused and
     the distances are the raster ones.
+    cache_format: None keeps the compressed cache in the config dtype;
+    HKV_Q8 or HKV_Q4 quantises it after compression (fused path only).
+    shared_prompt: with a cache_format, the conditioning tokens, which must
+    then be the same for every sequence, are kept once for all of them.
     """
+    if cache_format is not None and not fused:
+        raise ValueError("a quantised cache needs the fused path")
+    if shared_prompt and (cache_format is None or first_step > 0 or engine.cfg.n_cond < 1):
+        raise ValueError("a shared prompt needs a cache_format, conditioning tokens and a whole run")
     if identify is None:   # the fused count is the raster one
         identify = "fused" if fused and engine.cfg.distance_mode == 0 else "separate"
     if identify not in ("fused", "separate", "multi") or (identify == "fused" and not fused):
@@ -48,6 +57,12 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
         for layer in range(L):
             provider.cond(kc, vc, layer, st)
             engine.prefill(layer, kc, vc)
+            if shared_prompt:
+                if layer == 0:
+                    prompt = (torch.empty(L, 1, H, C, D, dtype=dt, device=dev),
+                              torch.empty(L, 1, H, C, D, dtype=dt, device=dev))
+                prompt[0][layer, 0].copy_(kc[0])
+                prompt[1][layer, 0].copy_(vc[0])
     q = torch.empty(L, S, H, D, dtype=dt, device=dev)
     k, v = torch.empty_like(q), torch.empty_like(q)
     out = torch.empty(L, S, H, D, dtype=torch.float32, device=dev)
@@ -76,3 +91,5 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
             if before_compress is not None:
                 before_compress(engine)
             engine.compress()
+            if cache_format is not None:
+                engine.quantise(cache_format, prompt if shared_prompt else None)

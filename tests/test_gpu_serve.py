@@ -1,0 +1,661 @@
+"""The serving cache on the GPU: rows in 8 and 4 bits written, read back,
+attended over and trimmed, and attention over shared prompts, each against the
+fp64 oracle (oracle/serve.py, oracle/headkv.py).
+
+Tolerances. A logit x = sum q_i k_i / sqrt(D) is off by at most 2^-19 A with
+A = sum |q_i k_i| / sqrt(D): operands in two 11-bit parts (2^-22) and at most
+D / 16 = 8 chained sums whose rounding may truncate (8 x 2^-23). Weights off
+by eps each move an output by at most 2 eps max|v|, and the sums over the
+rows add 2^-19 max|v| (at most 16 chained sums between fp32 additions, and the
+base-2 exponential's 2 ulp). Codes, scales, positions and counters are exact.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import headkv as O
+from oracle import serve as S
+from synth import configs, gen
+
+from _gpu_util import cfg_of, flat
+
+pytestmark = pytest.mark.gpu
+
+FMT = [8, 4]
+
+
+def tolerances(q, K, V):
+    A = float((np.abs(K) @ np.abs(q)).max()) / math.sqrt(q.shape[0]) if len(K) else 0.0
+    eps = 2.0 ** -19 * A
+    vmax = float(np.abs(V).max()) if len(V) else 0.0
+    return (2 * eps + 2.0 ** -19) * vmax, eps + 2.0 ** -20 * 8
+
+
+def to_torch(x, dtype, device="cuda"):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(
+        torch.bfloat16 if dtype == "bf16" else torch.float32).to(device)
+
+
+def rounded(x, dtype):
+    return gen.round_bf16(np.asarray(x, np.float32)) if dtype == "bf16" else np.asarray(x, np.float32)
+
+
+class QCache:
+    """A quantised cache with heads of given lengths; rows past a head's
+    length hold NaN scales and arbitrary codes."""
+
+    def __init__(self, lens, D, bits, dtype, seed=0, slack=3, period=4, label=255, n_seqs=1,
+                 max_len=None, lead=0):
+        import torch
+        from paper_2605_20600_gb300 import hkv as H
+        rng = np.random.default_rng(seed)
+        self.H, self.D, self.bits, self.dtype = H, D, bits, dtype
+        self.lens = np.asarray(lens, dtype=np.int64)
+        n = self.lens.size
+        self.n = n
+        caps = self.lens + slack
+        self.off = lead + np.cumsum(caps) - caps
+        tokens = int(lead + caps.sum())
+        self.tokens = tokens
+        most = int(max_len or caps.max() + 1)
+        self.cfg = H.make_config(n_layers=1, n_seqs=n_seqs, n_heads=n // n_seqs, head_dim=D,
+                                 dtype=dtype, n_cond=0, n_image=most + period, row_len=1, recent_w=1,
+                                 local_w=1, period=period, group_at=max(most, period),
+                                 global_budget=1)
+        gain = np.exp(0.7 * rng.normal(size=D))
+        self.k_codes, self.k_scales = S.quantise(rng.normal(size=(tokens, D)) * gain, bits)
+        self.v_codes, self.v_scales = S.quantise(rng.normal(size=(tokens, D)), bits)
+        live = np.zeros(tokens, bool)
+        for o, ln in zip(self.off, self.lens):
+            live[o:o + ln] = True
+        ks, vs = self.k_scales.copy(), self.v_scales.copy()
+        ks[~live] = np.nan
+        vs[~live] = np.nan
+        dev = "cuda"
+        self.ck = torch.from_numpy(S.packed(self.k_codes, bits)).to(dev)
+        self.cv = torch.from_numpy(S.packed(self.v_codes, bits)).to(dev)
+        self.sk, self.sv = to_torch(ks, "bf16"), to_torch(vs, "bf16")
+        self.pos = torch.full((tokens,), -7, dtype=torch.int32, device=dev)
+        self.toff = torch.from_numpy(self.off).to(dev)
+        self.cap = torch.from_numpy(caps.astype(np.int32)).to(dev)
+        self.len = torch.from_numpy(self.lens.astype(np.int32)).to(dev)
+        self.nbuf = torch.zeros(n, dtype=torch.int32, device=dev)
+        self.ntok = torch.from_numpy(self.lens.astype(np.int32)).to(dev)
+        self.label = torch.full((n,), label, dtype=torch.uint8, device=dev)
+        self.qbuf = torch.zeros(n, period, D, device=dev,
+                                dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+        self.err = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.c = H.make_qcache(bits, self.ck, self.cv, self.sk, self.sv, self.pos, self.toff, self.cap,
+                               self.len, self.nbuf, self.ntok, self.label, self.qbuf, self.err, tokens)
+        self.ws_bytes = H.hkv_quant_workspace_size(self.cfg)
+        self.ws = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=dev)
+        self.q = rounded(rng.normal(size=(n, D)) * 1.5, dtype)
+        self.k_new = rounded(rng.normal(size=(n, D)) * gain, dtype)
+        self.v_new = rounded(rng.normal(size=(n, D)), dtype)
+
+    def rows(self, h, step=False):
+        a = slice(self.off[h], self.off[h] + self.lens[h])
+        K = S.values(self.k_codes[a], self.k_scales[a])
+        V = S.values(self.v_codes[a], self.v_scales[a])
+        if step:
+            K = np.concatenate([K, S.stored(self.k_new[h:h + 1], self.bits)])
+            V = np.concatenate([V, S.stored(self.v_new[h:h + 1], self.bits)])
+        return K, V
+
+
+def joined(o1, l1, o2, l2):
+    both = np.logaddexp(l1, l2)
+    if both == -np.inf:
+        return np.zeros_like(o1), both
+    return math.exp(l1 - both) * o1 + math.exp(l2 - both) * o2, both
+
+
+LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 511, 513, 1000,
+        1025, 2049]
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("prior", [False, True])
+def test_attention_over_codes(bits, D, dtype, prior):
+    import torch
+    c = QCache(LENS, D, bits, dtype, seed=1 + bits + D, lead=5)
+    H, rng = c.H, np.random.default_rng(99)
+    q = to_torch(c.q, dtype)
+    out = torch.full((c.n, D), -1.0, device="cuda")
+    lse = torch.full((c.n,), -1.0, device="cuda")
+    pr = None
+    if prior:
+        po = rng.normal(size=(c.n, D)).astype(np.float32)
+        pl = (rng.normal(size=c.n) * 4).astype(np.float32)
+        pl[[0, 3, 7]] = -np.inf       # an empty prior: its outputs are not looked at
+        po[[0, 3, 7]] = np.nan
+        pr = (to_torch(po, "fp32"), to_torch(pl, "fp32"))
+    for _ in range(2):                # the workspace is left ready for the next call
+        H.hkv_quant_attention(c.cfg, c.c, 0, q, out, c.ws, c.ws_bytes, prior=pr, lse=lse)
+    H.hkv_quant_check(c.c)
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    for h in range(c.n):
+        K, V = c.rows(h)
+        o, l = S.attention_lse(c.q[h], K, V)
+        to, tl = tolerances(c.q[h], K, V)
+        if prior:
+            if pl[h] != -np.inf:
+                to += 2.0 ** -19 * np.abs(po[h]).max() + 2 * tl * np.abs(po[h]).max()
+                o, l = joined(o, l, po[h].astype(np.float64), float(pl[h]))
+        assert np.abs(got[h] - o).max() <= to, (h, c.lens[h], np.abs(got[h] - o).max(), to)
+        assert gl[h] == l or abs(gl[h] - l) <= tl, (h, gl[h], l, tl)
+    assert int(c.ws[:4 * c.n].sum()) == 0
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("label", [255, 0])
+def test_step_appends_and_attends(bits, D, dtype, label):
+    import torch
+    c = QCache(LENS, D, bits, dtype, seed=5 + bits + D, label=label)
+    H = c.H
+    before = [x.clone() for x in (c.ck, c.cv, c.sk, c.sv)]
+    q, k, v = (to_torch(x, dtype) for x in (c.q, c.k_new, c.v_new))
+    out = torch.empty(c.n, D, device="cuda")
+    lse = torch.empty(c.n, device="cuda")
+    H.hkv_quant_step(c.cfg, c.c, 0, q, k, v, out, c.ws, c.ws_bytes, lse=lse)
+    H.hkv_quant_check(c.c)
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    rows = c.off + c.lens
+    for x, codes, scales in ((c.k_new, c.ck, c.sk), (c.v_new, c.cv, c.sv)):
+        cc, ss = S.quantise(x, bits)
+        assert np.array_equal(codes.cpu().numpy()[rows], S.packed(cc, bits))
+        assert np.array_equal(scales.float().cpu().numpy()[rows], ss)
+    other = np.setdiff1d(np.arange(c.tokens), rows)
+    for a, b in zip(before, (c.ck, c.cv, c.sk, c.sv)):   # nothing else moved
+        assert torch.equal(a.view(torch.uint8)[other], b.view(torch.uint8)[other])
+    assert np.array_equal(c.len.cpu().numpy(), c.lens + 1)
+    assert np.array_equal(c.ntok.cpu().numpy(), c.lens + 1)
+    assert np.array_equal(c.nbuf.cpu().numpy(), np.full(c.n, 0 if label == 255 else 1))
+    pos = c.pos.cpu().numpy()
+    assert np.array_equal(pos[rows], c.lens) and (pos[other] == -7).all()
+    ring = c.qbuf.float().cpu().numpy()
+    for h in range(c.n):
+        assert np.array_equal(ring[h, c.lens[h] % 4], c.q[h])
+        K, V = c.rows(h, step=True)
+        o, l = S.attention_lse(c.q[h], K, V)
+        to, tl = tolerances(c.q[h], K, V)
+        assert np.abs(got[h] - o).max() <= to, (h, np.abs(got[h] - o).max(), to)
+        assert abs(gl[h] - l) <= tl
+
+
+def test_step_refuses_per_head_through_the_error_word():
+    import torch
+    for what, code in (("full", 3), ("buffer", 4), ("outside", 5)):
+        c = QCache([40, 41, 300, 7], 64, 8, "bf16", label=1)
+        if what == "full":
+            c.cap[1] = 41
+        elif what == "buffer":
+            c.nbuf[1] = 4
+        else:
+            c.toff[1] = c.tokens
+        q, k, v = (to_torch(x, "bf16") for x in (c.q, c.k_new, c.v_new))
+        out = torch.full((4, 64), 9.0, device="cuda")
+        c.H.hkv_quant_step(c.cfg, c.c, 0, q, k, v, out, c.ws, c.ws_bytes)
+        with pytest.raises(c.H.HkvError) as e:
+            c.H.hkv_quant_check(c.c)
+        assert e.value.status == code
+        assert c.len.tolist() == [41, 41, 301, 8] and c.ntok.tolist() == [41, 41, 301, 8]
+        got = out.cpu().numpy()
+        assert (got[1] == 9.0).all() and (got[[0, 2, 3]] != 9.0).all()
+
+
+def test_segment_longer_than_the_config_is_a_capacity_error():
+    import torch
+    c = QCache([40, 2000], 64, 4, "bf16", max_len=100)
+    q = to_torch(c.q, "bf16")
+    out = torch.full((2, 64), 9.0, device="cuda")
+    c.H.hkv_quant_attention(c.cfg, c.c, 0, q, out, c.ws, c.ws_bytes)
+    with pytest.raises(c.H.HkvError) as e:
+        c.H.hkv_quant_check(c.c)
+    assert e.value.status == 3
+    assert (out[1] == 9.0).all() and (out[0] != 9.0).all()
+
+
+@pytest.mark.parametrize("bits", FMT)
+def test_attention_with_extreme_rows(bits):
+    """Groups of zeros, very large and very small scales, one row that takes
+    all the weight, and a NaN row that reaches only its own head."""
+    import torch
+    D = 128
+    c = QCache([70, 70, 70, 70], D, bits, "fp32", seed=3)
+    rng = np.random.default_rng(8)
+    ks, vs = c.k_scales.copy(), c.v_scales.copy()
+    o = c.off
+    ks[o[0]:o[0] + 70, 1] = 0.0                                   # a group of zeros
+    vs[o[0] + 5:o[0] + 20] = 0.0
+    vs[o[1]:o[1] + 70] = S.round_bf16((2.0 ** rng.uniform(-60, 60, size=(70, 4))).astype(np.float32))
+    ks[o[2] + 33] = S.round_bf16(np.full(4, 300.0, np.float32))     # a logit far above the others
+    vs[o[3] + 69, 2] = np.nan
+    for x, t in ((ks, c.sk), (vs, c.sv)):
+        for h in range(4):
+            t[o[h]:o[h] + 70] = to_torch(x[o[h]:o[h] + 70], "bf16")
+    c.k_scales, c.v_scales = ks, vs
+    out = torch.empty(4, D, device="cuda")
+    c.H.hkv_quant_attention(c.cfg, c.c, 0, to_torch(c.q, "fp32"), out, c.ws, c.ws_bytes)
+    got = out.cpu().numpy()
+    for h in range(4):
+        K, V = c.rows(h)
+        if h == 3:
+            assert np.isnan(got[h, 64:96]).all()
+            keep = np.r_[0:64, 96:128]
+            got_h, V = got[h, keep], V[:, keep]
+        else:
+            got_h = got[h]
+        want, _ = S.attention_lse(c.q[h], K, V)
+        A = float((np.abs(K) @ np.abs(c.q[h])).max()) / math.sqrt(D)
+        # each channel against the largest magnitude of its own group
+        vmax = np.repeat(np.abs(V).reshape(70, -1, 32).max((0, 2)), 32)
+        assert (np.abs(got_h - want) <= (2 * 2.0 ** -19 * A + 2.0 ** -19) * vmax).all(), h
+
+
+@pytest.mark.parametrize("bits", FMT)
+def test_offsets_past_32_bits(bits):
+    """A head whose rows start beyond 2^32 bytes of the arena."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    D, rb = 128, 128 * bits // 8
+    lead = (1 << 32) // rb + 11
+    c = QCache([77, 301], D, bits, "bf16", seed=4)
+    tokens = lead + c.tokens
+    big = [torch.empty(tokens, w, dtype=t.dtype, device="cuda")
+           for t, w in ((c.ck, rb), (c.cv, rb), (c.sk, 4), (c.sv, 4))]
+    for b, t in zip(big, (c.ck, c.cv, c.sk, c.sv)):
+        b[lead:] = t
+    pos = torch.zeros(tokens, dtype=torch.int32, device="cuda")
+    off = c.toff + lead
+    qc = H.make_qcache(bits, *big, pos, off, c.cap, c.len, c.nbuf, c.ntok, c.label, c.qbuf, c.err, tokens)
+    q, k, v = (to_torch(x, "bf16") for x in (c.q, c.k_new, c.v_new))
+    out = torch.empty(2, D, device="cuda")
+    H.hkv_quant_step(c.cfg, qc, 0, q, k, v, out, c.ws, c.ws_bytes)
+    H.hkv_quant_check(qc)
+    for h in range(2):
+        K, V = c.rows(h, step=True)
+        o, _ = S.attention_lse(c.q[h], K, V)
+        assert np.abs(out[h].cpu().numpy() - o).max() <= tolerances(c.q[h], K, V)[0]
+        cc, _ = S.quantise(c.k_new[h], bits)
+        assert np.array_equal(big[0][lead + int(c.off[h] + c.lens[h])].cpu().numpy(), S.packed(cc, bits))
+
+
+def plain_cache(H, cfg, lens, caps, dtype, k, v, device="cuda"):
+    """CacheBuffers holding rows k, v [tokens, D] (segments back to back)."""
+    import torch
+    from paper_2605_20600_gb300.engine import CacheBuffers
+    cb = CacheBuffers(cfg, int(np.sum(caps)), device)
+    cb.k.copy_(to_torch(k, dtype))
+    cb.v.copy_(to_torch(v, dtype))
+    cb.off.copy_(torch.from_numpy((np.cumsum(caps) - caps).astype(np.int64)))
+    cb.cap.copy_(torch.from_numpy(np.asarray(caps, np.int32)))
+    cb.len.copy_(torch.from_numpy(np.asarray(lens, np.int32)))
+    cb.pos.copy_(torch.arange(int(np.sum(caps)), dtype=torch.int32))
+    return cb
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("skip", [0, 5])
+def test_pack_and_unpack(bits, D, dtype, skip):
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import CacheBuffers, QuantCacheBuffers
+    rng = np.random.default_rng(17)
+    lens = np.array([5, 6, 63, 64, 65, 130, 200, 7] if skip else [0, 1, 63, 64, 65, 130, 200, 7])
+    caps = lens + 2
+    n, tokens = lens.size, int(caps.sum())
+    cfg = H.make_config(n_layers=2, n_seqs=2, n_heads=2, head_dim=D, dtype=dtype, n_cond=5,
+                        n_image=300, row_len=1, recent_w=1, local_w=1, period=4, group_at=300,
+                        global_budget=1)
+    k = rounded(rng.normal(size=(tokens, D)) * np.exp(rng.normal(size=D)), dtype)
+    v = rounded(rng.normal(size=(tokens, D)), dtype)
+    off = np.cumsum(caps) - caps
+    # groups of zeros, exact ties, tiny (the scale underflows), huge, infinite, NaN
+    r = int(off[5]) + 6
+    k[r, :32] = 0.0
+    k[r + 1, :32] = rounded(np.arange(32) * 0.5 + 111.5, dtype)
+    k[r + 2, :32] = 1e-41 if dtype == "fp32" else 0.0
+    k[r + 3, :32] = rounded(np.float32(3e38) * np.linspace(-1, 1, 32), dtype)
+    k[r + 4, 3], k[r + 5, 40] = np.inf, np.nan
+    k[r + 6, :32] = rounded(np.float32(2.0 ** -126) * np.linspace(-1, 1, 32), dtype)
+    src = plain_cache(H, cfg, lens, caps, dtype, k, v)
+    src.nbuf.copy_(torch.arange(n))
+    src.ntok.copy_(torch.arange(n) + 100)
+    qc = QuantCacheBuffers(cfg, bits, tokens, "cuda", qbuf=src.qbuf, label=src.label, off=src.off,
+                           cap=src.cap)
+    for t in (qc.k, qc.v, qc.ks, qc.vs):
+        t.view(torch.uint8).fill_(0x5A)
+    H.hkv_quant_pack(cfg, src.c, qc.c, H.HKV_ALL_LAYERS, H.HKV_PACK_SKIP_COND if skip else 0)
+    H.hkv_quant_check(qc.c)
+    assert np.array_equal(qc.len.cpu().numpy(), lens - skip)
+    assert torch.equal(qc.nbuf, src.nbuf) and torch.equal(qc.ntok, src.ntok)
+    got = [t.cpu() for t in (qc.k, qc.v, qc.ks, qc.vs, qc.pos)]
+    live = np.zeros(tokens, bool)
+    for h in range(n):
+        o, ln = int(off[h]), int(lens[h]) - skip
+        live[o:o + ln] = True
+        for x, codes, scales in ((k, got[0], got[2]), (v, got[1], got[3])):
+            cc, ss = S.quantise(x[o + skip:o + skip + ln], bits)
+            assert np.array_equal(codes[o:o + ln].numpy(), S.packed(cc, bits)), h
+            assert np.array_equal(scales[o:o + ln].float().numpy(), ss, equal_nan=True), h
+        assert np.array_equal(got[4][o:o + ln].numpy(), np.arange(o, o + ln))
+    for t in (qc.k, qc.v, qc.ks, qc.vs):      # rows past a head's length are left alone
+        assert (t.view(torch.uint8).cpu().numpy()[~live] == 0x5A).all()
+    back = CacheBuffers(cfg, tokens, "cuda", qbuf=src.qbuf, label=src.label, off=src.off, cap=src.cap)
+    back.k.fill_(77.0)
+    H.hkv_quant_unpack(cfg, qc.c, back.c, H.HKV_ALL_LAYERS)
+    H.hkv_check(back.c)
+    bk, bv = back.k.float().cpu().numpy(), back.v.float().cpu().numpy()
+    assert (bk[~live] == 77.0).all()
+    for h in range(n):
+        o, ln = int(off[h]), int(lens[h]) - skip
+        for x, y in ((k, bk), (v, bv)):
+            want = rounded(S.stored(x[o + skip:o + skip + ln], bits).astype(np.float32), dtype)
+            assert np.array_equal(y[o:o + ln], want, equal_nan=True), h
+    assert torch.equal(back.len, qc.len)
+    # one layer alone: the other layer's heads are left alone
+    qc.len.fill_(-5)
+    H.hkv_quant_pack(cfg, src.c, qc.c, 1, H.HKV_PACK_SKIP_COND if skip else 0)
+    assert np.array_equal(qc.len.cpu().numpy(), np.r_[np.full(4, -5), lens[4:] - skip])
+
+
+def test_pack_reports_heads_that_do_not_fit():
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import QuantCacheBuffers
+    cfg = H.make_config(n_layers=1, n_seqs=1, n_heads=3, head_dim=64, dtype="bf16", n_cond=9,
+                        n_image=64, row_len=1, recent_w=1, local_w=1, period=4, group_at=64,
+                        global_budget=1)
+    rows = np.ones((60, 64), np.float32)
+    for what, code in (("room", 3), ("cond", 4), ("outside", 5)):
+        src = plain_cache(H, cfg, [10, 20, 15], [20, 20, 20], "bf16", rows, rows)
+        cap, off = src.cap.clone(), src.off.clone()
+        if what == "room":
+            cap[1] = 19
+        elif what == "cond":
+            src.len[1] = 8
+        else:
+            off[1] = 41
+        qc = QuantCacheBuffers(cfg, 8, 60, "cuda", qbuf=src.qbuf, label=src.label, off=off, cap=cap)
+        H.hkv_quant_pack(cfg, src.c, qc.c, 0, H.HKV_PACK_SKIP_COND if what == "cond" else 0)
+        with pytest.raises(H.HkvError) as e:
+            H.hkv_quant_check(qc.c)
+        assert e.value.status == code
+        want = [1, 0, 6] if what == "cond" else [10, 0, 15]
+        assert qc.len.tolist() == want
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D,dtype", [(64, "fp32"), (128, "bf16")])
+@pytest.mark.parametrize("r_s,distance", [(0.5, 0), (0.0, 0), (1.0, 0), (0.5, 1)])
+def test_update_of_codes(bits, D, dtype, r_s, distance):
+    """Evicted rows as the oracle's update chooses them from what the rows
+    stand for; survivors keep their codes and scales; heads whose buffer is
+    not full, and uncompressed heads, are left alone."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import QuantCacheBuffers
+    C, P, w, B, N, rl = 7, 12, 16, 60, 400, 20
+    cfg = H.make_config(n_layers=2, n_seqs=1, n_heads=6, head_dim=D, dtype=dtype, n_cond=C, n_image=N,
+                        row_len=rl, recent_w=w, local_w=w, period=P, group_at=40, global_budget=B,
+                        r_s=r_s, distance_mode=distance)
+    hp = O.HeadParams(n_cond=C, n_image=N, recent_w=w, local_w=w, period=P, group_at=40,
+                      global_budget=B, tau=0.9, r_s=r_s, row_len=rl,
+                      distance=O.GRID2D if distance else O.RASTER)
+    rng = np.random.default_rng(bits + D)
+    label = np.array([1, 1, 0, 255, 1, 0, 1, 1, 1, 0, 1, 1])
+    hist = np.array([B - w + P, B - w + 3, 20, 30, B - w + P, 0, B - w + P, 5, B - w + 1, 44, B - w + P,
+                     B - w + P])
+    nbuf = np.array([P, P, P, P, P - 1, P, P, P, P, P, P, P])
+    n = 12
+    ln = C + hist + w
+    caps = C + np.where(label == 0, w, B) + P
+    caps = np.maximum(caps, ln)              # the local and dense heads of this test hold more
+    caps[label == 1] = C + B + P
+    tokens = int(caps.sum())
+    off = np.cumsum(caps) - caps
+    ntok = rng.integers(N // 2, N, size=n)
+    k = rng.normal(size=(tokens, D)).astype(np.float32)
+    k[off[10]:off[10] + ln[10]] = k[off[10]]          # equal scores: the older goes first
+    v = rng.normal(size=(tokens, D)).astype(np.float32)
+    kc, ks = S.quantise(k, bits)
+    vc, vs = S.quantise(v, bits)
+    pos = np.zeros(tokens, np.int32)
+    for h in range(n):
+        img = np.sort(rng.choice(ntok[h] - w, size=hist[h], replace=False))
+        p = np.r_[np.arange(C), C + img, C + np.arange(ntok[h] - w, ntok[h])]
+        tail = p[C:].copy()
+        rng.shuffle(tail)                              # storage order is not position order
+        pos[off[h]:off[h] + ln[h]] = np.r_[p[:C], tail]
+    ring = rounded(rng.normal(size=(n, P, D)), dtype)
+    t = lambda x, d: torch.from_numpy(np.ascontiguousarray(x)).to(d).cuda()  # noqa: E731
+    qc = QuantCacheBuffers(cfg, bits, tokens, "cuda", qbuf=to_torch(ring, dtype),
+                           label=t(label, torch.uint8), off=t(off, torch.int64), cap=t(caps, torch.int32))
+    qc.k.copy_(t(S.packed(kc, bits), torch.uint8))
+    qc.v.copy_(t(S.packed(vc, bits), torch.uint8))
+    qc.ks.copy_(to_torch(ks, "bf16"))
+    qc.vs.copy_(to_torch(vs, "bf16"))
+    qc.pos.copy_(t(pos, torch.int32))
+    for a, b in ((qc.len, ln), (qc.nbuf, nbuf), (qc.ntok, ntok)):
+        a.copy_(t(b, torch.int32))
+    H.hkv_quant_evict(cfg, qc.c, 0)
+    mid = qc.len.cpu().numpy()
+    assert np.array_equal(mid[6:], ln[6:])             # one layer only
+    H.hkv_quant_evict_all(cfg, qc.c)
+    H.hkv_quant_check(qc.c)
+    K, kS, V, vS, ps = (x.float().cpu().numpy() for x in (qc.k, qc.ks, qc.v, qc.vs, qc.pos))
+    new_len, new_buf = qc.len.cpu().numpy(), qc.nbuf.cpu().numpy()
+    pk, pv, kv = S.packed(kc, bits), S.packed(vc, bits), S.values(kc, ks)
+    for h in range(n):
+        a = slice(off[h], off[h] + ln[h])
+        row_of = {int(p): off[h] + j for j, p in enumerate(pos[a])}
+        if label[h] == 255 or nbuf[h] < P:
+            want = np.sort(pos[a])
+            assert new_buf[h] == nbuf[h]
+        else:
+            keys = np.zeros((C + N, D), np.float32)
+            for p, r in row_of.items():
+                keys[p] = kv[r]
+            # the ring in the order of its tokens
+            q = np.zeros((N, D), np.float32)
+            for tt in range(ntok[h] - P, ntok[h]):
+                q[tt] = ring[h, tt % P]
+            want = np.sort(O.cache_update(np.sort(pos[a]).astype(np.int64), int(label[h]), hp, q, keys,
+                                          int(ntok[h]) - 1).pos)
+            assert new_buf[h] == 0
+        b = slice(off[h], off[h] + new_len[h])
+        assert np.array_equal(np.sort(ps[b]), want), h
+        src = np.array([row_of[int(p)] for p in ps[b]])
+        for got, ref in ((K, pk), (V, pv), (kS, ks), (vS, vs)):
+            assert np.array_equal(got[b], ref[src]), h
+
+
+def prefix_rows(rng, G, Hh, T, D, dtype, layout):
+    """k, v [G][H][T][D] views over memory of the given layout."""
+    import torch
+    gain = np.exp(0.5 * rng.normal(size=D))
+    k = to_torch(rounded(rng.normal(size=(G, Hh, T, D)) * gain, dtype), dtype)
+    v = to_torch(rounded(rng.normal(size=(G, Hh, T, D)), dtype), dtype)
+    if layout == "thd":              # [G][T][H][D]
+        k, v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+    elif layout == "padded":         # rows 16 bytes apart from packed, offset base
+        pad = 16 // k.element_size()
+        def spread(x):
+            y = torch.full((G, Hh, T + 1, D + pad), float("nan"), dtype=x.dtype, device="cuda")
+            z = y[:, :, 1:, :D]
+            z.copy_(x)
+            return z
+        k, v = spread(k), spread(v)
+    return k, v
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp32"), (128, "fp32")])
+@pytest.mark.parametrize("G,seqs,T,lens,layout", [
+    (1, 1, 1, [1], "htd"), (1, 3, 17, [17], "thd"), (1, 16, 64, [64], "padded"),
+    (2, 9, 130, [130, 0], "htd"), (3, 17, 333, [200, 333, 1], "thd"), (1, 40, 1025, [1025], "htd"),
+    (2, 70, 257, [255, 256], "padded"), (1, 130, 500, [463], "thd")])
+def test_prefix_attention(D, dtype, G, seqs, T, lens, layout):
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    rng = np.random.default_rng(D + T + seqs)
+    Hh = 3
+    cfg = H.make_config(n_layers=1, n_seqs=G * seqs, n_heads=Hh, head_dim=D, dtype=dtype, n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k, v = prefix_rows(rng, G, Hh, T, D, dtype, layout)
+    for g, ln in enumerate(lens):       # rows past a prompt's length are not looked at
+        k[g, :, ln:], v[g, :, ln:] = float("nan"), float("nan")
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pre = H.make_prefix(k, v, ln, err)
+    q = rounded(rng.normal(size=(G * seqs, Hh, D)) * 1.5, dtype)
+    ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+    out = torch.full((G * seqs, Hh, D), 3.0, device="cuda")
+    lse = torch.full((G * seqs, Hh), 3.0, device="cuda")
+    for _ in range(2):
+        H.hkv_prefix_attention(cfg, pre, to_torch(q, dtype), out, lse, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    kf, vf = k.float().cpu().numpy(), v.float().cpu().numpy()
+    for s in range(G * seqs):
+        g = s // seqs
+        for h in range(Hh):
+            K, V = kf[g, h, :lens[g]], vf[g, h, :lens[g]]
+            o, l = S.attention_lse(q[s, h], K, V)
+            to, tl = tolerances(q[s, h], K, V)
+            assert np.abs(got[s, h] - o).max() <= to, (s, h, np.abs(got[s, h] - o).max(), to)
+            assert gl[s, h] == l or abs(gl[s, h] - l) <= tl, (s, h)
+
+
+def test_prefix_length_out_of_range():
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    cfg = H.make_config(n_layers=1, n_seqs=4, n_heads=2, head_dim=64, dtype="bf16", n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k = torch.ones(2, 2, 50, 64, dtype=torch.bfloat16, device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pre = H.make_prefix(k, k, torch.tensor([50, 51], dtype=torch.int32, device="cuda"), err)
+    ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+    q = torch.ones(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros(4, 2, 64, device="cuda"), torch.zeros(4, 2, device="cuda")
+    H.hkv_prefix_attention(cfg, pre, q, out, lse, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert int(err) == H.HKV_ERR_BOUNDS
+    assert torch.isnan(out[2:]).all() and torch.isnan(lse[2:]).all()
+    assert torch.allclose(out[:2], torch.ones_like(out[:2]))
+
+
+class SharedPrompt:
+    """DeviceSynth whose conditioning tokens are sequence 0's for everyone."""
+
+    def __init__(self, w):
+        from synth.gpu import DeviceSynth
+        self.base = DeviceSynth(w, "cuda")
+        self.image = self.base.image
+
+    def cond(self, kc, vc, layer, stream):
+        self.base.cond(kc, vc, layer, stream)
+        kc.copy_(kc[:1].expand_as(kc))
+        vc.copy_(vc[:1].expand_as(vc))
+
+
+@pytest.mark.parametrize("bits,shared,name", [(8, False, "tiny"), (8, True, "tiny"), (4, False, "tiny"),
+                                              (4, True, "tiny"), (8, True, "janus_pro_7b"),
+                                              (4, False, "llamagen_xl")])
+def test_generation_with_a_quantised_cache(bits, shared, name):
+    """A whole generation: plain until the grouping token, then on codes, the
+    shared conditioning tokens in a prompt; outputs and retained positions as
+    the oracle's, step by step."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import Engine
+    from paper_2605_20600_gb300.runner import generate
+    from synth.gpu import DeviceSynth
+    w = configs.ALL[name].with_(n_seqs=2, n_layers=min(2, configs.ALL[name].n_layers), n_heads=8)
+    if name != "tiny":
+        w = w.with_(beta_fixed=(4.0, 4.0, 0.3, 4.0, 0.3, 0.3, 0.3, 4.0))
+    eng = Engine(cfg_of(H, w), "cuda")
+    E, N = w.group_at, w.n_image
+    steps = sorted({0, E - 1, E, E + 1, E + w.period - 1, E + w.period, E + 3 * w.period + 1, N - 1})
+    got = {}
+    generate(eng, (SharedPrompt if shared else lambda x: DeviceSynth(x, "cuda"))(w),
+             on_step=lambda t, out: got.__setitem__(t, out.cpu().numpy()) if t in steps else None,
+             cache_format=bits, shared_prompt=shared)
+    eng.check()
+    labels = eng.labels.cpu().numpy()
+    off, ln = eng.quant.off.cpu().numpy(), eng.quant.len.cpu().numpy()
+    pos = eng.quant.pos.cpu().numpy()
+    hp = O.HeadParams.of(w)
+    C = w.n_cond
+    heads = [(s, l, h) for s in range(2) for l in range(w.n_layers) for h in (0, 2, 5, 7)]
+    for s, l, h in heads:
+        hi = gen.HeadInputs(w, s, l, h)
+        k, v = hi.k.copy(), hi.v.copy()
+        if shared:
+            first = gen.HeadInputs(w, 0, l, h)
+            k[:C], v[:C] = first.k[:C], first.v[:C]
+        i = flat(w, s, l, h)
+        outs, want_pos = S.run_head_stored(hp, hi.q, k, v, bits, int(labels[i]), steps, plain_cond=shared)
+        p = np.sort(pos[off[i]:off[i] + ln[i]]) + (C if shared else 0)
+        assert np.array_equal(p, want_pos[want_pos >= C] if shared else want_pos), (s, l, h)
+        for t in steps:
+            to = 2e-3 if t < E and w.dtype == "bf16" else tolerances(hi.q[t], k[:C + t + 1], v[:C + t + 1])[0]
+            assert np.abs(got[t][l, s, h] - outs[t]).max() <= 2 * to, (s, l, h, t)
+
+
+def test_steps_in_a_graph_on_a_side_stream():
+    """Prompt attention and steps of two layers captured once and replayed:
+    the same cache and outputs as eager calls."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    D, n = 128, 8
+    res = []
+    for graph in (False, True):
+        c = QCache([300, 1, 64, 900, 0, 17, 511, 40] * 2, D, 8, "bf16", seed=2, n_seqs=4, slack=6)
+        c.cfg.n_layers, c.cfg.n_heads = 2, 2
+        ws_bytes = H.hkv_quant_workspace_size(c.cfg)
+        ws = torch.zeros(ws_bytes, dtype=torch.uint8, device="cuda")
+        rng = np.random.default_rng(0)
+        k, v = prefix_rows(rng, 2, 2, 90, D, "bf16", "htd")
+        pre = H.make_prefix(k, v, torch.tensor([90, 13], dtype=torch.int32, device="cuda"), c.err)
+        pws = torch.zeros(H.hkv_prefix_workspace_size(c.cfg, pre), dtype=torch.uint8, device="cuda")
+        q, kn, vn = (to_torch(x, "bf16").view(2, n, D) for x in (c.q, c.k_new, c.v_new))
+        out = torch.zeros(2, n, D, device="cuda")
+        po, pl = torch.zeros(n, D, device="cuda"), torch.zeros(n, device="cuda")
+
+        def token(st):
+            for layer in range(2):
+                H.hkv_prefix_attention(c.cfg, pre, q[layer], po, pl, pws, pws.numel(), st)
+                H.hkv_quant_step(c.cfg, c.c, layer, q[layer], kn[layer], vn[layer], out[layer], ws,
+                                 ws_bytes, prior=(po, pl), flags=H.HKV_STEP_PREFETCH, stream=st)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            token(side.cuda_stream)
+            if graph:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=side):
+                    token(side.cuda_stream)
+                g.replay()
+                g.replay()
+            else:
+                token(side.cuda_stream)
+                token(side.cuda_stream)
+        side.synchronize()
+        H.hkv_quant_check(c.c, side.cuda_stream)
+        res.append([out.cpu(), c.len.cpu(), c.ntok.cpu(), c.ck.cpu(), c.cv.cpu()])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+    assert np.array_equal(res[0][1].numpy(), c.lens + 3)

@@ -1,0 +1,198 @@
+"""The serving cache without a GPU: the library exports what the header
+declares, its host-side checks answer before any CUDA call, and the oracle's
+row format holds what it promises."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from conftest import ROOT
+
+from oracle import serve as S
+
+HEADER = os.path.join(ROOT, "include", "hkv_serve.h")
+
+
+@pytest.fixture(scope="module")
+def H():
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2605_20600_gb300 import hkv
+    hkv.lib()
+    return hkv
+
+
+def cfg_of(H, **kw):
+    base = dict(n_layers=2, n_seqs=4, n_heads=4, head_dim=64, dtype="bf16", n_cond=8, n_image=64,
+                row_len=8, recent_w=16, local_w=16, period=8, group_at=16, global_budget=24)
+    base.update(kw)
+    return H.make_config(**base)
+
+
+def caches(H):
+    # aligned host addresses: never dereferenced by the checks tested here
+    buf = ctypes.create_string_buffer(8192)
+    a = (ctypes.addressof(buf) + 255) & ~255
+    plain = H.hkv_cache(a, a, a, a, a, a, a, a, a, a, a, 1000)
+    quant = H.hkv_qcache(a, a, a, a, a, a, a, a, a, a, a, a, a, 1000, 8, 0)
+    prefix = H.hkv_prefix(a, a, a, None, 4 * 50 * 64, 50 * 64, 64, 2, 50)
+    return buf, a, plain, quant, prefix
+
+
+def test_every_declared_symbol_is_exported(H):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(hkv_[a-z_]+)\s*\(", text))
+    assert names == {"hkv_quant_pack", "hkv_quant_unpack", "hkv_quant_workspace_size",
+                     "hkv_quant_attention", "hkv_quant_step", "hkv_quant_evict",
+                     "hkv_quant_evict_all", "hkv_quant_check", "hkv_prefix_workspace_size", "hkv_prefix_attention"}
+    for n in names:
+        assert hasattr(H.lib(), n) and hasattr(H, n), n
+
+
+def test_struct_sizes(H):
+    assert ctypes.sizeof(H.hkv_qcache) == 14 * 8 + 8
+    assert ctypes.sizeof(H.hkv_prefix) == 7 * 8 + 8
+
+
+def status(f, *args):
+    return f(*args)
+
+
+def test_refusals(H):
+    buf, a, plain, quant, prefix = caches(H)
+    lib, R = H.lib(), ctypes.byref
+    cfg = cfg_of(H)
+    big = 1 << 30
+
+    def change(base, **kw):
+        x = type(base).from_buffer_copy(base)
+        for k, v in kw.items():
+            setattr(x, k, v)
+        return x
+
+    def attention(cfg=cfg, c=quant, layer=0, q=a, po=None, pl=None, out=a, ws=a, n=big):
+        return lib.hkv_quant_attention(R(cfg), R(c), layer, q, po, pl, out, None, ws, n, None)
+
+    assert attention(q=None) == 1 and attention(out=None) == 1 and attention(ws=None) == 1
+    assert attention(layer=2) == 1 and attention(layer=-1) == 1
+    assert attention(po=a) == 1 and attention(pl=a) == 1
+    assert attention(q=a + 8) == 8 and attention(out=a + 4) == 8 and attention(po=a + 8, pl=a) == 8
+    assert attention(n=8) == 3
+    assert attention(cfg=cfg_of(H, head_dim=96)) == 2
+    for field in ("k", "v", "ks", "vs", "pos", "off", "cap", "len", "nbuf", "ntok", "label", "qbuf", "err"):
+        assert attention(c=change(quant, **{field: None})) == 1, field
+    for field in ("k", "v", "ks", "vs", "qbuf"):
+        assert attention(c=change(quant, **{field: a + 8})) == 8, field
+    assert attention(c=change(quant, format=6)) == 1 and attention(c=change(quant, reserved=1)) == 1
+    assert attention(c=change(quant, capacity_tokens=0)) == 3
+    assert lib.hkv_quant_attention(R(cfg), None, 0, a, None, None, a, None, a, big, None) == 1
+
+    def step(k=a, v=a, flags=0, n=big):
+        return lib.hkv_quant_step(R(cfg), R(quant), 0, a, k, v, None, None, a, None, a, n, flags, None)
+
+    assert step(k=None) == 1 and step(v=None) == 1 and step(flags=2) == 1
+    assert step(k=a + 8) == 8 and step(n=16) == 3
+
+    assert lib.hkv_quant_pack(R(cfg), R(plain), R(quant), 2, 0, None) == 1
+    assert lib.hkv_quant_pack(R(cfg), R(plain), R(quant), -2, 0, None) == 1
+    assert lib.hkv_quant_pack(R(cfg), R(plain), R(quant), 0, 2, None) == 1
+    assert lib.hkv_quant_pack(R(cfg), R(plain), R(change(quant, qbuf=a + 256)), 0, 0, None) == 1
+    assert lib.hkv_quant_pack(R(cfg), None, R(quant), 0, 0, None) == 1
+    assert lib.hkv_quant_unpack(R(cfg), R(change(quant, qbuf=a + 256)), R(plain), 0, None) == 1
+    assert lib.hkv_quant_unpack(R(cfg), R(quant), None, 0, None) == 1
+    assert lib.hkv_quant_evict(R(cfg), R(quant), -1, None) == 1
+    assert lib.hkv_quant_evict(R(cfg), R(quant), 2, None) == 1
+    assert lib.hkv_quant_evict_all(R(cfg), None, None) == 1
+    assert lib.hkv_quant_check(None, None) == 1
+    assert lib.hkv_quant_check(R(change(quant, err=None)), None) == 1
+    # a ring that does not fit shared memory
+    assert lib.hkv_quant_evict_all(R(cfg_of(H, n_image=4000, period=2000, group_at=2000)), R(quant), None) == 3
+
+    def prefix_call(cfg=cfg, p=prefix, q=a, out=a, lse=a, ws=a, n=big):
+        return lib.hkv_prefix_attention(R(cfg), R(p), q, out, lse, ws, n, None)
+
+    assert prefix_call(q=None) == 1 and prefix_call(out=None) == 1 and prefix_call(lse=None) == 1
+    assert prefix_call(ws=None) == 1 and prefix_call(n=4) == 3
+    assert prefix_call(q=a + 2) == 8 and prefix_call(p=change(prefix, k=a + 8)) == 8
+    assert prefix_call(p=change(prefix, len=None)) == 1 and prefix_call(p=change(prefix, v=None)) == 1
+    assert prefix_call(p=change(prefix, n_groups=3)) == 2 and prefix_call(p=change(prefix, n_groups=0)) == 2
+    assert prefix_call(p=change(prefix, max_len=0)) == 2
+    for s in ("group_stride", "head_stride", "token_stride"):
+        assert prefix_call(p=change(prefix, **{s: 68})) == 2, s
+        assert prefix_call(p=change(prefix, **{s: 0})) == 2, s
+    assert H.hkv_prefix_workspace_size(cfg, change(prefix, n_groups=3)) == 0
+    assert H.hkv_quant_workspace_size(cfg_of(H, head_dim=32)) == 0
+    assert H.hkv_prefix_workspace_size(cfg, prefix) > 0 and H.hkv_quant_workspace_size(cfg) > 0
+
+
+@pytest.mark.parametrize("name", ["quant_pack", "quant_unpack", "quant_attention", "quant_step",
+                                  "quant_evict", "quant_evict_all", "quant_check",
+                                  "prefix_attention"])
+def test_fault_injection(H, name, monkeypatch):
+    monkeypatch.setenv("HKV_FAULT_INJECT", f"{name}:6")
+    buf, a, plain, quant, prefix = caches(H)
+    cfg = cfg_of(H)
+    calls = {
+        "quant_pack": lambda: H.hkv_quant_pack(cfg, plain, quant, 0),
+        "quant_unpack": lambda: H.hkv_quant_unpack(cfg, quant, plain, 0),
+        "quant_attention": lambda: H.hkv_quant_attention(cfg, quant, 0, a, a, a, 1 << 30),
+        "quant_step": lambda: H.hkv_quant_step(cfg, quant, 0, a, a, a, a, a, 1 << 30),
+        "quant_evict": lambda: H.hkv_quant_evict(cfg, quant, 0),
+        "quant_evict_all": lambda: H.hkv_quant_evict_all(cfg, quant),
+        "quant_check": lambda: H.hkv_quant_check(quant),
+        "prefix_attention": lambda: H.hkv_prefix_attention(cfg, prefix, a, a, a, a, 1 << 30),
+    }
+    with pytest.raises(H.HkvError) as e:
+        calls[name]()
+    assert e.value.status == 6
+
+
+def test_make_prefix_refuses(H):
+    import torch
+    k = torch.zeros(2, 3, 10, 64)
+    n = torch.zeros(2, dtype=torch.int32)
+    H.make_prefix(k, torch.zeros(2, 3, 10, 64), n)
+    for bad in (lambda: H.make_prefix(k[0], k[0], n), lambda: H.make_prefix(k, k[:, :2], n),
+                lambda: H.make_prefix(k.transpose(2, 3), k.transpose(2, 3), n),
+                lambda: H.make_prefix(k, k.transpose(1, 2).contiguous().transpose(1, 2), n),
+                lambda: H.make_prefix(k, k, n[:1])):
+        with pytest.raises(H.HkvError):
+            bad()
+
+
+def test_runner_refuses_what_it_cannot_run(H):
+    from paper_2605_20600_gb300.runner import generate
+
+    class Fake:
+        cfg = cfg_of(H)
+
+    with pytest.raises(ValueError):
+        generate(Fake(), None, fused=False, cache_format=8)
+    with pytest.raises(ValueError):
+        generate(Fake(), None, shared_prompt=True)
+    Fake.cfg = cfg_of(H, n_cond=0)
+    with pytest.raises(ValueError):
+        generate(Fake(), None, cache_format=8, shared_prompt=True)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_oracle_row_format(bits):
+    """What a row stands for is within half a step (and the rounding of the
+    scale) of the row; storing and reading the codes is exact."""
+    rng = np.random.default_rng(0)
+    x = (rng.normal(size=(200, 128)) * np.exp(rng.normal(size=(200, 1)) * 5)).astype(np.float32)
+    c, s = S.quantise(x, bits)
+    M = 127 if bits == 8 else 7
+    assert np.abs(c).max() == M
+    assert np.array_equal(S.unpacked(S.packed(c, bits), bits), c)
+    err = np.abs(S.values(c, s) - x).reshape(200, 4, 32)
+    # half a step, or what the clamp cuts where the scale was rounded down
+    assert (err <= s[..., None] * (0.5 + M * 2.0 ** -8)).all()
+    z, sz = S.quantise(np.zeros((1, 32), np.float32), bits)
+    assert (z == 0).all() and (sz == 0).all()
+    bad = np.zeros((2, 32), np.float32)
+    bad[0, 1], bad[1, 2] = np.inf, np.nan
+    c, s = S.quantise(bad, bits)
+    assert np.isnan(s).all() and (c == 0).all()
