@@ -38,13 +38,13 @@ struct QAttnArgs {
   float *out, *lse;                       // [nheads][D], [nheads] or null
   uint32_t *count;             // [nheads] arrivals, zero between launches
   float *part;                 // [nheads][nchunks][D + 4] partial results
-  int nchunks;                 // chunks of quant_chunk_tokens per head
+  int chunk, nchunks;          // rows a CTA takes at most, CTAs per head
   int P, C, prefetch;
   float qscale;                // log2(e) / sqrt(D)
 };
 
-// tokens of a head one CTA attends over, and chunks of the longest segment
-int quant_chunks(int max_segment);
+// rows of a head one CTA attends over at most
+int quant_chunk(int nheads, int max_segment);
 cudaError_t launch_quant_attention(const QAttnArgs &a, int D, int dtype, int bits, cudaStream_t s);
 
 // attention of a batch over shared prompts, one layer

@@ -65,8 +65,14 @@ size_t quant_counts_bytes(const hkv_config *c) {
   return align256((size_t)heads_per_layer(c) * sizeof(uint32_t));
 }
 
+// CTAs per head of the attention
+int quant_chunks(const hkv_config *c) {
+  const int seg = max_segment(c), chunk = quant_chunk(heads_per_layer(c), seg);
+  return (seg + chunk - 1) / chunk;
+}
+
 size_t quant_ws_bytes(const hkv_config *c) {
-  const int nch = quant_chunks(max_segment(c));
+  const int nch = quant_chunks(c);
   const size_t parts =
       nch > 1 ? (size_t)heads_per_layer(c) * nch * (c->head_dim + 4) * sizeof(float) : 0;
   return quant_counts_bytes(c) + align256(parts);
@@ -101,7 +107,8 @@ hkv_status quant_attend(const char *name, const hkv_config *cfg, const hkv_qcach
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   a.count = reinterpret_cast<uint32_t *>(ws);
   a.part = reinterpret_cast<float *>(ws + quant_counts_bytes(cfg));
-  a.nchunks = quant_chunks(max_segment(cfg));
+  a.chunk = quant_chunk(a.nheads, max_segment(cfg));
+  a.nchunks = quant_chunks(cfg);
   a.P = cfg->period;
   a.C = cfg->n_cond;
   a.prefetch = (flags & HKV_STEP_PREFETCH) ? 1 : 0;
