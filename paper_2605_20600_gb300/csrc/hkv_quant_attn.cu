@@ -38,7 +38,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 32;    // rows a warp handles at a time
-constexpr int kStages = 2;   // tiles in flight per warp
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLoScale = 2048.f, kLoUnscale = 1.f / 2048.f;  // second parts, 2^11
@@ -109,16 +108,16 @@ __device__ __forceinline__ float inv_pow2(float p) {
   return __uint_as_float(0x7F000000u - __float_as_uint(p));
 }
 
-// Shared memory of a warp: kStages tiles (codes of K and V, scales of K and
+// Shared memory of a warp: STAGES tiles (codes of K and V, scales of K and
 // V), the query's two parts, the weights' B operand.
-template <int D, int BITS>
+template <int D, int BITS, int STAGES>
 struct Smem {
   using R = QRow<D, BITS>;
   static constexpr int kCodes = kTile * R::kBytes, kScales = kTile * R::kScaleBytes;
   static constexpr int kStage = 2 * (kCodes + kScales);
   static constexpr int kQ = 2 * D * 2;        // fp16 [2][D]
   static constexpr int kW = 8 * kTile * 2;    // fp16 [8][kTile]
-  static constexpr int kWarp = kStages * kStage + kQ + kW;
+  static constexpr int kWarp = STAGES * kStage + kQ + kW;
   static constexpr int kTotal = kWarps * kWarp;
 };
 
@@ -131,16 +130,20 @@ __device__ __forceinline__ int piece_at(int r, int c) {
   return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
 }
 
-template <int D, typename T, int BITS, bool STEP>
-__global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p) {
+// STAGES = 1: every warp has at most one tile (ranges of at most kThreads
+// rows); more: it walks through its tiles, that many of them in flight.
+template <int D, typename T, int BITS, bool STEP, int STAGES>
+__global__ void __launch_bounds__(kThreads, STAGES == 1 ? 6 : 4)
+    quant_attn_kernel(const QAttnArgs p) {
   using R = QRow<D, BITS>;
-  using SM = Smem<D, BITS>;
+  using SM = Smem<D, BITS, STAGES>;
   constexpr int RB = R::kBytes, SB = R::kScaleBytes, G = R::kGroups;
   constexpr int PF = D + 4;          // floats of a partial result
   constexpr int KM = D / 16;         // products per 16 rows, scores and output alike
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ float s_acc[kWarps][D];
   __shared__ float s_m[kWarps], s_l[kWarps];
+  __shared__ float s_factor[kThreads];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row8 = lane >> 2, quad = lane & 3;
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
   };
   const int first = lo + warp * kTile;
 #pragma unroll
-  for (int st = 0; st < kStages; ++st) {
+  for (int st = 0; st < STAGES; ++st) {
     const int r0 = first + st * kWarps * kTile;
     if (r0 < hi) load_tile(r0, st);
     cp_async_commit();
@@ -223,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
     }
     const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
     const float xscale = q2 * p.qscale;
-    __half *sq = reinterpret_cast<__half *>(ws + kStages * SM::kStage);
+    __half *sq = reinterpret_cast<__half *>(ws + STAGES * SM::kStage);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int d = lane * E + e;
@@ -250,14 +253,14 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
         qf[2 * x + 1][1] = u.w;
       }
     }
-    __half *sw = reinterpret_cast<__half *>(ws + kStages * SM::kStage + SM::kQ);
+    __half *sw = reinterpret_cast<__half *>(ws + STAGES * SM::kStage + SM::kQ);
     // where this lane's row (row8 + 8 quad) sits in the weights' columns
     const int own = row8 + 8 * quad;
     const int own_at = ((own >> 1) & 3) * 8 + (own >> 4) * 4 + ((own >> 3) & 1) * 2 + (own & 1);
 
     int st = 0;
     for (int r0 = first; r0 < hi; r0 += kWarps * kTile) {
-      cp_async_wait<kStages - 1>();
+      cp_async_wait<STAGES - 1>();
       __syncwarp();
       unsigned char *sk = ws + st * SM::kStage, *sv = sk + SM::kCodes;
       unsigned char *ss = sv + SM::kCodes;
@@ -350,7 +353,9 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
       float mt = x;
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, o));
-      if (mt > m) {  // the same for the whole warp
+      if (STAGES == 1) {
+        m = mt;
+      } else if (mt > m) {  // the same for the whole warp
         const float f = ex2_approx(m - mt);
         m = mt;
         l *= f;
@@ -433,11 +438,12 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
         acc[y][0] = fmaf(fmaf(o[y][1], kLoUnscale, o[y][0]), unit, acc[y][0]);
         acc[y][1] = fmaf(fmaf(o[y][3], kLoUnscale, o[y][2]), unit, acc[y][1]);
       }
+      if (STAGES == 1) break;
       __syncwarp();  // the stage and the weights are rewritten from here on
-      const int next = r0 + kStages * kWarps * kTile;
+      const int next = r0 + STAGES * kWarps * kTile;
       if (next < hi) load_tile(next, st);
       cp_async_commit();
-      st = st + 1 == kStages ? 0 : st + 1;
+      st = st + 1 == STAGES ? 0 : st + 1;
     }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
@@ -474,28 +480,43 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
     float *part = p.part + ((size_t)hl * p.nchunks + ch) * PF;
     if (active) {
       if (tid < D) part[tid] = out;
-      if (tid == 0) {
-        part[D] = m;
-        part[D + 1] = l;
-      }
+      if (tid == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      __threadfence();  // after the barrier it covers the whole CTA's writes
+      s_last = atomicAdd(p.count + hl, 1u) == (uint32_t)p.nchunks - 1u;
       __threadfence();
     }
     __syncthreads();
-    if (tid == 0) s_last = atomicAdd(p.count + hl, 1u) == (uint32_t)p.nchunks - 1u;
-    __syncthreads();
     if (!s_last) return;
-    __threadfence();
+    // at most kThreads ranges (quant_chunk): one thread each for their factors
     const int np = n > 0 ? (n + per - 1) / per : 1;
-    const float *first = p.part + (size_t)hl * p.nchunks * PF;
-    m = -INFINITY;
-    for (int j = 0; j < np; ++j) m = fmaxf(m, __ldcg(first + (size_t)j * PF + D));
-    l = out = 0.f;
-    for (int j = 0; j < np; ++j) {
-      const float lj = __ldcg(first + (size_t)j * PF + D + 1);
-      if (lj == 0.f) continue;
-      const float f = ex2_approx(__ldcg(first + (size_t)j * PF + D) - m);
-      l += lj * f;
-      if (tid < D) out += __ldcg(first + (size_t)j * PF + tid) * f;
+    const float *first_part = p.part + (size_t)hl * p.nchunks * PF;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (tid < np) ml = __ldcg(reinterpret_cast<const float2 *>(first_part + (size_t)tid * PF + D));
+    float mx = ml.x;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
+    if (lane == 0) s_m[warp] = mx;
+    __syncthreads();
+    m = s_m[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_m[w]);
+    const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - m);
+    s_factor[tid] = f;
+    l = ml.y * f;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) l += s_l[w];
+    out = 0.f;
+    if (tid < D) {
+#pragma unroll 8
+      for (int j = 0; j < np; ++j) out += __ldcg(first_part + (size_t)j * PF + tid) * s_factor[j];
     }
     if (tid == 0) p.count[hl] = 0u;
   }
@@ -524,32 +545,37 @@ __global__ void __launch_bounds__(kThreads) quant_attn_kernel(const QAttnArgs p)
 
 }  // namespace
 
+// Rows of a CTA's range at most: one tile per warp, or, for segments of more
+// than kMostRanges such ranges, as many as keep to that number (the CTA that
+// joins a head's ranges handles one per thread).
+constexpr int kMostRanges = 96;
 int quant_chunk(int nheads, int max_segment) {
   (void)nheads;
-  (void)max_segment;
-  return 256;
+  constexpr int one = kWarps * kTile;
+  const int tiles = (max_segment + kMostRanges * one - 1) / (kMostRanges * one);
+  return one * (tiles < 1 ? 1 : tiles);
 }
 
 namespace {
 
-template <int D, typename T, int BITS, bool STEP>
+template <int D, typename T, int BITS, bool STEP, int STAGES>
 cudaError_t launch(const QAttnArgs &a, int grid, cudaStream_t s) {
-  constexpr int smem = Smem<D, BITS>::kTotal;
+  constexpr int smem = Smem<D, BITS, STAGES>::kTotal;
   static std::atomic<uint64_t> ready{0};  // devices whose limit is set
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP>,
+    e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP, STAGES>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP>,
+      e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP, STAGES>,
                                cudaFuncAttributePreferredSharedMemoryCarveout, 100);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  return pdl_launch(quant_attn_kernel<D, T, BITS, STEP>, grid, kThreads, smem, s, a);
+  return pdl_launch(quant_attn_kernel<D, T, BITS, STEP, STAGES>, grid, kThreads, smem, s, a);
 }
 
 }  // namespace
@@ -559,12 +585,18 @@ cudaError_t launch_quant_attention(const QAttnArgs &a, int D, int dtype, int bit
   const long long grid = (long long)a.nheads * a.nchunks;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
 #define HKV_QATTN(BITS_, STEP_) \
-  HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_>(a, (int)grid, s))
+  if (a.chunk == kWarps * kTile)                                              \
+    HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_, 1>(a, (int)grid, s)); \
+  HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_, 2>(a, (int)grid, s))
   if (bits == HKV_Q8) {
-    if (a.k_new) HKV_QATTN(8, true);
+    if (a.k_new) {
+      HKV_QATTN(8, true);
+    }
     HKV_QATTN(8, false);
   }
-  if (a.k_new) HKV_QATTN(4, true);
+  if (a.k_new) {
+    HKV_QATTN(4, true);
+  }
   HKV_QATTN(4, false);
 #undef HKV_QATTN
   return cudaErrorInvalidValue;

@@ -153,7 +153,7 @@ def _p(x) -> int | None:
 
 
 def _call(name: str, *args) -> None:
-    st = getattr(lib(), "hkv_" + name)(*args)
+    st = getattr(_lib or lib(), "hkv_" + name)(*args)
     if st != HKV_OK:
         raise HkvError(name, st)
 
