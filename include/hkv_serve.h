@@ -155,9 +155,9 @@ hkv_status hkv_quant_evict_all(const hkv_config *cfg, const hkv_qcache *cache, h
  * status recorded in its error word. */
 hkv_status hkv_quant_check(const hkv_qcache *cache, hkv_stream_t stream);
 
-/* Bytes of device workspace hkv_prefix_attention needs; zero-fill it before
- * the first use, every call leaves it ready for the next, calls that may
- * overlap must not share it. Host only; 0 for bad arguments. */
+/* Bytes of device workspace hkv_prefix_attention needs (partial results; it
+ * may hold anything). Calls that may overlap must not share it. Host only; 0
+ * for bad arguments. */
 size_t hkv_prefix_workspace_size(const hkv_config *cfg, const hkv_prefix *prefix);
 
 /* Attention of one query per sequence and head over the sequence's shared

@@ -1,10 +1,16 @@
 // Attention of a batch over prompts that its sequences share: every prompt
 // row serves all sequences of its group.
 //
-// A CTA takes a tile of queries of one (group, head) and a range of the
-// prompt's keys, one query per warp. Ranges of the same tile leave partial
-// results in the workspace; the CTA that arrives last joins them in range
-// order.
+// A CTA takes up to 64 queries of one (group, head) and a range of the
+// prompt's keys, tile by tile (64 keys), on the tensor cores (mma.sync
+// m16n8k16, bf16 operands, fp32 sums). MW warps lie along the queries, 16
+// each, the others along the keys of a tile; their results are joined in
+// shared memory. Ranges of one prompt are joined by a second kernel.
+//
+// Precision: bf16 queries, keys and values enter as they are, and the weights
+// as three bf16 parts (24 bits); an fp32 element is three parts as well, and
+// the six products of parts that reach past 2^-24 are taken, the small ones
+// first. Products chain in the tensor core within a tile only.
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
@@ -12,16 +18,119 @@
 namespace hkv {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = kThreads / 32;  // queries per CTA
-
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kKeys = 64;       // keys of a tile
+constexpr int kMostSplits = 32; // key ranges of a prompt: a lane each in the join
 constexpr float kLn2 = 0.6931471805599453f;
 
+template <typename T>
+struct Parts {
+  static constexpr int kPlanes = 1, kStages = 2;
+};
+template <>
+struct Parts<float> {
+  static constexpr int kPlanes = 3, kStages = 1;
+};
+
+template <int D, typename T, int MW>
+struct PSmem {
+  static constexpr int kRow = D * 2;                            // bytes of a bf16 row
+  static constexpr int kPlane = kKeys * kRow;
+  static constexpr int kStage = 2 * Parts<T>::kPlanes * kPlane;  // K planes, V planes
+  static constexpr int kQPlane = MW * 16 * kRow;
+  static constexpr int kQ = Parts<T>::kPlanes * kQPlane;
+  static constexpr int kTiles = Parts<T>::kStages * kStage;
+  static constexpr int kTotal = kTiles + kQ;
+  static_assert(kWarps * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
+};
+
+// byte offset of 16-byte piece c of row r: pieces permuted over the banks
+template <int D>
+__device__ __forceinline__ int at16(int r, int c) {
+  return r * (D * 2) + ((c ^ (r & 7)) << 4);
+}
+
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes to shared memory, zeros where `on` is false (nothing is read then)
+__device__ __forceinline__ void cp_async16_zfill(void *dst, const void *src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src),
+               "r"(on ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+// a pair of fp32 as bf16 parts of falling size; the remainder is exact
+__device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[3]) {
+#pragma unroll
+  for (int j = 0; j < 3; ++j) {
+    p[j] = pack2(x, y);
+    x -= __uint_as_float(p[j] << 16);
+    y -= __uint_as_float(p[j] & 0xFFFF0000u);
+  }
+}
+
+// Copies `rows` rows of D elements into the planes at dst (row stride as
+// at16), rows from `live` on as zeros. bf16: asynchronous.
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads) prefix_kernel(const PrefixArgs p, int split_len) {
-  constexpr int PF = D + 4, E = D / 32;
-  __shared__ int s_last;
+__device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T *src,
+                                          long long stride, int rows, int live) {
+  constexpr int PPR = D / 8;
+  for (int e = threadIdx.x; e < rows * PPR; e += kThreads) {
+    const int r = e / PPR, c = e % PPR;
+    const bool on = r < live;
+    const T *from = src + (on ? r * stride : 0) + c * 8;
+    if (sizeof(T) == 2) {
+      cp_async16_zfill(dst + at16<D>(r, c), from, on);
+    } else {
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (on) {
+        Elem<float>::unpack(reinterpret_cast<const uint4 *>(from)[0], x);
+        Elem<float>::unpack(reinterpret_cast<const uint4 *>(from)[1], x + 4);
+      }
+      uint32_t p[4][3];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) split2(x[2 * j], x[2 * j + 1], p[j]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        *reinterpret_cast<uint4 *>(dst + k * plane + at16<D>(r, c)) =
+            make_uint4(p[0][k], p[1][k], p[2][k], p[3][k]);
+    }
+  }
+}
+
+template <int D, typename T, int MW>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
+    prefix_kernel(const PrefixArgs p, int split_len) {
+  using SM = PSmem<D, T, MW>;
+  constexpr int NP = Parts<T>::kPlanes, STAGES = Parts<T>::kStages;
+  constexpr int KW = kWarps / MW, NKW = kKeys / KW;  // keys of a tile per warp
+  constexpr int PF = D + 4;
+  extern __shared__ __align__(128) unsigned char dyn[];
+  __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int mw = warp % MW, kw = warp / MW;
   int b = blockIdx.x;
   const int tile = b % p.tiles;
   b /= p.tiles;
@@ -36,89 +145,304 @@ __global__ void __launch_bounds__(kThreads) prefix_kernel(const PrefixArgs p, in
     if (p.err && tid == 0 && sp == 0) set_err(p.err, HKV_ERR_BOUNDS);
     len = 0;
   }
-  const int sl = tile * kTile + warp;  // sequence within the group
-  const bool on = sl < p.seqs;
-  const size_t qi = ((size_t)g * p.seqs + sl) * p.heads + h;
+  const int q0 = tile * MW * 16;                 // first sequence within the group
+  const int nq = min(MW * 16, p.seqs - q0);
+  const size_t qrow = ((size_t)g * p.seqs + q0) * p.heads + h;  // row of query q0; next: + heads
   const int lo = sp * split_len, hi = min(len, lo + split_len);
-  float q[E], acc[E];
-  float m = -INFINITY, l = 0.f;
+  const T *K = static_cast<const T *>(p.k) + g * p.gs + h * p.hs;
+  const T *V = static_cast<const T *>(p.v) + g * p.gs + h * p.hs;
+  unsigned char *sq = dyn + SM::kTiles;
+
+  auto load_tile = [&](int k0, int st) {
+    unsigned char *s = dyn + st * SM::kStage;
+    load_rows<D, T>(s, SM::kPlane, K + k0 * p.ts, p.ts, kKeys, hi - k0);
+    load_rows<D, T>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.ts, p.ts, kKeys, hi - k0);
+  };
+
+  float o[D / 8][4];
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  if (lo < hi) {
+    load_rows<D, T>(sq, SM::kQPlane, static_cast<const T *>(p.q) + qrow * D,
+                    (long long)p.heads * D, MW * 16, nq);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (STAGES > 1) {
+#pragma unroll
+      for (int st = 0; st < STAGES; ++st) {
+        if (lo + st * kKeys < hi) load_tile(lo + st * kKeys, st);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+    }
+    // fragment addresses: which row and piece of a 16 x 16 block a lane names
+    const int mi = lane >> 3, mr = lane & 7;
+    const uint32_t q_base = smem_u32(sq), t_base = smem_u32(dyn);
+    const int q_row = mw * 16 + (mi & 1) * 8 + mr, q_pc = mi >> 1;
+    const int k_row = kw * NKW + (mi >> 1) * 8 + mr, k_pc = mi & 1;
+    const int v_row = kw * NKW + (mi & 1) * 8 + mr, v_pc = mi >> 1;
+    uint32_t qf[NP == 1 ? D / 16 : 1][4];
+
+    int st = 0;
+    bool have_q = false;
+    for (int k0 = lo; k0 < hi; k0 += kKeys) {
+      if (STAGES == 1) {
+        __syncthreads();  // the tile before this one has been read
+        load_tile(k0, 0);
+      } else {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      }
+      __syncthreads();
+      if (NP == 1 && !have_q) {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) ldm4(qf[ks], q_base + at16<D>(q_row, 2 * ks + q_pc));
+        have_q = true;
+      }
+      const uint32_t kb = t_base + st * SM::kStage, vb = kb + NP * SM::kPlane;
+      float s[NKW / 8][4];
+#pragma unroll
+      for (int x = 0; x < NKW / 8; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+      if (NP == 1) {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+#pragma unroll
+          for (int nb = 0; nb < NKW / 16; ++nb) {
+            uint32_t f[4];
+            ldm4(f, kb + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
+            mma_bf16(s[2 * nb], qf[NP == 1 ? ks : 0], f[0], f[1]);
+            mma_bf16(s[2 * nb + 1], qf[NP == 1 ? ks : 0], f[2], f[3]);
+          }
+        }
+      } else {
+        // parts (2,0) (1,1) (0,2), then (1,0) (0,1), then (0,0)
+#pragma unroll
+        for (int order = 2; order >= 0; --order) {
+#pragma unroll 1
+          for (int ks = 0; ks < D / 16; ++ks) {
+#pragma unroll
+            for (int a = order; a >= 0; --a) {
+              uint32_t qa[4];
+              ldm4(qa, q_base + a * SM::kQPlane + at16<D>(q_row, 2 * ks + q_pc));
+#pragma unroll
+              for (int nb = 0; nb < NKW / 16; ++nb) {
+                uint32_t f[4];
+                ldm4(f, kb + (order - a) * SM::kPlane + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
+                mma_bf16(s[2 * nb], qa, f[0], f[1]);
+                mma_bf16(s[2 * nb + 1], qa, f[2], f[3]);
+              }
+            }
+          }
+        }
+      }
+      // weights of rows lane / 4 (j = 0) and lane / 4 + 8 (j = 1)
+      const int left = hi - k0 - kw * NKW;  // keys of this warp's part that count
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int x = 0; x < NKW / 8; ++x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = x * 8 + (lane & 3) * 2 + (e & 1);
+          s[x][e] = key < left ? s[x][e] * p.qscale : -INFINITY;
+          mx[e >> 1] = fmaxf(mx[e >> 1], s[x][e]);
+        }
+      }
+      float f[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xFFFFFFFFu, mx[j], 1));
+        mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xFFFFFFFFu, mx[j], 2));
+        const float mn = fmaxf(m[j], mx[j]);
+        f[j] = mn == m[j] ? 1.f : ex2_approx(m[j] - mn);
+        m[j] = mn;
+        l[j] *= f[j];
+      }
+      if (__any_sync(0xFFFFFFFFu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) {
+          o[x][0] *= f[0];
+          o[x][1] *= f[0];
+          o[x][2] *= f[1];
+          o[x][3] *= f[1];
+        }
+      }
+      uint32_t pf[NKW / 16][3][4];
+#pragma unroll
+      for (int x = 0; x < NKW / 8; ++x) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          // a key that does not count weighs nothing (all of them: m is -inf)
+          const int key = x * 8 + (lane & 3) * 2;
+          const float w0 = key < left ? ex2_approx(s[x][2 * j] - m[j]) : 0.f;
+          const float w1 = key + 1 < left ? ex2_approx(s[x][2 * j + 1] - m[j]) : 0.f;
+          l[j] += w0 + w1;
+          uint32_t pr[3];
+          split2(w0, w1, pr);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) pf[x / 2][k][(x & 1) * 2 + j] = pr[k];
+        }
+      }
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        float t[2][4] = {};
+        if (NP == 1) {
+          uint32_t vf[NKW / 16][4];
+#pragma unroll
+          for (int kk = 0; kk < NKW / 16; ++kk)
+            ldm4t(vf[kk], vb + at16<D>(v_row + kk * 16, 2 * db + v_pc));
+#pragma unroll
+          for (int a = 2; a >= 0; --a) {
+#pragma unroll
+            for (int kk = 0; kk < NKW / 16; ++kk) {
+              mma_bf16(t[0], pf[kk][a], vf[kk][0], vf[kk][1]);
+              mma_bf16(t[1], pf[kk][a], vf[kk][2], vf[kk][3]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int order = 2; order >= 0; --order) {
+#pragma unroll
+            for (int a = order; a >= 0; --a) {
+#pragma unroll
+              for (int kk = 0; kk < NKW / 16; ++kk) {
+                uint32_t vf[4];
+                ldm4t(vf, vb + (order - a) * SM::kPlane + at16<D>(v_row + kk * 16, 2 * db + v_pc));
+                mma_bf16(t[0], pf[kk][a], vf[0], vf[1]);
+                mma_bf16(t[1], pf[kk][a], vf[2], vf[3]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[2 * db + x][e] += t[x][e];
+      }
+      if (STAGES > 1) {
+        __syncthreads();  // the stage is rewritten
+        const int next = k0 + STAGES * kKeys;
+        if (next < hi) load_tile(next, st);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        st = st + 1 == STAGES ? 0 : st + 1;
+      }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    l[j] += __shfl_xor_sync(0xFFFFFFFFu, l[j], 1);
+    l[j] += __shfl_xor_sync(0xFFFFFFFFu, l[j], 2);
+    if ((lane & 3) == 0) {
+      s_m[warp][(lane >> 2) + 8 * j] = m[j];
+      s_l[warp][(lane >> 2) + 8 * j] = l[j];
+    }
+  }
+  __syncthreads();
+  float *so = reinterpret_cast<float *>(dyn);  // [warp][16][D]
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<float2 *>(
+          so + (size_t)(warp * 16 + (lane >> 2) + 8 * j) * D + x * 8 + (lane & 3) * 2) =
+          make_float2(o[x][2 * j], o[x][2 * j + 1]);
+  }
+  __syncthreads();
+  // rows of D / 4 threads each: the warps along the keys joined
+  for (int e = tid; e < nq * (D / 4); e += kThreads) {
+    const int r = e / (D / 4), c = e % (D / 4), w0 = r >> 4, rr = r & 15;
+    float mj = -INFINITY, lj = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) mj = fmaxf(mj, s_m[w0 + k * MW][rr]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const int w = w0 + k * MW;
+      if (s_l[w][rr] == 0.f) continue;
+      const float fk = ex2_approx(s_m[w][rr] - mj);
+      const float4 u = *reinterpret_cast<const float4 *>(so + (size_t)(w * 16 + rr) * D + c * 4);
+      lj += s_l[w][rr] * fk;
+      v.x += u.x * fk, v.y += u.y * fk, v.z += u.z * fk, v.w += u.w * fk;
+    }
+    const size_t row = qrow + (size_t)r * p.heads;
+    if (p.splits > 1) {
+      float *part = p.part + (row * p.splits + sp) * PF;
+      *reinterpret_cast<float4 *>(part + c * 4) = v;
+      if (c == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(bad ? NAN : mj, lj);
+    } else {
+      const float inv = bad ? NAN : lj == 0.f ? 0.f : 1.f / lj;
+      *reinterpret_cast<float4 *>(p.out + row * D + c * 4) =
+          make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      if (c == 0) p.lse[row] = bad ? NAN : lj == 0.f ? -INFINITY : (mj + log2f(lj)) * kLn2;
+    }
+  }
+}
+
+// Joins a query's ranges in their order, a warp per query: lane j < splits
+// holds range j's maximum and sum.
+constexpr int kJoinThreads = 128;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixArgs p, int rows) {
+  constexpr int PF = D + 4, E = D / 32;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int row = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const float *first = p.part + (size_t)row * p.splits * PF;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < p.splits) ml = *reinterpret_cast<const float2 *>(first + (size_t)lane * PF + D);
+  const bool bad = __any_sync(0xFFFFFFFFu, ml.x != ml.x && ml.y == 0.f);
+  float m = ml.x;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - m);
+  float l = ml.y * f;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+  float acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  if (on) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      q[e] = (float)static_cast<const T *>(p.q)[qi * D + lane * E + e] * p.qscale;
-    const T *K = static_cast<const T *>(p.k) + g * p.gs + h * p.hs + lane * E;
-    const T *V = static_cast<const T *>(p.v) + g * p.gs + h * p.hs + lane * E;
-    for (int t = lo; t < hi; ++t) {
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(q[e], (float)K[t * p.ts + e], x);
-#pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-      const float mn = fmaxf(m, x);
-      const float f = exp2f(m - mn), w = exp2f(x - mn);
-      m = mn;
-      l = l * f + w;
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + w * (float)V[t * p.ts + e];
+#pragma unroll 8
+  for (int j = 0; j < p.splits; ++j) {
+    const float fj = __shfl_sync(0xFFFFFFFFu, f, j);
+    const float *src = first + (size_t)j * PF + lane * E;
+    if (E == 4) {
+      const float4 u = *reinterpret_cast<const float4 *>(src);
+      acc[0] += u.x * fj, acc[1 % E] += u.y * fj, acc[2 % E] += u.z * fj, acc[3 % E] += u.w * fj;
+    } else {
+      const float2 u = *reinterpret_cast<const float2 *>(src);
+      acc[0] += u.x * fj, acc[1 % E] += u.y * fj;
     }
   }
-  if (p.splits > 1) {
-    float *part = p.part + (qi * p.splits + sp) * PF;
-    if (on) {
+  const float inv = bad ? NAN : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-      for (int e = 0; e < E; ++e) part[lane * E + e] = acc[e];
-      if (lane == 0) {
-        part[D] = m;
-        part[D + 1] = l;
-      }
-      __threadfence();
-    }
-    __syncthreads();
-    uint32_t *count = p.count + ((size_t)g * p.heads + h) * p.tiles + tile;
-    if (tid == 0) s_last = atomicAdd(count, 1u) == (uint32_t)p.splits - 1u;
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    if (tid == 0) *count = 0u;
-    if (on) {
-      const float *first = p.part + qi * p.splits * PF;
-      m = -INFINITY;
-      for (int j = 0; j < p.splits; ++j) m = fmaxf(m, __ldcg(first + (size_t)j * PF + D));
-      l = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = 0.f;
-      for (int j = 0; j < p.splits; ++j) {
-        const float lj = __ldcg(first + (size_t)j * PF + D + 1);
-        if (lj == 0.f) continue;
-        const float f = exp2f(__ldcg(first + (size_t)j * PF + D) - m);
-        l += lj * f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += __ldcg(first + (size_t)j * PF + lane * E + e) * f;
-      }
-    }
-  }
-  if (!on) return;
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    p.out[qi * D + lane * E + e] = bad ? NAN : l == 0.f ? 0.f : acc[e] / l;
-  if (lane == 0) p.lse[qi] = bad ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  for (int e = 0; e < E; ++e) p.out[(size_t)row * D + lane * E + e] = acc[e] * inv;
+  if (lane == 0) p.lse[row] = bad ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <int D, typename T, int MW>
+cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStream_t s) {
+  constexpr int smem = PSmem<D, T, MW>::kTotal;
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(prefix_kernel<D, T, MW>, smem, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(prefix_kernel<D, T, MW>, grid, kThreads, smem, s, a, split_len);
 }
 
 }  // namespace
 
-PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int D, int dtype) {
-  (void)D;
-  (void)dtype;
+// As many key ranges as fill the device twice over (2 CTAs an SM), each a
+// whole number of tiles.
+PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len) {
   PrefixPlan pl;
-  pl.tiles = (seqs + kTile - 1) / kTile;
+  pl.mw = seqs <= 16 ? 1 : seqs <= 32 ? 2 : 4;
+  pl.tiles = (seqs + pl.mw * 16 - 1) / (pl.mw * 16);
   const long long base = (long long)groups * heads * pl.tiles;
-  long long want = (608 + base - 1) / base;  // about four CTAs an SM
-  const long long most = (max_len + 63) / 64;
+  long long want = 304 / base;
+  const long long most = (max_len + kKeys - 1) / kKeys;
+  if (want > kMostSplits) want = kMostSplits;
   if (want > most) want = most;
   if (want < 1) want = 1;
-  pl.split_len = (int)((max_len + want - 1) / want);
+  pl.split_len = (int)(((max_len + want - 1) / want + kKeys - 1) / kKeys * kKeys);
   pl.splits = (max_len + pl.split_len - 1) / pl.split_len;
   return pl;
 }
@@ -127,9 +451,17 @@ cudaError_t launch_prefix(const PrefixArgs &a, const PrefixPlan &pl, int D, int 
                           cudaStream_t s) {
   const long long grid = (long long)a.groups * a.heads * pl.tiles * pl.splits;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  HKV_DISPATCH(D, dtype, return pdl_launch(prefix_kernel<kD, kT>, (int)grid, kThreads, 0, s, a,
-                                           pl.split_len));
-  return cudaErrorInvalidValue;
+  cudaError_t e = cudaErrorInvalidValue;
+  HKV_DISPATCH(D, dtype, {
+    if (pl.mw == 1) e = launch_tiles<kD, kT, 1>(a, (int)grid, pl.split_len, s);
+    else if (pl.mw == 2) e = launch_tiles<kD, kT, 2>(a, (int)grid, pl.split_len, s);
+    else e = launch_tiles<kD, kT, 4>(a, (int)grid, pl.split_len, s);
+  });
+  if (e != cudaSuccess || a.splits == 1) return e;
+  const int rows = a.groups * a.seqs * a.heads;
+  const int blocks = (rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  if (D == 64) return pdl_launch(prefix_join_kernel<64>, blocks, kJoinThreads, 0, s, a, rows);
+  return pdl_launch(prefix_join_kernel<128>, blocks, kJoinThreads, 0, s, a, rows);
 }
 
 }  // namespace hkv

@@ -56,16 +56,16 @@ struct PrefixArgs {
   int groups, max_len, seqs, heads;   // seqs per group
   const void *q;               // [groups * seqs][heads][D]
   float *out, *lse;
-  uint32_t *count;             // arrivals of each (group, head, query tile)
   float *part;                 // [groups * seqs * heads][splits][D + 4]
   int splits, tiles;           // key ranges, query tiles per (group, head)
   float qscale;
 };
 
 struct PrefixPlan {
-  int splits, tiles, split_len;
+  int mw;                        // warps of a CTA along the queries, 16 each
+  int splits, tiles, split_len;  // key ranges, query tiles, keys of a range
 };
-PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int D, int dtype);
+PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len);
 cudaError_t launch_prefix(const PrefixArgs &a, const PrefixPlan &plan, int D, int dtype,
                           cudaStream_t s);
 

@@ -26,8 +26,6 @@
 //    group; a channel uses its own group's two columns.
 // Sums chain over at most 8 (scores) or 2 (output) products in the tensor core
 // and are added in fp32 registers beyond that.
-#include <atomic>
-
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
@@ -561,20 +559,9 @@ namespace {
 template <int D, typename T, int BITS, bool STEP, int STAGES>
 cudaError_t launch(const QAttnArgs &a, int grid, cudaStream_t s) {
   constexpr int smem = Smem<D, BITS, STAGES>::kTotal;
-  static std::atomic<uint64_t> ready{0};  // devices whose limit is set
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(quant_attn_kernel<D, T, BITS, STEP, STAGES>, smem, ready);
   if (e != cudaSuccess) return e;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP, STAGES>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(quant_attn_kernel<D, T, BITS, STEP, STAGES>,
-                               cudaFuncAttributePreferredSharedMemoryCarveout, 100);
-    if (e != cudaSuccess) return e;
-    ready.fetch_or(bit, std::memory_order_release);
-  }
   return pdl_launch(quant_attn_kernel<D, T, BITS, STEP, STAGES>, grid, kThreads, smem, s, a);
 }
 

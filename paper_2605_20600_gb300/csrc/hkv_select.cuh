@@ -7,6 +7,8 @@
 #include <math.h>
 #include <stdlib.h>
 
+#include <atomic>
+
 #include "hkv_device.cuh"
 #include "hkv_kernels.h"
 
@@ -404,6 +406,22 @@ inline cudaError_t pdl_launch(void (*kernel)(KArgs...), int grid, int block, siz
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Raises a kernel's limit of dynamic shared memory to `smem`, with all of an
+// SM's L1 as shared memory, once per device and kernel.
+template <typename... KArgs>
+inline cudaError_t allow_smem_of(void (*kernel)(KArgs...), int smem, std::atomic<uint64_t> &ready) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (ready.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  if (e == cudaSuccess) ready.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 inline size_t update_smem_of(int max_len, int D, int P, int es) {

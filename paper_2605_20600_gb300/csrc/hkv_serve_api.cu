@@ -169,20 +169,15 @@ hkv_status check_prefix(const hkv_config *cfg, const hkv_prefix *p) {
   return HKV_OK;
 }
 
-size_t prefix_counts_bytes(const hkv_config *c, const hkv_prefix *p, const PrefixPlan &pl) {
-  return align256((size_t)p->n_groups * c->n_heads * pl.tiles * sizeof(uint32_t));
-}
-
 PrefixPlan plan_of(const hkv_config *c, const hkv_prefix *p) {
-  return prefix_plan(p->n_groups, c->n_seqs / p->n_groups, c->n_heads, p->max_len, c->head_dim,
-                     c->dtype);
+  return prefix_plan(p->n_groups, c->n_seqs / p->n_groups, c->n_heads, p->max_len);
 }
 
-size_t prefix_ws_bytes(const hkv_config *c, const hkv_prefix *p, const PrefixPlan &pl) {
+size_t prefix_ws_bytes(const hkv_config *c, const PrefixPlan &pl) {
   const size_t parts = pl.splits > 1 ? (size_t)heads_per_layer(c) * pl.splits *
                                            (c->head_dim + 4) * sizeof(float)
                                      : 0;
-  return prefix_counts_bytes(c, p, pl) + align256(parts);
+  return align256(parts) + 256;
 }
 
 }  // namespace
@@ -264,7 +259,7 @@ hkv_status hkv_quant_check(const hkv_qcache *cache, hkv_stream_t stream) {
 
 size_t hkv_prefix_workspace_size(const hkv_config *cfg, const hkv_prefix *prefix) {
   if (!cfg || hkv_validate_config(cfg) != HKV_OK || check_prefix(cfg, prefix) != HKV_OK) return 0;
-  return prefix_ws_bytes(cfg, prefix, plan_of(cfg, prefix));
+  return prefix_ws_bytes(cfg, plan_of(cfg, prefix));
 }
 
 hkv_status hkv_prefix_attention(const hkv_config *cfg, const hkv_prefix *prefix, const void *q,
@@ -276,7 +271,7 @@ hkv_status hkv_prefix_attention(const hkv_config *cfg, const hkv_prefix *prefix,
   if (!q || !out || !lse || !workspace) return HKV_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return HKV_ERR_ALIGN;
   const PrefixPlan pl = plan_of(cfg, prefix);
-  if (ws_bytes < prefix_ws_bytes(cfg, prefix, pl)) return HKV_ERR_CAPACITY;
+  if (ws_bytes < prefix_ws_bytes(cfg, pl)) return HKV_ERR_CAPACITY;
   PrefixArgs a = {};
   a.k = prefix->k;
   a.v = prefix->v;
@@ -292,9 +287,7 @@ hkv_status hkv_prefix_attention(const hkv_config *cfg, const hkv_prefix *prefix,
   a.q = q;
   a.out = out;
   a.lse = lse;
-  unsigned char *ws = static_cast<unsigned char *>(workspace);
-  a.count = reinterpret_cast<uint32_t *>(ws);
-  a.part = reinterpret_cast<float *>(ws + prefix_counts_bytes(cfg, prefix, pl));
+  a.part = static_cast<float *>(workspace);
   a.splits = pl.splits;
   a.tiles = pl.tiles;
   a.qscale = (float)(1.4426950408889634 / sqrt((double)cfg->head_dim));
