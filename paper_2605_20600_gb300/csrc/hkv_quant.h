@@ -37,14 +37,17 @@ struct QAttnArgs {
   const float *prior_out, *prior_lse;     // [nheads][D], [nheads], or both null
   float *out, *lse;                       // [nheads][D], [nheads] or null
   uint32_t *count;             // [nheads] arrivals, zero between launches
-  float *part;                 // [nheads][nchunks][D + 4] partial results
-  int chunk, nchunks;          // rows a CTA takes at most, CTAs per head
+  uint32_t *done;              // [2] CTAs on their way and heads left to the
+                               // last one, zero between launches
+  float *part;                 // [kQuantMaxGrid][2][D + 4] partial results
+  int max_rows;                // rows of the longest segment
+  int sms;
   int P, C, prefetch;
   float qscale;                // log2(e) / sqrt(D)
 };
 
-// rows of a head one CTA attends over at most
-int quant_chunk(int nheads, int max_segment);
+// most CTAs of the attention (the workspace holds two partial results of each)
+constexpr int kQuantMaxGrid = 1024;
 cudaError_t launch_quant_attention(const QAttnArgs &a, int D, int dtype, int bits, cudaStream_t s);
 
 // attention of a batch over shared prompts, one layer

@@ -1,15 +1,19 @@
 // Decode attention over a cache in 8 or 4 bits, with or without the append of
 // the step's new token: one launch per layer.
 //
-// A CTA takes one range of one head's rows; its warps share the range tile by
-// tile (32 rows), each with its own running maximum, sum and accumulator,
-// joined in shared memory at the end. Heads of more than one range leave
-// partial results (accumulator, maximum, sum) in the workspace; the CTA that
-// arrives last at the head's counter joins them in range order (so the result
-// does not depend on who is last), joins the prior, writes the outputs and, in
-// a step, advances the head's counters. Every CTA of a head arrives, whether
-// its range holds rows or not: each reads the head's length, which may change
-// only after all have.
+// The layer's rows, head after head in tiles of 32, are cut into equal runs of
+// tiles, one per warp of a grid that fills the device once. A warp streams its
+// run through its own ring of tiles in shared memory, whatever heads it
+// crosses, with a running maximum, sum and accumulator per head. The part of a
+// head that a warp holds (a piece) is written out at once if it is the whole
+// head. Else the CTA joins its warps' pieces in shared memory, and a head that
+// is cut between CTAs leaves partial results in the workspace: the CTA that
+// arrives last at the head's counter joins them, in CTA order, so the result
+// does not depend on who is last. No CTA waits for another.
+//
+// Every CTA reads the layer's lengths to find its run, so a step may advance a
+// head's counters only when all have: whoever finishes a head advances them if
+// every CTA has reported that, else leaves it to the CTA that exits last.
 //
 // The products run on the tensor cores (mma.sync m16n8k16, fp16 operands, fp32
 // sums), not because one query per head fills them (a sixteenth does) but
@@ -33,12 +37,12 @@
 namespace hkv {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-constexpr int kTile = 32;    // rows a warp handles at a time
+constexpr int kTile = 32;  // rows a warp handles at a time
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kQUp = 4096.f;                               // the query's parts, below 2^13
 constexpr float kLoScale = 2048.f, kLoUnscale = 1.f / 2048.f;  // second parts, 2^11
+constexpr float kRawHi = 0x1p24f / kQUp, kRawLo = kRawHi * kLoUnscale;  // sums of raw codes
 
 __device__ __forceinline__ uint32_t lop_and_or(uint32_t a, uint32_t m, uint32_t o) {
   uint32_t r;
@@ -56,8 +60,22 @@ __device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
   return r;
 }
 
-// fp16 pairs from stored codes, exact. 0x64uu is the fp16 number 1024 + uu.
-// codes8: bytes (0, 2) and (1, 3) of a word, less the bias of 128.
+// Stored codes u as fp16 pairs. raw*: the bits themselves, which read as the
+// subnormal numbers u 2^-24 (an odd nibble sits four bits up: u 2^-20); exact
+// in the tensor core, and the bias is taken off the sum. For the scores.
+__device__ __forceinline__ void raw8(uint32_t w, uint32_t &even, uint32_t &odd) {
+  even = w & 0x00FF00FFu;                     // bytes (0, 2)
+  odd = __byte_perm(w, 0u, 0x4341);           // bytes (1, 3)
+}
+__device__ __forceinline__ void raw4(uint32_t w, uint32_t (&c)[4]) {
+  const uint32_t v = w >> 8;                  // nibbles (0, 4) (1, 5) (2, 6) (3, 7)
+  c[0] = w & 0x000F000Fu;
+  c[1] = w & 0x00F000F0u;
+  c[2] = v & 0x000F000Fu;
+  c[3] = v & 0x00F000F0u;
+}
+// codes*: less the bias, exact. 0x64uu is the fp16 number 1024 + uu. For the
+// output, where the bias would be large beside the sum.
 __device__ __forceinline__ void codes8(uint32_t w, uint32_t &even, uint32_t &odd) {
   constexpr uint32_t kOne = 0x64006400u, kSub = 0xE480E480u;  // 1024, -1152
   even = h2_add(lop_and_or(w, 0x00FF00FFu, kOne), kSub);
@@ -83,6 +101,22 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the first of a chain: c = a b + (e0, e1, e0, e1)
+__device__ __forceinline__ void mma_f16_from(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                             uint32_t a3, uint32_t b0, uint32_t b1, float e0,
+                                             float e1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%10,%11,%10,%11};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(e0), "f"(e1));
+}
+// maximum over the warp
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 
 template <int BYTES>
 __device__ __forceinline__ void cp_async_small(void *dst, const void *src) {
@@ -106,17 +140,28 @@ __device__ __forceinline__ float inv_pow2(float p) {
   return __uint_as_float(0x7F000000u - __float_as_uint(p));
 }
 
-// Shared memory of a warp: STAGES tiles (codes of K and V, scales of K and
-// V), the query's two parts, the weights' B operand.
-template <int D, int BITS, int STAGES>
+// Warps of a CTA and tiles in flight of a warp, two CTAs an SM: as much of an
+// SM's shared memory as goes into whole tiles, or as many warps as registers.
+template <int RB>
+struct Shape {
+  static constexpr int kWarps = RB == 128 ? 6 : 8, kStages = RB == 32 ? 4 : 2;
+};
+
+// Shared memory of a warp: its tiles (codes of K and V, scales of K and V),
+// the B operand being made (the query's two parts, then the weights), and the
+// piece of the head its run starts inside.
+template <int D, int BITS>
 struct Smem {
   using R = QRow<D, BITS>;
+  static constexpr int kWarps = Shape<R::kBytes>::kWarps, kStages = Shape<R::kBytes>::kStages;
   static constexpr int kCodes = kTile * R::kBytes, kScales = kTile * R::kScaleBytes;
   static constexpr int kStage = 2 * (kCodes + kScales);
-  static constexpr int kQ = 2 * D * 2;        // fp16 [2][D]
-  static constexpr int kW = 8 * kTile * 2;    // fp16 [8][kTile]
-  static constexpr int kWarp = STAGES * kStage + kQ + kW;
+  static constexpr int kOperand = kStages * kStage;      // fp16 [2][D], [8][kTile]
+  static constexpr int kPiece = kOperand + 512;          // fp32 [D]
+  static constexpr int kWarp = kPiece + D * 4;
   static constexpr int kTotal = kWarps * kWarp;
+  static_assert(2 * D * 2 <= 512 && 8 * kTile * 2 <= 512, "one operand at a time");
+  static_assert(kStage >= D * 4, "the last piece takes a tile's place");
 };
 
 // Byte offset of the 16-byte piece `c` of row `r` in a tile: rows lie back to
@@ -128,462 +173,668 @@ __device__ __forceinline__ int piece_at(int r, int c) {
   return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
 }
 
-// STAGES = 1: every warp has at most one tile (ranges of at most kThreads
-// rows); more: it walks through its tiles, that many of them in flight.
-template <int D, typename T, int BITS, bool STEP, int STAGES>
-__global__ void __launch_bounds__(kThreads, STAGES == 1 ? 6 : 4)
+// A head as its tiles see it.
+struct HeadRef {
+  long long off;
+  int len, n, tiles;   // old rows, rows to attend over, tiles (at least one)
+  uint32_t bad;        // status of a head that cannot be served
+  bool dense;
+};
+
+// Tiles of a head of `len` rows: one at least, so that some warp reports,
+// or writes the outputs of an empty head.
+template <bool STEP>
+__device__ __forceinline__ int head_tiles(int len, int max_rows) {
+  const int n = len + (STEP ? 1 : 0);
+  return n <= 0 || n > max_rows || len < 0 ? 1 : (n + kTile - 1) / kTile;
+}
+
+template <bool STEP>
+__device__ __forceinline__ HeadRef head_ref(const QAttnArgs &p, int hl) {
+  const CacheArgs &c = p.q8.c;
+  const int i = p.base + hl;
+  HeadRef r;
+  r.off = c.off[i];
+  r.len = c.len[i];
+  const int cap = c.cap[i];
+  r.n = r.len + (STEP ? 1 : 0);
+  r.tiles = head_tiles<STEP>(r.len, p.max_rows);
+  r.bad = 0;
+  r.dense = STEP ? c.label[i] == HKV_DENSE : false;
+  if (r.off < 0 || cap < 0 || r.off + cap > c.arena_tokens || r.len < 0 || r.len > cap)
+    r.bad = HKV_ERR_BOUNDS;
+  else if (STEP && !r.dense && c.nbuf[i] >= p.P)
+    r.bad = HKV_ERR_STATE;
+  else if (r.n > cap || r.n > p.max_rows)
+    r.bad = HKV_ERR_CAPACITY;
+  return r;
+}
+
+// A head's result, channels lane * E .. of the unnormalised output: joined
+// with the prior, normalised and written. The whole warp calls.
+template <int D>
+__device__ __forceinline__ void finish_head(const QAttnArgs &p, int hl, float m, float l,
+                                            float (&o)[D / 32]) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  if (p.prior_lse) {
+    const float pm = p.prior_lse[hl] * kLog2e;
+    if (!(pm == -INFINITY)) {  // an empty prior's outputs are not looked at
+      const float mn = fmaxf(m, pm);
+      const float f = l == 0.f ? 0.f : ex2_approx(m - mn), w = ex2_approx(pm - mn);
+      l = l * f + w;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        o[e] = o[e] * f + w * p.prior_out[(size_t)hl * D + lane * E + e];
+      m = mn;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) p.out[(size_t)hl * D + lane * E + e] = o[e] * inv;
+  if (p.lse && lane == 0) p.lse[hl] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// A finished head's counters advance (a step), now or by the CTA that exits
+// last. done[0]: CTAs that have read the lengths (low half) and exited (high
+// half); done[1]: heads left to the last; kLater marks them in count[].
+constexpr uint32_t kLater = 0x80000000u;
+__device__ __forceinline__ void advance_head(const QAttnArgs &p, int hl, bool dense) {
+  const CacheArgs &c = p.q8.c;
+  const int i = p.base + hl;
+  atomicAdd(c.len + i, 1);
+  atomicAdd(c.ntok + i, 1);
+  if (!dense) atomicAdd(c.nbuf + i, 1);
+}
+__device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense) {
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.done) : "memory");
+  if ((v & 0xFFFFu) == gridDim.x) {
+    advance_head(p, hl, dense);
+  } else {
+    p.count[hl] = kLater;
+    atomicAdd(p.done + 1, 1u);
+    __threadfence();
+  }
+}
+
+// Adds a piece (maximum pm, sum pl, channels at src) to (m, l, o).
+template <int E>
+__device__ __forceinline__ void add_piece(float &m, float &l, float (&o)[E], float pm, float pl,
+                                          const float *src) {
+  const float mn = fmaxf(m, pm);
+  const float f = l == 0.f ? 0.f : ex2_approx(m - mn), g = pl == 0.f ? 0.f : ex2_approx(pm - mn);
+  m = mn;
+  l = l * f + pl * g;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = o[e] * f + src[e] * g;
+}
+
+template <int D, typename T, int BITS, bool STEP>
+__global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
     quant_attn_kernel(const QAttnArgs p) {
   using R = QRow<D, BITS>;
-  using SM = Smem<D, BITS, STAGES>;
-  constexpr int RB = R::kBytes, SB = R::kScaleBytes, G = R::kGroups;
+  using SM = Smem<D, BITS>;
+  constexpr int RB = R::kBytes, SB = R::kScaleBytes, G = R::kGroups, E = D / 32;
+  constexpr int WARPS = SM::kWarps, STAGES = SM::kStages, THREADS = WARPS * 32;
   constexpr int PF = D + 4;          // floats of a partial result
   constexpr int KM = D / 16;         // products per 16 rows, scores and output alike
+  constexpr float kRawBias = R::kBias * 0x1p-24f;  // of a code read as a subnormal
   extern __shared__ __align__(16) unsigned char dyn[];
-  __shared__ float s_acc[kWarps][D];
-  __shared__ float s_m[kWarps], s_l[kWarps];
-  __shared__ float s_factor[kThreads];
-  __shared__ int s_last;
+  // the runs' first heads, and those heads' first tiles in the layer
+  __shared__ int s_head[WARPS], s_base[WARPS], s_scan[33];
+  // pieces of heads that a warp does not hold whole: [0] its run starts inside
+  // the head, [1] the head starts in its run
+  __shared__ float s_m[WARPS][2], s_l[WARPS][2];
+  __shared__ int s_piece[WARPS][2];  // head, -1 for none
+  __shared__ int s_ends[WARPS][2];   // whether the head ends with the piece
+  __shared__ int s_first[WARPS][2], s_tiles[WARPS][2];  // the head's first tile and tiles
+  __shared__ uint32_t s_later;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row8 = lane >> 2, quad = lane & 3;
-  const int hl = (int)(blockIdx.x % p.nheads), ch = (int)(blockIdx.x / p.nheads);
-  const int i = p.base + hl;
   const CacheArgs &c = p.q8.c;
   if (!p.prefetch) pdl_wait();
-  const int len = c.len[i], cap = c.cap[i];
-  const long long off = c.off[i];
-  const uint8_t lab = c.label[i];
-  const int ntok = STEP ? c.ntok[i] : 0, nbuf = STEP ? c.nbuf[i] : 0;
-  const int n = len + (STEP ? 1 : 0);
-  uint32_t bad = 0;
-  if (off < 0 || cap < 0 || off + cap > c.arena_tokens || len < 0 || len > cap)
-    bad = HKV_ERR_BOUNDS;
-  else if (STEP && lab != HKV_DENSE && nbuf >= p.P)
-    bad = HKV_ERR_STATE;
-  else if (n > cap || n > (long long)p.nchunks * p.chunk)
-    bad = HKV_ERR_CAPACITY;
-  if (bad) {  // the same for every CTA of the head
-    pdl_wait();
-    pdl_launch_dependents();
-    if (ch == 0 && tid == 0) set_err(c.err, bad);
-    return;
+
+  // the runs: an exclusive scan of the heads' tiles, a stretch of heads a
+  // thread; each warp gets `share` tiles, the first `rest` warps one more
+  const int hp = (p.nheads + THREADS - 1) / THREADS;
+  const int h0 = min(tid * hp, p.nheads), h1 = min(h0 + hp, p.nheads);
+  const int len0 = h0 < h1 ? c.len[p.base + h0] : 0;
+  int mine = h0 < h1 ? head_tiles<STEP>(len0, p.max_rows) : 0;
+  for (int h = h0 + 1; h < h1; ++h) mine += head_tiles<STEP>(c.len[p.base + h], p.max_rows);
+  int total;
+  const int before = block_excl_scan<int>(mine, s_scan, &total);
+  const int ctas = min((int)gridDim.x, (total + WARPS - 1) / WARPS);
+  const int share = total / (ctas * WARPS), rest = total - share * ctas * WARPS;
+  const int cta = blockIdx.x;
+  auto run_start = [&](int w) { return w * share + min(w, rest); };
+  const int run0 = run_start(cta * WARPS + warp);
+  int left = cta < ctas ? run_start(cta * WARPS + warp + 1) - run0 : 0;
+  if (cta < ctas) {
+    if (tid < WARPS * 2) s_piece[tid >> 1][tid & 1] = -1;
+#pragma unroll 1
+    for (int w = 0; w < WARPS; ++w) {
+      const int t = run_start(cta * WARPS + w);
+      if (t >= before && t < before + mine) {
+        int at = before, h = h0;
+        if (h1 - h0 > 1) {
+          for (; h < h1 - 1; ++h) {
+            const int nt = head_tiles<STEP>(c.len[p.base + h], p.max_rows);
+            if (t < at + nt) break;
+            at += nt;
+          }
+        }
+        s_head[w] = h;
+        s_base[w] = at;
+      }
+    }
+    __syncthreads();
   }
-  unsigned char *K = static_cast<unsigned char *>(c.K) + off * RB;
-  unsigned char *V = static_cast<unsigned char *>(c.V) + off * RB;
-  unsigned char *KS = static_cast<unsigned char *>(p.q8.ks) + off * SB;
-  unsigned char *VS = static_cast<unsigned char *>(p.q8.vs) + off * SB;
-  // the head's rows in equal ranges of whole tiles, one per CTA
-  const int na = n > 0 ? (n + p.chunk - 1) / p.chunk : 1;
-  const int per = n > 0 ? ((n + na - 1) / na + kTile - 1) / kTile * kTile : kTile;
-  const int lo = ch * per, hi = min(n, lo + per);
-  const bool active = ch == 0 || lo < n;
   unsigned char *ws = dyn + warp * SM::kWarp;
 
-  // rows [r0, r0 + kTile) of the range into stage st: the old rows among them
-  auto load_tile = [&](int r0, int st) {
-    const int rows = min(kTile, min(hi, len) - r0);
-    unsigned char *sk = ws + st * SM::kStage, *sv = sk + SM::kCodes;
-    unsigned char *ss = sv + SM::kCodes;
+  // the ring: tiles of the run in order, old rows only
+  int pl_left = left, pl_head = 0, pl_tile = 0, pl_st = 0;
+  HeadRef pr = {};
+  const int my_at = piece_at<RB>(lane / (RB / 16), lane % (RB / 16));
+  if (left > 0) {
+    pl_head = s_head[warp];
+    pl_tile = run0 - s_base[warp];
+    pr = head_ref<STEP>(p, pl_head);
+  }
+  auto issue = [&]() {
+    if (pl_left > 0) {
+      const int r0 = pl_tile * kTile;
+      const int rows = pr.bad ? 0 : min(kTile, pr.len - r0);
+      unsigned char *sk = ws + pl_st * SM::kStage, *sv = sk + SM::kCodes;
+      unsigned char *ss = sv + SM::kCodes;
+      // the tile's codes are one stretch of the arena: lane e of each 512 bytes
+      // takes piece e; its place in the tile moves by whole rows from one to
+      // the next, which flips one swizzle bit at 128-byte rows
+      const size_t src = (size_t)(pr.off + r0) * RB + lane * 16;
+      const unsigned char *K = static_cast<const unsigned char *>(c.K) + src;
+      const unsigned char *V = static_cast<const unsigned char *>(c.V) + src;
+      const int pieces = rows * (RB / 16) - lane;
 #pragma unroll
-    for (int e = lane; e < kTile * (RB / 16); e += 32) {
-      const int r = e / (RB / 16), pc = e % (RB / 16);
-      if (r < rows) {
-        const size_t src = (size_t)(r0 + r) * RB + pc * 16;
-        cp_async16(sk + piece_at<RB>(r, pc), K + src);
-        cp_async16(sv + piece_at<RB>(r, pc), V + src);
+      for (int e = 0; e < RB / 16; ++e) {
+        const int at = (RB == 128 && (e & 1) ? my_at ^ 64 : my_at) + e * 512;
+        if (e * 32 < pieces) {
+          cp_async16(sk + at, K + e * 512);
+          cp_async16(sv + at, V + e * 512);
+        }
+      }
+      if (lane < rows) {
+        cp_async_small<SB>(ss + lane * SB, static_cast<const unsigned char *>(p.q8.ks) +
+                                               (pr.off + r0 + lane) * SB);
+        cp_async_small<SB>(ss + SM::kScales + lane * SB,
+                           static_cast<const unsigned char *>(p.q8.vs) + (pr.off + r0 + lane) * SB);
+      }
+      ++pl_tile;
+      --pl_left;
+      if (pl_tile == pr.tiles && pl_left > 0) {
+        pl_tile = 0;
+        pr = head_ref<STEP>(p, ++pl_head);
       }
     }
-    if (lane < rows) {
-      cp_async_small<SB>(ss + lane * SB, KS + (size_t)(r0 + lane) * SB);
-      cp_async_small<SB>(ss + SM::kScales + lane * SB, VS + (size_t)(r0 + lane) * SB);
-    }
-  };
-  const int first = lo + warp * kTile;
-#pragma unroll
-  for (int st = 0; st < STAGES; ++st) {
-    const int r0 = first + st * kWarps * kTile;
-    if (r0 < hi) load_tile(r0, st);
     cp_async_commit();
-  }
+    pl_st = pl_st + 1 == STAGES ? 0 : pl_st + 1;
+  };
+#pragma unroll
+  for (int st = 0; st < STAGES; ++st) issue();
   if (p.prefetch) pdl_wait();  // the step's inputs are visible from here on
   pdl_launch_dependents();
+  // this CTA's runs are found (the barrier above): it has read the lengths
+  if (STEP && tid == 0) atomicAdd(p.done, 1u);
 
-  float m = -INFINITY, l = 0.f;
-  float acc[KM][2];
+  if (left > 0) {
+    int hl = s_head[warp], base = s_base[warp], tile = run0 - base, st = 0;
+    HeadRef hd = head_ref<STEP>(p, hl), nx = hd;
+    float qv[E], qn[E];  // this head's query, the next one's
+    auto fetch_q = [&](int h, float (&q)[E]) {
 #pragma unroll
-  for (int x = 0; x < KM; ++x) acc[x][0] = acc[x][1] = 0.f;
-  if (first < hi) {
-    // the query over a power of two, in two fp16 parts, in the order in which
-    // the codes of a word come out in pairs
-    constexpr int E = D / 32;
-    float qv[E];
-    uint32_t qm = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      qv[e] = (float)static_cast<const T *>(p.q)[(size_t)hl * D + lane * E + e];
-      qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
-    }
-    const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
-    const float xscale = q2 * p.qscale;
-    __half *sq = reinterpret_cast<__half *>(ws + STAGES * SM::kStage);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int d = lane * E + e;
-      const int at = BITS == 8 ? (d & ~3) + ((d & 1) << 1) + ((d >> 1) & 1)
-                               : (d & ~7) + ((d & 3) << 1) + ((d >> 2) & 1);
-      const float x = qv[e] * qi;
-      const __half h = __float2half_rn(x);
-      sq[at] = h;
-      sq[D + at] = __float2half_rn((x - __half2float(h)) * kLoScale);
-    }
-    __syncwarp();
-    // B operand of the scores: this lane's column is part (row8 & 1) of group
-    // row8 / 2, its channels those of the lanes `quad` of the A operand
-    uint32_t qf[KM][2];
-    {
-      const uint4 *src = reinterpret_cast<const uint4 *>(sq + (row8 & 1) * D + quad * (D / 4));
-      const bool mine = (row8 >> 1) == quad * (D / 4) / 32;
-#pragma unroll
-      for (int x = 0; x < KM / 2; ++x) {
-        const uint4 u = mine ? src[x] : make_uint4(0u, 0u, 0u, 0u);
-        qf[2 * x][0] = u.x;
-        qf[2 * x][1] = u.y;
-        qf[2 * x + 1][0] = u.z;
-        qf[2 * x + 1][1] = u.w;
-      }
-    }
-    __half *sw = reinterpret_cast<__half *>(ws + STAGES * SM::kStage + SM::kQ);
+      for (int e = 0; e < E; ++e)
+        q[e] = (float)static_cast<const T *>(p.q)[(size_t)h * D + lane * E + e];
+    };
+    fetch_q(hl, qn);
+    __half *sq = reinterpret_cast<__half *>(ws + SM::kOperand), *sw = sq;
     // where this lane's row (row8 + 8 quad) sits in the weights' columns
     const int own = row8 + 8 * quad;
     const int own_at = ((own >> 1) & 3) * 8 + (own >> 4) * 4 + ((own >> 3) & 1) * 2 + (own & 1);
 
-    int st = 0;
-    for (int r0 = first; r0 < hi; r0 += kWarps * kTile) {
-      cp_async_wait<STAGES - 1>();
+    while (left > 0) {
+      // a head: this warp's piece of it
+      const int from = tile;
+      const int i = p.base + hl;
+      const bool more = left > hd.tiles - tile;  // another head follows in the run
+#pragma unroll
+      for (int e = 0; e < E; ++e) qv[e] = qn[e];
+      if (more) {
+        nx = head_ref<STEP>(p, hl + 1);
+        fetch_q(hl + 1, qn);
+      }
+      if (hd.bad && tile == 0 && lane == 0) set_err(c.err, hd.bad);
+      // the query over a power of two, in two fp16 parts, in the order in which
+      // the codes of a word come out in pairs
+      uint32_t qm = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
+      const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
+      const float xscale = q2 * p.qscale;
+      float sum_hi = 0.f, sum_lo = 0.f;  // of the lane's channels' parts
       __syncwarp();
-      unsigned char *sk = ws + st * SM::kStage, *sv = sk + SM::kCodes;
-      unsigned char *ss = sv + SM::kCodes;
-      const int rows = min(kTile, hi - r0);
-      if (STEP && len - r0 < kTile && len < hi && len >= r0) {
-        // the new row: quantised into the arena and into the tile
-        if (lane < D / 4) {
-          constexpr int TPR = D / 8;
-          const int kv = lane / TPR, col = lane % TPR, r = len - r0;
-          float x[8];
-          load8<T>(static_cast<const T *>(kv ? p.v_new : p.k_new) + (size_t)hl * D + col * 8, x);
-          uint32_t a, b;
-          const uint32_t sb = quant_group<BITS>(x, 0xFu << (lane & 28), a, b);
-          unsigned char *row = (kv ? V : K) + (size_t)len * RB;
-          unsigned char *tile = kv ? sv : sk;
-          if (BITS == 8) {
-            reinterpret_cast<uint2 *>(row)[col] = make_uint2(a, b);
-            *reinterpret_cast<uint2 *>(tile + piece_at<RB>(r, col >> 1) + (col & 1) * 8) =
-                make_uint2(a, b);
-          } else {
-            reinterpret_cast<uint32_t *>(row)[col] = a;
-            *reinterpret_cast<uint32_t *>(tile + piece_at<RB>(r, col >> 2) + (col & 3) * 4) = a;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = lane * E + e;
+        const int at = BITS == 8 ? (d & ~3) + ((d & 1) << 1) + ((d >> 1) & 1)
+                                 : (d & ~7) + ((d & 3) << 1) + ((d >> 2) & 1);
+        // the channels whose codes sit four bits up are taken down by that
+        const float up = BITS == 4 && (e & 1) ? 16.f : 1.f;
+        const float x = qv[e] * qi * (kQUp / up);
+        const __half h = __float2half_rn(x);
+        const __half lo = __float2half_rn((x - __half2float(h)) * kLoScale);
+        sq[at] = h;
+        sq[D + at] = lo;
+        sum_hi += __half2float(h) * up;
+        sum_lo += __half2float(lo) * up;
+      }
+#pragma unroll
+      for (int o = 1; o < 32 / E; o <<= 1) {  // over the lanes of a group
+        sum_hi += __shfl_xor_sync(0xFFFFFFFFu, sum_hi, o);
+        sum_lo += __shfl_xor_sync(0xFFFFFFFFu, sum_lo, o);
+      }
+      // what the codes' bias adds to this lane's two columns (group `quad`)
+      float bias_hi = __shfl_sync(0xFFFFFFFFu, sum_hi, (quad * 32 / E) & 31) * -kRawBias;
+      float bias_lo = __shfl_sync(0xFFFFFFFFu, sum_lo, (quad * 32 / E) & 31) * -kRawBias;
+      if (quad >= G) bias_hi = bias_lo = 0.f;
+      __syncwarp();
+      // B operand of the scores: this lane's column is part (row8 & 1) of group
+      // row8 / 2, its channels those of the lanes `quad` of the A operand
+      uint32_t qf[KM][2];
+      {
+        const uint4 *src = reinterpret_cast<const uint4 *>(sq + (row8 & 1) * D + quad * (D / 4));
+        const bool in_group = (row8 >> 1) == quad * (D / 4) / 32;
+#pragma unroll
+        for (int x = 0; x < KM / 2; ++x) {
+          const uint4 u = in_group ? src[x] : make_uint4(0u, 0u, 0u, 0u);
+          qf[2 * x][0] = u.x;
+          qf[2 * x][1] = u.y;
+          qf[2 * x + 1][0] = u.z;
+          qf[2 * x + 1][1] = u.w;
+        }
+      }
+      float m = -INFINITY, l = 0.f;
+      float acc[KM][2];
+#pragma unroll
+      for (int x = 0; x < KM; ++x) acc[x][0] = acc[x][1] = 0.f;
+      __syncwarp();  // the weights take the query's place
+
+      for (; tile < hd.tiles && left > 0; ++tile, --left) {
+        cp_async_wait<STAGES - 1>();
+        __syncwarp();
+        unsigned char *sk = ws + st * SM::kStage, *sv = sk + SM::kCodes;
+        unsigned char *ss = sv + SM::kCodes;
+        const int r0 = tile * kTile;
+        const int rows = hd.bad ? 0 : min(kTile, hd.n - r0);
+        if (STEP && hd.len - r0 < rows && rows > 0 && hd.len >= r0) {
+          // the new row: quantised into the arena and into the tile
+          const int ntok = c.ntok[i];
+          if (lane < D / 4) {
+            constexpr int TPR = D / 8;
+            const int kv = lane / TPR, col = lane % TPR, r = hd.len - r0;
+            float x[8];
+            load8<T>(static_cast<const T *>(kv ? p.v_new : p.k_new) + (size_t)hl * D + col * 8, x);
+            uint32_t a, b;
+            const uint32_t sb = quant_group<BITS>(x, 0xFu << (lane & 28), a, b);
+            const size_t at = (size_t)(hd.off + hd.len);
+            unsigned char *row = static_cast<unsigned char *>(kv ? c.V : c.K) + at * RB;
+            unsigned char *to = kv ? sv : sk;
+            if (BITS == 8) {
+              reinterpret_cast<uint2 *>(row)[col] = make_uint2(a, b);
+              *reinterpret_cast<uint2 *>(to + piece_at<RB>(r, col >> 1) + (col & 1) * 8) =
+                  make_uint2(a, b);
+            } else {
+              reinterpret_cast<uint32_t *>(row)[col] = a;
+              *reinterpret_cast<uint32_t *>(to + piece_at<RB>(r, col >> 2) + (col & 3) * 4) = a;
+            }
+            if ((col & 3) == 0) {
+              static_cast<uint16_t *>(kv ? p.q8.vs : p.q8.ks)[at * G + col / 4] = (uint16_t)sb;
+              reinterpret_cast<uint16_t *>(ss + kv * SM::kScales + r * SB)[col / 4] = (uint16_t)sb;
+            }
           }
-          if ((col & 3) == 0) {
-            reinterpret_cast<uint16_t *>((kv ? VS : KS) + (size_t)len * SB)[col / 4] = (uint16_t)sb;
-            reinterpret_cast<uint16_t *>(ss + kv * SM::kScales + r * SB)[col / 4] = (uint16_t)sb;
+          T *ring = static_cast<T *>(c.qbuf) + ((size_t)i * p.P + ntok % p.P) * D;
+#pragma unroll
+          for (int e = 0; e < E; ++e) ring[lane * E + e] = (T)qv[e];
+          if (lane == 0) c.pos[hd.off + hd.len] = p.C + ntok;
+          __syncwarp();
+        }
+        if (rows > 0) {
+          // scores: x[b2] is the sum of row row8 + 8 b2 over this lane's group
+          float xs[4];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int ra = b * 16 + row8, rb = ra + 8;
+            float s[4];
+            uint32_t wa[RB / 16], wb[RB / 16];  // this lane's quarter of the two rows
+            if (RB == 128) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, 2 * quad + h));
+                const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, 2 * quad + h));
+                wa[h * 4] = ua.x, wa[h * 4 + 1] = ua.y, wa[h * 4 + 2] = ua.z, wa[h * 4 + 3] = ua.w;
+                wb[h * 4] = ub.x, wb[h * 4 + 1] = ub.y, wb[h * 4 + 2] = ub.z, wb[h * 4 + 3] = ub.w;
+              }
+            } else if (RB == 64) {
+              const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, quad));
+              const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, quad));
+              wa[0] = ua.x, wa[1] = ua.y, wa[2] = ua.z, wa[3] = ua.w;
+              wb[0] = ub.x, wb[1] = ub.y, wb[2] = ub.z, wb[3] = ub.w;
+            } else {
+              const uint2 ua = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(ra, quad >> 1) +
+                                                                (quad & 1) * 8);
+              const uint2 ub = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(rb, quad >> 1) +
+                                                                (quad & 1) * 8);
+              wa[0] = ua.x, wa[1] = ua.y;
+              wb[0] = ub.x, wb[1] = ub.y;
+            }
+#pragma unroll
+            for (int w = 0; w < RB / 16; ++w) {
+              if (BITS == 8) {
+                uint32_t a0, a1, a2, a3;
+                raw8(wa[w], a0, a2);
+                raw8(wb[w], a1, a3);
+                if (w == 0) mma_f16_from(s, a0, a1, a2, a3, qf[0][0], qf[0][1], bias_hi, bias_lo);
+                else mma_f16(s, a0, a1, a2, a3, qf[w][0], qf[w][1]);
+              } else {
+                uint32_t ca[4], cb[4];
+                raw4(wa[w], ca);
+                raw4(wb[w], cb);
+                if (w == 0)
+                  mma_f16_from(s, ca[0], cb[0], ca[1], cb[1], qf[0][0], qf[0][1], bias_hi, bias_lo);
+                else
+                  mma_f16(s, ca[0], cb[0], ca[1], cb[1], qf[2 * w][0], qf[2 * w][1]);
+                mma_f16(s, ca[2], cb[2], ca[3], cb[3], qf[2 * w + 1][0], qf[2 * w + 1][1]);
+              }
+            }
+            const uint16_t *sc = reinterpret_cast<const uint16_t *>(ss);
+            const bool grp = quad < G;  // the columns beyond the groups are empty
+            const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) : 0.f;
+            const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) : 0.f;
+            xs[2 * b] = fa * fmaf(s[1], kRawLo, s[0] * kRawHi);
+            xs[2 * b + 1] = fb * fmaf(s[3], kRawLo, s[2] * kRawHi);
           }
+          // sums over the groups: lane (row8, quad) ends up with row row8 + 8 quad
+          const bool b0 = quad & 1, b1 = quad & 2;
+          float k0 = (b0 ? xs[1] : xs[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[0] : xs[1], 1);
+          float k1 = (b0 ? xs[3] : xs[2]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[2] : xs[3], 1);
+          float x = (b1 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? k0 : k1, 2);
+          const bool on = own < rows;
+          x = on ? x * xscale : -INFINITY;
+
+          const float mt = warp_max(x);
+          if (mt > m) {  // the same for the whole warp
+            const float f = ex2_approx(m - mt);
+            m = mt;
+            l *= f;
+#pragma unroll
+            for (int y = 0; y < KM; ++y) {
+              acc[y][0] *= f;
+              acc[y][1] *= f;
+            }
+          }
+          const float w = on ? ex2_approx(x - m) : 0.f;
+          l += w;
+
+          // weights times scales, over the power of two of the tile's largest
+          // scale of the group, in two parts
+          float unit = 1.f;  // of group `quad`
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const uint32_t sb =
+                on ? reinterpret_cast<const uint16_t *>(ss + SM::kScales)[own * G + g] : 0u;
+            const float u = pow2_of(__reduce_max_sync(0xFFFFFFFFu, sb << 16));
+            if (quad == g) unit = u;
+            const float y = on ? w * (bf16_bits_to_float(sb) * inv_pow2(u)) : 0.f;
+            const __half h = __float2half_rn(y);
+            sw[(2 * g) * kTile + own_at] = h;
+            sw[(2 * g + 1) * kTile + own_at] = __float2half_rn((y - __half2float(h)) * kLoScale);
+          }
+          __syncwarp();
+          // B operand: this lane's column row8, rows 2 quad, + 1, + 8, + 9 of each half
+          uint4 wf = make_uint4(0u, 0u, 0u, 0u);
+          if (row8 < 2 * G) wf = *reinterpret_cast<const uint4 *>(sw + row8 * kTile + quad * 8);
+
+          // output: this lane's channels [row8 D / 8, + D / 8), two per product
+          constexpr int VW = D * BITS / 256;  // words of the lane's channels in a row
+          float o[KM][4];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t vw[4][VW];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = b * 16 + 2 * quad + (e & 1) + (e >> 1) * 8;
+              if (VW == 4) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(sv + piece_at<RB>(r, row8));
+                vw[e][0] = u.x, vw[e][1] = u.y, vw[e][2] = u.z, vw[e][3] = u.w;
+              } else if (VW == 2) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(sv + piece_at<RB>(r, row8 >> 1) +
+                                                                 (row8 & 1) * 8);
+                vw[e][0] = u.x, vw[e][1] = u.y;
+              } else {
+                vw[e][0] = *reinterpret_cast<const uint32_t *>(sv + piece_at<RB>(r, row8 >> 2) +
+                                                               (row8 & 3) * 4);
+              }
+            }
+            const uint32_t bw0 = b ? wf.z : wf.x, bw1 = b ? wf.w : wf.y;
+#pragma unroll
+            for (int w2 = 0; w2 < VW; ++w2) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t sel = h ? 0x7632 : 0x5410;
+                const uint32_t v01 = __byte_perm(vw[0][w2], vw[1][w2], sel);
+                const uint32_t v23 = __byte_perm(vw[2][w2], vw[3][w2], sel);
+                if (BITS == 8) {
+                  uint32_t a0, a1, a2, a3;
+                  codes8(v01, a0, a1);
+                  codes8(v23, a2, a3);
+                  if (b == 0) mma_f16_from(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1, 0.f, 0.f);
+                  else mma_f16(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1);
+                } else {
+                  uint32_t ca[4], cb[4];
+                  codes4(v01, ca);
+                  codes4(v23, cb);
+                  if (b == 0) {
+                    mma_f16_from(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1, 0.f, 0.f);
+                    mma_f16_from(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1, 0.f,
+                                 0.f);
+                  } else {
+                    mma_f16(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1);
+                    mma_f16(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1);
+                  }
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < KM; ++y) {
+            acc[y][0] = fmaf(fmaf(o[y][1], kLoUnscale, o[y][0]), unit, acc[y][0]);
+            acc[y][1] = fmaf(fmaf(o[y][3], kLoUnscale, o[y][2]), unit, acc[y][1]);
+          }
+        }
+        __syncwarp();  // the stage and the weights are rewritten from here on
+        issue();
+        st = st + 1 == STAGES ? 0 : st + 1;
+      }
+      // the piece: [from, tile) of the head's tiles
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+      if (!hd.bad) {
+        const bool starts = from == 0, ends = tile == hd.tiles;
+        // a piece that outlives the head is the run's last unless the run
+        // started inside it: the ring has no tile in flight by then
+        float *to = reinterpret_cast<float *>(starts ? ws : ws + SM::kPiece);
+        if (starts && ends) to = reinterpret_cast<float *>(ws + SM::kOperand);
+        // the lanes whose columns are their channels' group hold the output
+        if (quad == row8 * (D / 8) / 32) {
+#pragma unroll
+          for (int y = 0; y < KM; ++y)
+            *reinterpret_cast<float2 *>(to + row8 * (D / 8) + 2 * y) =
+                make_float2(acc[y][0], acc[y][1]);
+        }
+        __syncwarp();
+        if (starts && ends) {
+          float o[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = to[lane * E + e];
+          finish_head<D>(p, hl, m, l, o);
+          if (STEP && lane == 0) advance_or_leave(p, hl, hd.dense);
+        } else if (lane == 0) {
+          const int slot = starts ? 1 : 0;
+          s_m[warp][slot] = m;
+          s_l[warp][slot] = l;
+          s_piece[warp][slot] = hl;
+          s_ends[warp][slot] = ends;
+          s_first[warp][slot] = base;
+          s_tiles[warp][slot] = hd.tiles;
         }
         __syncwarp();
       }
-
-      // scores: x[b2] is the sum of row row8 + 8 b2 over this lane's group
-      float xs[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int ra = b * 16 + row8, rb = ra + 8;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t wa[RB / 16], wb[RB / 16];  // this lane's quarter of the two rows
-        if (RB == 128) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, 2 * quad + h));
-            const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, 2 * quad + h));
-            wa[h * 4] = ua.x, wa[h * 4 + 1] = ua.y, wa[h * 4 + 2] = ua.z, wa[h * 4 + 3] = ua.w;
-            wb[h * 4] = ub.x, wb[h * 4 + 1] = ub.y, wb[h * 4 + 2] = ub.z, wb[h * 4 + 3] = ub.w;
-          }
-        } else if (RB == 64) {
-          const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, quad));
-          const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, quad));
-          wa[0] = ua.x, wa[1] = ua.y, wa[2] = ua.z, wa[3] = ua.w;
-          wb[0] = ub.x, wb[1] = ub.y, wb[2] = ub.z, wb[3] = ub.w;
-        } else {
-          const uint2 ua = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(ra, quad >> 1) +
-                                                            (quad & 1) * 8);
-          const uint2 ub = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(rb, quad >> 1) +
-                                                            (quad & 1) * 8);
-          wa[0] = ua.x, wa[1] = ua.y;
-          wb[0] = ub.x, wb[1] = ub.y;
-        }
-#pragma unroll
-        for (int w = 0; w < RB / 16; ++w) {
-          if (BITS == 8) {
-            uint32_t a0, a1, a2, a3;
-            codes8(wa[w], a0, a2);
-            codes8(wb[w], a1, a3);
-            mma_f16(s, a0, a1, a2, a3, qf[w][0], qf[w][1]);
-          } else {
-            uint32_t ca[4], cb[4];
-            codes4(wa[w], ca);
-            codes4(wb[w], cb);
-            mma_f16(s, ca[0], cb[0], ca[1], cb[1], qf[2 * w][0], qf[2 * w][1]);
-            mma_f16(s, ca[2], cb[2], ca[3], cb[3], qf[2 * w + 1][0], qf[2 * w + 1][1]);
-          }
-        }
-        const uint16_t *sc = reinterpret_cast<const uint16_t *>(ss);
-        const bool grp = quad < G;  // the columns beyond the groups are empty
-        const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) : 0.f;
-        const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) : 0.f;
-        xs[2 * b] = fa * fmaf(s[1], kLoUnscale, s[0]);
-        xs[2 * b + 1] = fb * fmaf(s[3], kLoUnscale, s[2]);
-      }
-      // sums over the groups: lane (row8, quad) ends up with row row8 + 8 quad
-      const bool b0 = quad & 1, b1 = quad & 2;
-      float k0 = (b0 ? xs[1] : xs[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[0] : xs[1], 1);
-      float k1 = (b0 ? xs[3] : xs[2]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[2] : xs[3], 1);
-      float x = (b1 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? k0 : k1, 2);
-      const bool on = own < rows;
-      x = on ? x * xscale : -INFINITY;
-
-      float mt = x;
-#pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, o));
-      if (STAGES == 1) {
-        m = mt;
-      } else if (mt > m) {  // the same for the whole warp
-        const float f = ex2_approx(m - mt);
-        m = mt;
-        l *= f;
-#pragma unroll
-        for (int y = 0; y < KM; ++y) {
-          acc[y][0] *= f;
-          acc[y][1] *= f;
-        }
-      }
-      const float w = on ? ex2_approx(x - m) : 0.f;
-      l += w;
-
-      // weights times scales, over the power of two of the tile's largest
-      // scale of the group, in two parts
-      float unit = 1.f;  // of group `quad`
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const uint32_t sb =
-            on ? reinterpret_cast<const uint16_t *>(ss + SM::kScales)[own * G + g] : 0u;
-        const float u = pow2_of(__reduce_max_sync(0xFFFFFFFFu, sb << 16));
-        if (quad == g) unit = u;
-        const float y = on ? w * (bf16_bits_to_float(sb) * inv_pow2(u)) : 0.f;
-        const __half h = __float2half_rn(y);
-        sw[(2 * g) * kTile + own_at] = h;
-        sw[(2 * g + 1) * kTile + own_at] = __float2half_rn((y - __half2float(h)) * kLoScale);
-      }
-      __syncwarp();
-      // B operand: this lane's column row8, rows 2 quad, + 1, + 8, + 9 of each half
-      uint4 wf = make_uint4(0u, 0u, 0u, 0u);
-      if (row8 < 2 * G) wf = *reinterpret_cast<const uint4 *>(sw + row8 * kTile + quad * 8);
-
-      // output: this lane's channels [row8 D / 8, + D / 8), two per product
-      constexpr int VW = D * BITS / 256;  // words of the lane's channels in a row
-      float o[KM][4];
-#pragma unroll
-      for (int y = 0; y < KM; ++y) o[y][0] = o[y][1] = o[y][2] = o[y][3] = 0.f;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        uint32_t vw[4][VW];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = b * 16 + 2 * quad + (e & 1) + (e >> 1) * 8;
-          if (VW == 4) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(sv + piece_at<RB>(r, row8));
-            vw[e][0] = u.x, vw[e][1] = u.y, vw[e][2] = u.z, vw[e][3] = u.w;
-          } else if (VW == 2) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(sv + piece_at<RB>(r, row8 >> 1) +
-                                                             (row8 & 1) * 8);
-            vw[e][0] = u.x, vw[e][1] = u.y;
-          } else {
-            vw[e][0] = *reinterpret_cast<const uint32_t *>(sv + piece_at<RB>(r, row8 >> 2) +
-                                                           (row8 & 3) * 4);
-          }
-        }
-        const uint32_t bw0 = b ? wf.z : wf.x, bw1 = b ? wf.w : wf.y;
-#pragma unroll
-        for (int w2 = 0; w2 < VW; ++w2) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t sel = h ? 0x7632 : 0x5410;
-            const uint32_t v01 = __byte_perm(vw[0][w2], vw[1][w2], sel);
-            const uint32_t v23 = __byte_perm(vw[2][w2], vw[3][w2], sel);
-            if (BITS == 8) {
-              uint32_t a0, a1, a2, a3;
-              codes8(v01, a0, a1);
-              codes8(v23, a2, a3);
-              mma_f16(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1);
-            } else {
-              uint32_t ca[4], cb[4];
-              codes4(v01, ca);
-              codes4(v23, cb);
-              mma_f16(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1);
-              mma_f16(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1);
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < KM; ++y) {
-        acc[y][0] = fmaf(fmaf(o[y][1], kLoUnscale, o[y][0]), unit, acc[y][0]);
-        acc[y][1] = fmaf(fmaf(o[y][3], kLoUnscale, o[y][2]), unit, acc[y][1]);
-      }
-      if (STAGES == 1) break;
-      __syncwarp();  // the stage and the weights are rewritten from here on
-      const int next = r0 + STAGES * kWarps * kTile;
-      if (next < hi) load_tile(next, st);
-      cp_async_commit();
-      st = st + 1 == STAGES ? 0 : st + 1;
-    }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-    // the lanes whose columns are their channels' group hold the output
-    if (quad == row8 * (D / 8) / 32) {
-#pragma unroll
-      for (int y = 0; y < KM; ++y) {
-        s_acc[warp][row8 * (D / 8) + 2 * y] = acc[y][0];
-        s_acc[warp][row8 * (D / 8) + 2 * y + 1] = acc[y][1];
+      if (left > 0) {
+        ++hl;
+        base += hd.tiles;
+        tile = 0;
+        hd = nx;
       }
     }
   }
-  if (STEP && active && len >= lo && len < hi) {  // this CTA holds the new row
-    for (int e = tid; e < D; e += kThreads)
-      static_cast<T *>(c.qbuf)[((size_t)i * p.P + ntok % p.P) * D + e] =
-          static_cast<const T *>(p.q)[(size_t)hl * D + e];
-    if (tid == 0) c.pos[off + len] = p.C + ntok;
-  }
-  if (lane == 0) {
-    s_m[warp] = m;
-    s_l[warp] = l;
-  }
-  const int warps = active ? min(kWarps, (hi - lo + kTile - 1) / kTile) : 0;  // with rows
   __syncthreads();
-  m = -INFINITY, l = 0.f;
-  float out = 0.f;  // thread d < D: channel d
-  for (int w = 0; w < warps; ++w) m = fmaxf(m, s_m[w]);
-  for (int w = 0; w < warps; ++w) {
-    const float f = ex2_approx(s_m[w] - m);
-    l += s_l[w] * f;
-    if (tid < D) out += s_acc[w][tid] * f;
+
+  // pieces joined: a warp those of the head that starts in its run, warp 0
+  // (which has a run if any has) also those of the head the run starts inside
+  if (cta < ctas) {
+    auto piece = [&](int w, int slot) {
+      return reinterpret_cast<const float *>(dyn + w * SM::kWarp + (slot ? 0 : SM::kPiece)) +
+             lane * E;
+    };
+#pragma unroll 1
+    for (int slot = 1; slot >= 0; --slot) {
+      if (slot == 0 && warp != 0) break;
+      const int h = s_piece[warp][slot];
+      if (h < 0) continue;
+      float m = s_m[warp][slot], l = s_l[warp][slot], o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = piece(warp, slot)[e];
+      bool ends = s_ends[warp][slot];
+      for (int w = warp + 1; w < WARPS && !ends; ++w) {
+        if (s_piece[w][0] != h) continue;  // a warp without a run
+        add_piece<E>(m, l, o, s_m[w][0], s_l[w][0], piece(w, 0));
+        ends = s_ends[w][0];
+      }
+      // (its label does not change; its length only once it is finished)
+      const bool dense = STEP ? c.label[p.base + h] == HKV_DENSE : false;
+      if (slot == 1 && ends) {
+        finish_head<D>(p, h, m, l, o);
+        if (STEP && lane == 0) advance_or_leave(p, h, dense);
+        continue;
+      }
+      // cut between CTAs: this one's part to the workspace
+      float *part = p.part + ((size_t)cta * 2 + slot) * PF;
+#pragma unroll
+      for (int e = 0; e < E; ++e) part[lane * E + e] = o[e];
+      if (lane == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
+      __syncwarp();
+      // the CTAs that hold the head: those of its first and last tile, and between
+      auto cta_of = [&](int t) {
+        const int longer = rest * (share + 1);  // tiles of the warps with one more
+        const int w = t < longer ? t / (share + 1) : rest + (t - longer) / share;
+        return w / WARPS;
+      };
+      const int c0 = cta_of(s_first[warp][slot]);
+      const int c1 = cta_of(s_first[warp][slot] + s_tiles[warp][slot] - 1);
+      int last = 0;
+      if (lane == 0) {
+        __threadfence();
+        last = atomicAdd(p.count + h, 1u) == (uint32_t)(c1 - c0);
+        __threadfence();
+      }
+      if (!__shfl_sync(0xFFFFFFFFu, last, 0)) continue;
+      float mx = -INFINITY;
+      for (int j = c0 + lane; j <= c1; j += 32)
+        mx = fmaxf(mx, __ldcg(p.part + ((size_t)j * 2 + (j == c0)) * PF + D));
+#pragma unroll
+      for (int x = 16; x >= 1; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+      l = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = 0.f;
+      for (int j0 = c0; j0 <= c1; j0 += 32) {
+        float f = 0.f, lj = 0.f;
+        if (j0 + lane <= c1) {
+          const float2 ml = __ldcg(reinterpret_cast<const float2 *>(
+              p.part + ((size_t)(j0 + lane) * 2 + (j0 + lane == c0)) * PF + D));
+          f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mx);
+          lj = ml.y * f;
+        }
+#pragma unroll
+        for (int x = 16; x >= 1; x >>= 1) lj += __shfl_xor_sync(0xFFFFFFFFu, lj, x);
+        l += lj;
+        const int n = min(32, c1 - j0 + 1);
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+          const float fj = __shfl_sync(0xFFFFFFFFu, f, j);
+          const float *src = p.part + ((size_t)(j0 + j) * 2 + (j0 + j == c0)) * PF + lane * E;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] += __ldcg(src + e) * fj;
+        }
+      }
+      finish_head<D>(p, h, mx, l, o);
+      if (lane == 0) {
+        p.count[h] = 0u;
+        if (STEP) advance_or_leave(p, h, dense);
+      }
+    }
   }
-  if (p.nchunks > 1) {
-    float *part = p.part + ((size_t)hl * p.nchunks + ch) * PF;
-    if (active) {
-      if (tid < D) part[tid] = out;
-      if (tid == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      __threadfence();  // after the barrier it covers the whole CTA's writes
-      s_last = atomicAdd(p.count + hl, 1u) == (uint32_t)p.nchunks - 1u;
-      __threadfence();
-    }
-    __syncthreads();
-    if (!s_last) return;
-    // at most kThreads ranges (quant_chunk): one thread each for their factors
-    const int np = n > 0 ? (n + per - 1) / per : 1;
-    const float *first_part = p.part + (size_t)hl * p.nchunks * PF;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (tid < np) ml = __ldcg(reinterpret_cast<const float2 *>(first_part + (size_t)tid * PF + D));
-    float mx = ml.x;
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
-    if (lane == 0) s_m[warp] = mx;
-    __syncthreads();
-    m = s_m[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_m[w]);
-    const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - m);
-    s_factor[tid] = f;
-    l = ml.y * f;
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-    if (lane == 0) s_l[warp] = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) l += s_l[w];
-    out = 0.f;
-    if (tid < D) {
-#pragma unroll 8
-      for (int j = 0; j < np; ++j) out += __ldcg(first_part + (size_t)j * PF + tid) * s_factor[j];
-    }
-    if (tid == 0) p.count[hl] = 0u;
-  }
-  // the prior: another set of keys with its own normalised output
-  if (p.prior_lse) {
-    const float pm = p.prior_lse[hl] * kLog2e;
-    if (!(pm == -INFINITY)) {
-      const float mn = fmaxf(m, pm);
-      const float f = l == 0.f ? 0.f : ex2_approx(m - mn), w = ex2_approx(pm - mn);
-      l = l * f + w;
-      out = out * f;
-      if (tid < D) out += w * p.prior_out[(size_t)hl * D + tid];
-      m = mn;
-    }
-  }
-  if (tid < D) p.out[(size_t)hl * D + tid] = l == 0.f ? 0.f : out / l;
+  if (!STEP) return;
+  __syncthreads();  // this CTA's heads are advanced or left
   if (tid == 0) {
-    if (p.lse) p.lse[hl] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-    if (STEP) {
-      c.len[i] = len + 1;
-      c.ntok[i] = ntok + 1;
-      if (lab != HKV_DENSE) c.nbuf[i] = nbuf + 1;
+    uint32_t later = 0;
+    if ((atomicAdd(p.done, 1u << 16) >> 16) == gridDim.x - 1u) {
+      __threadfence();
+      later = atomicExch(p.done + 1, 0u);
+      *p.done = 0u;
     }
+    s_later = later;
+  }
+  __syncthreads();
+  if (s_later == 0) return;
+  for (int h = tid; h < p.nheads; h += THREADS) {
+    if (__ldcg(p.count + h) != kLater) continue;
+    p.count[h] = 0u;
+    advance_head(p, h, c.label[p.base + h] == HKV_DENSE);
   }
 }
 
-}  // namespace
-
-// Rows of a CTA's range at most: one tile per warp, or, for segments of more
-// than kMostRanges such ranges, as many as keep to that number (the CTA that
-// joins a head's ranges handles one per thread).
-constexpr int kMostRanges = 96;
-int quant_chunk(int nheads, int max_segment) {
-  (void)nheads;
-  constexpr int one = kWarps * kTile;
-  const int tiles = (max_segment + kMostRanges * one - 1) / (kMostRanges * one);
-  return one * (tiles < 1 ? 1 : tiles);
-}
-
-namespace {
-
-template <int D, typename T, int BITS, bool STEP, int STAGES>
-cudaError_t launch(const QAttnArgs &a, int grid, cudaStream_t s) {
-  constexpr int smem = Smem<D, BITS, STAGES>::kTotal;
+template <int D, typename T, int BITS, bool STEP>
+cudaError_t launch(const QAttnArgs &a, cudaStream_t s) {
+  using SM = Smem<D, BITS>;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(quant_attn_kernel<D, T, BITS, STEP, STAGES>, smem, ready);
+  cudaError_t e = allow_smem_of(quant_attn_kernel<D, T, BITS, STEP>, SM::kTotal, ready);
   if (e != cudaSuccess) return e;
-  return pdl_launch(quant_attn_kernel<D, T, BITS, STEP, STAGES>, grid, kThreads, smem, s, a);
+  // two CTAs an SM, or a warp for every tile there can be
+  const long long tiles = (long long)a.nheads * ((a.max_rows + kTile - 1) / kTile);
+  const long long want = (tiles + SM::kWarps - 1) / SM::kWarps;
+  const int full = 2 * a.sms < kQuantMaxGrid ? 2 * a.sms : kQuantMaxGrid;
+  const int grid = (int)(want < full ? want : full);
+  return pdl_launch(quant_attn_kernel<D, T, BITS, STEP>, grid, SM::kWarps * 32, SM::kTotal, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_quant_attention(const QAttnArgs &a, int D, int dtype, int bits,
                                    cudaStream_t s) {
-  const long long grid = (long long)a.nheads * a.nchunks;
-  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-#define HKV_QATTN(BITS_, STEP_) \
-  if (a.chunk == kWarps * kTile)                                              \
-    HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_, 1>(a, (int)grid, s)); \
-  HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_, 2>(a, (int)grid, s))
+#define HKV_QATTN(BITS_, STEP_) HKV_DISPATCH(D, dtype, return launch<kD, kT, BITS_, STEP_>(a, s))
   if (bits == HKV_Q8) {
-    if (a.k_new) {
-      HKV_QATTN(8, true);
-    }
+    if (a.k_new) HKV_QATTN(8, true);
     HKV_QATTN(8, false);
   }
-  if (a.k_new) {
-    HKV_QATTN(4, true);
-  }
+  if (a.k_new) HKV_QATTN(4, true);
   HKV_QATTN(4, false);
 #undef HKV_QATTN
   return cudaErrorInvalidValue;

@@ -60,22 +60,30 @@ hkv_status layer_heads(const hkv_config *cfg, int layer, int *first, int *count)
   return HKV_OK;
 }
 
-// workspace of the attention: arrival counters, then partial results
+// workspace of the attention: two words of the grid's progress and the heads'
+// arrival counters, then partial results
 size_t quant_counts_bytes(const hkv_config *c) {
-  return align256((size_t)heads_per_layer(c) * sizeof(uint32_t));
-}
-
-// CTAs per head of the attention
-int quant_chunks(const hkv_config *c) {
-  const int seg = max_segment(c), chunk = quant_chunk(heads_per_layer(c), seg);
-  return (seg + chunk - 1) / chunk;
+  return align256(((size_t)heads_per_layer(c) + 2) * sizeof(uint32_t));
 }
 
 size_t quant_ws_bytes(const hkv_config *c) {
-  const int nch = quant_chunks(c);
-  const size_t parts =
-      nch > 1 ? (size_t)heads_per_layer(c) * nch * (c->head_dim + 4) * sizeof(float) : 0;
-  return quant_counts_bytes(c) + align256(parts);
+  return quant_counts_bytes(c) +
+         align256((size_t)kQuantMaxGrid * 2 * (c->head_dim + 4) * sizeof(float));
+}
+
+// SMs of the current device, looked up once
+hkv_status device_sms(int *sms) {
+  static std::atomic<int> known[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return HKV_ERR_CUDA;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+      return HKV_ERR_CUDA;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  *sms = n;
+  return HKV_OK;
 }
 
 hkv_status quant_attend(const char *name, const hkv_config *cfg, const hkv_qcache *cache,
@@ -105,10 +113,13 @@ hkv_status quant_attend(const char *name, const hkv_config *cfg, const hkv_qcach
   a.out = out;
   a.lse = lse;
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  a.count = reinterpret_cast<uint32_t *>(ws);
+  a.done = reinterpret_cast<uint32_t *>(ws);
+  a.count = a.done + 2;
   a.part = reinterpret_cast<float *>(ws + quant_counts_bytes(cfg));
-  a.chunk = quant_chunk(a.nheads, max_segment(cfg));
-  a.nchunks = quant_chunks(cfg);
+  a.max_rows = max_segment(cfg);
+  // tiles of 32 rows are counted in 31 bits
+  if ((long long)a.nheads * ((a.max_rows + 31) / 32) > 0x7FFFFFFFLL) return HKV_ERR_SHAPE;
+  HKV_TRY(device_sms(&a.sms));
   a.P = cfg->period;
   a.C = cfg->n_cond;
   a.prefetch = (flags & HKV_STEP_PREFETCH) ? 1 : 0;
