@@ -210,6 +210,22 @@ __device__ __forceinline__ HeadRef head_ref(const QAttnArgs &p, int hl) {
   return r;
 }
 
+template <int E>
+__device__ __forceinline__ void store_row(float *to, const float (&o)[E]) {
+  if (E == 4) *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1 % E], o[2 % E], o[3 % E]);
+  else *reinterpret_cast<float2 *>(to) = make_float2(o[0], o[1 % E]);
+}
+template <int E>
+__device__ __forceinline__ void load_row(const float *from, float (&o)[E]) {  // past L1
+  if (E == 4) {
+    const float4 u = __ldcg(reinterpret_cast<const float4 *>(from));
+    o[0] = u.x, o[1 % E] = u.y, o[2 % E] = u.z, o[3 % E] = u.w;
+  } else {
+    const float2 u = __ldcg(reinterpret_cast<const float2 *>(from));
+    o[0] = u.x, o[1 % E] = u.y;
+  }
+}
+
 // A head's result, channels lane * E .. of the unnormalised output: joined
 // with the prior, normalised and written. The whole warp calls.
 template <int D>
@@ -231,7 +247,8 @@ __device__ __forceinline__ void finish_head(const QAttnArgs &p, int hl, float m,
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < E; ++e) p.out[(size_t)hl * D + lane * E + e] = o[e] * inv;
+  for (int e = 0; e < E; ++e) o[e] *= inv;
+  store_row<E>(p.out + (size_t)hl * D + lane * E, o);
   if (p.lse && lane == 0) p.lse[hl] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
@@ -248,7 +265,7 @@ __device__ __forceinline__ void advance_head(const QAttnArgs &p, int hl, bool de
 }
 __device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense) {
   uint32_t v;
-  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.done) : "memory");
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.done) : "memory");
   if ((v & 0xFFFFu) == gridDim.x) {
     advance_head(p, hl, dense);
   } else {
@@ -301,6 +318,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   const int h0 = min(tid * hp, p.nheads), h1 = min(h0 + hp, p.nheads);
   const int len0 = h0 < h1 ? c.len[p.base + h0] : 0;
   int mine = h0 < h1 ? head_tiles<STEP>(len0, p.max_rows) : 0;
+#pragma unroll 8
   for (int h = h0 + 1; h < h1; ++h) mine += head_tiles<STEP>(c.len[p.base + h], p.max_rows);
   int total;
   const int before = block_excl_scan<int>(mine, s_scan, &total);
@@ -341,6 +359,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
     pl_tile = run0 - s_base[warp];
     pr = head_ref<STEP>(p, pl_head);
   }
+  HeadRef hd = pr;
   auto issue = [&]() {
     if (pl_left > 0) {
       const int r0 = pl_tile * kTile;
@@ -387,7 +406,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
 
   if (left > 0) {
     int hl = s_head[warp], base = s_base[warp], tile = run0 - base, st = 0;
-    HeadRef hd = head_ref<STEP>(p, hl), nx = hd;
+    HeadRef nx = hd;
     float qv[E], qn[E];  // this head's query, the next one's
     auto fetch_q = [&](int h, float (&q)[E]) {
 #pragma unroll
@@ -714,16 +733,18 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       return reinterpret_cast<const float *>(dyn + w * SM::kWarp + (slot ? 0 : SM::kPiece)) +
              lane * E;
     };
+    // (the middle warp does the latter: its own run seldom starts a head too)
 #pragma unroll 1
     for (int slot = 1; slot >= 0; --slot) {
-      if (slot == 0 && warp != 0) break;
-      const int h = s_piece[warp][slot];
+      if (slot == 0 && warp != WARPS / 2) break;
+      const int from = slot ? warp : 0;
+      const int h = s_piece[from][slot];
       if (h < 0) continue;
-      float m = s_m[warp][slot], l = s_l[warp][slot], o[E];
+      float m = s_m[from][slot], l = s_l[from][slot], o[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = piece(warp, slot)[e];
-      bool ends = s_ends[warp][slot];
-      for (int w = warp + 1; w < WARPS && !ends; ++w) {
+      for (int e = 0; e < E; ++e) o[e] = piece(from, slot)[e];
+      bool ends = s_ends[from][slot];
+      for (int w = from + 1; w < WARPS && !ends; ++w) {
         if (s_piece[w][0] != h) continue;  // a warp without a run
         add_piece<E>(m, l, o, s_m[w][0], s_l[w][0], piece(w, 0));
         ends = s_ends[w][0];
@@ -737,8 +758,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       }
       // cut between CTAs: this one's part to the workspace
       float *part = p.part + ((size_t)cta * 2 + slot) * PF;
-#pragma unroll
-      for (int e = 0; e < E; ++e) part[lane * E + e] = o[e];
+      store_row<E>(part + lane * E, o);
       if (lane == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
       __syncwarp();
       // the CTAs that hold the head: those of its first and last tile, and between
@@ -747,44 +767,54 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         const int w = t < longer ? t / (share + 1) : rest + (t - longer) / share;
         return w / WARPS;
       };
-      const int c0 = cta_of(s_first[warp][slot]);
-      const int c1 = cta_of(s_first[warp][slot] + s_tiles[warp][slot] - 1);
-      int last = 0;
-      if (lane == 0) {
-        __threadfence();
-        last = atomicAdd(p.count + h, 1u) == (uint32_t)(c1 - c0);
-        __threadfence();
-      }
-      if (!__shfl_sync(0xFFFFFFFFu, last, 0)) continue;
-      float mx = -INFINITY;
-      for (int j = c0 + lane; j <= c1; j += 32)
-        mx = fmaxf(mx, __ldcg(p.part + ((size_t)j * 2 + (j == c0)) * PF + D));
-#pragma unroll
-      for (int x = 16; x >= 1; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-      l = 0.f;
+      const int c0 = cta_of(s_first[from][slot]);
+      const int c1 = cta_of(s_first[from][slot] + s_tiles[from][slot] - 1);
+      uint32_t seen = 0;
+      if (lane == 0)  // releases the warp's part, acquires the others'
+        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;"
+                     : "=r"(seen)
+                     : "l"(p.count + h)
+                     : "memory");
+      if (__shfl_sync(0xFFFFFFFFu, seen, 0) != (uint32_t)(c1 - c0)) continue;
+      m = -INFINITY, l = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = 0.f;
-      for (int j0 = c0; j0 <= c1; j0 += 32) {
-        float f = 0.f, lj = 0.f;
-        if (j0 + lane <= c1) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2 *>(
-              p.part + ((size_t)(j0 + lane) * 2 + (j0 + lane == c0)) * PF + D));
-          f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mx);
-          lj = ml.y * f;
-        }
+      for (int j0 = c0; j0 <= c1; j0 += 32) {  // a lane per part, then all of it
+        const int n = min(32, c1 - j0 + 1);
+        auto part_of = [&](int j) {
+          return p.part + ((size_t)(j0 + j) * 2 + (j0 + j == c0)) * PF;
+        };
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml = __ldcg(reinterpret_cast<const float2 *>(part_of(lane) + D));
+        float v[4][E];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < n) load_row<E>(part_of(j) + lane * E, v[j]);
+        const float mn = fmaxf(m, warp_max(ml.x));
+        const float f = l == 0.f ? 0.f : ex2_approx(m - mn);
+        const float g = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mn);
+        float lj = ml.y * g;
 #pragma unroll
         for (int x = 16; x >= 1; x >>= 1) lj += __shfl_xor_sync(0xFFFFFFFFu, lj, x);
-        l += lj;
-        const int n = min(32, c1 - j0 + 1);
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-          const float fj = __shfl_sync(0xFFFFFFFFu, f, j);
-          const float *src = p.part + ((size_t)(j0 + j) * 2 + (j0 + j == c0)) * PF + lane * E;
+        m = mn;
+        l = l * f + lj;
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] += __ldcg(src + e) * fj;
+        for (int e = 0; e < E; ++e) o[e] *= f;
+        for (int j1 = 0; j1 < n; j1 += 4) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float gj = __shfl_sync(0xFFFFFFFFu, g, (j1 + j) & 31);
+            if (j1 + j < n) {
+#pragma unroll
+              for (int e = 0; e < E; ++e) o[e] += v[j][e] * gj;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j1 + 4 + j < n) load_row<E>(part_of(j1 + 4 + j) + lane * E, v[j]);
         }
       }
-      finish_head<D>(p, h, mx, l, o);
+      finish_head<D>(p, h, m, l, o);
       if (lane == 0) {
         p.count[h] = 0u;
         if (STEP) advance_or_leave(p, h, dense);
