@@ -1,6 +1,9 @@
 // Decode attention over a cache in 8 or 4 bits, with or without the append of
 // the step's new token: one launch per layer.
 //
+// Two kernels, by the longest segment the config allows. Up to kHeadRows rows a
+// CTA takes a whole head (quant_head_kernel). Else (quant_attn_kernel):
+//
 // The layer's rows, head after head in tiles of 32, are cut into equal runs of
 // tiles, one per warp of a grid that fills the device once. A warp streams its
 // run through its own ring of tiles in shared memory, whatever heads it
@@ -14,130 +17,91 @@
 // Every CTA reads the layer's lengths to find its run, so a step may advance a
 // head's counters only when all have: whoever finishes a head advances them if
 // every CTA has reported that, else leaves it to the CTA that exits last.
-//
-// The products run on the tensor cores (mma.sync m16n8k16, fp16 operands, fp32
-// sums), not because one query per head fills them (a sixteenth does) but
-// because codes then need no conversion to fp32: a code is an exact fp16
-// number two of which a bit operation and one packed subtraction make, and the
-// eight columns carry what one query leaves empty:
-//  * scores, 16 rows of K (M) x 16 channels (K): the columns hold the query cut
-//    into two fp16 parts (hi, and the rest times 2^11: 22 bits), once per group
-//    of 32 channels, zero outside the group. The sums of a row come out per
-//    group, ready for the group's scale in fp32;
-//  * output, 16 channels of V^T (M) x 16 rows (K): the columns hold the rows'
-//    weights times the row's scale of each group, cut in two the same way,
-//    after division by a power of two near the tile's largest scale of the
-//    group; a channel uses its own group's two columns.
-// Sums chain over at most 8 (scores) or 2 (output) products in the tensor core
-// and are added in fp32 registers beyond that.
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
+#include "hkv_quant_tile.cuh"
 #include "hkv_select.cuh"
 
 namespace hkv {
 namespace {
 
-constexpr int kTile = 32;  // rows a warp handles at a time
+// Short segments: a CTA per head, its warps taking the head's tiles in turn,
+// the first STAGES of each in flight at once (all of them, as launched);
+// nothing outlives the CTA.
+constexpr int kHeadWarps = 4;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kQUp = 4096.f;                               // the query's parts, below 2^13
-constexpr float kLoScale = 2048.f, kLoUnscale = 1.f / 2048.f;  // second parts, 2^11
-constexpr float kRawHi = 0x1p24f / kQUp, kRawLo = kRawHi * kLoUnscale;  // sums of raw codes
-
-__device__ __forceinline__ uint32_t lop_and_or(uint32_t a, uint32_t m, uint32_t o) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(m), "r"(o));  // (a & m) | o
-  return r;
-}
-__device__ __forceinline__ uint32_t h2_add(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
-}
-
-// Stored codes u as fp16 pairs. raw*: the bits themselves, which read as the
-// subnormal numbers u 2^-24 (an odd nibble sits four bits up: u 2^-20); exact
-// in the tensor core, and the bias is taken off the sum. For the scores.
-__device__ __forceinline__ void raw8(uint32_t w, uint32_t &even, uint32_t &odd) {
-  even = w & 0x00FF00FFu;                     // bytes (0, 2)
-  odd = __byte_perm(w, 0u, 0x4341);           // bytes (1, 3)
-}
-__device__ __forceinline__ void raw4(uint32_t w, uint32_t (&c)[4]) {
-  const uint32_t v = w >> 8;                  // nibbles (0, 4) (1, 5) (2, 6) (3, 7)
-  c[0] = w & 0x000F000Fu;
-  c[1] = w & 0x00F000F0u;
-  c[2] = v & 0x000F000Fu;
-  c[3] = v & 0x00F000F0u;
-}
-// codes*: less the bias, exact. 0x64uu is the fp16 number 1024 + uu. For the
-// output, where the bias would be large beside the sum.
-__device__ __forceinline__ void codes8(uint32_t w, uint32_t &even, uint32_t &odd) {
-  constexpr uint32_t kOne = 0x64006400u, kSub = 0xE480E480u;  // 1024, -1152
-  even = h2_add(lop_and_or(w, 0x00FF00FFu, kOne), kSub);
-  odd = h2_add(__byte_perm(w, kOne | 0x00640064u, 0x4341), kSub);
-}
-// codes4: nibbles (0, 4), (1, 5), (2, 6), (3, 7) of a word, less the bias of
-// 8; an odd nibble sits four bits up and reads as 1024 + 16 u
-__device__ __forceinline__ void codes4(uint32_t w, uint32_t (&c)[4]) {
-  constexpr uint32_t kOne = 0x64006400u, kSub = 0xE408E408u;       // -1032
-  constexpr uint32_t kSix = 0x2C002C00u, kSubSix = 0xD480D480u;    // 1/16, -72
-  const uint32_t v = w >> 8;
-  c[0] = h2_add(lop_and_or(w, 0x000F000Fu, kOne), kSub);
-  c[1] = h2_fma(lop_and_or(w, 0x00F000F0u, kOne), kSix, kSubSix);
-  c[2] = h2_add(lop_and_or(v, 0x000F000Fu, kOne), kSub);
-  c[3] = h2_fma(lop_and_or(v, 0x00F000F0u, kOne), kSix, kSubSix);
-}
-
-__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                        uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-      "{%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// the first of a chain: c = a b + (e0, e1, e0, e1)
-__device__ __forceinline__ void mma_f16_from(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                             uint32_t a3, uint32_t b0, uint32_t b1, float e0,
-                                             float e1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-      "{%10,%11,%10,%11};"
-      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(e0), "f"(e1));
-}
-// maximum over the warp
-__device__ __forceinline__ float warp_max(float x) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-template <int BYTES>
-__device__ __forceinline__ void cp_async_small(void *dst, const void *src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() {
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-// 2^e and 2^-e for the exponent e of a non-negative fp32 (its bits), e kept in
-// [-126, 126]
-__device__ __forceinline__ float pow2_of(uint32_t bits) {
-  return __uint_as_float(min(max(bits & 0x7F800000u, 0x00800000u), 0x7E800000u));
-}
-__device__ __forceinline__ float inv_pow2(float p) {
-  return __uint_as_float(0x7F000000u - __float_as_uint(p));
+template <int D, typename T, int BITS, bool STEP, int STAGES>
+__global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
+    quant_head_kernel(const QAttnArgs p) {
+  using TL = TileOf<D, BITS>;
+  constexpr int E = D / 32;
+  extern __shared__ __align__(16) unsigned char dyn[];
+  __shared__ float s_acc[kHeadWarps][D];
+  __shared__ float s_m[kHeadWarps], s_l[kHeadWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hl = blockIdx.x;
+  unsigned char *ws = dyn + warp * (STAGES * TL::kBytes + TL::kOperand);
+  if (!p.prefetch) pdl_wait();
+  const HeadRef hd = head_ref<STEP>(p, hl);
+  if (hd.bad) {
+    pdl_wait();
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) set_err(p.q8.c.err, hd.bad);
+    return;
+  }
+  auto load = [&](int tile, int st) {
+    const int r0 = tile * kTile;
+    load_tile<D, BITS>(ws + st * TL::kBytes, p.q8, hd.off + r0, min(kTile, hd.len - r0));
+  };
+#pragma unroll
+  for (int st = 0; st < STAGES; ++st) {
+    if (warp + st * kHeadWarps < hd.tiles) load(warp + st * kHeadWarps, st);
+    cp_async_commit();
+  }
+  if (p.prefetch) pdl_wait();  // the step's inputs are visible from here on
+  pdl_launch_dependents();
+  float m = -INFINITY, l = 0.f;
+  if (warp < hd.tiles && hd.n > 0) {
+    float acc[D / 16][2] = {};
+    float qv[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      qv[e] = (float)static_cast<const T *>(p.q)[(size_t)hl * D + lane * E + e];
+    __half *operand = reinterpret_cast<__half *>(ws + STAGES * TL::kBytes);
+    const Query<D, BITS> qr = make_query<D, BITS>(qv, p.qscale, operand);
+    int st = 0;
+    for (int tile = warp; tile < hd.tiles; tile += kHeadWarps) {
+      cp_async_wait<STAGES - 1>();
+      __syncwarp();
+      unsigned char *stage = ws + st * TL::kBytes;
+      const int r0 = tile * kTile, rows = min(kTile, hd.n - r0);
+      if (STEP && hd.len >= r0 && hd.len - r0 < rows)
+        append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, qv);
+      attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
+      if (STAGES == 1) break;  // no warp has a second tile
+      __syncwarp();            // the stage and the weights are rewritten from here on
+      if (tile + STAGES * kHeadWarps < hd.tiles) load(tile + STAGES * kHeadWarps, st);
+      cp_async_commit();
+      st = st + 1 == STAGES ? 0 : st + 1;
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+    store_acc<D>(s_acc[warp], acc);
+  }
+  if (lane == 0) {
+    s_m[warp] = m;
+    s_l[warp] = l;
+  }
+  __syncthreads();
+  if (warp != 0) return;
+  float o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kHeadWarps; ++w)
+    if (s_l[w] != 0.f) add_piece<E>(m, l, o, s_m[w], s_l[w], &s_acc[w][lane * E]);
+  finish_head<D>(p, hl, m, l, o);
+  if (STEP && lane == 0) advance_head(p, hl, hd.dense);
 }
 
 // Warps of a CTA and tiles in flight of a warp, two CTAs an SM: as much of an
@@ -147,122 +111,24 @@ struct Shape {
   static constexpr int kWarps = RB == 128 ? 6 : 8, kStages = RB == 32 ? 4 : 2;
 };
 
-// Shared memory of a warp: its tiles (codes of K and V, scales of K and V),
-// the B operand being made (the query's two parts, then the weights), and the
-// piece of the head its run starts inside.
+// Shared memory of a warp: its tiles, the operand area, and the piece of the
+// head its run starts inside.
 template <int D, int BITS>
 struct Smem {
   using R = QRow<D, BITS>;
   static constexpr int kWarps = Shape<R::kBytes>::kWarps, kStages = Shape<R::kBytes>::kStages;
-  static constexpr int kCodes = kTile * R::kBytes, kScales = kTile * R::kScaleBytes;
-  static constexpr int kStage = 2 * (kCodes + kScales);
-  static constexpr int kOperand = kStages * kStage;      // fp16 [2][D], [8][kTile]
-  static constexpr int kPiece = kOperand + 512;          // fp32 [D]
+  static constexpr int kStage = TileOf<D, BITS>::kBytes;
+  static constexpr int kOperand = kStages * kStage;
+  static constexpr int kPiece = kOperand + TileOf<D, BITS>::kOperand;  // fp32 [D]
   static constexpr int kWarp = kPiece + D * 4;
   static constexpr int kTotal = kWarps * kWarp;
-  static_assert(2 * D * 2 <= 512 && 8 * kTile * 2 <= 512, "one operand at a time");
   static_assert(kStage >= D * 4, "the last piece takes a tile's place");
 };
 
-// Byte offset of the 16-byte piece `c` of row `r` in a tile: rows lie back to
-// back, the pieces permuted so that the reads below spread over all banks.
-template <int RB>
-__device__ __forceinline__ int piece_at(int r, int c) {
-  if (RB == 128) return r * 128 + ((c ^ (r & 7)) << 4);
-  if (RB == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
-  return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
-}
-
-// A head as its tiles see it.
-struct HeadRef {
-  long long off;
-  int len, n, tiles;   // old rows, rows to attend over, tiles (at least one)
-  uint32_t bad;        // status of a head that cannot be served
-  bool dense;
-};
-
-// Tiles of a head of `len` rows: one at least, so that some warp reports,
-// or writes the outputs of an empty head.
-template <bool STEP>
-__device__ __forceinline__ int head_tiles(int len, int max_rows) {
-  const int n = len + (STEP ? 1 : 0);
-  return n <= 0 || n > max_rows || len < 0 ? 1 : (n + kTile - 1) / kTile;
-}
-
-template <bool STEP>
-__device__ __forceinline__ HeadRef head_ref(const QAttnArgs &p, int hl) {
-  const CacheArgs &c = p.q8.c;
-  const int i = p.base + hl;
-  HeadRef r;
-  r.off = c.off[i];
-  r.len = c.len[i];
-  const int cap = c.cap[i];
-  r.n = r.len + (STEP ? 1 : 0);
-  r.tiles = head_tiles<STEP>(r.len, p.max_rows);
-  r.bad = 0;
-  r.dense = STEP ? c.label[i] == HKV_DENSE : false;
-  if (r.off < 0 || cap < 0 || r.off + cap > c.arena_tokens || r.len < 0 || r.len > cap)
-    r.bad = HKV_ERR_BOUNDS;
-  else if (STEP && !r.dense && c.nbuf[i] >= p.P)
-    r.bad = HKV_ERR_STATE;
-  else if (r.n > cap || r.n > p.max_rows)
-    r.bad = HKV_ERR_CAPACITY;
-  return r;
-}
-
-template <int E>
-__device__ __forceinline__ void store_row(float *to, const float (&o)[E]) {
-  if (E == 4) *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1 % E], o[2 % E], o[3 % E]);
-  else *reinterpret_cast<float2 *>(to) = make_float2(o[0], o[1 % E]);
-}
-template <int E>
-__device__ __forceinline__ void load_row(const float *from, float (&o)[E]) {  // past L1
-  if (E == 4) {
-    const float4 u = __ldcg(reinterpret_cast<const float4 *>(from));
-    o[0] = u.x, o[1 % E] = u.y, o[2 % E] = u.z, o[3 % E] = u.w;
-  } else {
-    const float2 u = __ldcg(reinterpret_cast<const float2 *>(from));
-    o[0] = u.x, o[1 % E] = u.y;
-  }
-}
-
-// A head's result, channels lane * E .. of the unnormalised output: joined
-// with the prior, normalised and written. The whole warp calls.
-template <int D>
-__device__ __forceinline__ void finish_head(const QAttnArgs &p, int hl, float m, float l,
-                                            float (&o)[D / 32]) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  if (p.prior_lse) {
-    const float pm = p.prior_lse[hl] * kLog2e;
-    if (!(pm == -INFINITY)) {  // an empty prior's outputs are not looked at
-      const float mn = fmaxf(m, pm);
-      const float f = l == 0.f ? 0.f : ex2_approx(m - mn), w = ex2_approx(pm - mn);
-      l = l * f + w;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        o[e] = o[e] * f + w * p.prior_out[(size_t)hl * D + lane * E + e];
-      m = mn;
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] *= inv;
-  store_row<E>(p.out + (size_t)hl * D + lane * E, o);
-  if (p.lse && lane == 0) p.lse[hl] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-}
-
-// A finished head's counters advance (a step), now or by the CTA that exits
+// A finished head's counters advance now, or are left to the CTA that exits
 // last. done[0]: CTAs that have read the lengths (low half) and exited (high
 // half); done[1]: heads left to the last; kLater marks them in count[].
 constexpr uint32_t kLater = 0x80000000u;
-__device__ __forceinline__ void advance_head(const QAttnArgs &p, int hl, bool dense) {
-  const CacheArgs &c = p.q8.c;
-  const int i = p.base + hl;
-  atomicAdd(c.len + i, 1);
-  atomicAdd(c.ntok + i, 1);
-  if (!dense) atomicAdd(c.nbuf + i, 1);
-}
 __device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense) {
   uint32_t v;
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.done) : "memory");
@@ -275,28 +141,14 @@ __device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, boo
   }
 }
 
-// Adds a piece (maximum pm, sum pl, channels at src) to (m, l, o).
-template <int E>
-__device__ __forceinline__ void add_piece(float &m, float &l, float (&o)[E], float pm, float pl,
-                                          const float *src) {
-  const float mn = fmaxf(m, pm);
-  const float f = l == 0.f ? 0.f : ex2_approx(m - mn), g = pl == 0.f ? 0.f : ex2_approx(pm - mn);
-  m = mn;
-  l = l * f + pl * g;
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = o[e] * f + src[e] * g;
-}
-
 template <int D, typename T, int BITS, bool STEP>
 __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
     quant_attn_kernel(const QAttnArgs p) {
-  using R = QRow<D, BITS>;
   using SM = Smem<D, BITS>;
-  constexpr int RB = R::kBytes, SB = R::kScaleBytes, G = R::kGroups, E = D / 32;
+  constexpr int E = D / 32;
   constexpr int WARPS = SM::kWarps, STAGES = SM::kStages, THREADS = WARPS * 32;
   constexpr int PF = D + 4;          // floats of a partial result
   constexpr int KM = D / 16;         // products per 16 rows, scores and output alike
-  constexpr float kRawBias = R::kBias * 0x1p-24f;  // of a code read as a subnormal
   extern __shared__ __align__(16) unsigned char dyn[];
   // the runs' first heads, and those heads' first tiles in the layer
   __shared__ int s_head[WARPS], s_base[WARPS], s_scan[33];
@@ -308,7 +160,6 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   __shared__ int s_first[WARPS][2], s_tiles[WARPS][2];  // the head's first tile and tiles
   __shared__ uint32_t s_later;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row8 = lane >> 2, quad = lane & 3;
   const CacheArgs &c = p.q8.c;
   if (!p.prefetch) pdl_wait();
 
@@ -353,7 +204,6 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   // the ring: tiles of the run in order, old rows only
   int pl_left = left, pl_head = 0, pl_tile = 0, pl_st = 0;
   HeadRef pr = {};
-  const int my_at = piece_at<RB>(lane / (RB / 16), lane % (RB / 16));
   if (left > 0) {
     pl_head = s_head[warp];
     pl_tile = run0 - s_base[warp];
@@ -364,29 +214,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
     if (pl_left > 0) {
       const int r0 = pl_tile * kTile;
       const int rows = pr.bad ? 0 : min(kTile, pr.len - r0);
-      unsigned char *sk = ws + pl_st * SM::kStage, *sv = sk + SM::kCodes;
-      unsigned char *ss = sv + SM::kCodes;
-      // the tile's codes are one stretch of the arena: lane e of each 512 bytes
-      // takes piece e; its place in the tile moves by whole rows from one to
-      // the next, which flips one swizzle bit at 128-byte rows
-      const size_t src = (size_t)(pr.off + r0) * RB + lane * 16;
-      const unsigned char *K = static_cast<const unsigned char *>(c.K) + src;
-      const unsigned char *V = static_cast<const unsigned char *>(c.V) + src;
-      const int pieces = rows * (RB / 16) - lane;
-#pragma unroll
-      for (int e = 0; e < RB / 16; ++e) {
-        const int at = (RB == 128 && (e & 1) ? my_at ^ 64 : my_at) + e * 512;
-        if (e * 32 < pieces) {
-          cp_async16(sk + at, K + e * 512);
-          cp_async16(sv + at, V + e * 512);
-        }
-      }
-      if (lane < rows) {
-        cp_async_small<SB>(ss + lane * SB, static_cast<const unsigned char *>(p.q8.ks) +
-                                               (pr.off + r0 + lane) * SB);
-        cp_async_small<SB>(ss + SM::kScales + lane * SB,
-                           static_cast<const unsigned char *>(p.q8.vs) + (pr.off + r0 + lane) * SB);
-      }
+      load_tile<D, BITS>(ws + pl_st * SM::kStage, p.q8, pr.off + r0, rows);
       ++pl_tile;
       --pl_left;
       if (pl_tile == pr.tiles && pl_left > 0) {
@@ -414,15 +242,11 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         q[e] = (float)static_cast<const T *>(p.q)[(size_t)h * D + lane * E + e];
     };
     fetch_q(hl, qn);
-    __half *sq = reinterpret_cast<__half *>(ws + SM::kOperand), *sw = sq;
-    // where this lane's row (row8 + 8 quad) sits in the weights' columns
-    const int own = row8 + 8 * quad;
-    const int own_at = ((own >> 1) & 3) * 8 + (own >> 4) * 4 + ((own >> 3) & 1) * 2 + (own & 1);
+    __half *operand = reinterpret_cast<__half *>(ws + SM::kOperand);
 
     while (left > 0) {
       // a head: this warp's piece of it
       const int from = tile;
-      const int i = p.base + hl;
       const bool more = left > hd.tiles - tile;  // another head follows in the run
 #pragma unroll
       for (int e = 0; e < E; ++e) qv[e] = qn[e];
@@ -431,253 +255,22 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         fetch_q(hl + 1, qn);
       }
       if (hd.bad && tile == 0 && lane == 0) set_err(c.err, hd.bad);
-      // the query over a power of two, in two fp16 parts, in the order in which
-      // the codes of a word come out in pairs
-      uint32_t qm = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
-      const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
-      const float xscale = q2 * p.qscale;
-      float sum_hi = 0.f, sum_lo = 0.f;  // of the lane's channels' parts
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int d = lane * E + e;
-        const int at = BITS == 8 ? (d & ~3) + ((d & 1) << 1) + ((d >> 1) & 1)
-                                 : (d & ~7) + ((d & 3) << 1) + ((d >> 2) & 1);
-        // the channels whose codes sit four bits up are taken down by that
-        const float up = BITS == 4 && (e & 1) ? 16.f : 1.f;
-        const float x = qv[e] * qi * (kQUp / up);
-        const __half h = __float2half_rn(x);
-        const __half lo = __float2half_rn((x - __half2float(h)) * kLoScale);
-        sq[at] = h;
-        sq[D + at] = lo;
-        sum_hi += __half2float(h) * up;
-        sum_lo += __half2float(lo) * up;
-      }
-#pragma unroll
-      for (int o = 1; o < 32 / E; o <<= 1) {  // over the lanes of a group
-        sum_hi += __shfl_xor_sync(0xFFFFFFFFu, sum_hi, o);
-        sum_lo += __shfl_xor_sync(0xFFFFFFFFu, sum_lo, o);
-      }
-      // what the codes' bias adds to this lane's two columns (group `quad`)
-      float bias_hi = __shfl_sync(0xFFFFFFFFu, sum_hi, (quad * 32 / E) & 31) * -kRawBias;
-      float bias_lo = __shfl_sync(0xFFFFFFFFu, sum_lo, (quad * 32 / E) & 31) * -kRawBias;
-      if (quad >= G) bias_hi = bias_lo = 0.f;
-      __syncwarp();
-      // B operand of the scores: this lane's column is part (row8 & 1) of group
-      // row8 / 2, its channels those of the lanes `quad` of the A operand
-      uint32_t qf[KM][2];
-      {
-        const uint4 *src = reinterpret_cast<const uint4 *>(sq + (row8 & 1) * D + quad * (D / 4));
-        const bool in_group = (row8 >> 1) == quad * (D / 4) / 32;
-#pragma unroll
-        for (int x = 0; x < KM / 2; ++x) {
-          const uint4 u = in_group ? src[x] : make_uint4(0u, 0u, 0u, 0u);
-          qf[2 * x][0] = u.x;
-          qf[2 * x][1] = u.y;
-          qf[2 * x + 1][0] = u.z;
-          qf[2 * x + 1][1] = u.w;
-        }
-      }
+      const Query<D, BITS> qr = make_query<D, BITS>(qv, p.qscale, operand);
       float m = -INFINITY, l = 0.f;
       float acc[KM][2];
 #pragma unroll
       for (int x = 0; x < KM; ++x) acc[x][0] = acc[x][1] = 0.f;
-      __syncwarp();  // the weights take the query's place
 
       for (; tile < hd.tiles && left > 0; ++tile, --left) {
         cp_async_wait<STAGES - 1>();
         __syncwarp();
-        unsigned char *sk = ws + st * SM::kStage, *sv = sk + SM::kCodes;
-        unsigned char *ss = sv + SM::kCodes;
+        unsigned char *stage = ws + st * SM::kStage;
         const int r0 = tile * kTile;
         const int rows = hd.bad ? 0 : min(kTile, hd.n - r0);
         if (STEP && hd.len - r0 < rows && rows > 0 && hd.len >= r0) {
-          // the new row: quantised into the arena and into the tile
-          const int ntok = c.ntok[i];
-          if (lane < D / 4) {
-            constexpr int TPR = D / 8;
-            const int kv = lane / TPR, col = lane % TPR, r = hd.len - r0;
-            float x[8];
-            load8<T>(static_cast<const T *>(kv ? p.v_new : p.k_new) + (size_t)hl * D + col * 8, x);
-            uint32_t a, b;
-            const uint32_t sb = quant_group<BITS>(x, 0xFu << (lane & 28), a, b);
-            const size_t at = (size_t)(hd.off + hd.len);
-            unsigned char *row = static_cast<unsigned char *>(kv ? c.V : c.K) + at * RB;
-            unsigned char *to = kv ? sv : sk;
-            if (BITS == 8) {
-              reinterpret_cast<uint2 *>(row)[col] = make_uint2(a, b);
-              *reinterpret_cast<uint2 *>(to + piece_at<RB>(r, col >> 1) + (col & 1) * 8) =
-                  make_uint2(a, b);
-            } else {
-              reinterpret_cast<uint32_t *>(row)[col] = a;
-              *reinterpret_cast<uint32_t *>(to + piece_at<RB>(r, col >> 2) + (col & 3) * 4) = a;
-            }
-            if ((col & 3) == 0) {
-              static_cast<uint16_t *>(kv ? p.q8.vs : p.q8.ks)[at * G + col / 4] = (uint16_t)sb;
-              reinterpret_cast<uint16_t *>(ss + kv * SM::kScales + r * SB)[col / 4] = (uint16_t)sb;
-            }
-          }
-          T *ring = static_cast<T *>(c.qbuf) + ((size_t)i * p.P + ntok % p.P) * D;
-#pragma unroll
-          for (int e = 0; e < E; ++e) ring[lane * E + e] = (T)qv[e];
-          if (lane == 0) c.pos[hd.off + hd.len] = p.C + ntok;
-          __syncwarp();
+          append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, qv);
         }
-        if (rows > 0) {
-          // scores: x[b2] is the sum of row row8 + 8 b2 over this lane's group
-          float xs[4];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int ra = b * 16 + row8, rb = ra + 8;
-            float s[4];
-            uint32_t wa[RB / 16], wb[RB / 16];  // this lane's quarter of the two rows
-            if (RB == 128) {
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, 2 * quad + h));
-                const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, 2 * quad + h));
-                wa[h * 4] = ua.x, wa[h * 4 + 1] = ua.y, wa[h * 4 + 2] = ua.z, wa[h * 4 + 3] = ua.w;
-                wb[h * 4] = ub.x, wb[h * 4 + 1] = ub.y, wb[h * 4 + 2] = ub.z, wb[h * 4 + 3] = ub.w;
-              }
-            } else if (RB == 64) {
-              const uint4 ua = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(ra, quad));
-              const uint4 ub = *reinterpret_cast<const uint4 *>(sk + piece_at<RB>(rb, quad));
-              wa[0] = ua.x, wa[1] = ua.y, wa[2] = ua.z, wa[3] = ua.w;
-              wb[0] = ub.x, wb[1] = ub.y, wb[2] = ub.z, wb[3] = ub.w;
-            } else {
-              const uint2 ua = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(ra, quad >> 1) +
-                                                                (quad & 1) * 8);
-              const uint2 ub = *reinterpret_cast<const uint2 *>(sk + piece_at<RB>(rb, quad >> 1) +
-                                                                (quad & 1) * 8);
-              wa[0] = ua.x, wa[1] = ua.y;
-              wb[0] = ub.x, wb[1] = ub.y;
-            }
-#pragma unroll
-            for (int w = 0; w < RB / 16; ++w) {
-              if (BITS == 8) {
-                uint32_t a0, a1, a2, a3;
-                raw8(wa[w], a0, a2);
-                raw8(wb[w], a1, a3);
-                if (w == 0) mma_f16_from(s, a0, a1, a2, a3, qf[0][0], qf[0][1], bias_hi, bias_lo);
-                else mma_f16(s, a0, a1, a2, a3, qf[w][0], qf[w][1]);
-              } else {
-                uint32_t ca[4], cb[4];
-                raw4(wa[w], ca);
-                raw4(wb[w], cb);
-                if (w == 0)
-                  mma_f16_from(s, ca[0], cb[0], ca[1], cb[1], qf[0][0], qf[0][1], bias_hi, bias_lo);
-                else
-                  mma_f16(s, ca[0], cb[0], ca[1], cb[1], qf[2 * w][0], qf[2 * w][1]);
-                mma_f16(s, ca[2], cb[2], ca[3], cb[3], qf[2 * w + 1][0], qf[2 * w + 1][1]);
-              }
-            }
-            const uint16_t *sc = reinterpret_cast<const uint16_t *>(ss);
-            const bool grp = quad < G;  // the columns beyond the groups are empty
-            const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) : 0.f;
-            const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) : 0.f;
-            xs[2 * b] = fa * fmaf(s[1], kRawLo, s[0] * kRawHi);
-            xs[2 * b + 1] = fb * fmaf(s[3], kRawLo, s[2] * kRawHi);
-          }
-          // sums over the groups: lane (row8, quad) ends up with row row8 + 8 quad
-          const bool b0 = quad & 1, b1 = quad & 2;
-          float k0 = (b0 ? xs[1] : xs[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[0] : xs[1], 1);
-          float k1 = (b0 ? xs[3] : xs[2]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[2] : xs[3], 1);
-          float x = (b1 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? k0 : k1, 2);
-          const bool on = own < rows;
-          x = on ? x * xscale : -INFINITY;
-
-          const float mt = warp_max(x);
-          if (mt > m) {  // the same for the whole warp
-            const float f = ex2_approx(m - mt);
-            m = mt;
-            l *= f;
-#pragma unroll
-            for (int y = 0; y < KM; ++y) {
-              acc[y][0] *= f;
-              acc[y][1] *= f;
-            }
-          }
-          const float w = on ? ex2_approx(x - m) : 0.f;
-          l += w;
-
-          // weights times scales, over the power of two of the tile's largest
-          // scale of the group, in two parts
-          float unit = 1.f;  // of group `quad`
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const uint32_t sb =
-                on ? reinterpret_cast<const uint16_t *>(ss + SM::kScales)[own * G + g] : 0u;
-            const float u = pow2_of(__reduce_max_sync(0xFFFFFFFFu, sb << 16));
-            if (quad == g) unit = u;
-            const float y = on ? w * (bf16_bits_to_float(sb) * inv_pow2(u)) : 0.f;
-            const __half h = __float2half_rn(y);
-            sw[(2 * g) * kTile + own_at] = h;
-            sw[(2 * g + 1) * kTile + own_at] = __float2half_rn((y - __half2float(h)) * kLoScale);
-          }
-          __syncwarp();
-          // B operand: this lane's column row8, rows 2 quad, + 1, + 8, + 9 of each half
-          uint4 wf = make_uint4(0u, 0u, 0u, 0u);
-          if (row8 < 2 * G) wf = *reinterpret_cast<const uint4 *>(sw + row8 * kTile + quad * 8);
-
-          // output: this lane's channels [row8 D / 8, + D / 8), two per product
-          constexpr int VW = D * BITS / 256;  // words of the lane's channels in a row
-          float o[KM][4];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint32_t vw[4][VW];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int r = b * 16 + 2 * quad + (e & 1) + (e >> 1) * 8;
-              if (VW == 4) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(sv + piece_at<RB>(r, row8));
-                vw[e][0] = u.x, vw[e][1] = u.y, vw[e][2] = u.z, vw[e][3] = u.w;
-              } else if (VW == 2) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(sv + piece_at<RB>(r, row8 >> 1) +
-                                                                 (row8 & 1) * 8);
-                vw[e][0] = u.x, vw[e][1] = u.y;
-              } else {
-                vw[e][0] = *reinterpret_cast<const uint32_t *>(sv + piece_at<RB>(r, row8 >> 2) +
-                                                               (row8 & 3) * 4);
-              }
-            }
-            const uint32_t bw0 = b ? wf.z : wf.x, bw1 = b ? wf.w : wf.y;
-#pragma unroll
-            for (int w2 = 0; w2 < VW; ++w2) {
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint32_t sel = h ? 0x7632 : 0x5410;
-                const uint32_t v01 = __byte_perm(vw[0][w2], vw[1][w2], sel);
-                const uint32_t v23 = __byte_perm(vw[2][w2], vw[3][w2], sel);
-                if (BITS == 8) {
-                  uint32_t a0, a1, a2, a3;
-                  codes8(v01, a0, a1);
-                  codes8(v23, a2, a3);
-                  if (b == 0) mma_f16_from(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1, 0.f, 0.f);
-                  else mma_f16(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1);
-                } else {
-                  uint32_t ca[4], cb[4];
-                  codes4(v01, ca);
-                  codes4(v23, cb);
-                  if (b == 0) {
-                    mma_f16_from(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1, 0.f, 0.f);
-                    mma_f16_from(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1, 0.f,
-                                 0.f);
-                  } else {
-                    mma_f16(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1);
-                    mma_f16(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1);
-                  }
-                }
-              }
-            }
-          }
-#pragma unroll
-          for (int y = 0; y < KM; ++y) {
-            acc[y][0] = fmaf(fmaf(o[y][1], kLoUnscale, o[y][0]), unit, acc[y][0]);
-            acc[y][1] = fmaf(fmaf(o[y][3], kLoUnscale, o[y][2]), unit, acc[y][1]);
-          }
-        }
+        if (rows > 0) attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
         __syncwarp();  // the stage and the weights are rewritten from here on
         issue();
         st = st + 1 == STAGES ? 0 : st + 1;
@@ -691,13 +284,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         // started inside it: the ring has no tile in flight by then
         float *to = reinterpret_cast<float *>(starts ? ws : ws + SM::kPiece);
         if (starts && ends) to = reinterpret_cast<float *>(ws + SM::kOperand);
-        // the lanes whose columns are their channels' group hold the output
-        if (quad == row8 * (D / 8) / 32) {
-#pragma unroll
-          for (int y = 0; y < KM; ++y)
-            *reinterpret_cast<float2 *>(to + row8 * (D / 8) + 2 * y) =
-                make_float2(acc[y][0], acc[y][1]);
-        }
+        store_acc<D>(to, acc);
         __syncwarp();
         if (starts && ends) {
           float o[E];
@@ -841,8 +428,24 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   }
 }
 
+// Rows up to which a CTA takes a head whole: every tile in flight at once.
+constexpr int kHeadRows = 2 * kHeadWarps * kTile;
+
+template <int D, typename T, int BITS, bool STEP, int STAGES>
+cudaError_t launch_heads(const QAttnArgs &a, cudaStream_t s) {
+  using TL = TileOf<D, BITS>;
+  constexpr int smem = kHeadWarps * (STAGES * TL::kBytes + TL::kOperand);
+  static std::atomic<uint64_t> ready{0};
+  cudaError_t e = allow_smem_of(quant_head_kernel<D, T, BITS, STEP, STAGES>, smem, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(quant_head_kernel<D, T, BITS, STEP, STAGES>, a.nheads, kHeadWarps * 32, smem,
+                    s, a);
+}
+
 template <int D, typename T, int BITS, bool STEP>
 cudaError_t launch(const QAttnArgs &a, cudaStream_t s) {
+  if (a.max_rows <= kHeadWarps * kTile) return launch_heads<D, T, BITS, STEP, 1>(a, s);
+  if (a.max_rows <= kHeadRows) return launch_heads<D, T, BITS, STEP, 2>(a, s);
   using SM = Smem<D, BITS>;
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = allow_smem_of(quant_attn_kernel<D, T, BITS, STEP>, SM::kTotal, ready);
