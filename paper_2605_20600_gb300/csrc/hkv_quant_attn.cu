@@ -40,7 +40,11 @@ __global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
   __shared__ float s_m[kHeadWarps], s_l[kHeadWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hl = blockIdx.x;
   unsigned char *ws = dyn + warp * (STAGES * TL::kBytes + TL::kOperand);
-  if (!p.prefetch) pdl_wait();
+  float qv[E];
+  if (!p.prefetch) {
+    pdl_wait();
+    load_query<D, T>(p, hl, qv);
+  }
   const HeadRef hd = head_ref<STEP>(p, hl);
   if (hd.bad) {
     pdl_wait();
@@ -57,15 +61,17 @@ __global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
     if (warp + st * kHeadWarps < hd.tiles) load(warp + st * kHeadWarps, st);
     cp_async_commit();
   }
-  if (p.prefetch) pdl_wait();  // the step's inputs are visible from here on
+  if (p.prefetch) {
+    pdl_wait();  // the step's inputs are visible from here on
+    load_query<D, T>(p, hl, qv);
+  }
   pdl_launch_dependents();
+  NewRow nr;
+  const int new_tile = hd.len / kTile;  // its warp: the last with a tile
+  if (STEP && new_tile % kHeadWarps == warp) load_new_row<D, T>(p, hl, nr);
   float m = -INFINITY, l = 0.f;
   if (warp < hd.tiles && hd.n > 0) {
     float acc[D / 16][2] = {};
-    float qv[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      qv[e] = (float)static_cast<const T *>(p.q)[(size_t)hl * D + lane * E + e];
     __half *operand = reinterpret_cast<__half *>(ws + STAGES * TL::kBytes);
     const Query<D, BITS> qr = make_query<D, BITS>(qv, p.qscale, operand);
     int st = 0;
@@ -74,8 +80,8 @@ __global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
       __syncwarp();
       unsigned char *stage = ws + st * TL::kBytes;
       const int r0 = tile * kTile, rows = min(kTile, hd.n - r0);
-      if (STEP && hd.len >= r0 && hd.len - r0 < rows)
-        append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, qv);
+      if (STEP && tile == new_tile)
+        append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, nr, qv);
       attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
       if (STAGES == 1) break;  // no warp has a second tile
       __syncwarp();            // the stage and the weights are rewritten from here on
@@ -236,12 +242,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
     int hl = s_head[warp], base = s_base[warp], tile = run0 - base, st = 0;
     HeadRef nx = hd;
     float qv[E], qn[E];  // this head's query, the next one's
-    auto fetch_q = [&](int h, float (&q)[E]) {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        q[e] = (float)static_cast<const T *>(p.q)[(size_t)h * D + lane * E + e];
-    };
-    fetch_q(hl, qn);
+    load_query<D, T>(p, hl, qn);
     __half *operand = reinterpret_cast<__half *>(ws + SM::kOperand);
 
     while (left > 0) {
@@ -252,9 +253,13 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       for (int e = 0; e < E; ++e) qv[e] = qn[e];
       if (more) {
         nx = head_ref<STEP>(p, hl + 1);
-        fetch_q(hl + 1, qn);
+        load_query<D, T>(p, hl + 1, qn);
       }
       if (hd.bad && tile == 0 && lane == 0) set_err(c.err, hd.bad);
+      NewRow nr;
+      const int new_tile = STEP && !hd.bad ? hd.len / kTile : -1;
+      const bool appends = new_tile >= tile && new_tile - tile < left;
+      if (appends) load_new_row<D, T>(p, hl, nr);
       const Query<D, BITS> qr = make_query<D, BITS>(qv, p.qscale, operand);
       float m = -INFINITY, l = 0.f;
       float acc[KM][2];
@@ -267,9 +272,8 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         unsigned char *stage = ws + st * SM::kStage;
         const int r0 = tile * kTile;
         const int rows = hd.bad ? 0 : min(kTile, hd.n - r0);
-        if (STEP && hd.len - r0 < rows && rows > 0 && hd.len >= r0) {
-          append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, qv);
-        }
+        if (STEP && appends && tile == new_tile)
+          append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, nr, qv);
         if (rows > 0) attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
         __syncwarp();  // the stage and the weights are rewritten from here on
         issue();

@@ -284,30 +284,40 @@ __device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32], 
   return r;
 }
 
-// The step's new token: its K and V quantised to arena row hd.off + hd.len and
-// to row r of the tile, its query (qv) and position stored.
+// The step's new token, as the warp that holds its tile loads it: 8 channels of
+// K (the first D / 8 lanes) or V (the next), and the token's number.
+struct NewRow {
+  float x[8];
+  int ntok;
+};
+template <int D, typename T>
+__device__ __forceinline__ void load_new_row(const QAttnArgs &p, int hl, NewRow &nr) {
+  const int lane = threadIdx.x & 31;
+  if (lane < D / 4)
+    load8<T>(static_cast<const T *>(lane < D / 8 ? p.k_new : p.v_new) + (size_t)hl * D +
+                 lane % (D / 8) * 8,
+             nr.x);
+  nr.ntok = p.q8.c.ntok[p.base + hl];
+}
+
+// Quantises it to arena row hd.off + hd.len and to row r of the tile, and
+// stores its query (qv) and position.
 template <int D, typename T, int BITS>
 __device__ __forceinline__ void append_row(const QAttnArgs &p, int hl, const HeadRef &hd,
-                                           unsigned char *stage, int r,
+                                           unsigned char *stage, int r, const NewRow &nr,
                                            const float (&qv)[D / 32]) {
-  // the new row: quantised into the arena and into the tile
   using R = QRow<D, BITS>;
   using TL = TileOf<D, BITS>;
   constexpr int RB = R::kBytes, SB = R::kScaleBytes, G = R::kGroups, E = D / 32;
   const CacheArgs &c = p.q8.c;
-  const int i = p.base + hl, lane = threadIdx.x & 31;
-  unsigned char *sk = stage, *sv = sk + TL::kCodes, *ss = sv + TL::kCodes;
-  const int ntok = c.ntok[i];
+  const int lane = threadIdx.x & 31;
   if (lane < D / 4) {
-    constexpr int TPR = D / 8;
-    const int kv = lane / TPR, col = lane % TPR;
-    float x[8];
-    load8<T>(static_cast<const T *>(kv ? p.v_new : p.k_new) + (size_t)hl * D + col * 8, x);
+    const int kv = lane / (D / 8), col = lane % (D / 8);
     uint32_t a, b;
-    const uint32_t sb = quant_group<BITS>(x, 0xFu << (lane & 28), a, b);
+    const uint32_t sb = quant_group<BITS>(nr.x, 0xFu << (lane & 28), a, b);
     const size_t at = (size_t)(hd.off + hd.len);
     unsigned char *row = static_cast<unsigned char *>(kv ? c.V : c.K) + at * RB;
-    unsigned char *to = kv ? sv : sk;
+    unsigned char *to = stage + kv * TL::kCodes;
     if (BITS == 8) {
       reinterpret_cast<uint2 *>(row)[col] = make_uint2(a, b);
       *reinterpret_cast<uint2 *>(to + piece_at<RB>(r, col >> 1) + (col & 1) * 8) =
@@ -318,14 +328,24 @@ __device__ __forceinline__ void append_row(const QAttnArgs &p, int hl, const Hea
     }
     if ((col & 3) == 0) {
       static_cast<uint16_t *>(kv ? p.q8.vs : p.q8.ks)[at * G + col / 4] = (uint16_t)sb;
-      reinterpret_cast<uint16_t *>(ss + kv * TL::kScales + r * SB)[col / 4] = (uint16_t)sb;
+      reinterpret_cast<uint16_t *>(stage + 2 * TL::kCodes + kv * TL::kScales + r * SB)[col / 4] =
+          (uint16_t)sb;
     }
   }
-  T *ring = static_cast<T *>(c.qbuf) + ((size_t)i * p.P + ntok % p.P) * D;
+  T *ring = static_cast<T *>(c.qbuf) + ((size_t)(p.base + hl) * p.P + nr.ntok % p.P) * D;
 #pragma unroll
   for (int e = 0; e < E; ++e) ring[lane * E + e] = (T)qv[e];
-  if (lane == 0) c.pos[hd.off + hd.len] = p.C + ntok;
+  if (lane == 0) c.pos[hd.off + hd.len] = p.C + nr.ntok;
   __syncwarp();
+}
+
+// The lane's channels of a head's query.
+template <int D, typename T>
+__device__ __forceinline__ void load_query(const QAttnArgs &p, int hl, float (&q)[D / 32]) {
+  constexpr int E = D / 32;
+  const T *from = static_cast<const T *>(p.q) + (size_t)hl * D + (threadIdx.x & 31) * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) q[e] = (float)from[e];
 }
 
 // One tile into the running maximum m, the lane's part of the sum l, and the
