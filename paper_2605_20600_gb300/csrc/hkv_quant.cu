@@ -18,7 +18,7 @@ __device__ __forceinline__ bool segment_ok(long long off, int cap, int len, long
 // One CTA: up to kRowsPerCta rows of one head. Block 0 of a head also sets
 // its counters.
 template <int D, typename T, int BITS>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 5)
     pack_kernel(const CacheArgs src, const QCacheArgs dst, int first, int blocks, int skip,
                 int max_len) {
   using R = QRow<D, BITS>;
@@ -50,23 +50,42 @@ __global__ void __launch_bounds__(kRowThreads)
   }
   const int r_end = min(n, (b + 1) * kRowsPerCta);
   const int col = tid % TPR;
-  for (int r = b * kRowsPerCta + tid / TPR; r < r_end; r += kRowThreads / TPR) {
-    const long long so = soff + skip + r, dof = doff + r;
-    const uint32_t mask = 0xFu << (threadIdx.x & 28);  // the four lanes of a group
+  const uint32_t mask = 0xFu << (threadIdx.x & 28);  // the four lanes of a group
+  constexpr int STEP = kRowThreads / TPR, U = 2;  // rows in flight a thread
+  constexpr int PCS = (int)sizeof(T) / 2;         // 16-byte pieces of 8 values
+  for (int r0 = b * kRowsPerCta + tid / TPR; r0 < r_end; r0 += U * STEP) {
+    uint4 raw[U][2][PCS];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      float x[8];
-      const T *row = static_cast<const T *>(kv ? src.V : src.K) + so * D;
-      load8<T>(row + col * 8, x);
-      uint32_t lo, hi;
-      const uint32_t sb = quant_group<BITS>(x, mask, lo, hi);
-      unsigned char *out = static_cast<unsigned char *>(kv ? dst.c.V : dst.c.K) + dof * R::kBytes;
-      if (BITS == 8) reinterpret_cast<uint2 *>(out)[col] = make_uint2(lo, hi);
-      else reinterpret_cast<uint32_t *>(out)[col] = lo;
-      if ((col & 3) == 0)
-        static_cast<uint16_t *>(kv ? dst.vs : dst.ks)[dof * R::kGroups + col / 4] = (uint16_t)sb;
+    for (int u = 0; u < U; ++u) {
+      if (r0 + u * STEP < r_end) {
+        const long long so = ((soff + skip + r0 + u * STEP) * (D / 8) + col) * PCS;
+#pragma unroll
+        for (int j = 0; j < PCS; ++j) {
+          raw[u][0][j] = static_cast<const uint4 *>(src.K)[so + j];
+          raw[u][1][j] = static_cast<const uint4 *>(src.V)[so + j];
+        }
+      }
     }
-    if (col == 0) dst.c.pos[dof] = src.pos[so] - skip;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * STEP;
+      if (r >= r_end) break;
+      const long long dof = doff + r;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < PCS; ++j) Elem<T>::unpack(raw[u][kv][j], x + j * Elem<T>::kPerPiece);
+        uint32_t lo, hi;
+        const uint32_t sb = quant_group<T, BITS>(x, mask, lo, hi);
+        unsigned char *out = static_cast<unsigned char *>(kv ? dst.c.V : dst.c.K) + dof * R::kBytes;
+        if (BITS == 8) reinterpret_cast<uint2 *>(out)[col] = make_uint2(lo, hi);
+        else reinterpret_cast<uint32_t *>(out)[col] = lo;
+        if ((col & 3) == 0)
+          static_cast<uint16_t *>(kv ? dst.vs : dst.ks)[dof * R::kGroups + col / 4] = (uint16_t)sb;
+      }
+      if (col == 0) dst.c.pos[dof] = src.pos[soff + skip + r] - skip;
+    }
   }
 }
 
@@ -86,7 +105,7 @@ __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, const fl
 }
 
 template <int D, typename T, int BITS>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 6)
     unpack_kernel(const QCacheArgs src, const CacheArgs dst, int first, int blocks, int max_len) {
   using R = QRow<D, BITS>;
   constexpr int TPR = D / 8;
@@ -112,32 +131,41 @@ __global__ void __launch_bounds__(kRowThreads)
   }
   const int r_end = min(n, (b + 1) * kRowsPerCta);
   const int col = tid % TPR;
-  for (int r = b * kRowsPerCta + tid / TPR; r < r_end; r += kRowThreads / TPR) {
-    const long long so = soff + r, dof = doff + r;
+  constexpr int STEP = kRowThreads / TPR, U = 2;  // rows in flight a thread
+  for (int r0 = b * kRowsPerCta + tid / TPR; r0 < r_end; r0 += U * STEP) {
+    uint2 w[U][2];
+    uint32_t sc[U][2];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const unsigned char *row =
-          static_cast<const unsigned char *>(kv ? src.c.V : src.c.K) + so * R::kBytes;
-      const float s = bf16_bits_to_float(
-          static_cast<const uint16_t *>(kv ? src.vs : src.ks)[so * R::kGroups + col / 4]);
-      uint32_t lo, hi = 0;
-      if (BITS == 8) {
-        const uint2 u = reinterpret_cast<const uint2 *>(row)[col];
-        lo = u.x;
-        hi = u.y;
-      } else {
-        lo = reinterpret_cast<const uint32_t *>(row)[col];
-      }
-      float x[8];
+    for (int u = 0; u < U; ++u) {
+      if (r0 + u * STEP < r_end) {
+        const long long so = soff + r0 + u * STEP;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = BITS == 4 ? (int)((lo >> (4 * j)) & 15u)
-                                : (int)(((j < 4 ? lo : hi) >> (8 * (j & 3))) & 255u);
-        x[j] = s * (float)(c - R::kBias);
+        for (int kv = 0; kv < 2; ++kv) {
+          const unsigned char *row =
+              static_cast<const unsigned char *>(kv ? src.c.V : src.c.K) + so * R::kBytes;
+          w[u][kv].y = 0;
+          if (BITS == 8) w[u][kv] = reinterpret_cast<const uint2 *>(row)[col];
+          else w[u][kv].x = reinterpret_cast<const uint32_t *>(row)[col];
+          sc[u][kv] = static_cast<const uint16_t *>(kv ? src.vs : src.ks)[so * R::kGroups + col / 4];
+        }
       }
-      store8<T>(static_cast<T *>(kv ? dst.V : dst.K) + dof * D + col * 8, x);
     }
-    if (col == 0) dst.pos[dof] = src.c.pos[so];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * STEP;
+      if (r >= r_end) break;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const float s = bf16_bits_to_float(sc[u][kv]);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[j] = s * (BITS == 4 ? code4(w[u][kv].x, j)
+                                : code8(j < 4 ? w[u][kv].x : w[u][kv].y, j & 3));
+        store8<T>(static_cast<T *>(kv ? dst.V : dst.K) + (doff + r) * D + col * 8, x);
+      }
+      if (col == 0) dst.pos[doff + r] = src.c.pos[soff + r];
+    }
   }
 }
 
@@ -149,19 +177,20 @@ struct CodeRows {
   static constexpr int kBytes = QRow<D, BITS>::kBytes;
   const uint16_t *scale;  // the segment's first row
   __device__ __forceinline__ float dot(const unsigned char *krow, const float *qbar, int r) const {
-    constexpr int G = QRow<D, BITS>::kGroups, BIAS = QRow<D, BITS>::kBias;
-    constexpr int WPG = BITS;  // 32-bit words per group of 32 codes
+    constexpr int G = QRow<D, BITS>::kGroups, PPG = BITS / 4;  // 16-byte pieces a group
     float s = 0.f;
-#pragma unroll
+#pragma unroll 1
     for (int g = 0; g < G; ++g) {
       const float sc = bf16_bits_to_float(scale[(size_t)r * G + g]);
 #pragma unroll
-      for (int w = 0; w < WPG; ++w) {
-        const uint32_t u = reinterpret_cast<const uint32_t *>(krow)[g * WPG + w];
+      for (int pc = 0; pc < PPG; ++pc) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(krow + (g * PPG + pc) * 16);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const float *q = qbar + g * 32 + pc * (128 / BITS);
 #pragma unroll
-        for (int j = 0; j < 32 / BITS; ++j) {
-          const float c = (float)((int)((u >> (BITS * j)) & (BITS == 8 ? 255u : 15u)) - BIAS);
-          s = __fadd_rn(s, __fmul_rn(qbar[g * 32 + w * (32 / BITS) + j], __fmul_rn(sc, c)));
+        for (int j = 0; j < 128 / BITS; ++j) {
+          const float c = BITS == 8 ? code8(w[j / 4], j % 4) : code4(w[j / 8], j % 8);
+          s = __fadd_rn(s, __fmul_rn(q[j], __fmul_rn(sc, c)));
         }
       }
     }
@@ -202,7 +231,7 @@ __global__ void __launch_bounds__(NT, kQuantUpdCtasPerSm)
   int32_t *pos = c.pos + off;
   const unsigned char *ring =
       static_cast<const unsigned char *>(c.qbuf) + (size_t)i * m.P * D * sizeof(T);
-  const UpdSmem u = carve(dyn, max_len, D, m.P, (int)sizeof(T));
+  const UpdSmem u = carve(dyn, max_len, D, m.P, (int)sizeof(T), KB);
   SegRef sg{K, V, pos, K, V, pos, len, cp, true, c.err};
   const CodeRows<D, BITS> rows{reinterpret_cast<const uint16_t *>(KS)};
   const int M = select_evictions<D, T>(sg, lab, m, ring, ntok, u, sh, rows);
@@ -264,6 +293,10 @@ cudaError_t launch_quant_unpack(const QCacheArgs &src, const CacheArgs &dst, int
   return cudaErrorInvalidValue;
 }
 
+size_t quant_evict_smem(int max_len, int D, int P, int dtype, int bits) {
+  return update_smem_of(max_len, D, P, dtype == HKV_BF16 ? 2 : 4, D * bits / 8);
+}
+
 cudaError_t quant_evict_prepare(int D, int dtype, int bits, size_t smem) {
   HKV_QDISPATCH(D, dtype, bits, {
     cudaError_t e = cudaFuncSetAttribute(quant_evict_kernel<kD, kT, kBits>,
@@ -278,7 +311,7 @@ cudaError_t quant_evict_prepare(int D, int dtype, int bits, size_t smem) {
 
 cudaError_t launch_quant_evict(const QCacheArgs &c, const MethodArgs &m, int first, int count,
                                int D, int dtype, int bits, size_t smem, cudaStream_t s) {
-  const int max_len = update_max_len(smem, D, m.P, dtype == HKV_BF16 ? 2 : 4);
+  const int max_len = update_max_len(smem, D, m.P, dtype == HKV_BF16 ? 2 : 4, D * bits / 8);
   HKV_QDISPATCH(D, dtype, bits,
                 return pdl_launch(quant_evict_kernel<kD, kT, kBits>, count, NT, smem, s, c, m,
                                   first, max_len));

@@ -36,13 +36,32 @@ __device__ __forceinline__ float bf16_bits_to_float(uint32_t b) {
   return __uint_as_float(b << 16);
 }
 
+// A stored code as the fp32 number it stands for before its scale: byte b of w
+// (8 bits) or nibble n of w (4 bits), less the bias. 0x4B0000uu is the fp32
+// number 2^23 + uu.
+__device__ __forceinline__ float code8(uint32_t w, int b) {
+  return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + b)) - (8388608.f + 128.f);
+}
+__device__ __forceinline__ float code4(uint32_t w, int n) {
+  return __uint_as_float(((w >> (4 * n)) & 15u) | 0x4B000000u) - (8388608.f + 8.f);
+}
+
 // Quantises a group of 32 values held by four neighbouring lanes (8 each, in
-// channel order; the four call together, `mask` names the lanes of the warp
-// that call). Returns the scale's bf16 bits (the same in the four lanes) and
-// leaves this lane's biased codes in lo and hi: 8 bits, bytes of lo then hi;
-// 4 bits, nibbles of lo. The magnitudes are compared as integers, so that a
-// NaN or an infinity in the group shows (its bits are the largest).
-template <int BITS>
+// channel order; the four call together, `mask` names them). Returns the
+// scale's bf16 bits (the same in the four lanes) and leaves this lane's biased
+// codes in lo and hi: 8 bits, bytes of lo then hi; 4 bits, nibbles of lo. The
+// magnitudes are compared as integers, so that a NaN or an infinity in the
+// group shows (its bits are the largest).
+//
+// bf16 values, without a division: q = x * rcp(s) is within 2^-21 of x / s;
+// q + (x - q s) rcp(s), the remainder exact in an fma, is within 2^-40, so a
+// quotient that fp32 holds comes out exactly, every tie k + 1/2 among them.
+// Other quotients are at least 2^-16 from a tie (x and s have 8 bits and k + 1/2
+// at most 8: 2 x and (2 k + 1) s are integers below 2^16 on a common grid), so
+// adding 1.5 * 2^23 rounds them as x / s itself would be. a / M is at least as
+// far from the midpoint of two bf16 numbers, so a product with 1 / M rounds
+// alike. fp32 values, and groups whose scale is tiny, take the quotients.
+template <typename T, int BITS>
 __device__ __forceinline__ uint32_t quant_group(const float *x, uint32_t mask, uint32_t &lo,
                                                 uint32_t &hi) {
   constexpr int kMax = BITS == 8 ? 127 : 7, kBias = BITS == 8 ? 128 : 8;
@@ -51,19 +70,38 @@ __device__ __forceinline__ uint32_t quant_group(const float *x, uint32_t mask, u
   for (int j = 0; j < 8; ++j) a = max(a, __float_as_uint(x[j]) & 0x7FFFFFFFu);
   a = max(a, __shfl_xor_sync(mask, a, 1));
   a = max(a, __shfl_xor_sync(mask, a, 2));
-  const bool finite = a < 0x7F800000u;
-  const float q = __fdiv_rn(__uint_as_float(a), (float)kMax);
-  const uint32_t sb = finite ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(q)) : 0x7FC0u;
-  const float s = bf16_bits_to_float(sb);
-  lo = hi = 0;
+  uint32_t c[8];  // biased codes in the low bits, something above them
+  float s;
+  uint32_t sb;
+  if (sizeof(T) == 2 && a >= 0x0E000000u && a < 0x7F800000u) {  // 2^-99 <= a, finite
+    constexpr float kMagic = 12582912.f + kBias;
+    sb = __bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(a) * (1.f / kMax)));
+    s = bf16_bits_to_float(sb);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    int c = 0;
-    if (s > 0.f) c = max(-kMax, min(kMax, __float2int_rn(__fdiv_rn(x[j], s))));
-    const uint32_t b = (uint32_t)(c + kBias);
-    if (BITS == 4) lo |= b << (4 * j);
-    else if (j < 4) lo |= b << (8 * j);
-    else hi |= b << (8 * (j - 4));
+    for (int j = 0; j < 8; ++j) {
+      const float q = x[j] * inv;
+      c[j] = __float_as_uint(__fadd_rn(fmaf(fmaf(-q, s, x[j]), inv, q), kMagic));
+    }
+  } else {
+    const bool finite = a < 0x7F800000u;
+    const float q = __fdiv_rn(__uint_as_float(a), (float)kMax);
+    sb = finite ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(q)) : 0x7FC0u;
+    s = bf16_bits_to_float(sb);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      c[j] = (uint32_t)(kBias + (s > 0.f ? max(-kMax, min(kMax, __float2int_rn(__fdiv_rn(x[j], s))))
+                                         : 0));
+  }
+  if (BITS == 8) {
+    lo = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    hi = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+  } else {
+    lo = c[0] & 15u;
+#pragma unroll
+    for (int j = 1; j < 8; ++j) lo |= (c[j] & 15u) << (4 * j);
+    hi = 0;
   }
   return sb;
 }

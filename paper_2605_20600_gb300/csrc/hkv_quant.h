@@ -23,7 +23,9 @@ cudaError_t launch_quant_pack(const CacheArgs &src, const QCacheArgs &dst, int f
 cudaError_t launch_quant_unpack(const QCacheArgs &src, const CacheArgs &dst, int first, int count,
                                 int max_len, int D, int dtype, int bits, cudaStream_t s);
 
-// the periodic update; smem from update_smem_bytes
+// the periodic update; smem from quant_evict_smem (which, unlike that of a
+// plain cache's update, goes by the rows' codes)
+size_t quant_evict_smem(int max_len, int D, int P, int dtype, int bits);
 cudaError_t quant_evict_prepare(int D, int dtype, int bits, size_t smem);
 cudaError_t launch_quant_evict(const QCacheArgs &c, const MethodArgs &m, int first, int count,
                                int D, int dtype, int bits, size_t smem, cudaStream_t s);
@@ -37,8 +39,8 @@ struct QAttnArgs {
   const float *prior_out, *prior_lse;     // [nheads][D], [nheads], or both null
   float *out, *lse;                       // [nheads][D], [nheads] or null
   uint32_t *count;             // [nheads] arrivals, zero between launches
-  uint32_t *done;              // [2] CTAs on their way and heads left to the
-                               // last one, zero between launches
+  uint32_t *done;              // [2] CTAs that have read the lengths and heads
+                               // left to the last one, zero between launches
   float *part;                 // [kQuantMaxGrid][2][D + 4] partial results
   int max_rows;                // rows of the longest segment
   int sms;

@@ -15,8 +15,7 @@
 // does not depend on who is last. No CTA waits for another.
 //
 // Every CTA reads the layer's lengths to find its run, so a step may advance a
-// head's counters only when all have: whoever finishes a head advances them if
-// every CTA has reported that, else leaves it to the CTA that exits last.
+// head's counters only when all have (advance_or_leave).
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_quant_tile.cuh"
@@ -131,20 +130,36 @@ struct Smem {
   static_assert(kStage >= D * 4, "the last piece takes a tile's place");
 };
 
-// A finished head's counters advance now, or are left to the CTA that exits
-// last. done[0]: CTAs that have read the lengths (low half) and exited (high
-// half); done[1]: heads left to the last; kLater marks them in count[].
-constexpr uint32_t kLater = 0x80000000u;
-__device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense) {
+// A finished head's counters may advance when every CTA has read the lengths.
+// done[0] counts the CTAs that have (and wraps to zero at the last one, so that
+// it reads zero from then on and at the next launch). Who finishes a head
+// earlier than that leaves it: a mark in count[], counted in done[1]. The CTA
+// that reads last takes the marks over; between the two, whoever takes the
+// mark out advances the head.
+constexpr uint32_t kLeft = 0x80000000u;
+
+__device__ __forceinline__ void take_left(const QAttnArgs &p, int hl, bool dense) {
+  if (atomicCAS(p.count + hl, kLeft, 0u) != kLeft) return;
+  atomicSub(p.done + 1, 1u);
+  advance_head(p, hl, dense);
+}
+// `reported`: whether this CTA has (zero also means that none has yet)
+__device__ __forceinline__ bool all_read(const QAttnArgs &p, volatile int *reported) {
+  if (!*reported) return false;
   uint32_t v;
   asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.done) : "memory");
-  if ((v & 0xFFFFu) == gridDim.x) {
+  return v == 0u;
+}
+__device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense,
+                                                 volatile int *reported) {
+  if (all_read(p, reported)) {
     advance_head(p, hl, dense);
-  } else {
-    p.count[hl] = kLater;
-    atomicAdd(p.done + 1, 1u);
-    __threadfence();
+    return;
   }
+  atomicAdd(p.done + 1, 1u);
+  atomicExch(p.count + hl, kLeft);
+  __threadfence();  // the mark, then the look back; the last reader the other way round
+  if (all_read(p, reported)) take_left(p, hl, dense);
 }
 
 template <int D, typename T, int BITS, bool STEP>
@@ -158,13 +173,14 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   extern __shared__ __align__(16) unsigned char dyn[];
   // the runs' first heads, and those heads' first tiles in the layer
   __shared__ int s_head[WARPS], s_base[WARPS], s_scan[33];
+  __shared__ HeadRef s_ref[WARPS];
+  __shared__ int s_reported;
   // pieces of heads that a warp does not hold whole: [0] its run starts inside
   // the head, [1] the head starts in its run
   __shared__ float s_m[WARPS][2], s_l[WARPS][2];
   __shared__ int s_piece[WARPS][2];  // head, -1 for none
   __shared__ int s_ends[WARPS][2];   // whether the head ends with the piece
   __shared__ int s_first[WARPS][2], s_tiles[WARPS][2];  // the head's first tile and tiles
-  __shared__ uint32_t s_later;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const CacheArgs &c = p.q8.c;
   if (!p.prefetch) pdl_wait();
@@ -173,10 +189,21 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   // thread; each warp gets `share` tiles, the first `rest` warps one more
   const int hp = (p.nheads + THREADS - 1) / THREADS;
   const int h0 = min(tid * hp, p.nheads), h1 = min(h0 + hp, p.nheads);
-  const int len0 = h0 < h1 ? c.len[p.base + h0] : 0;
-  int mine = h0 < h1 ? head_tiles<STEP>(len0, p.max_rows) : 0;
+  // (up to two heads a thread, with all that the runs' first heads need)
+  HeadRef ref[2] = {};
+  int mine = 0;
+  if (hp <= 2) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (h0 + j < h1) {
+        ref[j] = head_ref<STEP>(p, h0 + j);
+        mine += ref[j].tiles;
+      }
+    }
+  } else {
 #pragma unroll 8
-  for (int h = h0 + 1; h < h1; ++h) mine += head_tiles<STEP>(c.len[p.base + h], p.max_rows);
+    for (int h = h0; h < h1; ++h) mine += head_tiles<STEP>(c.len[p.base + h], p.max_rows);
+  }
   int total;
   const int before = block_excl_scan<int>(mine, s_scan, &total);
   const int ctas = min((int)gridDim.x, (total + WARPS - 1) / WARPS);
@@ -187,17 +214,24 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   int left = cta < ctas ? run_start(cta * WARPS + warp + 1) - run0 : 0;
   if (cta < ctas) {
     if (tid < WARPS * 2) s_piece[tid >> 1][tid & 1] = -1;
+    if (tid == 0) s_reported = 0;
 #pragma unroll 1
     for (int w = 0; w < WARPS; ++w) {
       const int t = run_start(cta * WARPS + w);
       if (t >= before && t < before + mine) {
         int at = before, h = h0;
-        if (h1 - h0 > 1) {
+        if (hp <= 2) {
+          const bool second = t >= before + ref[0].tiles;
+          h += second;
+          at += second ? ref[0].tiles : 0;
+          s_ref[w] = second ? ref[1] : ref[0];
+        } else {
           for (; h < h1 - 1; ++h) {
             const int nt = head_tiles<STEP>(c.len[p.base + h], p.max_rows);
             if (t < at + nt) break;
             at += nt;
           }
+          s_ref[w] = head_ref<STEP>(p, h);
         }
         s_head[w] = h;
         s_base[w] = at;
@@ -213,7 +247,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   if (left > 0) {
     pl_head = s_head[warp];
     pl_tile = run0 - s_base[warp];
-    pr = head_ref<STEP>(p, pl_head);
+    pr = s_ref[warp];
   }
   HeadRef hd = pr;
   auto issue = [&]() {
@@ -235,8 +269,23 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
   for (int st = 0; st < STAGES; ++st) issue();
   if (p.prefetch) pdl_wait();  // the step's inputs are visible from here on
   pdl_launch_dependents();
-  // this CTA's runs are found (the barrier above): it has read the lengths
-  if (STEP && tid == 0) atomicAdd(p.done, 1u);
+  if (STEP && warp == WARPS - 1) {
+    // this CTA's runs are found (the barrier above): it has read the lengths
+    uint32_t old = 0;
+    if (lane == 0) {
+      old = atomicInc(p.done, gridDim.x - 1u);
+      *reinterpret_cast<volatile int *>(&s_reported) = 1;
+    }
+    if (__shfl_sync(0xFFFFFFFFu, old, 0) == gridDim.x - 1u) {  // the last to
+      __threadfence();
+      uint32_t marks = 0;
+      if (lane == 0) marks = *reinterpret_cast<volatile uint32_t *>(p.done + 1);
+      if (__shfl_sync(0xFFFFFFFFu, marks, 0) != 0u)
+        for (int h = lane; h < p.nheads; h += 32)
+          if (*reinterpret_cast<volatile uint32_t *>(p.count + h) == kLeft)
+            take_left(p, h, c.label[p.base + h] == HKV_DENSE);
+    }
+  }
 
   if (left > 0) {
     int hl = s_head[warp], base = s_base[warp], tile = run0 - base, st = 0;
@@ -295,7 +344,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
 #pragma unroll
           for (int e = 0; e < E; ++e) o[e] = to[lane * E + e];
           finish_head<D>(p, hl, m, l, o);
-          if (STEP && lane == 0) advance_or_leave(p, hl, hd.dense);
+          if (STEP && lane == 0) advance_or_leave(p, hl, hd.dense, &s_reported);
         } else if (lane == 0) {
           const int slot = starts ? 1 : 0;
           s_m[warp][slot] = m;
@@ -344,7 +393,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       const bool dense = STEP ? c.label[p.base + h] == HKV_DENSE : false;
       if (slot == 1 && ends) {
         finish_head<D>(p, h, m, l, o);
-        if (STEP && lane == 0) advance_or_leave(p, h, dense);
+        if (STEP && lane == 0) advance_or_leave(p, h, dense, &s_reported);
         continue;
       }
       // cut between CTAs: this one's part to the workspace
@@ -408,27 +457,9 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       finish_head<D>(p, h, m, l, o);
       if (lane == 0) {
         p.count[h] = 0u;
-        if (STEP) advance_or_leave(p, h, dense);
+        if (STEP) advance_or_leave(p, h, dense, &s_reported);
       }
     }
-  }
-  if (!STEP) return;
-  __syncthreads();  // this CTA's heads are advanced or left
-  if (tid == 0) {
-    uint32_t later = 0;
-    if ((atomicAdd(p.done, 1u << 16) >> 16) == gridDim.x - 1u) {
-      __threadfence();
-      later = atomicExch(p.done + 1, 0u);
-      *p.done = 0u;
-    }
-    s_later = later;
-  }
-  __syncthreads();
-  if (s_later == 0) return;
-  for (int h = tid; h < p.nheads; h += THREADS) {
-    if (__ldcg(p.count + h) != kLater) continue;
-    p.count[h] = 0u;
-    advance_head(p, h, c.label[p.base + h] == HKV_DENSE);
   }
 }
 

@@ -151,8 +151,7 @@ __device__ __forceinline__ int piece_at(int r, int c) {
 struct HeadRef {
   long long off;
   int len, n, tiles;   // old rows, rows to attend over, tiles (at least one)
-  uint32_t bad;        // status of a head that cannot be served
-  bool dense;
+  uint16_t bad, dense; // status of a head that cannot be served; its label
 };
 
 // Tiles of a head of `len` rows: one at least, so that some warp reports,
@@ -314,7 +313,7 @@ __device__ __forceinline__ void append_row(const QAttnArgs &p, int hl, const Hea
   if (lane < D / 4) {
     const int kv = lane / (D / 8), col = lane % (D / 8);
     uint32_t a, b;
-    const uint32_t sb = quant_group<BITS>(nr.x, 0xFu << (lane & 28), a, b);
+    const uint32_t sb = quant_group<T, BITS>(nr.x, 0xFu << (lane & 28), a, b);
     const size_t at = (size_t)(hd.off + hd.len);
     unsigned char *row = static_cast<unsigned char *>(kv ? c.V : c.K) + at * RB;
     unsigned char *to = stage + kv * TL::kCodes;

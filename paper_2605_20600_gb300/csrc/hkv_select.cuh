@@ -77,17 +77,19 @@ __host__ __device__ constexpr int stage_rows(int max_len) {
 
 // the query ring (P rows of es-byte elements); after q-bar it is the score
 // stage: NT/32 warps x stage_rows rows of D * es + 16 bytes
-__host__ __device__ constexpr size_t ring_bytes(int P, int D, int es, int max_len) {
-  return (size_t)P * D * es > (size_t)(NT / 32) * stage_rows(max_len) * (D * es + 16)
-             ? (size_t)P * D * es
-             : (size_t)(NT / 32) * stage_rows(max_len) * (D * es + 16);
+// (or of kb + 16, key rows of kb bytes)
+__host__ __device__ constexpr size_t ring_bytes(int P, int D, int es, int max_len, int kb = 0) {
+  const size_t ring = (size_t)P * D * es;
+  const size_t stage = (size_t)(NT / 32) * stage_rows(max_len) * ((kb ? kb : D * es) + 16);
+  return ring > stage ? ring : stage;
 }
 
-__device__ __forceinline__ UpdSmem carve(unsigned char *dyn, int max_len, int D, int P, int es) {
+__device__ __forceinline__ UpdSmem carve(unsigned char *dyn, int max_len, int D, int P, int es,
+                                         int kb = 0) {
   UpdSmem u;
   u.ring = dyn;
   u.stage_rows = stage_rows(max_len);
-  u.keys = reinterpret_cast<unsigned long long *>(dyn + ring_bytes(P, D, es, max_len));
+  u.keys = reinterpret_cast<unsigned long long *>(dyn + ((ring_bytes(P, D, es, max_len, kb) + 7) & ~(size_t)7));
   u.ps = reinterpret_cast<int *>(u.keys + max_len);
   u.aux = u.ps + max_len;
   u.qbar = reinterpret_cast<float *>(u.aux + max_len);
@@ -424,19 +426,19 @@ inline cudaError_t allow_smem_of(void (*kernel)(KArgs...), int smem, std::atomic
   return e;
 }
 
-inline size_t update_smem_of(int max_len, int D, int P, int es) {
+inline size_t update_smem_of(int max_len, int D, int P, int es, int kb = 0) {
   // the query ring / score stage; keys (8 B), positions (4 B), class/flag/
   // rank (4 B) per row; q-bar; two 256-bin histograms
-  return ring_bytes(P, D, es, max_len) + (size_t)max_len * 16 + (size_t)D * 4 + 512 * 4 + 64;
+  return ring_bytes(P, D, es, max_len, kb) + (size_t)max_len * 16 + (size_t)D * 4 + 512 * 4 + 64;
 }
 
 // the longest segment a launch with `smem` bytes takes (the inverse of
 // update_smem_of, which grows with max_len)
-inline int update_max_len(size_t smem, int D, int P, int es) {
+inline int update_max_len(size_t smem, int D, int P, int es, int kb = 0) {
   int lo = 0, hi = 1 << 20;
   while (lo < hi) {
     const int mid = lo + (hi - lo + 1) / 2;
-    if (update_smem_of(mid, D, P, es) <= smem) lo = mid;
+    if (update_smem_of(mid, D, P, es, kb) <= smem) lo = mid;
     else hi = mid - 1;
   }
   return lo;

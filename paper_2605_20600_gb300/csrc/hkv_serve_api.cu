@@ -156,7 +156,8 @@ hkv_status quant_evict(const char *name, const hkv_config *cfg, const hkv_qcache
   HKV_TRY(check_qcache(cache));
   int first, count;
   HKV_TRY(layer_heads(cfg, layer, &first, &count));
-  const size_t smem = update_smem_bytes(max_segment(cfg), cfg->head_dim, cfg->period, cfg->dtype);
+  const size_t smem = quant_evict_smem(max_segment(cfg), cfg->head_dim, cfg->period, cfg->dtype,
+                                       cache->format);
   HKV_TRY(evict_ready(cfg, cache->format, smem));
   return cuda_status(launch_quant_evict(qcache_args(cache), method_args(cfg), first, count,
                                         cfg->head_dim, cfg->dtype, cache->format, smem,
