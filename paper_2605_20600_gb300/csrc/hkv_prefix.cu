@@ -14,6 +14,7 @@
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
+#include "hkv_tcgen05.cuh"
 
 namespace hkv {
 namespace {
@@ -93,11 +94,11 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[3]) {
 
 // Copies `rows` rows of D elements into the planes at dst (row stride as
 // at16), rows from `live` on as zeros. bf16: asynchronous.
-template <int D, typename T>
+template <int D, typename T, int THREADS>
 __device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T *src,
                                           long long stride, int rows, int live) {
   constexpr int PPR = D / 8;
-  for (int e = threadIdx.x; e < rows * PPR; e += kThreads) {
+  for (int e = threadIdx.x; e < rows * PPR; e += THREADS) {
     const int r = e / PPR, c = e % PPR;
     const bool on = r < live;
     const T *from = src + (on ? r * stride : 0) + c * 8;
@@ -155,8 +156,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
 
   auto load_tile = [&](int k0, int st) {
     unsigned char *s = dyn + st * SM::kStage;
-    load_rows<D, T>(s, SM::kPlane, K + k0 * p.ts, p.ts, kKeys, hi - k0);
-    load_rows<D, T>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.ts, p.ts, kKeys, hi - k0);
+    load_rows<D, T, kThreads>(s, SM::kPlane, K + k0 * p.ts, p.ts, kKeys, hi - k0);
+    load_rows<D, T, kThreads>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.ts, p.ts, kKeys, hi - k0);
   };
 
   float o[D / 8][4];
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
   for (int x = 0; x < D / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   if (lo < hi) {
-    load_rows<D, T>(sq, SM::kQPlane, static_cast<const T *>(p.q) + qrow * D,
+    load_rows<D, T, kThreads>(sq, SM::kQPlane, static_cast<const T *>(p.q) + qrow * D,
                     (long long)p.heads * D, MW * 16, nq);
     asm volatile("cp.async.commit_group;" ::: "memory");
     if (STAGES > 1) {
@@ -180,10 +181,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
     const int q_row = mw * 16 + (mi & 1) * 8 + mr, q_pc = mi >> 1;
     const int k_row = kw * NKW + (mi >> 1) * 8 + mr, k_pc = mi & 1;
     const int v_row = kw * NKW + (mi & 1) * 8 + mr, v_pc = mi >> 1;
-    uint32_t qf[NP == 1 ? D / 16 : 1][4];
-
     int st = 0;
-    bool have_q = false;
     for (int k0 = lo; k0 < hi; k0 += kKeys) {
       if (STAGES == 1) {
         __syncthreads();  // the tile before this one has been read
@@ -192,11 +190,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       }
       __syncthreads();
-      if (NP == 1 && !have_q) {
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) ldm4(qf[ks], q_base + at16<D>(q_row, 2 * ks + q_pc));
-        have_q = true;
-      }
       const uint32_t kb = t_base + st * SM::kStage, vb = kb + NP * SM::kPlane;
       float s[NKW / 8][4];
 #pragma unroll
@@ -204,12 +197,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
       if (NP == 1) {
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
+          uint32_t qa[4];
+          ldm4(qa, q_base + at16<D>(q_row, 2 * ks + q_pc));
 #pragma unroll
           for (int nb = 0; nb < NKW / 16; ++nb) {
             uint32_t f[4];
             ldm4(f, kb + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
-            mma_bf16(s[2 * nb], qf[NP == 1 ? ks : 0], f[0], f[1]);
-            mma_bf16(s[2 * nb + 1], qf[NP == 1 ? ks : 0], f[2], f[3]);
+            mma_bf16(s[2 * nb], qa, f[0], f[1]);
+            mma_bf16(s[2 * nb + 1], qa, f[2], f[3]);
           }
         }
       } else {
@@ -280,39 +275,34 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
           for (int k = 0; k < 3; ++k) pf[x / 2][k][(x & 1) * 2 + j] = pr[k];
         }
       }
+      // 16 DBS channels at a time: 2 DBS chains of products side by side
+      constexpr int DBS = 1;
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) {
-        float t[2][4] = {};
-        if (NP == 1) {
-          uint32_t vf[NKW / 16][4];
+      for (int db = 0; db < D / 16; db += DBS) {
+        float t[2 * DBS][4] = {};
 #pragma unroll
-          for (int kk = 0; kk < NKW / 16; ++kk)
-            ldm4t(vf[kk], vb + at16<D>(v_row + kk * 16, 2 * db + v_pc));
+        for (int plane = NP - 1; plane >= 0; --plane) {  // parts of V, the small ones first
+          uint32_t vf[DBS][NKW / 16][4];
 #pragma unroll
-          for (int a = 2; a >= 0; --a) {
+          for (int x = 0; x < DBS; ++x)
+#pragma unroll
+            for (int kk = 0; kk < NKW / 16; ++kk)
+              ldm4t(vf[x][kk],
+                    vb + plane * SM::kPlane + at16<D>(v_row + kk * 16, 2 * (db + x) + v_pc));
+#pragma unroll
+          for (int a = 2 - plane; a >= 0; --a) {  // parts of w
 #pragma unroll
             for (int kk = 0; kk < NKW / 16; ++kk) {
-              mma_bf16(t[0], pf[kk][a], vf[kk][0], vf[kk][1]);
-              mma_bf16(t[1], pf[kk][a], vf[kk][2], vf[kk][3]);
-            }
-          }
-        } else {
 #pragma unroll
-          for (int order = 2; order >= 0; --order) {
-#pragma unroll
-            for (int a = order; a >= 0; --a) {
-#pragma unroll
-              for (int kk = 0; kk < NKW / 16; ++kk) {
-                uint32_t vf[4];
-                ldm4t(vf, vb + (order - a) * SM::kPlane + at16<D>(v_row + kk * 16, 2 * db + v_pc));
-                mma_bf16(t[0], pf[kk][a], vf[0], vf[1]);
-                mma_bf16(t[1], pf[kk][a], vf[2], vf[3]);
+              for (int x = 0; x < DBS; ++x) {
+                mma_bf16(t[2 * x], pf[kk][a], vf[x][kk][0], vf[x][kk][1]);
+                mma_bf16(t[2 * x + 1], pf[kk][a], vf[x][kk][2], vf[x][kk][3]);
               }
             }
           }
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2 * DBS; ++x)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[2 * db + x][e] += t[x][e];
       }
@@ -376,6 +366,226 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
   }
 }
 
+// Batches: up to 128 queries of one (group, head) a CTA, on tcgen05. Per tile of
+// 64 keys: S = Q K^T into TMEM; a thread per query reads its row of S, makes the
+// weights and writes them back as three bf16 parts, the A operand of O += W V.
+// O stays in TMEM; a query's reference maximum moves (and O and its sum are
+// rescaled) only when a tile's maximum is more than 2^8 above it, so that the
+// weights stay below 2^8. The copies of the next tile run meanwhile, and two
+// CTAs an SM fill each other's waits.
+constexpr int kTcQueries = 128, kTcThreads = 128;
+constexpr int kTcCols = 256, kTcP = 0, kTcO = 128;  // TMEM: S and the parts of W, then O
+
+template <int D>
+struct TcSmem {
+  static constexpr int kQ = kTcQueries * D * 2, kTile = kKeys * D * 2;
+  // 1024-byte aligned tiles; no less than 80 KB, so that at most two CTAs, and
+  // with them their TMEM, fit an SM
+  static constexpr int kUsed = kQ + 4 * kTile + 1024;
+  static constexpr int kTotal = kUsed > 80 * 1024 ? kUsed : 80 * 1024;
+};
+
+// `rows` rows of D elements as column blocks of 128 bytes, 128-byte swizzle;
+// rows from `live` on zero
+template <int D>
+__device__ __forceinline__ void tc_load_rows(unsigned char *dst, const __nv_bfloat16 *src,
+                                             long long stride, int rows, int live) {
+  constexpr int PPR = D / 8;
+  for (int e = threadIdx.x; e < rows * PPR; e += kTcThreads) {
+    const int r = e / PPR, c = e % PPR;
+    const bool on = r < live;
+    cp_async16_zfill(dst + (c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
+                     src + (on ? r * stride : 0) + c * 8, on);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTcThreads, 2)
+    prefix_tc_kernel(const PrefixArgs p, int split_len) {
+  using SM = TcSmem<D>;
+  constexpr int PF = D + 4;
+  extern __shared__ unsigned char dyn_raw[];
+  __shared__ uint64_t s_bar[2];  // S ready, O ready
+  __shared__ uint32_t s_tmem;
+  unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
+  const int tid = threadIdx.x, warp = tid >> 5;
+  int b = blockIdx.x;
+  const int tile = b % p.tiles;
+  b /= p.tiles;
+  const int h = b % p.heads;
+  b /= p.heads;
+  const int g = b % p.groups, sp = b / p.groups;
+  if (warp == 0) tmem_alloc(&s_tmem, kTcCols);
+  if (tid == 0) {
+    mbar_init(&s_bar[0], 1);
+    mbar_init(&s_bar[1], 1);
+    fence_barrier_init();
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  int len = p.len[g];
+  const bool bad = len < 0 || len > p.max_len;
+  if (bad) {
+    if (p.err && tid == 0 && sp == 0) set_err(p.err, HKV_ERR_BOUNDS);
+    len = 0;
+  }
+  const int q0 = tile * kTcQueries, nq = min(kTcQueries, p.seqs - q0);
+  const size_t qrow = ((size_t)g * p.seqs + q0) * p.heads + h;
+  const int lo = sp * split_len, hi = min(len, lo + split_len);
+  const __nv_bfloat16 *K = static_cast<const __nv_bfloat16 *>(p.k) + g * p.gs + h * p.hs;
+  const __nv_bfloat16 *V = static_cast<const __nv_bfloat16 *>(p.v) + g * p.gs + h * p.hs;
+  unsigned char *sq = dyn, *skv = dyn + SM::kQ;  // [stage][K, V]
+  auto load_tile = [&](int k0, int st) {
+    unsigned char *s = skv + st * 2 * SM::kTile;
+    tc_load_rows<D>(s, K + k0 * p.ts, p.ts, kKeys, hi - k0);
+    tc_load_rows<D>(s + SM::kTile, V + k0 * p.ts, p.ts, kKeys, hi - k0);
+  };
+  if (lo < hi) {
+    tc_load_rows<D>(sq, static_cast<const __nv_bfloat16 *>(p.q) + qrow * D,
+                    (long long)p.heads * D, kTcQueries, nq);
+    load_tile(lo, 0);
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem, mine = tmem + ((uint32_t)(warp * 32) << 16);
+  const bool works = warp * 32 < nq;  // this warp holds queries
+  float m = -INFINITY, l = 0.f;
+  bool ok = true;
+  uint32_t phase = 0;
+  int st = 0;
+  for (int k0 = lo; k0 < hi; k0 += kKeys, phase ^= 1, st ^= 1) {
+    // O holds the tiles before this one, and their stage is free
+    if (k0 > lo) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
+    if (__syncthreads_or(!ok)) break;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (k0 + kKeys < hi) load_tile(k0 + kKeys, st ^ 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const uint32_t kb = smem_u32(skv + st * 2 * SM::kTile), vb = kb + SM::kTile;
+    if (tid == 0) {
+      tc_fence_after();
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
+        tc_mma(tmem + kTcP,
+               tc_desc(smem_u32(sq) + (ks >> 2) * kTcQueries * 128 + (ks & 3) * 32, 16),
+               tc_desc(kb + (ks >> 2) * kKeys * 128 + (ks & 3) * 32, 16),
+               tc_instr(kTcQueries, kKeys, false), ks > 0);
+      tc_commit(&s_bar[0]);
+    }
+    ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[0], phase));
+    tc_fence_after();
+    if (works && ok) {
+      uint32_t s[2][32];
+      tmem_ld32(s[0], mine + kTcP);
+      tmem_ld32(s[1], mine + kTcP + 32);
+      tmem_wait_ld();
+      const int left = hi - k0;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) {
+        const float x = j < left ? __uint_as_float(s[j >> 5][j & 31]) * p.qscale : -INFINITY;
+        s[j >> 5][j & 31] = __float_as_uint(x);
+        mx = fmaxf(mx, x);
+      }
+      float f = 1.f;
+      if (mx > m + 8.f) {
+        f = ex2_approx(m - mx);  // (zero for the first tile)
+        m = mx;
+        l *= f;
+      }
+      if (k0 > lo && __any_sync(0xFFFFFFFFu, f != 1.f)) {
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(o, mine + kTcO + c);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+          tmem_st32(mine + kTcO + c, o);
+        }
+      }
+#pragma unroll
+      for (int j0 = 0; j0 < kKeys; j0 += 16) {  // 8 columns of each part at a time
+        uint32_t w[3][8];
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+          const int a = j0 + j;
+          // a key that does not count weighs nothing (m may be -inf)
+          const float w0 =
+              a < left ? ex2_approx(__uint_as_float(s[a >> 5][a & 31]) - m) : 0.f;
+          const float w1 =
+              a + 1 < left ? ex2_approx(__uint_as_float(s[a >> 5][(a & 31) + 1]) - m) : 0.f;
+          l += w0 + w1;
+          uint32_t part[3];
+          split2(w0, w1, part);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) w[k][j / 2] = part[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) tmem_st8(mine + kTcP + k * 32 + j0 / 2, w[k]);
+      }
+      tmem_wait_st();
+    }
+    tc_fence_before();
+    if (__syncthreads_or(!ok)) break;
+    if (tid == 0) {
+      tc_fence_after();
+#pragma unroll
+      for (int part = 2; part >= 0; --part)  // the small parts first
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 16; ++kk)
+          tc_mma_ta(tmem + kTcO, tmem + kTcP + part * 32 + kk * 8,
+                    tc_desc(vb + kk * 16 * 128, kKeys * 128), tc_instr(kTcQueries, D, true),
+                    k0 > lo || part < 2 || kk > 0);
+      tc_commit(&s_bar[1]);
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  // phase: that of the tile after the last
+  if (ok && lo < hi) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
+  tc_fence_after();
+  if (!ok && tid == 0 && p.err) set_err(p.err, HKV_ERR_TIMEOUT);
+  if (works) {
+    const bool wrong = bad || !ok;
+    const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
+    const size_t row = qrow + (size_t)tid * p.heads;
+    float *part = p.part + (row * p.splits + sp) * PF;
+    float *to = p.splits > 1 ? part : p.out + row * D;
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+      uint32_t o[32];
+      if (lo < hi) {
+        tmem_ld32(o, mine + kTcO + c);
+        tmem_wait_ld();
+      }
+      if (tid < nq) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (lo < hi)
+            v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                            __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+          if (p.splits == 1) v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
+          *reinterpret_cast<float4 *>(to + c + e) = v;
+        }
+      }
+    }
+    if (tid < nq) {
+      if (p.splits > 1)
+        *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
+      else
+        p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_free(tmem, kTcCols);
+}
+
 // Joins a query's ranges in their order, a warp per query: lane j < splits
 // holds range j's maximum and sum.
 constexpr int kJoinThreads = 128;
@@ -419,6 +629,15 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   if (lane == 0) p.lse[row] = bad ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+template <int D>
+cudaError_t launch_tc(const PrefixArgs &a, int grid, int split_len, cudaStream_t s) {
+  constexpr int smem = TcSmem<D>::kTotal;
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(prefix_tc_kernel<D>, smem, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(prefix_tc_kernel<D>, grid, kTcThreads, smem, s, a, split_len);
+}
+
 template <int D, typename T, int MW>
 cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStream_t s) {
   constexpr int smem = PSmem<D, T, MW>::kTotal;
@@ -431,10 +650,12 @@ cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStrea
 }  // namespace
 
 // As many key ranges as fill the device twice over (2 CTAs an SM), each a
-// whole number of tiles.
-PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len) {
+// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05,
+// where 128 queries cost what 16 do here.
+PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int dtype) {
   PrefixPlan pl;
   pl.mw = seqs <= 16 ? 1 : seqs <= 32 ? 2 : 4;
+  if (dtype == HKV_BF16 && seqs > 16) pl.mw = 8;
   pl.tiles = (seqs + pl.mw * 16 - 1) / (pl.mw * 16);
   const long long base = (long long)groups * heads * pl.tiles;
   long long want = 304 / base;
@@ -453,9 +674,10 @@ cudaError_t launch_prefix(const PrefixArgs &a, const PrefixPlan &pl, int D, int 
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   cudaError_t e = cudaErrorInvalidValue;
   HKV_DISPATCH(D, dtype, {
-    if (pl.mw == 1) e = launch_tiles<kD, kT, 1>(a, (int)grid, pl.split_len, s);
-    else if (pl.mw == 2) e = launch_tiles<kD, kT, 2>(a, (int)grid, pl.split_len, s);
-    else e = launch_tiles<kD, kT, 4>(a, (int)grid, pl.split_len, s);
+    if (pl.mw == 8) e = launch_tc<kD>(a, (int)grid, pl.split_len, s);
+    else if (pl.mw == 1) e = launch_tiles<kD, kT, 1>(a, (int)grid, pl.split_len, s);
+    else if (pl.mw == 2) e = launch_tiles<kD, float, 2>(a, (int)grid, pl.split_len, s);
+    else e = launch_tiles<kD, float, 4>(a, (int)grid, pl.split_len, s);
   });
   if (e != cudaSuccess || a.splits == 1) return e;
   const int rows = a.groups * a.seqs * a.heads;

@@ -67,10 +67,10 @@ struct PrefixArgs {
 };
 
 struct PrefixPlan {
-  int mw;                        // warps of a CTA along the queries, 16 each
+  int mw;                        // queries of a CTA, over 16 (8: the tcgen05 kernel)
   int splits, tiles, split_len;  // key ranges, query tiles, keys of a range
 };
-PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len);
+PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int dtype);
 cudaError_t launch_prefix(const PrefixArgs &a, const PrefixPlan &plan, int D, int dtype,
                           cudaStream_t s);
 

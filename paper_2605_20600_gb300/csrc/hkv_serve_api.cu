@@ -182,7 +182,8 @@ hkv_status check_prefix(const hkv_config *cfg, const hkv_prefix *p) {
 }
 
 PrefixPlan plan_of(const hkv_config *c, const hkv_prefix *p) {
-  return prefix_plan(p->n_groups, c->n_seqs / p->n_groups, c->n_heads, p->max_len);
+  return prefix_plan(p->n_groups, c->n_seqs / p->n_groups, c->n_heads, p->max_len,
+                     c->dtype);
 }
 
 size_t prefix_ws_bytes(const hkv_config *c, const PrefixPlan &pl) {
