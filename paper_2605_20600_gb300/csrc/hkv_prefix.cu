@@ -372,34 +372,41 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
 // O stays in TMEM; a query's reference maximum moves (and O and its sum are
 // rescaled) only when a tile's maximum is more than 2^8 above it, so that the
 // weights stay below 2^8. The copies of the next tile run meanwhile, and two
-// CTAs an SM fill each other's waits.
+// CTAs an SM fill each other's waits. Up to 64 queries (TWO): the rows hold them
+// twice, and each copy takes half of a tile's keys (its weights of the other
+// half are zero), so that all four warps have work; the copies are joined at the
+// end.
 constexpr int kTcQueries = 128, kTcThreads = 128;
 constexpr int kTcCols = 256, kTcP = 0, kTcO = 128;  // TMEM: S and the parts of W, then O
 
 template <int D>
 struct TcSmem {
   static constexpr int kQ = kTcQueries * D * 2, kTile = kKeys * D * 2;
+  static_assert(64 * (D + 4) * 4 <= 4 * kTile, "the second copies' results take the tiles' place");
   // 1024-byte aligned tiles; no less than 80 KB, so that at most two CTAs, and
   // with them their TMEM, fit an SM
   static constexpr int kUsed = kQ + 4 * kTile + 1024;
   static constexpr int kTotal = kUsed > 80 * 1024 ? kUsed : 80 * 1024;
 };
 
-// `rows` rows of D elements as column blocks of 128 bytes, 128-byte swizzle;
-// rows from `live` on zero
-template <int D>
+// ROWS rows of D elements as column blocks of 128 bytes, 128-byte swizzle; the
+// source's rows repeat after PERIOD, those from `live` on read as zero
+template <int D, int ROWS, int PERIOD>
 __device__ __forceinline__ void tc_load_rows(unsigned char *dst, const __nv_bfloat16 *src,
-                                             long long stride, int rows, int live) {
-  constexpr int PPR = D / 8;
-  for (int e = threadIdx.x; e < rows * PPR; e += kTcThreads) {
-    const int r = e / PPR, c = e % PPR;
-    const bool on = r < live;
-    cp_async16_zfill(dst + (c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4),
-                     src + (on ? r * stride : 0) + c * 8, on);
+                                             long long stride, int live) {
+  constexpr int PPR = D / 8, STEP = kTcThreads / PPR;  // pieces a row, rows a pass
+  const int c = threadIdx.x % PPR, r0 = threadIdx.x / PPR;
+  unsigned char *to = dst + (c >> 3) * ROWS * 128 + r0 * 128;
+#pragma unroll 8
+  for (int i = 0; i < ROWS / STEP; ++i) {
+    const int r = r0 + i * STEP, from = r % PERIOD;
+    const bool on = from < live;
+    cp_async16_zfill(to + i * STEP * 128 + (((c & 7) ^ (r & 7)) << 4),
+                     src + (on ? from * stride : 0) + c * 8, on);
   }
 }
 
-template <int D>
+template <int D, bool TWO>
 __global__ void __launch_bounds__(kTcThreads, 2)
     prefix_tc_kernel(const PrefixArgs p, int split_len) {
   using SM = TcSmem<D>;
@@ -437,12 +444,12 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   unsigned char *sq = dyn, *skv = dyn + SM::kQ;  // [stage][K, V]
   auto load_tile = [&](int k0, int st) {
     unsigned char *s = skv + st * 2 * SM::kTile;
-    tc_load_rows<D>(s, K + k0 * p.ts, p.ts, kKeys, hi - k0);
-    tc_load_rows<D>(s + SM::kTile, V + k0 * p.ts, p.ts, kKeys, hi - k0);
+    tc_load_rows<D, kKeys, kKeys>(s, K + k0 * p.ts, p.ts, hi - k0);
+    tc_load_rows<D, kKeys, kKeys>(s + SM::kTile, V + k0 * p.ts, p.ts, hi - k0);
   };
   if (lo < hi) {
-    tc_load_rows<D>(sq, static_cast<const __nv_bfloat16 *>(p.q) + qrow * D,
-                    (long long)p.heads * D, kTcQueries, nq);
+    tc_load_rows<D, kTcQueries, TWO ? 64 : kTcQueries>(
+        sq, static_cast<const __nv_bfloat16 *>(p.q) + qrow * D, (long long)p.heads * D, nq);
     load_tile(lo, 0);
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
@@ -450,7 +457,10 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem, mine = tmem + ((uint32_t)(warp * 32) << 16);
-  const bool works = warp * 32 < nq;  // this warp holds queries
+  const int first = TWO ? (warp & 1) * 32 : warp * 32;   // the warp's first query
+  const bool works = first < nq;
+  constexpr int CH = TWO ? 1 : 2;                       // 32 keys of a tile at a time
+  const int key0 = TWO ? (warp >> 1) * 32 : 0;          // the row's keys of a tile
   float m = -INFINITY, l = 0.f;
   bool ok = true;
   uint32_t phase = 0;
@@ -478,24 +488,27 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[0], phase));
     tc_fence_after();
     if (works && ok) {
-      uint32_t s[2][32];
-      tmem_ld32(s[0], mine + kTcP);
-      tmem_ld32(s[1], mine + kTcP + 32);
+      uint32_t s[CH][32];
+#pragma unroll
+      for (int c = 0; c < CH; ++c) tmem_ld32(s[c], mine + kTcP + key0 + c * 32);
       tmem_wait_ld();
-      const int left = hi - k0;
+      const int left = hi - k0 - key0;  // keys that count, from the row's first on
+      if (left < CH * 32) {
+#pragma unroll
+        for (int j = 0; j < CH * 32; ++j)
+          if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
+      }
       float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < kKeys; ++j) {
-        const float x = j < left ? __uint_as_float(s[j >> 5][j & 31]) * p.qscale : -INFINITY;
-        s[j >> 5][j & 31] = __float_as_uint(x);
-        mx = fmaxf(mx, x);
-      }
+      for (int j = 0; j < CH * 32; ++j) mx = fmaxf(mx, __uint_as_float(s[j >> 5][j & 31]));
+      mx *= p.qscale;
       float f = 1.f;
       if (mx > m + 8.f) {
-        f = ex2_approx(m - mx);  // (zero for the first tile)
+        f = ex2_approx(m - mx);  // (zero for the first keys)
         m = mx;
         l *= f;
       }
+      const float ref = m == -INFINITY ? 0.f : m;  // no key yet: weights of zero
       if (k0 > lo && __any_sync(0xFFFFFFFFu, f != 1.f)) {
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -507,25 +520,34 @@ __global__ void __launch_bounds__(kTcThreads, 2)
           tmem_st32(mine + kTcO + c, o);
         }
       }
+      float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-      for (int j0 = 0; j0 < kKeys; j0 += 16) {  // 8 columns of each part at a time
+      for (int j0 = 0; j0 < CH * 32; j0 += 16) {  // 8 columns of each part at a time
         uint32_t w[3][8];
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
           const int a = j0 + j;
-          // a key that does not count weighs nothing (m may be -inf)
-          const float w0 =
-              a < left ? ex2_approx(__uint_as_float(s[a >> 5][a & 31]) - m) : 0.f;
+          const float w0 = ex2_approx(fmaf(__uint_as_float(s[a >> 5][a & 31]), p.qscale, -ref));
           const float w1 =
-              a + 1 < left ? ex2_approx(__uint_as_float(s[a >> 5][(a & 31) + 1]) - m) : 0.f;
-          l += w0 + w1;
+              ex2_approx(fmaf(__uint_as_float(s[a >> 5][(a & 31) + 1]), p.qscale, -ref));
+          l0 += w0;
+          l1 += w1;
           uint32_t part[3];
           split2(w0, w1, part);
 #pragma unroll
           for (int k = 0; k < 3; ++k) w[k][j / 2] = part[k];
         }
 #pragma unroll
-        for (int k = 0; k < 3; ++k) tmem_st8(mine + kTcP + k * 32 + j0 / 2, w[k]);
+        for (int k = 0; k < 3; ++k) tmem_st8(mine + kTcP + k * 32 + (key0 + j0) / 2, w[k]);
+      }
+      l += l0 + l1;
+      if (TWO) {
+        const uint32_t zero[8] = {};
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+          for (int j0 = 0; j0 < 32; j0 += 16)
+            tmem_st8(mine + kTcP + k * 32 + ((key0 ^ 32) + j0) / 2, zero);
       }
       tmem_wait_st();
     }
@@ -548,28 +570,61 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   if (ok && lo < hi) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
   tc_fence_after();
   if (!ok && tid == 0 && p.err) set_err(p.err, HKV_ERR_TIMEOUT);
-  if (works) {
-    const bool wrong = bad || !ok;
-    const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
+  const bool wrong = bad || !ok, any = lo < hi && ok;
+  // the two copies of a query joined: the second half of the rows hands its
+  // result over (the tiles' place is free)
+  float *so = reinterpret_cast<float *>(dyn + SM::kQ);  // [64][D + 4]
+  float fa = 1.f, fb = 0.f;
+  if (TWO) {
+    if (warp >= 2 && works) {
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32] = {};
+        if (any) {
+          tmem_ld32(o, mine + kTcO + c);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<uint4 *>(so + (tid - 64) * PF + c + e) =
+              make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      }
+      *reinterpret_cast<float2 *>(so + (tid - 64) * PF + D) = make_float2(m, l);
+    }
+    __syncthreads();
+    if (warp < 2 && works) {
+      const float2 ml = *reinterpret_cast<const float2 *>(so + tid * PF + D);
+      const float mn = fmaxf(m, ml.x);
+      fa = l == 0.f ? 0.f : ex2_approx(m - mn);
+      fb = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mn);
+      m = mn;
+      l = l * fa + ml.y * fb;
+    }
+  }
+  if (works && (!TWO || warp < 2)) {
+    const float inv = p.splits > 1 ? 1.f : wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
     const size_t row = qrow + (size_t)tid * p.heads;
     float *part = p.part + (row * p.splits + sp) * PF;
     float *to = p.splits > 1 ? part : p.out + row * D;
 #pragma unroll 1
     for (int c = 0; c < D; c += 32) {
-      uint32_t o[32];
-      if (lo < hi) {
+      uint32_t o[32] = {};
+      if (any) {
         tmem_ld32(o, mine + kTcO + c);
         tmem_wait_ld();
       }
       if (tid < nq) {
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (lo < hi)
-            v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
-                            __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
-          if (p.splits == 1) v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-          *reinterpret_cast<float4 *>(to + c + e) = v;
+          float4 v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                                 __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+          if (TWO) {
+            const float4 u = *reinterpret_cast<const float4 *>(so + tid * PF + c + e);
+            v.x = v.x * fa + u.x * fb, v.y = v.y * fa + u.y * fb;
+            v.z = v.z * fa + u.z * fb, v.w = v.w * fa + u.w * fb;
+          }
+          *reinterpret_cast<float4 *>(to + c + e) =
+              make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
         }
       }
     }
@@ -629,13 +684,13 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   if (lane == 0) p.lse[row] = bad ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-template <int D>
+template <int D, bool TWO>
 cudaError_t launch_tc(const PrefixArgs &a, int grid, int split_len, cudaStream_t s) {
   constexpr int smem = TcSmem<D>::kTotal;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(prefix_tc_kernel<D>, smem, ready);
+  const cudaError_t e = allow_smem_of(prefix_tc_kernel<D, TWO>, smem, ready);
   if (e != cudaSuccess) return e;
-  return pdl_launch(prefix_tc_kernel<D>, grid, kTcThreads, smem, s, a, split_len);
+  return pdl_launch(prefix_tc_kernel<D, TWO>, grid, kTcThreads, smem, s, a, split_len);
 }
 
 template <int D, typename T, int MW>
@@ -674,7 +729,8 @@ cudaError_t launch_prefix(const PrefixArgs &a, const PrefixPlan &pl, int D, int 
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   cudaError_t e = cudaErrorInvalidValue;
   HKV_DISPATCH(D, dtype, {
-    if (pl.mw == 8) e = launch_tc<kD>(a, (int)grid, pl.split_len, s);
+    if (pl.mw == 8 && a.seqs <= 64) e = launch_tc<kD, true>(a, (int)grid, pl.split_len, s);
+    else if (pl.mw == 8) e = launch_tc<kD, false>(a, (int)grid, pl.split_len, s);
     else if (pl.mw == 1) e = launch_tiles<kD, kT, 1>(a, (int)grid, pl.split_len, s);
     else if (pl.mw == 2) e = launch_tiles<kD, float, 2>(a, (int)grid, pl.split_len, s);
     else e = launch_tiles<kD, float, 4>(a, (int)grid, pl.split_len, s);
