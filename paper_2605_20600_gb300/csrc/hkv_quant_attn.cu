@@ -151,8 +151,8 @@ __device__ __forceinline__ bool all_read(const QAttnArgs &p, volatile int *repor
   return v == 0u;
 }
 __device__ __forceinline__ void advance_or_leave(const QAttnArgs &p, int hl, bool dense,
-                                                 volatile int *reported) {
-  if (all_read(p, reported)) {
+                                                 volatile int *reported, bool known = false) {
+  if (known || all_read(p, reported)) {
     advance_head(p, hl, dense);
     return;
   }
@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       }
     }
   }
+  const bool early = STEP && lane == 0 && all_read(p, &s_reported);  // (stays so)
   __syncthreads();
 
   // pieces joined: a warp those of the head that starts in its run, warp 0
@@ -393,15 +394,10 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       const bool dense = STEP ? c.label[p.base + h] == HKV_DENSE : false;
       if (slot == 1 && ends) {
         finish_head<D>(p, h, m, l, o);
-        if (STEP && lane == 0) advance_or_leave(p, h, dense, &s_reported);
+        if (STEP && lane == 0) advance_or_leave(p, h, dense, &s_reported, early);
         continue;
       }
-      // cut between CTAs: this one's part to the workspace
-      float *part = p.part + ((size_t)cta * 2 + slot) * PF;
-      store_row<E>(part + lane * E, o);
-      if (lane == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
-      __syncwarp();
-      // the CTAs that hold the head: those of its first and last tile, and between
+      // cut between CTAs: those of the head's first and last tile, and between
       auto cta_of = [&](int t) {
         const int longer = rest * (share + 1);  // tiles of the warps with one more
         const int w = t < longer ? t / (share + 1) : rest + (t - longer) / share;
@@ -409,13 +405,31 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       };
       const int c0 = cta_of(s_first[from][slot]);
       const int c1 = cta_of(s_first[from][slot] + s_tiles[from][slot] - 1);
+      // where all others have been, this one has no need to leave its part
       uint32_t seen = 0;
-      if (lane == 0)  // releases the warp's part, acquires the others'
-        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;"
+      if (lane == 0)
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];"
                      : "=r"(seen)
                      : "l"(p.count + h)
                      : "memory");
-      if (__shfl_sync(0xFFFFFFFFu, seen, 0) != (uint32_t)(c1 - c0)) continue;
+      const bool others = __shfl_sync(0xFFFFFFFFu, seen, 0) == (uint32_t)(c1 - c0);
+      if (!others) {
+        float *part = p.part + ((size_t)cta * 2 + slot) * PF;
+        store_row<E>(part + lane * E, o);
+        if (lane == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
+        __syncwarp();
+        if (lane == 0)  // releases the warp's part, acquires the others'
+          asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;"
+                       : "=r"(seen)
+                       : "l"(p.count + h)
+                       : "memory");
+        if (__shfl_sync(0xFFFFFFFFu, seen, 0) != (uint32_t)(c1 - c0)) continue;
+      }
+      // joined in CTA order, this one's part from here
+      const float my_m = m, my_l = l;
+      float my_o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) my_o[e] = o[e];
       m = -INFINITY, l = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -426,10 +440,17 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         };
         float2 ml = make_float2(-INFINITY, 0.f);
         if (lane < n) ml = __ldcg(reinterpret_cast<const float2 *>(part_of(lane) + D));
+        if (j0 + lane == cta) ml = make_float2(my_m, my_l);
         float v[4][E];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (j < n) load_row<E>(part_of(j) + lane * E, v[j]);
+        auto mine_at = [&](int j, float (&x)[E]) {
+          if (j0 + j == cta) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = my_o[e];
+          }
+        };
         const float mn = fmaxf(m, warp_max(ml.x));
         const float f = l == 0.f ? 0.f : ex2_approx(m - mn);
         const float g = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mn);
@@ -444,6 +465,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float gj = __shfl_sync(0xFFFFFFFFu, g, (j1 + j) & 31);
+            mine_at(j1 + j, v[j]);
             if (j1 + j < n) {
 #pragma unroll
               for (int e = 0; e < E; ++e) o[e] += v[j][e] * gj;
@@ -457,7 +479,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
       finish_head<D>(p, h, m, l, o);
       if (lane == 0) {
         p.count[h] = 0u;
-        if (STEP) advance_or_leave(p, h, dense, &s_reported);
+        if (STEP) advance_or_leave(p, h, dense, &s_reported, early);
       }
     }
   }
