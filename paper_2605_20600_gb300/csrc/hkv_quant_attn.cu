@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
       const int r0 = tile * kTile, rows = min(kTile, hd.n - r0);
       if (STEP && tile == new_tile)
         append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, nr, qv);
-      attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
+      attend_tile<D, BITS>(stage, rows, qr, m, l, acc);
       if (STAGES == 1) break;  // no warp has a second tile
       __syncwarp();            // the stage and the weights are rewritten from here on
       if (tile + STAGES * kHeadWarps < hd.tiles) load(tile + STAGES * kHeadWarps, st);
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(Smem<D, BITS>::kWarps * 32, 2)
         const int rows = hd.bad ? 0 : min(kTile, hd.n - r0);
         if (STEP && appends && tile == new_tile)
           append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, nr, qv);
-        if (rows > 0) attend_tile<D, BITS>(stage, rows, qr, operand, m, l, acc);
+        if (rows > 0) attend_tile<D, BITS>(stage, rows, qr, m, l, acc);
         __syncwarp();  // the stage and the weights are rewritten from here on
         issue();
         st = st + 1 == STAGES ? 0 : st + 1;

@@ -132,10 +132,8 @@ struct TileOf {
   using R = QRow<D, BITS>;
   static constexpr int kCodes = kTile * R::kBytes, kScales = kTile * R::kScaleBytes;
   static constexpr int kBytes = 2 * (kCodes + kScales);
-  // the B operand being made: the query's two parts (fp16 [2][D]), then the
-  // weights (fp16 [8][kTile])
-  static constexpr int kOperand = 512;
-  static_assert(2 * D * 2 <= kOperand && 8 * kTile * 2 <= kOperand, "one at a time");
+  // the query's two parts being made (fp16 [2][D])
+  static constexpr int kOperand = 2 * D * 2;
 };
 
 // Byte offset of the 16-byte piece `c` of row `r` in a tile: rows lie back to
@@ -349,19 +347,17 @@ __device__ __forceinline__ void load_query(const QAttnArgs &p, int hl, float (&q
 
 // One tile into the running maximum m, the lane's part of the sum l, and the
 // accumulator: acc[y] are channels row8 D / 8 + 2 y, + 1, in the lanes whose
-// `quad` is those channels' group. sw: the warp's operand area.
+// `quad` is those channels' group.
 template <int D, int BITS>
 __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows,
-                                            const Query<D, BITS> &q, __half *sw, float &m,
+                                            const Query<D, BITS> &q, float &m,
                                             float &l, float (&acc)[D / 16][2]) {
   using R = QRow<D, BITS>;
   using TL = TileOf<D, BITS>;
   constexpr int RB = R::kBytes, G = R::kGroups, KM = D / 16;
   const int lane = threadIdx.x & 31, row8 = lane >> 2, quad = lane & 3;
   const unsigned char *sk = stage, *sv = sk + TL::kCodes, *ss = sv + TL::kCodes;
-  // this lane's row, and where it sits in the weights' columns
-  const int own = row8 + 8 * quad;
-  const int own_at = ((own >> 1) & 3) * 8 + (own >> 4) * 4 + ((own >> 3) & 1) * 2 + (own & 1);
+  const int own = row8 + 8 * quad;  // this lane's row
   // scores: x[b2] is the sum of row row8 + 8 b2 over this lane's group
   float xs[4];
 #pragma unroll
@@ -438,24 +434,31 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
   const float w = on ? ex2_approx(x - m) : 0.f;
   l += w;
 
-  // weights times scales, over the power of two of the tile's largest
-  // scale of the group, in two parts
-  float unit = 1.f;  // of group `quad`
+  // weights times scales of group `quad`, rows row8 + 8 b, over the power of two
+  // of the tile's largest scale of the group, as two fp16 parts: the columns
+  // 2 quad, 2 quad + 1 of an 8 x 8 block whose transpose is the B operand
+  // (this lane: column row8, rows 2 quad, + 1 of the block)
+  uint32_t sb[4], top = 0;
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    const uint32_t sb =
-        on ? reinterpret_cast<const uint16_t *>(ss + TL::kScales)[own * G + g] : 0u;
-    const float u = pow2_of(__reduce_max_sync(0xFFFFFFFFu, sb << 16));
-    if (quad == g) unit = u;
-    const float y = on ? w * (bf16_bits_to_float(sb) * inv_pow2(u)) : 0.f;
-    const __half h = __float2half_rn(y);
-    sw[(2 * g) * kTile + own_at] = h;
-    sw[(2 * g + 1) * kTile + own_at] = __float2half_rn((y - __half2float(h)) * kLoScale);
+  for (int b = 0; b < 4; ++b) {
+    sb[b] = 0;
+    if (quad < G && row8 + 8 * b < rows)
+      sb[b] = reinterpret_cast<const uint16_t *>(ss + TL::kScales)[(row8 + 8 * b) * G + quad];
+    top = max(top, sb[b]);
   }
-  __syncwarp();
-  // B operand: this lane's column row8, rows 2 quad, + 1, + 8, + 9 of each half
-  uint4 wf = make_uint4(0u, 0u, 0u, 0u);
-  if (row8 < 2 * G) wf = *reinterpret_cast<const uint4 *>(sw + row8 * kTile + quad * 8);
+#pragma unroll
+  for (int x2 = 4; x2 <= 16; x2 <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, x2));
+  const float unit = pow2_of(top << 16), inv = inv_pow2(unit);
+  uint32_t wf[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const float y = __shfl_sync(0xFFFFFFFFu, w, (lane & ~3) | b) * (bf16_bits_to_float(sb[b]) * inv);
+    const float lo = (y - __half2float(__float2half_rn(y))) * kLoScale;
+    const __half2 pair = __floats2half2_rn(y, lo);
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;"
+        : "=r"(wf[b])
+        : "r"(*reinterpret_cast<const uint32_t *>(&pair)));
+  }
 
   // output: this lane's channels [row8 D / 8, + D / 8), two per product
   constexpr int VW = D * BITS / 256;  // words of the lane's channels in a row
@@ -478,7 +481,7 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
                                                        (row8 & 3) * 4);
       }
     }
-    const uint32_t bw0 = b ? wf.z : wf.x, bw1 = b ? wf.w : wf.y;
+    const uint32_t bw0 = wf[2 * b], bw1 = wf[2 * b + 1];
 #pragma unroll
     for (int w2 = 0; w2 < VW; ++w2) {
 #pragma unroll
