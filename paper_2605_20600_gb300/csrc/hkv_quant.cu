@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(kRowThreads, 6)
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          x[j] = s * (BITS == 4 ? code4(w[u][kv].x, j)
-                                : code8(j < 4 ? w[u][kv].x : w[u][kv].y, j & 3));
+          x[j] = s * (lifted<BITS>(BITS == 4 || j < 4 ? w[u][kv].x : w[u][kv].y,
+                                   BITS == 4 ? j : j & 3) - kLift<BITS>);
         store8<T>(static_cast<T *>(kv ? dst.V : dst.K) + (doff + r) * D + col * 8, x);
       }
       if (col == 0) dst.pos[doff + r] = src.c.pos[soff + r];
@@ -176,23 +176,34 @@ template <int D, int BITS>
 struct CodeRows {
   static constexpr int kBytes = QRow<D, BITS>::kBytes;
   const uint16_t *scale;  // the segment's first row
+  // one group's part: HUGE where s 2^16 might overflow, else s c = s (2^15 + u) -
+  // s (2^15 + bias) in one fma, exact: the second product has at most 21 bits
+  template <bool HUGE>
+  __device__ __forceinline__ float group(const unsigned char *codes, const float *q, float sc,
+                                         float s) const {
+    const float minus = -sc * kLift<BITS>;
+#pragma unroll
+    for (int pc = 0; pc < BITS / 4; ++pc) {
+      const uint4 u = reinterpret_cast<const uint4 *>(codes)[pc];
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      constexpr int CPW = 32 / BITS;  // codes a word
+#pragma unroll
+      for (int j = 0; j < 4 * CPW; ++j) {
+        const float f = lifted<BITS>(w[j / CPW], j % CPW);
+        const float k = HUGE ? sc * (f - kLift<BITS>) : fmaf(sc, f, minus);
+        s = __fadd_rn(s, __fmul_rn(q[pc * 4 * CPW + j], k));
+      }
+    }
+    return s;
+  }
   __device__ __forceinline__ float dot(const unsigned char *krow, const float *qbar, int r) const {
-    constexpr int G = QRow<D, BITS>::kGroups, PPG = BITS / 4;  // 16-byte pieces a group
+    constexpr int G = QRow<D, BITS>::kGroups;
     float s = 0.f;
 #pragma unroll 1
     for (int g = 0; g < G; ++g) {
       const float sc = bf16_bits_to_float(scale[(size_t)r * G + g]);
-#pragma unroll
-      for (int pc = 0; pc < PPG; ++pc) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(krow + (g * PPG + pc) * 16);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        const float *q = qbar + g * 32 + pc * (128 / BITS);
-#pragma unroll
-        for (int j = 0; j < 128 / BITS; ++j) {
-          const float c = BITS == 8 ? code8(w[j / 4], j % 4) : code4(w[j / 8], j % 8);
-          s = __fadd_rn(s, __fmul_rn(q[j], __fmul_rn(sc, c)));
-        }
-      }
+      s = sc < 0x1p100f ? group<false>(krow + g * 4 * BITS, qbar + g * 32, sc, s)
+                        : group<true>(krow + g * 4 * BITS, qbar + g * 32, sc, s);
     }
     return s;
   }
@@ -238,21 +249,50 @@ __global__ void __launch_bounds__(NT, kQuantUpdCtasPerSm)
   if (M > 0) {
     int *hole, *fill;
     const int k = pair_holes(len, M, u, sh, &hole, &fill);
-    for (int w = tid; w < k * PPR; w += NT) {
-      const size_t src = (size_t)fill[w / PPR] * KB + (w % PPR) * 16;
-      const size_t dst = (size_t)hole[w / PPR] * KB + (w % PPR) * 16;
-      const uint4 a = __ldcg(reinterpret_cast<const uint4 *>(K + src));
-      const uint4 b = __ldcg(reinterpret_cast<const uint4 *>(V + src));
-      *reinterpret_cast<uint4 *>(K + dst) = a;
-      *reinterpret_cast<uint4 *>(V + dst) = b;
+    // scales and positions ride with the first round of codes; every load of a
+    // round is on its way before its first store (sources lie above the new
+    // length, destinations below it)
+    constexpr int B = 2, SW = SB / 4;
+    uint32_t ks = 0, vs = 0;
+    int ps = 0;
+    if (tid < k * SW) {
+      ks = *reinterpret_cast<const uint32_t *>(KS + (size_t)fill[tid / SW] * SB + tid % SW * 4);
+      vs = *reinterpret_cast<const uint32_t *>(VS + (size_t)fill[tid / SW] * SB + tid % SW * 4);
     }
-    for (int w = tid; w < k * (SB / 4); w += NT) {
-      const size_t src = (size_t)fill[w / (SB / 4)] * SB + (w % (SB / 4)) * 4;
-      const size_t dst = (size_t)hole[w / (SB / 4)] * SB + (w % (SB / 4)) * 4;
+    if (tid < k) ps = u.ps[fill[tid]];
+    for (int w0 = 0; w0 < k * PPR; w0 += NT * B) {
+      uint4 kb[B], vb[B];
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        const int w = w0 + j * NT + tid;
+        if (w < k * PPR) {
+          const size_t src = (size_t)fill[w / PPR] * KB + (w % PPR) * 16;
+          kb[j] = __ldcg(reinterpret_cast<const uint4 *>(K + src));
+          vb[j] = __ldcg(reinterpret_cast<const uint4 *>(V + src));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        const int w = w0 + j * NT + tid;
+        if (w < k * PPR) {
+          const size_t dst = (size_t)hole[w / PPR] * KB + (w % PPR) * 16;
+          *reinterpret_cast<uint4 *>(K + dst) = kb[j];
+          *reinterpret_cast<uint4 *>(V + dst) = vb[j];
+        }
+      }
+    }
+    if (tid < k * SW) {
+      *reinterpret_cast<uint32_t *>(KS + (size_t)hole[tid / SW] * SB + tid % SW * 4) = ks;
+      *reinterpret_cast<uint32_t *>(VS + (size_t)hole[tid / SW] * SB + tid % SW * 4) = vs;
+    }
+    if (tid < k) pos[hole[tid]] = ps;
+    for (int w = tid + NT; w < k * SW; w += NT) {
+      const size_t src = (size_t)fill[w / SW] * SB + w % SW * 4;
+      const size_t dst = (size_t)hole[w / SW] * SB + w % SW * 4;
       *reinterpret_cast<uint32_t *>(KS + dst) = *reinterpret_cast<const uint32_t *>(KS + src);
       *reinterpret_cast<uint32_t *>(VS + dst) = *reinterpret_cast<const uint32_t *>(VS + src);
     }
-    for (int j = tid; j < k; j += NT) pos[hole[j]] = u.ps[fill[j]];
+    for (int j = tid + NT; j < k; j += NT) pos[hole[j]] = u.ps[fill[j]];
   }
   if (tid == 0) {
     c.len[i] = len - M;

@@ -36,15 +36,16 @@ __device__ __forceinline__ float bf16_bits_to_float(uint32_t b) {
   return __uint_as_float(b << 16);
 }
 
-// A stored code as the fp32 number it stands for before its scale: byte b of w
-// (8 bits) or nibble n of w (4 bits), less the bias. 0x4B0000uu is the fp32
-// number 2^23 + uu.
-__device__ __forceinline__ float code8(uint32_t w, int b) {
-  return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + b)) - (8388608.f + 128.f);
+// 2^15 + uu for the stored code uu: byte b of w (8 bits) or nibble n (4 bits).
+// 0x4700uu00 is that fp32 number. Less 2^15 + bias it is the code c, exactly.
+template <int BITS>
+__device__ __forceinline__ float lifted(uint32_t w, int j) {
+  if (BITS == 8) return __uint_as_float(__byte_perm(w, 0x47000000u, 0x7504 + (j << 4)));
+  const uint32_t u = j < 2 ? w << (8 - 4 * j) : w >> (4 * j - 8);
+  return __uint_as_float((u & 0xF00u) | 0x47000000u);
 }
-__device__ __forceinline__ float code4(uint32_t w, int n) {
-  return __uint_as_float(((w >> (4 * n)) & 15u) | 0x4B000000u) - (8388608.f + 8.f);
-}
+template <int BITS>
+constexpr float kLift = 32768.f + (BITS == 8 ? 128.f : 8.f);
 
 // Quantises a group of 32 values held by four neighbouring lanes (8 each, in
 // channel order; the four call together, `mask` names them). Returns the

@@ -222,6 +222,17 @@ __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m
   else if (NH > hist_budget) M = NH - hist_budget;
 
   if (label == HKV_GLOBAL && M > 0) {
+    // the query ring comes in with one bulk copy, behind the choice of the
+    // subsets
+    const int P = m.P;
+    if (tid == 0) {
+      mbar_init(&sh.ring_bar, 1);
+      fence_barrier_init();
+      const uint32_t bytes = (uint32_t)P * RB;
+      mbar_arrive_expect_tx(&sh.ring_bar, bytes);
+      bulk_g2s(u.ring, qring, bytes, &sh.ring_bar);
+    }
+    __syncthreads();
     // Eq. 5: the floor(NH r_s) oldest history tokens are long-range (or,
     // in the grid-distance variant, the farthest from the newest image
     // token, equal distances older first)
@@ -251,26 +262,17 @@ __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m
         if (u.aux[r] == 0) u.aux[r] = n_long == NH ? 0 : 1;
     }
     HKV_UTRACE(2);
-    // Eq. 6 scores: q-bar = the P buffered queries, oldest first. The ring
-    // comes in with one bulk copy; the sums keep their order.
-    const int P = m.P;
-    if (tid == 0) {
-      mbar_init(&sh.ring_bar, 1);
-      fence_barrier_init();
-    }
-    __syncthreads();
-    if (tid == 0) {
-      const uint32_t bytes = (uint32_t)P * RB;
-      mbar_arrive_expect_tx(&sh.ring_bar, bytes);
-      bulk_g2s(u.ring, qring, bytes, &sh.ring_bar);
-    }
+    // Eq. 6 scores: q-bar = the P buffered queries, oldest first; the sums keep
+    // their order
     if (!mbar_wait(&sh.ring_bar, 0) && tid == 0) set_err(sg.err, HKV_ERR_TIMEOUT);
     for (int d = tid; d < D; d += NT) {
       float acc = 0.f;
+      int slot = (ntok - P) % P;
+      if (slot < 0) slot += P;
+#pragma unroll 4
       for (int pp = 0; pp < P; ++pp) {
-        int slot = (ntok - P + pp) % P;
-        if (slot < 0) slot += P;
         acc = __fadd_rn(acc, Elem<T>::load1(u.ring, (size_t)slot * D + d));
+        slot = slot + 1 == P ? 0 : slot + 1;
       }
       u.qbar[d] = acc;
     }
