@@ -26,9 +26,7 @@ namespace hkv {
 constexpr int kTile = 32;  // rows a warp handles at a time
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kQUp = 4096.f;                               // the query's parts, below 2^13
 constexpr float kLoScale = 2048.f, kLoUnscale = 1.f / 2048.f;  // second parts, 2^11
-constexpr float kRawHi = 0x1p24f / kQUp, kRawLo = kRawHi * kLoUnscale;  // sums of raw codes
 
 __device__ __forceinline__ uint32_t lop_and_or(uint32_t a, uint32_t m, uint32_t o) {
   uint32_t r;
@@ -46,22 +44,11 @@ __device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c) {
   return r;
 }
 
-// Stored codes u as fp16 pairs. raw*: the bits themselves, which read as the
-// subnormal numbers u 2^-24 (an odd nibble sits four bits up: u 2^-20); exact
-// in the tensor core, and the bias is taken off the sum. For the scores.
-__device__ __forceinline__ void raw8(uint32_t w, uint32_t &even, uint32_t &odd) {
-  even = w & 0x00FF00FFu;                     // bytes (0, 2)
-  odd = __byte_perm(w, 0u, 0x4341);           // bytes (1, 3)
-}
-__device__ __forceinline__ void raw4(uint32_t w, uint32_t (&c)[4]) {
-  const uint32_t v = w >> 8;                  // nibbles (0, 4) (1, 5) (2, 6) (3, 7)
-  c[0] = w & 0x000F000Fu;
-  c[1] = w & 0x00F000F0u;
-  c[2] = v & 0x000F000Fu;
-  c[3] = v & 0x00F000F0u;
-}
-// codes*: less the bias, exact. 0x64uu is the fp16 number 1024 + uu. For the
-// output, where the bias would be large beside the sum.
+// fp16 pairs of codes from stored ones, exact: 0x64uu is the fp16 number
+// 1024 + uu, and 1024 + bias comes off. (The stored bits are fp16 numbers too,
+// subnormal ones, and the bias could come off the sums: 64 operations a tile
+// less for 1 % of the time, but the scores lose a factor of four in precision.)
+// codes8: bytes (0, 2) and (1, 3) of a word.
 __device__ __forceinline__ void codes8(uint32_t w, uint32_t &even, uint32_t &odd) {
   constexpr uint32_t kOne = 0x64006400u, kSub = 0xE480E480u;  // 1024, -1152
   even = h2_add(lop_and_or(w, 0x00FF00FFu, kOne), kSub);
@@ -87,15 +74,14 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// the first of a chain: c = a b + (e0, e1, e0, e1)
-__device__ __forceinline__ void mma_f16_from(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                             uint32_t a3, uint32_t b0, uint32_t b1, float e0,
-                                             float e1) {
+// the first of a chain: c = a b
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                              uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-      "{%10,%11,%10,%11};"
+      "{%10,%10,%10,%10};"
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(e0), "f"(e1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // maximum over the warp
 __device__ __forceinline__ float warp_max(float x) {
@@ -217,7 +203,6 @@ __device__ __forceinline__ void load_tile(unsigned char *stage, const QCacheArgs
 template <int D, int BITS>
 struct Query {
   uint32_t f[D / 16][2];
-  float bias_hi, bias_lo;  // what the codes' bias adds to the lane's two columns
   float scale;             // of the sums, to logits in powers of two
 };
 
@@ -228,8 +213,7 @@ __device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32], 
                                                      __half *sq) {
   // the query over a power of two, in two fp16 parts, in the order in which
   // the codes of a word come out in pairs
-  constexpr int E = D / 32, KM = D / 16, G = D / 32;
-  constexpr float kRawBias = QRow<D, BITS>::kBias * 0x1p-24f;  // of a code read as a subnormal
+  constexpr int E = D / 32, KM = D / 16;
   const int lane = threadIdx.x & 31, row8 = lane >> 2, quad = lane & 3;
   Query<D, BITS> r;
   uint32_t qm = 0;
@@ -237,32 +221,17 @@ __device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32], 
   for (int e = 0; e < E; ++e) qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
   const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
   r.scale = q2 * qscale;
-  float sum_hi = 0.f, sum_lo = 0.f;  // of the lane's channels' parts
   __syncwarp();
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int d = lane * E + e;
     const int at = BITS == 8 ? (d & ~3) + ((d & 1) << 1) + ((d >> 1) & 1)
                              : (d & ~7) + ((d & 3) << 1) + ((d >> 2) & 1);
-    // the channels whose codes sit four bits up are taken down by that
-    const float up = BITS == 4 && (e & 1) ? 16.f : 1.f;
-    const float x = qv[e] * qi * (kQUp / up);
+    const float x = qv[e] * qi;
     const __half h = __float2half_rn(x);
-    const __half lo = __float2half_rn((x - __half2float(h)) * kLoScale);
     sq[at] = h;
-    sq[D + at] = lo;
-    sum_hi += __half2float(h) * up;
-    sum_lo += __half2float(lo) * up;
+    sq[D + at] = __float2half_rn((x - __half2float(h)) * kLoScale);
   }
-#pragma unroll
-  for (int o = 1; o < 32 / E; o <<= 1) {  // over the lanes of a group
-    sum_hi += __shfl_xor_sync(0xFFFFFFFFu, sum_hi, o);
-    sum_lo += __shfl_xor_sync(0xFFFFFFFFu, sum_lo, o);
-  }
-  // what the codes' bias adds to this lane's two columns (group `quad`)
-  r.bias_hi = __shfl_sync(0xFFFFFFFFu, sum_hi, (quad * 32 / E) & 31) * -kRawBias;
-  r.bias_lo = __shfl_sync(0xFFFFFFFFu, sum_lo, (quad * 32 / E) & 31) * -kRawBias;
-  if (quad >= G) r.bias_hi = r.bias_lo = 0.f;
   __syncwarp();
   // B operand of the scores: this lane's column is part (row8 & 1) of group
   // row8 / 2, its channels those of the lanes `quad` of the A operand
@@ -390,16 +359,16 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
     for (int w = 0; w < RB / 16; ++w) {
       if (BITS == 8) {
         uint32_t a0, a1, a2, a3;
-        raw8(wa[w], a0, a2);
-        raw8(wb[w], a1, a3);
-        if (w == 0) mma_f16_from(s, a0, a1, a2, a3, q.f[0][0], q.f[0][1], q.bias_hi, q.bias_lo);
+        codes8(wa[w], a0, a2);
+        codes8(wb[w], a1, a3);
+        if (w == 0) mma_f16_first(s, a0, a1, a2, a3, q.f[0][0], q.f[0][1]);
         else mma_f16(s, a0, a1, a2, a3, q.f[w][0], q.f[w][1]);
       } else {
         uint32_t ca[4], cb[4];
-        raw4(wa[w], ca);
-        raw4(wb[w], cb);
+        codes4(wa[w], ca);
+        codes4(wb[w], cb);
         if (w == 0)
-          mma_f16_from(s, ca[0], cb[0], ca[1], cb[1], q.f[0][0], q.f[0][1], q.bias_hi, q.bias_lo);
+          mma_f16_first(s, ca[0], cb[0], ca[1], cb[1], q.f[0][0], q.f[0][1]);
         else
           mma_f16(s, ca[0], cb[0], ca[1], cb[1], q.f[2 * w][0], q.f[2 * w][1]);
         mma_f16(s, ca[2], cb[2], ca[3], cb[3], q.f[2 * w + 1][0], q.f[2 * w + 1][1]);
@@ -409,8 +378,8 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
     const bool grp = quad < G;  // the columns beyond the groups are empty
     const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) : 0.f;
     const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) : 0.f;
-    xs[2 * b] = fa * fmaf(s[1], kRawLo, s[0] * kRawHi);
-    xs[2 * b + 1] = fb * fmaf(s[3], kRawLo, s[2] * kRawHi);
+    xs[2 * b] = fa * fmaf(s[1], kLoUnscale, s[0]);
+    xs[2 * b + 1] = fb * fmaf(s[3], kLoUnscale, s[2]);
   }
   // sums over the groups: lane (row8, quad) ends up with row row8 + 8 quad
   const bool b0 = quad & 1, b1 = quad & 2;
@@ -493,16 +462,15 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
           uint32_t a0, a1, a2, a3;
           codes8(v01, a0, a1);
           codes8(v23, a2, a3);
-          if (b == 0) mma_f16_from(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1, 0.f, 0.f);
+          if (b == 0) mma_f16_first(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1);
           else mma_f16(o[2 * w2 + h], a0, a1, a2, a3, bw0, bw1);
         } else {
           uint32_t ca[4], cb[4];
           codes4(v01, ca);
           codes4(v23, cb);
           if (b == 0) {
-            mma_f16_from(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1, 0.f, 0.f);
-            mma_f16_from(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1, 0.f,
-                         0.f);
+            mma_f16_first(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1);
+            mma_f16_first(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1);
           } else {
             mma_f16(o[4 * w2 + 2 * h], ca[0], ca[1], cb[0], cb[1], bw0, bw1);
             mma_f16(o[4 * w2 + 2 * h + 1], ca[2], ca[3], cb[2], cb[3], bw0, bw1);
