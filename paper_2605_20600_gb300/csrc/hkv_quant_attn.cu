@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, STAGES == 1 ? 6 : 4)
 // SM's shared memory as goes into whole tiles, or as many warps as registers.
 template <int RB>
 struct Shape {
-  static constexpr int kWarps = RB == 128 ? 6 : 8, kStages = RB == 32 ? 4 : 2;
+  static constexpr int kWarps = RB == 128 ? 6 : RB == 64 ? 7 : 8, kStages = 2;
 };
 
 // Shared memory of a warp: its tiles, the operand area, and the piece of the
