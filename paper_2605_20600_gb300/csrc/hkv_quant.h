@@ -39,17 +39,16 @@ struct QAttnArgs {
   const float *prior_out, *prior_lse;     // [nheads][D], [nheads], or both null
   float *out, *lse;                       // [nheads][D], [nheads] or null
   uint32_t *count;             // [nheads] arrivals, zero between launches
-  uint32_t *done;              // [2] CTAs that have read the lengths and heads
-                               // left to the last one, zero between launches
-  float *part;                 // [kQuantMaxGrid][2][D + 4] partial results
+  float *part;                 // [kQuantMaxParts][D + 4] partial results
   int max_rows;                // rows of the longest segment
-  int sms;
+  int sms, splits;             // of the device; CTAs of a head (the launcher's)
   int P, C, prefetch;
   float qscale;                // log2(e) / sqrt(D)
 };
 
-// most CTAs of the attention (the workspace holds two partial results of each)
-constexpr int kQuantMaxGrid = 1024;
+// most CTAs of the attention that share heads (the workspace holds a partial
+// result of each)
+constexpr int kQuantMaxParts = 2048;
 cudaError_t launch_quant_attention(const QAttnArgs &a, int D, int dtype, int bits, cudaStream_t s);
 
 // attention of a batch over shared prompts, one layer

@@ -60,15 +60,14 @@ hkv_status layer_heads(const hkv_config *cfg, int layer, int *first, int *count)
   return HKV_OK;
 }
 
-// workspace of the attention: two words of the grid's progress and the heads'
-// arrival counters, then partial results
+// workspace of the attention: the heads' arrival counters, then partial results
 size_t quant_counts_bytes(const hkv_config *c) {
-  return align256(((size_t)heads_per_layer(c) + 2) * sizeof(uint32_t));
+  return align256((size_t)heads_per_layer(c) * sizeof(uint32_t));
 }
 
 size_t quant_ws_bytes(const hkv_config *c) {
   return quant_counts_bytes(c) +
-         align256((size_t)kQuantMaxGrid * 2 * (c->head_dim + 4) * sizeof(float));
+         align256((size_t)kQuantMaxParts * (c->head_dim + 4) * sizeof(float));
 }
 
 // SMs of the current device, looked up once
@@ -113,8 +112,7 @@ hkv_status quant_attend(const char *name, const hkv_config *cfg, const hkv_qcach
   a.out = out;
   a.lse = lse;
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  a.done = reinterpret_cast<uint32_t *>(ws);
-  a.count = a.done + 2;
+  a.count = reinterpret_cast<uint32_t *>(ws);
   a.part = reinterpret_cast<float *>(ws + quant_counts_bytes(cfg));
   a.max_rows = max_segment(cfg);
   // tiles of 32 rows are counted in 31 bits

@@ -189,6 +189,40 @@ def test_step_appends_and_attends(bits, D, dtype, label):
         assert abs(gl[h] - l) <= tl
 
 
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[40003], [20000, 3, 256, 0, 257, 9000]])
+def test_long_heads_cut_into_many_parts(bits, D, lens):
+    """Heads cut between CTAs, next to heads too short for it: attention, then
+    steps over one workspace, each bit-identical when it is run again."""
+    import torch
+    c = QCache(lens, D, bits, "bf16", seed=31 + bits + D, lead=3)
+    H = c.H
+    q, k, v = (to_torch(x, "bf16") for x in (c.q, c.k_new, c.v_new))
+    outs = [torch.full((c.n, D), -1.0, device="cuda") for _ in range(2)]
+    for o in outs:
+        H.hkv_quant_attention(c.cfg, c.c, 0, q, o, c.ws, c.ws_bytes)
+    assert torch.equal(*outs)
+    state = (c.ck, c.cv, c.sk, c.sv, c.pos, c.len, c.nbuf, c.ntok, c.qbuf)
+    before = [x.clone() for x in state]
+    steps = []
+    for o in outs:
+        for x, b in zip(state, before):
+            x.copy_(b)
+        H.hkv_quant_step(c.cfg, c.c, 0, q, k, v, o, c.ws, c.ws_bytes)
+        steps.append([x.clone().view(torch.uint8) for x in state])
+    H.hkv_quant_check(c.c)
+    assert torch.equal(*outs) and all(torch.equal(a, b) for a, b in zip(*steps))
+    assert np.array_equal(c.len.cpu().numpy(), c.lens + 1)
+    got = outs[0].cpu().numpy()
+    for h in range(c.n):
+        K, V = c.rows(h, step=True)
+        o, _ = S.attention_lse(c.q[h], K, V)
+        to, _ = tolerances(c.q[h], K, V)
+        assert np.abs(got[h] - o).max() <= to, (h, np.abs(got[h] - o).max(), to)
+    assert int(c.ws[:4 * c.n].sum()) == 0
+
+
 def test_step_refuses_per_head_through_the_error_word():
     import torch
     for what, code in (("full", 3), ("buffer", 4), ("outside", 5)):
