@@ -146,9 +146,9 @@ hkv_status hkv_quant_step(const hkv_config *cfg, const hkv_qcache *cache, int la
  * taken from what the key rows stand for (s c in fp32, the sums in the same
  * fixed fp32 order); rows move with their scales. The i-th evicted row below
  * the new length, in storage order, takes the i-th surviving row above it.
- * The larger of period * head_dim * elem (elem of the config dtype) and 256 *
- * (head_dim * format / 8 + 16) bytes, plus 16 bytes per token of the longest
- * segment, must fit in 227 KB, else HKV_ERR_CAPACITY. */
+ * The larger of period * head_dim * elem (elem of the config dtype) and 32 *
+ * head_dim * format bytes, plus 16 bytes per token of the longest segment,
+ * must fit in 227 KB, else HKV_ERR_CAPACITY. */
 hkv_status hkv_quant_evict(const hkv_config *cfg, const hkv_qcache *cache, int layer,
                            hkv_stream_t stream);
 hkv_status hkv_quant_evict_all(const hkv_config *cfg, const hkv_qcache *cache, hkv_stream_t stream);

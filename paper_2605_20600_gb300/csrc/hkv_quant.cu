@@ -1,5 +1,7 @@
 // The quantised cache outside its attention: rows written from a plain cache
 // (pack), read back into one (unpack), and the periodic head-aware update.
+#include <type_traits>
+
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
@@ -174,17 +176,24 @@ __global__ void __launch_bounds__(kRowThreads, 6)
 // sum rounded to fp32 by itself.
 template <int D, int BITS>
 struct CodeRows {
-  static constexpr int kBytes = QRow<D, BITS>::kBytes;
+  static constexpr int kBytes = QRow<D, BITS>::kBytes, kStride = kBytes;
+  static constexpr int G = QRow<D, BITS>::kGroups;
   const uint16_t *scale;  // the segment's first row
+  // the row's scales, loaded while its codes are on their way
+  using Ahead = typename std::conditional<G == 4, unsigned long long, uint32_t>::type;
+  __device__ __forceinline__ Ahead ahead(int r) const {
+    return reinterpret_cast<const Ahead *>(scale)[r];
+  }
+  __device__ __forceinline__ static int piece(int rr, int pc) { return piece_at<kBytes>(rr, pc); }
   // one group's part: HUGE where s 2^16 might overflow, else s c = s (2^15 + u) -
   // s (2^15 + bias) in one fma, exact: the second product has at most 21 bits
   template <bool HUGE>
-  __device__ __forceinline__ float group(const unsigned char *codes, const float *q, float sc,
-                                         float s) const {
+  __device__ __forceinline__ float group(const unsigned char *stage, int rr, int g, const float *q,
+                                         float sc, float s) const {
     const float minus = -sc * kLift<BITS>;
 #pragma unroll
     for (int pc = 0; pc < BITS / 4; ++pc) {
-      const uint4 u = reinterpret_cast<const uint4 *>(codes)[pc];
+      const uint4 u = *reinterpret_cast<const uint4 *>(stage + piece(rr, g * (BITS / 4) + pc));
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
       constexpr int CPW = 32 / BITS;  // codes a word
 #pragma unroll
@@ -196,14 +205,14 @@ struct CodeRows {
     }
     return s;
   }
-  __device__ __forceinline__ float dot(const unsigned char *krow, const float *qbar, int r) const {
-    constexpr int G = QRow<D, BITS>::kGroups;
+  __device__ __forceinline__ float dot(const unsigned char *stage, int rr, const float *qbar,
+                                       Ahead scales) const {
     float s = 0.f;
 #pragma unroll 1
     for (int g = 0; g < G; ++g) {
-      const float sc = bf16_bits_to_float(scale[(size_t)r * G + g]);
-      s = sc < 0x1p100f ? group<false>(krow + g * 4 * BITS, qbar + g * 32, sc, s)
-                        : group<true>(krow + g * 4 * BITS, qbar + g * 32, sc, s);
+      const float sc = bf16_bits_to_float((uint32_t)(scales >> (16 * g)) & 0xFFFFu);
+      s = sc < 0x1p100f ? group<false>(stage, rr, g, qbar + g * 32, sc, s)
+                        : group<true>(stage, rr, g, qbar + g * 32, sc, s);
     }
     return s;
   }

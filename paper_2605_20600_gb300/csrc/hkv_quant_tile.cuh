@@ -122,15 +122,6 @@ struct TileOf {
   static constexpr int kOperand = 2 * D * 2;
 };
 
-// Byte offset of the 16-byte piece `c` of row `r` in a tile: rows lie back to
-// back, the pieces permuted so that the reads below spread over all banks.
-template <int RB>
-__device__ __forceinline__ int piece_at(int r, int c) {
-  if (RB == 128) return r * 128 + ((c ^ (r & 7)) << 4);
-  if (RB == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
-  return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
-}
-
 // A head as its tiles see it.
 struct HeadRef {
   long long off;

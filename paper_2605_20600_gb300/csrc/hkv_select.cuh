@@ -77,10 +77,10 @@ __host__ __device__ constexpr int stage_rows(int max_len) {
 
 // the query ring (P rows of es-byte elements); after q-bar it is the score
 // stage: NT/32 warps x stage_rows rows of D * es + 16 bytes
-// (or of kb + 16, key rows of kb bytes)
+// (or of kb bytes, key rows of codes)
 __host__ __device__ constexpr size_t ring_bytes(int P, int D, int es, int max_len, int kb = 0) {
   const size_t ring = (size_t)P * D * es;
-  const size_t stage = (size_t)(NT / 32) * stage_rows(max_len) * ((kb ? kb : D * es) + 16);
+  const size_t stage = (size_t)(NT / 32) * stage_rows(max_len) * (kb ? kb : D * es + 16);
   return ring > stage ? ring : stage;
 }
 
@@ -176,8 +176,16 @@ __device__ __forceinline__ int block_sum(int x, UpdShared &sh) {
 template <int D, typename T>
 struct PlainRows {
   static constexpr int kBytes = D * (int)sizeof(T);
-  __device__ __forceinline__ float dot(const unsigned char *krow, const float *qbar, int) const {
+  static constexpr int kStride = kBytes + 16;  // of a staged row
+  struct Ahead {};
+  __device__ __forceinline__ Ahead ahead(int) const { return {}; }
+  // byte offset of piece pc of staged row rr: lanes that read one piece of
+  // successive rows hit distinct banks
+  __device__ __forceinline__ static int piece(int rr, int pc) { return rr * kStride + pc * 16; }
+  __device__ __forceinline__ float dot(const unsigned char *stage, int rr, const float *qbar,
+                                       Ahead) const {
     constexpr int EPL = Elem<T>::kPerPiece;
+    const unsigned char *krow = stage + rr * kStride;
     float s = 0.f;
 #pragma unroll 4
     for (int pc = 0; pc < kBytes / 16; ++pc) {
@@ -279,24 +287,26 @@ __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m
     __syncthreads();
     HKV_UTRACE(3);
     // Each warp stages 32 rows at a time in the (now free) ring area with
-    // coalesced 16-byte async copies, at a row stride of LPR + 1 pieces so
-    // that lane l reading row l, piece j, hits distinct banks; then lane l
-    // sums its row in the fixed order.
-    constexpr int RS = LPR + 1;  // row stride in 16-byte pieces
+    // coalesced 16-byte async copies, laid out so that lane l reading row l,
+    // piece j, hits distinct banks; then lane l sums its row in the fixed
+    // order.
     const int warp = tid >> 5, lane = tid & 31;
     const int SR = u.stage_rows;
-    unsigned char *stage = u.ring + (size_t)warp * SR * RS * 16;
+    unsigned char *stage = u.ring + (size_t)warp * SR * Rows::kStride;
     for (int base = warp * SR; base < sg.len; base += (NT / 32) * SR) {
       const int nrows = sg.len - base < SR ? sg.len - base : SR;
       for (int w = lane; w < nrows * LPR; w += 32) {
         const int rr = w / LPR, pc = w % LPR;
-        cp_async16(stage + (rr * RS + pc) * 16, sg.sk + (size_t)(base + rr) * KB + pc * 16);
+        cp_async16(stage + Rows::piece(rr, pc), sg.sk + (size_t)(base + rr) * KB + pc * 16);
       }
+      const int r = base + lane;
+      const bool scored = lane < nrows && u.aux[r] >= 0;
+      typename Rows::Ahead ah = {};
+      if (scored) ah = rows.ahead(r);
       cp_async_wait_all();
       __syncwarp();
-      const int r = base + lane;
-      if (lane < nrows && u.aux[r] >= 0) {
-        float s = rows.dot(stage + lane * RS * 16, u.qbar, r);
+      if (scored) {
+        float s = rows.dot(stage, lane, u.qbar, ah);
         s = __fadd_rn(s, 0.f);  // -0 reads as +0
         uint32_t bits = __float_as_uint(s);
         bits = (bits & 0x80000000u) ? ~bits : (bits | 0x80000000u);  // order-preserving
