@@ -167,7 +167,10 @@ size_t hkv_prefix_workspace_size(const hkv_config *cfg, const hkv_prefix *prefix
  * lse[s][h] as hkv_quant_attention defines them (both required), to be given
  * to hkv_quant_step or hkv_quant_attention as prior. A prompt of length 0
  * yields zeros and -inf. n_seqs not a multiple of n_groups, or strides that
- * are not multiples of 16 bytes -> HKV_ERR_SHAPE. */
+ * are not multiples of 16 bytes -> HKV_ERR_SHAPE. A group whose length is
+ * negative or above max_len gets NaN, and HKV_ERR_BOUNDS in the error word;
+ * so does one whose products did not finish within the kernel's limit of two
+ * seconds, with HKV_ERR_TIMEOUT. */
 hkv_status hkv_prefix_attention(const hkv_config *cfg, const hkv_prefix *prefix, const void *q,
                                 float *out, float *lse, void *workspace, size_t ws_bytes,
                                 hkv_stream_t stream);

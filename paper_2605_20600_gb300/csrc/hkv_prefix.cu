@@ -1,16 +1,29 @@
 // Attention of a batch over prompts that its sequences share: every prompt
 // row serves all sequences of its group.
 //
-// A CTA takes up to 64 queries of one (group, head) and a range of the
-// prompt's keys, tile by tile (64 keys), on the tensor cores (mma.sync
-// m16n8k16, bf16 operands, fp32 sums). MW warps lie along the queries, 16
-// each, the others along the keys of a tile; their results are joined in
-// shared memory. Ranges of one prompt are joined by a second kernel.
+// A CTA takes the queries of one (group, head) and a range of the prompt's
+// keys, in tiles of 64 keys; the ranges of one prompt are joined by a second
+// kernel. bf16 batches of more than 16 sequences a group go to tcgen05
+// (prefix_tc_kernel). Up to 16 queries, which fill an eighth of a tcgen05
+// product's rows, and fp32, whose six products of parts would not leave room in
+// TMEM, are prefix_kernel's (mma.sync m16n8k16): MW warps lie along the
+// queries, 16 each, the others along the keys of a tile, joined in shared
+// memory.
 //
 // Precision: bf16 queries, keys and values enter as they are, and the weights
 // as three bf16 parts (24 bits); an fp32 element is three parts as well, and
 // the six products of parts that reach past 2^-24 are taken, the small ones
-// first. Products chain in the tensor core within a tile only.
+// first. Sums are fp32; products chain in the tensor core within a tile
+// (prefix_kernel) or a range (O of prefix_tc_kernel).
+//
+// What bounds it: the chain of one tile (scores, weights, output, with a wait
+// between any two), about 2 us a tile, and the start and the join around it.
+// 32 heads x 4099 keys of 128 channels, 64 queries: 29 us, of which DRAM (67 MB)
+// needs 10; 20 heads, two prompts of 1000 and 667 keys of 64 channels: 14 us;
+// fp32, 8 heads x 777 keys, 5 queries: 12 us. One launch with the ranges of a
+// prompt in a cluster, joined through distributed shared memory, took 18 us
+// for the second (a cluster waits for room for all its CTAs, and half of its
+// warps wait while the others join).
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
@@ -705,8 +718,9 @@ cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStrea
 }  // namespace
 
 // As many key ranges as fill the device twice over (2 CTAs an SM), each a
-// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05,
-// where 128 queries cost what 16 do here.
+// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05:
+// over 32 heads x 4099 keys, 16 sequences take 23 us with mma.sync and 27 with
+// tcgen05, 32 take 29 and 28, 64 take 43 and 32.
 PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int dtype) {
   PrefixPlan pl;
   pl.mw = seqs <= 16 ? 1 : seqs <= 32 ? 2 : 4;
