@@ -54,14 +54,15 @@ constexpr float kLift = 32768.f + (BITS == 8 ? 128.f : 8.f);
 // magnitudes are compared as integers, so that a NaN or an infinity in the
 // group shows (its bits are the largest).
 //
-// bf16 values, without a division: q = x * rcp(s) is within 2^-21 of x / s;
-// q + (x - q s) rcp(s), the remainder exact in an fma, is within 2^-40, so a
-// quotient that fp32 holds comes out exactly, every tie k + 1/2 among them.
-// Other quotients are at least 2^-16 from a tie (x and s have 8 bits and k + 1/2
-// at most 8: 2 x and (2 k + 1) s are integers below 2^16 on a common grid), so
-// adding 1.5 * 2^23 rounds them as x / s itself would be. a / M is at least as
-// far from the midpoint of two bf16 numbers, so a product with 1 / M rounds
-// alike. fp32 values, and groups whose scale is tiny, take the quotients.
+// bf16 values, without a division: x rcp(s) is within 2^-16 of x / s (at most
+// 2^7 in magnitude), and one fma rounds it to a grid of 2^-12. A tie k + 1/2
+// lies on the grid and is met exactly; any other quotient is more than 2^-10
+// from a tie (x and s have 8 bits, so 2 x - (2 k + 1) s is at least a unit of
+// 2 x or of s, which is 1/255 of it or more) and stays on its side; so rounding
+// that to an integer, the sum with 1.5 * 2^23, rounds as x / s itself would be.
+// a / M is at least 2^-16 (relative) from the midpoint of two bf16 numbers, so a
+// product with 1 / M rounds alike. fp32 values, and groups whose scale is tiny,
+// take the quotients.
 template <typename T, int BITS>
 __device__ __forceinline__ uint32_t quant_group(const float *x, uint32_t mask, uint32_t &lo,
                                                 uint32_t &hi) {
@@ -75,16 +76,14 @@ __device__ __forceinline__ uint32_t quant_group(const float *x, uint32_t mask, u
   float s;
   uint32_t sb;
   if (sizeof(T) == 2 && a >= 0x0E000000u && a < 0x7F800000u) {  // 2^-99 <= a, finite
-    constexpr float kMagic = 12582912.f + kBias;
+    constexpr float kGrid = 2560.f, kInt = 12582912.f + kBias - kGrid;
     sb = __bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(a) * (1.f / kMax)));
     s = bf16_bits_to_float(sb);
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float q = x[j] * inv;
-      c[j] = __float_as_uint(__fadd_rn(fmaf(fmaf(-q, s, x[j]), inv, q), kMagic));
-    }
+    for (int j = 0; j < 8; ++j)
+      c[j] = __float_as_uint(__fadd_rn(__fmaf_rn(x[j], inv, kGrid), kInt));
   } else {
     const bool finite = a < 0x7F800000u;
     const float q = __fdiv_rn(__uint_as_float(a), (float)kMax);

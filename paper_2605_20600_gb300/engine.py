@@ -217,6 +217,8 @@ class Engine:
         self.quant_ws = torch.zeros(self.quant_ws_bytes, dtype=torch.uint8, device=dev)
         self.off, self.cap, self.total_tokens = off, cap, total
         self.cache = self.quant = quant
+        for x in (self.ragged.k, self.ragged.v, self.ragged.pos):
+            x.record_stream(torch.cuda.current_stream())   # the pack may still have to read it
         self.ragged.k = self.ragged.v = self.ragged.pos = None
 
     def _quant_step(self, layer: int, q, k, v, out, flags: int) -> None:

@@ -223,6 +223,41 @@ def test_long_heads_cut_into_many_parts(bits, D, lens):
     assert int(c.ws[:4 * c.n].sum()) == 0
 
 
+@pytest.mark.parametrize("bits", FMT)
+def test_every_bf16_quotient_rounds_as_defined(bits):
+    """Groups whose largest value has each bf16 significand, holding every bf16
+    value from it down to where all codes are 0, both signs: exact codes."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import QuantCacheBuffers
+    D, M = 128, 127 if bits == 8 else 7
+    steps = int(math.ceil(math.log2(4 * M)))
+    groups = []
+    for i in range(128):
+        top = 1 + i / 128
+        x = np.array([(1 + j / 128) * 2.0 ** -e for e in range(steps) for j in range(128)])
+        x = x[x <= top]
+        x = np.concatenate([x, -x])
+        x = np.concatenate([x, np.zeros(-len(x) % 31)]).reshape(-1, 31)
+        groups.append(np.concatenate([np.full((len(x), 1), top), x], 1))
+    g = np.concatenate(groups)
+    g = np.concatenate([g, np.zeros((-len(g) % 4, 32))]).reshape(-1, D).astype(np.float32)
+    v = g[::-1].copy()
+    n = len(g)
+    cfg = H.make_config(n_layers=1, n_seqs=1, n_heads=1, head_dim=D, dtype="bf16", n_cond=0,
+                        n_image=n, row_len=1, recent_w=1, local_w=1, period=1, group_at=n,
+                        global_budget=1)
+    src = plain_cache(H, cfg, [n], [n], "bf16", g, v)
+    dst = QuantCacheBuffers(cfg, bits, n, "cuda", qbuf=src.qbuf, label=src.label, off=src.off,
+                            cap=src.cap)
+    H.hkv_quant_pack(cfg, src.c, dst.c, 0, 0, 0)
+    H.hkv_quant_check(dst.c)
+    for x, codes, scales in ((g, dst.k, dst.ks), (v, dst.v, dst.vs)):
+        cc, ss = S.quantise(x, bits)
+        assert np.array_equal(scales.float().cpu().numpy(), ss)
+        assert np.array_equal(codes.cpu().numpy(), S.packed(cc, bits))
+
+
 def test_step_refuses_per_head_through_the_error_word():
     import torch
     for what, code in (("full", 3), ("buffer", 4), ("outside", 5)):
