@@ -9,24 +9,32 @@
 namespace hkv {
 namespace {
 
-// Pack and unpack: 8 values of K and V a thread, D / 8 threads a row, two rows
-// in flight a thread; a group's maximum comes from its four lanes. DRAM bounds
-// them: 512 heads of up to 1168 rows of 128 bf16 channels go to 8 bits and back
-// in 115 us (578 MB: 5.0 TB/s, 74 % of a copy), the reads alone of two passes
-// with a dependent chain of length, offset and row in front of each CTA.
+// Pack and unpack: 8 values of K and V a thread, D / 8 threads a row; a group's
+// maximum comes from its four lanes. DRAM bounds them: 512 heads of up to 1168
+// rows of 128 bf16 channels go to 8 bits and back in 104 us (578 MB: 5.6 TB/s,
+// 82 % of a copy). Pack computes more than half of the time, so it takes the
+// threads of eight CTAs an SM over a second row in flight (five with two rows:
+// 111 us); unpack waits more and keeps two. A CTA takes 64 rows, or 32 where the
+// launch has few CTAs: 99 heads of up to 393 fp32 rows to 4 bits and back 13.7 us
+// against 14.7 with 64 (the case above 115 with 32). fp32 rows, whose quotients
+// are taken, keep the registers of five CTAs: 12.1 us for the 99 heads.
 constexpr int kRowThreads = 256;
-constexpr int kRowsPerCta = 64;
+constexpr int kManyCtas = 1024;
+
+int rows_of(int count, int max_len) {
+  return (long long)count * ((max_len + 63) / 64) < kManyCtas ? 32 : 64;
+}
 
 __device__ __forceinline__ bool segment_ok(long long off, int cap, int len, long long arena) {
   return off >= 0 && cap >= 0 && off + cap <= arena && len >= 0 && len <= cap;
 }
 
-// One CTA: up to kRowsPerCta rows of one head. Block 0 of a head also sets
+// One CTA: up to `rows` rows of one head. Block 0 of a head also sets
 // its counters.
 template <int D, typename T, int BITS>
-__global__ void __launch_bounds__(kRowThreads, 5)
+__global__ void __launch_bounds__(kRowThreads, sizeof(T) == 2 ? 8 : 5)
     pack_kernel(const CacheArgs src, const QCacheArgs dst, int first, int blocks, int skip,
-                int max_len) {
+                int max_len, int rows) {
   using R = QRow<D, BITS>;
   constexpr int TPR = D / 8;  // threads per row
   // no early launch of the next kernel: a decode step that prefetches this
@@ -54,44 +62,32 @@ __global__ void __launch_bounds__(kRowThreads, 5)
     dst.c.nbuf[i] = src.nbuf[i];
     dst.c.ntok[i] = src.ntok[i];
   }
-  const int r_end = min(n, (b + 1) * kRowsPerCta);
+  const int r_end = min(n, (b + 1) * rows);
   const int col = tid % TPR;
   const uint32_t mask = 0xFu << (threadIdx.x & 28);  // the four lanes of a group
-  constexpr int STEP = kRowThreads / TPR, U = 2;  // rows in flight a thread
-  constexpr int PCS = (int)sizeof(T) / 2;         // 16-byte pieces of 8 values
-  for (int r0 = b * kRowsPerCta + tid / TPR; r0 < r_end; r0 += U * STEP) {
-    uint4 raw[U][2][PCS];
+  constexpr int PCS = (int)sizeof(T) / 2;            // 16-byte pieces of 8 values
+  for (int r = b * rows + tid / TPR; r < r_end; r += kRowThreads / TPR) {
+    uint4 raw[2][PCS];
+    const long long so = ((soff + skip + r) * (D / 8) + col) * PCS, dof = doff + r;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (r0 + u * STEP < r_end) {
-        const long long so = ((soff + skip + r0 + u * STEP) * (D / 8) + col) * PCS;
-#pragma unroll
-        for (int j = 0; j < PCS; ++j) {
-          raw[u][0][j] = static_cast<const uint4 *>(src.K)[so + j];
-          raw[u][1][j] = static_cast<const uint4 *>(src.V)[so + j];
-        }
-      }
+    for (int j = 0; j < PCS; ++j) {
+      raw[0][j] = static_cast<const uint4 *>(src.K)[so + j];
+      raw[1][j] = static_cast<const uint4 *>(src.V)[so + j];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * STEP;
-      if (r >= r_end) break;
-      const long long dof = doff + r;
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[8];
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < PCS; ++j) Elem<T>::unpack(raw[u][kv][j], x + j * Elem<T>::kPerPiece);
-        uint32_t lo, hi;
-        const uint32_t sb = quant_group<T, BITS>(x, mask, lo, hi);
-        unsigned char *out = static_cast<unsigned char *>(kv ? dst.c.V : dst.c.K) + dof * R::kBytes;
-        if (BITS == 8) reinterpret_cast<uint2 *>(out)[col] = make_uint2(lo, hi);
-        else reinterpret_cast<uint32_t *>(out)[col] = lo;
-        if ((col & 3) == 0)
-          static_cast<uint16_t *>(kv ? dst.vs : dst.ks)[dof * R::kGroups + col / 4] = (uint16_t)sb;
-      }
-      if (col == 0) dst.c.pos[dof] = src.pos[soff + skip + r] - skip;
+      for (int j = 0; j < PCS; ++j) Elem<T>::unpack(raw[kv][j], x + j * Elem<T>::kPerPiece);
+      uint32_t lo, hi;
+      const uint32_t sb = quant_group<T, BITS>(x, mask, lo, hi);
+      unsigned char *out = static_cast<unsigned char *>(kv ? dst.c.V : dst.c.K) + dof * R::kBytes;
+      if (BITS == 8) reinterpret_cast<uint2 *>(out)[col] = make_uint2(lo, hi);
+      else reinterpret_cast<uint32_t *>(out)[col] = lo;
+      if ((col & 3) == 0)
+        static_cast<uint16_t *>(kv ? dst.vs : dst.ks)[dof * R::kGroups + col / 4] = (uint16_t)sb;
     }
+    if (col == 0) dst.c.pos[dof] = src.pos[soff + skip + r] - skip;
   }
 }
 
@@ -112,7 +108,8 @@ __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, const fl
 
 template <int D, typename T, int BITS>
 __global__ void __launch_bounds__(kRowThreads, 6)
-    unpack_kernel(const QCacheArgs src, const CacheArgs dst, int first, int blocks, int max_len) {
+    unpack_kernel(const QCacheArgs src, const CacheArgs dst, int first, int blocks, int max_len,
+                  int rows) {
   using R = QRow<D, BITS>;
   constexpr int TPR = D / 8;
   pdl_wait();  // no early launch of the next kernel, as in pack_kernel
@@ -135,10 +132,10 @@ __global__ void __launch_bounds__(kRowThreads, 6)
     dst.nbuf[i] = src.c.nbuf[i];
     dst.ntok[i] = src.c.ntok[i];
   }
-  const int r_end = min(n, (b + 1) * kRowsPerCta);
+  const int r_end = min(n, (b + 1) * rows);
   const int col = tid % TPR;
   constexpr int STEP = kRowThreads / TPR, U = 2;  // rows in flight a thread
-  for (int r0 = b * kRowsPerCta + tid / TPR; r0 < r_end; r0 += U * STEP) {
+  for (int r0 = b * rows + tid / TPR; r0 < r_end; r0 += U * STEP) {
     uint2 w[U][2];
     uint32_t sc[U][2];
 #pragma unroll
@@ -337,21 +334,21 @@ __global__ void __launch_bounds__(NT, kQuantUpdCtasPerSm)
 
 cudaError_t launch_quant_pack(const CacheArgs &src, const QCacheArgs &dst, int first, int count,
                               int skip, int max_len, int D, int dtype, int bits, cudaStream_t s) {
-  const int blocks = (max_len + kRowsPerCta - 1) / kRowsPerCta;
+  const int rows = rows_of(count, max_len), blocks = (max_len + rows - 1) / rows;
   if ((long long)blocks * count > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   HKV_QDISPATCH(D, dtype, bits,
                 return pdl_launch(pack_kernel<kD, kT, kBits>, blocks * count, kRowThreads, 0, s,
-                                  src, dst, first, blocks, skip, max_len));
+                                  src, dst, first, blocks, skip, max_len, rows));
   return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_quant_unpack(const QCacheArgs &src, const CacheArgs &dst, int first, int count,
                                 int max_len, int D, int dtype, int bits, cudaStream_t s) {
-  const int blocks = (max_len + kRowsPerCta - 1) / kRowsPerCta;
+  const int rows = rows_of(count, max_len), blocks = (max_len + rows - 1) / rows;
   if ((long long)blocks * count > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   HKV_QDISPATCH(D, dtype, bits,
                 return pdl_launch(unpack_kernel<kD, kT, kBits>, blocks * count, kRowThreads, 0, s,
-                                  src, dst, first, blocks, max_len));
+                                  src, dst, first, blocks, max_len, rows));
   return cudaErrorInvalidValue;
 }
 
