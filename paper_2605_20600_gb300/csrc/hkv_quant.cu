@@ -15,7 +15,7 @@ namespace {
 // 82 % of a copy). Pack computes more than half of the time, so it takes the
 // threads of eight CTAs an SM over a second row in flight (five with two rows:
 // 111 us); unpack waits more and keeps two. A CTA takes 64 rows, or 32 where the
-// launch has few CTAs: 99 heads of up to 393 fp32 rows to 4 bits and back 13.7 us
+// launch has few CTAs: 99 heads of up to 357 fp32 rows to 4 bits and back 13.7 us
 // against 14.7 with 64 (the case above 115 with 32). fp32 rows, whose quotients
 // are taken, keep the registers of five CTAs: 12.1 us for the 99 heads.
 constexpr int kRowThreads = 256;
