@@ -19,10 +19,10 @@
 // What bounds it: the chain of one tile (scores, weights, output, with a wait
 // between any two), about 2 us a tile, and the start and the join around it.
 // 32 heads x 4099 keys of 128 channels, 64 queries: 29 us, of which DRAM (67 MB)
-// needs 10; 20 heads, two prompts of 1000 and 667 keys of 64 channels: 14 us;
-// fp32, 8 heads x 777 keys, 5 queries: 12 us. One launch with the ranges of a
+// needs 10; 20 heads, two prompts of 1000 and 667 keys of 64 channels: 12 us;
+// fp32, 8 heads x 777 keys, 5 queries: 10 us. One launch with the ranges of a
 // prompt in a cluster, joined through distributed shared memory, took 18 us
-// for the second (a cluster waits for room for all its CTAs, and half of its
+// for the second, 15 for two launches then (a cluster waits for room for all its CTAs, and half of its
 // warps wait while the others join).
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
@@ -481,12 +481,9 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   for (int k0 = lo; k0 < hi; k0 += kKeys, phase ^= 1, st ^= 1) {
     // O holds the tiles before this one, and their stage is free
     if (k0 > lo) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
-    if (__syncthreads_or(!ok)) break;
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
-    if (k0 + kKeys < hi) load_tile(k0 + kKeys, st ^ 1);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (__syncthreads_or(!ok)) break;
     const uint32_t kb = smem_u32(skv + st * 2 * SM::kTile), vb = kb + SM::kTile;
     if (tid == 0) {
       tc_fence_after();
@@ -498,6 +495,8 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                tc_instr(kTcQueries, kKeys, false), ks > 0);
       tc_commit(&s_bar[0]);
     }
+    if (k0 + kKeys < hi) load_tile(k0 + kKeys, st ^ 1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
     ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[0], phase));
     tc_fence_after();
     if (works && ok) {
@@ -668,6 +667,14 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   const float *first = p.part + (size_t)row * p.splits * PF;
   float2 ml = make_float2(-INFINITY, 0.f);
   if (lane < p.splits) ml = *reinterpret_cast<const float2 *>(first + (size_t)lane * PF + D);
+  constexpr int B = 8;  // parts on their way at a time, the first before their weights
+  float v[B][E];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int j = 0; j < B; ++j)
+      if (j0 + j < p.splits) load_row<E>(first + (size_t)(j0 + j) * PF + lane * E, v[j]);
+  };
+  load(0);
   const bool bad = __any_sync(0xFFFFFFFFu, ml.x != ml.x && ml.y == 0.f);
   float m = ml.x;
 #pragma unroll
@@ -679,17 +686,16 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   float acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 8
-  for (int j = 0; j < p.splits; ++j) {
-    const float fj = __shfl_sync(0xFFFFFFFFu, f, j);
-    const float *src = first + (size_t)j * PF + lane * E;
-    if (E == 4) {
-      const float4 u = *reinterpret_cast<const float4 *>(src);
-      acc[0] += u.x * fj, acc[1 % E] += u.y * fj, acc[2 % E] += u.z * fj, acc[3 % E] += u.w * fj;
-    } else {
-      const float2 u = *reinterpret_cast<const float2 *>(src);
-      acc[0] += u.x * fj, acc[1 % E] += u.y * fj;
+  for (int j0 = 0; j0 < p.splits; j0 += B) {
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const float fj = __shfl_sync(0xFFFFFFFFu, f, (j0 + j) & 31);
+      if (j0 + j < p.splits) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += v[j][e] * fj;
+      }
     }
+    load(j0 + B);
   }
   const float inv = bad ? NAN : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll

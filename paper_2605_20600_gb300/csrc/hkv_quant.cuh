@@ -115,4 +115,16 @@ __device__ __forceinline__ int piece_at(int r, int c) {
   return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
 }
 
+// E neighbouring fp32 numbers of a partial result, past L1
+template <int E>
+__device__ __forceinline__ void load_row(const float *from, float (&o)[E]) {
+  if (E == 4) {
+    const float4 u = __ldcg(reinterpret_cast<const float4 *>(from));
+    o[0] = u.x, o[1 % E] = u.y, o[2 % E] = u.z, o[3 % E] = u.w;
+  } else {
+    const float2 u = __ldcg(reinterpret_cast<const float2 *>(from));
+    o[0] = u.x, o[1 % E] = u.y;
+  }
+}
+
 }  // namespace hkv

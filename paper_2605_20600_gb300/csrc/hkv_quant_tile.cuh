@@ -493,17 +493,6 @@ __device__ __forceinline__ void store_row(float *to, const float (&o)[E]) {
   if (E == 4) *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1 % E], o[2 % E], o[3 % E]);
   else *reinterpret_cast<float2 *>(to) = make_float2(o[0], o[1 % E]);
 }
-template <int E>
-__device__ __forceinline__ void load_row(const float *from, float (&o)[E]) {  // past L1
-  if (E == 4) {
-    const float4 u = __ldcg(reinterpret_cast<const float4 *>(from));
-    o[0] = u.x, o[1 % E] = u.y, o[2 % E] = u.z, o[3 % E] = u.w;
-  } else {
-    const float2 u = __ldcg(reinterpret_cast<const float2 *>(from));
-    o[0] = u.x, o[1 % E] = u.y;
-  }
-}
-
 // A head's result, channels lane * E .. of the unnormalised output: joined
 // with the prior, normalised and written. The whole warp calls.
 template <int D>
