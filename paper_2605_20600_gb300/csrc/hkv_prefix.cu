@@ -3,12 +3,12 @@
 //
 // A CTA takes the queries of one (group, head) and a range of the prompt's
 // keys, in tiles of 64 keys; the ranges of one prompt are joined by a second
-// kernel. bf16 batches of more than 16 sequences a group go to tcgen05
-// (prefix_tc_kernel). Up to 16 queries, which fill an eighth of a tcgen05
-// product's rows, and fp32, whose six products of parts would not leave room in
-// TMEM, are prefix_kernel's (mma.sync m16n8k16): MW warps lie along the
-// queries, 16 each, the others along the keys of a tile, joined in shared
-// memory.
+// kernel. bf16 batches of more than 16 sequences a group and more than a few
+// tiles go to tcgen05 (prefix_tc_kernel). Up to 16 queries, which fill an eighth
+// of a tcgen05 product's rows, small batches, and fp32, whose six products of
+// parts would not leave room in TMEM, are prefix_kernel's (mma.sync m16n8k16):
+// MW warps lie along the queries, 16 each, the others along the keys of a tile,
+// joined in shared memory.
 //
 // Precision: bf16 queries, keys and values enter as they are, and the weights
 // as three bf16 parts (24 bits); an fp32 element is three parts as well, and
@@ -724,19 +724,23 @@ cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStrea
 }  // namespace
 
 // As many key ranges as fill the device twice over (2 CTAs an SM), each a
-// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05:
-// over 32 heads x 4099 keys, 16 sequences take 23 us with mma.sync and 27 with
-// tcgen05, 32 take 29 and 28, 64 take 43 and 32.
+// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05
+// unless all their products of 16 queries and a tile are done in two rounds of
+// CTAs: over 32 heads of 128 channels, 16 sequences and 4099 keys take 23 us
+// with mma.sync and 27 with tcgen05; 32 take 29 and 28; 64 take 43 and 32, with
+// 500 keys 14 and 14, with 64 keys 6 and 8.
 PrefixPlan prefix_plan(int groups, int seqs, int heads, int max_len, int dtype) {
+  constexpr int kCtas = 304;
   PrefixPlan pl;
-  pl.mw = seqs <= 16 ? 1 : seqs <= 32 ? 2 : 4;
-  if (dtype == HKV_BF16 && seqs > 16) pl.mw = 8;
+  const long long key_tiles = (max_len + kKeys - 1) / kKeys;
+  const long long products = (long long)groups * heads * ((seqs + 15) / 16) * key_tiles;
+  if (dtype == HKV_BF16) pl.mw = seqs <= 16 || products <= 2 * kCtas ? 1 : 8;
+  else pl.mw = seqs <= 16 ? 1 : seqs <= 32 ? 2 : 4;
   pl.tiles = (seqs + pl.mw * 16 - 1) / (pl.mw * 16);
   const long long base = (long long)groups * heads * pl.tiles;
-  long long want = 304 / base;
-  const long long most = (max_len + kKeys - 1) / kKeys;
+  long long want = kCtas / base;
   if (want > kMostSplits) want = kMostSplits;
-  if (want > most) want = most;
+  if (want > key_tiles) want = key_tiles;
   if (want < 1) want = 1;
   pl.split_len = (int)(((max_len + want - 1) / want + kKeys - 1) / kKeys * kKeys);
   pl.splits = (max_len + pl.split_len - 1) / pl.split_len;

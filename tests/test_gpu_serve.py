@@ -567,16 +567,10 @@ def prefix_rows(rng, G, Hh, T, D, dtype, layout):
     return k, v
 
 
-@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp32"), (128, "fp32")])
-@pytest.mark.parametrize("G,seqs,T,lens,layout", [
-    (1, 1, 1, [1], "htd"), (1, 3, 17, [17], "thd"), (1, 16, 64, [64], "padded"),
-    (2, 9, 130, [130, 0], "htd"), (3, 17, 333, [200, 333, 1], "thd"), (1, 40, 1025, [1025], "htd"),
-    (2, 70, 257, [255, 256], "padded"), (1, 130, 500, [463], "thd")])
-def test_prefix_attention(D, dtype, G, seqs, T, lens, layout):
+def check_prefix(D, dtype, G, seqs, T, lens, layout, Hh):
     import torch
     from paper_2605_20600_gb300 import hkv as H
     rng = np.random.default_rng(D + T + seqs)
-    Hh = 3
     cfg = H.make_config(n_layers=1, n_seqs=G * seqs, n_heads=Hh, head_dim=D, dtype=dtype, n_cond=0,
                         n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
                         global_budget=1)
@@ -604,6 +598,24 @@ def test_prefix_attention(D, dtype, G, seqs, T, lens, layout):
             to, tl = tolerances(q[s, h], K, V)
             assert np.abs(got[s, h] - o).max() <= to, (s, h, np.abs(got[s, h] - o).max(), to)
             assert gl[s, h] == l or abs(gl[s, h] - l) <= tl, (s, h)
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "bf16"), (64, "fp32"), (128, "fp32")])
+@pytest.mark.parametrize("G,seqs,T,lens,layout", [
+    (1, 1, 1, [1], "htd"), (1, 3, 17, [17], "thd"), (1, 16, 64, [64], "padded"),
+    (2, 9, 130, [130, 0], "htd"), (3, 17, 333, [200, 333, 1], "thd"), (1, 40, 1025, [1025], "htd"),
+    (2, 70, 257, [255, 256], "padded"), (1, 130, 500, [463], "thd")])
+def test_prefix_attention(D, dtype, G, seqs, T, lens, layout):
+    check_prefix(D, dtype, G, seqs, T, lens, layout, 3)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,seqs,T,lens,layout,heads", [
+    (2, 40, 333, [200, 333], "thd", 20), (1, 64, 1025, [1025], "padded", 10),
+    (1, 130, 500, [463], "thd", 10), (3, 70, 257, [255, 0, 256], "htd", 12),
+    (1, 17, 2049, [2049], "htd", 10)])
+def test_prefix_attention_of_large_batches(D, G, seqs, T, lens, layout, heads):
+    check_prefix(D, "bf16", G, seqs, T, lens, layout, heads)
 
 
 def test_prefix_length_out_of_range():
