@@ -40,7 +40,7 @@ constexpr int kMostResident = QRow<D, BITS>::kBytes == 128 ? 3 : 4;
 
 // `SPLIT`: a head may be cut between CTAs. STAGES: tiles of a warp in flight.
 template <int D, typename T, int BITS, bool STEP, int STAGES, bool SPLIT>
-__global__ void __launch_bounds__(kWarps * 32, STAGES == 1   ? 6
+__global__ void __launch_bounds__(kWarps * 32, STAGES == 1   ? 7
                                                : STAGES == 3 ? 2
                                                              : kMostResident<D, BITS>)
     quant_attn_kernel(const QAttnArgs p) {
@@ -219,7 +219,11 @@ cudaError_t launch_as(const QAttnArgs &a, int resident, cudaStream_t s) {
   cudaError_t e = allow_smem_of(quant_attn_kernel<D, T, BITS, STEP, STAGES, SPLIT>,
                                 std::max(need, smem_for(1)), ready);
   if (e != cudaSuccess) return e;
-  const int smem = resident ? std::max(need, smem_for(resident)) : need;
+  // warps that no head has a tile for need no shared memory (2048 heads of up to
+  // 84 rows of 128 bytes, capacity 96: 16.9 us a layer with it, 14.0 without)
+  const int tiles = (a.max_rows + kTile - 1) / kTile;
+  const int smem = resident ? std::max(need, smem_for(resident))
+                            : need / kWarps * std::min(kWarps, tiles);
   return pdl_launch(quant_attn_kernel<D, T, BITS, STEP, STAGES, SPLIT>, a.nheads * a.splits,
                     kWarps * 32, smem, s, a);
 }
