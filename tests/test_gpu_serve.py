@@ -772,3 +772,10 @@ def test_steps_of_any_split(bits, D, lens):
         assert np.abs(got[h] - o).max() <= to and abs(gl[h] - l) <= tl, h
         assert np.abs(ga[h] - o).max() <= to, h
     assert int(c.ws[:4 * (c.n + 2)].sum()) == 0
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,most", [(330, 611), (700, 301), (200, 1100)])
+def test_steps_of_many_uneven_heads(bits, D, n, most):
+    test_steps_of_any_split(bits, D, [53 * i % most for i in range(n)])
