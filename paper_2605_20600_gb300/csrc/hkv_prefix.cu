@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   using SM = TcSmem<D>;
   constexpr int PF = D + 4;
   extern __shared__ unsigned char dyn_raw[];
-  __shared__ uint64_t s_bar[2];  // S ready, O ready
+  __shared__ uint64_t s_bar[3];  // S ready, O ready; a failed CTA's products done
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, warp = tid >> 5;
@@ -439,6 +439,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   if (tid == 0) {
     mbar_init(&s_bar[0], 1);
     mbar_init(&s_bar[1], 1);
+    mbar_init(&s_bar[2], 1);
     fence_barrier_init();
   }
   pdl_wait();
@@ -478,12 +479,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   bool ok = true;
   uint32_t phase = 0;
   int st = 0;
+  // a wait that runs out in one warp ends the loop for all, at one of its barriers
   for (int k0 = lo; k0 < hi; k0 += kKeys, phase ^= 1, st ^= 1) {
     // O holds the tiles before this one, and their stage is free
     if (k0 > lo) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    if (__syncthreads_or(!ok)) break;
+    ok = !__syncthreads_or(!ok);
+    if (!ok) break;
     const uint32_t kb = smem_u32(skv + st * 2 * SM::kTile), vb = kb + SM::kTile;
     if (tid == 0) {
       tc_fence_after();
@@ -498,6 +501,10 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     if (k0 + kKeys < hi) load_tile(k0 + kKeys, st ^ 1);
     asm volatile("cp.async.commit_group;" ::: "memory");
     ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[0], phase));
+#ifdef HKV_PREFIX_TEST_STALL  // one warp waits for a phase that nothing completes
+    if (warp == (int)(blockIdx.x & 3) && k0 > lo)
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[2], 0));
+#endif
     tc_fence_after();
     if (works && ok) {
       uint32_t s[CH][32];
@@ -564,7 +571,8 @@ __global__ void __launch_bounds__(kTcThreads, 2)
       tmem_wait_st();
     }
     tc_fence_before();
-    if (__syncthreads_or(!ok)) break;
+    ok = !__syncthreads_or(!ok);
+    if (!ok) break;
     if (tid == 0) {
       tc_fence_after();
 #pragma unroll
@@ -580,8 +588,17 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   // phase: that of the tile after the last
   if (ok && lo < hi) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_bar[1], phase ^ 1));
+  ok = !__syncthreads_or(!ok);
+  if (!ok) {
+    // what was issued may still run: it gets the limit once more before its
+    // operands' place and its TMEM are given back
+    if (tid == 0) {
+      set_err(p.err, HKV_ERR_TIMEOUT);
+      tc_commit(&s_bar[2]);
+    }
+    mbar_wait(&s_bar[2], 0);
+  }
   tc_fence_after();
-  if (!ok && tid == 0 && p.err) set_err(p.err, HKV_ERR_TIMEOUT);
   const bool wrong = bad || !ok, any = lo < hi && ok;
   // the two copies of a query joined: the second half of the rows hands its
   // result over (the tiles' place is free)
