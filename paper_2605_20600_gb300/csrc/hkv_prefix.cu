@@ -435,15 +435,21 @@ __global__ void __launch_bounds__(kTcThreads, 2)
   const int h = b % p.heads;
   b /= p.heads;
   const int g = b % p.groups, sp = b / p.groups;
-  if (warp == 0) tmem_alloc(&s_tmem, kTcCols);
   if (tid == 0) {
     mbar_init(&s_bar[0], 1);
     mbar_init(&s_bar[1], 1);
     mbar_init(&s_bar[2], 1);
     fence_barrier_init();
   }
+  // TMEM only after the wait, and the next kernel's CTAs only after TMEM: an
+  // allocation waits for columns, so a CTA that held some while it waited for
+  // the kernel before, or let a CTA of the kernel after take them first, could
+  // wait for one that waits for it
   pdl_wait();
-  pdl_launch_dependents();
+  if (warp == 0) {
+    tmem_alloc(&s_tmem, kTcCols);
+    pdl_launch_dependents();
+  }
   int len = p.len[g];
   const bool bad = len < 0 || len > p.max_len;
   if (bad) {

@@ -779,3 +779,54 @@ def test_steps_of_any_split(bits, D, lens):
 @pytest.mark.parametrize("n,most", [(330, 611), (700, 301), (200, 1100)])
 def test_steps_of_many_uneven_heads(bits, D, n, most):
     test_steps_of_any_split(bits, D, [53 * i % most for i in range(n)])
+
+
+def test_prompts_between_products_of_a_library():
+    """Prompt attention on tcgen05 in a row with bf16 products that may hold
+    tensor memory of their own, eager and in a graph: nothing waits for
+    anything for good, and the results stay the same."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    D, Hh, seqs, T = 128, 12, 64, 700
+    rng = np.random.default_rng(3)
+    cfg = H.make_config(n_layers=1, n_seqs=seqs, n_heads=Hh, head_dim=D, dtype="bf16", n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k, v = prefix_rows(rng, 1, Hh, T, D, "bf16", "htd")
+    pre = H.make_prefix(k, v, torch.tensor([T], dtype=torch.int32, device="cuda"))
+    ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+    q = to_torch(rng.normal(size=(seqs, Hh, D)), "bf16")
+    a = to_torch(rng.normal(size=(2048, 2048)), "bf16")
+    outs = [torch.zeros(seqs, Hh, D, device="cuda") for _ in range(4)]
+    lse = torch.zeros(seqs, Hh, device="cuda")
+
+    def row(st):
+        prods = []
+        for o in outs:
+            prods.append(a @ a)
+            H.hkv_prefix_attention(cfg, pre, q, o, lse, ws, ws.numel(), st)
+        return prods
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(5):
+            prods = row(side.cuda_stream)
+        side.synchronize()
+        want, prod = outs[0].clone(), prods[0].clone()
+        for x in outs:
+            assert torch.equal(x, want)
+            x.zero_()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            prods = row(side.cuda_stream)
+        for _ in range(5):
+            g.replay()
+        side.synchronize()
+    for x, y in zip(outs, prods):
+        assert torch.equal(x, want) and torch.equal(y, prod)
+    o, _ = S.attention_lse(q[5, 3].float().cpu().numpy(), k[0, 3].float().cpu().numpy(),
+                           v[0, 3].float().cpu().numpy())
+    to, _ = tolerances(q[5, 3].float().cpu().numpy(), k[0, 3].float().cpu().numpy(),
+                       v[0, 3].float().cpu().numpy())
+    assert np.abs(want[5, 3].cpu().numpy() - o).max() <= to
