@@ -64,6 +64,7 @@ class hkv_qcache(Structure):
 
 
 class hkv_prefix(Structure):
+    dtype = None   # HKV_FP32 or HKV_BF16 where make_prefix knows it
     _fields_ = [
         ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
         ("group_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
@@ -305,17 +306,27 @@ def make_qcache(fmt, k, v, ks, vs, pos, off, cap, length, nbuf, ntok, label, qbu
     return c
 
 
+_PROMPT_DTYPES = {"torch.float32": HKV_FP32, "torch.bfloat16": HKV_BF16}
+
+
 def make_prefix(k, v, length, err=None) -> hkv_prefix:
-    """An hkv_prefix from tensors k and v of [groups][heads][tokens][head_dim]
-    (any strides whose last is 1, the same in both) and the prompts' lengths,
-    int32 on the device; keeps them alive."""
+    """An hkv_prefix from tensors k and v of [groups][heads][tokens][head_dim],
+    fp32 or bf16 (any strides whose last is 1, the same in both), and the
+    prompts' lengths, contiguous int32, all on one device; keeps them alive.
+    Calls with a config of another dtype refuse it."""
     if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
         raise HkvError("make_prefix", HKV_ERR_SHAPE)
     if length.numel() != k.shape[0]:
         raise HkvError("make_prefix", HKV_ERR_SHAPE)
+    dtype = _PROMPT_DTYPES.get(str(k.dtype))
+    if dtype is None or v.dtype != k.dtype or str(length.dtype) != "torch.int32":
+        raise HkvError("make_prefix", HKV_ERR_SHAPE)
+    if not length.is_contiguous() or not k.device == v.device == length.device:
+        raise HkvError("make_prefix", HKV_ERR_INVALID_ARG)
     p = hkv_prefix(k.data_ptr(), v.data_ptr(), length.data_ptr(), _p(err), k.stride(0),
                    k.stride(1), k.stride(2), k.shape[0], k.shape[2])
     p.arrays = (k, v, length, err)
+    p.dtype = dtype
     return p
 
 
@@ -359,9 +370,13 @@ def hkv_quant_check(cache, stream=0) -> None:
 
 
 def hkv_prefix_workspace_size(cfg, prefix) -> int:
+    if prefix.dtype not in (None, cfg.dtype):
+        return 0
     return int(lib().hkv_prefix_workspace_size(ctypes.byref(cfg), ctypes.byref(prefix)))
 
 
 def hkv_prefix_attention(cfg, prefix, q, out, lse, workspace, ws_bytes, stream=0) -> None:
+    if prefix.dtype not in (None, cfg.dtype):
+        raise HkvError("prefix_attention", HKV_ERR_SHAPE)
     _call("prefix_attention", ctypes.byref(cfg), ctypes.byref(prefix), _p(q), _p(out), _p(lse),
           _p(workspace), ws_bytes, stream)

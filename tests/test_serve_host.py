@@ -196,3 +196,33 @@ def test_oracle_row_format(bits):
     bad[0, 1], bad[1, 2] = np.inf, np.nan
     c, s = S.quantise(bad, bits)
     assert np.isnan(s).all() and (c == 0).all()
+
+
+def test_make_prefix_refuses_types_the_kernel_would_misread(H):
+    import torch
+    bf, n = torch.bfloat16, torch.zeros(2, dtype=torch.int32)
+    k = torch.zeros(2, 3, 10, 64, dtype=bf)
+    H.make_prefix(k, k, n)
+    for bad in (lambda: H.make_prefix(k, k, n.long()), lambda: H.make_prefix(k, k, n.float()),
+                lambda: H.make_prefix(k, k, torch.zeros(4, dtype=torch.int32)[::2]),
+                lambda: H.make_prefix(k, k.float(), n), lambda: H.make_prefix(k.half(), k.half(), n),
+                lambda: H.make_prefix(k, k.to("meta"), n), lambda: H.make_prefix(k, k, n.to("meta"))):
+        with pytest.raises(H.HkvError):
+            bad()
+
+
+def test_a_prompt_of_another_type_than_the_config_is_refused(H):
+    """bf16 rows read as fp32 would be read past their end."""
+    import torch
+    buf, a, _, _, _ = caches(H)
+    n = torch.zeros(2, dtype=torch.int32)
+    for dtype, other in (("fp32", torch.bfloat16), ("bf16", torch.float32)):
+        cfg = cfg_of(H, dtype=dtype)
+        k = torch.zeros(2, 4, 10, 64, dtype=other)
+        pre = H.make_prefix(k, k, n)
+        assert H.hkv_prefix_workspace_size(cfg, pre) == 0
+        with pytest.raises(H.HkvError) as e:
+            H.hkv_prefix_attention(cfg, pre, a, a, a, a, 1 << 30)
+        assert e.value.status == 2
+        k = k.to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+        assert H.hkv_prefix_workspace_size(cfg, H.make_prefix(k, k, n)) > 0
