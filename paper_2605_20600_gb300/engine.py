@@ -180,45 +180,52 @@ class Engine:
         """Puts the compressed cache into 8 or 4 bits (HKV_Q8 or HKV_Q4) and
         frees its plain rows; decode steps and updates run on the codes from
         here on. prompt: None, or (k, v), [L][groups][H][C][head_dim] tensors
-        of the conditioning tokens that each of `groups` equal runs of
-        sequences shares; they then stay plain and are kept once instead of
-        in every sequence's segments."""
+        in the config dtype of the conditioning tokens that each of `groups`
+        equal runs of sequences shares; they then stay plain and are kept once
+        instead of in every sequence's segments. Synchronises the stream: an
+        error leaves the engine as it was, on its plain rows."""
         if self.ragged is None or self.quant is not None:
             raise H.HkvError("quantise", H.HKV_ERR_STATE)
         cfg, dev = self.cfg, self.device
         off, cap, total = self.off, self.cap, self.total_tokens
         flags = 0
-        self.quant_cfg = copy.copy(cfg)
+        quant_cfg = copy.copy(cfg)
         if prompt is not None:
             k, v = prompt
-            if k.shape[0] != cfg.n_layers or k.shape[2:] != (cfg.n_heads, cfg.n_cond, cfg.head_dim) \
-                    or k.shape != v.shape or cfg.n_cond < 1:
+            shape = (cfg.n_layers, k.shape[1] if k.dim() == 5 else 0, cfg.n_heads, cfg.n_cond,
+                     cfg.head_dim)
+            if k.shape != shape or v.shape != shape or cfg.n_cond < 1 or shape[1] < 1 \
+                    or cfg.n_seqs % shape[1] != 0 or not k.dtype == v.dtype == torch_dtype(cfg):
                 raise H.HkvError("quantise", H.HKV_ERR_SHAPE)
-            self.quant_cfg.n_cond = 0
+            if not k.device == v.device == self.labels.device:
+                raise H.HkvError("quantise", H.HKV_ERR_INVALID_ARG)
+            quant_cfg.n_cond = 0
             off, cap = torch.empty_like(off), torch.empty_like(cap)
-            total = H.hkv_allocate_budgets(self.quant_cfg, self.labels, torch.empty_like(self.budget),
+            total = H.hkv_allocate_budgets(quant_cfg, self.labels, torch.empty_like(self.budget),
                                            cap, off, self.stream())
             flags = H.HKV_PACK_SKIP_COND
         quant = QuantCacheBuffers(cfg, fmt, total, dev, qbuf=self.ragged.qbuf, label=self.labels,
                                   off=off, cap=cap)
-        H.hkv_quant_pack(cfg, self.ragged.c, quant.c, H.HKV_ALL_LAYERS, flags, self.stream())
+        ws_bytes = H.hkv_quant_workspace_size(quant_cfg)
+        ws = torch.zeros(ws_bytes, dtype=torch.uint8, device=dev)
         if prompt is not None:
-            groups = k.shape[1]
-            self.prompt_len = torch.full((groups,), cfg.n_cond, dtype=torch.int32, device=dev)
-            self.prompt_rows = (k, v)
-            self.prompt = [H.make_prefix(k[layer], v[layer], self.prompt_len, quant.err)
-                           for layer in range(cfg.n_layers)]
-            self.prompt_ws_bytes = H.hkv_prefix_workspace_size(cfg, self.prompt[0])
-            self.prompt_ws = torch.zeros(self.prompt_ws_bytes, dtype=torch.uint8, device=dev)
-            shape = (cfg.n_seqs, cfg.n_heads)
-            self.prior = (torch.empty(*shape, cfg.head_dim, dtype=torch.float32, device=dev),
-                          torch.empty(*shape, dtype=torch.float32, device=dev))
-        self.quant_ws_bytes = H.hkv_quant_workspace_size(self.quant_cfg)
-        self.quant_ws = torch.zeros(self.quant_ws_bytes, dtype=torch.uint8, device=dev)
+            prompt_len = torch.full((shape[1],), cfg.n_cond, dtype=torch.int32, device=dev)
+            prefixes = [H.make_prefix(k[layer], v[layer], prompt_len, quant.err)
+                        for layer in range(cfg.n_layers)]
+            prompt_ws_bytes = min(H.hkv_prefix_workspace_size(cfg, p) for p in prefixes)
+            if prompt_ws_bytes == 0:       # strides or alignment the attention does not take
+                raise H.HkvError("quantise", H.HKV_ERR_SHAPE)
+            prompt_ws = torch.zeros(prompt_ws_bytes, dtype=torch.uint8, device=dev)
+            prior = (torch.empty(cfg.n_seqs, cfg.n_heads, cfg.head_dim, dtype=torch.float32, device=dev),
+                     torch.empty(cfg.n_seqs, cfg.n_heads, dtype=torch.float32, device=dev))
+        H.hkv_quant_pack(cfg, self.ragged.c, quant.c, H.HKV_ALL_LAYERS, flags, self.stream())
+        H.hkv_quant_check(quant.c, self.stream())     # every head is in, or nothing changes
+        if prompt is not None:
+            self.prompt, self.prompt_ws_bytes, self.prompt_ws = prefixes, prompt_ws_bytes, prompt_ws
+            self.prior = prior
+        self.quant_cfg, self.quant_ws_bytes, self.quant_ws = quant_cfg, ws_bytes, ws
         self.off, self.cap, self.total_tokens = off, cap, total
         self.cache = self.quant = quant
-        for x in (self.ragged.k, self.ragged.v, self.ragged.pos):
-            x.record_stream(torch.cuda.current_stream())   # the pack may still have to read it
         self.ragged.k = self.ragged.v = self.ragged.pos = None
 
     def _quant_step(self, layer: int, q, k, v, out, flags: int) -> None:

@@ -830,3 +830,41 @@ def test_prompts_between_products_of_a_library():
     to, _ = tolerances(q[5, 3].float().cpu().numpy(), k[0, 3].float().cpu().numpy(),
                        v[0, 3].float().cpu().numpy())
     assert np.abs(want[5, 3].cpu().numpy() - o).max() <= to
+
+
+@pytest.mark.parametrize("what", ["head", "strides"])
+def test_a_refused_quantisation_leaves_the_plain_cache(what):
+    """A head that the pack refuses, or a prompt whose rows the attention does
+    not take: the engine keeps its plain rows and goes on with them, and can
+    be quantised when the cause is gone."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import Engine
+    from paper_2605_20600_gb300.runner import generate
+    from synth.gpu import DeviceSynth
+    w = configs.TINY
+    engines = []
+    for refused in (False, True):
+        eng = Engine(cfg_of(H, w), "cuda")
+        generate(eng, DeviceSynth(w, "cuda"), last_step=w.group_at - 1)
+        if refused:
+            old, prompt = eng.ragged.len.clone(), None
+            if what == "head":
+                eng.ragged.len[3] = -1
+            else:
+                x = torch.zeros(1, 1, w.n_heads, w.n_cond, w.head_dim + 1, device="cuda")
+                prompt = (x[..., :-1], x[..., :-1])
+            with pytest.raises(H.HkvError):
+                eng.quantise(8, prompt)
+            eng.ragged.len.copy_(old)
+            assert eng.quant is None and eng.prompt is None and eng.cache is eng.ragged
+            assert eng.off is eng.ragged.off and eng.ragged.k is not None
+        generate(eng, DeviceSynth(w, "cuda"), first_step=w.group_at, last_step=w.group_at + 20)
+        eng.quantise(8)
+        outs = []
+        generate(eng, DeviceSynth(w, "cuda"), first_step=w.group_at + 21, last_step=w.group_at + 40,
+                 on_step=lambda t, out: outs.append(out.clone()))
+        eng.check()
+        engines.append((outs, eng.quant.len.clone(), eng.quant.k.clone()))
+    a, b = engines
+    assert all(torch.equal(x, y) for x, y in zip(a[0], b[0])) and torch.equal(a[1], b[1])

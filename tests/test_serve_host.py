@@ -226,3 +226,27 @@ def test_a_prompt_of_another_type_than_the_config_is_refused(H):
         assert e.value.status == 2
         k = k.to(torch.float32 if dtype == "fp32" else torch.bfloat16)
         assert H.hkv_prefix_workspace_size(cfg, H.make_prefix(k, k, n)) > 0
+
+
+def test_engine_refuses_a_prompt_before_it_changes_anything(H):
+    import torch
+    from paper_2605_20600_gb300.engine import Engine
+    cfg = cfg_of(H)                                       # 2 layers, 4 sequences, 4 heads, C = 8
+    good = torch.zeros(2, 2, 4, 8, 64, dtype=torch.bfloat16)
+    wide = torch.zeros(2, 2, 4, 8, 65, dtype=torch.bfloat16)[..., :64]
+    for k, v in ((good[:, :1].expand(2, 3, 4, 8, 64), None),      # 3 groups of 4 sequences
+                 (good[:, :0], None), (good[:1], None), (good[:, 0], None), (good[:, :, :, :7], None),
+                 (good.float(), None), (good, good.float()), (good.half(), None), (good, good[:, :1]),
+                 (good.to("meta"), None)):
+        eng = Engine.__new__(Engine)
+        eng.cfg, eng.device, eng.quant, eng.prompt = cfg, torch.device("cpu"), None, None
+        eng.ragged, eng.labels = object(), torch.zeros(32, dtype=torch.uint8)
+        eng.off, eng.cap, eng.total_tokens = object(), object(), 5
+        before = dict(vars(eng))
+        with pytest.raises(H.HkvError) as e:
+            eng.quantise(8, (k, k if v is None else v))
+        assert e.value.status in (H.HKV_ERR_SHAPE, H.HKV_ERR_INVALID_ARG)
+        assert vars(eng) == before
+    # what the strides would make the attention refuse is known to the workspace query
+    pre = H.make_prefix(wide[0], wide[0], torch.zeros(2, dtype=torch.int32))
+    assert H.hkv_prefix_workspace_size(cfg, pre) == 0
