@@ -16,7 +16,7 @@ from .engine import Engine, torch_dtype
 def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=None,
              before_compress=None, fused: bool = True, first_step: int = 0,
              identify: str | None = None, cache_format: int | None = None,
-             shared_prompt: bool = False) -> None:
+             shared_prompt: int = False) -> None:
     """Runs image tokens first_step..last_step (default N-1) for every layer.
 
     fused: hkv_evict_all (every layer in one launch) when the update is due,
@@ -33,13 +33,18 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
     the distances are the raster ones.
     cache_format: None keeps the compressed cache in the config dtype;
     HKV_Q8 or HKV_Q4 quantises it after compression (fused path only).
-    shared_prompt: with a cache_format, the conditioning tokens, which must
-    then be the same for every sequence, are kept once for all of them.
+    shared_prompt: with a cache_format, the number of prompts (True: one) of
+    which each belongs to an equal run of sequences, whose conditioning tokens
+    are then kept once for the run. Tokens that differ within a run raise
+    ValueError: with guidance, the conditional and the unconditional sequences
+    are two runs.
     """
     if cache_format is not None and not fused:
         raise ValueError("a quantised cache needs the fused path")
     if shared_prompt and (cache_format is None or first_step > 0 or engine.cfg.n_cond < 1):
         raise ValueError("a shared prompt needs a cache_format, conditioning tokens and a whole run")
+    if shared_prompt and (shared_prompt < 0 or engine.cfg.n_seqs % shared_prompt != 0):
+        raise ValueError(f"{engine.cfg.n_seqs} sequences are not {shared_prompt} equal runs")
     if identify is None:   # the fused count is the raster one
         identify = "fused" if fused and engine.cfg.distance_mode == 0 else "separate"
     if identify not in ("fused", "separate", "multi") or (identify == "fused" and not fused):
@@ -56,13 +61,19 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
         vc = torch.empty_like(kc)
         for layer in range(L):
             provider.cond(kc, vc, layer, st)
-            engine.prefill(layer, kc, vc)
             if shared_prompt:
+                G = int(shared_prompt)
                 if layer == 0:
-                    prompt = (torch.empty(L, 1, H, C, D, dtype=dt, device=dev),
-                              torch.empty(L, 1, H, C, D, dtype=dt, device=dev))
-                prompt[0][layer, 0].copy_(kc[0])
-                prompt[1][layer, 0].copy_(vc[0])
+                    prompt = (torch.empty(L, G, H, C, D, dtype=dt, device=dev),
+                              torch.empty(L, G, H, C, D, dtype=dt, device=dev))
+                for x, rows in zip((kc, vc), prompt):
+                    runs = x.view(G, S // G, H, C, D)
+                    bits = runs.view(torch.int16 if dt == torch.bfloat16 else torch.int32)
+                    if not torch.equal(bits, bits[:, :1].expand_as(bits)):
+                        raise ValueError(f"the conditioning tokens of layer {layer} differ between "
+                                         f"sequences that share a prompt ({G} of {S} sequences)")
+                    rows[layer].copy_(runs[:, 0])
+            engine.prefill(layer, kc, vc)
     q = torch.empty(L, S, H, D, dtype=dt, device=dev)
     k, v = torch.empty_like(q), torch.empty_like(q)
     out = torch.empty(L, S, H, D, dtype=torch.float32, device=dev)

@@ -868,3 +868,40 @@ def test_a_refused_quantisation_leaves_the_plain_cache(what):
         engines.append((outs, eng.quant.len.clone(), eng.quant.k.clone()))
     a, b = engines
     assert all(torch.equal(x, y) for x, y in zip(a[0], b[0])) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("bits", FMT)
+def test_generation_of_a_guided_batch(bits):
+    """Two prompts, two sequences each: conditional and unconditional."""
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import Engine
+    from paper_2605_20600_gb300.runner import generate
+    from synth.gpu import DeviceSynth
+
+    class Guided(DeviceSynth):
+        def cond(self, kc, vc, layer, stream=0):
+            super().cond(kc, vc, layer, stream)
+            for x in (kc, vc):
+                x[1], x[3] = x[0].clone(), x[2].clone()
+
+    w = configs.TINY.with_(n_seqs=4)
+    E, N, C = w.group_at, w.n_image, w.n_cond
+    steps = sorted({E, E + w.period, N - 1})
+    with pytest.raises(ValueError):       # the two prompts differ
+        generate(Engine(cfg_of(H, w), "cuda"), Guided(w), cache_format=bits, shared_prompt=True)
+    eng = Engine(cfg_of(H, w), "cuda")
+    got = {}
+    generate(eng, Guided(w), cache_format=bits, shared_prompt=2,
+             on_step=lambda t, out: got.__setitem__(t, out.cpu().numpy()) if t in steps else None)
+    eng.check()
+    labels, hp = eng.labels.cpu().numpy(), O.HeadParams.of(w)
+    for s in range(4):
+        for h in (1, 6):
+            hi, first = gen.HeadInputs(w, s, 0, h), gen.HeadInputs(w, s // 2 * 2, 0, h)
+            k, v = hi.k.copy(), hi.v.copy()
+            k[:C], v[:C] = first.k[:C], first.v[:C]
+            outs, _ = S.run_head_stored(hp, hi.q, k, v, bits, int(labels[flat(w, s, 0, h)]), steps,
+                                        plain_cond=True)
+            for t in steps:
+                to = tolerances(hi.q[t], k[:C + t + 1], v[:C + t + 1])[0]
+                assert np.abs(got[t][0, s, h] - outs[t]).max() <= 2 * to, (s, h, t)

@@ -250,3 +250,53 @@ def test_engine_refuses_a_prompt_before_it_changes_anything(H):
     # what the strides would make the attention refuse is known to the workspace query
     pre = H.make_prefix(wide[0], wide[0], torch.zeros(2, dtype=torch.int32))
     assert H.hkv_prefix_workspace_size(cfg, pre) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_runner_takes_only_prompts_that_are_shared(H, dtype):
+    """The conditioning tokens of every run of sequences are looked at before
+    they are prefilled; without image tokens nothing else runs."""
+    import torch
+    from paper_2605_20600_gb300.runner import generate
+
+    class Fake:
+        cfg = cfg_of(H, dtype=dtype)      # 4 sequences
+        device, quant = torch.device("cpu"), None
+
+        def __init__(self):
+            self.filled = []
+
+        def stream(self):
+            return 0
+
+        def prefill(self, layer, kc, vc):
+            self.filled.append(layer)
+
+    class Provider:
+        def __init__(self, runs, odd=None):
+            self.runs, self.odd = runs, odd
+
+        def cond(self, kc, vc, layer, st):
+            for x, sign in ((kc, 1.0), (vc, -1.0)):
+                for s in range(4):
+                    x[s] = sign * (1 + layer + s * self.runs // 4)
+            if self.odd == "v" and layer == 1:
+                vc[3, 2, 5, 7] += 1.0
+            elif self.odd == "zero":       # other bits, equal as numbers
+                kc[:] = 0.0
+                kc[2] = -0.0
+            elif self.odd == "nan":        # the same bits
+                kc[:] = float("nan")
+
+    def run(prompts, provider):
+        f = Fake()
+        generate(f, provider, last_step=-1, cache_format=8, shared_prompt=prompts)
+        return f.filled
+
+    assert run(True, Provider(1)) == [0, 1] and run(2, Provider(2)) == [0, 1] and run(4, Provider(4)) == [0, 1]
+    assert run(1, Provider(1, "nan")) == [0, 1]
+    for prompts, provider in ((True, Provider(2)), (True, Provider(4)), (2, Provider(4)),
+                              (1, Provider(1, "v")), (1, Provider(1, "zero")), (3, Provider(1)),
+                              (8, Provider(1)), (-1, Provider(1))):
+        with pytest.raises(ValueError):
+            run(prompts, provider)
