@@ -105,11 +105,17 @@ class Engine:
     def prefill(self, layer: int, kc, vc) -> None:
         H.hkv_prefill(self.cfg, self.dense.c, layer, kc, vc, self.stream())
 
+    def _plain(self, name: str) -> None:
+        if self.quant is not None:     # calls that have no form for codes
+            raise H.HkvError(name, H.HKV_ERR_STATE)
+
     # per decode step and layer
     def append(self, layer: int, q, k, v) -> None:
+        self._plain("append_evict")
         H.hkv_append_evict(self.cfg, self.cache.c, layer, q, k, v, self.stream())
 
     def attend(self, layer: int, q, out) -> None:
+        self._plain("decode_attention")
         H.hkv_decode_attention(self.cfg, self.cache.c, layer, q, out, self.ws, self.ws_bytes,
                                self.stream())
 
@@ -147,6 +153,7 @@ class Engine:
     def step_identify(self, layer: int, q, k, v, out) -> None:
         """The decode step of the grouping token with the head types (Sec. 4,
         Step 2) decided in the same pass, into self.labels (no n_h)."""
+        self._plain("decode_step_identify")
         flags = H.HKV_STEP_PREFETCH if self.cfg.n_layers >= 2 else 0
         H.hkv_decode_step_identify(self.cfg, self.cache.c, layer, q, k, v, out, self.labels, self.ws,
                                    self.ws_bytes, flags, self.stream())

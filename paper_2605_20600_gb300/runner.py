@@ -32,7 +32,9 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
     attention; labels and n_h). Default: fused when the path is fused and
     the distances are the raster ones.
     cache_format: None keeps the compressed cache in the config dtype;
-    HKV_Q8 or HKV_Q4 quantises it after compression (fused path only).
+    HKV_Q8 or HKV_Q4 quantises it after compression, at the start where the
+    engine continues with a compressed cache (fused path only). An engine that
+    is quantised already goes on with its format.
     shared_prompt: with a cache_format, the number of prompts (True: one) of
     which each belongs to an equal run of sequences, whose conditioning tokens
     are then kept once for the run. Tokens that differ within a run raise
@@ -56,6 +58,12 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
     E = cfg.group_at
     dev, dt = engine.device, torch_dtype(cfg)
     st = engine.stream()
+    quant = engine.quant
+    if quant is not None and (not fused or cache_format not in (None, quant.c.format)):
+        raise ValueError(f"the engine's cache is quantised (format {quant.c.format}): "
+                         f"fused={fused}, cache_format={cache_format}")
+    if cache_format is not None and quant is None and first_step >= E:
+        engine.quantise(cache_format)
     if C > 0 and first_step == 0:
         kc = torch.empty(S, H, C, D, dtype=dt, device=dev)
         vc = torch.empty_like(kc)

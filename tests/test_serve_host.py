@@ -300,3 +300,45 @@ def test_runner_takes_only_prompts_that_are_shared(H, dtype):
                               (8, Provider(1)), (-1, Provider(1))):
         with pytest.raises(ValueError):
             run(prompts, provider)
+
+
+def test_runner_quantises_a_cache_it_continues_with(H):
+    import torch
+    from paper_2605_20600_gb300.engine import Engine
+    from paper_2605_20600_gb300.runner import generate
+
+    class Fake:
+        cfg = cfg_of(H)                    # E = 16, N = 64
+        device = torch.device("cpu")
+
+        def __init__(self, fmt=None):
+            self.calls, self.quant = [], None
+            if fmt is not None:
+                self.quantise(fmt)
+                self.calls.clear()
+
+        def stream(self):
+            return 0
+
+        def quantise(self, fmt, prompt=None):
+            self.calls.append((fmt, prompt))
+            self.quant = type("Q", (), {"c": H.hkv_qcache(format=fmt)})
+
+    def run(f, first, **kw):               # no token left: only what comes before the first
+        generate(f, None, first_step=first, last_step=first - 1, **kw)
+        return f.calls
+
+    for first in (16, 17, 40):
+        assert run(Fake(), first, cache_format=4) == [(4, None)]
+    assert run(Fake(), 15, cache_format=4) == [] and run(Fake(), 40) == []
+    assert run(Fake(8), 40) == [] and run(Fake(8), 40, cache_format=8) == []
+    for kw in (dict(cache_format=4), dict(fused=False)):
+        with pytest.raises(ValueError):
+            run(Fake(8), 40, **kw)
+    eng = Engine.__new__(Engine)           # calls that the codes have no form of
+    eng.quant = object()
+    for call in (lambda: eng.append(0, 1, 1, 1), lambda: eng.attend(0, 1, 1),
+                 lambda: eng.step_identify(0, 1, 1, 1, 1)):
+        with pytest.raises(H.HkvError) as e:
+            call()
+        assert e.value.status == H.HKV_ERR_STATE
