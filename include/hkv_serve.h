@@ -119,8 +119,10 @@ size_t hkv_quant_workspace_size(const hkv_config *cfg);
  * prior_out, prior_lse: NULL, or the out and lse of the same queries over
  * other keys (hkv_prefix_attention); out and lse are then those over both
  * sets of keys. A head without keys yields zeros and -inf.
- * Nothing is rounded below fp32 but the products' operands: q and the weights
- * are each cut into two fp16 parts, 22 bits together. */
+ * Nothing is rounded below fp32 but the products' operands. q is cut into two
+ * fp16 parts over a power of two of each group of 32 channels: off by at most
+ * 2^-22 of an element or 2^-36 of the group's largest, whichever is more. The
+ * weights are cut the same way. */
 hkv_status hkv_quant_attention(const hkv_config *cfg, const hkv_qcache *cache, int layer,
                                const void *q, const float *prior_out, const float *prior_lse,
                                float *out, float *lse, void *workspace, size_t ws_bytes,

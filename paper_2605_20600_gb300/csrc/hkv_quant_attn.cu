@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kWarps * 32, STAGES == 1   ? 7
   if (t0 + warp < t1 && hd.n > 0) {
     float acc[D / 16][2] = {};
     __half *operand = reinterpret_cast<__half *>(ws + STAGES * TL::kBytes);
-    const Query<D, BITS> qr = make_query<D, BITS>(qv, p.qscale, operand);
+    const Query<D, BITS> qr = make_query<D, BITS>(qv, operand);
     int st = 0;
     for (int tile = t0 + warp; tile < t1; tile += kWarps) {
       cp_async_wait<STAGES - 1>();
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kWarps * 32, STAGES == 1   ? 7
       const int r0 = tile * kTile, rows = min(kTile, hd.n - r0);
       if (STEP && tile == new_tile)
         append_row<D, T, BITS>(p, hl, hd, stage, hd.len - r0, nr, qv);
-      attend_tile<D, BITS>(stage, rows, qr, m, l, acc);
+      attend_tile<D, BITS>(stage, rows, qr, p.qscale, m, l, acc);
       if (STAGES == 1) break;  // no warp has a second tile
       __syncwarp();            // the stage is rewritten from here on
       if (tile + STAGES * kWarps < t1) load(tile + STAGES * kWarps, st);

@@ -5,10 +5,11 @@
 // because codes then need no conversion to fp32: a code is an exact fp16
 // number two of which a bit operation and one packed subtraction make, and the
 // eight columns carry what one query leaves empty:
-//  * scores, 16 rows of K (M) x 16 channels (K): the columns hold the query cut
-//    into two fp16 parts (hi, and the rest times 2^11: 22 bits), once per group
-//    of 32 channels, zero outside the group. The sums of a row come out per
-//    group, ready for the group's scale in fp32;
+//  * scores, 16 rows of K (M) x 16 channels (K): the columns hold the query's
+//    channels of each group of 32, over a power of two near the group's largest,
+//    cut into two fp16 parts (hi, and the rest times 2^11: 22 bits, down to 2^-36
+//    of the largest), zero outside the group. The sums of a row come out per
+//    group, ready for the group's scale and power of two in fp32;
 //  * output, 16 channels of V^T (M) x 16 rows (K): the columns hold the rows'
 //    weights times the row's scale of each group, cut in two the same way,
 //    after division by a power of two near the tile's largest scale of the
@@ -196,24 +197,26 @@ __device__ __forceinline__ void load_tile(unsigned char *stage, const QCacheArgs
 template <int D, int BITS>
 struct Query {
   uint32_t f[D / 16][2];
-  float scale;             // of the sums, to logits in powers of two
+  float unit;              // power of two of group `quad`
 };
 
 // From the lane's channels lane * E ..; sq: the warp's operand area, free again
 // on return. The whole warp calls.
 template <int D, int BITS>
-__device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32], float qscale,
+__device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32],
                                                      __half *sq) {
-  // the query over a power of two, in two fp16 parts, in the order in which
-  // the codes of a word come out in pairs
-  constexpr int E = D / 32, KM = D / 16;
+  // the query, each group over its power of two, in two fp16 parts, in the order
+  // in which the codes of a word come out in pairs
+  constexpr int E = D / 32, KM = D / 16, LPG = 32 / E;  // lanes of a group
   const int lane = threadIdx.x & 31, row8 = lane >> 2, quad = lane & 3;
   Query<D, BITS> r;
   uint32_t qm = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
-  const float q2 = pow2_of(__reduce_max_sync(0xFFFFFFFFu, qm)), qi = inv_pow2(q2);
-  r.scale = q2 * qscale;
+#pragma unroll
+  for (int o = LPG / 2; o >= 1; o >>= 1) qm = max(qm, __shfl_xor_sync(0xFFFFFFFFu, qm, o));
+  const float q2 = pow2_of(qm), qi = inv_pow2(q2);
+  r.unit = __shfl_sync(0xFFFFFFFFu, q2, quad * LPG & 31);  // (no group: any)
   __syncwarp();
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -310,7 +313,7 @@ __device__ __forceinline__ void load_query(const QAttnArgs &p, int hl, float (&q
 // `quad` is those channels' group.
 template <int D, int BITS>
 __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows,
-                                            const Query<D, BITS> &q, float &m,
+                                            const Query<D, BITS> &q, float qscale, float &m,
                                             float &l, float (&acc)[D / 16][2]) {
   using R = QRow<D, BITS>;
   using TL = TileOf<D, BITS>;
@@ -367,8 +370,8 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
     }
     const uint16_t *sc = reinterpret_cast<const uint16_t *>(ss);
     const bool grp = quad < G;  // the columns beyond the groups are empty
-    const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) : 0.f;
-    const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) : 0.f;
+    const float fa = grp ? bf16_bits_to_float(sc[ra * G + (grp ? quad : 0)]) * q.unit : 0.f;
+    const float fb = grp ? bf16_bits_to_float(sc[rb * G + (grp ? quad : 0)]) * q.unit : 0.f;
     xs[2 * b] = fa * fmaf(s[1], kLoUnscale, s[0]);
     xs[2 * b + 1] = fb * fmaf(s[3], kLoUnscale, s[2]);
   }
@@ -378,7 +381,7 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
   float k1 = (b0 ? xs[3] : xs[2]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? xs[2] : xs[3], 1);
   float x = (b1 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? k0 : k1, 2);
   const bool on = own < rows;
-  x = on ? x * q.scale : -INFINITY;
+  x = on ? x * qscale : -INFINITY;  // logits in powers of two
 
   const float mt = warp_max(x);
   if (mt > m) {  // the same for the whole warp

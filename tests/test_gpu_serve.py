@@ -905,3 +905,32 @@ def test_generation_of_a_guided_batch(bits):
             for t in steps:
                 to = tolerances(hi.q[t], k[:C + t + 1], v[:C + t + 1])[0]
                 assert np.abs(got[t][0, s, h] - outs[t]).max() <= 2 * to, (s, h, t)
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("spread", [20, 30, 60])
+def test_queries_whose_groups_differ_in_size(bits, D, spread):
+    """Queries small by 2^-spread in one group, whose keys are as much larger:
+    the group counts as much as the others, and the scores keep the accuracy
+    of any other query. Within a group the elements are of one size, so that
+    two parts hold 22 bits of them (elements far below their group's largest
+    keep fewer, down to 2^-36 of that)."""
+    import torch
+    c = QCache([1, 70, 300, 4000], D, bits, "fp32", seed=bits + D + spread)
+    for h, g in ((1, 0), (2, 1), (3, D // 32 - 1)):
+        a = slice(c.off[h], c.off[h] + c.lens[h])
+        c.q[h, g * 32:g * 32 + 32] *= np.float32(2.0 ** -spread)
+        c.k_scales[a, g] *= np.float32(2.0 ** spread)
+        c.sk[a] = to_torch(c.k_scales[a], "bf16")
+    out = torch.empty(c.n, D, device="cuda")
+    lse = torch.empty(c.n, device="cuda")
+    c.H.hkv_quant_attention(c.cfg, c.c, 0, to_torch(c.q, "fp32"), out, c.ws, c.ws_bytes, lse=lse)
+    c.H.hkv_quant_check(c.c)
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    for h in range(c.n):
+        K, V = c.rows(h)
+        o, l = S.attention_lse(c.q[h], K, V)
+        to, tl = tolerances(c.q[h], K, V)
+        assert np.abs(got[h] - o).max() <= to, (h, np.abs(got[h] - o).max(), to)
+        assert abs(gl[h] - l) <= tl, (h, gl[h], l, tl)
