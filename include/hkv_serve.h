@@ -119,10 +119,12 @@ size_t hkv_quant_workspace_size(const hkv_config *cfg);
  * prior_out, prior_lse: NULL, or the out and lse of the same queries over
  * other keys (hkv_prefix_attention); out and lse are then those over both
  * sets of keys. A head without keys yields zeros and -inf.
- * Nothing is rounded below fp32 but the products' operands. q is cut into two
- * fp16 parts over a power of two of each group of 32 channels: off by at most
- * 2^-22 of an element or 2^-36 of the group's largest, whichever is more. The
- * weights are cut the same way. */
+ * Nothing is rounded below fp32 but the products' operands, which are cut into
+ * two fp16 parts over a power of two: q by groups of 32 channels, off by at
+ * most 2^-22 of an element or 2^-50 of the group's largest, whichever is more;
+ * the weights exp(x - the largest so far) times the rows' V scales by groups
+ * and 32 rows, off by at most 2^-22 of a product or 2^-50 of the largest of
+ * these scales. */
 hkv_status hkv_quant_attention(const hkv_config *cfg, const hkv_qcache *cache, int layer,
                                const void *q, const float *prior_out, const float *prior_lse,
                                float *out, float *lse, void *workspace, size_t ws_bytes,

@@ -6,14 +6,15 @@
 // number two of which a bit operation and one packed subtraction make, and the
 // eight columns carry what one query leaves empty:
 //  * scores, 16 rows of K (M) x 16 channels (K): the columns hold the query's
-//    channels of each group of 32, over a power of two near the group's largest,
-//    cut into two fp16 parts (hi, and the rest times 2^11: 22 bits, down to 2^-36
+//    channels of each group of 32, over a power of two by the group's largest,
+//    cut into two fp16 parts (hi, and the rest times 2^11: 22 bits, down to 2^-50
 //    of the largest), zero outside the group. The sums of a row come out per
 //    group, ready for the group's scale and power of two in fp32;
 //  * output, 16 channels of V^T (M) x 16 rows (K): the columns hold the rows'
-//    weights times the row's scale of each group, cut in two the same way,
-//    after division by a power of two near the tile's largest scale of the
-//    group; a channel uses its own group's two columns.
+//    weights times the row's scale of each group, cut in two the same way over
+//    a power of two by the tile's largest scale of the group (the largest
+//    product would be known only after the scores: 115 us instead of 112 for
+//    eight layers of 256 heads); a channel uses its own group's two columns.
 // Sums chain over at most 8 (scores) or 2 (output) products in the tensor core
 // and are added in fp32 registers beyond that. A tile is 580 (4 bits) to 670
 // instructions of a warp at D = 128; converting each code to fp32 for plain
@@ -106,10 +107,11 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// 2^e and 2^-e for the exponent e of a non-negative fp32 (its bits), e kept in
-// [-126, 126]
-__device__ __forceinline__ float pow2_of(uint32_t bits) {
-  return __uint_as_float(min(max(bits & 0x7F800000u, 0x00800000u), 0x7E800000u));
+// The power of two over which numbers up to `bits` (a non-negative fp32's) are cut
+// into two fp16 parts: they come out below 2^15, half of fp16's largest, so that
+// parts are normal numbers down to 2^-28 of the largest. Kept in [2^-126, 2^113].
+__device__ __forceinline__ float part_unit(uint32_t bits) {
+  return __uint_as_float(min(max(bits & 0x7F800000u, 0x07800000u), 0x7F000000u) - 0x07000000u);
 }
 __device__ __forceinline__ float inv_pow2(float p) {
   return __uint_as_float(0x7F000000u - __float_as_uint(p));
@@ -215,7 +217,7 @@ __device__ __forceinline__ Query<D, BITS> make_query(const float (&qv)[D / 32],
   for (int e = 0; e < E; ++e) qm = max(qm, __float_as_uint(qv[e]) & 0x7FFFFFFFu);
 #pragma unroll
   for (int o = LPG / 2; o >= 1; o >>= 1) qm = max(qm, __shfl_xor_sync(0xFFFFFFFFu, qm, o));
-  const float q2 = pow2_of(qm), qi = inv_pow2(q2);
+  const float q2 = part_unit(qm), qi = inv_pow2(q2);
   r.unit = __shfl_sync(0xFFFFFFFFu, q2, quad * LPG & 31);  // (no group: any)
   __syncwarp();
 #pragma unroll
@@ -397,8 +399,8 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
   const float w = on ? ex2_approx(x - m) : 0.f;
   l += w;
 
-  // weights times scales of group `quad`, rows row8 + 8 b, over the power of two
-  // of the tile's largest scale of the group, as two fp16 parts: the columns
+  // weights times scales of group `quad`, rows row8 + 8 b, over a power of two by
+  // the tile's largest scale of the group, as two fp16 parts: the columns
   // 2 quad, 2 quad + 1 of an 8 x 8 block whose transpose is the B operand
   // (this lane: column row8, rows 2 quad, + 1 of the block)
   uint32_t sb[4], top = 0;
@@ -411,7 +413,7 @@ __device__ __forceinline__ void attend_tile(const unsigned char *stage, int rows
   }
 #pragma unroll
   for (int x2 = 4; x2 <= 16; x2 <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, x2));
-  const float unit = pow2_of(top << 16), inv = inv_pow2(unit);
+  const float unit = part_unit(top << 16), inv = inv_pow2(unit);
   uint32_t wf[4];
 #pragma unroll
   for (int b = 0; b < 4; ++b) {

@@ -934,3 +934,64 @@ def test_queries_whose_groups_differ_in_size(bits, D, spread):
         to, tl = tolerances(c.q[h], K, V)
         assert np.abs(got[h] - o).max() <= to, (h, np.abs(got[h] - o).max(), to)
         assert abs(gl[h] - l) <= tl, (h, gl[h], l, tl)
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("spread", [16, 22, 28])
+def test_a_row_that_takes_the_weight_with_small_values(bits, D, spread):
+    """One row has all the weight but 2^-spread of it, and V values 2^-spread of
+    the others': both count alike. A channel is off by 2 eps + 2^-19 (the
+    tolerance of any attention) of its own sum of |w v|, and for each row by
+    2^-50 of the largest scale times a code of up to M; not by a part of the
+    largest |v|."""
+    import torch
+    c = QCache([1, 31, 32, 300], D, bits, "fp32", seed=D + spread)
+    M = 127 if bits == 8 else 7
+    for h in range(c.n):
+        a, top = slice(c.off[h], c.off[h] + c.lens[h]), int(c.off[h] + c.lens[h] // 2)
+        # K: equal logits of 0 but the row's, which is spread * ln 2
+        c.k_codes[a] = 0
+        c.k_codes[top, 0], c.k_scales[top, 0] = 1, 1.0
+        c.q[h, 0] = np.float32(spread * math.log(2) * math.sqrt(D))
+        c.v_scales[a] *= np.float32(2.0 ** spread)
+        c.v_scales[top] *= np.float32(2.0 ** -spread)
+        c.ck[a] = torch.from_numpy(S.packed(c.k_codes[a], bits)).cuda()
+        c.sk[a], c.sv[a] = to_torch(c.k_scales[a], "bf16"), to_torch(c.v_scales[a], "bf16")
+    out = torch.empty(c.n, D, device="cuda")
+    c.H.hkv_quant_attention(c.cfg, c.c, 0, to_torch(c.q, "fp32"), out, c.ws, c.ws_bytes)
+    c.H.hkv_quant_check(c.c)
+    got = out.cpu().numpy()
+    for h in range(c.n):
+        K, V = c.rows(h)
+        want, _ = S.attention_lse(c.q[h], K, V)
+        x = (K @ c.q[h].astype(np.float64)) / math.sqrt(D)
+        w = np.exp(x - x.max())
+        w /= w.sum()
+        eps = 2.0 ** -19 * float((np.abs(K) @ np.abs(c.q[h])).max()) / math.sqrt(D)
+        scales = c.v_scales[c.off[h]:c.off[h] + c.lens[h]].astype(np.float64)
+        floor = np.repeat(scales.max(0), 32) * len(w) * M * 2.0 ** -50
+        tol = (2 * eps + 2.0 ** -19) * (w @ np.abs(V)) + floor
+        assert (np.abs(got[h] - want) <= tol).all(), (h, (np.abs(got[h] - want) / tol).max())
+
+
+@pytest.mark.parametrize("bits", FMT)
+@pytest.mark.parametrize("power", [-100, -60, 60, 110, 125])
+def test_queries_of_any_size(bits, power):
+    """fp32 queries near both ends of the range against keys near the other."""
+    import torch
+    D = 128
+    c = QCache([1, 33, 200], D, bits, "fp32", seed=bits)
+    c.q = np.clip(c.q, -3.9, 3.9) * np.float32(2.0 ** power)
+    c.k_scales = S.round_bf16(c.k_scales * np.float32(2.0 ** -power)).reshape(c.k_scales.shape)
+    for o, n in zip(c.off, c.lens):
+        c.sk[o:o + n] = to_torch(c.k_scales[o:o + n], "bf16")
+    out, lse = torch.empty(c.n, D, device="cuda"), torch.empty(c.n, device="cuda")
+    c.H.hkv_quant_attention(c.cfg, c.c, 0, to_torch(c.q, "fp32"), out, c.ws, c.ws_bytes, lse=lse)
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    for h in range(c.n):
+        K, V = c.rows(h)
+        q = c.q[h].astype(np.float64)
+        o, l = S.attention_lse(q, K, V)
+        to, tl = tolerances(q, K, V)
+        assert np.abs(got[h] - o).max() <= to and abs(gl[h] - l) <= tl, h
