@@ -95,11 +95,16 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&h);
 }
-// a pair of fp32 as bf16 parts of falling size; the remainder is exact
+// a pair of fp32 as bf16 parts of falling size; the remainder is exact. ANY: the
+// first part stays finite where an element lies above the largest bf16 number
+// (an infinity's parts hold a NaN, as a NaN's do).
+template <bool ANY>
 __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[3]) {
+  constexpr float kMost = 0x1.fep127f;
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
-    p[j] = pack2(x, y);
+    p[j] = ANY && j == 0 ? pack2(fminf(fmaxf(x, -kMost), kMost), fminf(fmaxf(y, -kMost), kMost))
+                         : pack2(x, y);
     x -= __uint_as_float(p[j] << 16);
     y -= __uint_as_float(p[j] & 0xFFFF0000u);
   }
@@ -125,7 +130,7 @@ __device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T
       }
       uint32_t p[4][3];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) split2(x[2 * j], x[2 * j + 1], p[j]);
+      for (int j = 0; j < 4; ++j) split2<true>(x[2 * j], x[2 * j + 1], p[j]);
 #pragma unroll
       for (int k = 0; k < 3; ++k)
         *reinterpret_cast<uint4 *>(dst + k * plane + at16<D>(r, c)) =
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
           const float w1 = key + 1 < left ? ex2_approx(s[x][2 * j + 1] - m[j]) : 0.f;
           l[j] += w0 + w1;
           uint32_t pr[3];
-          split2(w0, w1, pr);
+          split2<false>(w0, w1, pr);
 #pragma unroll
           for (int k = 0; k < 3; ++k) pf[x / 2][k][(x & 1) * 2 + j] = pr[k];
         }
@@ -558,7 +563,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
           l0 += w0;
           l1 += w1;
           uint32_t part[3];
-          split2(w0, w1, part);
+          split2<false>(w0, w1, part);
 #pragma unroll
           for (int k = 0; k < 3; ++k) w[k][j / 2] = part[k];
         }

@@ -995,3 +995,43 @@ def test_queries_of_any_size(bits, power):
         o, l = S.attention_lse(q, K, V)
         to, tl = tolerances(q, K, V)
         assert np.abs(got[h] - o).max() <= to and abs(gl[h] - l) <= tl, h
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("seqs", [1, 20, 40])
+def test_prompt_elements_near_the_largest_fp32(D, seqs):
+    """fp32 elements above the largest bf16 number (3.39e38): in V, in
+    K against a query element of 2^-126, and in the query against such a key.
+    One row has (nearly) all the weight, so that no sum leaves the range."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    rng = np.random.default_rng(seqs + D)
+    T, Hh, big = 150, 3, np.float32(3.4e38)
+    cfg = H.make_config(n_layers=1, n_seqs=seqs, n_heads=Hh, head_dim=D, dtype="fp32", n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k = rng.normal(size=(1, Hh, T, D)).astype(np.float32)
+    v = rng.normal(size=(1, Hh, T, D)).astype(np.float32)
+    q = rng.normal(size=(seqs, Hh, D)).astype(np.float32)
+    # head 0: V; row 77 has the weight
+    k[0, 0, :, 0], q[:, 0, 0] = 0.0, 8.0 * math.sqrt(D)
+    k[0, 0, 77, 0] = 8.0
+    v[0, 0, 77] = np.linspace(-1, 1, D).astype(np.float32) * big
+    v[0, 0, 77, -1] = np.finfo(np.float32).max
+    # heads 1 and 2: a key's element, a query's
+    q[:, 1, 5], k[0, 1, :, 5] = np.float32(2.0 ** -126), 0.0
+    k[0, 1, 33, 5], k[0, 1, 140, 5] = big, -big
+    q[:, 2, 5], k[0, 2, :, 5] = big, 0.0
+    k[0, 2, 33, 5], k[0, 2, 140, 5] = np.float32(2.0 ** -126), np.float32(-2.0 ** -126)
+    kt, vt, qt = (to_torch(x, "fp32") for x in (k, v, q))
+    pre = H.make_prefix(kt, vt, torch.tensor([T], dtype=torch.int32, device="cuda"))
+    ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros(seqs, Hh, D, device="cuda"), torch.zeros(seqs, Hh, device="cuda")
+    H.hkv_prefix_attention(cfg, pre, qt, out, lse, ws, ws.numel())
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    for s in range(seqs):
+        for h in range(Hh):
+            K, V = (x[0, h].astype(np.float64) for x in (k, v))
+            o, l = S.attention_lse(q[s, h], K, V)
+            to, tl = tolerances(q[s, h], K, V)
+            assert np.abs(got[s, h] - o).max() <= to and abs(gl[s, h] - l) <= tl, (s, h)
