@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
   float o[D / 8][4];
 #pragma unroll
   for (int x = 0; x < D / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[2] = {kNoKey, kNoKey}, l[2] = {0.f, 0.f};
   if (lo < hi) {
     load_rows<D, T, kThreads>(sq, SM::kQPlane, static_cast<const T *>(p.q) + qrow * D,
                     (long long)p.heads * D, MW * 16, nq);
@@ -282,10 +282,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1)
       for (int x = 0; x < NKW / 8; ++x) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          // a key that does not count weighs nothing (all of them: m is -inf)
-          const int key = x * 8 + (lane & 3) * 2;
-          const float w0 = key < left ? ex2_approx(s[x][2 * j] - m[j]) : 0.f;
-          const float w1 = key + 1 < left ? ex2_approx(s[x][2 * j + 1] - m[j]) : 0.f;
+          // (a key that does not count has a score of -inf)
+          const float w0 = ex2_approx(s[x][2 * j] - m[j]);
+          const float w1 = ex2_approx(s[x][2 * j + 1] - m[j]);
           l[j] += w0 + w1;
           uint32_t pr[3];
           split2<false>(w0, w1, pr);

@@ -106,6 +106,10 @@ __device__ __forceinline__ uint32_t quant_group(const float *x, uint32_t mask, u
   return sb;
 }
 
+// A running maximum before its first key: finite, so that keys whose scores are
+// -inf (or that do not count) weigh nothing against it.
+constexpr float kNoKey = -0x1.fffffep127f;
+
 // Byte offset of the 16-byte piece `c` of row `r` in a tile: rows lie back to
 // back, the pieces permuted so that the reads below spread over all banks.
 template <int RB>

@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kWarps * 32, STAGES == 1   ? 7
   const int new_tile = hd.len / kTile;
   if (STEP && new_tile >= t0 && new_tile < t1 && (new_tile - t0) % kWarps == warp)
     load_new_row<D, T>(p, hl, nr);
-  float m = -INFINITY, l = 0.f;
+  float m = kNoKey, l = 0.f;
   if (t0 + warp < t1 && hd.n > 0) {
     float acc[D / 16][2] = {};
     __half *operand = reinterpret_cast<__half *>(ws + STAGES * TL::kBytes);

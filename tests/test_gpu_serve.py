@@ -1035,3 +1035,46 @@ def test_prompt_elements_near_the_largest_fp32(D, seqs):
             o, l = S.attention_lse(q[s, h], K, V)
             to, tl = tolerances(q[s, h], K, V)
             assert np.abs(got[s, h] - o).max() <= to and abs(gl[s, h] - l) <= tl, (s, h)
+
+
+def test_scores_below_the_range_weigh_nothing():
+    """Keys whose scores leave fp32 downwards, whole tiles of them before any
+    other key: no weight, as in 64 bits, where theirs underflow. Tolerances
+    from the keys that count."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    rng = np.random.default_rng(11)
+    D, T, low, Hh = 64, 300, 130, 3
+    for dtype, seqs, heads in (("bf16", 3, Hh), ("fp32", 3, Hh), ("fp32", 40, Hh), ("bf16", 64, 32)):
+        cfg = H.make_config(n_layers=1, n_seqs=seqs, n_heads=heads, head_dim=D, dtype=dtype, n_cond=0,
+                            n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                            global_budget=1)
+        k = rounded(rng.normal(size=(1, heads, T, D)), dtype)
+        v = rounded(rng.normal(size=(1, heads, T, D)), dtype)
+        q = rounded(1 + np.abs(rng.normal(size=(seqs, heads, D))), dtype)
+        k[0, :, :low] = rounded(np.float32(-3e38), dtype)
+        pre = H.make_prefix(to_torch(k, dtype), to_torch(v, dtype),
+                            torch.tensor([T], dtype=torch.int32, device="cuda"))
+        ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+        out, lse = torch.zeros(seqs, heads, D, device="cuda"), torch.zeros(seqs, heads, device="cuda")
+        H.hkv_prefix_attention(cfg, pre, to_torch(q, dtype), out, lse, ws, ws.numel())
+        got, gl = out.cpu().numpy(), lse.cpu().numpy()
+        for s in range(seqs):
+            for h in range(heads):
+                o, l = S.attention_lse(q[s, h], k[0, h, low:], v[0, h, low:])
+                to, tl = tolerances(q[s, h], k[0, h, low:], v[0, h, low:])
+                assert np.abs(got[s, h] - o).max() <= to and abs(gl[s, h] - l) <= tl, (dtype, seqs, s, h)
+    for bits in FMT:
+        c = QCache([T, 2000], D, bits, "fp32", seed=bits)
+        c.q = 1 + np.abs(c.q)
+        for h in range(2):
+            a = slice(c.off[h], c.off[h] + low)
+            c.k_codes[a], c.k_scales[a] = -7, np.float32(2.0 ** 120)
+            c.ck[a], c.sk[a] = torch.from_numpy(S.packed(c.k_codes[a], bits)).cuda(), to_torch(c.k_scales[a], "bf16")
+        out, lse = torch.empty(2, D, device="cuda"), torch.empty(2, device="cuda")
+        H.hkv_quant_attention(c.cfg, c.c, 0, to_torch(c.q, "fp32"), out, c.ws, c.ws_bytes, lse=lse)
+        for h in range(2):
+            K, V = (x[low:] for x in c.rows(h))
+            o, l = S.attention_lse(c.q[h], K, V)
+            to, tl = tolerances(c.q[h], K, V)
+            assert np.abs(out[h].cpu().numpy() - o).max() <= to and abs(float(lse[h]) - l) <= tl, (bits, h)
