@@ -171,7 +171,10 @@ size_t hkv_prefix_workspace_size(const hkv_config *cfg, const hkv_prefix *prefix
  * lse[s][h] as hkv_quant_attention defines them (both required), to be given
  * to hkv_quant_step or hkv_quant_attention as prior. A prompt of length 0
  * yields zeros and -inf. n_seqs not a multiple of n_groups, or strides that
- * are not multiples of 16 bytes -> HKV_ERR_SHAPE. A group whose length is
+ * are not multiples of 16 bytes -> HKV_ERR_SHAPE. An infinite or NaN element of
+ * q, k or v shows in the outputs that its products enter, and in no others, as
+ * a number that is not finite: NaN also where the definition gives an infinity
+ * (the weights enter as parts, which may be zero). A group whose length is
  * negative or above max_len gets NaN, and HKV_ERR_BOUNDS in the error word;
  * so does one whose products did not finish within the kernel's limit of two
  * seconds, with HKV_ERR_TIMEOUT. */

@@ -1078,3 +1078,44 @@ def test_scores_below_the_range_weigh_nothing():
             o, l = S.attention_lse(c.q[h], K, V)
             to, tl = tolerances(c.q[h], K, V)
             assert np.abs(out[h].cpu().numpy() - o).max() <= to and abs(float(lse[h]) - l) <= tl, (bits, h)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,seqs,heads", [("bf16", 3, 5), ("fp32", 3, 5), ("fp32", 40, 5), ("bf16", 64, 20),
+                                              ("bf16", 100, 20)])
+def test_prompt_elements_that_are_not_finite(D, dtype, seqs, heads):
+    """They show where their products enter, and nowhere else: a V element in
+    its channel, a key's or a query's in the head or the query."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    rng = np.random.default_rng(D + seqs)
+    T = 520
+    cfg = H.make_config(n_layers=1, n_seqs=seqs, n_heads=heads, head_dim=D, dtype=dtype, n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k = rounded(rng.normal(size=(1, heads, T, D)), dtype)
+    v = rounded(rng.normal(size=(1, heads, T, D)), dtype)
+    q = rounded(rng.normal(size=(seqs, heads, D)), dtype)
+    v[0, 0, 100, 3], v[0, 0, 300, 40], v[0, 0, 519, 62] = np.inf, -np.inf, np.nan
+    k[0, 1, 77, 9] = np.nan
+    q[seqs - 1, 2, 5] = np.nan
+    finite = np.ones((seqs, heads, D), bool)
+    finite[:, 0, [3, 40, 62]] = False
+    finite[:, 1] = False
+    finite[seqs - 1, 2] = False
+    pre = H.make_prefix(to_torch(k, dtype), to_torch(v, dtype),
+                        torch.tensor([T], dtype=torch.int32, device="cuda"))
+    ws = torch.zeros(H.hkv_prefix_workspace_size(cfg, pre), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros(seqs, heads, D, device="cuda"), torch.zeros(seqs, heads, device="cuda")
+    H.hkv_prefix_attention(cfg, pre, to_torch(q, dtype), out, lse, ws, ws.numel())
+    got, gl = out.cpu().numpy(), lse.cpu().numpy()
+    assert np.array_equal(np.isfinite(got), finite)
+    assert np.array_equal(np.isfinite(gl), finite[:, :, 0])
+    for s in (0, seqs - 1):
+        for h in (0, 2, 3):
+            if not np.isfinite(gl[s, h]):
+                continue
+            vv = np.where(np.isfinite(v[0, h]), v[0, h], 0)
+            o, l = S.attention_lse(q[s, h], k[0, h], vv)
+            to, tl = tolerances(q[s, h], k[0, h], vv)
+            assert np.abs(got[s, h] - o)[finite[s, h]].max() <= to and abs(gl[s, h] - l) <= tl, (s, h)
