@@ -115,8 +115,6 @@ hkv_status quant_attend(const char *name, const hkv_config *cfg, const hkv_qcach
   a.count = reinterpret_cast<uint32_t *>(ws);
   a.part = reinterpret_cast<float *>(ws + quant_counts_bytes(cfg));
   a.max_rows = max_segment(cfg);
-  // tiles of 32 rows are counted in 31 bits
-  if ((long long)a.nheads * ((a.max_rows + 31) / 32) > 0x7FFFFFFFLL) return HKV_ERR_SHAPE;
   HKV_TRY(device_sms(&a.sms));
   a.P = cfg->period;
   a.C = cfg->n_cond;

@@ -342,3 +342,16 @@ def test_runner_quantises_a_cache_it_continues_with(H):
         with pytest.raises(H.HkvError) as e:
             call()
         assert e.value.status == H.HKV_ERR_STATE
+
+
+def test_many_long_heads_are_not_refused(H):
+    """Tiles are counted per head: heads times tiles past 31 bits is no fault.
+    Without a GPU the call gets as far as asking for the device."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not the device's")
+    buf, a, _, quant, _ = caches(H)
+    cfg = cfg_of(H, n_seqs=256, n_heads=32, n_image=1 << 23, group_at=1 << 23)
+    st = H.lib().hkv_quant_attention(ctypes.byref(cfg), ctypes.byref(quant), 0, a, None, None, a, None, a,
+                                     1 << 30, None)
+    assert st == H.HKV_ERR_CUDA
