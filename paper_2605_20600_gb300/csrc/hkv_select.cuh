@@ -77,7 +77,7 @@ __host__ __device__ constexpr int stage_rows(int max_len) {
 
 // the query ring (P rows of es-byte elements); after q-bar it is the score
 // stage: NT/32 warps x stage_rows rows of D * es + 16 bytes
-// (or of kb bytes, key rows of codes)
+// (or of kb bytes, key rows of codes); a multiple of 16
 __host__ __device__ constexpr size_t ring_bytes(int P, int D, int es, int max_len, int kb = 0) {
   const size_t ring = (size_t)P * D * es;
   const size_t stage = (size_t)(NT / 32) * stage_rows(max_len) * (kb ? kb : D * es + 16);
@@ -89,7 +89,7 @@ __device__ __forceinline__ UpdSmem carve(unsigned char *dyn, int max_len, int D,
   UpdSmem u;
   u.ring = dyn;
   u.stage_rows = stage_rows(max_len);
-  u.keys = reinterpret_cast<unsigned long long *>(dyn + ((ring_bytes(P, D, es, max_len, kb) + 7) & ~(size_t)7));
+  u.keys = reinterpret_cast<unsigned long long *>(dyn + ring_bytes(P, D, es, max_len, kb));
   u.ps = reinterpret_cast<int *>(u.keys + max_len);
   u.aux = u.ps + max_len;
   u.qbar = reinterpret_cast<float *>(u.aux + max_len);
