@@ -151,8 +151,8 @@ hkv_status hkv_quant_step(const hkv_config *cfg, const hkv_qcache *cache, int la
  * fixed fp32 order); rows move with their scales. The i-th evicted row below
  * the new length, in storage order, takes the i-th surviving row above it.
  * The larger of period * head_dim * elem (elem of the config dtype) and 32 *
- * head_dim * format bytes, plus 16 bytes per token of the longest segment,
- * must fit in 227 KB, else HKV_ERR_CAPACITY. */
+ * head_dim * format bytes, plus 16 bytes per token of the longest segment, 4 *
+ * head_dim and 2544 bytes, must fit in 227 KB, else HKV_ERR_CAPACITY. */
 hkv_status hkv_quant_evict(const hkv_config *cfg, const hkv_qcache *cache, int layer,
                            hkv_stream_t stream);
 hkv_status hkv_quant_evict_all(const hkv_config *cfg, const hkv_qcache *cache, hkv_stream_t stream);

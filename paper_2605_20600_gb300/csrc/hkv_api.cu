@@ -76,7 +76,7 @@ hkv_status attention_ctas(DeviceState *st, int D, int dtype, int *ctas) {
 
 hkv_status update_ready(DeviceState *st, int D, int dtype, size_t smem) {
   std::atomic<size_t> &have = st->update_smem[dt_index(dtype)][d_index(D)];
-  if (smem > kMaxSmem) return HKV_ERR_CAPACITY;
+  if (smem > kMaxUpdateSmem) return HKV_ERR_CAPACITY;
   if (have.load(std::memory_order_acquire) < smem) {
     std::lock_guard<std::mutex> lk(g_mu);
     if (have.load(std::memory_order_relaxed) < smem) {

@@ -13,7 +13,8 @@
 namespace hkv {
 
 constexpr int kMaxDevices = 64;
-constexpr size_t kMaxSmem = 227 * 1024;
+// dynamic shared memory of the update kernels: what a CTA may have, less theirs
+constexpr size_t kMaxUpdateSmem = 227 * 1024 - kUpdateStatic;
 
 inline hkv_status injected(const char *name) {
   const char *s = getenv("HKV_FAULT_INJECT");

@@ -135,6 +135,7 @@ struct MethodArgs {
 };
 
 constexpr int kCacheThreads = 256;
+constexpr size_t kUpdateStatic = 432;  // static shared memory of the update kernels, bytes
 
 // dynamic shared memory of the update paths for segments of up to max_len
 // tokens and a query ring of P rows

@@ -56,6 +56,7 @@ struct UpdShared {
   long long lscan[33];
   uint64_t ring_bar;  // completion of the bulk copy of the query ring
 };
+static_assert(sizeof(UpdShared) == kUpdateStatic, "the host subtracts it from a CTA's 227 KB");
 
 // Shared-memory work area of one update (dynamic).
 struct UpdSmem {

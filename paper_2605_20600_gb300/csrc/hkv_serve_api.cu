@@ -129,7 +129,7 @@ std::atomic<size_t> g_evict_smem[kMaxDevices][2][2][2];
 std::mutex g_serve_mu;
 
 hkv_status evict_ready(const hkv_config *cfg, int bits, size_t smem) {
-  if (smem > kMaxSmem) return HKV_ERR_CAPACITY;
+  if (smem > kMaxUpdateSmem) return HKV_ERR_CAPACITY;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return HKV_ERR_CUDA;
   std::atomic<size_t> &have = g_evict_smem[dev][cfg->dtype == HKV_BF16][cfg->head_dim == 128]

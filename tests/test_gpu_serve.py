@@ -1119,3 +1119,31 @@ def test_prompt_elements_that_are_not_finite(D, dtype, seqs, heads):
             o, l = S.attention_lse(q[s, h], k[0, h], vv)
             to, tl = tolerances(q[s, h], k[0, h], vv)
             assert np.abs(got[s, h] - o)[finite[s, h]].max() <= to and abs(gl[s, h] - l) <= tl, (s, h)
+
+
+def test_updates_of_the_longest_segments_that_fit():
+    """The longest segment the header's rule admits is launched, one token more
+    is a capacity error, for plain and quantised caches (uncompressed heads:
+    nothing is due)."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    from paper_2605_20600_gb300.engine import CacheBuffers, QuantCacheBuffers
+    D, room = 64, 227 * 1024 - 4 * 64 - 2544
+    for stage, quant in ((256 * (D * 2 + 16), False), (32 * D * 8, True)):
+        for over in (0, 1, 20):
+            cfg = H.make_config(n_layers=1, n_seqs=1, n_heads=2, head_dim=D, dtype="bf16", n_cond=0,
+                                n_image=20000, row_len=100, recent_w=16, local_w=16, period=8,
+                                group_at=(room - stage) // 16 + over, global_budget=24)
+            c = CacheBuffers(cfg, 16, "cuda")
+            if quant:
+                c = QuantCacheBuffers(cfg, 8, 16, "cuda", qbuf=c.qbuf, label=c.label, off=c.off, cap=c.cap)
+            for call in ((lambda: H.hkv_quant_evict_all(cfg, c.c), lambda: H.hkv_quant_evict(cfg, c.c, 0))
+                         if quant else (lambda: H.hkv_evict_all(cfg, c.c), lambda: H.hkv_evict(cfg, c.c, 0))):
+                if over == 0:
+                    call()
+                else:
+                    with pytest.raises(H.HkvError) as e:
+                        call()
+                    assert e.value.status == H.HKV_ERR_CAPACITY
+            (H.hkv_quant_check if quant else H.hkv_check)(c.c)
+    assert torch.ones(3, device="cuda").sum().item() == 3     # no error left behind

@@ -355,3 +355,24 @@ def test_many_long_heads_are_not_refused(H):
     st = H.lib().hkv_quant_attention(ctypes.byref(cfg), ctypes.byref(quant), 0, a, None, None, a, None, a,
                                      1 << 30, None)
     assert st == H.HKV_ERR_CUDA
+
+
+def test_updates_that_just_do_not_fit_shared_memory(H):
+    """Segments whose work area fits 227 KB only without the kernels' own
+    432 bytes: a capacity error, with the longest that fits beside it."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not the device's")
+    buf, a, plain, quant, _ = caches(H)
+    room = 227 * 1024 - 4 * 64 - 2544
+
+    def cfg(stage, over):              # n_cond = 8; 16 bytes a token
+        n = (room - stage) // 16 + over
+        return cfg_of(H, n_image=20000, row_len=100, group_at=n - 8)
+
+    for call in (lambda c: H.hkv_quant_evict_all(c, quant), lambda c: H.hkv_quant_evict(c, quant, 0)):
+        for over, want in ((0, H.HKV_ERR_CUDA), (1, H.HKV_ERR_CAPACITY), (26, H.HKV_ERR_CAPACITY),
+                           (28, H.HKV_ERR_CAPACITY)):   # the first fits, but there is no device
+            with pytest.raises(H.HkvError) as e:
+                call(cfg(32 * 64 * 8, over))
+            assert e.value.status == want, over
