@@ -93,10 +93,11 @@ typedef struct {
  * layers) of a plain cache into the head's segment of the quantised one, in
  * storage order, and sets pos, len, nbuf and ntok there. off, cap and label
  * of dst are the caller's (they may be src's own arrays); dst->qbuf must be
- * src->qbuf. A head that does not fit its segment, or is longer than the
- * config allows, sets HKV_ERR_CAPACITY, one outside an arena HKV_ERR_BOUNDS,
- * and with HKV_PACK_SKIP_COND one of fewer than n_cond rows HKV_ERR_STATE in
- * dst's error word; that head is left unchanged. */
+ * src->qbuf. With HKV_PACK_SKIP_COND dst's pos and len must be other arrays
+ * than src's (HKV_ERR_INVALID_ARG). A head that does not fit its segment, or
+ * is longer than the config allows, sets HKV_ERR_CAPACITY, one outside an
+ * arena HKV_ERR_BOUNDS, and with HKV_PACK_SKIP_COND one of fewer than n_cond
+ * rows HKV_ERR_STATE in dst's error word; that head is left unchanged. */
 hkv_status hkv_quant_pack(const hkv_config *cfg, const hkv_cache *src, const hkv_qcache *dst,
                           int layer, int flags, hkv_stream_t stream);
 

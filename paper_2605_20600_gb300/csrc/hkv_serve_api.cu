@@ -204,6 +204,8 @@ hkv_status hkv_quant_pack(const hkv_config *cfg, const hkv_cache *src, const hkv
   int first, count;
   HKV_TRY(layer_heads(cfg, layer, &first, &count));
   const int skip = (flags & HKV_PACK_SKIP_COND) ? cfg->n_cond : 0;
+  // a head's CTAs read src's while one of them writes dst's
+  if (skip && (dst->len == src->len || dst->pos == src->pos)) return HKV_ERR_INVALID_ARG;
   return cuda_status(launch_quant_pack(cache_args(src), qcache_args(dst), first, count, skip,
                                        max_segment(cfg), cfg->head_dim, cfg->dtype, dst->format,
                                        (cudaStream_t)stream));

@@ -376,3 +376,24 @@ def test_updates_that_just_do_not_fit_shared_memory(H):
             with pytest.raises(H.HkvError) as e:
                 call(cfg(32 * 64 * 8, over))
             assert e.value.status == want, over
+
+
+def test_pack_without_the_conditioning_rows_wants_lengths_of_its_own(H):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not the device's")
+    buf, a, plain, quant, _ = caches(H)
+    cfg, call = cfg_of(H), H.lib().hkv_quant_pack
+
+    def pack(flags, cfg=cfg, **kw):
+        q = H.hkv_qcache.from_buffer_copy(quant)
+        for k, v in kw.items():
+            setattr(q, k, v)
+        return call(ctypes.byref(cfg), ctypes.byref(plain), ctypes.byref(q), 0, flags, None)
+
+    assert pack(H.HKV_PACK_SKIP_COND, len=a + 256) == H.HKV_ERR_INVALID_ARG
+    assert pack(H.HKV_PACK_SKIP_COND, pos=a + 256) == H.HKV_ERR_INVALID_ARG
+    # accepted, up to the launch: own arrays, or no rows left out
+    for st in (pack(H.HKV_PACK_SKIP_COND, len=a + 256, pos=a + 512), pack(0),
+               pack(H.HKV_PACK_SKIP_COND, cfg=cfg_of(H, n_cond=0))):
+        assert st == H.HKV_ERR_CUDA
