@@ -1147,3 +1147,56 @@ def test_updates_of_the_longest_segments_that_fit():
                     assert e.value.status == H.HKV_ERR_CAPACITY
             (H.hkv_quant_check if quant else H.hkv_check)(c.c)
     assert torch.ones(3, device="cuda").sum().item() == 3     # no error left behind
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,seqs,T,lens,layout,heads", [
+    (1, 40, 200, [187], "htd", 160), (2, 64, 333, [333, 0], "thd", 80), (1, 17, 640, [577], "padded", 160),
+    (1, 100, 257, [257], "padded", 160), (2, 130, 130, [64, 129], "htd", 40), (2, 65, 200, [0, 1], "thd", 80)])
+def test_prefix_attention_of_many_heads(D, G, seqs, T, lens, layout, heads):
+    """Batches whose (group, head) pairs fill the device: one range of keys
+    each, finished without a join."""
+    from paper_2605_20600_gb300 import hkv as H
+    import torch
+    cfg = H.make_config(n_layers=1, n_seqs=G * seqs, n_heads=heads, head_dim=D, dtype="bf16", n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k = torch.zeros(G, heads, T, D, dtype=torch.bfloat16)
+    assert H.hkv_prefix_workspace_size(cfg, H.make_prefix(k, k, torch.zeros(G, dtype=torch.int32))) == 256
+    check_prefix(D, "bf16", G, seqs, T, lens, layout, heads)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,seqs,heads,T,joined", [
+    ("bf16", 3, 2, 300, True), ("bf16", 3, 160, 70, False), ("fp32", 40, 2, 300, True),
+    ("bf16", 40, 20, 600, True), ("bf16", 100, 20, 600, True), ("bf16", 40, 100, 300, False),
+    ("bf16", 100, 100, 300, False)])
+def test_prefix_length_out_of_range_on_every_kernel(D, dtype, seqs, heads, T, joined):
+    """The group gets NaN, the other groups are as without it, and the error
+    word says so, with one range of keys and with several."""
+    import torch
+    from paper_2605_20600_gb300 import hkv as H
+    rng = np.random.default_rng(T)
+    cfg = H.make_config(n_layers=1, n_seqs=3 * seqs, n_heads=heads, head_dim=D, dtype=dtype, n_cond=0,
+                        n_image=8, row_len=1, recent_w=1, local_w=1, period=1, group_at=8,
+                        global_budget=1)
+    k, v = prefix_rows(rng, 3, heads, T, D, dtype, "htd")
+    q = to_torch(rng.normal(size=(3 * seqs, heads, D)), dtype)
+    res = []
+    for bad in (None, T + 1, -1, 1 << 30):
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        lens = [T, T if bad is None else bad, T - 5]
+        pre = H.make_prefix(k, v, torch.tensor(lens, dtype=torch.int32, device="cuda"), err)
+        n = H.hkv_prefix_workspace_size(cfg, pre)
+        assert (n > 256) == joined
+        ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+        out, lse = torch.zeros(3, seqs, heads, D, device="cuda"), torch.zeros(3, seqs, heads, device="cuda")
+        H.hkv_prefix_attention(cfg, pre, q, out, lse, ws, n)
+        torch.cuda.synchronize()
+        assert int(err) == (0 if bad is None else H.HKV_ERR_BOUNDS)
+        res.append((out, lse))
+    for out, lse in res[1:]:
+        assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
+        for g in (0, 2):
+            assert torch.equal(out[g], res[0][0][g]) and torch.equal(lse[g], res[0][1][g])
+    assert torch.isfinite(res[0][0]).all() and torch.isfinite(res[0][1]).all()
