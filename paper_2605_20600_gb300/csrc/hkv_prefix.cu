@@ -19,11 +19,14 @@
 // What bounds it: the chain of one tile (scores, weights, output, with a wait
 // between any two), about 2 us a tile, and the start and the join around it.
 // 32 heads x 4099 keys of 128 channels, 64 queries: 29 us, of which DRAM (67 MB)
-// needs 10; 20 heads, two prompts of 1000 and 667 keys of 64 channels: 12 us;
-// fp32, 8 heads x 777 keys, 5 queries: 10 us. One launch with the ranges of a
+// needs 10, and 128 queries 39; 20 heads, two prompts of 1000 and 667 keys of 64
+// channels: 12 us; fp32, 8 heads x 777 keys, 5 queries: 10 us, and 32 heads x 4099
+// keys of 128 channels, 64 queries: 259 us (100 TFLOP/s of bf16 products: its
+// tiles are loaded and split between two barriers, with nothing in flight during
+// the products, by one CTA an SM). One launch with the ranges of a
 // prompt in a cluster, joined through distributed shared memory, took 18 us
-// for the second, 15 for two launches then (a cluster waits for room for all its CTAs, and half of its
-// warps wait while the others join).
+// for the second, 15 for two launches then (a cluster waits for room for all its
+// CTAs, and half of its warps wait while the others join).
 #include "hkv_quant.cuh"
 #include "hkv_quant.h"
 #include "hkv_select.cuh"
@@ -751,7 +754,8 @@ cudaError_t launch_tiles(const PrefixArgs &a, int grid, int split_len, cudaStrea
 }  // namespace
 
 // As many key ranges as fill the device twice over (2 CTAs an SM), each a
-// whole number of tiles. bf16 batches of more than 16 sequences go to tcgen05
+// whole number of tiles. The 152 SMs are a constant here, so that the workspace
+// a caller allocated does not depend on the device of the call. bf16 batches of more than 16 sequences go to tcgen05
 // unless all their products of 16 queries and a tile are done in two rounds of
 // CTAs: over 32 heads of 128 channels, 16 sequences and 4099 keys take 23 us
 // with mma.sync and 27 with tcgen05; 32 take 29 and 28; 64 take 43 and 32, with

@@ -14,7 +14,8 @@ namespace {
 // rows of 128 bf16 channels go to 8 bits and back in 104 us (578 MB: 5.6 TB/s,
 // 82 % of a copy). Pack computes more than half of the time, so it takes the
 // threads of eight CTAs an SM over a second row in flight (five with two rows:
-// 111 us); unpack waits more and keeps two. A CTA takes 64 rows, or 32 where the
+// 111 us), although bf16 rows then spill 20 bytes a thread at 32 registers;
+// unpack waits more and keeps two. A CTA takes 64 rows, or 32 where the
 // launch has few CTAs: 99 heads of up to 357 fp32 rows to 4 bits and back 13.7 us
 // against 14.7 with 64 (the case above 115 with 32). fp32 rows, whose quotients
 // are taken, keep the registers of five CTAs: 12.1 us for the 99 heads.
@@ -223,7 +224,7 @@ struct CodeRows {
 // moves. What bounds it is one head's chain: positions, the queries' sum, the
 // scores (one lane a row, in a fixed order of 128 dependent sums), two radix
 // selections, the moves, each with a trip to memory or a barrier in between.
-// 1024 heads, half of them with 975 scored rows of 128 codes: 46 us, of which
+// 1024 heads, half of them with 975 scored rows of 128 codes: 47 us, of which
 // the bytes need 14; without the scored heads 19. So that as many chains as
 // possible overlap, the work area is kept small: codes are staged as they are
 // and without padding, which at up to 1233 rows leaves room for four CTAs an

@@ -12,9 +12,9 @@
 // A step's CTAs all read a head's length to find their part, so its counters
 // advance only when all of them have arrived, those without a part too.
 //
-// What bounds it: DRAM for rows of 128 bytes, 65537 x 32 of them take 95 us
-// (6.0 TB/s), the issue of ~600 instructions a tile for rows of 32 bytes, 42 us
-// (3.6 TB/s); and for short segments the launch, one round trip to memory and
+// What bounds it: DRAM for rows of 128 bytes, 65537 x 32 of them take 96 us
+// (5.9 TB/s), the issue of ~600 instructions a tile for rows of 32 bytes, 43 us
+// (3.5 TB/s); and for short segments the launch, one round trip to memory and
 // the join, 4 to 5 us a layer, some of which the next layer's CTAs hide: with
 // HKV_STEP_PREFETCH they load their first tiles before they wait. A kernel that
 // streamed equal runs of tiles, whatever heads they cross, through a grid of two

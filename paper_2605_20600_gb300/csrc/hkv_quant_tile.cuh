@@ -16,7 +16,7 @@
 //    product would be known only after the scores: 115 us instead of 112 for
 //    eight layers of 256 heads); a channel uses its own group's two columns.
 // Sums chain over at most 8 (scores) or 2 (output) products in the tensor core
-// and are added in fp32 registers beyond that. A tile is 580 (4 bits) to 670
+// and are added in fp32 registers beyond that. A tile is 585 (4 bits) to 675
 // instructions of a warp at D = 128; converting each code to fp32 for plain
 // fused multiply-adds takes two a code, 512 a lane and tile before any product.
 #pragma once
