@@ -64,7 +64,7 @@ class hkv_qcache(Structure):
 
 
 class hkv_prefix(Structure):
-    dtype = None   # HKV_FP32 or HKV_BF16 where make_prefix knows it
+    of = None   # (dtype, heads, head_dim) of the rows, where make_prefix knows them
     _fields_ = [
         ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
         ("group_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
@@ -313,7 +313,7 @@ def make_prefix(k, v, length, err=None) -> hkv_prefix:
     """An hkv_prefix from tensors k and v of [groups][heads][tokens][head_dim],
     fp32 or bf16 (any strides whose last is 1, the same in both), and the
     prompts' lengths, contiguous int32, all on one device; keeps them alive.
-    Calls with a config of another dtype refuse it."""
+    Calls with a config of another dtype, n_heads or head_dim refuse it."""
     if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
         raise HkvError("make_prefix", HKV_ERR_SHAPE)
     if length.numel() != k.shape[0]:
@@ -326,7 +326,7 @@ def make_prefix(k, v, length, err=None) -> hkv_prefix:
     p = hkv_prefix(k.data_ptr(), v.data_ptr(), length.data_ptr(), _p(err), k.stride(0),
                    k.stride(1), k.stride(2), k.shape[0], k.shape[2])
     p.arrays = (k, v, length, err)
-    p.dtype = dtype
+    p.of = (dtype, k.shape[1], k.shape[3])
     return p
 
 
@@ -370,13 +370,13 @@ def hkv_quant_check(cache, stream=0) -> None:
 
 
 def hkv_prefix_workspace_size(cfg, prefix) -> int:
-    if prefix.dtype not in (None, cfg.dtype):
+    if prefix.of not in (None, (cfg.dtype, cfg.n_heads, cfg.head_dim)):
         return 0
     return int(lib().hkv_prefix_workspace_size(ctypes.byref(cfg), ctypes.byref(prefix)))
 
 
 def hkv_prefix_attention(cfg, prefix, q, out, lse, workspace, ws_bytes, stream=0) -> None:
-    if prefix.dtype not in (None, cfg.dtype):
+    if prefix.of not in (None, (cfg.dtype, cfg.n_heads, cfg.head_dim)):
         raise HkvError("prefix_attention", HKV_ERR_SHAPE)
     _call("prefix_attention", ctypes.byref(cfg), ctypes.byref(prefix), _p(q), _p(out), _p(lse),
           _p(workspace), ws_bytes, stream)

@@ -397,3 +397,19 @@ def test_pack_without_the_conditioning_rows_wants_lengths_of_its_own(H):
     for st in (pack(H.HKV_PACK_SKIP_COND, len=a + 256, pos=a + 512), pack(0),
                pack(H.HKV_PACK_SKIP_COND, cfg=cfg_of(H, n_cond=0))):
         assert st == H.HKV_ERR_CUDA
+
+
+def test_a_prompt_of_other_heads_than_the_config_is_refused(H):
+    """Heads that the prompt does not have would be read past its end."""
+    import torch
+    buf, a, _, _, _ = caches(H)
+    cfg = cfg_of(H)                                       # 4 heads of 64, bf16
+    n = torch.zeros(2, dtype=torch.int32)
+    for heads, dim, ok in ((4, 64, True), (3, 64, False), (5, 64, False), (4, 128, False), (2, 128, False)):
+        k = torch.zeros(2, heads, 10, dim, dtype=torch.bfloat16)
+        pre = H.make_prefix(k, k, n)
+        assert (H.hkv_prefix_workspace_size(cfg, pre) > 0) == ok
+        if not ok:
+            with pytest.raises(H.HkvError) as e:
+                H.hkv_prefix_attention(cfg, pre, a, a, a, a, 1 << 30)
+            assert e.value.status == H.HKV_ERR_SHAPE
