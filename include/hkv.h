@@ -244,7 +244,9 @@ hkv_status hkv_append_evict(const hkv_config *cfg, const hkv_cache *cache, int l
  * buffered queries, then rows of keys, in shared memory: the larger of
  * P * head_dim * elem and 256 * (head_dim * elem + 16) bytes, plus 16 bytes
  * per token of the longest segment, 4 * head_dim and 2544 bytes, must fit in
- * 227 KB, else HKV_ERR_CAPACITY (also for hkv_append_evict and hkv_repack). */
+ * 227 KB, else HKV_ERR_CAPACITY (also for hkv_append_evict and hkv_repack).
+ * A head whose queries did not arrive within the limit of a device wait is
+ * left as it is, with HKV_ERR_TIMEOUT in the error word. */
 hkv_status hkv_evict(const hkv_config *cfg, const hkv_cache *cache, int layer, hkv_stream_t stream);
 
 /* hkv_evict for every layer in one launch (one CTA per head of the model):

@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(NT, kQuantUpdCtasPerSm)
     }
     for (int j = tid + NT; j < k; j += NT) pos[hole[j]] = u.ps[fill[j]];
   }
-  if (tid == 0) {
+  if (tid == 0 && M >= 0) {
     c.len[i] = len - M;
     c.nbuf[i] = 0;
   }

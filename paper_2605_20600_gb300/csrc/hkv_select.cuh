@@ -205,8 +205,9 @@ struct PlainRows {
 
 // Decides which rows of a segment the update evicts (Eqs. 2-6). On return
 // u.aux[r] is 1 for a kept row and 0 for an evicted one (r < len), u.ps
-// holds the rows' positions, and the number of evicted rows is returned.
-// Block-uniform. D, T: the queries' row; Rows: the format of the key rows.
+// holds the rows' positions, and the number of evicted rows is returned; or -1,
+// with HKV_ERR_TIMEOUT in the error word, where the queries did not arrive in
+// time: the head is then left as it is. Block-uniform. D, T: the queries' row; Rows: the format of the key rows.
 template <int D, typename T, class Rows>
 __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m,
                                 const unsigned char *qring, int ntok, const UpdSmem &u,
@@ -277,7 +278,10 @@ __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m
     HKV_UTRACE(2);
     // Eq. 6 scores: q-bar = the P buffered queries, oldest first; the sums keep
     // their order
-    if (!mbar_wait(&sh.ring_bar, 0) && tid == 0) set_err(sg.err, HKV_ERR_TIMEOUT);
+    bool arrived = mbar_wait(&sh.ring_bar, 0);
+#ifdef HKV_UPD_TEST_STALL  // one warp waits for a phase that nothing completes
+    if (arrived && tid >> 5 == (int)(blockIdx.x & 7)) arrived = mbar_wait(&sh.ring_bar, 1);
+#endif
     for (int d = tid; d < D; d += NT) {
       float acc = 0.f;
       int slot = (ntok - P) % P;
@@ -289,7 +293,11 @@ __device__ int select_evictions(const SegRef &sg, int label, const MethodArgs &m
       }
       u.qbar[d] = acc;
     }
-    __syncthreads();
+    if (!__syncthreads_and(arrived)) {
+      if (tid == 0) set_err(sg.err, HKV_ERR_TIMEOUT);
+      mbar_wait(&sh.ring_bar, 0);  // the copy gets the limit once more to end in
+      return -1;
+    }
     HKV_UTRACE(3);
     // Each warp stages 32 rows at a time in the (now free) ring area with
     // coalesced 16-byte async copies, laid out so that lane l reading row l,

@@ -117,7 +117,7 @@ __device__ int update_in_place(const SegRef &sg, int label, const MethodArgs &m,
                                const unsigned char *qring, int ntok, const UpdSmem &u,
                                UpdShared &sh) {
   const int M = select_evictions<D, T>(sg, label, m, qring, ntok, u, sh, PlainRows<D, T>{});
-  return fill_holes<D, T>(sg, M, u, sh);
+  return M < 0 ? -1 : fill_holes<D, T>(sg, M, u, sh);
 }
 
 template <int D, typename T>
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(NT, kUpdCtasPerSm)
   const int nl =
       update_in_place<D, T>(sg, lab, m, qring, c.ntok[i], carve(dyn, max_len, D, m.P, (int)sizeof(T)), sh);
   HKV_UTRACE(6);
-  if (tid == 0) {
+  if (tid == 0 && nl >= 0) {
     c.len[i] = nl;
     c.nbuf[i] = 0;
   }
@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(NT, kUpdCtasPerSm)
     }
     SegRef sg{K, V, pos, K, V, pos, len, cp, true, c.err};
     len = update_in_place<D, T>(sg, lab, m, qring, ntok, carve(dyn, max_len, D, m.P, (int)sizeof(T)), sh);
+    if (len < 0) return;
     nbuf = 0;
   }
   if (len >= cp) {
@@ -261,6 +262,7 @@ __global__ void __launch_bounds__(NT, kUpdCtasPerSm)
   const unsigned char *qring = static_cast<const unsigned char *>(dn.qbuf) + (size_t)i * m.P * RB;
   const UpdSmem u = carve(dyn, max_len, D, m.P, (int)sizeof(T));
   const int M = select_evictions<D, T>(sg, lab, m, qring, dn.ntok[i], u, sh, PlainRows<D, T>{});
+  if (M < 0) return;
   if (slen - M > dcap) {
     if (tid == 0) set_err(rg.err, HKV_ERR_CAPACITY);
     return;
