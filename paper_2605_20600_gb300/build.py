@@ -24,7 +24,8 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", 
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 SOURCES = ["hkv_api.cu", "hkv_attention.cu", "hkv_step.cu", "hkv_update.cu", "hkv_noalloc.cu",
-           "hkv_serve_api.cu", "hkv_quant.cu", "hkv_quant_attn.cu", "hkv_prefix.cu"]
+           "hkv_serve_api.cu", "hkv_quant.cu", "hkv_quant_attn.cu", "hkv_prefix.cu",
+           "hkv_prompt_api.cu", "hkv_rope.cu", "hkv_cross.cu"]
 
 
 def nvcc() -> str:
@@ -64,7 +65,7 @@ def build(force: bool = False, extra_flags=(), lib_path: str | None = None,
     os.makedirs(bdir, exist_ok=True)
     cc = nvcc()
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    headers += [os.path.join(ROOT, "include", h) for h in ("hkv.h", "hkv_serve.h")]
+    headers += [os.path.join(ROOT, "include", h) for h in ("hkv.h", "hkv_serve.h", "hkv_prompt.h")]
     objs, cmds = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

@@ -75,6 +75,25 @@ class QuantCacheBuffers:
                                capacity_tokens)
 
 
+class Heads:
+    """What a model does to queries and keys before the cache: rope, an
+    hkv_rope or None; norms, None or one hkv_norm per layer; positions, int32
+    [axes][sequences or 1][places] of every token, conditioning and image
+    (default: the places themselves, on every axis)."""
+
+    def __init__(self, cfg: H.hkv_config, *, rope=None, norms=None, positions=None, device="cuda"):
+        places = cfg.n_cond + cfg.n_image
+        if norms is not None and len(norms) != cfg.n_layers:
+            raise H.HkvError("heads", H.HKV_ERR_SHAPE)
+        if positions is None and rope is not None:
+            positions = torch.arange(places, dtype=torch.int32, device=device).expand(rope.n_axes, 1, places)
+        if positions is not None:
+            positions = positions.unsqueeze(0) if positions.dim() == 2 else positions
+            if positions.dim() != 3 or positions.shape[2] != places:
+                raise H.HkvError("heads", H.HKV_ERR_SHAPE)
+        self.rope, self.norms, self.positions = rope, norms, positions
+
+
 class Engine:
     """One batch of sequences through the HeadKV decode path."""
 
@@ -100,6 +119,18 @@ class Engine:
     @staticmethod
     def stream() -> int:
         return torch.cuda.current_stream().cuda_stream
+
+    # before the cache
+    def prepare(self, heads: Heads, layer: int, q, k, first: int) -> None:
+        """Norms and rotates, in place, the queries and keys of the places from
+        `first` on; q (or None) and k: [S][T][H][D], or [S][H][D] of one token,
+        of any strides whose last is 1."""
+        T = k.shape[1] if k.dim() == 4 else 1
+        pos = None if heads.positions is None else heads.positions[:, :, first:first + T]
+        rows = [None if x is None else H.make_rows(x) for x in (q, k)]
+        H.hkv_qk_norm_rope(self.cfg, None if heads.norms is None else heads.norms[layer], heads.rope,
+                           H.make_tokens(T, None, pos), rows[0], rows[1], None, rows[0], rows[1], None,
+                           self.stream())
 
     # Step 1
     def prefill(self, layer: int, kc, vc) -> None:

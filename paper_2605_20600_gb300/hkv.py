@@ -1,4 +1,5 @@
-"""ctypes binding of the HeadKV C-ABI (include/hkv.h, include/hkv_serve.h).
+"""ctypes binding of the HeadKV C-ABI (include/hkv.h, include/hkv_serve.h,
+include/hkv_prompt.h).
 
 Argument marshalling only: every function has the name of the C entry point
 it forwards to, accepts integers (device addresses) or objects with a
@@ -10,7 +11,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_double, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import (POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t,
+                    c_uint64, c_void_p)
 from fractions import Fraction
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -34,6 +36,11 @@ HKV_DIST_RASTER, HKV_DIST_GRID2D = 0, 1
 HKV_Q8, HKV_Q4 = 8, 4
 HKV_ALL_LAYERS = -1
 HKV_PACK_SKIP_COND = 1
+HKV_ROPE_HALF, HKV_ROPE_PAIRS = 0, 1
+HKV_ROPE_PLAIN, HKV_ROPE_LINEAR, HKV_ROPE_BASE, HKV_ROPE_PARTS = 0, 1, 2, 3
+HKV_ROPE_BACK = 1
+HKV_NORM_RMS, HKV_NORM_LAYER = 1, 2
+HKV_ATTN_CAUSAL = 1
 
 
 class hkv_config(Structure):
@@ -69,6 +76,56 @@ class hkv_prefix(Structure):
         ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
         ("group_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
         ("n_groups", c_int32), ("max_len", c_int32),
+    ]
+
+
+class hkv_rope_params(Structure):
+    _fields_ = [
+        ("head_dim", c_int32), ("rot_dim", c_int32), ("layout", c_int32), ("n_axes", c_int32),
+        ("section", c_int32 * 3), ("joint", c_int32), ("scaling", c_int32), ("reserved", c_int32),
+        ("base", c_double), ("factor", c_double), ("original", c_double), ("low", c_double),
+        ("high", c_double), ("amplitude", c_double),
+    ]
+
+
+class hkv_rope(Structure):
+    _fields_ = [
+        ("head_dim", c_int32), ("rot_dim", c_int32), ("layout", c_int32), ("n_axes", c_int32),
+        ("section", c_int32 * 3), ("amplitude", c_float), ("turns", c_uint64 * 64),
+    ]
+
+
+class hkv_rows(Structure):
+    of = None   # (sequences, tokens, head_dim) of the rows, where make_rows knows them
+    _fields_ = [
+        ("data", c_void_p), ("seq_stride", c_int64), ("token_stride", c_int64),
+        ("head_stride", c_int64), ("n_heads", c_int32), ("dtype", c_int32),
+    ]
+
+
+class hkv_tokens(Structure):
+    of = None   # (sequences or None, axes, rows of positions), where make_tokens knows them
+    _fields_ = [
+        ("n_tokens", c_int32), ("reserved", c_int32), ("len", c_void_p), ("pos", c_void_p),
+        ("pos_axis_stride", c_int64), ("pos_seq_stride", c_int64), ("err", c_void_p),
+    ]
+
+
+class hkv_norm(Structure):
+    of = None   # (dtype, head_dim, heads of q's and of k's weights or None), where make_norm knows them
+    _fields_ = [
+        ("kind", c_int32), ("eps", c_float), ("q_weight", c_void_p), ("q_bias", c_void_p),
+        ("k_weight", c_void_p), ("k_bias", c_void_p), ("q_head_stride", c_int64),
+        ("k_head_stride", c_int64),
+    ]
+
+
+class hkv_states(Structure):
+    of = None   # (dtype, sequences, head_dim) of the states, where make_states knows them
+    _fields_ = [
+        ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
+        ("seq_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
+        ("n_heads", c_int32), ("max_len", c_int32),
     ]
 
 
@@ -127,6 +184,16 @@ _SIGNATURES = {
     "hkv_prefix_workspace_size": ([POINTER(hkv_config), POINTER(hkv_prefix)], c_size_t),
     "hkv_prefix_attention": ([POINTER(hkv_config), POINTER(hkv_prefix), c_void_p, c_void_p, c_void_p,
                               c_void_p, c_size_t, c_void_p], c_int),
+    "hkv_make_rope": ([POINTER(hkv_rope_params), POINTER(hkv_rope)], c_int),
+    "hkv_rope_rotate": ([POINTER(hkv_config), POINTER(hkv_rope), POINTER(hkv_tokens), POINTER(hkv_rows),
+                         POINTER(hkv_rows), c_int, c_void_p], c_int),
+    "hkv_qk_norm_rope": ([POINTER(hkv_config), POINTER(hkv_norm), POINTER(hkv_rope), POINTER(hkv_tokens)]
+                         + [POINTER(hkv_rows)] * 6 + [c_void_p], c_int),
+    "hkv_cross_workspace_size": ([POINTER(hkv_config), POINTER(hkv_states), POINTER(hkv_tokens)],
+                                 c_size_t),
+    "hkv_cross_attention": ([POINTER(hkv_config), POINTER(hkv_states), POINTER(hkv_tokens),
+                             POINTER(hkv_rows), POINTER(hkv_rows), c_void_p, c_void_p, c_size_t, c_int,
+                             c_void_p], c_int),
 }
 
 
@@ -380,3 +447,161 @@ def hkv_prefix_attention(cfg, prefix, q, out, lse, workspace, ws_bytes, stream=0
         raise HkvError("prefix_attention", HKV_ERR_SHAPE)
     _call("prefix_attention", ctypes.byref(cfg), ctypes.byref(prefix), _p(q), _p(out), _p(lse),
           _p(workspace), ws_bytes, stream)
+
+
+# ---------------------------------------------------------------------------
+# around the cache: rotary positions, norms, attention over other states
+# (include/hkv_prompt.h)
+# ---------------------------------------------------------------------------
+_DTYPES = _PROMPT_DTYPES
+
+
+def hkv_make_rope(*, head_dim, rot_dim=None, layout=HKV_ROPE_HALF, sections=None, joint=False,
+                  base=10000.0, scaling=HKV_ROPE_PLAIN, factor=1.0, original=1.0, low=1.0, high=32.0,
+                  amplitude=1.0) -> hkv_rope:
+    """A rotation of the first rot_dim channels (default: all) of a head;
+    sections: the pairs of each axis (default: one axis)."""
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    sections = (rot_dim // 2,) if sections is None else tuple(sections)
+    if not 1 <= len(sections) <= 3:
+        raise HkvError("make_rope", HKV_ERR_SHAPE)
+    p = hkv_rope_params(head_dim, rot_dim, layout, len(sections), (c_int32 * 3)(*sections), int(joint),
+                        scaling, 0, base, factor, original, low, high, amplitude)
+    rope = hkv_rope()
+    _call("make_rope", ctypes.byref(p), ctypes.byref(rope))
+    return rope
+
+
+def make_rows(x) -> hkv_rows:
+    """hkv_rows over a tensor of [sequences][tokens][heads][head_dim], or
+    [sequences][heads][head_dim] for one token each, fp32 or bf16 (any strides
+    whose last is 1); keeps it alive. Calls of other sizes refuse it."""
+    y = x.unsqueeze(1) if x.dim() == 3 else x
+    dtype = _DTYPES.get(str(y.dtype))
+    if y.dim() != 4 or dtype is None or y.stride(3) != 1:
+        raise HkvError("make_rows", HKV_ERR_SHAPE)
+    r = hkv_rows(y.data_ptr(), y.stride(0), y.stride(1), y.stride(2), y.shape[2], dtype)
+    r.arrays = x
+    r.of = (y.shape[0], y.shape[1], y.shape[3])
+    return r
+
+
+def make_tokens(n_tokens, length=None, pos=None, err=None) -> hkv_tokens:
+    """hkv_tokens of n_tokens places a sequence; length: None, or contiguous
+    int32 [sequences]; pos: None, or int32 positions of [axes][sequences or
+    1][n_tokens] or [sequences or 1][n_tokens], the last stride 1."""
+    if length is not None and (str(length.dtype) != "torch.int32" or length.dim() != 1
+                               or not length.is_contiguous()):
+        raise HkvError("make_tokens", HKV_ERR_SHAPE)
+    strides, axes, rows = (0, 0), 0, None
+    if pos is not None:
+        p = pos.unsqueeze(0) if pos.dim() == 2 else pos
+        if p.dim() != 3 or str(p.dtype) != "torch.int32" or p.shape[2] != n_tokens or \
+                (n_tokens > 1 and p.stride(2) != 1):
+            raise HkvError("make_tokens", HKV_ERR_SHAPE)
+        axes, rows = p.shape[0], p.shape[1]
+        strides = (p.stride(0) if axes > 1 else 0, p.stride(1) if rows > 1 else 0)
+    if length is not None and pos is not None and length.device != pos.device:
+        raise HkvError("make_tokens", HKV_ERR_INVALID_ARG)
+    t = hkv_tokens(n_tokens, 0, _p(length), _p(pos), strides[0], strides[1], _p(err))
+    t.arrays = (length, pos, err)
+    t.of = (None if length is None else length.numel(), axes, rows)
+    return t
+
+
+def make_norm(kind, eps, q_weight=None, k_weight=None, q_bias=None, k_bias=None) -> hkv_norm:
+    """hkv_norm of weights and biases of [head_dim] or [heads][head_dim] in the
+    config dtype (any head stride; a weight and its bias alike); keeps them alive."""
+    given = [x for x in (q_weight, q_bias, k_weight, k_bias) if x is not None]
+    heads, strides = [], []
+    for pair in ((q_weight, q_bias), (k_weight, k_bias)):
+        have = [x for x in pair if x is not None]
+        if any(x.dim() not in (1, 2) or x.stride(-1) != 1 or str(x.dtype) not in _DTYPES for x in have) \
+                or len({(tuple(x.shape), x.stride() if x.dim() == 2 and x.shape[0] > 1 else 0)
+                        for x in have}) > 1:
+            raise HkvError("make_norm", HKV_ERR_SHAPE)
+        rows = [x for x in have if x.dim() == 2]
+        heads.append(rows[0].shape[0] if rows else None)
+        strides.append(rows[0].stride(0) if rows and rows[0].shape[0] > 1 else 0)
+    if len({(x.dtype, x.shape[-1]) for x in given}) > 1:
+        raise HkvError("make_norm", HKV_ERR_SHAPE)
+    n = hkv_norm(kind, eps, _p(q_weight), _p(q_bias), _p(k_weight), _p(k_bias), strides[0], strides[1])
+    n.arrays = given
+    if given:
+        n.of = (_DTYPES[str(given[0].dtype)], given[0].shape[-1], heads[0], heads[1])
+    return n
+
+
+def make_states(k, v, length=None, err=None) -> hkv_states:
+    """hkv_states from tensors k and v of [sequences][heads][states][head_dim],
+    fp32 or bf16 (any strides whose last is 1, the same in both), and the
+    sequences' numbers of states, contiguous int32, or None, all on one
+    device; keeps them alive. Calls of other sizes refuse it."""
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+        raise HkvError("make_states", HKV_ERR_SHAPE)
+    dtype = _DTYPES.get(str(k.dtype))
+    if dtype is None or v.dtype != k.dtype:
+        raise HkvError("make_states", HKV_ERR_SHAPE)
+    if length is not None and (length.numel() != k.shape[0] or str(length.dtype) != "torch.int32"
+                               or not length.is_contiguous()):
+        raise HkvError("make_states", HKV_ERR_SHAPE)
+    if k.device != v.device or (length is not None and length.device != k.device):
+        raise HkvError("make_states", HKV_ERR_INVALID_ARG)
+    s = hkv_states(k.data_ptr(), v.data_ptr(), _p(length), _p(err), k.stride(0), k.stride(1), k.stride(2),
+                   k.shape[1], k.shape[2])
+    s.arrays = (k, v, length, err)
+    s.of = (dtype, k.shape[0], k.shape[3])
+    return s
+
+
+def _fit(name, cfg, tokens, rope, *rows) -> None:
+    """Refuses views whose known sizes are not the call's."""
+    ok = all(r is None or r.of in (None, (cfg.n_seqs, tokens.n_tokens, cfg.head_dim)) for r in rows)
+    if tokens.of is not None:
+        seqs, axes, pos_rows = tokens.of
+        ok = ok and seqs in (None, cfg.n_seqs)
+        if rope is not None and tokens.pos:
+            ok = ok and axes >= rope.n_axes and pos_rows in (1, cfg.n_seqs)
+    if not ok:
+        raise HkvError(name, HKV_ERR_SHAPE)
+
+
+def _r(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def hkv_rope_rotate(cfg, rope, tokens, x, out, flags=0, stream=0) -> None:
+    _fit("rope_rotate", cfg, tokens, rope, x, out)
+    _call("rope_rotate", ctypes.byref(cfg), ctypes.byref(rope), ctypes.byref(tokens), ctypes.byref(x),
+          ctypes.byref(out), flags, stream)
+
+
+def hkv_qk_norm_rope(cfg, norm, rope, tokens, q, k, v, q_out, k_out, v_out, stream=0) -> None:
+    """norm and rope may be None, and pairs of q, k, v and their outs."""
+    _fit("qk_norm_rope", cfg, tokens, rope, q, k, v, q_out, k_out, v_out)
+    if norm is not None and norm.of is not None:
+        dtype, dim, q_heads, k_heads = norm.of
+        if (dtype, dim) != (cfg.dtype, cfg.head_dim) or (q and q_heads not in (None, q.n_heads)) \
+                or (k and k_heads not in (None, k.n_heads)):
+            raise HkvError("qk_norm_rope", HKV_ERR_SHAPE)
+    _call("qk_norm_rope", ctypes.byref(cfg), _r(norm), _r(rope), ctypes.byref(tokens), _r(q), _r(k), _r(v),
+          _r(q_out), _r(k_out), _r(v_out), stream)
+
+
+def _states_fit(cfg, states) -> bool:
+    return states.of in (None, (cfg.dtype, cfg.n_seqs, cfg.head_dim))
+
+
+def hkv_cross_workspace_size(cfg, states, tokens) -> int:
+    if not _states_fit(cfg, states):
+        return 0
+    return int(lib().hkv_cross_workspace_size(ctypes.byref(cfg), ctypes.byref(states),
+                                              ctypes.byref(tokens)))
+
+
+def hkv_cross_attention(cfg, states, tokens, q, out, lse, workspace, ws_bytes, flags=0, stream=0) -> None:
+    _fit("cross_attention", cfg, tokens, None, q, out)
+    if not _states_fit(cfg, states):
+        raise HkvError("cross_attention", HKV_ERR_SHAPE)
+    _call("cross_attention", ctypes.byref(cfg), ctypes.byref(states), ctypes.byref(tokens), ctypes.byref(q),
+          ctypes.byref(out), _p(lse), _p(workspace), ws_bytes, flags, stream)

@@ -10,13 +10,13 @@ from __future__ import annotations
 
 import torch
 
-from .engine import Engine, torch_dtype
+from .engine import Engine, Heads, torch_dtype
 
 
 def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=None,
              before_compress=None, fused: bool = True, first_step: int = 0,
              identify: str | None = None, cache_format: int | None = None,
-             shared_prompt: int = False) -> None:
+             shared_prompt: int = False, heads: Heads | None = None) -> None:
     """Runs image tokens first_step..last_step (default N-1) for every layer.
 
     fused: hkv_evict_all (every layer in one launch) when the update is due,
@@ -40,6 +40,9 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
     are then kept once for the run. Tokens that differ within a run raise
     ValueError: with guidance, the conditional and the unconditional sequences
     are two runs.
+    heads: what the model does to queries and keys between its projections and
+    the cache (norms and rotary positions); the provider's q, k and kc are then
+    the projections' outputs. None: they are ready for the cache.
     """
     if cache_format is not None and not fused:
         raise ValueError("a quantised cache needs the fused path")
@@ -69,6 +72,8 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
         vc = torch.empty_like(kc)
         for layer in range(L):
             provider.cond(kc, vc, layer, st)
+            if heads is not None:
+                engine.prepare(heads, layer, None, kc.transpose(1, 2), 0)
             if shared_prompt:
                 G = int(shared_prompt)
                 if layer == 0:
@@ -92,6 +97,8 @@ def generate(engine: Engine, provider, *, last_step: int | None = None, on_step=
         if fused and due:
             engine.evict_all()       # every layer's buffer fills at the same token
         for layer in range(L):
+            if heads is not None:
+                engine.prepare(heads, layer, q[layer], k[layer], C + t)
             if fused:
                 if t == E - 1 and identify == "fused":
                     engine.step_identify(layer, q[layer], k[layer], v[layer], out[layer])
