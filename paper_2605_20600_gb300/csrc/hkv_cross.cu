@@ -13,10 +13,8 @@
 // leaves nothing of them out, and two, off by 2^-18 of a weight, for bf16 outs,
 // whose own rounding is 2^-9. Sums are fp32; products chain in the tensor core
 // within a tile.
-#include "hkv_heads.h"
-#include "hkv_mma.cuh"
+#include "hkv_cross.cuh"
 #include "hkv_quant.cuh"
-#include "hkv_select.cuh"
 
 namespace hkv {
 namespace {
@@ -24,7 +22,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kKeys = 64;  // keys of a tile
-constexpr float kLn2 = 0.6931471805599453f;
 
 template <typename T>
 struct Planes {
@@ -46,12 +43,6 @@ struct CSmem {
   static constexpr int kTotal = kTiles + kQ;
   static_assert(kWarps * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
 };
-
-// Four neighbouring results to an output row.
-__device__ __forceinline__ void store4(float *to, float4 v) { *reinterpret_cast<float4 *>(to) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16 *to, float4 v) {
-  *reinterpret_cast<uint2 *>(to) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
-}
 
 // A piece of 8 elements of a row (zeros where `on` is false) into the planes at
 // dst. bf16: asynchronous.
@@ -83,60 +74,6 @@ __device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T
     const bool on = r < live;
     load_piece<T>(dst + at16<D>(r, c), plane, src + (on ? r * stride : 0) + c * 8, on);
   }
-}
-
-// what a CTA works on
-struct Work {
-  int s, kvh, tile, sp;   // sequence, key head, query tile, key range
-  int qlen, klen;         // 0 where a length is out of range
-  bool bad;               // the states' length is: NaN
-};
-__device__ __forceinline__ Work work_of(const CrossArgs &p) {
-  Work w;
-  int b = blockIdx.x;
-  w.tile = b % p.tiles;
-  b /= p.tiles;
-  w.kvh = b % p.kv;
-  b /= p.kv;
-  w.s = b % p.seqs;
-  w.sp = b / p.seqs;
-  w.qlen = p.qlen ? p.qlen[w.s] : p.tokens;
-  w.klen = p.klen ? p.klen[w.s] : p.keys;
-  w.bad = w.klen < 0 || w.klen > p.keys;
-  const bool first = threadIdx.x == 0 && w.tile == 0 && w.kvh == 0 && w.sp == 0;
-  if (w.bad) {
-    if (first) set_err(p.err, HKV_ERR_BOUNDS);
-    w.klen = 0;
-  }
-  if (w.qlen < 0 || w.qlen > p.tokens) {
-    if (first) set_err(p.qerr, HKV_ERR_BOUNDS);
-    w.qlen = 0;
-  }
-  return w;
-}
-// a query row of a (sequence, key head): which head of the group, which token
-struct Row {
-  int head, token;
-};
-__device__ __forceinline__ Row row_of(const CrossArgs &p, int kvh, int r) {
-  Row x;
-  const int g = r / p.tokens;
-  x.head = kvh * p.group + g;
-  x.token = r - g * p.tokens;
-  return x;
-}
-// keys that a query sees
-__device__ __forceinline__ int keys_seen(const CrossArgs &p, const Work &w, int token) {
-  if (token >= w.qlen) return 0;
-  return p.causal ? max(0, min(w.klen, w.klen - w.qlen + token + 1)) : w.klen;
-}
-// keys that any of the rows [r0, r1) sees
-__device__ __forceinline__ int keys_of_rows(const CrossArgs &p, const Work &w, int r0, int r1) {
-  if (w.qlen == 0 || r0 >= r1) return 0;
-  const int g0 = r0 / p.tokens, g1 = (r1 - 1) / p.tokens;
-  const int first = r0 - g0 * p.tokens, last = g0 == g1 ? r1 - 1 - g1 * p.tokens : w.qlen - 1;
-  if (g0 == g1 && first >= w.qlen) return 0;
-  return keys_seen(p, w, min(last, w.qlen - 1));
 }
 
 template <int D, typename T, typename O, int MW>
@@ -470,7 +407,8 @@ cudaError_t launch_rows(const CrossArgs &a, const CrossPlan &pl, cudaStream_t s)
   const long long grid = (long long)a.seqs * a.kv * a.tiles * a.splits;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   cudaError_t e;
-  if (pl.rows == 16) e = launch_tiles<D, T, O, 1>(a, (int)grid, s);
+  if (pl.rows >= 128) e = launch_cross_tc(a, pl, D, s);
+  else if (pl.rows == 16) e = launch_tiles<D, T, O, 1>(a, (int)grid, s);
   else if (pl.rows == 32) e = launch_tiles<D, T, O, 2>(a, (int)grid, s);
   else e = launch_tiles<D, T, O, 4>(a, (int)grid, s);
   if (e != cudaSuccess || a.splits == 1) return e;
@@ -488,13 +426,16 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   constexpr int kCtas = 304, kMostSplits = 304;
   CrossPlan pl;
   const long long all = (long long)(heads / kv) * tokens;
-  pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
+  const bool tc = dtype == HKV_BF16 && out_dtype == HKV_BF16 && all > 64;
+  if (tc) pl.rows = all > 128 ? 256 : 128;
+  else pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
+  const int tile = tc ? 128 : kKeys, ctas = pl.rows == 256 ? kCtas / 2 : kCtas;
   pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
-  const long long base = (long long)seqs * kv * pl.tiles, key_tiles = (keys + kKeys - 1) / kKeys;
-  long long want = base >= kCtas ? 1 : kCtas / base;
+  const long long base = (long long)seqs * kv * pl.tiles, key_tiles = (keys + tile - 1) / tile;
+  long long want = base >= ctas ? 1 : ctas / base;
   if (want > kMostSplits) want = kMostSplits;
   if (want > key_tiles) want = key_tiles;
-  pl.split_len = (int)(((keys + want - 1) / want + kKeys - 1) / kKeys * kKeys);
+  pl.split_len = (int)(((keys + want - 1) / want + tile - 1) / tile * tile);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
   pl.part_bytes =
       pl.splits > 1 ? (size_t)seqs * heads * tokens * pl.splits * (D + 4) * sizeof(float) : 0;

@@ -1,0 +1,363 @@
+// Attention of many bf16 queries over their sequence's states on tcgen05.
+//
+// A CTA takes TILES tiles of 128 query rows of one (sequence, key head) and a
+// range of keys in tiles of 128. One warp loads K and V tiles (TMA) into a ring
+// of slots, one issues the products, and four warps per query tile, a thread per
+// row, turn scores into weights: S = Q K^T lies in TMEM, a thread reads its row
+// of S, writes the weights as bf16 over it, and they are the A operand of
+// O += W V, which stays in TMEM. With two tiles the tensor core works on one
+// while the other's weights are made.
+//
+// A row's reference maximum moves (and O and its sum are rescaled) only when a
+// tile's maximum is more than 2^8 above it, so that weights stay below 2^8. The
+// weights are rounded to bf16, off by at most 2^-9 each, as the outs are; their
+// sum is that of the fp32 weights.
+//
+// Rows of V past the last state are set to zero in shared memory (a weight of
+// zero times what lies there could be NaN); scores past it are masked.
+#include <cuda.h>
+
+#include "hkv_cross.cuh"
+#include "hkv_tcgen05.cuh"
+
+namespace hkv {
+namespace {
+
+constexpr int kTile = 128;  // queries of a tile, and keys of one
+
+template <int D, int TILES>
+struct TcPlan {
+  static constexpr int kThreads = TILES * 128 + 64;
+  static constexpr int kQ = kTile * D * 2;          // bytes of a query tile, and of a K or V tile
+  static constexpr int kSlots = (TILES == 2 ? 4 : 2) * (D == 64 ? 2 : 1);
+  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * kQ;
+  static constexpr int kCols = TILES * 256;         // TMEM: S of each tile, then O of each
+};
+
+__device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int c, int row, int head,
+                                         int seq, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(c), "r"(row), "r"(head), "r"(seq), "r"(smem_u32(bar))
+      : "memory");
+}
+
+template <int D, int TILES>
+__global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
+    cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap kmap,
+                    const __grid_constant__ CUtensorMap vmap) {
+  using TP = TcPlan<D, TILES>;
+  constexpr int PF = D + 4, SLOTS = TP::kSlots;
+  extern __shared__ unsigned char dyn_raw[];
+  __shared__ uint64_t s_full[SLOTS], s_empty[SLOTS];  // slots of the ring
+  __shared__ uint64_t s_s[TILES], s_p[TILES];         // S is ready (and O holds what came before); W is
+  __shared__ uint64_t s_edge, s_drain;
+  __shared__ uint32_t s_tmem;
+  unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
+  unsigned char *ring = dyn + TILES * TP::kQ;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < SLOTS; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_empty[i], 1);
+    }
+    for (int t = 0; t < TILES; ++t) {
+      mbar_init(&s_s[t], 1);
+      mbar_init(&s_p[t], 128);
+    }
+    mbar_init(&s_edge, 1);
+    mbar_init(&s_drain, 1);
+    fence_barrier_init();
+  }
+  // TMEM only after the wait, and the next kernel's CTAs only after TMEM: an
+  // allocation waits for columns, so a CTA that held some while it waited for
+  // the kernel before, or let a CTA of the kernel after take them first, could
+  // wait for one that waits for it
+  pdl_wait();
+  if (warp == 0) {
+    tmem_alloc(&s_tmem, TP::kCols);
+    pdl_launch_dependents();
+  }
+  const Work w = work_of(p);
+  const int all = p.group * p.tokens;
+  const int r0 = w.tile * TILES * kTile;
+  const int lo = w.sp * p.split_len;
+  int n[TILES], most = 0;  // key tiles of each query tile
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int hi = min(keys_of_rows(p, w, r0 + t * kTile, min(all, r0 + (t + 1) * kTile)),
+                       lo + p.split_len);
+    n[t] = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    most = max(most, n[t]);
+  }
+  if (most > 0 && warp < TILES * 4) {
+    for (int e = tid; e < TILES * kTile * (D / 8); e += TILES * 128) {
+      const int r = e / (D / 8), c = e % (D / 8), rr = r & (kTile - 1);
+      const Row x = row_of(p, w.kvh, min(r0 + r, all - 1));
+      const bool on = r0 + r < all && x.token < w.qlen;
+      cp_async16_zfill(dyn + (r / kTile) * TP::kQ + (c >> 3) * kTile * 128 + rr * 128 +
+                           (((c & 7) ^ (rr & 7)) << 4),
+                       static_cast<const __nv_bfloat16 *>(p.q) + w.s * p.qs +
+                           (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on);
+    }
+    cp_async_wait_all();
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  bool ok = true;
+  int issued = 0;  // loads (the load warp), for the wait of a failed CTA
+  if (warp == TILES * 4) {
+    // loads: K of tile 0, V of tile 0, K of tile 1, ...
+    for (int j = 0; j < 2 * most && ok; ++j) {
+      const int slot = j % SLOTS, k0 = lo + (j >> 1) * kTile, past = k0 + kTile - w.klen;
+      if (j >= SLOTS) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_empty[slot], (j / SLOTS - 1) & 1));
+      if (!ok) break;
+      unsigned char *dst = ring + slot * TP::kQ;
+      const bool edge = (j & 1) && past > 0;
+      if (lane == 0) {
+        uint64_t *bar = edge ? &s_edge : &s_full[slot];
+        mbar_arrive_expect_tx(bar, TP::kQ);
+#pragma unroll
+        for (int c = 0; c < D; c += 64)
+          tma_tile(dst + (c >> 6) * kTile * 128, (j & 1) ? &vmap : &kmap, c, k0, w.kvh, w.s, bar);
+      }
+      ++issued;
+      if (edge) {  // at most one tile of a sequence: its last
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_edge, 0));
+        if (!ok) break;
+        for (int e = lane; e < past * (D / 8); e += 32) {
+          const int r = kTile - past + e / (D / 8), c = e % (D / 8);
+          *reinterpret_cast<uint4 *>(dst + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
+              make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_full[slot]);
+      }
+    }
+  } else if (warp == TILES * 4 + 1) {
+    if (lane == 0) {
+      auto scores = [&](int t, int j) {  // S of tile t with the K tile in load j's slot
+        const uint32_t kb = smem_u32(ring + (j % SLOTS) * TP::kQ), qb = smem_u32(dyn + t * TP::kQ);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
+          tc_mma(tmem + t * 128, tc_desc(qb + (ks >> 2) * kTile * 128 + (ks & 3) * 32, 16),
+                 tc_desc(kb + (ks >> 2) * kTile * 128 + (ks & 3) * 32, 16),
+                 tc_instr(kTile, kTile, false), ks > 0);
+        tc_commit(&s_s[t]);
+      };
+      if (most > 0) {
+        ok = mbar_wait(&s_full[0], 0);
+        if (ok) {
+          tc_fence_after();
+          for (int t = 0; t < TILES; ++t)
+            if (n[t] > 0) scores(t, 0);
+          tc_commit(&s_empty[0]);
+        }
+      }
+      for (int i = 0; i < most && ok; ++i) {
+        const int jv = 2 * i + 1, jk = 2 * i + 2;
+        ok = mbar_wait(&s_full[jv % SLOTS], (jv / SLOTS) & 1);
+        if (ok && i + 1 < most) ok = mbar_wait(&s_full[jk % SLOTS], (jk / SLOTS) & 1);
+        const uint32_t vb = smem_u32(ring + (jv % SLOTS) * TP::kQ);
+        for (int t = 0; t < TILES && ok; ++t) {
+          if (i >= n[t]) continue;
+          ok = mbar_wait(&s_p[t], i & 1);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + kk * 8,
+                      tc_desc(vb + kk * 16 * 128, kTile * 128), tc_instr(kTile, D, true),
+                      i > 0 || kk > 0);
+          if (i + 1 < n[t]) scores(t, jk);  // over the weights, after the products that read them
+          else tc_commit(&s_s[t]);
+        }
+        if (ok) {
+          tc_commit(&s_empty[jv % SLOTS]);
+          if (i + 1 < most) tc_commit(&s_empty[jk % SLOTS]);
+        }
+      }
+    }
+  } else {
+    const int t = warp >> 2;
+    const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t mine_o = mine + TILES * 128;
+    const int r = r0 + tid;
+    Row x = {};
+    int seen = 0;
+    if (r < all) {
+      x = row_of(p, w.kvh, r);
+      seen = keys_seen(p, w, x.token);
+    }
+    seen = min(seen, lo + p.split_len);
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < n[t]; ++i) {
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[t], i & 1));
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(s[c], mine + c * 32);
+      tmem_wait_ld();
+      const int left = seen - lo - i * kTile;  // keys of the tile that count
+      if (left < kTile) {
+#pragma unroll
+        for (int j = 0; j < kTile; ++j)
+          if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kTile; ++j) mx = fmaxf(mx, __uint_as_float(s[j >> 5][j & 31]));
+      mx *= p.qscale;
+      float f = 1.f;
+      if (mx > m + 8.f) {
+        f = ex2_approx(m - mx);  // (zero for the first keys)
+        m = mx;
+        l *= f;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;  // no key yet: weights of zero
+      if (i > 0 && __any_sync(0xFFFFFFFFu, f != 1.f)) {
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(o, mine_o + c);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+          tmem_st32(mine_o + c, o);
+        }
+      }
+      float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const int a = c * 64 + 2 * j;
+          const float w0 = ex2_approx(fmaf(__uint_as_float(s[a >> 5][a & 31]), p.qscale, -ref));
+          const float w1 = ex2_approx(fmaf(__uint_as_float(s[a >> 5][(a & 31) + 1]), p.qscale, -ref));
+          l0 += w0;
+          l1 += w1;
+          v[j] = pack2(w0, w1);
+        }
+        tmem_st32(mine + c * 32, v);
+      }
+      l += l0 + l1;
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(&s_p[t]);
+    }
+    // O is complete
+    if (ok && n[t] > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[t], n[t] & 1));
+    tc_fence_after();
+    const bool wrong = w.bad || !ok, any = n[t] > 0 && ok, live = r < all && x.token < w.qlen;
+    const size_t row = ((size_t)w.s * p.heads + x.head) * p.tokens + x.token;
+    const float inv = p.splits > 1 ? 1.f : wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
+    float *part = p.part + (row * p.splits + w.sp) * PF;
+    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(p.out) + w.s * p.os + x.token * p.ot + x.head * p.oh;
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+      uint32_t o[32] = {};
+      if (any) {
+        tmem_ld32(o, mine_o + c);
+        tmem_wait_ld();
+      }
+      if (!live) continue;
+      if (p.splits > 1) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<uint4 *>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          uint32_t v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            v[k] = pack2(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+          *reinterpret_cast<uint4 *>(to + c + e) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      }
+    }
+    if (live) {
+      if (p.splits > 1)
+        *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
+      else if (p.lse)
+        p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    }
+  }
+  tc_fence_before();
+  const bool failed = __syncthreads_or(!ok);
+  tc_fence_after();
+  if (failed) {
+    // copies and products that were issued may still run: they get the limit
+    // once more before their place and the TMEM are given back
+    if (warp == TILES * 4 + 1 && lane == 0) {
+      set_err(p.err, HKV_ERR_TIMEOUT);
+      tc_commit(&s_drain);
+    }
+    if (warp == TILES * 4)
+      for (int j = max(0, issued - SLOTS); j < issued; ++j)
+        mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1);
+    mbar_wait(&s_drain, 0);
+    __syncthreads();
+  }
+  if (warp == 0) tmem_free(tmem, TP::kCols);
+}
+
+// K or V as a tensor of [sequences][heads][states][D], read in tiles of 128
+// rows and 64 channels (128 bytes, 128-byte swizzle); rows past the last are zero
+cudaError_t encode(CUtensorMap *map, const void *base, const CrossArgs &a, int D) {
+  using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                              const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+  static std::atomic<Encode> known{nullptr};
+  Encode f = known.load(std::memory_order_acquire);
+  if (!f) {
+    void *at = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e =
+        cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &at, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return e;
+    if (found != cudaDriverEntryPointSuccess || !at) return cudaErrorNotSupported;
+    f = reinterpret_cast<Encode>(at);
+    known.store(f, std::memory_order_release);
+  }
+  const auto stride = [&](long long s, int count) { return (cuuint64_t)(count > 1 ? s : D) * 2; };
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)a.keys, (cuuint64_t)a.kv, (cuuint64_t)a.seqs};
+  const cuuint64_t strides[3] = {stride(a.kt, a.keys), stride(a.kh, a.kv), stride(a.ks, a.seqs)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)kTile, 1, 1}, step[4] = {1, 1, 1, 1};
+  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides,
+                       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D, int TILES>
+cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
+  using TP = TcPlan<D, TILES>;
+  static std::atomic<uint64_t> ready{0};
+  cudaError_t e = allow_smem_of(cross_tc_kernel<D, TILES>, TP::kBytes, ready);
+  CUtensorMap k, v;
+  if (e == cudaSuccess) e = encode(&k, a.k, a, D);
+  if (e == cudaSuccess) e = encode(&v, a.v, a, D);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, k, v);
+}
+
+}  // namespace
+
+cudaError_t launch_cross_tc(const CrossArgs &a, const CrossPlan &plan, int D, cudaStream_t s) {
+  const long long grid = (long long)a.seqs * a.kv * a.tiles * a.splits;
+  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  if (plan.rows == 256)
+    return D == 64 ? launch<64, 2>(a, (int)grid, s) : launch<128, 2>(a, (int)grid, s);
+  return D == 64 ? launch<64, 1>(a, (int)grid, s) : launch<128, 1>(a, (int)grid, s);
+}
+
+}  // namespace hkv

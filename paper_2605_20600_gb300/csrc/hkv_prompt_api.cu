@@ -23,7 +23,7 @@ template <int N>
 bool strides_ok(const Axis (&axes)[N], int head_dim, int dtype) {
   const int64_t unit = 16 / elem_size(dtype);
   for (const Axis &a : axes)
-    if (a.n > 1 && (a.stride < head_dim || a.stride % unit != 0 || a.stride > (1ll << 40)))
+    if (a.n > 1 && (a.stride < head_dim || a.stride % unit != 0 || a.stride >= (1ll << 38)))
       return false;
   return true;
 }
