@@ -427,7 +427,11 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   CrossPlan pl;
   const long long all = (long long)(heads / kv) * tokens;
   const bool tc = dtype == HKV_BF16 && out_dtype == HKV_BF16 && all > 64;
+#ifdef HKV_TC_ROWS
+  if (tc) pl.rows = HKV_TC_ROWS;
+#else
   if (tc) pl.rows = all > 128 ? 256 : 128;
+#endif
   else pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
   const int tile = tc ? 128 : kKeys, ctas = pl.rows == 256 ? kCtas / 2 : kCtas;
   pl.tiles = (int)((all + pl.rows - 1) / pl.rows);

@@ -29,8 +29,10 @@ template <int D, int TILES>
 struct TcPlan {
   static constexpr int kThreads = TILES * 128 + 64;
   static constexpr int kQ = kTile * D * 2;          // bytes of a query tile, and of a K or V tile
-  static constexpr int kSlots = (TILES == 2 ? 4 : 2) * (D == 64 ? 2 : 1);
-  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * kQ;
+  // slots of the ring: slot p % kSlots holds K of key tile p and V of tile p - 1,
+  // which the products need together
+  static constexpr int kSlots = TILES * (D == 64 ? 2 : 1);
+  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kQ;
   static constexpr int kCols = TILES * 256;         // TMEM: S of each tile, then O of each
 };
 
@@ -42,6 +44,28 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
       "l"(map), "r"(c), "r"(row), "r"(head), "r"(seq), "r"(smem_u32(bar))
       : "memory");
 }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// pairs of fp32 in one operation each
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  return (uint64_t)lo | ((uint64_t)hi << 32);
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float low(uint64_t a) { return __uint_as_float((uint32_t)a); }
+__device__ __forceinline__ float high(uint64_t a) { return __uint_as_float((uint32_t)(a >> 32)); }
 
 template <int D, int TILES>
 __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
@@ -56,7 +80,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
   unsigned char *ring = dyn + TILES * TP::kQ;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) {
       mbar_init(&s_full[i], 1);
@@ -64,7 +89,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     }
     for (int t = 0; t < TILES; ++t) {
       mbar_init(&s_s[t], 1);
-      mbar_init(&s_p[t], 128);
+      mbar_init(&s_p[t], 4);
     }
     mbar_init(&s_edge, 1);
     mbar_init(&s_drain, 1);
@@ -107,31 +132,33 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem, 0);
   bool ok = true;
+  float row_m = -INFINITY, row_l = 0.f;
   int issued = 0;  // loads (the load warp), for the wait of a failed CTA
   if (warp == TILES * 4) {
-    // loads: K of tile 0, V of tile 0, K of tile 1, ...
-    for (int j = 0; j < 2 * most && ok; ++j) {
-      const int slot = j % SLOTS, k0 = lo + (j >> 1) * kTile, past = k0 + kTile - w.klen;
+    for (int j = 0; most > 0 && j <= most && ok; ++j) {
+      const int slot = j % SLOTS, k0 = lo + j * kTile, past = k0 - w.klen;
       if (j >= SLOTS) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_empty[slot], (j / SLOTS - 1) & 1));
       if (!ok) break;
-      unsigned char *dst = ring + slot * TP::kQ;
-      const bool edge = (j & 1) && past > 0;
+      unsigned char *dst = ring + slot * 2 * TP::kQ;
+      const bool edge = past > 0;  // V's tile is the sequence's last, and not a whole one
       if (lane == 0) {
         uint64_t *bar = edge ? &s_edge : &s_full[slot];
-        mbar_arrive_expect_tx(bar, TP::kQ);
+        mbar_arrive_expect_tx(bar, ((j < most) + (j > 0)) * TP::kQ);
 #pragma unroll
-        for (int c = 0; c < D; c += 64)
-          tma_tile(dst + (c >> 6) * kTile * 128, (j & 1) ? &vmap : &kmap, c, k0, w.kvh, w.s, bar);
+        for (int c = 0; c < D; c += 64) {
+          if (j < most) tma_tile(dst + (c >> 6) * kTile * 128, &kmap, c, k0, w.kvh, w.s, bar);
+          if (j > 0) tma_tile(dst + TP::kQ + (c >> 6) * kTile * 128, &vmap, c, k0 - kTile, w.kvh, w.s, bar);
+        }
       }
       ++issued;
-      if (edge) {  // at most one tile of a sequence: its last
+      if (edge) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_edge, 0));
         if (!ok) break;
         for (int e = lane; e < past * (D / 8); e += 32) {
           const int r = kTile - past + e / (D / 8), c = e % (D / 8);
-          *reinterpret_cast<uint4 *>(dst + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
+          *reinterpret_cast<uint4 *>(dst + TP::kQ + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
               make_uint4(0, 0, 0, 0);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -139,61 +166,66 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         if (lane == 0) mbar_arrive(&s_full[slot]);
       }
     }
-  } else if (warp == TILES * 4 + 1) {
-    if (lane == 0) {
-      auto scores = [&](int t, int j) {  // S of tile t with the K tile in load j's slot
-        const uint32_t kb = smem_u32(ring + (j % SLOTS) * TP::kQ), qb = smem_u32(dyn + t * TP::kQ);
+  } else if (warp > TILES * 4) {
+    // products, issued by one lane; the whole warp waits. The tiles take turns,
+    // one's weights are made during the other's products.
+    const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(dyn);
+    auto here = [&](int j) {  // slot j is filled
+      return __all_sync(0xFFFFFFFFu, mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1));
+    };
+    auto scores = [&](int t, int j) {  // S of tile t with the K tile of slot j
+      const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kQ, 16);
+      const uint64_t qd = tc_desc(q_at + t * TP::kQ, 16);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
-          tc_mma(tmem + t * 128, tc_desc(qb + (ks >> 2) * kTile * 128 + (ks & 3) * 32, 16),
-                 tc_desc(kb + (ks >> 2) * kTile * 128 + (ks & 3) * 32, 16),
-                 tc_instr(kTile, kTile, false), ks > 0);
-        tc_commit(&s_s[t]);
-      };
-      if (most > 0) {
-        ok = mbar_wait(&s_full[0], 0);
-        if (ok) {
-          tc_fence_after();
+      for (int ks = 0; ks < D / 16; ++ks) {  // 16 channels: 32 bytes of a column block
+        const uint64_t at = ((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4;
+        tc_mma(tmem + t * 128, qd + at, kd + at, tc_instr(kTile, kTile, false), ks > 0);
+      }
+      tc_commit(&s_s[t]);
+    };
+    if (most > 0) {
+      ok = here(0);
+      if (ok) {
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
           for (int t = 0; t < TILES; ++t)
             if (n[t] > 0) scores(t, 0);
           tc_commit(&s_empty[0]);
         }
+        __syncwarp();
+        ok = here(1);
       }
-      for (int i = 0; i < most && ok; ++i) {
-        const int jv = 2 * i + 1, jk = 2 * i + 2;
-        ok = mbar_wait(&s_full[jv % SLOTS], (jv / SLOTS) & 1);
-        if (ok && i + 1 < most) ok = mbar_wait(&s_full[jk % SLOTS], (jk / SLOTS) & 1);
-        const uint32_t vb = smem_u32(ring + (jv % SLOTS) * TP::kQ);
-        for (int t = 0; t < TILES && ok; ++t) {
-          if (i >= n[t]) continue;
-          ok = mbar_wait(&s_p[t], i & 1);
-          if (!ok) break;
-          tc_fence_after();
+    }
+    for (int i = 0; i < most && ok; ++i) {
 #pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)
-            tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + kk * 8,
-                      tc_desc(vb + kk * 16 * 128, kTile * 128), tc_instr(kTile, D, true),
-                      i > 0 || kk > 0);
-          if (i + 1 < n[t]) scores(t, jk);  // over the weights, after the products that read them
-          else tc_commit(&s_s[t]);
+      for (int t = 0; t < TILES; ++t) {
+        const bool mine = i < n[t];
+        if (mine) ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(&s_p[t], i & 1));
+        if (!ok) continue;
+        tc_fence_after();
+        if (elect_one()) {
+          if (mine) {
+            const uint64_t vd = tc_desc(ring_at + ((i + 1) % SLOTS) * 2 * TP::kQ + TP::kQ, kTile * 128);
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+              tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (16 * 128 >> 4),
+                        tc_instr(kTile, D, true), i > 0 || kk > 0);
+            if (i + 1 < n[t]) scores(t, i + 1);  // over the weights, after the products that read them
+            else tc_commit(&s_s[t]);
+          }
+          if (t == TILES - 1) tc_commit(&s_empty[(i + 1) % SLOTS]);
         }
-        if (ok) {
-          tc_commit(&s_empty[jv % SLOTS]);
-          if (i + 1 < most) tc_commit(&s_empty[jk % SLOTS]);
-        }
+        __syncwarp();
       }
+      if (ok && i + 1 < most) ok = here(i + 2);
     }
   } else {
     const int t = warp >> 2;
     const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t mine_o = mine + TILES * 128;
     const int r = r0 + tid;
-    Row x = {};
-    int seen = 0;
-    if (r < all) {
-      x = row_of(p, w.kvh, r);
-      seen = keys_seen(p, w, x.token);
-    }
+    int seen = r < all ? keys_seen(p, w, row_of(p, w.kvh, r).token) : 0;
     seen = min(seen, lo + p.split_len);
     float m = -INFINITY, l = 0.f;
     for (int i = 0; i < n[t]; ++i) {
@@ -210,9 +242,14 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         for (int j = 0; j < kTile; ++j)
           if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
       }
-      float mx = -INFINITY;
+      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int j = 0; j < kTile; ++j) mx = fmaxf(mx, __uint_as_float(s[j >> 5][j & 31]));
+      for (int j = 0; j < kTile; j += 8)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
+                        __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
+      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
       mx *= p.qscale;
       float f = 1.f;
       if (mx > m + 8.f) {
@@ -232,30 +269,43 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           tmem_st32(mine_o + c, o);
         }
       }
-      float l0 = 0.f, l1 = 0.f;
+      const uint64_t scale2 = pair_of(__float_as_uint(p.qscale), __float_as_uint(p.qscale));
+      const uint64_t ref2 = pair_of(__float_as_uint(-ref), __float_as_uint(-ref));
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t v[32];
+      for (int c = 0; c < 4; ++c) {
+        uint32_t v[16];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const int a = c * 64 + 2 * j;
-          const float w0 = ex2_approx(fmaf(__uint_as_float(s[a >> 5][a & 31]), p.qscale, -ref));
-          const float w1 = ex2_approx(fmaf(__uint_as_float(s[a >> 5][(a & 31) + 1]), p.qscale, -ref));
-          l0 += w0;
-          l1 += w1;
+        for (int j = 0; j < 16; ++j) {
+          const uint64_t e = fma2(pair_of(s[c][2 * j], s[c][2 * j + 1]), scale2, ref2);
+          const float w0 = ex2_approx(low(e)), w1 = ex2_approx(high(e));
+          sum[j & 1] = add2(sum[j & 1], pair_of(__float_as_uint(w0), __float_as_uint(w1)));
           v[j] = pack2(w0, w1);
         }
-        tmem_st32(mine + c * 32, v);
+        tmem_st16(mine + c * 16, v);
       }
-      l += l0 + l1;
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(&s_p[t]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_p[t]);
+      sum[0] = add2(sum[0], sum[1]);
+      l += low(sum[0]) + high(sum[0]);
     }
     // O is complete
     if (ok && n[t] > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[t], n[t] & 1));
-    tc_fence_after();
-    const bool wrong = w.bad || !ok, any = n[t] > 0 && ok, live = r < all && x.token < w.qlen;
+    row_m = m;
+    row_l = l;
+  }
+  // one wait that ran out fails the whole CTA
+  const bool failed = __syncthreads_or(!ok);
+  tc_fence_after();
+  if (warp < TILES * 4) {
+    const int t = warp >> 2, r = r0 + tid;
+    const uint32_t mine_o = tmem + (TILES + t) * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+    const float m = row_m, l = row_l;
+    Row x = {};
+    if (r < all) x = row_of(p, w.kvh, r);
+    const bool wrong = w.bad || failed, any = n[t] > 0 && !failed, live = r < all && x.token < w.qlen;
     const size_t row = ((size_t)w.s * p.heads + x.head) * p.tokens + x.token;
     const float inv = p.splits > 1 ? 1.f : wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
     float *part = p.part + (row * p.splits + w.sp) * PF;
@@ -291,12 +341,12 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     }
   }
   tc_fence_before();
-  const bool failed = __syncthreads_or(!ok);
+  __syncthreads();
   tc_fence_after();
   if (failed) {
     // copies and products that were issued may still run: they get the limit
     // once more before their place and the TMEM are given back
-    if (warp == TILES * 4 + 1 && lane == 0) {
+    if (warp > TILES * 4 && elect_one()) {
       set_err(p.err, HKV_ERR_TIMEOUT);
       tc_commit(&s_drain);
     }
