@@ -434,7 +434,19 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
 #endif
   else pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
   const int tile = tc ? 128 : kKeys, ctas = pl.rows == 256 ? kCtas / 2 : kCtas;
-  pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
+  // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as
+  // many heads of a group as fit 128 rows
+  const int group = heads / kv;
+  pl.box_tokens = tokens < 128 ? tokens : 128;
+  pl.box_heads = 128 / pl.box_tokens < group ? 128 / pl.box_tokens : group;
+  if (tc) {
+    const long long units = (long long)((group + pl.box_heads - 1) / pl.box_heads) *
+                            ((tokens + pl.box_tokens - 1) / pl.box_tokens);
+    if (units == 1) pl.rows = 128;
+    pl.tiles = (int)((units + pl.rows / 128 - 1) / (pl.rows / 128));
+  } else {
+    pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
+  }
   const long long base = (long long)seqs * kv * pl.tiles, key_tiles = (keys + tile - 1) / tile;
   long long want = base >= ctas ? 1 : ctas / base;
   if (want > kMostSplits) want = kMostSplits;

@@ -1,8 +1,9 @@
 // Attention of many bf16 queries over their sequence's states on tcgen05.
 //
-// A CTA takes TILES tiles of 128 query rows of one (sequence, key head) and a
-// range of keys in tiles of 128. One warp loads K and V tiles (TMA) into a ring
-// of slots, one issues the products, and four warps per query tile, a thread per
+// A CTA takes TILES query tiles of one (sequence, key head) and a range of keys
+// in tiles of 128. A query tile is 128 tokens of a head, or all tokens of a few
+// heads of the group, 128 rows at most. One warp loads Q, and K and V tiles into a ring
+// of slots (TMA), one issues the products, and four warps per query tile, a thread per
 // row, turn scores into weights: S = Q K^T lies in TMEM, a thread reads its row
 // of S, writes the weights as bf16 over it, and they are the A operand of
 // O += W V, which stays in TMEM. With two tiles the tensor core works on one
@@ -69,14 +70,15 @@ __device__ __forceinline__ float high(uint64_t a) { return __uint_as_float((uint
 
 template <int D, int TILES>
 __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
-    cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap kmap,
+    cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap qmap,
+                    const __grid_constant__ CUtensorMap kmap,
                     const __grid_constant__ CUtensorMap vmap) {
   using TP = TcPlan<D, TILES>;
   constexpr int PF = D + 4, SLOTS = TP::kSlots;
   extern __shared__ unsigned char dyn_raw[];
   __shared__ uint64_t s_full[SLOTS], s_empty[SLOTS];  // slots of the ring
   __shared__ uint64_t s_s[TILES], s_p[TILES];         // S is ready (and O holds what came before); W is
-  __shared__ uint64_t s_edge, s_drain;
+  __shared__ uint64_t s_q[TILES], s_edge, s_drain;
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
   unsigned char *ring = dyn + TILES * TP::kQ;
@@ -90,6 +92,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     for (int t = 0; t < TILES; ++t) {
       mbar_init(&s_s[t], 1);
       mbar_init(&s_p[t], 4);
+      mbar_init(&s_q[t], 1);
     }
     mbar_init(&s_edge, 1);
     mbar_init(&s_drain, 1);
@@ -105,29 +108,20 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     pdl_launch_dependents();
   }
   const Work w = work_of(p);
-  const int all = p.group * p.tokens;
-  const int r0 = w.tile * TILES * kTile;
   const int lo = w.sp * p.split_len;
-  int n[TILES], most = 0;  // key tiles of each query tile
+  const int token_tiles = (p.tokens + p.box_tokens - 1) / p.box_tokens;
+  int head0[TILES], token0[TILES];  // of the query tiles, heads within the group
+  int n[TILES], most = 0;           // their key tiles
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
-    const int hi = min(keys_of_rows(p, w, r0 + t * kTile, min(all, r0 + (t + 1) * kTile)),
-                       lo + p.split_len);
+    const int u = w.tile * TILES + t;
+    head0[t] = u / token_tiles * p.box_heads;
+    token0[t] = u % token_tiles * p.box_tokens;
+    int hi = 0;
+    if (head0[t] < p.group && token0[t] < w.qlen)
+      hi = min(keys_seen(p, w, min(token0[t] + p.box_tokens, w.qlen) - 1), lo + p.split_len);
     n[t] = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
     most = max(most, n[t]);
-  }
-  if (most > 0 && warp < TILES * 4) {
-    for (int e = tid; e < TILES * kTile * (D / 8); e += TILES * 128) {
-      const int r = e / (D / 8), c = e % (D / 8), rr = r & (kTile - 1);
-      const Row x = row_of(p, w.kvh, min(r0 + r, all - 1));
-      const bool on = r0 + r < all && x.token < w.qlen;
-      cp_async16_zfill(dyn + (r / kTile) * TP::kQ + (c >> 3) * kTile * 128 + rr * 128 +
-                           (((c & 7) ^ (rr & 7)) << 4),
-                       static_cast<const __nv_bfloat16 *>(p.q) + w.s * p.qs +
-                           (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on);
-    }
-    cp_async_wait_all();
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -137,6 +131,17 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   float row_m = -INFINITY, row_l = 0.f;
   int issued = 0;  // loads (the load warp), for the wait of a failed CTA
   if (warp == TILES * 4) {
+    if (lane == 0) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        if (n[t] == 0) continue;
+        mbar_arrive_expect_tx(&s_q[t], p.box_tokens * p.box_heads * D * 2);
+#pragma unroll
+        for (int c = 0; c < D; c += 64)
+          tma_tile(dyn + t * TP::kQ + (c >> 6) * kTile * 128, &qmap, c, token0[t],
+                   w.kvh * p.group + head0[t], w.s, &s_q[t]);
+      }
+    }
     for (int j = 0; most > 0 && j <= most && ok; ++j) {
       const int slot = j % SLOTS, k0 = lo + j * kTile, past = k0 - w.klen;
       if (j >= SLOTS) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_empty[slot], (j / SLOTS - 1) & 1));
@@ -185,6 +190,9 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     };
     if (most > 0) {
       ok = here(0);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+        if (ok && n[t] > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_q[t], 0));
       if (ok) {
         tc_fence_after();
         if (elect_one()) {
@@ -224,8 +232,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     const int t = warp >> 2;
     const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t mine_o = mine + TILES * 128;
-    const int r = r0 + tid;
-    int seen = r < all ? keys_seen(p, w, row_of(p, w.kvh, r).token) : 0;
+    int seen = keys_seen(p, w, token0[t] + (tid & 127) % p.box_tokens);
     seen = min(seen, lo + p.split_len);
     float m = -INFINITY, l = 0.f;
     for (int i = 0; i < n[t]; ++i) {
@@ -298,70 +305,93 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   }
   // one wait that ran out fails the whole CTA
   const bool failed = __syncthreads_or(!ok);
+  if (failed) {
+    // copies and products that were issued may still run: they get the limit
+    // once more before their place and the TMEM are used again
+    if (warp > TILES * 4 && elect_one()) {
+      set_err(p.err, HKV_ERR_TIMEOUT);
+      tc_commit(&s_drain);
+    }
+    if (warp == TILES * 4) {
+      for (int t = 0; t < TILES; ++t)
+        if (n[t] > 0) mbar_wait(&s_q[t], 0);
+      for (int j = max(0, issued - SLOTS); j < issued; ++j)
+        mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1);
+    }
+    mbar_wait(&s_drain, 0);
+    __syncthreads();
+  }
   tc_fence_after();
   if (warp < TILES * 4) {
-    const int t = warp >> 2, r = r0 + tid;
+    const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens;
     const uint32_t mine_o = tmem + (TILES + t) * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const float m = row_m, l = row_l;
-    Row x = {};
-    if (r < all) x = row_of(p, w.kvh, r);
-    const bool wrong = w.bad || failed, any = n[t] > 0 && !failed, live = r < all && x.token < w.qlen;
-    const size_t row = ((size_t)w.s * p.heads + x.head) * p.tokens + x.token;
-    const float inv = p.splits > 1 ? 1.f : wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
-    float *part = p.part + (row * p.splits + w.sp) * PF;
-    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(p.out) + w.s * p.os + x.token * p.ot + x.head * p.oh;
+    const int token = token0[t] + r - h * p.box_tokens, head = w.kvh * p.group + head0[t] + h;
+    const bool live = h < p.box_heads && head0[t] + h < p.group && token < w.qlen;
+    const bool wrong = w.bad || failed, any = n[t] > 0 && !failed;
+    const size_t row = ((size_t)w.s * p.heads + head) * p.tokens + token;
+    if (p.splits > 1) {
+      float *part = p.part + (row * p.splits + w.sp) * PF;
 #pragma unroll 1
-    for (int c = 0; c < D; c += 32) {
-      uint32_t o[32] = {};
-      if (any) {
-        tmem_ld32(o, mine_o + c);
-        tmem_wait_ld();
-      }
-      if (!live) continue;
-      if (p.splits > 1) {
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32] = {};
+        if (any) {
+          tmem_ld32(o, mine_o + c);
+          tmem_wait_ld();
+        }
+        if (!live) continue;
 #pragma unroll
         for (int e = 0; e < 32; e += 4)
           *reinterpret_cast<uint4 *>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-      } else {
+      }
+      if (live) *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
+    } else {
+      // rows to shared memory, in the place of Q's, then whole rows out
+      const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
+      unsigned char *rows = dyn + t * TP::kQ + (warp & 3) * 32 * D * 2;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32] = {};
+        if (any) {
+          tmem_ld32(o, mine_o + c);
+          tmem_wait_ld();
+        }
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint32_t v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             v[k] = pack2(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-          *reinterpret_cast<uint4 *>(to + c + e) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4 *>(rows + at16<D>(lane, (c + e) >> 3)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
-    }
-    if (live) {
-      if (p.splits > 1)
-        *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
-      else if (p.lse)
-        p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      __syncwarp();
+      __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(p.out) + w.s * p.os + token * p.ot + head * p.oh;
+      constexpr int PPR = D / 8, RPP = 32 / PPR;  // pieces a row, rows a pass
+#pragma unroll 4
+      for (int i = 0; i < 32; i += RPP) {
+        const int rr = i + lane / PPR;
+        const bool on = __shfl_sync(0xFFFFFFFFu, live, rr);
+        __nv_bfloat16 *at = reinterpret_cast<__nv_bfloat16 *>(
+            __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), rr));
+        if (on)
+          *reinterpret_cast<uint4 *>(at + (lane % PPR) * 8) =
+              *reinterpret_cast<const uint4 *>(rows + at16<D>(rr, lane % PPR));
+      }
+      if (live && p.lse) p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (failed) {
-    // copies and products that were issued may still run: they get the limit
-    // once more before their place and the TMEM are given back
-    if (warp > TILES * 4 && elect_one()) {
-      set_err(p.err, HKV_ERR_TIMEOUT);
-      tc_commit(&s_drain);
-    }
-    if (warp == TILES * 4)
-      for (int j = max(0, issued - SLOTS); j < issued; ++j)
-        mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1);
-    mbar_wait(&s_drain, 0);
-    __syncthreads();
-  }
   if (warp == 0) tmem_free(tmem, TP::kCols);
 }
 
-// K or V as a tensor of [sequences][heads][states][D], read in tiles of 128
-// rows and 64 channels (128 bytes, 128-byte swizzle); rows past the last are zero
-cudaError_t encode(CUtensorMap *map, const void *base, const CrossArgs &a, int D) {
+// Rows as a tensor of [sequences][heads][tokens][D], read in boxes of 64
+// channels (128 bytes, 128-byte swizzle); rows past the last are zero
+cudaError_t encode(CUtensorMap *map, const void *base, int D, int tokens, long long token_stride,
+                   int heads, long long head_stride, int seqs, long long seq_stride, int box_tokens,
+                   int box_heads) {
   using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                               const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
                               CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -379,9 +409,11 @@ cudaError_t encode(CUtensorMap *map, const void *base, const CrossArgs &a, int D
     known.store(f, std::memory_order_release);
   }
   const auto stride = [&](long long s, int count) { return (cuuint64_t)(count > 1 ? s : D) * 2; };
-  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)a.keys, (cuuint64_t)a.kv, (cuuint64_t)a.seqs};
-  const cuuint64_t strides[3] = {stride(a.kt, a.keys), stride(a.kh, a.kv), stride(a.ks, a.seqs)};
-  const cuuint32_t box[4] = {64, (cuuint32_t)kTile, 1, 1}, step[4] = {1, 1, 1, 1};
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)seqs};
+  const cuuint64_t strides[3] = {stride(token_stride, tokens), stride(head_stride, heads),
+                                 stride(seq_stride, seqs)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, (cuuint32_t)box_heads, 1};
+  const cuuint32_t step[4] = {1, 1, 1, 1};
   const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides,
                        box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -393,11 +425,13 @@ cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
   using TP = TcPlan<D, TILES>;
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = allow_smem_of(cross_tc_kernel<D, TILES>, TP::kBytes, ready);
-  CUtensorMap k, v;
-  if (e == cudaSuccess) e = encode(&k, a.k, a, D);
-  if (e == cudaSuccess) e = encode(&v, a.v, a, D);
+  CUtensorMap q, k, v;
+  if (e == cudaSuccess)
+    e = encode(&q, a.q, D, a.tokens, a.qt, a.heads, a.qh, a.seqs, a.qs, a.box_tokens, a.box_heads);
+  if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kTile, 1);
+  if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kTile, 1);
   if (e != cudaSuccess) return e;
-  return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, k, v);
+  return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v);
 }
 
 }  // namespace

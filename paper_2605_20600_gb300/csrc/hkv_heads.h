@@ -50,6 +50,7 @@ struct CrossArgs {
   int tokens, keys;                   // most of a sequence
   int causal;
   int splits, split_len, tiles;       // key ranges; query tiles of a key head
+  int box_tokens, box_heads;          // a query tile of the tcgen05 kernel
   float *part;                        // [rows of (sequence, head, token)][splits][D + 4]
   float qscale;                       // log2(e) / sqrt(D)
 };
@@ -57,6 +58,7 @@ struct CrossArgs {
 struct CrossPlan {
   int rows;                           // queries of a CTA (256, 128: the tcgen05 kernel)
   int splits, split_len, tiles;
+  int box_tokens, box_heads;
   size_t part_bytes;
 };
 CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, int dtype,

@@ -301,6 +301,8 @@ hkv_status hkv_cross_attention(const hkv_config *cfg, const hkv_states *states,
   a.splits = pl.splits;
   a.split_len = pl.split_len;
   a.tiles = pl.tiles;
+  a.box_tokens = pl.box_tokens;
+  a.box_heads = pl.box_heads;
   a.part = static_cast<float *>(workspace);
   a.qscale = (float)(1.4426950408889634 / sqrt((double)cfg->head_dim));
   return cuda_status(
