@@ -51,23 +51,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// pairs of fp32 in one operation each
-__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
-  return (uint64_t)lo | ((uint64_t)hi << 32);
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ float low(uint64_t a) { return __uint_as_float((uint32_t)a); }
-__device__ __forceinline__ float high(uint64_t a) { return __uint_as_float((uint32_t)(a >> 32)); }
-
 template <int D, int TILES>
 __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
     cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap qmap,
@@ -276,8 +259,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           tmem_st32(mine_o + c, o);
         }
       }
-      const uint64_t scale2 = pair_of(__float_as_uint(p.qscale), __float_as_uint(p.qscale));
-      const uint64_t ref2 = pair_of(__float_as_uint(-ref), __float_as_uint(-ref));
+      const uint64_t scale2 = pair_of(p.qscale, p.qscale);
+      const uint64_t ref2 = pair_of(-ref, -ref);
       uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -286,7 +269,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         for (int j = 0; j < 16; ++j) {
           const uint64_t e = fma2(pair_of(s[c][2 * j], s[c][2 * j + 1]), scale2, ref2);
           const float w0 = ex2_approx(low(e)), w1 = ex2_approx(high(e));
-          sum[j & 1] = add2(sum[j & 1], pair_of(__float_as_uint(w0), __float_as_uint(w1)));
+          sum[j & 1] = add2(sum[j & 1], pair_of(w0, w1));
           v[j] = pack2(w0, w1);
         }
         tmem_st16(mine + c * 16, v);

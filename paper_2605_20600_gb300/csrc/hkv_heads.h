@@ -19,9 +19,11 @@ struct HeadSet {
   long long wh;                       // head stride of weight and bias
   int heads;
   int norm, rotate;                   // whether the set is normed and rotated
+  int first_block;                    // blocks of the set, and how they share its
+  int per, tokens, chunks;            // rows (launch_heads fills these in)
 };
 
-// The sets q, k, v of a call (those that it has), all heads of a token in a row.
+// The sets q, k, v of a call (those that it has).
 struct HeadsArgs {
   HeadSet set[3];
   int sets, heads;                    // sets in use, heads of all of them

@@ -6,14 +6,16 @@
 // integers, p times f_i / 2 pi in units of 2^-64, so that no position loses
 // digits, and its high word, a signed fraction of a turn, goes to sincospif.
 //
-// heads_kernel: a thread holds two 16-byte pieces of a row, chosen so that both
-// channels of each of its pairs are its own (half layout: a piece and the one
-// rot_dim / 2 further; interleaved: two neighbours); rows are then rotated
-// without an exchange, and in place. Norms sum over the G threads of a row with
-// shuffles. A thread keeps the cosines and sines of its pairs for a few heads
-// of the same token, so that the angles cost a fraction of the copies.
+// heads_kernel: a block works on one of q, k and v; a thread holds two pieces of
+// 4 channels of a row, chosen so that both channels of each of its pairs are its
+// own (half layout: a piece and the one rot_dim / 2 further; interleaved: two
+// neighbours); rows are then rotated without an exchange, and in place. Norms
+// sum over the D / 8 threads of a row with shuffles. A thread keeps the cosines
+// and sines of its pairs, and weights that all heads share, for several heads of
+// the same token, so that the angles cost a fraction of the copies, and loads a
+// few rows ahead of the first one's arithmetic.
 // heads_any_kernel takes half layouts whose pieces do not fall together
-// (rot_dim / 2 not a multiple of a piece): a warp per row, through shared memory.
+// (rot_dim / 2 not a multiple of 4): a warp per row, through shared memory.
 #include <cuda_bf16.h>
 
 #include "hkv_device.cuh"
@@ -36,33 +38,32 @@ __device__ __forceinline__ void turn(const HeadsArgs &a, int pair, const int (&p
   s *= a.sign;  // (holds the amplitude)
 }
 
-__device__ __forceinline__ const HeadSet &set_of(const HeadsArgs &a, int &head) {
-  int i = 0;
-  if (i + 1 < a.sets && head >= a.set[0].heads) head -= a.set[i++].heads;
-  if (i == 1 && a.sets > 2 && head >= a.set[1].heads) head -= a.set[i++].heads;
-  return a.set[i];
-}
-
+// a piece of 4 neighbouring channels as two pairs, and back
 template <typename T>
 struct Piece;
 template <>
 struct Piece<float> {
-  static constexpr int kN = 4;
-  __device__ static __forceinline__ uint4 pack(const float *f) {
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
-                      __float_as_uint(f[3]));
+  using Raw = uint4;
+  __device__ static __forceinline__ void unpack(const uint4 &u, uint64_t (&f)[2]) {
+    f[0] = pair_of(u.x, u.y), f[1] = pair_of(u.z, u.w);
+  }
+  __device__ static __forceinline__ uint4 pack(const uint64_t (&f)[2]) {
+    return make_uint4((uint32_t)f[0], (uint32_t)(f[0] >> 32), (uint32_t)f[1], (uint32_t)(f[1] >> 32));
   }
   __device__ static __forceinline__ void store1(void *p, float f) { *static_cast<float *>(p) = f; }
 };
 template <>
 struct Piece<__nv_bfloat16> {
-  static constexpr int kN = 8;
-  __device__ static __forceinline__ uint32_t two(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  using Raw = uint2;
+  __device__ static __forceinline__ void unpack(const uint2 &u, uint64_t (&f)[2]) {
+    f[0] = pair_of(u.x << 16, u.x & 0xFFFF0000u), f[1] = pair_of(u.y << 16, u.y & 0xFFFF0000u);
+  }
+  __device__ static __forceinline__ uint32_t two(uint64_t a) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(low(a), high(a));
     return *reinterpret_cast<const uint32_t *>(&h);
   }
-  __device__ static __forceinline__ uint4 pack(const float *f) {
-    return make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7]));
+  __device__ static __forceinline__ uint2 pack(const uint64_t (&f)[2]) {
+    return make_uint2(two(f[0]), two(f[1]));
   }
   __device__ static __forceinline__ void store1(void *p, float f) {
     *static_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(f);
@@ -80,133 +81,152 @@ __device__ __forceinline__ int tokens_of(const HeadsArgs &a, int s) {
 
 // NORM: 0 none, else HKV_NORM_*. A block's threads are row slots of G: `per`
 // slots for each of its tokens, which take heads first, first + per, ...
-template <typename T, int D, int NORM>
-__global__ void __launch_bounds__(kHeadThreads)
-    heads_kernel(const __grid_constant__ HeadsArgs a, int per, int tokens_per_block, int chunks,
-                 long long places) {
-  constexpr int N = Piece<T>::kN, G = D / (2 * N), U = 2;
+template <typename T, int D, int NORM, bool PAIRS>
+__global__ void __launch_bounds__(kHeadThreads, 4)
+    heads_kernel(const __grid_constant__ HeadsArgs a, long long places) {
+  constexpr int N = 4, G = D / (2 * N), U = 4;
+  using P = Piece<T>;
+  using Raw = typename P::Raw;
   pdl_wait();
   pdl_launch_dependents();
+  const int i = (a.sets > 1 && blockIdx.x >= a.set[1].first_block) +
+                (a.sets > 2 && blockIdx.x >= a.set[2].first_block);
+  const HeadSet &x = a.set[i];
+  const int block = blockIdx.x - x.first_block;
   const int g = threadIdx.x % G, slot = threadIdx.x / G;
-  const int tok = slot / per, first = slot % per;
-  const int chunk = blockIdx.x % chunks;
-  const long long place = (long long)(blockIdx.x / chunks) * tokens_per_block + tok;
-  bool on = tok < tokens_per_block && place < places;
+  const int tok = slot / x.per, first = slot % x.per;
+  const int chunk = block % x.chunks;
+  const long long place = (long long)(block / x.chunks) * x.tokens + tok;
+  bool on = tok < x.tokens && place < places;
   const int s = on ? (int)(place / a.tokens) : 0, t = on ? (int)(place % a.tokens) : 0;
   if (on) on = t < tokens_of(a, s);
   // (whole groups of G lanes, a power of two, are on or off together)
-  const int R = a.rope.rot_dim;
-  // the thread's two pieces
-  const bool pairs = a.rope.layout == HKV_ROPE_PAIRS;
-  const bool apart = !pairs && N * g < R / 2;  // the other channels two by two behind R
-  const int ca = apart ? N * g : 2 * N * g, cb = apart ? ca + R / 2 : ca + N;
-  const int heads_here = (a.heads + chunks - 1) / chunks;
-  const int h1 = min(a.heads, (chunk + 1) * heads_here);
-  float c[N], sn[N];
-  bool have = false;
-  for (int hb = chunk * heads_here; hb < h1; hb += U * per) {  // the same for all lanes
-    const int h0 = hb + first;
-    uint4 ra[U], rb[U];
-    if (on) {
+  const int R = x.rotate ? a.rope.rot_dim : 0;
+  // the thread's two pieces; the channels behind R of a half layout two by two
+  const bool apart = !PAIRS && N * g < R / 2;
+  const int ca = apart ? N * g : 2 * N * g, step = apart ? R / 2 : N;
+  const int heads_here = (x.heads + x.chunks - 1) / x.chunks;
+  const int h1 = min(x.heads, (chunk + 1) * heads_here);
+  const int hfirst = chunk * heads_here + first;
+  const T *in = static_cast<const T *>(x.in) + s * x.is + t * x.it + hfirst * x.ih + ca;
+  T *out = static_cast<T *>(x.out) + s * x.os + t * x.ot + hfirst * x.oh + ca;
+  const long long in_step = x.per * x.ih, out_step = x.per * x.oh;
+  const int rows = on ? (h1 - hfirst + x.per - 1) / x.per : 0;   // of this thread (may be below 0)
+  const int most = (heads_here + x.per - 1) / x.per;             // of any in the block
+  // cosines and sines; half layout: of the pairs of channels 2 i, 2 i + 1 of the
+  // two pieces; interleaved: of the pairs themselves, the first piece's first
+  uint64_t c[2], sn[2], wa[2], wb[2], ba[2], bb[2];
+  const bool shared = NORM != 0 && x.wh == 0;
+  for (int r0 = 0; r0 < most; r0 += U) {
+    Raw ra[U], rb[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        int h = h0 + u * per;
-        if (h < h1) {
-          const HeadSet &x = set_of(a, h);
-          const T *row = static_cast<const T *>(x.in) + s * x.is + t * x.it + h * x.ih;
-          ra[u] = *reinterpret_cast<const uint4 *>(row + ca);
-          rb[u] = *reinterpret_cast<const uint4 *>(row + cb);
-        }
+    for (int u = 0; u < U; ++u)
+      if (r0 + u < rows) {
+        ra[u] = *reinterpret_cast<const Raw *>(in + (r0 + u) * in_step);
+        rb[u] = *reinterpret_cast<const Raw *>(in + (r0 + u) * in_step + step);
       }
-    }
-    if (on && !have && R > 0) {
-      have = true;
-      int pos[3];
+    if (r0 == 0) {
+      if (shared && x.weight) {
+        const T *w = static_cast<const T *>(x.weight) + ca;
+        P::unpack(*reinterpret_cast<const Raw *>(w), wa);
+        P::unpack(*reinterpret_cast<const Raw *>(w + step), wb);
+      }
+      if (shared && x.bias) {
+        const T *b = static_cast<const T *>(x.bias) + ca;
+        P::unpack(*reinterpret_cast<const Raw *>(b), ba);
+        P::unpack(*reinterpret_cast<const Raw *>(b + step), bb);
+      }
+      if (rows > 0 && R > 0) {
+        int pos[3];
 #pragma unroll
-      for (int x = 0; x < 3; ++x)
-        pos[x] = x < a.rope.n_axes ? a.pos[x * a.pa + s * a.ps + t] : 0;
+        for (int k = 0; k < 3; ++k)
+          pos[k] = k < a.rope.n_axes ? a.pos[k * a.pa + s * a.ps + t] : 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        // half layout: pair of (a[i], b[i]); interleaved: of neighbours, a's then b's
-        const int pair = pairs ? N * g + i : ca + i;
-        c[i] = 1.f, sn[i] = 0.f;
-        if (pair < R / 2) turn(a, pair, pos, c[i], sn[i]);
+        for (int k = 0; k < 2; ++k) {
+          float cc[2] = {1.f, 1.f}, ss[2] = {0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int pair = PAIRS ? N * g + 2 * k + e : ca + 2 * k + e;
+            if (pair < R / 2) turn(a, pair, pos, cc[e], ss[e]);
+          }
+          c[k] = pair_of(cc[0], cc[1]);
+          sn[k] = pair_of(ss[0], ss[1]);
+        }
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      int h = h0 + u * per;
-      const bool live = on && h < h1;
-      const HeadSet &x = set_of(a, h);
-      float va[N], vb[N];
-      if (live) {
-        Elem<T>::unpack(ra[u], va);
-        Elem<T>::unpack(rb[u], vb);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) va[i] = vb[i] = 0.f;
+      if (r0 + u >= most) break;
+      const bool live = r0 + u < rows;
+      if ((NORM == 0 || !x.norm) && R == 0) {  // a copy
+        if (live) {
+          *reinterpret_cast<Raw *>(out + (r0 + u) * out_step) = ra[u];
+          *reinterpret_cast<Raw *>(out + (r0 + u) * out_step + step) = rb[u];
+        }
+        continue;
       }
-      if (NORM != 0) {  // every lane takes part in the shuffles
-        float mean = 0.f, sum = 0.f;
+      uint64_t va[2], vb[2];
+      P::unpack(ra[u], va);
+      P::unpack(rb[u], vb);
+      if (NORM != 0 && x.norm) {  // every lane takes part in the shuffles
         if (NORM == HKV_NORM_LAYER) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) mean += va[i] + vb[i];
+          const uint64_t both = add2(add2(va[0], va[1]), add2(vb[0], vb[1]));
+          float mean = low(both) + high(both);
 #pragma unroll
           for (int o = G / 2; o >= 1; o >>= 1) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, o);
-          mean *= 1.f / D;
-        }
+          mean *= -1.f / D;
+          const uint64_t less = pair_of(mean, mean);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float da = va[i] - mean, db = vb[i] - mean;
-          sum += da * da + db * db;
+          for (int k = 0; k < 2; ++k) va[k] = add2(va[k], less), vb[k] = add2(vb[k], less);
         }
+        const uint64_t squares =
+            fma2(vb[1], vb[1], fma2(vb[0], vb[0], fma2(va[1], va[1], mul2(va[0], va[0]))));
+        float sum = low(squares) + high(squares);
 #pragma unroll
         for (int o = G / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        if (live && x.norm) {
-          const float inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
-          float w[N], b[N];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float *v = half ? vb : va;
-            const int at = half ? cb : ca;
-            if (x.weight)
-              Elem<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(x.weight) +
-                                                               h * x.wh + at), w);
-            if (NORM == HKV_NORM_LAYER && x.bias)
-              Elem<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(x.bias) +
-                                                               h * x.wh + at), b);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              v[i] = (v[i] - mean) * inv;
-              if (x.weight) v[i] *= w[i];
-              if (NORM == HKV_NORM_LAYER && x.bias) v[i] += b[i];
-            }
+        const float inv = rsqrtf(sum * (1.f / D) + a.eps);
+        const uint64_t by = pair_of(inv, inv);
+        if (!shared && live) {  // the head's own
+          const long long h = hfirst + (r0 + u) * x.per;
+          if (x.weight) {
+            const T *w = static_cast<const T *>(x.weight) + h * x.wh + ca;
+            P::unpack(*reinterpret_cast<const Raw *>(w), wa);
+            P::unpack(*reinterpret_cast<const Raw *>(w + step), wb);
           }
+          if (NORM == HKV_NORM_LAYER && x.bias) {
+            const T *b = static_cast<const T *>(x.bias) + h * x.wh + ca;
+            P::unpack(*reinterpret_cast<const Raw *>(b), ba);
+            P::unpack(*reinterpret_cast<const Raw *>(b + step), bb);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          va[k] = mul2(va[k], by), vb[k] = mul2(vb[k], by);
+          if (x.weight) va[k] = mul2(va[k], wa[k]), vb[k] = mul2(vb[k], wb[k]);
+          if (NORM == HKV_NORM_LAYER && x.bias) va[k] = add2(va[k], ba[k]), vb[k] = add2(vb[k], bb[k]);
         }
       }
       if (!live) continue;
-      if (x.rotate) {
-        if (pairs) {
+      if (PAIRS) {
+        if (R > 0) {
 #pragma unroll
-          for (int i = 0; i < N / 2; ++i) {
-            const float x0 = va[2 * i], y0 = va[2 * i + 1], x1 = vb[2 * i], y1 = vb[2 * i + 1];
-            va[2 * i] = x0 * c[i] - y0 * sn[i];
-            va[2 * i + 1] = x0 * sn[i] + y0 * c[i];
-            vb[2 * i] = x1 * c[N / 2 + i] - y1 * sn[N / 2 + i];
-            vb[2 * i + 1] = x1 * sn[N / 2 + i] + y1 * c[N / 2 + i];
-          }
-        } else if (apart) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float x0 = va[i], y0 = vb[i];
-            va[i] = x0 * c[i] - y0 * sn[i];
-            vb[i] = x0 * sn[i] + y0 * c[i];
+          for (int k = 0; k < 4; ++k) {  // pairs (x, y): c x - s y, s x + c y
+            uint64_t &v = k < 2 ? va[k & 1] : vb[k & 1];
+            const float cc = k & 1 ? high(c[k / 2]) : low(c[k / 2]);
+            const float ss = k & 1 ? high(sn[k / 2]) : low(sn[k / 2]);
+            v = pair_of(low(v) * cc - high(v) * ss, low(v) * ss + high(v) * cc);
           }
         }
+      } else if (apart) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint64_t x0 = va[k], y0 = vb[k];
+          va[k] = fma2(x0, c[k], mul2(y0, sn[k] ^ 0x8000000080000000ull));
+          vb[k] = fma2(x0, sn[k], mul2(y0, c[k]));
+        }
       }
-      T *row = static_cast<T *>(x.out) + s * x.os + t * x.ot + h * x.oh;
-      *reinterpret_cast<uint4 *>(row + ca) = Piece<T>::pack(va);
-      *reinterpret_cast<uint4 *>(row + cb) = Piece<T>::pack(vb);
+      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step) = P::pack(va);
+      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step + step) = P::pack(vb);
     }
   }
 }
@@ -226,7 +246,9 @@ __global__ void __launch_bounds__(kHeadThreads)
   const long long place = r / a.heads;
   const int s = (int)(place / a.tokens), t = (int)(place % a.tokens);
   if (t >= tokens_of(a, s)) return;
-  const HeadSet &x = set_of(a, h);
+  int i = 0;
+  while (i + 1 < a.sets && h >= a.set[i].heads) h -= a.set[i++].heads;
+  const HeadSet &x = a.set[i];
   const T *in = static_cast<const T *>(x.in) + s * x.is + t * x.it + h * x.ih;
   float v[E];
 #pragma unroll
@@ -244,7 +266,7 @@ __global__ void __launch_bounds__(kHeadThreads)
     for (int e = 0; e < E; ++e) sum += (v[e] - mean) * (v[e] - mean);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    const float inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+    const float inv = rsqrtf(sum * (1.f / D) + a.eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       v[e] = (v[e] - mean) * inv;
@@ -276,28 +298,35 @@ __global__ void __launch_bounds__(kHeadThreads)
 }
 
 template <typename T, int D, int NORM>
-cudaError_t launch(const HeadsArgs &a, cudaStream_t s) {
-  constexpr int N = Piece<T>::kN, kSlots = kHeadThreads / (D / (2 * N));
+cudaError_t launch(HeadsArgs a, cudaStream_t s) {
+  constexpr int kSlots = kHeadThreads / (D / 8);
   const long long places = (long long)a.seqs * a.tokens;
-  if (a.rope.layout == HKV_ROPE_HALF && a.rope.rot_dim / 2 % N != 0) {
+  if (a.rope.layout == HKV_ROPE_HALF && a.rope.rot_dim / 2 % 4 != 0) {
     constexpr int kRows = kHeadThreads / 32;
     const long long rows = places * a.heads, grid = (rows + kRows - 1) / kRows;
     if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
     return pdl_launch(heads_any_kernel<T, D, NORM>, (int)grid, kHeadThreads, 0, s, a, rows);
   }
+  // several heads a thread as soon as the device is full
   int iters = 8;
   while (iters > 1 && places * a.heads < 608LL * kSlots * iters) iters >>= 1;
-  int per = (a.heads + iters - 1) / iters;
-  int chunks = 1;
-  if (per > kSlots) {
-    chunks = (a.heads + kSlots * iters - 1) / (kSlots * iters);
-    per = kSlots;
+  long long grid = 0;
+  for (int i = 0; i < a.sets; ++i) {
+    HeadSet &x = a.set[i];
+    x.per = (x.heads + iters - 1) / iters;
+    x.chunks = 1;
+    if (x.per > kSlots) {
+      x.chunks = (x.heads + kSlots * iters - 1) / (kSlots * iters);
+      x.per = kSlots;
+    }
+    x.tokens = kSlots / x.per;
+    x.first_block = (int)grid;
+    grid += (places + x.tokens - 1) / x.tokens * x.chunks;
+    if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   }
-  const int tpb = kSlots / per;
-  const long long grid = (places + tpb - 1) / tpb * chunks;
-  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
-  return pdl_launch(heads_kernel<T, D, NORM>, (int)grid, kHeadThreads, 0, s, a, per, tpb, chunks,
-                    places);
+  return pdl_launch(a.rope.layout == HKV_ROPE_PAIRS ? heads_kernel<T, D, NORM, true>
+                                                    : heads_kernel<T, D, NORM, false>,
+                    (int)grid, kHeadThreads, 0, s, a, places);
 }
 
 template <typename T, int D>
