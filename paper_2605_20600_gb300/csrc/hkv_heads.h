@@ -20,7 +20,8 @@ struct HeadSet {
   int heads;
   int norm, rotate;                   // whether the set is normed and rotated
   int first_block;                    // blocks of the set, and how they share its
-  int per, tokens, chunks;            // rows (launch_heads fills these in)
+  int per, tokens, chunks;            // rows (launch_heads fills these in):
+  int chunk, most;                    // heads of a chunk, and rows of a thread
 };
 
 // The sets q, k, v of a call (those that it has).

@@ -82,37 +82,37 @@ __device__ __forceinline__ int tokens_of(const HeadsArgs &a, int s) {
 // NORM: 0 none, else HKV_NORM_*. A block's threads are row slots of G: `per`
 // slots for each of its tokens, which take heads first, first + per, ...
 template <typename T, int D, int NORM, bool PAIRS>
-__global__ void __launch_bounds__(kHeadThreads, 4)
-    heads_kernel(const __grid_constant__ HeadsArgs a, long long places) {
+__global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
+    heads_kernel(const __grid_constant__ HeadsArgs a, uint32_t places) {
   constexpr int N = 4, G = D / (2 * N), U = 4;
   using P = Piece<T>;
   using Raw = typename P::Raw;
   pdl_wait();
   pdl_launch_dependents();
-  const int i = (a.sets > 1 && blockIdx.x >= a.set[1].first_block) +
-                (a.sets > 2 && blockIdx.x >= a.set[2].first_block);
+  const int i = (a.sets > 1 && (int)blockIdx.x >= a.set[1].first_block) +
+                (a.sets > 2 && (int)blockIdx.x >= a.set[2].first_block);
   const HeadSet &x = a.set[i];
-  const int block = blockIdx.x - x.first_block;
-  const int g = threadIdx.x % G, slot = threadIdx.x / G;
-  const int tok = slot / x.per, first = slot % x.per;
-  const int chunk = block % x.chunks;
-  const long long place = (long long)(block / x.chunks) * x.tokens + tok;
-  bool on = tok < x.tokens && place < places;
-  const int s = on ? (int)(place / a.tokens) : 0, t = on ? (int)(place % a.tokens) : 0;
+  const uint32_t block = blockIdx.x - x.first_block;
+  const uint32_t g = threadIdx.x % G, slot = threadIdx.x / G;
+  const uint32_t tok = slot / (uint32_t)x.per, first = slot - tok * x.per;
+  uint32_t group = block, chunk = 0;  // of tokens, of heads
+  if (x.chunks > 1) group = block / (uint32_t)x.chunks, chunk = block - group * x.chunks;
+  const uint32_t place = group * x.tokens + tok;
+  bool on = (int)tok < x.tokens && place < places;
+  const int s = on ? place / (uint32_t)a.tokens : 0, t = on ? place - (uint32_t)s * a.tokens : 0;
   if (on) on = t < tokens_of(a, s);
   // (whole groups of G lanes, a power of two, are on or off together)
   const int R = x.rotate ? a.rope.rot_dim : 0;
   // the thread's two pieces; the channels behind R of a half layout two by two
   const bool apart = !PAIRS && N * g < R / 2;
   const int ca = apart ? N * g : 2 * N * g, step = apart ? R / 2 : N;
-  const int heads_here = (x.heads + x.chunks - 1) / x.chunks;
-  const int h1 = min(x.heads, (chunk + 1) * heads_here);
-  const int hfirst = chunk * heads_here + first;
+  const int hfirst = chunk * x.chunk + first, h1 = min(x.heads, (int)(chunk + 1) * x.chunk);
   const T *in = static_cast<const T *>(x.in) + s * x.is + t * x.it + hfirst * x.ih + ca;
   T *out = static_cast<T *>(x.out) + s * x.os + t * x.ot + hfirst * x.oh + ca;
   const long long in_step = x.per * x.ih, out_step = x.per * x.oh;
-  const int rows = on ? (h1 - hfirst + x.per - 1) / x.per : 0;   // of this thread (may be below 0)
-  const int most = (heads_here + x.per - 1) / x.per;             // of any in the block
+  // rows of this thread (x.most: of any in the block)
+  const int rows = on && hfirst < h1 ? (int)((uint32_t)(h1 - hfirst + x.per - 1) / (uint32_t)x.per) : 0;
+  const int most = x.most;
   // cosines and sines; half layout: of the pairs of channels 2 i, 2 i + 1 of the
   // two pieces; interleaved: of the pairs themselves, the first piece's first
   uint64_t c[2], sn[2], wa[2], wb[2], ba[2], bb[2];
@@ -242,9 +242,9 @@ __global__ void __launch_bounds__(kHeadThreads)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long r = (long long)blockIdx.x * (kHeadThreads / 32) + warp;
   if (r >= rows) return;
-  int h = (int)(r % a.heads);
-  const long long place = r / a.heads;
-  const int s = (int)(place / a.tokens), t = (int)(place % a.tokens);
+  const uint32_t place = (uint32_t)(r / a.heads);  // at most 2^30
+  int h = (int)(r - (long long)place * a.heads);
+  const int s = place / (uint32_t)a.tokens, t = place - (uint32_t)s * a.tokens;
   if (t >= tokens_of(a, s)) return;
   int i = 0;
   while (i + 1 < a.sets && h >= a.set[i].heads) h -= a.set[i++].heads;
@@ -308,8 +308,9 @@ cudaError_t launch(HeadsArgs a, cudaStream_t s) {
     return pdl_launch(heads_any_kernel<T, D, NORM>, (int)grid, kHeadThreads, 0, s, a, rows);
   }
   // several heads a thread as soon as the device is full
-  int iters = 8;
-  while (iters > 1 && places * a.heads < 608LL * kSlots * iters) iters >>= 1;
+  const long long once = 608LL * kSlots;  // rows of four blocks an SM
+  const long long want = (places * a.heads + once - 1) / once;
+  const int iters = (int)(want < 8 ? want : 8);
   long long grid = 0;
   for (int i = 0; i < a.sets; ++i) {
     HeadSet &x = a.set[i];
@@ -320,13 +321,15 @@ cudaError_t launch(HeadsArgs a, cudaStream_t s) {
       x.per = kSlots;
     }
     x.tokens = kSlots / x.per;
+    x.chunk = (x.heads + x.chunks - 1) / x.chunks;
+    x.most = (x.chunk + x.per - 1) / x.per;
     x.first_block = (int)grid;
     grid += (places + x.tokens - 1) / x.tokens * x.chunks;
     if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   }
   return pdl_launch(a.rope.layout == HKV_ROPE_PAIRS ? heads_kernel<T, D, NORM, true>
                                                     : heads_kernel<T, D, NORM, false>,
-                    (int)grid, kHeadThreads, 0, s, a, places);
+                    (int)grid, kHeadThreads, 0, s, a, (uint32_t)places);
 }
 
 template <typename T, int D>
