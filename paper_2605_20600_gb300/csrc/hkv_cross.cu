@@ -64,20 +64,22 @@ __device__ __forceinline__ void load_piece(unsigned char *dst, int plane, const 
       *reinterpret_cast<uint4 *>(dst + k * plane) = make_uint4(p[0][k], p[1][k], p[2][k], p[3][k]);
   }
 }
-// `rows` rows of a tile, those from `live` on as zeros
-template <int D, typename T>
+// Rows [r0, r0 + rows) of a tile, those from `live` on as zeros, by the block
+// or by each warp its own.
+template <int D, typename T, int THREADS>
 __device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T *src,
-                                          long long stride, int rows, int live) {
+                                          long long stride, int r0, int rows, int live) {
   constexpr int PPR = D / 8;
-  for (int e = threadIdx.x; e < rows * PPR; e += kThreads) {
-    const int r = e / PPR, c = e % PPR;
+  for (int e = threadIdx.x % THREADS; e < rows * PPR; e += THREADS) {
+    const int r = r0 + e / PPR, c = e % PPR;
     const bool on = r < live;
     load_piece<T>(dst + at16<D>(r, c), plane, src + (on ? r * stride : 0) + c * 8, on);
   }
 }
 
 template <int D, typename T, typename O, int MW>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel(const CrossArgs p) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2)
+    cross_kernel(const CrossArgs p) {
   using SM = CSmem<D, T, MW>;
   constexpr int NP = Planes<T>::kN, STAGES = Planes<T>::kStages;
   constexpr int WP = sizeof(O) == 4 ? 3 : 2;         // parts of a weight
@@ -98,10 +100,19 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel
   const T *V = static_cast<const T *>(p.v) + w.s * p.ks + w.kvh * p.kh;
   unsigned char *sq = dyn + SM::kTiles;
 
+  // a tile's rows: with one warp of queries each warp loads the keys that it
+  // works on, and waits for no other
+  constexpr bool ALONE = MW == 1 && STAGES > 1;
   auto load_tile = [&](int k0, int st) {
     unsigned char *s = dyn + st * SM::kStage;
-    load_rows<D, T>(s, SM::kPlane, K + k0 * p.kt, p.kt, kKeys, hi - k0);
-    load_rows<D, T>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.kt, p.kt, kKeys, hi - k0);
+    constexpr int FIRST = ALONE ? 32 : kThreads;
+    const int r0 = ALONE ? kw * NKW : 0, n = ALONE ? NKW : kKeys;
+    load_rows<D, T, FIRST>(s, SM::kPlane, K + k0 * p.kt, p.kt, r0, n, hi - k0);
+    load_rows<D, T, FIRST>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.kt, p.kt, r0, n, hi - k0);
+  };
+  auto together = [&] {
+    if (ALONE) __syncwarp();
+    else __syncthreads();
   };
 
   float o[D / 8][4];
@@ -145,7 +156,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel
       } else {
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       }
-      __syncthreads();
+      if (ALONE && k0 == lo) __syncthreads();  // the queries are everyone's
+      else together();
       const uint32_t kb = t_base + st * SM::kStage, vb = kb + NP * SM::kPlane;
       float s[NKW / 8][4];
 #pragma unroll
@@ -263,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel
           for (int e = 0; e < 4; ++e) o[2 * db + x][e] += t[x][e];
       }
       if (STAGES > 1) {
-        __syncthreads();  // the stage is rewritten
+        together();  // the stage is rewritten
         const int next = k0 + STAGES * kKeys;
         if (next < hi) load_tile(next, st);
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -284,12 +296,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel
   __syncthreads();
   float *so = reinterpret_cast<float *>(dyn);  // [warp][16][D]
 #pragma unroll
-  for (int x = 0; x < D / 8; ++x) {
+  for (int j = 0; j < 2; ++j) {
+    const int r = (lane >> 2) + 8 * j;
+    if (mw * 16 + r < nq) {
+      float *to = so + (size_t)(warp * 16 + r) * D + (lane & 3) * 2;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      *reinterpret_cast<float2 *>(
-          so + (size_t)(warp * 16 + (lane >> 2) + 8 * j) * D + x * 8 + (lane & 3) * 2) =
-          make_float2(o[x][2 * j], o[x][2 * j + 1]);
+      for (int x = 0; x < D / 8; ++x)
+        *reinterpret_cast<float2 *>(to + x * 8) = make_float2(o[x][2 * j], o[x][2 * j + 1]);
+    }
   }
   __syncthreads();
   // rows of D / 4 threads each: the warps along the keys joined
@@ -324,65 +338,89 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) cross_kernel
   }
 }
 
-// Joins a query's ranges in their order, a warp per query.
-constexpr int kJoinThreads = 128;
-template <int D, typename O>
+// Joins a query's ranges: W warps a query, each a run of its ranges in order.
+constexpr int kJoinThreads = 256;
+template <int D, typename O, int W>
 __global__ void __launch_bounds__(kJoinThreads)
     cross_join_kernel(const CrossArgs p, long long rows) {
-  constexpr int PF = D + 4, E = D / 32;
+  constexpr int PF = D + 4, E = D / 32, ROWS = kJoinThreads / 32 / W;
+  __shared__ float s_acc[ROWS][W][D], s_ml[ROWS][W][2];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  if (row >= rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w = warp % W, slot = warp / W;
+  const long long row = (long long)blockIdx.x * ROWS + slot;
   const int token = (int)(row % p.tokens);
   const long long sh = row / p.tokens;
   const int h = (int)(sh % p.heads), s = (int)(sh / p.heads);
-  const int qlen = p.qlen ? p.qlen[s] : p.tokens;
-  if (token >= qlen || qlen > p.tokens) return;
-  const float *first = p.part + (size_t)row * p.splits * PF;
-  // a lane holds every 32nd range's maximum and sum at a time
-  auto range = [&](int j) {
-    return j < p.splits ? *reinterpret_cast<const float2 *>(first + (size_t)j * PF + D)
-                        : make_float2(-INFINITY, 0.f);
-  };
-  float m = -INFINITY;
-  bool bad = false;
-  for (int j = lane; j < p.splits; j += 32) {
-    const float2 ml = range(j);
-    bad |= ml.x != ml.x && ml.y == 0.f;
-    if (ml.y != 0.f) m = fmaxf(m, ml.x);
-  }
-  bad = __any_sync(0xFFFFFFFFu, bad);
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-  float l = 0.f, acc[E];
+  const int qlen = row < rows ? p.qlen ? p.qlen[s] : p.tokens : 0;
+  const bool live = token < qlen && qlen <= p.tokens;
+  const int per = (p.splits + W - 1) / W, j0 = w * per, n = live ? min(per, p.splits - j0) : 0;
+  const float *first = p.part + ((size_t)row * p.splits + j0) * PF;
+  float m = -INFINITY, l = 0.f, acc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  for (int j0 = 0; j0 < p.splits; j0 += 32) {
-    const float2 ml = range(j0 + lane);
-    const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - m);
-    l += ml.y * f;
-    const int n = min(32, p.splits - j0);
+  bool bad = false;
+  // the ranges' maxima and sums, a lane each, 32 at a time; then their rows, a
+  // few on the way at a time
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    const int here = min(32, n - k0);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < here) ml = *reinterpret_cast<const float2 *>(first + (size_t)(k0 + lane) * PF + D);
+    bad |= __any_sync(0xFFFFFFFFu, ml.x != ml.x && ml.y == 0.f);
+    float top = ml.y != 0.f ? ml.x : -INFINITY;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    const float mn = fmaxf(m, top), old = l == 0.f ? 0.f : ex2_approx(m - mn);
+    const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mn);
+    m = mn;
+    float sum = ml.y * f;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    l = l * old + sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= old;
     constexpr int B = 8;
-    for (int j = 0; j < n; j += B) {
+    for (int j = 0; j < here; j += B) {
       float v[B][E];
 #pragma unroll
       for (int u = 0; u < B; ++u)
-        if (j + u < n) load_row<E>(first + (size_t)(j0 + j + u) * PF + lane * E, v[u]);
+        if (j + u < here) load_row<E>(first + (size_t)(k0 + j + u) * PF + lane * E, v[u]);
 #pragma unroll
       for (int u = 0; u < B; ++u) {
         const float fj = __shfl_sync(0xFFFFFFFFu, f, (j + u) & 31);
-        if (j + u < n && fj != 0.f) {
+        if (j + u < here && fj != 0.f) {
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[e] += v[u][e] * fj;
         }
       }
     }
   }
+  if (bad) l = NAN;
+  if (W > 1) {  // the warps' parts, in order
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-  const float inv = bad ? NAN : l == 0.f ? 0.f : 1.f / l;
+    for (int e = 0; e < E; ++e) s_acc[slot][w][lane * E + e] = acc[e];
+    if (lane == 0) s_ml[slot][w][0] = m, s_ml[slot][w][1] = l;
+    __syncthreads();
+    if (w > 0) return;
+    float mn = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (s_ml[slot][i][1] != 0.f) mn = fmaxf(mn, s_ml[slot][i][0]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float li = s_ml[slot][i][1], f = li == 0.f ? 0.f : ex2_approx(s_ml[slot][i][0] - mn);
+      if (li == 0.f) continue;
+      l += li * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += s_acc[slot][i][lane * E + e] * f;
+    }
+    m = mn;
+  }
+  if (!live) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   O *to = static_cast<O *>(p.out) + s * p.os + token * p.ot + h * p.oh + lane * E;
   if (E == 4)
     store4(to, make_float4(acc[0] * inv, acc[1] * inv, acc[2 % E] * inv, acc[3 % E] * inv));
@@ -390,7 +428,7 @@ __global__ void __launch_bounds__(kJoinThreads)
     *reinterpret_cast<float2 *>(to) = make_float2(acc[0] * inv, acc[1] * inv);
   else
     *reinterpret_cast<uint32_t *>(to) = pack2(acc[0] * inv, acc[1] * inv);
-  if (lane == 0 && p.lse) p.lse[row] = bad ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 template <int D, typename T, typename O, int MW>
@@ -407,13 +445,19 @@ cudaError_t launch_rows(const CrossArgs &a, const CrossPlan &pl, cudaStream_t s)
   const long long grid = (long long)a.seqs * a.kv * a.tiles * a.splits;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
   cudaError_t e;
-  if (pl.rows >= 128) e = launch_cross_tc(a, pl, D, s);
-  else if (pl.rows == 16) e = launch_tiles<D, T, O, 1>(a, (int)grid, s);
-  else if (pl.rows == 32) e = launch_tiles<D, T, O, 2>(a, (int)grid, s);
-  else e = launch_tiles<D, T, O, 4>(a, (int)grid, s);
+  if constexpr (sizeof(O) == 2) {  // (more than 16 rows are the tcgen05 kernel's)
+    e = pl.rows >= 128 ? launch_cross_tc(a, pl, D, s) : launch_tiles<D, T, O, 1>(a, (int)grid, s);
+  } else {
+    if (pl.rows == 16) e = launch_tiles<D, T, O, 1>(a, (int)grid, s);
+    else if (pl.rows == 32) e = launch_tiles<D, T, O, 2>(a, (int)grid, s);
+    else e = launch_tiles<D, T, O, 4>(a, (int)grid, s);
+  }
   if (e != cudaSuccess || a.splits == 1) return e;
+  // a warp a query, or eight where there are many ranges
   const long long rows = (long long)a.seqs * a.heads * a.tokens;
-  return pdl_launch(cross_join_kernel<D, O>, (int)((rows + 3) / 4), kJoinThreads, 0, s, a, rows);
+  if (a.splits > 16)
+    return pdl_launch(cross_join_kernel<D, O, 8>, (int)rows, kJoinThreads, 0, s, a, rows);
+  return pdl_launch(cross_join_kernel<D, O, 1>, (int)((rows + 7) / 8), kJoinThreads, 0, s, a, rows);
 }
 
 }  // namespace
@@ -423,17 +467,18 @@ cudaError_t launch_rows(const CrossArgs &a, const CrossPlan &pl, cudaStream_t s)
 // caller allocated does not depend on the device of the call.
 CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, int dtype,
                      int out_dtype) {
-  constexpr int kCtas = 304, kMostSplits = 304;
+  constexpr int kMostSplits = 456;
   CrossPlan pl;
   const long long all = (long long)(heads / kv) * tokens;
-  const bool tc = dtype == HKV_BF16 && out_dtype == HKV_BF16 && all > 64;
+  const bool tc = dtype == HKV_BF16 && out_dtype == HKV_BF16 && all > 16;
 #ifdef HKV_TC_ROWS
   if (tc) pl.rows = HKV_TC_ROWS;
 #else
   if (tc) pl.rows = all > 128 ? 256 : 128;
 #endif
   else pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
-  const int tile = tc ? 128 : kKeys, ctas = pl.rows == 256 ? kCtas / 2 : kCtas;
+  const int tile = tc ? 128 : kKeys;
+  const int ctas = pl.rows == 256 ? 152 : pl.rows == 16 && dtype == HKV_BF16 ? 456 : dtype == HKV_BF16 ? 304 : 152;
   // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as
   // many heads of a group as fit 128 rows
   const int group = heads / kv;
@@ -447,10 +492,15 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   } else {
     pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
   }
-  const long long base = (long long)seqs * kv * pl.tiles, key_tiles = (keys + tile - 1) / tile;
-  long long want = base >= ctas ? 1 : ctas / base;
+  const long long base = (long long)seqs * kv * pl.tiles;
+  // several rounds of CTAs, or one, and no range that takes less time than its
+  // partial result is worth
+  constexpr int kLeast = 512;
+  long long want = base < ctas ? ctas / base : 1;
+  if (pl.rows == 16 && base >= ctas && base < 4LL * ctas) want = (4LL * ctas + base - 1) / base;
   if (want > kMostSplits) want = kMostSplits;
-  if (want > key_tiles) want = key_tiles;
+  if (want > keys / kLeast) want = keys / kLeast;
+  if (want < 1) want = 1;
   pl.split_len = (int)(((keys + want - 1) / want + tile - 1) / tile * tile);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
   pl.part_bytes =

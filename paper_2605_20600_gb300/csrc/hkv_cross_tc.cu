@@ -12,7 +12,8 @@
 // A row's reference maximum moves (and O and its sum are rescaled) only when a
 // tile's maximum is more than 2^8 above it, so that weights stay below 2^8. The
 // weights are rounded to bf16, off by at most 2^-9 each, as the outs are; their
-// sum is that of the fp32 weights.
+// sum is that of the fp32 weights. One query tile a CTA (few queries, where the
+// loads take longer than the products) takes them in two parts, off by 2^-18.
 //
 // Rows of V past the last state are set to zero in shared memory (a weight of
 // zero times what lies there could be NaN); scores past it are masked.
@@ -34,6 +35,7 @@ struct TcPlan {
   // which the products need together
   static constexpr int kSlots = TILES * (D == 64 ? 2 : 1);
   static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kQ;
+  static constexpr int kParts = TILES == 1 ? 2 : 1;  // bf16 parts of a weight
   static constexpr int kCols = TILES * 256;         // TMEM: S of each tile, then O of each
 };
 
@@ -199,9 +201,12 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           if (mine) {
             const uint64_t vd = tc_desc(ring_at + ((i + 1) % SLOTS) * 2 * TP::kQ + TP::kQ, kTile * 128);
 #pragma unroll
-            for (int kk = 0; kk < kTile / 16; ++kk)
-              tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + kk * 8, vd + kk * (16 * 128 >> 4),
-                        tc_instr(kTile, D, true), i > 0 || kk > 0);
+            for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
+#pragma unroll
+              for (int kk = 0; kk < kTile / 16; ++kk)
+                tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + part * 64 + kk * 8,
+                          vd + kk * (16 * 128 >> 4), tc_instr(kTile, D, true),
+                          i > 0 || kk > 0 || part < TP::kParts - 1);
             if (i + 1 < n[t]) scores(t, i + 1);  // over the weights, after the products that read them
             else tc_commit(&s_s[t]);
           }
@@ -264,15 +269,18 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        uint32_t v[16];
+        uint32_t v[16], v2[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const uint64_t e = fma2(pair_of(s[c][2 * j], s[c][2 * j + 1]), scale2, ref2);
           const float w0 = ex2_approx(low(e)), w1 = ex2_approx(high(e));
           sum[j & 1] = add2(sum[j & 1], pair_of(w0, w1));
           v[j] = pack2(w0, w1);
+          if (TP::kParts == 2)
+            v2[j] = pack2(w0 - __uint_as_float(v[j] << 16), w1 - __uint_as_float(v[j] & 0xFFFF0000u));
         }
         tmem_st16(mine + c * 16, v);
+        if (TP::kParts == 2) tmem_st16(mine + 64 + c * 16, v2);
       }
       tmem_wait_st();
       tc_fence_before();

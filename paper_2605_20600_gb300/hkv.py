@@ -184,16 +184,12 @@ _SIGNATURES = {
     "hkv_prefix_workspace_size": ([POINTER(hkv_config), POINTER(hkv_prefix)], c_size_t),
     "hkv_prefix_attention": ([POINTER(hkv_config), POINTER(hkv_prefix), c_void_p, c_void_p, c_void_p,
                               c_void_p, c_size_t, c_void_p], c_int),
-    "hkv_make_rope": ([POINTER(hkv_rope_params), POINTER(hkv_rope)], c_int),
-    "hkv_rope_rotate": ([POINTER(hkv_config), POINTER(hkv_rope), POINTER(hkv_tokens), POINTER(hkv_rows),
-                         POINTER(hkv_rows), c_int, c_void_p], c_int),
-    "hkv_qk_norm_rope": ([POINTER(hkv_config), POINTER(hkv_norm), POINTER(hkv_rope), POINTER(hkv_tokens)]
-                         + [POINTER(hkv_rows)] * 6 + [c_void_p], c_int),
-    "hkv_cross_workspace_size": ([POINTER(hkv_config), POINTER(hkv_states), POINTER(hkv_tokens)],
-                                 c_size_t),
-    "hkv_cross_attention": ([POINTER(hkv_config), POINTER(hkv_states), POINTER(hkv_tokens),
-                             POINTER(hkv_rows), POINTER(hkv_rows), c_void_p, c_void_p, c_size_t, c_int,
-                             c_void_p], c_int),
+    # (addresses of structures: a POINTER argument costs several times an integer)
+    "hkv_make_rope": ([c_void_p] * 2, c_int),
+    "hkv_rope_rotate": ([c_void_p] * 5 + [c_int, c_void_p], c_int),
+    "hkv_qk_norm_rope": ([c_void_p] * 11, c_int),
+    "hkv_cross_workspace_size": ([c_void_p] * 3, c_size_t),
+    "hkv_cross_attention": ([c_void_p] * 7 + [c_size_t, c_int, c_void_p], c_int),
 }
 
 
@@ -468,7 +464,7 @@ def hkv_make_rope(*, head_dim, rot_dim=None, layout=HKV_ROPE_HALF, sections=None
     p = hkv_rope_params(head_dim, rot_dim, layout, len(sections), (c_int32 * 3)(*sections), int(joint),
                         scaling, 0, base, factor, original, low, high, amplitude)
     rope = hkv_rope()
-    _call("make_rope", ctypes.byref(p), ctypes.byref(rope))
+    _call("make_rope", _addr(p), _addr(rope))
     return rope
 
 
@@ -554,54 +550,69 @@ def make_states(k, v, length=None, err=None) -> hkv_states:
     return s
 
 
-def _fit(name, cfg, tokens, rope, *rows) -> None:
+_addr = ctypes.addressof
+
+
+def _at(x):
+    return None if x is None else _addr(x)
+
+
+def _fit(name, cfg, tokens, rope, rows) -> None:
     """Refuses views whose known sizes are not the call's."""
-    ok = all(r is None or r.of in (None, (cfg.n_seqs, tokens.n_tokens, cfg.head_dim)) for r in rows)
+    seqs = cfg.n_seqs
+    want = (seqs, tokens.n_tokens, cfg.head_dim)
+    ok = True
+    for r in rows:
+        if r is not None and r.of != want and r.of is not None:
+            ok = False
     if tokens.of is not None:
-        seqs, axes, pos_rows = tokens.of
-        ok = ok and seqs in (None, cfg.n_seqs)
-        if rope is not None and tokens.pos:
-            ok = ok and axes >= rope.n_axes and pos_rows in (1, cfg.n_seqs)
+        len_seqs, axes, pos_rows = tokens.of
+        if len_seqs is not None and len_seqs != seqs:
+            ok = False
+        if rope is not None and axes and (axes < rope.n_axes or pos_rows not in (1, seqs)):
+            ok = False
     if not ok:
         raise HkvError(name, HKV_ERR_SHAPE)
 
 
-def _r(x):
-    return None if x is None else ctypes.byref(x)
-
-
 def hkv_rope_rotate(cfg, rope, tokens, x, out, flags=0, stream=0) -> None:
-    _fit("rope_rotate", cfg, tokens, rope, x, out)
-    _call("rope_rotate", ctypes.byref(cfg), ctypes.byref(rope), ctypes.byref(tokens), ctypes.byref(x),
-          ctypes.byref(out), flags, stream)
+    _fit("rope_rotate", cfg, tokens, rope, (x, out))
+    st = (_lib or lib()).hkv_rope_rotate(_addr(cfg), _addr(rope), _addr(tokens), _addr(x), _addr(out),
+                                         flags, stream)
+    if st != HKV_OK:
+        raise HkvError("rope_rotate", st)
 
 
 def hkv_qk_norm_rope(cfg, norm, rope, tokens, q, k, v, q_out, k_out, v_out, stream=0) -> None:
     """norm and rope may be None, and pairs of q, k, v and their outs."""
-    _fit("qk_norm_rope", cfg, tokens, rope, q, k, v, q_out, k_out, v_out)
+    _fit("qk_norm_rope", cfg, tokens, rope, (q, k, v, q_out, k_out, v_out))
     if norm is not None and norm.of is not None:
         dtype, dim, q_heads, k_heads = norm.of
-        if (dtype, dim) != (cfg.dtype, cfg.head_dim) or (q and q_heads not in (None, q.n_heads)) \
-                or (k and k_heads not in (None, k.n_heads)):
+        if dtype != cfg.dtype or dim != cfg.head_dim \
+                or (q is not None and q_heads is not None and q_heads != q.n_heads) \
+                or (k is not None and k_heads is not None and k_heads != k.n_heads):
             raise HkvError("qk_norm_rope", HKV_ERR_SHAPE)
-    _call("qk_norm_rope", ctypes.byref(cfg), _r(norm), _r(rope), ctypes.byref(tokens), _r(q), _r(k), _r(v),
-          _r(q_out), _r(k_out), _r(v_out), stream)
+    st = (_lib or lib()).hkv_qk_norm_rope(_addr(cfg), _at(norm), _at(rope), _addr(tokens), _at(q), _at(k),
+                                          _at(v), _at(q_out), _at(k_out), _at(v_out), stream)
+    if st != HKV_OK:
+        raise HkvError("qk_norm_rope", st)
 
 
 def _states_fit(cfg, states) -> bool:
-    return states.of in (None, (cfg.dtype, cfg.n_seqs, cfg.head_dim))
+    return states.of is None or states.of == (cfg.dtype, cfg.n_seqs, cfg.head_dim)
 
 
 def hkv_cross_workspace_size(cfg, states, tokens) -> int:
     if not _states_fit(cfg, states):
         return 0
-    return int(lib().hkv_cross_workspace_size(ctypes.byref(cfg), ctypes.byref(states),
-                                              ctypes.byref(tokens)))
+    return int(lib().hkv_cross_workspace_size(_addr(cfg), _addr(states), _addr(tokens)))
 
 
 def hkv_cross_attention(cfg, states, tokens, q, out, lse, workspace, ws_bytes, flags=0, stream=0) -> None:
-    _fit("cross_attention", cfg, tokens, None, q, out)
+    _fit("cross_attention", cfg, tokens, None, (q, out))
     if not _states_fit(cfg, states):
         raise HkvError("cross_attention", HKV_ERR_SHAPE)
-    _call("cross_attention", ctypes.byref(cfg), ctypes.byref(states), ctypes.byref(tokens), ctypes.byref(q),
-          ctypes.byref(out), _p(lse), _p(workspace), ws_bytes, flags, stream)
+    st = (_lib or lib()).hkv_cross_attention(_addr(cfg), _addr(states), _addr(tokens), _addr(q), _addr(out),
+                                             _p(lse), _p(workspace), ws_bytes, flags, stream)
+    if st != HKV_OK:
+        raise HkvError("cross_attention", st)
