@@ -25,7 +25,7 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", 
 
 SOURCES = ["hkv_api.cu", "hkv_attention.cu", "hkv_step.cu", "hkv_update.cu", "hkv_noalloc.cu",
            "hkv_serve_api.cu", "hkv_quant.cu", "hkv_quant_attn.cu", "hkv_prefix.cu",
-           "hkv_prompt_api.cu", "hkv_rope.cu", "hkv_cross.cu", "hkv_cross_tc.cu"]
+           "hkv_prompt_api.cu", "hkv_rope.cu", "hkv_cross.cu", "hkv_cross_tc.cu", "hkv_cross_parts.cu"]
 
 
 def nvcc() -> str:

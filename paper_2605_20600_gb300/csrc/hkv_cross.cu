@@ -1,18 +1,16 @@
 // Attention of the tokens' queries over their sequence's states, or of a
 // prompt's tokens over the tokens up to themselves.
 //
-// A CTA takes up to 16 MW queries of one (sequence, key head), the heads of the
-// group one after the other, and a range of keys in tiles of 64; the ranges of
-// one query are joined by a second kernel. cross_kernel (mma.sync m16n8k16): MW
-// warps lie along the queries, 16 each, the others along the keys of a tile,
-// joined in shared memory.
+// cross_kernel (here) takes up to 16 query rows of a (sequence, key head), the
+// heads of the group one after the other, and a range of keys in tiles of 64 on
+// mma.sync m16n8k16, 16 keys of a tile a warp; the ranges of one query are
+// joined by a second kernel. More rows are hkv_cross_tc.cu's and
+// hkv_cross_parts.cu's.
 //
-// Precision: bf16 queries, keys and values enter as they are; an fp32 element
-// is three bf16 parts, and the six products of parts that reach past 2^-24 are
-// taken, the small ones first. The weights are three parts for fp32 outs, which
-// leaves nothing of them out, and two, off by 2^-18 of a weight, for bf16 outs,
-// whose own rounding is 2^-9. Sums are fp32; products chain in the tensor core
-// within a tile.
+// Precision: queries, keys and values (bf16) enter as they are, the weights as
+// three bf16 parts for fp32 outs, which leaves nothing of them out, and as two,
+// off by 2^-18 of a weight, for bf16 outs, whose own rounding is 2^-9. Sums are
+// fp32; products chain in the tensor core within a tile.
 #include "hkv_cross.cuh"
 #include "hkv_quant.cuh"
 
@@ -23,96 +21,46 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kKeys = 64;  // keys of a tile
 
-template <typename T>
-struct Planes {
-  static constexpr int kN = 1, kStages = 2;
-};
-template <>
-struct Planes<float> {
-  static constexpr int kN = 3, kStages = 1;
-};
+constexpr int kStages = 2;
+using bf16 = __nv_bfloat16;
 
-template <int D, typename T, int MW>
+template <int D>
 struct CSmem {
-  static constexpr int kRow = D * 2;                        // bytes of a bf16 row
-  static constexpr int kPlane = kKeys * kRow;
-  static constexpr int kStage = 2 * Planes<T>::kN * kPlane;  // K planes, V planes
-  static constexpr int kQPlane = MW * 16 * kRow;
-  static constexpr int kQ = Planes<T>::kN * kQPlane;
-  static constexpr int kTiles = Planes<T>::kStages * kStage;
-  static constexpr int kTotal = kTiles + kQ;
+  static constexpr int kPlane = kKeys * D * 2;     // K or V of a tile
+  static constexpr int kTiles = kStages * 2 * kPlane;
+  static constexpr int kTotal = kTiles + 16 * D * 2;
   static_assert(kWarps * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
 };
 
-// A piece of 8 elements of a row (zeros where `on` is false) into the planes at
-// dst. bf16: asynchronous.
-template <typename T>
-__device__ __forceinline__ void load_piece(unsigned char *dst, int plane, const T *from, bool on) {
-  if (sizeof(T) == 2) {
-    cp_async16_zfill(dst, from, on);
-  } else {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (on) {
-      Elem<float>::unpack(reinterpret_cast<const uint4 *>(from)[0], x);
-      Elem<float>::unpack(reinterpret_cast<const uint4 *>(from)[1], x + 4);
-    }
-    uint32_t p[4][3];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) split2<true>(x[2 * j], x[2 * j + 1], p[j]);
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      *reinterpret_cast<uint4 *>(dst + k * plane) = make_uint4(p[0][k], p[1][k], p[2][k], p[3][k]);
-  }
-}
-// Rows [r0, r0 + rows) of a tile, those from `live` on as zeros, by the block
-// or by each warp its own.
-template <int D, typename T, int THREADS>
-__device__ __forceinline__ void load_rows(unsigned char *dst, int plane, const T *src,
-                                          long long stride, int r0, int rows, int live) {
-  constexpr int PPR = D / 8;
-  for (int e = threadIdx.x % THREADS; e < rows * PPR; e += THREADS) {
-    const int r = r0 + e / PPR, c = e % PPR;
-    const bool on = r < live;
-    load_piece<T>(dst + at16<D>(r, c), plane, src + (on ? r * stride : 0) + c * 8, on);
-  }
-}
-
-template <int D, typename T, typename O, int MW>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2)
-    cross_kernel(const CrossArgs p) {
-  using SM = CSmem<D, T, MW>;
-  constexpr int NP = Planes<T>::kN, STAGES = Planes<T>::kStages;
-  constexpr int WP = sizeof(O) == 4 ? 3 : 2;         // parts of a weight
-  constexpr int KW = kWarps / MW, NKW = kKeys / KW;  // keys of a tile per warp
-  constexpr int PF = D + 4;
+template <int D, typename O>
+__global__ void __launch_bounds__(kThreads, 3) cross_kernel(const __grid_constant__ CrossArgs p) {
+  using SM = CSmem<D>;
+  constexpr int WP = sizeof(O) == 4 ? 3 : 2;  // parts of a weight
+  constexpr int PF = D + 4, PPR = D / 8;
   extern __shared__ __align__(128) unsigned char dyn[];
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int mw = warp % MW, kw = warp / MW;
   pdl_wait();
   pdl_launch_dependents();
   const Work w = work_of(p);
-  const int all = p.group * p.tokens;                // query rows of the (sequence, key head)
-  const int r0 = w.tile * MW * 16, nq = min(MW * 16, all - r0);
+  const int nq = p.group * p.tokens;  // query rows of the (sequence, key head)
   const int lo = w.sp * p.split_len;
-  const int hi = min(keys_of_rows(p, w, r0, r0 + nq), lo + p.split_len);
-  const T *K = static_cast<const T *>(p.k) + w.s * p.ks + w.kvh * p.kh;
-  const T *V = static_cast<const T *>(p.v) + w.s * p.ks + w.kvh * p.kh;
+  const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);
+  const bf16 *K = static_cast<const bf16 *>(p.k) + w.s * p.ks + w.kvh * p.kh;
+  const bf16 *V = static_cast<const bf16 *>(p.v) + w.s * p.ks + w.kvh * p.kh;
   unsigned char *sq = dyn + SM::kTiles;
 
-  // a tile's rows: with one warp of queries each warp loads the keys that it
-  // works on, and waits for no other
-  constexpr bool ALONE = MW == 1 && STAGES > 1;
+  // each warp loads the keys of a tile that it works on, and waits for no other
   auto load_tile = [&](int k0, int st) {
-    unsigned char *s = dyn + st * SM::kStage;
-    constexpr int FIRST = ALONE ? 32 : kThreads;
-    const int r0 = ALONE ? kw * NKW : 0, n = ALONE ? NKW : kKeys;
-    load_rows<D, T, FIRST>(s, SM::kPlane, K + k0 * p.kt, p.kt, r0, n, hi - k0);
-    load_rows<D, T, FIRST>(s + NP * SM::kPlane, SM::kPlane, V + k0 * p.kt, p.kt, r0, n, hi - k0);
-  };
-  auto together = [&] {
-    if (ALONE) __syncwarp();
-    else __syncthreads();
+    unsigned char *s = dyn + st * 2 * SM::kPlane;
+#pragma unroll
+    for (int e = lane; e < 16 * PPR; e += 32) {
+      const int r = warp * 16 + e / PPR, c = e % PPR;
+      const bool on = k0 + r < hi;
+      const long long at = (on ? (k0 + r) * p.kt : 0) + c * 8;
+      cp_async16_zfill(s + at16<D>(r, c), K + at, on);
+      cp_async16_zfill(s + SM::kPlane + at16<D>(r, c), V + at, on);
+    }
   };
 
   float o[D / 8][4];
@@ -120,88 +68,53 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
   for (int x = 0; x < D / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
   float m[2] = {kNoKey, kNoKey}, l[2] = {0.f, 0.f};
   if (lo < hi) {
-    for (int e = tid; e < MW * 16 * (D / 8); e += kThreads) {
-      const int r = e / (D / 8), c = e % (D / 8);
-      const Row x = row_of(p, w.kvh, r0 + min(r, nq - 1));
+    for (int e = tid; e < 16 * PPR; e += kThreads) {
+      const int r = e / PPR, c = e % PPR;
+      const Row x = row_of(p, w.kvh, min(r, nq - 1));
       const bool on = r < nq && x.token < w.qlen;
-      load_piece<T>(sq + at16<D>(r, c), SM::kQPlane,
-                    static_cast<const T *>(p.q) + w.s * p.qs +
-                        (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on);
+      cp_async16_zfill(sq + at16<D>(r, c),
+                       static_cast<const bf16 *>(p.q) + w.s * p.qs +
+                           (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    if (STAGES > 1) {
 #pragma unroll
-      for (int st = 0; st < STAGES; ++st) {
-        if (lo + st * kKeys < hi) load_tile(lo + st * kKeys, st);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      }
+    for (int st = 0; st < kStages; ++st) {
+      if (lo + st * kKeys < hi) load_tile(lo + st * kKeys, st);
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // fragment addresses: which row and piece of a 16 x 16 block a lane names
     int seen[2];  // keys that the thread's two rows see
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int r = r0 + mw * 16 + (lane >> 2) + 8 * j;
-      seen[j] = r < r0 + nq ? keys_seen(p, w, row_of(p, w.kvh, r).token) : 0;
+      const int r = (lane >> 2) + 8 * j;
+      seen[j] = r < nq ? keys_seen(p, w, row_of(p, w.kvh, r).token) : 0;
     }
+    // fragment addresses: which row and piece of a 16 x 16 block a lane names
     const int mi = lane >> 3, mr = lane & 7;
     const uint32_t q_base = smem_u32(sq), t_base = smem_u32(dyn);
-    const int q_row = mw * 16 + (mi & 1) * 8 + mr, q_pc = mi >> 1;
-    const int k_row = kw * NKW + (mi >> 1) * 8 + mr, k_pc = mi & 1;
-    const int v_row = kw * NKW + (mi & 1) * 8 + mr, v_pc = mi >> 1;
+    const int q_row = (mi & 1) * 8 + mr, q_pc = mi >> 1;
+    const int k_row = warp * 16 + (mi >> 1) * 8 + mr, k_pc = mi & 1;
+    const int v_row = warp * 16 + (mi & 1) * 8 + mr, v_pc = mi >> 1;
     int st = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys) {
-      if (STAGES == 1) {
-        __syncthreads();  // the tile before this one has been read
-        load_tile(k0, 0);
-      } else {
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      if (k0 == lo) __syncthreads();  // the queries are everyone's
+      else __syncwarp();
+      const uint32_t kb = t_base + st * 2 * SM::kPlane, vb = kb + SM::kPlane;
+      float s[2][4] = {};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint32_t qa[4], f[4];
+        ldm4(qa, q_base + at16<D>(q_row, 2 * ks + q_pc));
+        ldm4(f, kb + at16<D>(k_row, 2 * ks + k_pc));
+        mma_bf16(s[0], qa, f[0], f[1]);
+        mma_bf16(s[1], qa, f[2], f[3]);
       }
-      if (ALONE && k0 == lo) __syncthreads();  // the queries are everyone's
-      else together();
-      const uint32_t kb = t_base + st * SM::kStage, vb = kb + NP * SM::kPlane;
-      float s[NKW / 8][4];
-#pragma unroll
-      for (int x = 0; x < NKW / 8; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
-      if (NP == 1) {
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          uint32_t qa[4];
-          ldm4(qa, q_base + at16<D>(q_row, 2 * ks + q_pc));
-#pragma unroll
-          for (int nb = 0; nb < NKW / 16; ++nb) {
-            uint32_t f[4];
-            ldm4(f, kb + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
-            mma_bf16(s[2 * nb], qa, f[0], f[1]);
-            mma_bf16(s[2 * nb + 1], qa, f[2], f[3]);
-          }
-        }
-      } else {
-        // parts (2,0) (1,1) (0,2), then (1,0) (0,1), then (0,0)
-#pragma unroll
-        for (int order = 2; order >= 0; --order) {
-#pragma unroll 1
-          for (int ks = 0; ks < D / 16; ++ks) {
-#pragma unroll
-            for (int a = order; a >= 0; --a) {
-              uint32_t qa[4];
-              ldm4(qa, q_base + a * SM::kQPlane + at16<D>(q_row, 2 * ks + q_pc));
-#pragma unroll
-              for (int nb = 0; nb < NKW / 16; ++nb) {
-                uint32_t f[4];
-                ldm4(f, kb + (order - a) * SM::kPlane + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
-                mma_bf16(s[2 * nb], qa, f[0], f[1]);
-                mma_bf16(s[2 * nb + 1], qa, f[2], f[3]);
-              }
-            }
-          }
-        }
-      }
-      // weights of rows lane / 4 (j = 0) and lane / 4 + 8 (j = 1)
-      // keys of this warp's part that count for either row
-      const int left[2] = {min(seen[0], hi) - k0 - kw * NKW, min(seen[1], hi) - k0 - kw * NKW};
+      // weights of rows lane / 4 (j = 0) and lane / 4 + 8 (j = 1); keys of this
+      // warp's part that count for either
+      const int left[2] = {min(seen[0], hi) - k0 - warp * 16, min(seen[1], hi) - k0 - warp * 16};
       float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int x = 0; x < NKW / 8; ++x) {
+      for (int x = 0; x < 2; ++x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = x * 8 + (lane & 3) * 2 + (e & 1);
@@ -228,9 +141,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
           o[x][3] *= f[1];
         }
       }
-      uint32_t pf[NKW / 16][WP][4];
+      uint32_t pf[WP][4];
 #pragma unroll
-      for (int x = 0; x < NKW / 8; ++x) {
+      for (int x = 0; x < 2; ++x) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           // (a key that does not count has a score of -inf)
@@ -240,47 +153,29 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
           uint32_t pr[3];
           split2<false>(w0, w1, pr);
 #pragma unroll
-          for (int k = 0; k < WP; ++k) pf[x / 2][k][(x & 1) * 2 + j] = pr[k];
+          for (int k = 0; k < WP; ++k) pf[k][x * 2 + j] = pr[k];
         }
       }
-      // 16 DBS channels at a time: 2 DBS chains of products side by side
-      constexpr int DBS = 1;
 #pragma unroll
-      for (int db = 0; db < D / 16; db += DBS) {
-        float t[2 * DBS][4] = {};
+      for (int db = 0; db < D / 16; ++db) {  // 16 channels at a time
+        float t[2][4] = {};
+        uint32_t vf[4];
+        ldm4t(vf, vb + at16<D>(v_row, 2 * db + v_pc));
 #pragma unroll
-        for (int plane = NP - 1; plane >= 0; --plane) {  // parts of V, the small ones first
-          uint32_t vf[DBS][NKW / 16][4];
-#pragma unroll
-          for (int x = 0; x < DBS; ++x)
-#pragma unroll
-            for (int kk = 0; kk < NKW / 16; ++kk)
-              ldm4t(vf[x][kk],
-                    vb + plane * SM::kPlane + at16<D>(v_row + kk * 16, 2 * (db + x) + v_pc));
-#pragma unroll
-          for (int a = WP - 1 - plane; a >= 0; --a) {  // parts of w
-#pragma unroll
-            for (int kk = 0; kk < NKW / 16; ++kk) {
-#pragma unroll
-              for (int x = 0; x < DBS; ++x) {
-                mma_bf16(t[2 * x], pf[kk][a], vf[x][kk][0], vf[x][kk][1]);
-                mma_bf16(t[2 * x + 1], pf[kk][a], vf[x][kk][2], vf[x][kk][3]);
-              }
-            }
-          }
+        for (int a = WP - 1; a >= 0; --a) {  // the small parts first
+          mma_bf16(t[0], pf[a], vf[0], vf[1]);
+          mma_bf16(t[1], pf[a], vf[2], vf[3]);
         }
 #pragma unroll
-        for (int x = 0; x < 2 * DBS; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[2 * db + x][e] += t[x][e];
       }
-      if (STAGES > 1) {
-        together();  // the stage is rewritten
-        const int next = k0 + STAGES * kKeys;
-        if (next < hi) load_tile(next, st);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        st = st + 1 == STAGES ? 0 : st + 1;
-      }
+      __syncwarp();  // the stage is rewritten
+      const int next = k0 + kStages * kKeys;
+      if (next < hi) load_tile(next, st);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      st = st + 1 == kStages ? 0 : st + 1;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
@@ -298,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int r = (lane >> 2) + 8 * j;
-    if (mw * 16 + r < nq) {
+    if (r < nq) {
       float *to = so + (size_t)(warp * 16 + r) * D + (lane & 3) * 2;
 #pragma unroll
       for (int x = 0; x < D / 8; ++x)
@@ -306,23 +201,22 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
     }
   }
   __syncthreads();
-  // rows of D / 4 threads each: the warps along the keys joined
+  // rows of D / 4 threads each: the warps joined
   for (int e = tid; e < nq * (D / 4); e += kThreads) {
-    const int r = e / (D / 4), c = e % (D / 4), w0 = r >> 4, rr = r & 15;
+    const int r = e / (D / 4), c = e % (D / 4);
     float mj = -INFINITY, lj = 0.f;
 #pragma unroll
-    for (int k = 0; k < KW; ++k) mj = fmaxf(mj, s_m[w0 + k * MW][rr]);
+    for (int k = 0; k < kWarps; ++k) mj = fmaxf(mj, s_m[k][r]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < KW; ++k) {
-      const int wk = w0 + k * MW;
-      if (s_l[wk][rr] == 0.f) continue;
-      const float fk = ex2_approx(s_m[wk][rr] - mj);
-      const float4 u = *reinterpret_cast<const float4 *>(so + (size_t)(wk * 16 + rr) * D + c * 4);
-      lj += s_l[wk][rr] * fk;
+    for (int k = 0; k < kWarps; ++k) {
+      if (s_l[k][r] == 0.f) continue;
+      const float fk = ex2_approx(s_m[k][r] - mj);
+      const float4 u = *reinterpret_cast<const float4 *>(so + (size_t)(k * 16 + r) * D + c * 4);
+      lj += s_l[k][r] * fk;
       v.x += u.x * fk, v.y += u.y * fk, v.z += u.z * fk, v.w += u.w * fk;
     }
-    const Row x = row_of(p, w.kvh, r0 + r);
+    const Row x = row_of(p, w.kvh, r);
     if (x.token >= w.qlen) continue;
     const size_t row = ((size_t)w.s * p.heads + x.head) * p.tokens + x.token;
     if (p.splits > 1) {
@@ -332,6 +226,172 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : MW == 1 ? 3 : 2
     } else {
       const float inv = w.bad ? NAN : lj == 0.f ? 0.f : 1.f / lj;
       store4(static_cast<O *>(p.out) + w.s * p.os + x.token * p.ot + x.head * p.oh + c * 4,
+             make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+      if (c == 0 && p.lse) p.lse[row] = w.bad ? NAN : lj == 0.f ? -INFINITY : (mj + log2f(lj)) * kLn2;
+    }
+  }
+}
+
+// fp32 queries and states, up to R query rows, without the tensor core: at 16
+// rows the 4096 multiply-adds a key (32 cycles of an SM) still take less time
+// than its 1024 bytes. A warp takes 32 keys at a time, a lane each: K and V rows
+// go to shared memory (rows 16 bytes apart more, so that eight lanes' pieces
+// spread over all banks); a lane makes its key's scores; then a lane has four
+// channels (of 64: every second key) and all keys' weights.
+template <int D, int R>
+struct FSmem {
+  static constexpr int kWarps = D == 128 ? 2 : 4;               // three CTAs an SM
+  static constexpr int kRow = D * 4 + 16, kTile = 32 * kRow;   // bytes
+  static constexpr int kWarp = 2 * kTile;                       // K, V
+  static constexpr int kTotal = kWarps * kWarp + R * D * 4 + kWarps * R * 32 * 4;
+  static_assert(R * D * 4 <= kWarp, "a warp's outputs reuse its tiles");
+};
+template <int D, int R>
+__global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(const __grid_constant__ CrossArgs p) {
+  using SM = FSmem<D, R>;
+  constexpr int PF = D + 4, PPR = D / 4, kWarps = SM::kWarps, kThreads = kWarps * 32;
+  extern __shared__ __align__(128) unsigned char dyn[];
+  __shared__ float s_m[kWarps][R], s_l[kWarps][R];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_launch_dependents();
+  const Work w = work_of(p);
+  const int nq = p.group * p.tokens;
+  const int lo = w.sp * p.split_len;
+  const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);
+  const float *K = static_cast<const float *>(p.k) + w.s * p.ks + w.kvh * p.kh;
+  const float *V = static_cast<const float *>(p.v) + w.s * p.ks + w.kvh * p.kh;
+  unsigned char *sk = dyn + warp * SM::kWarp, *sv = sk + SM::kTile;
+  float *sq = reinterpret_cast<float *>(dyn + kWarps * SM::kWarp);         // [R][D]
+  float *sw = sq + R * D + warp * R * 32;                                  // [R][32] weights
+  auto load_rows = [&](unsigned char *to, const float *from, int k0) {
+#pragma unroll 8
+    for (int e = lane; e < 32 * PPR; e += 32) {
+      const int r = e / PPR, c = e % PPR;
+      const bool on = k0 + r < hi;
+      cp_async16_zfill(to + r * SM::kRow + c * 16, from + (on ? (k0 + r) * p.kt : 0) + c * 4, on);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float o[R][4], m[R], l[R];
+  int seen[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    o[r][0] = o[r][1] = o[r][2] = o[r][3] = 0.f;
+    m[r] = kNoKey;
+    l[r] = 0.f;
+    seen[r] = r < nq ? min(keys_seen(p, w, row_of(p, w.kvh, r).token), hi) : 0;
+  }
+  if (lo < hi) {
+    int k0 = lo + warp * 32;
+    if (k0 < hi) {
+      load_rows(sk, K, k0);
+      load_rows(sv, V, k0);
+    }
+    for (int e = tid; e < R * D; e += kThreads) {
+      const int r = e / D;
+      const Row x = row_of(p, w.kvh, min(r, nq - 1));
+      const bool on = r < nq && x.token < w.qlen;
+      sq[e] = on ? static_cast<const float *>(p.q)[w.s * p.qs + x.token * p.qt + x.head * p.qh + e % D] : 0.f;
+    }
+    __syncthreads();
+    for (; k0 < hi; k0 += kWarps * 32) {
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      __syncwarp();
+      float s[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r] = 0.f;
+      const float4 *row = reinterpret_cast<const float4 *>(sk + lane * SM::kRow);
+#pragma unroll 4
+      for (int c = 0; c < PPR; ++c) {
+        const float4 kv = row[c];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float4 qv = reinterpret_cast<const float4 *>(sq + r * D)[c];
+          s[r] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, s[r]))));
+        }
+      }
+      __syncwarp();
+      const int next = k0 + kWarps * 32;
+      if (next < hi) load_rows(sk, K, next);
+      else asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        s[r] = k0 + lane < seen[r] ? s[r] * p.qscale : -INFINITY;
+        float mx = s[r];
+#pragma unroll
+        for (int x = 16; x >= 1; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+        const float mn = fmaxf(m[r], mx), f = mn == m[r] ? 1.f : ex2_approx(m[r] - mn);
+        m[r] = mn;
+        const float e = ex2_approx(s[r] - mn);
+        l[r] = l[r] * f + e;  // this lane's keys
+        sw[r * 32 + lane] = e;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[r][x] *= f;
+      }
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      __syncwarp();
+      // four channels a lane; heads of 64: lanes 16-31 take the odd keys
+      constexpr int KS = 128 / D;
+      const int first = lane / PPR, ch = lane % PPR;
+#pragma unroll 4
+      for (int j = first; j < 32; j += KS) {
+        const float4 vv = *reinterpret_cast<const float4 *>(sv + j * SM::kRow + ch * 16);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float wj = sw[r * 32 + j];
+          o[r][0] = fmaf(wj, vv.x, o[r][0]);
+          o[r][1] = fmaf(wj, vv.y, o[r][1]);
+          o[r][2] = fmaf(wj, vv.z, o[r][2]);
+          o[r][3] = fmaf(wj, vv.w, o[r][3]);
+        }
+      }
+      __syncwarp();
+      if (next < hi) load_rows(sv, V, next);
+      else asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+  }
+  __syncwarp();
+  // the warps joined through shared memory, each in its tiles' place
+  float *so = reinterpret_cast<float *>(sk);  // [R][D]
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int x = 16; x >= 1; x >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], x);
+    if (D == 64) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[r][x] += __shfl_xor_sync(0xFFFFFFFFu, o[r][x], 16);
+    }
+    if (lane == 0) s_m[warp][r] = m[r], s_l[warp][r] = l[r];
+    if (lane < PPR)
+      *reinterpret_cast<float4 *>(so + r * D + lane * 4) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+  }
+  __syncthreads();
+  for (int e = tid; e < nq * PPR; e += kThreads) {
+    const int r = e / PPR, c = e % PPR;
+    float mj = -INFINITY, lj = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) mj = fmaxf(mj, s_m[k][r]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      if (s_l[k][r] == 0.f) continue;
+      const float fk = ex2_approx(s_m[k][r] - mj);
+      const float4 u = reinterpret_cast<const float4 *>(dyn + k * SM::kWarp)[r * PPR + c];
+      lj += s_l[k][r] * fk;
+      v.x += u.x * fk, v.y += u.y * fk, v.z += u.z * fk, v.w += u.w * fk;
+    }
+    const Row x = row_of(p, w.kvh, r);
+    if (x.token >= w.qlen) continue;
+    const size_t row = ((size_t)w.s * p.heads + x.head) * p.tokens + x.token;
+    if (p.splits > 1) {
+      float *part = p.part + (row * p.splits + w.sp) * PF;
+      *reinterpret_cast<float4 *>(part + c * 4) = v;
+      if (c == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(w.bad ? NAN : mj, lj);
+    } else {
+      const float inv = w.bad ? NAN : lj == 0.f ? 0.f : 1.f / lj;
+      store4(static_cast<float *>(p.out) + w.s * p.os + x.token * p.ot + x.head * p.oh + c * 4,
              make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
       if (c == 0 && p.lse) p.lse[row] = w.bad ? NAN : lj == 0.f ? -INFINITY : (mj + log2f(lj)) * kLn2;
     }
@@ -431,33 +491,45 @@ __global__ void __launch_bounds__(kJoinThreads)
   if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-template <int D, typename T, typename O, int MW>
-cudaError_t launch_tiles(const CrossArgs &a, int grid, cudaStream_t s) {
-  constexpr int smem = CSmem<D, T, MW>::kTotal;
+template <int D, typename O>
+cudaError_t launch_rows(const CrossArgs &a, int grid, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(cross_kernel<D, T, O, MW>, smem, ready);
+  const cudaError_t e = allow_smem_of(cross_kernel<D, O>, CSmem<D>::kTotal, ready);
   if (e != cudaSuccess) return e;
-  return pdl_launch(cross_kernel<D, T, O, MW>, grid, kThreads, smem, s, a);
+  return pdl_launch(cross_kernel<D, O>, grid, kThreads, CSmem<D>::kTotal, s, a);
+}
+template <int D, int R>
+cudaError_t launch_few(const CrossArgs &a, int grid, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(cross_few_kernel<D, R>, FSmem<D, R>::kTotal, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(cross_few_kernel<D, R>, grid, FSmem<D, R>::kWarps * 32, FSmem<D, R>::kTotal, s, a);
 }
 
-template <int D, typename T, typename O>
-cudaError_t launch_rows(const CrossArgs &a, const CrossPlan &pl, cudaStream_t s) {
+template <int D>
+cudaError_t launch(const CrossArgs &a, const CrossPlan &pl, int dtype, int out_dtype, cudaStream_t s) {
   const long long grid = (long long)a.seqs * a.kv * a.tiles * a.splits;
   if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidValue;
+  const int g = (int)grid, rows = a.group * a.tokens;
   cudaError_t e;
-  if constexpr (sizeof(O) == 2) {  // (more than 16 rows are the tcgen05 kernel's)
-    e = pl.rows >= 128 ? launch_cross_tc(a, pl, D, s) : launch_tiles<D, T, O, 1>(a, (int)grid, s);
+  if (pl.rows > 16) {
+    e = out_dtype == HKV_BF16 ? launch_cross_tc(a, pl, D, s) : launch_cross_parts(a, D, dtype, s);
+  } else if (dtype == HKV_BF16) {
+    e = out_dtype == HKV_BF16 ? launch_rows<D, bf16>(a, g, s) : launch_rows<D, float>(a, g, s);
   } else {
-    if (pl.rows == 16) e = launch_tiles<D, T, O, 1>(a, (int)grid, s);
-    else if (pl.rows == 32) e = launch_tiles<D, T, O, 2>(a, (int)grid, s);
-    else e = launch_tiles<D, T, O, 4>(a, (int)grid, s);
+    e = rows == 1 ? launch_few<D, 1>(a, g, s) : rows <= 4 ? launch_few<D, 4>(a, g, s)
+                                                          : launch_few<D, 16>(a, g, s);
   }
   if (e != cudaSuccess || a.splits == 1) return e;
   // a warp a query, or eight where there are many ranges
-  const long long rows = (long long)a.seqs * a.heads * a.tokens;
-  if (a.splits > 16)
-    return pdl_launch(cross_join_kernel<D, O, 8>, (int)rows, kJoinThreads, 0, s, a, rows);
-  return pdl_launch(cross_join_kernel<D, O, 1>, (int)((rows + 7) / 8), kJoinThreads, 0, s, a, rows);
+  const long long queries = (long long)a.seqs * a.heads * a.tokens;
+  const bool many = a.splits > 16;
+  const int blocks = (int)(many ? queries : (queries + 7) / 8);
+  if (out_dtype == HKV_BF16)
+    return pdl_launch(many ? cross_join_kernel<D, bf16, 8> : cross_join_kernel<D, bf16, 1>, blocks,
+                      kJoinThreads, 0, s, a, queries);
+  return pdl_launch(many ? cross_join_kernel<D, float, 8> : cross_join_kernel<D, float, 1>, blocks,
+                    kJoinThreads, 0, s, a, queries);
 }
 
 }  // namespace
@@ -470,15 +542,16 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   constexpr int kMostSplits = 456;
   CrossPlan pl;
   const long long all = (long long)(heads / kv) * tokens;
-  const bool tc = dtype == HKV_BF16 && out_dtype == HKV_BF16 && all > 16;
+  const bool tc = all > 16 && out_dtype == HKV_BF16;
 #ifdef HKV_TC_ROWS
   if (tc) pl.rows = HKV_TC_ROWS;
+  else pl.rows = all > 16 ? 128 : 16;
 #else
-  if (tc) pl.rows = all > 128 ? 256 : 128;
+  pl.rows = all <= 16 ? 16 : tc && all > 128 ? 256 : 128;
 #endif
-  else pl.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
+  // keys of a tile; CTAs that the device holds at a time
   const int tile = tc ? 128 : kKeys;
-  const int ctas = pl.rows == 256 ? 152 : pl.rows == 16 && dtype == HKV_BF16 ? 456 : dtype == HKV_BF16 ? 304 : 152;
+  const int ctas = pl.rows == 16 ? 456 : tc && pl.rows == 128 ? 304 : 152;
   // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as
   // many heads of a group as fit 128 rows
   const int group = heads / kv;
@@ -510,12 +583,7 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
 
 cudaError_t launch_cross(const CrossArgs &a, const CrossPlan &pl, int D, int dtype, int out_dtype,
                          cudaStream_t s) {
-  if (dtype == HKV_BF16 && out_dtype == HKV_BF16)
-    return D == 64 ? launch_rows<64, __nv_bfloat16, __nv_bfloat16>(a, pl, s)
-                   : launch_rows<128, __nv_bfloat16, __nv_bfloat16>(a, pl, s);
-  cudaError_t e = cudaErrorInvalidValue;
-  HKV_DISPATCH(D, dtype, e = (launch_rows<kD, kT, float>(a, pl, s)));
-  return e;
+  return D == 64 ? launch<64>(a, pl, dtype, out_dtype, s) : launch<128>(a, pl, dtype, out_dtype, s);
 }
 
 }  // namespace hkv

@@ -70,7 +70,8 @@ __device__ __forceinline__ int keys_of_rows(const CrossArgs &p, const Work &w, i
   return keys_seen(p, w, min(last, w.qlen - 1));
 }
 
-// the tcgen05 kernel (bf16 in and out); plan.rows is 128 or 256
+// more than 16 query rows: bf16 in and out (plan.rows is 128 or 256), and fp32 outs
 cudaError_t launch_cross_tc(const CrossArgs &a, const CrossPlan &plan, int D, cudaStream_t s);
+cudaError_t launch_cross_parts(const CrossArgs &a, int D, int dtype, cudaStream_t s);
 
 }  // namespace hkv

@@ -354,6 +354,13 @@ CROSS = [
     ("fp32", "fp32", 64, 2, 3, 3, 1, 63),
     ("fp32", "fp32", 128, 2, 2, 1, 37, 200),
     ("fp32", "fp32", 64, 1, 8, 4, 130, 777),
+    ("fp32", "fp32", 128, 2, 4, 4, 1, 333),        # no tensor core: 1, 4, 16 rows
+    ("fp32", "fp32", 64, 2, 6, 2, 1, 2100),
+    ("fp32", "fp32", 128, 2, 4, 2, 8, 1500),
+    ("fp32", "fp32", 64, 1, 4, 2, 7, 31),
+    ("fp32", "fp32", 128, 2, 2, 2, 300, 400),      # three query tiles, several key tiles
+    ("bf16", "fp32", 64, 2, 4, 2, 200, 500),
+    ("bf16", "fp32", 64, 1, 2, 1, 9, 1300),
     ("bf16", "bf16", 64, 2, 4, 2, 100, 64),
     ("bf16", "bf16", 128, 2, 3, 3, 257, 300),
     ("bf16", "bf16", 64, 3, 4, 1, 130, 513),
