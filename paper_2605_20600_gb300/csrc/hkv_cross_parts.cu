@@ -9,7 +9,8 @@
 //   0-3    a thread per row: scores (TMEM) to weights, parts of weights to TMEM
 //   4-7    a thread per row: O = O f + (W V of the tile), O in registers: chained
 //          in the tensor core its sums would truncate once per 16 keys
-//   8-11   loads of Q, K and V, cut into parts in shared memory
+//   8-11   loads of Q, and then of K (two warps) and of V, cut into parts in
+//          shared memory
 //   12     issues the products; S of a tile is computed while the weights of the
 //          one before are made (two buffers of S, of the last parts and of O)
 #include "hkv_cross.cuh"
@@ -30,9 +31,26 @@ struct PartsSmem {
   static constexpr int kQPlane = kRows * D * 2, kPlane = kKeys * D * 2;
   static constexpr int kQ = kPlanes * kQPlane, kTile = kPlanes * kPlane;
   static constexpr int kOut = kRows * D * 4;   // the outs, where Q, K and V were
-  static constexpr int kUsed = kQ + 2 * kTile > kOut ? kQ + 2 * kTile : kOut;
+  static constexpr int kStages = kQ + 4 * kTile <= 220 * 1024 ? 2 : 1;  // of K and of V
+  static constexpr int kUsed = kQ + 2 * kStages * kTile > kOut ? kQ + 2 * kStages * kTile : kOut;
   static constexpr int kBytes = 1024 + kUsed;
 };
+
+// A pair of fp32 as three bf16 parts of falling size; the remainders are exact.
+// ANY: the first part stays finite where an element lies above the largest bf16
+// number.
+template <bool ANY>
+__device__ __forceinline__ void split3(uint64_t x, uint32_t (&p)[3]) {
+  const uint64_t minus = pair_of(-1.f, -1.f);
+#pragma unroll
+  for (int j = 0; j < 3; ++j) {
+    if (ANY && j == 0)
+      asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(p[0]) : "f"(high(x)), "f"(low(x)));
+    else
+      p[j] = pack2(low(x), high(x));
+    if (j < 2) x = fma2(pair_of(p[j] << 16, p[j] & 0xFFFF0000u), minus, x);
+  }
+}
 
 // The 8 elements of a piece as they lie in global memory.
 template <typename T>
@@ -57,7 +75,7 @@ __device__ __forceinline__ void put_piece(unsigned char *dst, int plane, const R
   uint32_t p[4][3];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    split2<true>(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]), p[j]);
+    split3<true>(pair_of(x[2 * j], x[2 * j + 1]), p[j]);
 #pragma unroll
   for (int k = 0; k < 3; ++k)
     *reinterpret_cast<uint4 *>(dst + k * plane) = make_uint4(p[0][k], p[1][k], p[2][k], p[3][k]);
@@ -70,22 +88,24 @@ __device__ __forceinline__ int piece_of(int r, int c) {
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_constant__ CrossArgs p) {
   using SM = PartsSmem<D, T>;
-  constexpr int NP = SM::kPlanes, PF = D + 4, PPR = D / 8;
+  constexpr int NP = SM::kPlanes, ST = SM::kStages, PF = D + 4, PPR = D / 8;
   extern __shared__ unsigned char dyn_raw[];
-  __shared__ uint64_t s_kf, s_ke, s_vf, s_ve;            // K and V: filled, free again
+  __shared__ uint64_t s_kvf[2][ST], s_kve[2][ST], s_q;   // K and V: filled, free again
   __shared__ uint64_t s_s[2], s_p[2], s_o[2], s_oe[2];   // S, W and O of a tile ready; O taken
   __shared__ uint64_t s_drain;
   __shared__ uint32_t s_tmem;
   __shared__ float s_f[2][kRows], s_ml[2][kRows];
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
-  unsigned char *sk = dyn + SM::kQ, *sv = sk + SM::kTile;
+  unsigned char *skv = dyn + SM::kQ;  // K's places, then V's
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   if (tid == 0) {
-    mbar_init(&s_kf, 4);
-    mbar_init(&s_ke, 1);
-    mbar_init(&s_vf, 4);
-    mbar_init(&s_ve, 1);
+    for (int j = 0; j < ST; ++j)
+      for (int kv = 0; kv < 2; ++kv) {
+        mbar_init(&s_kvf[kv][j], 2);
+        mbar_init(&s_kve[kv][j], 1);
+      }
+    mbar_init(&s_q, 4);
     for (int b = 0; b < 2; ++b) {
       mbar_init(&s_s[b], 1);
       mbar_init(&s_p[b], 4);
@@ -115,24 +135,22 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
   bool ok = true;
   float acc[D];  // warps 4-7
   if (n > 0 && warp >= 8 && warp < 12) {
-    const int lt = tid - 8 * 32;
-    const T *K = static_cast<const T *>(p.k) + w.s * p.ks + w.kvh * p.kh + lo * p.kt;
-    const T *V = static_cast<const T *>(p.v) + w.s * p.ks + w.kvh * p.kh + lo * p.kt;
-    constexpr int E = kKeys * PPR / 128;  // pieces a thread of a tile
+    const int kv = (warp - 8) >> 1, lt = tid & 63;
+    const T *from = static_cast<const T *>(kv ? p.v : p.k) + w.s * p.ks + w.kvh * p.kh + lo * p.kt;
+    // a tile in chunks of eight pieces a thread; the next chunk is on its way
+    // while a place for it is waited for
+    constexpr int E = 8, CH = kKeys * PPR / 64 / E, ROWS = kKeys / CH;
     RawPiece<T> next[E];
-    // loads go K, V of tile 0, K, V of tile 1, ...; the next one's are on their
-    // way while this one's place is waited for
     auto fetch = [&](int u) {
-      const T *from = (u & 1) ? V : K;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int r = (u >> 1) * kKeys + (lt + e * 128) / PPR, c = (lt + e * 128) % PPR;
+        const int r = u * ROWS + (lt + e * 64) / PPR, c = (lt + e * 64) % PPR;
         const bool on = lo + r < hi;
         next[e] = raw_piece<T>(from + (on ? r * p.kt : 0) + c * 8, on);
       }
     };
     fetch(0);
-    for (int e = lt; e < kRows * PPR; e += 128) {
+    for (int e = tid - 8 * 32; e < kRows * PPR; e += 128) {
       const int r = e / PPR, c = e % PPR;
       const Row x = row_of(p, w.kvh, min(r0 + r, all - 1));
       const bool on = r0 + r < all && x.token < w.qlen;
@@ -140,24 +158,34 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
                 raw_piece<T>(static_cast<const T *>(p.q) + w.s * p.qs +
                                  (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on));
     }
-    for (int u = 0; u < 2 * n && ok; ++u) {
-      const int i = u >> 1;
-      if (i > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait((u & 1) ? &s_ve : &s_ke, (i - 1) & 1));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s_q);
+    for (int u = 0; u < n * CH && ok; ++u) {
+      const int i = u / CH, j = i % ST;
+      if (u % CH == 0 && i >= ST)
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_kve[kv][j], (i / ST - 1) & 1));
       if (!ok) break;
-      unsigned char *dst = (u & 1) ? sv : sk;
+      unsigned char *dst = skv + (kv * ST + j) * SM::kTile;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        put_piece(dst + piece_of<kKeys>((lt + e * 128) / PPR, (lt + e * 128) % PPR), SM::kPlane, next[e]);
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive((u & 1) ? &s_vf : &s_kf);
-      if (u + 1 < 2 * n) fetch(u + 1);
+        put_piece(dst + piece_of<kKeys>(u % CH * ROWS + (lt + e * 64) / PPR, (lt + e * 64) % PPR),
+                  SM::kPlane, next[e]);
+      if (u % CH == CH - 1) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_kvf[kv][j]);
+      }
+      if (u + 1 < n * CH) fetch(u + 1);
     }
   } else if (n > 0 && warp == 12) {
-    const uint32_t q_at = smem_u32(dyn), k_at = smem_u32(sk), v_at = smem_u32(sv);
+    const uint32_t q_at = smem_u32(dyn);
+    auto filled = [&](int kv, int i) {
+      return __all_sync(0xFFFFFFFFu, mbar_wait(&s_kvf[kv][i % ST], (i / ST) & 1));
+    };
     auto scores = [&](int i) {  // S of tile i
       if (elect_one()) {
-        const uint32_t s = tmem + kS + (i & 1) * 64;
+        const uint32_t s = tmem + kS + (i & 1) * 64, k_at = smem_u32(skv) + i % ST * SM::kTile;
         bool add = false;
 #pragma unroll
         for (int order = NP - 1; order >= 0; --order)
@@ -174,25 +202,27 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
             }
           }
         tc_commit(&s_s[i & 1]);
-        tc_commit(&s_ke);
+        tc_commit(&s_kve[0][i % ST]);
       }
       __syncwarp();
     };
-    ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_kf, 0));
+    ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_q, 0)) && filled(0, 0);
+    tc_fence_after();
     if (ok) scores(0);
     for (int i = 0; i < n && ok; ++i) {
       const int b = i & 1;
       if (i + 1 < n) {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_kf, (i + 1) & 1));
+        ok = filled(0, i + 1);
         if (!ok) break;
         scores(i + 1);  // over the weights of tile i - 1, after the products that read them
       }
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_vf, i & 1));
+      ok = filled(1, i);
       if (ok && i > 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_oe[b], ((i >> 1) - 1) & 1));
       ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(&s_p[b], (i >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
+        const uint32_t v_at = smem_u32(skv) + (ST + i % ST) * SM::kTile;
         bool add = false;
 #pragma unroll
         for (int order = 2; order >= 0; --order)
@@ -209,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
             }
           }
         tc_commit(&s_o[b]);
-        tc_commit(&s_ve);
+        tc_commit(&s_kve[1][i % ST]);
       }
       __syncwarp();
     }
@@ -257,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
           l0 += w0;
           l1 += w1;
           uint32_t part[3];
-          split2<false>(w0, w1, part);
+          split3<false>(pair_of(w0, w1), part);
 #pragma unroll
           for (int k = 0; k < 3; ++k) wp[k][j / 2] = part[k];
         }
