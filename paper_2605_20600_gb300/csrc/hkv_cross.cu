@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kThreads, 3) cross_kernel(const __grid_constan
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  const Work w = work_of(p);
+  const Work w = work_of(p, blockIdx.x);
   const int nq = p.group * p.tokens;  // query rows of the (sequence, key head)
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  const Work w = work_of(p);
+  const Work w = work_of(p, blockIdx.x);
   const int nq = p.group * p.tokens;
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);

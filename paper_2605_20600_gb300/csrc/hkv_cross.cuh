@@ -22,9 +22,8 @@ struct Work {
   int qlen, klen;         // 0 where a length is out of range
   bool bad;               // the states' length is: NaN
 };
-__device__ __forceinline__ Work work_of(const CrossArgs &p) {
+__device__ __forceinline__ Work work_of(const CrossArgs &p, int b) {
   Work w;
-  int b = blockIdx.x;
   w.tile = p.tiles - 1 - b % p.tiles;  // causal: the longest rows of keys first
   b /= p.tiles;
   w.kvh = b % p.kv;

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
     tmem_alloc(&s_tmem, kCols);
     pdl_launch_dependents();
   }
-  const Work w = work_of(p);
+  const Work w = work_of(p, blockIdx.x);
   const int all = p.group * p.tokens, r0 = w.tile * kRows;
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, r0, min(all, r0 + kRows)), lo + p.split_len);

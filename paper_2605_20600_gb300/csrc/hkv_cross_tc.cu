@@ -34,7 +34,9 @@ struct TcPlan {
   // slots of the ring: slot p % kSlots holds K of key tile p and V of tile p - 1,
   // which the products need together
   static constexpr int kSlots = TILES * (D == 64 ? 2 : 1);
-  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kQ;
+  // channels of a row that go out at a time, through a warp's piece of shared memory
+  static constexpr int kOut = TILES == 2 ? 64 : 32;
+  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kQ + TILES * 4 * 32 * kOut * 2;
   static constexpr int kParts = TILES == 1 ? 2 : 1;  // bf16 parts of a weight
   static constexpr int kCols = TILES * 256;         // TMEM: S of each tile, then O of each
 };
@@ -53,6 +55,39 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// the query tiles of a CTA's work
+template <int TILES>
+struct Item {
+  Work w;
+  int lo;                            // first key
+  int head0[TILES], token0[TILES];   // heads within the group
+  int n[TILES], most;                // key tiles
+  bool any;                          // rows to write
+};
+template <int TILES>
+__device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
+  Item<TILES> x;
+  x.w = work_of(p, index);
+  x.lo = x.w.sp * p.split_len;
+  x.most = 0;
+  x.any = false;
+  const int token_tiles = (p.tokens + p.box_tokens - 1) / p.box_tokens;
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int u = x.w.tile * TILES + t, h = u / token_tiles;
+    x.head0[t] = h * p.box_heads;
+    x.token0[t] = (u - h * token_tiles) * p.box_tokens;
+    int hi = 0;
+    const bool live = x.head0[t] < p.group && x.token0[t] < x.w.qlen;
+    x.any |= live;
+    if (live)
+      hi = min(keys_seen(p, x.w, min(x.token0[t] + p.box_tokens, x.w.qlen) - 1), x.lo + p.split_len);
+    x.n[t] = hi > x.lo ? (hi - x.lo + kTile - 1) / kTile : 0;
+    x.most = max(x.most, x.n[t]);
+  }
+  return x;
+}
+
 template <int D, int TILES>
 __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
     cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap qmap,
@@ -61,15 +96,26 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   using TP = TcPlan<D, TILES>;
   constexpr int PF = D + 4, SLOTS = TP::kSlots;
   extern __shared__ unsigned char dyn_raw[];
+  __shared__ __align__(16) uint4 s_answer;            // to the load warp: another CTA's work
+  __shared__ uint64_t s_asked;
+  __shared__ int s_item[2];                           // the CTA's items, and whether they are
+  __shared__ uint64_t s_nf[2], s_ne[2];               // there, and read by the other warps
   __shared__ uint64_t s_full[SLOTS], s_empty[SLOTS];  // slots of the ring
   __shared__ uint64_t s_s[TILES], s_p[TILES];         // S is ready (and O holds what came before); W is
-  __shared__ uint64_t s_q[TILES], s_edge, s_drain;
+  __shared__ uint64_t s_q[TILES], s_qe[TILES];        // Q is there; its last product is done
+  __shared__ uint64_t s_oe[TILES];                    // O has been read
+  __shared__ uint64_t s_edge, s_drain;
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
-  unsigned char *ring = dyn + TILES * TP::kQ;
+  unsigned char *ring = dyn + TILES * TP::kQ, *stage = ring + SLOTS * 2 * TP::kQ;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_nf[i], 1);
+      mbar_init(&s_ne[i], TILES * 4 + 1);
+    }
+    mbar_init(&s_asked, 1);
     for (int i = 0; i < SLOTS; ++i) {
       mbar_init(&s_full[i], 1);
       mbar_init(&s_empty[i], 1);
@@ -78,6 +124,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       mbar_init(&s_s[t], 1);
       mbar_init(&s_p[t], 4);
       mbar_init(&s_q[t], 1);
+      mbar_init(&s_qe[t], 1);
+      mbar_init(&s_oe[t], 4);
     }
     mbar_init(&s_edge, 1);
     mbar_init(&s_drain, 1);
@@ -92,78 +140,114 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     tmem_alloc(&s_tmem, TP::kCols);
     pdl_launch_dependents();
   }
-  const Work w = work_of(p);
-  const int lo = w.sp * p.split_len;
-  const int token_tiles = (p.tokens + p.box_tokens - 1) / p.box_tokens;
-  int head0[TILES], token0[TILES];  // of the query tiles, heads within the group
-  int n[TILES], most = 0;           // their key tiles
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    const int u = w.tile * TILES + t;
-    head0[t] = u / token_tiles * p.box_heads;
-    token0[t] = u % token_tiles * p.box_tokens;
-    int hi = 0;
-    if (head0[t] < p.group && token0[t] < w.qlen)
-      hi = min(keys_seen(p, w, min(token0[t] + p.box_tokens, w.qlen) - 1), lo + p.split_len);
-    n[t] = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
-    most = max(most, n[t]);
-  }
+  Item<TILES> x = item_of<TILES>(p, blockIdx.x);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, s_tmem, 0);
+  // A wait that runs out fails all that the CTA has still to do: its warps then
+  // only go through the items, and write NaN.
   bool ok = true;
-  float row_m = -INFINITY, row_l = 0.f;
-  int issued = 0;  // loads (the load warp), for the wait of a failed CTA
+  auto wait = [&](uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity));
+  };
+  // The load warp finds the CTA's items, the work of CTAs that were not launched
+  // yet; the others read them, k = 0, 1, ... behind the first, until there is none.
+  auto next_item = [&](int k) {
+    int item = -1;
+    if (wait(&s_nf[k & 1], (k >> 1) & 1)) item = s_item[k & 1];
+    else ok = false;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s_ne[k & 1]);
+    if (item >= 0) x = item_of<TILES>(p, item);
+    return item >= 0;
+  };
   if (warp == TILES * 4) {
-    if (lane == 0) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        if (n[t] == 0) continue;
-        mbar_arrive_expect_tx(&s_q[t], p.box_tokens * p.box_heads * D * 2);
-#pragma unroll
-        for (int c = 0; c < D; c += 64)
-          tma_tile(dyn + t * TP::kQ + (c >> 6) * kTile * 128, &qmap, c, token0[t],
-                   w.kvh * p.group + head0[t], w.s, &s_q[t]);
-      }
-    }
-    for (int j = 0; most > 0 && j <= most && ok; ++j) {
-      const int slot = j % SLOTS, k0 = lo + j * kTile, past = k0 - w.klen;
-      if (j >= SLOTS) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_empty[slot], (j / SLOTS - 1) & 1));
-      if (!ok) break;
-      unsigned char *dst = ring + slot * 2 * TP::kQ;
-      const bool edge = past > 0;  // V's tile is the sequence's last, and not a whole one
-      if (lane == 0) {
-        uint64_t *bar = edge ? &s_edge : &s_full[slot];
-        mbar_arrive_expect_tx(bar, ((j < most) + (j > 0)) * TP::kQ);
-#pragma unroll
-        for (int c = 0; c < D; c += 64) {
-          if (j < most) tma_tile(dst + (c >> 6) * kTile * 128, &kmap, c, k0, w.kvh, w.s, bar);
-          if (j > 0) tma_tile(dst + TP::kQ + (c >> 6) * kTile * 128, &vmap, c, k0 - kTile, w.kvh, w.s, bar);
-        }
-      }
-      ++issued;
-      if (edge) {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_edge, 0));
+    // loads: Q and the ring's slots, as far ahead as there is room, of the next
+    // item too
+    uint32_t slots = 0, queries[TILES] = {}, edges = 0;  // so far
+    uint32_t asked = 0;
+    for (int k = 0, item = 0; item >= 0; ++k) {
+      for (int j = 0; x.most > 0 && j <= x.most && ok; ++j, ++slots) {
+        const uint32_t slot = slots % SLOTS;
+        const int k0 = x.lo + j * kTile, past = k0 - x.w.klen;
+        if (slots >= SLOTS) ok = wait(&s_empty[slot], (slots / SLOTS - 1) & 1);
         if (!ok) break;
-        for (int e = lane; e < past * (D / 8); e += 32) {
-          const int r = kTile - past + e / (D / 8), c = e % (D / 8);
-          *reinterpret_cast<uint4 *>(dst + TP::kQ + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
-              make_uint4(0, 0, 0, 0);
+        unsigned char *dst = ring + slot * 2 * TP::kQ;
+        const bool edge = past > 0;  // V's tile is the sequence's last, and not a whole one
+        if (lane == 0) {
+          uint64_t *bar = edge ? &s_edge : &s_full[slot];
+          mbar_arrive_expect_tx(bar, ((j < x.most) + (j > 0)) * TP::kQ);
+#pragma unroll
+          for (int c = 0; c < D; c += 64) {
+            if (j < x.most) tma_tile(dst + (c >> 6) * kTile * 128, &kmap, c, k0, x.w.kvh, x.w.s, bar);
+            if (j > 0)
+              tma_tile(dst + TP::kQ + (c >> 6) * kTile * 128, &vmap, c, k0 - kTile, x.w.kvh, x.w.s, bar);
+          }
         }
+        if (j == 0) {
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) {
+            if (x.n[t] == 0) continue;
+            if (queries[t] > 0) ok = ok && wait(&s_qe[t], (queries[t] - 1) & 1);
+            if (!ok) break;
+            ++queries[t];
+            if (lane == 0) {
+              mbar_arrive_expect_tx(&s_q[t], p.box_tokens * p.box_heads * D * 2);
+#pragma unroll
+              for (int c = 0; c < D; c += 64)
+                tma_tile(dyn + t * TP::kQ + (c >> 6) * kTile * 128, &qmap, c, x.token0[t],
+                         x.w.kvh * p.group + x.head0[t], x.w.s, &s_q[t]);
+            }
+          }
+        }
+        if (edge) {
+          ok = ok && wait(&s_edge, edges++ & 1);
+          if (!ok) break;
+          for (int e = lane; e < past * (D / 8); e += 32) {
+            const int r = kTile - past + e / (D / 8), c = e % (D / 8);
+            *reinterpret_cast<uint4 *>(dst + TP::kQ + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
+                make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_full[slot]);
+        }
+      }
+      // the next item that has rows to write; asked for only now, so that what is
+      // left at the end goes to the CTA that is free first
+      do {
+        if (lane == 0) next_cta_ask(&s_answer, &s_asked);
+        item = -1;
+        if (wait(&s_asked, asked++ & 1)) item = next_cta(&s_answer);
+        else ok = false;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_full[slot]);
+        if (item >= 0) x = item_of<TILES>(p, item);
+      } while (item >= 0 && !x.any);
+      if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
+        ok = false;
+        break;
       }
+      if (lane == 0) {
+        s_item[k & 1] = item;
+        mbar_arrive(&s_nf[k & 1]);
+      }
+    }
+    if (!ok) {  // what was issued may still run: the limit once more
+      for (uint32_t j = slots > SLOTS ? slots - SLOTS : 0; j < slots; ++j)
+        mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+        if (queries[t] > 0) mbar_wait(&s_q[t], (queries[t] - 1) & 1);
     }
   } else if (warp > TILES * 4) {
     // products, issued by one lane; the whole warp waits. The tiles take turns,
     // one's weights are made during the other's products.
     const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(dyn);
-    auto here = [&](int j) {  // slot j is filled
-      return __all_sync(0xFFFFFFFFu, mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1));
-    };
-    auto scores = [&](int t, int j) {  // S of tile t with the K tile of slot j
+    uint32_t slots = 0, queries[TILES] = {}, weights[TILES] = {};  // used so far
+    auto here = [&](uint32_t j) { return wait(&s_full[j % SLOTS], (j / SLOTS) & 1); };
+    auto scores = [&](int t, uint32_t j, bool last) {  // S of tile t with the K tile of slot j
       const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kQ, 16);
       const uint64_t qd = tc_desc(q_at + t * TP::kQ, 16);
 #pragma unroll
@@ -172,205 +256,218 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         tc_mma(tmem + t * 128, qd + at, kd + at, tc_instr(kTile, kTile, false), ks > 0);
       }
       tc_commit(&s_s[t]);
+      if (last) tc_commit(&s_qe[t]);
     };
-    if (most > 0) {
-      ok = here(0);
+    int k = 0;
+    do {
+      if (x.most > 0 && ok) {
+        ok = here(slots);
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
-        if (ok && n[t] > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_q[t], 0));
-      if (ok) {
-        tc_fence_after();
-        if (elect_one()) {
+        for (int t = 0; t < TILES; ++t)
+          if (ok && x.n[t] > 0) ok = wait(&s_q[t], queries[t]++ & 1);
+        if (ok) {
+          tc_fence_after();
+          if (elect_one()) {
 #pragma unroll
-          for (int t = 0; t < TILES; ++t)
-            if (n[t] > 0) scores(t, 0);
-          tc_commit(&s_empty[0]);
-        }
-        __syncwarp();
-        ok = here(1);
-      }
-    }
-    for (int i = 0; i < most && ok; ++i) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        const bool mine = i < n[t];
-        if (mine) ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(&s_p[t], i & 1));
-        if (!ok) continue;
-        tc_fence_after();
-        if (elect_one()) {
-          if (mine) {
-            const uint64_t vd = tc_desc(ring_at + ((i + 1) % SLOTS) * 2 * TP::kQ + TP::kQ, kTile * 128);
-#pragma unroll
-            for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
-#pragma unroll
-              for (int kk = 0; kk < kTile / 16; ++kk)
-                tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + part * 64 + kk * 8,
-                          vd + kk * (16 * 128 >> 4), tc_instr(kTile, D, true),
-                          i > 0 || kk > 0 || part < TP::kParts - 1);
-            if (i + 1 < n[t]) scores(t, i + 1);  // over the weights, after the products that read them
-            else tc_commit(&s_s[t]);
+            for (int t = 0; t < TILES; ++t)
+              if (x.n[t] > 0) scores(t, slots, x.n[t] == 1);
+            tc_commit(&s_empty[slots % SLOTS]);
           }
-          if (t == TILES - 1) tc_commit(&s_empty[(i + 1) % SLOTS]);
-        }
-        __syncwarp();
-      }
-      if (ok && i + 1 < most) ok = here(i + 2);
-    }
-  } else {
-    const int t = warp >> 2;
-    const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t mine_o = mine + TILES * 128;
-    int seen = keys_seen(p, w, token0[t] + (tid & 127) % p.box_tokens);
-    seen = min(seen, lo + p.split_len);
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < n[t]; ++i) {
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[t], i & 1));
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t s[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s[c], mine + c * 32);
-      tmem_wait_ld();
-      const int left = seen - lo - i * kTile;  // keys of the tile that count
-      if (left < kTile) {
-#pragma unroll
-        for (int j = 0; j < kTile; ++j)
-          if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
-      }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int j = 0; j < kTile; j += 8)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
-                        __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
-      float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      mx *= p.qscale;
-      float f = 1.f;
-      if (mx > m + 8.f) {
-        f = ex2_approx(m - mx);  // (zero for the first keys)
-        m = mx;
-        l *= f;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;  // no key yet: weights of zero
-      if (i > 0 && __any_sync(0xFFFFFFFFu, f != 1.f)) {
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          tmem_ld32(o, mine_o + c);
-          tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-          tmem_st32(mine_o + c, o);
+          __syncwarp();
+          ok = here(slots + 1);
         }
       }
-      const uint64_t scale2 = pair_of(p.qscale, p.qscale);
-      const uint64_t ref2 = pair_of(-ref, -ref);
-      uint64_t sum[2] = {0, 0};
+      for (int i = 0; i < x.most && ok; ++i) {
+        const uint32_t j = slots + i + 1;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t v[16], v2[16];
+        for (int t = 0; t < TILES; ++t) {
+          const bool mine = i < x.n[t];
+          if (mine) {
+            // O of the item before has been read
+            if (i == 0 && queries[t] > 1) ok = ok && wait(&s_oe[t], queries[t] & 1);
+            ok = ok && wait(&s_p[t], weights[t]++ & 1);
+          }
+          if (!ok) continue;
+          tc_fence_after();
+          if (elect_one()) {
+            if (mine) {
+              const uint64_t vd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kQ + TP::kQ, kTile * 128);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const uint64_t e = fma2(pair_of(s[c][2 * j], s[c][2 * j + 1]), scale2, ref2);
-          const float w0 = ex2_approx(low(e)), w1 = ex2_approx(high(e));
-          sum[j & 1] = add2(sum[j & 1], pair_of(w0, w1));
-          v[j] = pack2(w0, w1);
-          if (TP::kParts == 2)
-            v2[j] = pack2(w0 - __uint_as_float(v[j] << 16), w1 - __uint_as_float(v[j] & 0xFFFF0000u));
+              for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
+#pragma unroll
+                for (int kk = 0; kk < kTile / 16; ++kk)
+                  tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + part * 64 + kk * 8,
+                            vd + kk * (16 * 128 >> 4), tc_instr(kTile, D, true),
+                            i > 0 || kk > 0 || part < TP::kParts - 1);
+              // over the weights, after the products that read them
+              if (i + 1 < x.n[t]) scores(t, j, i + 2 == x.n[t]);
+              else tc_commit(&s_s[t]);
+            }
+            if (t == TILES - 1) tc_commit(&s_empty[j % SLOTS]);
+          }
+          __syncwarp();
         }
-        tmem_st16(mine + c * 16, v);
-        if (TP::kParts == 2) tmem_st16(mine + 64 + c * 16, v2);
+        if (ok && i + 1 < x.most) ok = here(j + 1);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s_p[t]);
-      sum[0] = add2(sum[0], sum[1]);
-      l += low(sum[0]) + high(sum[0]);
-    }
-    // O is complete
-    if (ok && n[t] > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[t], n[t] & 1));
-    row_m = m;
-    row_l = l;
-  }
-  // one wait that ran out fails the whole CTA
-  const bool failed = __syncthreads_or(!ok);
-  if (failed) {
-    // copies and products that were issued may still run: they get the limit
-    // once more before their place and the TMEM are used again
-    if (warp > TILES * 4 && elect_one()) {
+      if (x.most > 0) slots += x.most + 1;
+    } while (next_item(k++));
+    if (!ok && elect_one()) {
       set_err(p.err, HKV_ERR_TIMEOUT);
       tc_commit(&s_drain);
     }
-    if (warp == TILES * 4) {
-      for (int t = 0; t < TILES; ++t)
-        if (n[t] > 0) mbar_wait(&s_q[t], 0);
-      for (int j = max(0, issued - SLOTS); j < issued; ++j)
-        mbar_wait(&s_full[j % SLOTS], (j / SLOTS) & 1);
-    }
-    mbar_wait(&s_drain, 0);
-    __syncthreads();
-  }
-  tc_fence_after();
-  if (warp < TILES * 4) {
-    const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens;
-    const uint32_t mine_o = tmem + (TILES + t) * 128 + ((uint32_t)((warp & 3) * 32) << 16);
-    const float m = row_m, l = row_l;
-    const int token = token0[t] + r - h * p.box_tokens, head = w.kvh * p.group + head0[t] + h;
-    const bool live = h < p.box_heads && head0[t] + h < p.group && token < w.qlen;
-    const bool wrong = w.bad || failed, any = n[t] > 0 && !failed;
-    const size_t row = ((size_t)w.s * p.heads + head) * p.tokens + token;
-    if (p.splits > 1) {
-      float *part = p.part + (row * p.splits + w.sp) * PF;
+    if (!ok) mbar_wait(&s_drain, 0);
+  } else {
+    const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens, token_in = r - h * p.box_tokens;
+    const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t mine_o = mine + TILES * 128;
+    unsigned char *rows = stage + warp * 32 * TP::kOut * 2;
+    uint32_t phase = 0;                         // of S
+    int k = 0;
+    do {
+      const int n = TILES == 2 && t ? x.n[TILES - 1] : x.n[0];
+      const int first = TILES == 2 && t ? x.token0[TILES - 1] : x.token0[0];
+      const int head0 = TILES == 2 && t ? x.head0[TILES - 1] : x.head0[0], token = first + token_in;
+      const int seen = min(keys_seen(p, x.w, token), x.lo + p.split_len);
+      float m = -INFINITY, l = 0.f;
+      for (int i = 0; i < n && ok; ++i) {
+        ok = wait(&s_s[t], phase++ & 1);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(s[c], mine + c * 32);
+        tmem_wait_ld();
+        const int left = seen - x.lo - i * kTile;  // keys of the tile that count
+        if (left < kTile) {
+#pragma unroll
+          for (int j = 0; j < kTile; ++j)
+            if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kTile; j += 8)
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
+                          __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
+        float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        mx *= p.qscale;
+        float f = 1.f;
+        if (mx > m + 8.f) {
+          f = ex2_approx(m - mx);  // (zero for the first keys)
+          m = mx;
+          l *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;  // no key yet: weights of zero
+        if (i > 0 && __any_sync(0xFFFFFFFFu, f != 1.f)) {
 #pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32] = {};
-        if (any) {
-          tmem_ld32(o, mine_o + c);
-          tmem_wait_ld();
-        }
-        if (!live) continue;
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(o, mine_o + c);
+            tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<uint4 *>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st32(mine_o + c, o);
+          }
+        }
+        const uint64_t scale2 = pair_of(p.qscale, p.qscale), ref2 = pair_of(-ref, -ref);
+        uint64_t sum[2] = {0, 0};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t v[16], v2[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const uint64_t e = fma2(pair_of(s[c][2 * j], s[c][2 * j + 1]), scale2, ref2);
+            const float w0 = ex2_approx(low(e)), w1 = ex2_approx(high(e));
+            sum[j & 1] = add2(sum[j & 1], pair_of(w0, w1));
+            v[j] = pack2(w0, w1);
+            if (TP::kParts == 2)
+              v2[j] = pack2(w0 - __uint_as_float(v[j] << 16), w1 - __uint_as_float(v[j] & 0xFFFF0000u));
+          }
+          tmem_st16(mine + c * 16, v);
+          if (TP::kParts == 2) tmem_st16(mine + 64 + c * 16, v2);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_p[t]);
+        sum[0] = add2(sum[0], sum[1]);
+        l += low(sum[0]) + high(sum[0]);
       }
-      if (live) *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
-    } else {
-      // rows to shared memory, in the place of Q's, then whole rows out
-      const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
-      unsigned char *rows = dyn + t * TP::kQ + (warp & 3) * 32 * D * 2;
+      // O is complete
+      if (ok && n > 0) ok = wait(&s_s[t], phase++ & 1);
+      tc_fence_after();
+      const int head = x.w.kvh * p.group + head0 + h;
+      const bool live = h < p.box_heads && head0 + h < p.group && token < x.w.qlen;
+      const bool wrong = x.w.bad || !ok, any = n > 0 && ok;
+      const size_t row = ((size_t)x.w.s * p.heads + head) * p.tokens + token;
+      auto o_read = [&] {  // the next item's products may overwrite O
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_oe[t]);
+      };
+      if (p.splits > 1) {
+        float *part = p.part + (row * p.splits + x.w.sp) * PF;
 #pragma unroll 1
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32] = {};
-        if (any) {
-          tmem_ld32(o, mine_o + c);
-          tmem_wait_ld();
-        }
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32] = {};
+          if (any) {
+            tmem_ld32(o, mine_o + c);
+            tmem_wait_ld();
+          }
+          if (!live) continue;
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          uint32_t v[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            v[k] = pack2(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-          *reinterpret_cast<uint4 *>(rows + at16<D>(lane, (c + e) >> 3)) = make_uint4(v[0], v[1], v[2], v[3]);
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<uint4 *>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
+        if (any) o_read();
+        if (live) *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
+      } else {
+        // kOut channels at a time to shared memory, then whole rows of them out
+        const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
+        __nv_bfloat16 *to =
+            static_cast<__nv_bfloat16 *>(p.out) + x.w.s * p.os + token * p.ot + head * p.oh;
+        constexpr int CH = TP::kOut, PPR = CH / 8;
+        auto at = [](int rr, int c) {
+          return rr * CH * 2 + ((c ^ (CH == 64 ? rr & 7 : (rr >> 1) & 3)) << 4);
+        };
+#pragma unroll 1
+        for (int c = 0; c < D; c += CH) {
+#pragma unroll
+          for (int c1 = 0; c1 < CH; c1 += 32) {
+            uint32_t o[32] = {};
+            if (any) {
+              tmem_ld32(o, mine_o + c + c1);
+              tmem_wait_ld();
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                v[i] = pack2(__uint_as_float(o[e * 8 + 2 * i]) * inv,
+                             __uint_as_float(o[e * 8 + 2 * i + 1]) * inv);
+              *reinterpret_cast<uint4 *>(rows + at(lane, c1 / 8 + e)) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+          }
+          if (any && c + CH == D) o_read();
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 32; i += 32 / PPR) {
+            const int rr = i + lane / PPR, pc = lane % PPR;
+            const bool on = __shfl_sync(0xFFFFFFFFu, live, rr);
+            __nv_bfloat16 *row_at = reinterpret_cast<__nv_bfloat16 *>(
+                __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), rr));
+            if (on)
+              *reinterpret_cast<uint4 *>(row_at + c + pc * 8) =
+                  *reinterpret_cast<const uint4 *>(rows + at(rr, pc));
+          }
+          __syncwarp();
+        }
+        if (live && p.lse) p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       }
-      __syncwarp();
-      __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(p.out) + w.s * p.os + token * p.ot + head * p.oh;
-      constexpr int PPR = D / 8, RPP = 32 / PPR;  // pieces a row, rows a pass
-#pragma unroll 4
-      for (int i = 0; i < 32; i += RPP) {
-        const int rr = i + lane / PPR;
-        const bool on = __shfl_sync(0xFFFFFFFFu, live, rr);
-        __nv_bfloat16 *at = reinterpret_cast<__nv_bfloat16 *>(
-            __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), rr));
-        if (on)
-          *reinterpret_cast<uint4 *>(at + (lane % PPR) * 8) =
-              *reinterpret_cast<const uint4 *>(rows + at16<D>(rr, lane % PPR));
-      }
-      if (live && p.lse) p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-    }
+    } while (next_item(k++));
+    if (!ok && lane == 0) set_err(p.err, HKV_ERR_TIMEOUT);
   }
   tc_fence_before();
   __syncthreads();

@@ -124,4 +124,30 @@ __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
                : "memory");
 }
 
+// Asks for the next CTA of the grid that has not been launched, to do its work
+// here; the answer lands in *to (16 bytes, aligned) and counts on `bar`. Not
+// again after an answer that there is none.
+__device__ __forceinline__ void next_cta_ask(uint4 *to, uint64_t *bar) {
+  mbar_arrive_expect_tx(bar, 16);
+  asm volatile(
+      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+          smem_u32(to)),
+      "r"(smem_u32(bar))
+      : "memory");
+}
+// its blockIdx.x, or -1
+__device__ __forceinline__ int next_cta(const uint4 *to) {
+  uint32_t x, there;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %1, 1, 0, p;\n\tmov.u32 %0, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+      : "=r"(x), "=r"(there)
+      : "r"(smem_u32(to))
+      : "memory");
+  return there ? (int)x : -1;
+}
+
 }  // namespace hkv
