@@ -25,20 +25,20 @@
 namespace hkv {
 namespace {
 
-constexpr int kTile = 128;  // queries of a tile, and keys of one
+constexpr int kTile = 128, kKeys = 64;  // queries of a tile, keys of one
 
 template <int D, int TILES>
 struct TcPlan {
-  static constexpr int kThreads = TILES * 128 + 64;
-  static constexpr int kQ = kTile * D * 2;          // bytes of a query tile, and of a K or V tile
+  static constexpr int kThreads = TILES * 160 + 32;
+  static constexpr int kQ = kTile * D * 2, kKV = kKeys * D * 2;  // bytes of a query tile, of a K or V tile
   // slots of the ring: slot p % kSlots holds K of key tile p and V of tile p - 1,
   // which the products need together
-  static constexpr int kSlots = TILES * (D == 64 ? 2 : 1);
+  static constexpr int kSlots = TILES * (D == 64 ? 4 : 2);
   // channels of a row that go out at a time, through a warp's piece of shared memory
   static constexpr int kOut = TILES == 2 ? 64 : 32;
-  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kQ + TILES * 4 * 32 * kOut * 2;
+  static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kKV + TILES * 4 * 32 * kOut * 2;
   static constexpr int kParts = TILES == 1 ? 2 : 1;  // bf16 parts of a weight
-  static constexpr int kCols = TILES * 256;         // TMEM: S of each tile, then O of each
+  static constexpr int kCols = TILES * 256;         // TMEM: two buffers of S of each tile, then O of each
 };
 
 __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int c, int row, int head,
@@ -82,7 +82,7 @@ __device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
     x.any |= live;
     if (live)
       hi = min(keys_seen(p, x.w, min(x.token0[t] + p.box_tokens, x.w.qlen) - 1), x.lo + p.split_len);
-    x.n[t] = hi > x.lo ? (hi - x.lo + kTile - 1) / kTile : 0;
+    x.n[t] = hi > x.lo ? (hi - x.lo + kKeys - 1) / kKeys : 0;
     x.most = max(x.most, x.n[t]);
   }
   return x;
@@ -101,34 +101,38 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   __shared__ int s_item[2];                           // the CTA's items, and whether they are
   __shared__ uint64_t s_nf[2], s_ne[2];               // there, and read by the other warps
   __shared__ uint64_t s_full[SLOTS], s_empty[SLOTS];  // slots of the ring
-  __shared__ uint64_t s_s[TILES], s_p[TILES];         // S is ready (and O holds what came before); W is
+  __shared__ uint64_t s_s[TILES][2], s_p[TILES][2];   // S and W of a key tile are ready
+  __shared__ uint64_t s_v[TILES];                     // O holds a key tile's products
   __shared__ uint64_t s_q[TILES], s_qe[TILES];        // Q is there; its last product is done
   __shared__ uint64_t s_oe[TILES];                    // O has been read
   __shared__ uint64_t s_edge, s_drain;
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
-  unsigned char *ring = dyn + TILES * TP::kQ, *stage = ring + SLOTS * 2 * TP::kQ;
+  unsigned char *ring = dyn + TILES * TP::kQ, *stage = ring + SLOTS * 2 * TP::kKV;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_nf[i], 1);
-      mbar_init(&s_ne[i], TILES * 4 + 1);
+      mbar_init(&s_ne[i], TILES * 5);
     }
     mbar_init(&s_asked, 1);
     for (int i = 0; i < SLOTS; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&s_empty[i], 1);
+      mbar_init(&s_empty[i], TILES);
     }
     for (int t = 0; t < TILES; ++t) {
-      mbar_init(&s_s[t], 1);
-      mbar_init(&s_p[t], 4);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(&s_s[t][b], 1);
+        mbar_init(&s_p[t][b], 4);
+      }
+      mbar_init(&s_v[t], 1);
       mbar_init(&s_q[t], 1);
       mbar_init(&s_qe[t], 1);
       mbar_init(&s_oe[t], 4);
     }
     mbar_init(&s_edge, 1);
-    mbar_init(&s_drain, 1);
+    mbar_init(&s_drain, TILES);
     fence_barrier_init();
   }
   // TMEM only after the wait, and the next kernel's CTAs only after TMEM: an
@@ -170,19 +174,19 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     for (int k = 0, item = 0; item >= 0; ++k) {
       for (int j = 0; x.most > 0 && j <= x.most && ok; ++j, ++slots) {
         const uint32_t slot = slots % SLOTS;
-        const int k0 = x.lo + j * kTile, past = k0 - x.w.klen;
+        const int k0 = x.lo + j * kKeys, past = k0 - x.w.klen;
         if (slots >= SLOTS) ok = wait(&s_empty[slot], (slots / SLOTS - 1) & 1);
         if (!ok) break;
-        unsigned char *dst = ring + slot * 2 * TP::kQ;
+        unsigned char *dst = ring + slot * 2 * TP::kKV;
         const bool edge = past > 0;  // V's tile is the sequence's last, and not a whole one
         if (lane == 0) {
           uint64_t *bar = edge ? &s_edge : &s_full[slot];
-          mbar_arrive_expect_tx(bar, ((j < x.most) + (j > 0)) * TP::kQ);
+          mbar_arrive_expect_tx(bar, ((j < x.most) + (j > 0)) * TP::kKV);
 #pragma unroll
           for (int c = 0; c < D; c += 64) {
-            if (j < x.most) tma_tile(dst + (c >> 6) * kTile * 128, &kmap, c, k0, x.w.kvh, x.w.s, bar);
+            if (j < x.most) tma_tile(dst + (c >> 6) * kKeys * 128, &kmap, c, k0, x.w.kvh, x.w.s, bar);
             if (j > 0)
-              tma_tile(dst + TP::kQ + (c >> 6) * kTile * 128, &vmap, c, k0 - kTile, x.w.kvh, x.w.s, bar);
+              tma_tile(dst + TP::kKV + (c >> 6) * kKeys * 128, &vmap, c, k0 - kKeys, x.w.kvh, x.w.s, bar);
           }
         }
         if (j == 0) {
@@ -205,8 +209,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           ok = ok && wait(&s_edge, edges++ & 1);
           if (!ok) break;
           for (int e = lane; e < past * (D / 8); e += 32) {
-            const int r = kTile - past + e / (D / 8), c = e % (D / 8);
-            *reinterpret_cast<uint4 *>(dst + TP::kQ + (c >> 3) * kTile * 128 + r * 128 + ((c & 7) << 4)) =
+            const int r = kKeys - past + e / (D / 8), c = e % (D / 8);
+            *reinterpret_cast<uint4 *>(dst + TP::kKV + (c >> 3) * kKeys * 128 + r * 128 + ((c & 7) << 4)) =
                 make_uint4(0, 0, 0, 0);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -242,72 +246,66 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         if (queries[t] > 0) mbar_wait(&s_q[t], (queries[t] - 1) & 1);
     }
   } else if (warp > TILES * 4) {
-    // products, issued by one lane; the whole warp waits. The tiles take turns,
-    // one's weights are made during the other's products.
-    const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(dyn);
-    uint32_t slots = 0, queries[TILES] = {}, weights[TILES] = {};  // used so far
+    // products of one query tile, issued by one lane; the whole warp waits. A warp
+    // for each tile, so that one's products run while the other waits. S of the
+    // next key tile is computed before the weights of this one are there.
+    const int t = warp - TILES * 4 - 1;
+    const uint32_t ring_at = smem_u32(ring), at_s = tmem + t * 128, at_o = tmem + TILES * 128 + t * 128;
+    const uint64_t qd = tc_desc(smem_u32(dyn) + t * TP::kQ, 16);
+    uint32_t slots = 0, queries = 0, steps = 0;  // used so far: slots, items, key tiles
     auto here = [&](uint32_t j) { return wait(&s_full[j % SLOTS], (j / SLOTS) & 1); };
-    auto scores = [&](int t, uint32_t j, bool last) {  // S of tile t with the K tile of slot j
-      const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kQ, 16);
-      const uint64_t qd = tc_desc(q_at + t * TP::kQ, 16);
+    auto scores = [&](uint32_t step, uint32_t j, bool last) {  // S with the K tile of slot j
+      if (elect_one()) {
+        const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kKV, 16);
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {  // 16 channels: 32 bytes of a column block
-        const uint64_t at = ((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4;
-        tc_mma(tmem + t * 128, qd + at, kd + at, tc_instr(kTile, kTile, false), ks > 0);
+        for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
+          tc_mma(at_s + (step & 1) * 64, qd + (((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4),
+                 kd + (((ks >> 2) * kKeys * 128 + (ks & 3) * 32) >> 4), tc_instr(kTile, kKeys, false),
+                 ks > 0);
+        tc_commit(&s_s[t][step & 1]);
+        if (last) tc_commit(&s_qe[t]);
       }
-      tc_commit(&s_s[t]);
-      if (last) tc_commit(&s_qe[t]);
+      __syncwarp();
     };
     int k = 0;
     do {
-      if (x.most > 0 && ok) {
-        ok = here(slots);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t)
-          if (ok && x.n[t] > 0) ok = wait(&s_q[t], queries[t]++ & 1);
+      const int n = TILES == 2 && t ? x.n[TILES - 1] : x.n[0];
+      if (n > 0 && ok) {
+        ok = here(slots) && wait(&s_q[t], queries++ & 1);
         if (ok) {
           tc_fence_after();
-          if (elect_one()) {
-#pragma unroll
-            for (int t = 0; t < TILES; ++t)
-              if (x.n[t] > 0) scores(t, slots, x.n[t] == 1);
-            tc_commit(&s_empty[slots % SLOTS]);
-          }
+          scores(steps, slots, n == 1);
+          if (elect_one()) tc_commit(&s_empty[slots % SLOTS]);
           __syncwarp();
-          ok = here(slots + 1);
         }
       }
-      for (int i = 0; i < x.most && ok; ++i) {
-        const uint32_t j = slots + i + 1;
+      for (int i = 0; i < n && ok; ++i, ++steps) {
+        const uint32_t j = slots + i + 1, b = steps & 1;
+        ok = here(j);
+        if (!ok) break;
+        tc_fence_after();
+        if (i + 1 < n) scores(steps + 1, j, i + 2 == n);
+        if (i == 0 && queries > 1) ok = wait(&s_oe[t], queries & 1);  // O of the item before has been read
+        ok = ok && wait(&s_p[t][b], (steps >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t vd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kKV + TP::kKV, kKeys * 128);
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          const bool mine = i < x.n[t];
-          if (mine) {
-            // O of the item before has been read
-            if (i == 0 && queries[t] > 1) ok = ok && wait(&s_oe[t], queries[t] & 1);
-            ok = ok && wait(&s_p[t], weights[t]++ & 1);
-          }
-          if (!ok) continue;
-          tc_fence_after();
-          if (elect_one()) {
-            if (mine) {
-              const uint64_t vd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kQ + TP::kQ, kTile * 128);
+          for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
 #pragma unroll
-              for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
-#pragma unroll
-                for (int kk = 0; kk < kTile / 16; ++kk)
-                  tc_mma_ta(tmem + TILES * 128 + t * 128, tmem + t * 128 + part * 64 + kk * 8,
-                            vd + kk * (16 * 128 >> 4), tc_instr(kTile, D, true),
-                            i > 0 || kk > 0 || part < TP::kParts - 1);
-              // over the weights, after the products that read them
-              if (i + 1 < x.n[t]) scores(t, j, i + 2 == x.n[t]);
-              else tc_commit(&s_s[t]);
-            }
-            if (t == TILES - 1) tc_commit(&s_empty[j % SLOTS]);
-          }
-          __syncwarp();
+            for (int kk = 0; kk < kKeys / 16; ++kk)
+              tc_mma_ta(at_o, at_s + b * 64 + part * 32 + kk * 8, vd + kk * (16 * 128 >> 4),
+                        tc_instr(kTile, D, true), i > 0 || kk > 0 || part < TP::kParts - 1);
+          tc_commit(&s_v[t]);
+          tc_commit(&s_empty[j % SLOTS]);
         }
-        if (ok && i + 1 < x.most) ok = here(j + 1);
+        __syncwarp();
+      }
+      // slots that only the other tile uses are given back as they come
+      for (int j = n == 0 ? 0 : n + 1; x.most > 0 && j <= x.most && ok; ++j) {
+        ok = here(slots + j);
+        if (ok && lane == 0) mbar_arrive(&s_empty[(slots + j) % SLOTS]);
       }
       if (x.most > 0) slots += x.most + 1;
     } while (next_item(k++));
@@ -315,13 +313,14 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       set_err(p.err, HKV_ERR_TIMEOUT);
       tc_commit(&s_drain);
     }
+    if (ok && elect_one()) mbar_arrive(&s_drain);
     if (!ok) mbar_wait(&s_drain, 0);
   } else {
     const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens, token_in = r - h * p.box_tokens;
     const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t mine_o = mine + TILES * 128;
     unsigned char *rows = stage + warp * 32 * TP::kOut * 2;
-    uint32_t phase = 0;                         // of S
+    uint32_t steps = 0;                         // key tiles so far
     int k = 0;
     do {
       const int n = TILES == 2 && t ? x.n[TILES - 1] : x.n[0];
@@ -329,23 +328,24 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       const int head0 = TILES == 2 && t ? x.head0[TILES - 1] : x.head0[0], token = first + token_in;
       const int seen = min(keys_seen(p, x.w, token), x.lo + p.split_len);
       float m = -INFINITY, l = 0.f;
-      for (int i = 0; i < n && ok; ++i) {
-        ok = wait(&s_s[t], phase++ & 1);
+      for (int i = 0; i < n && ok; ++i, ++steps) {
+        const uint32_t b = steps & 1, mine_s = mine + b * 64;
+        ok = wait(&s_s[t][b], (steps >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        uint32_t s[4][32];
+        uint32_t s[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(s[c], mine + c * 32);
+        for (int c = 0; c < 2; ++c) tmem_ld32(s[c], mine_s + c * 32);
         tmem_wait_ld();
-        const int left = seen - x.lo - i * kTile;  // keys of the tile that count
-        if (left < kTile) {
+        const int left = seen - x.lo - i * kKeys;  // keys of the tile that count
+        if (left < kKeys) {
 #pragma unroll
-          for (int j = 0; j < kTile; ++j)
+          for (int j = 0; j < kKeys; ++j)
             if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
         }
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < kTile; j += 8)
+        for (int j = 0; j < kKeys; j += 8)
 #pragma unroll
           for (int u = 0; u < 4; ++u)
             top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
@@ -359,7 +359,16 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           l *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m;  // no key yet: weights of zero
-        if (i > 0 && __any_sync(0xFFFFFFFFu, f != 1.f)) {
+        const bool rescale = __any_sync(0xFFFFFFFFu, f != 1.f);
+        // O holds the tiles before this one. (A wait names a phase by its parity:
+        // those two before have passed with S, and the one of the last tile but one
+        // is waited for here, before the last one's can pass.)
+        if (i > 0 && (rescale || i + 1 == n)) {
+          ok = wait(&s_v[t], (steps - 1) & 1);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        if (i > 0 && rescale) {
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             uint32_t o[32];
@@ -373,7 +382,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         const uint64_t scale2 = pair_of(p.qscale, p.qscale), ref2 = pair_of(-ref, -ref);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
           uint32_t v[16], v2[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -384,18 +393,18 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
             if (TP::kParts == 2)
               v2[j] = pack2(w0 - __uint_as_float(v[j] << 16), w1 - __uint_as_float(v[j] & 0xFFFF0000u));
           }
-          tmem_st16(mine + c * 16, v);
-          if (TP::kParts == 2) tmem_st16(mine + 64 + c * 16, v2);
+          tmem_st16(mine_s + c * 16, v);
+          if (TP::kParts == 2) tmem_st16(mine_s + 32 + c * 16, v2);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s_p[t]);
+        if (lane == 0) mbar_arrive(&s_p[t][b]);
         sum[0] = add2(sum[0], sum[1]);
         l += low(sum[0]) + high(sum[0]);
       }
       // O is complete
-      if (ok && n > 0) ok = wait(&s_s[t], phase++ & 1);
+      if (ok && n > 0) ok = wait(&s_v[t], (steps - 1) & 1);
       tc_fence_after();
       const int head = x.w.kvh * p.group + head0 + h;
       const bool live = h < p.box_heads && head0 + h < p.group && token < x.w.qlen;
@@ -516,8 +525,8 @@ cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
   CUtensorMap q, k, v;
   if (e == cudaSuccess)
     e = encode(&q, a.q, D, a.tokens, a.qt, a.heads, a.qh, a.seqs, a.qs, a.box_tokens, a.box_heads);
-  if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kTile, 1);
-  if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kTile, 1);
+  if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kKeys, 1);
+  if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kKeys, 1);
   if (e != cudaSuccess) return e;
   return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v);
 }
