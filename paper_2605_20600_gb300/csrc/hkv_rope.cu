@@ -100,6 +100,11 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
   const uint32_t place = group * x.tokens + tok;
   bool on = (int)tok < x.tokens && place < places;
   const int s = on ? place / (uint32_t)a.tokens : 0, t = on ? place - (uint32_t)s * a.tokens : 0;
+  // (the position is on its way while the length is)
+  int pos[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    pos[k] = on && x.rotate && k < a.rope.n_axes ? a.pos[k * a.pa + s * a.ps + t] : 0;
   if (on) on = t < tokens_of(a, s);
   // (whole groups of G lanes, a power of two, are on or off together)
   const int R = x.rotate ? a.rope.rot_dim : 0;
@@ -137,10 +142,6 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
         P::unpack(*reinterpret_cast<const Raw *>(b + step), bb);
       }
       if (rows > 0 && R > 0) {
-        int pos[3];
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-          pos[k] = k < a.rope.n_axes ? a.pos[k * a.pa + s * a.ps + t] : 0;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           float cc[2] = {1.f, 1.f}, ss[2] = {0.f, 0.f};
