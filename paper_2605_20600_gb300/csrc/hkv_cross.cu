@@ -17,28 +17,28 @@
 namespace hkv {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
 constexpr int kKeys = 64;  // keys of a tile
 
 constexpr int kStages = 2;
 using bf16 = __nv_bfloat16;
 
-template <int D>
+template <int D, int W>
 struct CSmem {
-  static constexpr int kPlane = kKeys * D * 2;     // K or V of a tile
+  static constexpr int kKeys = W * 16;             // of a tile
+  static constexpr int kPlane = kKeys * D * 2;     // K or V of one
   static constexpr int kTiles = kStages * 2 * kPlane;
   static constexpr int kTotal = kTiles + 16 * D * 2;
-  static_assert(kWarps * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
+  static_assert(W * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
 };
 
-template <int D, typename O>
-__global__ void __launch_bounds__(kThreads, 3) cross_kernel(const __grid_constant__ CrossArgs p) {
-  using SM = CSmem<D>;
+template <int D, typename O, int W>
+__global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(const __grid_constant__ CrossArgs p) {
+  using SM = CSmem<D, W>;
+  constexpr int kKeys = SM::kKeys, kThreads = W * 32;
   constexpr int WP = sizeof(O) == 4 ? 3 : 2;  // parts of a weight
   constexpr int PF = D + 4, PPR = D / 8;
   extern __shared__ __align__(128) unsigned char dyn[];
-  __shared__ float s_m[kWarps][16], s_l[kWarps][16];
+  __shared__ float s_m[W][16], s_l[W][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
@@ -206,10 +206,10 @@ __global__ void __launch_bounds__(kThreads, 3) cross_kernel(const __grid_constan
     const int r = e / (D / 4), c = e % (D / 4);
     float mj = -INFINITY, lj = 0.f;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) mj = fmaxf(mj, s_m[k][r]);
+    for (int k = 0; k < W; ++k) mj = fmaxf(mj, s_m[k][r]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
+    for (int k = 0; k < W; ++k) {
       if (s_l[k][r] == 0.f) continue;
       const float fk = ex2_approx(s_m[k][r] - mj);
       const float4 u = *reinterpret_cast<const float4 *>(so + (size_t)(k * 16 + r) * D + c * 4);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kJoinThreads)
     l = l * old + sum;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] *= old;
-    constexpr int B = 8;
+    constexpr int B = W > 1 ? 16 : 8;
     for (int j = 0; j < here; j += B) {
       float v[B][E];
 #pragma unroll
@@ -491,12 +491,22 @@ __global__ void __launch_bounds__(kJoinThreads)
   if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+template <int D, typename O, int W>
+cudaError_t launch_warps(const CrossArgs &a, int grid, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(cross_kernel<D, O, W>, CSmem<D, W>::kTotal, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(cross_kernel<D, O, W>, grid, W * 32, CSmem<D, W>::kTotal, s, a);
+}
+// Twelve warps an SM as CTAs of two, whose starts and ends lie apart more, as
+// soon as there are enough of them: one query of 64 x 32 heads over up to 300
+// states takes 32 us, as CTAs of four 35, of one 37. Few CTAs of some length have
+// eight: 32 heads over 300 states take 6.5 us, with four 6.7; over 1000 12.6 and 16.
 template <int D, typename O>
 cudaError_t launch_rows(const CrossArgs &a, int grid, cudaStream_t s) {
-  static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(cross_kernel<D, O>, CSmem<D>::kTotal, ready);
-  if (e != cudaSuccess) return e;
-  return pdl_launch(cross_kernel<D, O>, grid, kThreads, CSmem<D>::kTotal, s, a);
+  if (grid >= 912) return launch_warps<D, O, 2>(a, grid, s);
+  if (grid <= 152 && a.split_len > 128) return launch_warps<D, O, 8>(a, grid, s);
+  return launch_warps<D, O, 4>(a, grid, s);
 }
 template <int D, int R>
 cudaError_t launch_few(const CrossArgs &a, int grid, cudaStream_t s) {
@@ -549,8 +559,7 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
 #else
   pl.rows = all <= 16 ? 16 : tc && all > 128 ? 256 : 128;
 #endif
-  // keys of a tile; CTAs that the device holds at a time
-  const int tile = tc ? 128 : kKeys;
+  // CTAs that the device holds at a time
   const int ctas = pl.rows == 16 ? 456 : tc && pl.rows == 128 ? 304 : 152;
   // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as
   // many heads of a group as fit 128 rows
@@ -566,15 +575,15 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
     pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
   }
   const long long base = (long long)seqs * kv * pl.tiles;
-  // several rounds of CTAs, or one, and no range that takes less time than its
-  // partial result is worth
-  constexpr int kLeast = 512;
-  long long want = base < ctas ? ctas / base : 1;
-  if (pl.rows == 16 && base >= ctas && base < 4LL * ctas) want = (4LL * ctas + base - 1) / base;
+  // One round of CTAs, or (few query rows, whose partial results are small) four;
+  // ranges long enough that joining them pays: a CTA takes about 3 us and 0.9 (16
+  // rows) or 0.5 more for 64 keys, and the join 2.5.
+  long long want = base < ctas ? ctas / base : 1, least = pl.rows == 16 ? 192 : 256;
+  if (pl.rows == 16 && base >= ctas && base < 4LL * ctas) want = (4LL * ctas + base - 1) / base, least = 512;
   if (want > kMostSplits) want = kMostSplits;
-  if (want > keys / kLeast) want = keys / kLeast;
-  if (want < 1) want = 1;
-  pl.split_len = (int)(((keys + want - 1) / want + tile - 1) / tile * tile);
+  if (want > keys / least) want = keys / least;
+  if (want < 1 || keys < 512) want = 1;
+  pl.split_len = (int)(((keys + want - 1) / want + kKeys - 1) / kKeys * kKeys);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
   pl.part_bytes =
       pl.splits > 1 ? (size_t)seqs * heads * tokens * pl.splits * (D + 4) * sizeof(float) : 0;
