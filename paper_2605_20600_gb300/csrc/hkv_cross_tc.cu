@@ -247,25 +247,25 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     }
   } else if (warp > TILES * 4) {
     // products of one query tile, issued by one lane; the whole warp waits. A warp
-    // for each tile, so that one's products run while the other waits. S of the
-    // next key tile is computed before the weights of this one are there.
+    // for each tile, so that one's products run while the other waits. With two
+    // query tiles the scores of two key tiles are computed ahead; then a key tile's
+    // weights take their V, and the scores of the tile after the next take the place
+    // that they leave: one wait for 512 cycles of products. With one, whose ring is
+    // shorter, the scores of the next tile only, before the weights are there.
     const int t = warp - TILES * 4 - 1;
     const uint32_t ring_at = smem_u32(ring), at_s = tmem + t * 128, at_o = tmem + TILES * 128 + t * 128;
     const uint64_t qd = tc_desc(smem_u32(dyn) + t * TP::kQ, 16);
     uint32_t slots = 0, queries = 0, steps = 0;  // used so far: slots, items, key tiles
     auto here = [&](uint32_t j) { return wait(&s_full[j % SLOTS], (j / SLOTS) & 1); };
     auto scores = [&](uint32_t step, uint32_t j, bool last) {  // S with the K tile of slot j
-      if (elect_one()) {
-        const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kKV, 16);
+      const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kKV, 16);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
-          tc_mma(at_s + (step & 1) * 64, qd + (((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4),
-                 kd + (((ks >> 2) * kKeys * 128 + (ks & 3) * 32) >> 4), tc_instr(kTile, kKeys, false),
-                 ks > 0);
-        tc_commit(&s_s[t][step & 1]);
-        if (last) tc_commit(&s_qe[t]);
-      }
-      __syncwarp();
+      for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
+        tc_mma(at_s + (step & 1) * 64, qd + (((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4),
+               kd + (((ks >> 2) * kKeys * 128 + (ks & 3) * 32) >> 4), tc_instr(kTile, kKeys, false),
+               ks > 0);
+      tc_commit(&s_s[t][step & 1]);
+      if (last) tc_commit(&s_qe[t]);
     };
     int k = 0;
     do {
@@ -274,19 +274,37 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         ok = here(slots) && wait(&s_q[t], queries++ & 1);
         if (ok) {
           tc_fence_after();
-          scores(steps, slots, n == 1);
-          if (elect_one()) tc_commit(&s_empty[slots % SLOTS]);
+          if (elect_one()) {
+            scores(steps, slots, n == 1);
+            tc_commit(&s_empty[slots % SLOTS]);
+          }
           __syncwarp();
+          if (TILES == 2) ok = here(slots + 1);
+          if (ok && TILES == 2 && n > 1) {
+            tc_fence_after();
+            if (elect_one()) scores(steps + 1, slots + 1, n == 2);
+            __syncwarp();
+          }
+          if (ok && queries > 1) ok = wait(&s_oe[t], queries & 1);  // O of the item before has been read
         }
       }
       for (int i = 0; i < n && ok; ++i, ++steps) {
-        const uint32_t j = slots + i + 1, b = steps & 1;
-        ok = here(j);
-        if (!ok) break;
-        tc_fence_after();
-        if (i + 1 < n) scores(steps + 1, j, i + 2 == n);
-        if (i == 0 && queries > 1) ok = wait(&s_oe[t], queries & 1);  // O of the item before has been read
-        ok = ok && wait(&s_p[t][b], (steps >> 1) & 1);
+        const uint32_t j = slots + i + 1, b = steps & 1;  // the slot of V; of K after the next: j + 1
+        uint64_t *weights = &s_p[t][b], *keys = &s_full[(j + 1) % SLOTS];
+        const uint32_t wp = (steps >> 1) & 1, kp = ((j + 1) / SLOTS) & 1;
+        if (TILES == 2) {
+          const bool w_here = mbar_try_wait(weights, wp), k_here = i + 2 > n || mbar_try_wait(keys, kp);
+          if (!__all_sync(0xFFFFFFFFu, w_here && k_here))
+            ok = wait(weights, wp) && (i + 2 > n || wait(keys, kp));
+        } else {
+          ok = here(j);
+          if (ok && i + 1 < n) {
+            tc_fence_after();
+            if (elect_one()) scores(steps + 1, j, i + 2 == n);
+            __syncwarp();
+          }
+          ok = ok && wait(weights, wp);
+        }
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
@@ -298,6 +316,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
               tc_mma_ta(at_o, at_s + b * 64 + part * 32 + kk * 8, vd + kk * (16 * 128 >> 4),
                         tc_instr(kTile, D, true), i > 0 || kk > 0 || part < TP::kParts - 1);
           tc_commit(&s_v[t]);
+          if (TILES == 2 && i + 2 < n) scores(steps + 2, j + 1, i + 3 == n);
           tc_commit(&s_empty[j % SLOTS]);
         }
         __syncwarp();
