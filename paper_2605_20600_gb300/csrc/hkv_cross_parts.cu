@@ -252,6 +252,9 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
       const int b = i & 1;
       ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_s[b], (i >> 1) & 1));
       if (ok && i > 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_oe[b], ((i >> 1) - 1) & 1));
+#ifdef HKV_CROSS_TEST_STALL  // one warp waits for a phase that nothing completes before its limit
+      if (warp == (int)(blockIdx.x & 3) && i == 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_drain, 0));
+#endif
       if (!ok) break;
       tc_fence_after();
       uint32_t s[2][32];

@@ -350,6 +350,9 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       for (int i = 0; i < n && ok; ++i, ++steps) {
         const uint32_t b = steps & 1, mine_s = mine + b * 64;
         ok = wait(&s_s[t][b], (steps >> 1) & 1);
+#ifdef HKV_CROSS_TEST_STALL  // one warp waits for a phase that nothing completes before its limit
+        if (warp == (int)(blockIdx.x & 3) && i == 1) ok = wait(&s_drain, 0);
+#endif
         if (!ok) break;
         tc_fence_after();
         uint32_t s[2][32];
