@@ -16,6 +16,12 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *to, float4 v) {
   *reinterpret_cast<uint2 *>(to) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // what a CTA works on
 struct Work {
   int s, kvh, tile, sp;   // sequence, key head, query tile, key range

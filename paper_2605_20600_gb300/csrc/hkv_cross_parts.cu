@@ -216,9 +216,12 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
         if (!ok) break;
         scores(i + 1);  // over the weights of tile i - 1, after the products that read them
       }
-      ok = filled(1, i);
-      if (ok && i > 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&s_oe[b], ((i >> 1) - 1) & 1));
-      ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(&s_p[b], (i >> 1) & 1));
+      // V, W and a place for O, asked for together
+      uint64_t *vf = &s_kvf[1][i % ST], *wf = &s_p[b], *oe = &s_oe[b];
+      const uint32_t vp = (i / ST) & 1, wp = (i >> 1) & 1, op = wp ^ 1;
+      const bool v_here = mbar_try_wait(vf, vp), w_here = mbar_try_wait(wf, wp);
+      if (!__all_sync(0xFFFFFFFFu, v_here && w_here && (i < 2 || mbar_try_wait(oe, op))))
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(vf, vp) && mbar_wait(wf, wp) && (i < 2 || mbar_wait(oe, op)));
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -272,33 +275,34 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
       for (int j = 0; j < kKeys; j += 8)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          top[u] = fmaxf(fmaxf(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u])),
-                         __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
+          top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
+                        __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
       const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.qscale;
       // (the reference stays finite: scores of -inf weigh nothing against it)
       const float mn = fmaxf(m, mx), f = mn == m ? 1.f : ex2_approx(m - mn);
       m = mn;
-      float l0 = 0.f, l1 = 0.f;
+      const uint64_t scale2 = pair_of(p.qscale, p.qscale), ref2 = pair_of(-m, -m);
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int j0 = 0; j0 < kKeys; j0 += 16) {  // 8 columns of each part at a time
         uint32_t wp[3][8];
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) {
-          const int a = j0 + j;
-          const float w0 = ex2_approx(__uint_as_float(s[a >> 5][a & 31]) * p.qscale - m);
-          const float w1 = ex2_approx(__uint_as_float(s[a >> 5][(a & 31) + 1]) * p.qscale - m);
-          l0 += w0;
-          l1 += w1;
+        for (int j = 0; j < 8; ++j) {
+          const int a = j0 + 2 * j;
+          const uint64_t e = fma2(pair_of(s[a >> 5][a & 31], s[a >> 5][(a & 31) + 1]), scale2, ref2);
+          const uint64_t wj = pair_of(ex2_approx(low(e)), ex2_approx(high(e)));
+          sum[j & 1] = add2(sum[j & 1], wj);
           uint32_t part[3];
-          split3<false>(pair_of(w0, w1), part);
+          split3<false>(wj, part);
 #pragma unroll
-          for (int k = 0; k < 3; ++k) wp[k][j / 2] = part[k];
+          for (int k = 0; k < 3; ++k) wp[k][j] = part[k];
         }
         tmem_st8(tmem + lanes + kS + b * 64 + j0 / 2, wp[0]);
         tmem_st8(tmem + lanes + kS + b * 64 + 32 + j0 / 2, wp[1]);
         tmem_st8(tmem + lanes + kThird + b * 32 + j0 / 2, wp[2]);
       }
-      l = l * f + (l0 + l1);
+      sum[0] = add2(sum[0], sum[1]);
+      l = l * f + (low(sum[0]) + high(sum[0]));
       s_f[b][tid] = f;
       tmem_wait_st();
       tc_fence_before();

@@ -50,11 +50,6 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
       : "memory");
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // the query tiles of a CTA's work
 template <int TILES>
 struct Item {

@@ -361,6 +361,9 @@ CROSS = [
     ("fp32", "fp32", 128, 2, 2, 2, 300, 400),      # three query tiles, several key tiles
     ("bf16", "fp32", 64, 2, 4, 2, 200, 500),
     ("bf16", "fp32", 64, 1, 2, 1, 9, 1300),
+    ("fp32", "fp32", 64, 1, 2, 1, 20, 9001),       # many key tiles, several ranges
+    ("bf16", "bf16", 64, 2, 16, 2, 17, 300),       # seven heads a query tile, eight a group
+    ("bf16", "bf16", 64, 3, 64, 64, 300, 300),     # more work than CTAs at a time
     ("bf16", "bf16", 64, 2, 4, 2, 100, 64),
     ("bf16", "bf16", 128, 2, 3, 3, 257, 300),
     ("bf16", "bf16", 64, 3, 4, 1, 130, 513),
