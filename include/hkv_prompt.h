@@ -193,7 +193,9 @@ size_t hkv_cross_workspace_size(const hkv_config *cfg, const hkv_states *states,
  * lse; their products with v take them in three bf16 parts for fp32 outs, and
  * for bf16 outs in two, or, for batches of many queries, rounded to bf16.
  * An infinite or NaN element of a query or of a state that counts shows in the
- * outputs that its products enter as a number that is not finite. A sequence
+ * outputs that its products enter as a number that is not finite; with
+ * HKV_ATTN_CAUSAL one of v may show in earlier queries too, whose weight of zero
+ * it meets. What lies in rows from a length on shows nowhere. A sequence
  * whose number of states is out of range gets NaN, and HKV_ERR_BOUNDS in the
  * states' error word; queries whose products did not finish within the
  * kernel's limit of two seconds get NaN, with HKV_ERR_TIMEOUT. out must not

@@ -553,12 +553,7 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   CrossPlan pl;
   const long long all = (long long)(heads / kv) * tokens;
   const bool tc = all > 16 && out_dtype == HKV_BF16;
-#ifdef HKV_TC_ROWS
-  if (tc) pl.rows = HKV_TC_ROWS;
-  else pl.rows = all > 16 ? 128 : 16;
-#else
   pl.rows = all <= 16 ? 16 : tc && all > 128 ? 256 : 128;
-#endif
   // CTAs that the device holds at a time
   const int ctas = pl.rows == 16 ? 456 : tc && pl.rows == 128 ? 304 : 152;
   // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as

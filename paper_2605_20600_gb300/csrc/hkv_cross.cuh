@@ -39,7 +39,8 @@ __device__ __forceinline__ Work work_of(const CrossArgs &p, int b) {
   w.qlen = p.qlen ? p.qlen[w.s] : p.tokens;
   w.klen = p.klen ? p.klen[w.s] : p.keys;
   w.bad = w.klen < 0 || w.klen > p.keys;
-  const bool first = threadIdx.x == 0 && w.tile == 0 && w.kvh == 0 && w.sp == 0;
+  // (a lane of every warp: not all of them see every piece of work)
+  const bool first = (threadIdx.x & 31) == 0 && w.tile == 0 && w.kvh == 0 && w.sp == 0;
   if (w.bad) {
     if (first) set_err(p.err, HKV_ERR_BOUNDS);
     w.klen = 0;

@@ -276,23 +276,42 @@ def test_lengths_out_of_range(bad):
         H.hkv_rope_rotate(cfg, H.hkv_make_rope(head_dim=D, rot_dim=rot), tok, H.make_rows(x), H.make_rows(out))
         assert int(err) == H.HKV_ERR_BOUNDS
         assert (out[1] == 3.0).all() and torch.equal(out[0], x[0]) and torch.equal(out[2], x[2])
-    # attention: bad numbers of queries leave their outputs, bad numbers of states give NaN
-    k, v = torch.randn(2, S, heads, 9, D, device="cuda").bfloat16()
-    for which in ("queries", "states"):
-        err = ints([0])
-        lens = ints([T if which == "queries" else 9, bad if bad != 6 or which == "queries" else 10, 2])
-        tok = H.make_tokens(T, lens if which == "queries" else None, None, err)
-        st = H.make_states(k, v, lens if which == "states" else None, err)
-        n = H.hkv_cross_workspace_size(cfg, st, tok)
-        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-        out, lse = torch.full_like(x, 3.0), torch.full((S, heads, T), 3.0, device="cuda")
-        H.hkv_cross_attention(cfg, st, tok, H.make_rows(x), H.make_rows(out), lse, ws, n)
-        assert int(err) == H.HKV_ERR_BOUNDS
-        assert torch.isfinite(out[0]).all() and torch.isfinite(out[2]).all()
-        if which == "queries":
-            assert (out[1] == 3.0).all() and (lse[1] == 3.0).all()
-        else:
-            assert torch.isnan(out[1]).all() and torch.isnan(lse[1]).all()
+
+
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+@pytest.mark.parametrize("which", ["queries", "states"])
+@pytest.mark.parametrize("dtype,out,S,T,N", [("bf16", "bf16", 3, 5, 9), ("bf16", "bf16", 3, 5, 4000),
+                                             ("fp32", "fp32", 3, 5, 9), ("bf16", "bf16", 3, 100, 70),
+                                             ("bf16", "bf16", 3, 300, 70), ("bf16", "bf16", 3, 300, 3000),
+                                             ("bf16", "bf16", 400, 300, 70), ("fp32", "fp32", 3, 100, 70),
+                                             ("bf16", "fp32", 3, 100, 2000)])
+def test_attention_lengths_out_of_range(dtype, out, S, T, N, which, bad):
+    """A bad number of queries leaves the sequence's outputs, one of states gives
+    NaN; the error word says so, also where most sequences are empty."""
+    torch, H = mods()
+    heads, D = 2, 64
+    cfg = cfg_of(H, S, heads, D, dtype)
+    q, k, v = qkv(torch, S, T, heads, heads, N, D, dtype)
+    err = ints([0])
+    ql, kl = [T] + [0] * (S - 2) + [max(1, T // 2)], [N] * (S - 1) + [N // 2]
+    (ql if which == "queries" else kl)[1] = bad
+    if which == "states":
+        ql[1] = T
+    tok, st = H.make_tokens(T, ints(ql), None, err), H.make_states(k, v, ints(kl), err)
+    n = H.hkv_cross_workspace_size(cfg, st, tok)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    o = torch.full(q.shape, 3.0, dtype=torch.float32 if out == "fp32" else torch.bfloat16, device="cuda")
+    lse = torch.full((S, heads, T), 3.0, device="cuda")
+    H.hkv_cross_attention(cfg, st, tok, H.make_rows(q), H.make_rows(o), lse, ws, n)
+    assert int(err) == H.HKV_ERR_BOUNDS
+    if which == "queries":
+        assert (o[1] == 3.0).all() and (lse[1] == 3.0).all()
+    else:
+        assert torch.isnan(o[1]).all() and torch.isnan(lse[1]).all()
+    keep = [0] + list(range(2, min(S, 4))) + ([S - 1] if S > 4 else [])
+    ql[1] = kl[1] = 0
+    check_cross(q[keep], k[keep], v[keep], o[keep], lse[keep], qlens=[ql[i] for i in keep],
+                klens=[kl[i] for i in keep])
 
 
 # attention over states ------------------------------------------------------
