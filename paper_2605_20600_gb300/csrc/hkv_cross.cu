@@ -1,13 +1,18 @@
 // Attention of the tokens' queries over their sequence's states, or of a
 // prompt's tokens over the tokens up to themselves.
 //
-// cross_kernel (here) takes up to 16 query rows of a (sequence, key head), the
-// heads of the group one after the other, and a range of keys in tiles of 64 on
-// mma.sync m16n8k16, 16 keys of a tile a warp; the ranges of one query are
-// joined by a second kernel. More rows are hkv_cross_tc.cu's and
-// hkv_cross_parts.cu's.
+// cross_kernel (here) takes up to 16 bf16 query rows of a (sequence, key head), the
+// heads of the group one after the other, and a range of keys on mma.sync
+// m16n8k16, 16 keys of a tile a warp; cross_few_kernel as many fp32 rows without
+// the tensor core; the ranges of one query are joined by a second kernel. More rows
+// are hkv_cross_tc.cu's and hkv_cross_parts.cu's.
 //
-// Precision: queries, keys and values (bf16) enter as they are, the weights as
+// What bounds them: DRAM. One bf16 query of 64 x 32 heads over 300 states of 128:
+// 59 us, 5.3 TB/s (tcgen05, with one of 128 rows in use, would take 64 keys a
+// microsecond and CTA); 8 key heads over 2000 states: 86 us, 6.1 TB/s; fp32, 32
+// heads over 300: 102 us, 6.2 TB/s (six products of parts on mma.sync: 400).
+//
+// Precision of cross_kernel: queries, keys and values (bf16) enter as they are, the weights as
 // three bf16 parts for fp32 outs, which leaves nothing of them out, and as two,
 // off by 2^-18 of a weight, for bf16 outs, whose own rounding is 2^-9. Sums are
 // fp32; products chain in the tensor core within a tile.
@@ -16,8 +21,6 @@
 
 namespace hkv {
 namespace {
-
-constexpr int kKeys = 64;  // keys of a tile
 
 constexpr int kStages = 2;
 using bf16 = __nv_bfloat16;
@@ -398,7 +401,9 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
   }
 }
 
-// Joins a query's ranges: W warps a query, each a run of its ranges in order.
+// Joins a query's ranges: W warps a query, each a run of its ranges in order. Two
+// dependent reads, 7 us for 40 queries of 147 ranges (with a warp a query the whole
+// call took 31 us instead of 25).
 constexpr int kJoinThreads = 256;
 template <int D, typename O, int W>
 __global__ void __launch_bounds__(kJoinThreads)
@@ -578,7 +583,7 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   if (want > kMostSplits) want = kMostSplits;
   if (want > keys / least) want = keys / least;
   if (want < 1 || keys < 512) want = 1;
-  pl.split_len = (int)(((keys + want - 1) / want + kKeys - 1) / kKeys * kKeys);
+  pl.split_len = (int)(((keys + want - 1) / want + 63) / 64 * 64);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
   pl.part_bytes =
       pl.splits > 1 ? (size_t)seqs * heads * tokens * pl.splits * (D + 4) * sizeof(float) : 0;

@@ -1,13 +1,15 @@
-// Attention of many bf16 queries over their sequence's states on tcgen05.
+// Attention of more than 16 bf16 query rows over their sequence's states, with
+// bf16 outs, on tcgen05.
 //
-// A CTA takes TILES query tiles of one (sequence, key head) and a range of keys
-// in tiles of 128. A query tile is 128 tokens of a head, or all tokens of a few
-// heads of the group, 128 rows at most. One warp loads Q, and K and V tiles into a ring
-// of slots (TMA), one issues the products, and four warps per query tile, a thread per
-// row, turn scores into weights: S = Q K^T lies in TMEM, a thread reads its row
-// of S, writes the weights as bf16 over it, and they are the A operand of
-// O += W V, which stays in TMEM. With two tiles the tensor core works on one
-// while the other's weights are made.
+// A CTA works on TILES query tiles of one (sequence, key head) and a range of keys
+// in tiles of 64. A query tile is 128 tokens of a head, or all tokens of a few
+// heads of the group, 128 rows at most. One warp loads Q, and K and V tiles into a
+// ring of slots (TMA); four warps a query tile, a thread per row, turn scores into
+// weights: S = Q K^T lies in TMEM in two buffers, a thread reads its row of S,
+// writes the weights as bf16 over it, and they are the A operand of O += W V, which
+// stays in TMEM; a warp a query tile issues its products. A CTA that has issued the
+// loads of its work takes over that of a CTA which was not launched yet, so that
+// loads and first scores run beside the outs of the work before.
 //
 // A row's reference maximum moves (and O and its sum are rescaled) only when a
 // tile's maximum is more than 2^8 above it, so that weights stay below 2^8. The
@@ -17,6 +19,18 @@
 //
 // Rows of V past the last state are set to zero in shared memory (a weight of
 // zero times what lies there could be NaN); scores past it are masked.
+//
+// What bounds it, heads of 128: the products, which keep the tensor pipe busy for
+// 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 322 us, 1705 TFLOP/s;
+// causal over 4288: 0.68, 230 us). On the way: products issued
+// from divergent code, each operand's descriptor moved to uniform registers, 470;
+// from uniform code, K and V in one wait, 387; S in two buffers, so that products
+// and weights of a tile overlap, 341; the scores after the next behind a tile's
+// W V, one wait a tile, 322. Two threads a row: 365 (their agreement on a maximum
+// costs more than half of the exponentials); one warp for both tiles' products in
+// turn: 387; tiles of 128 keys leave no room in TMEM for a second S. Heads of 64
+// have half of the products: 306 us, bound by the weights (64 exponentials a row
+// and tile, 512 cycles of two tiles, and the chain around them).
 #include <cuda.h>
 
 #include "hkv_cross.cuh"

@@ -14,6 +14,13 @@
 // and sines of its pairs, and weights that all heads share, for several heads of
 // the same token, so that the angles cost a fraction of the copies, and loads a
 // few rows ahead of the first one's arithmetic.
+// What bounds it: DRAM without norms (128 x 576 tokens of 20 heads of 64, bf16, two
+// axes: 58 us, 6.5 TB/s, 0.97 of a copy); with them instruction issue too (8 x 4288
+// tokens of 96 heads of 128, bf16, layer norms, q and k of three: 296 us, 5.7 TB/s;
+// RMS norms 6.2), and the smallest calls the launch and three dependent reads (2.1
+// us; a step of 8 sequences with norms 3.6). A thread with two 16-byte pieces of
+// bf16 took 643 us for the second (127 registers, two reads on their way), the sums
+// of four rows side by side 467 (spills).
 // heads_any_kernel takes half layouts whose pieces do not fall together
 // (rot_dim / 2 not a multiple of 4): a warp per row, through shared memory.
 #include <cuda_bf16.h>
