@@ -39,20 +39,22 @@
 namespace hkv {
 namespace {
 
-constexpr int kTile = 128, kKeys = 64;  // queries of a tile, keys of one
+constexpr int kTile = 128;  // queries of a tile
 
 template <int D, int TILES>
 struct TcPlan {
   static constexpr int kThreads = TILES * 160 + 32;
+  static constexpr int kKeys = D == 64 ? 96 : 64;   // of a tile: two buffers of S fill TMEM beside O
   static constexpr int kQ = kTile * D * 2, kKV = kKeys * D * 2;  // bytes of a query tile, of a K or V tile
   // slots of the ring: slot p % kSlots holds K of key tile p and V of tile p - 1,
   // which the products need together
-  static constexpr int kSlots = TILES * (D == 64 ? 4 : 2);
+  static constexpr int kSlots = TILES * (D == 64 ? 3 : 2);
   // channels of a row that go out at a time, through a warp's piece of shared memory
   static constexpr int kOut = TILES == 2 ? 64 : 32;
   static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kKV + TILES * 4 * 32 * kOut * 2;
   static constexpr int kParts = TILES == 1 ? 2 : 1;  // bf16 parts of a weight
   static constexpr int kCols = TILES * 256;         // TMEM: two buffers of S of each tile, then O of each
+  static constexpr int kO = TILES * 2 * kKeys;
 };
 
 __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int c, int row, int head,
@@ -73,8 +75,9 @@ struct Item {
   int n[TILES], most;                // key tiles
   bool any;                          // rows to write
 };
-template <int TILES>
+template <int D, int TILES>
 __device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
+  constexpr int kKeys = TcPlan<D, TILES>::kKeys;
   Item<TILES> x;
   x.w = work_of(p, index);
   x.lo = x.w.sp * p.split_len;
@@ -103,7 +106,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
                     const __grid_constant__ CUtensorMap kmap,
                     const __grid_constant__ CUtensorMap vmap) {
   using TP = TcPlan<D, TILES>;
-  constexpr int PF = D + 4, SLOTS = TP::kSlots;
+  constexpr int PF = D + 4, SLOTS = TP::kSlots, kKeys = TP::kKeys;
   extern __shared__ unsigned char dyn_raw[];
   __shared__ __align__(16) uint4 s_answer;            // to the load warp: another CTA's work
   __shared__ uint64_t s_asked;
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     tmem_alloc(&s_tmem, TP::kCols);
     pdl_launch_dependents();
   }
-  Item<TILES> x = item_of<TILES>(p, blockIdx.x);
+  Item<TILES> x = item_of<D, TILES>(p, blockIdx.x);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     else ok = false;
     __syncwarp();
     if (lane == 0) mbar_arrive(&s_ne[k & 1]);
-    if (item >= 0) x = item_of<TILES>(p, item);
+    if (item >= 0) x = item_of<D, TILES>(p, item);
     return item >= 0;
   };
   if (warp == TILES * 4) {
@@ -236,7 +239,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         else ok = false;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (item >= 0) x = item_of<TILES>(p, item);
+        if (item >= 0) x = item_of<D, TILES>(p, item);
       } while (item >= 0 && !x.any);
       if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
         ok = false;
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     // that they leave: one wait for 512 cycles of products. With one, whose ring is
     // shorter, the scores of the next tile only, before the weights are there.
     const int t = warp - TILES * 4 - 1;
-    const uint32_t ring_at = smem_u32(ring), at_s = tmem + t * 128, at_o = tmem + TILES * 128 + t * 128;
+    const uint32_t ring_at = smem_u32(ring), at_s = tmem + t * 2 * kKeys, at_o = tmem + TP::kO + t * D;
     const uint64_t qd = tc_desc(smem_u32(dyn) + t * TP::kQ, 16);
     uint32_t slots = 0, queries = 0, steps = 0;  // used so far: slots, items, key tiles
     auto here = [&](uint32_t j) { return wait(&s_full[j % SLOTS], (j / SLOTS) & 1); };
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       const uint64_t kd = tc_desc(ring_at + (j % SLOTS) * 2 * TP::kKV, 16);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)  // 16 channels: 32 bytes of a column block
-        tc_mma(at_s + (step & 1) * 64, qd + (((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4),
+        tc_mma(at_s + (step & 1) * kKeys, qd + (((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4),
                kd + (((ks >> 2) * kKeys * 128 + (ks & 3) * 32) >> 4), tc_instr(kTile, kKeys, false),
                ks > 0);
       tc_commit(&s_s[t][step & 1]);
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           for (int part = TP::kParts - 1; part >= 0; --part)  // the small part first
 #pragma unroll
             for (int kk = 0; kk < kKeys / 16; ++kk)
-              tc_mma_ta(at_o, at_s + b * 64 + part * 32 + kk * 8, vd + kk * (16 * 128 >> 4),
+              tc_mma_ta(at_o, at_s + b * kKeys + part * (kKeys / 2) + kk * 8, vd + kk * (16 * 128 >> 4),
                         tc_instr(kTile, D, true), i > 0 || kk > 0 || part < TP::kParts - 1);
           tc_commit(&s_v[t]);
           if (TILES == 2 && i + 2 < n) scores(steps + 2, j + 1, i + 3 == n);
@@ -345,8 +348,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     if (!ok) mbar_wait(&s_drain, 0);
   } else {
     const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens, token_in = r - h * p.box_tokens;
-    const uint32_t mine = tmem + t * 128 + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t mine_o = mine + TILES * 128;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t mine = tmem + t * 2 * kKeys + lanes, mine_o = tmem + TP::kO + t * D + lanes;
     unsigned char *rows = stage + warp * 32 * TP::kOut * 2;
     uint32_t steps = 0;                         // key tiles so far
     int k = 0;
@@ -357,16 +360,16 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       const int seen = min(keys_seen(p, x.w, token), x.lo + p.split_len);
       float m = -INFINITY, l = 0.f;
       for (int i = 0; i < n && ok; ++i, ++steps) {
-        const uint32_t b = steps & 1, mine_s = mine + b * 64;
+        const uint32_t b = steps & 1, mine_s = mine + b * kKeys;
         ok = wait(&s_s[t][b], (steps >> 1) & 1);
 #ifdef HKV_CROSS_TEST_STALL  // one warp waits for a phase that nothing completes before its limit
         if (warp == (int)(blockIdx.x & 3) && i == 1) ok = wait(&s_drain, 0);
 #endif
         if (!ok) break;
         tc_fence_after();
-        uint32_t s[2][32];
+        uint32_t s[kKeys / 32][32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) tmem_ld32(s[c], mine_s + c * 32);
+        for (int c = 0; c < kKeys / 32; ++c) tmem_ld32(s[c], mine_s + c * 32);
         tmem_wait_ld();
         const int left = seen - x.lo - i * kKeys;  // keys of the tile that count
         if (left < kKeys) {
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         const uint64_t scale2 = pair_of(p.qscale, p.qscale), ref2 = pair_of(-ref, -ref);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < kKeys / 32; ++c) {
           uint32_t v[16], v2[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -425,7 +428,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
               v2[j] = pack2(w0 - __uint_as_float(v[j] << 16), w1 - __uint_as_float(v[j] & 0xFFFF0000u));
           }
           tmem_st16(mine_s + c * 16, v);
-          if (TP::kParts == 2) tmem_st16(mine_s + 32 + c * 16, v2);
+          if (TP::kParts == 2) tmem_st16(mine_s + kKeys / 2 + c * 16, v2);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -556,8 +559,8 @@ cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
   CUtensorMap q, k, v;
   if (e == cudaSuccess)
     e = encode(&q, a.q, D, a.tokens, a.qt, a.heads, a.qh, a.seqs, a.qs, a.box_tokens, a.box_heads);
-  if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kKeys, 1);
-  if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, kKeys, 1);
+  if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
+  if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
   if (e != cudaSuccess) return e;
   return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v);
 }
