@@ -83,14 +83,16 @@ __device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
   x.lo = x.w.sp * p.split_len;
   x.most = 0;
   x.any = false;
-  const int token_tiles = (p.tokens + p.box_tokens - 1) / p.box_tokens;
+  // the heads of a group side by side: query tiles of a CTA see the same keys, and
+  // have rows or none together
+  const int head_tiles = (p.group + p.box_heads - 1) / p.box_heads;
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
-    const int u = x.w.tile * TILES + t, h = u / token_tiles;
-    x.head0[t] = h * p.box_heads;
-    x.token0[t] = (u - h * token_tiles) * p.box_tokens;
+    const int u = x.w.tile * TILES + t, token_tile = u / head_tiles;
+    x.head0[t] = (u - token_tile * head_tiles) * p.box_heads;
+    x.token0[t] = token_tile * p.box_tokens;
     int hi = 0;
-    const bool live = x.head0[t] < p.group && x.token0[t] < x.w.qlen;
+    const bool live = x.token0[t] < x.w.qlen;
     x.any |= live;
     if (live)
       hi = min(keys_seen(p, x.w, min(x.token0[t] + p.box_tokens, x.w.qlen) - 1), x.lo + p.split_len);
