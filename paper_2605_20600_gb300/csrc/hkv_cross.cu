@@ -575,13 +575,19 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
     pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
   }
   const long long base = (long long)seqs * kv * pl.tiles;
-  // One round of CTAs, or (few query rows, whose partial results are small) four;
-  // ranges long enough that joining them pays: a CTA takes about 3 us and 0.9 (16
-  // rows) or 0.5 more for 64 keys, and the join 2.5.
-  long long want = base < ctas ? ctas / base : 1, least = pl.rows == 16 ? 192 : 256;
-  if (pl.rows == 16 && base >= ctas && base < 4LL * ctas) want = (4LL * ctas + base - 1) / base, least = 512;
-  if (want > kMostSplits) want = kMostSplits;
+  // One round of CTAs, or (few query rows, whose partial results are small, and
+  // ranges of 512 keys) four, so that uneven ones even out; ranges long enough that
+  // joining them pays: a CTA takes about 3 us and 0.9 (16 rows) or 0.5 more for 64
+  // keys, and the join 2.5.
+  const long long least = pl.rows == 16 ? 192 : 256;
+  long long want = base < ctas ? ctas / base : 1;
   if (want > keys / least) want = keys / least;
+  if (pl.rows == 16 && base < 4LL * ctas) {
+    long long four = (4LL * ctas + base - 1) / base;
+    if (four > keys / 512) four = keys / 512;
+    if (want < four) want = four;
+  }
+  if (want > kMostSplits) want = kMostSplits;
   if (want < 1 || keys < 512) want = 1;
   pl.split_len = (int)(((keys + want - 1) / want + 63) / 64 * 64);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;

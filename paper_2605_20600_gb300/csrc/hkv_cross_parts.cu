@@ -9,8 +9,8 @@
 //   0-3    a thread per row: scores (TMEM) to weights, parts of weights to TMEM
 //   4-7    a thread per row: O = O f + (W V of the tile), O in registers: chained
 //          in the tensor core its sums would truncate once per 16 keys
-//   8-11   loads of Q, and then of K (two warps) and of V, cut into parts in
-//          shared memory
+//   8-11   loads of K (two warps) and of V, cut into parts in shared memory; those
+//          of Q are the first eight warps', which have nothing else to do yet
 //   12     issues the products; S of a tile is computed while the weights of the
 //          one before are made (two buffers of S, of the last parts and of O)
 //
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
         mbar_init(&s_kvf[kv][j], 2);
         mbar_init(&s_kve[kv][j], 1);
       }
-    mbar_init(&s_q, 4);
+    mbar_init(&s_q, 8);
     for (int b = 0; b < 2; ++b) {
       mbar_init(&s_s[b], 1);
       mbar_init(&s_p[b], 4);
@@ -140,6 +140,24 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
   const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
   bool ok = true;
   float acc[D];  // warps 4-7
+  if (n > 0 && warp < 8) {
+    constexpr int E = kRows * PPR / 256;  // pieces a thread, all on their way at once
+    RawPiece<T> raw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int r = (tid + e * 256) / PPR, c = (tid + e * 256) % PPR;
+      const Row x = row_of(p, w.kvh, min(r0 + r, all - 1));
+      const bool on = r0 + r < all && x.token < w.qlen;
+      raw[e] = raw_piece<T>(static_cast<const T *>(p.q) + w.s * p.qs +
+                                (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      put_piece(dyn + piece_of<kRows>((tid + e * 256) / PPR, (tid + e * 256) % PPR), SM::kQPlane, raw[e]);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s_q);
+  }
   if (n > 0 && warp >= 8 && warp < 12) {
     const int kv = (warp - 8) >> 1, lt = tid & 63;
     const T *from = static_cast<const T *>(kv ? p.v : p.k) + w.s * p.ks + w.kvh * p.kh + lo * p.kt;
@@ -156,17 +174,6 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
       }
     };
     fetch(0);
-    for (int e = tid - 8 * 32; e < kRows * PPR; e += 128) {
-      const int r = e / PPR, c = e % PPR;
-      const Row x = row_of(p, w.kvh, min(r0 + r, all - 1));
-      const bool on = r0 + r < all && x.token < w.qlen;
-      put_piece(dyn + piece_of<kRows>(r, c), SM::kQPlane,
-                raw_piece<T>(static_cast<const T *>(p.q) + w.s * p.qs +
-                                 (on ? x.token * p.qt + x.head * p.qh : 0) + c * 8, on));
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&s_q);
     for (int u = 0; u < n * CH && ok; ++u) {
       const int i = u / CH, j = i % ST;
       if (u % CH == 0 && i >= ST)
