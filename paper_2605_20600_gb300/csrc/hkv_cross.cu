@@ -3,7 +3,8 @@
 //
 // cross_kernel (here) takes up to 16 bf16 query rows of a (sequence, key head), the
 // heads of the group one after the other, and a range of keys on mma.sync
-// m16n8k16, 16 keys of a tile a warp; cross_few_kernel as many fp32 rows without
+// m16n8k16, 16 keys of a tile a warp (32 for heads of 64: as many bytes on their way;
+// single queries of 12 heads over up to 2861 states 30.4 -> 28.6 us); cross_few_kernel as many fp32 rows without
 // the tensor core; the ranges of one query are joined by a second kernel. More rows
 // are hkv_cross_tc.cu's and hkv_cross_parts.cu's.
 //
@@ -27,7 +28,8 @@ using bf16 = __nv_bfloat16;
 
 template <int D, int W>
 struct CSmem {
-  static constexpr int kKeys = W * 16;             // of a tile
+  static constexpr int kStep = D == 64 ? 32 : 16;  // keys of a tile a warp
+  static constexpr int kKeys = W * kStep;          // of a tile
   static constexpr int kPlane = kKeys * D * 2;     // K or V of one
   static constexpr int kTiles = kStages * 2 * kPlane;
   static constexpr int kTotal = kTiles + 16 * D * 2;
@@ -37,7 +39,7 @@ struct CSmem {
 template <int D, typename O, int W>
 __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(const __grid_constant__ CrossArgs p) {
   using SM = CSmem<D, W>;
-  constexpr int kKeys = SM::kKeys, kThreads = W * 32;
+  constexpr int kKeys = SM::kKeys, KW = SM::kStep, NB = KW / 16, kThreads = W * 32;
   constexpr int WP = sizeof(O) == 4 ? 3 : 2;  // parts of a weight
   constexpr int PF = D + 4, PPR = D / 8;
   extern __shared__ __align__(128) unsigned char dyn[];
@@ -57,8 +59,8 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
   auto load_tile = [&](int k0, int st) {
     unsigned char *s = dyn + st * 2 * SM::kPlane;
 #pragma unroll
-    for (int e = lane; e < 16 * PPR; e += 32) {
-      const int r = warp * 16 + e / PPR, c = e % PPR;
+    for (int e = lane; e < KW * PPR; e += 32) {
+      const int r = warp * KW + e / PPR, c = e % PPR;
       const bool on = k0 + r < hi;
       const long long at = (on ? (k0 + r) * p.kt : 0) + c * 8;
       cp_async16_zfill(s + at16<D>(r, c), K + at, on);
@@ -95,29 +97,33 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
     const int mi = lane >> 3, mr = lane & 7;
     const uint32_t q_base = smem_u32(sq), t_base = smem_u32(dyn);
     const int q_row = (mi & 1) * 8 + mr, q_pc = mi >> 1;
-    const int k_row = warp * 16 + (mi >> 1) * 8 + mr, k_pc = mi & 1;
-    const int v_row = warp * 16 + (mi & 1) * 8 + mr, v_pc = mi >> 1;
+    const int k_row = warp * KW + (mi >> 1) * 8 + mr, k_pc = mi & 1;
+    const int v_row = warp * KW + (mi & 1) * 8 + mr, v_pc = mi >> 1;
     int st = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       if (k0 == lo) __syncthreads();  // the queries are everyone's
       else __syncwarp();
       const uint32_t kb = t_base + st * 2 * SM::kPlane, vb = kb + SM::kPlane;
-      float s[2][4] = {};
+      float s[2 * NB][4] = {};
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
-        uint32_t qa[4], f[4];
+        uint32_t qa[4];
         ldm4(qa, q_base + at16<D>(q_row, 2 * ks + q_pc));
-        ldm4(f, kb + at16<D>(k_row, 2 * ks + k_pc));
-        mma_bf16(s[0], qa, f[0], f[1]);
-        mma_bf16(s[1], qa, f[2], f[3]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          uint32_t f[4];
+          ldm4(f, kb + at16<D>(k_row + nb * 16, 2 * ks + k_pc));
+          mma_bf16(s[2 * nb], qa, f[0], f[1]);
+          mma_bf16(s[2 * nb + 1], qa, f[2], f[3]);
+        }
       }
       // weights of rows lane / 4 (j = 0) and lane / 4 + 8 (j = 1); keys of this
       // warp's part that count for either
-      const int left[2] = {min(seen[0], hi) - k0 - warp * 16, min(seen[1], hi) - k0 - warp * 16};
+      const int left[2] = {min(seen[0], hi) - k0 - warp * KW, min(seen[1], hi) - k0 - warp * KW};
       float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < 2 * NB; ++x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = x * 8 + (lane & 3) * 2 + (e & 1);
@@ -144,9 +150,9 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
           o[x][3] *= f[1];
         }
       }
-      uint32_t pf[WP][4];
+      uint32_t pf[NB][WP][4];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < 2 * NB; ++x) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           // (a key that does not count has a score of -inf)
@@ -156,18 +162,22 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
           uint32_t pr[3];
           split2<false>(w0, w1, pr);
 #pragma unroll
-          for (int k = 0; k < WP; ++k) pf[k][x * 2 + j] = pr[k];
+          for (int k = 0; k < WP; ++k) pf[x / 2][k][(x & 1) * 2 + j] = pr[k];
         }
       }
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) {  // 16 channels at a time
         float t[2][4] = {};
-        uint32_t vf[4];
-        ldm4t(vf, vb + at16<D>(v_row, 2 * db + v_pc));
+        uint32_t vf[NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) ldm4t(vf[nb], vb + at16<D>(v_row + nb * 16, 2 * db + v_pc));
 #pragma unroll
         for (int a = WP - 1; a >= 0; --a) {  // the small parts first
-          mma_bf16(t[0], pf[a], vf[0], vf[1]);
-          mma_bf16(t[1], pf[a], vf[2], vf[3]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_bf16(t[0], pf[nb][a], vf[nb][0], vf[nb][1]);
+            mma_bf16(t[1], pf[nb][a], vf[nb][2], vf[nb][3]);
+          }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x)
