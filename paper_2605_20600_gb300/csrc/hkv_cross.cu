@@ -601,6 +601,10 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   if (want < 1 || keys < 512) want = 1;
   pl.split_len = (int)(((keys + want - 1) / want + 63) / 64 * 64);
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
+  // Where there are more CTAs than fit, by length: 16 x 577 padded queries of 20 heads
+  // on 4 over up to 1025 states 35.6 -> 29.8 us; fp32, 16 x 257 over up to 777, 60 -> 49,
+  // but 0.3 more a CTA (542 over up to 33: 56 -> 58.5).
+  pl.sorted = pl.rows != 16 && seqs > 1 && seqs <= 32 && base > ctas && (tc || keys >= 256);
   pl.part_bytes =
       pl.splits > 1 ? (size_t)seqs * heads * tokens * pl.splits * (D + 4) * sizeof(float) : 0;
   return pl;

@@ -51,6 +51,50 @@ __device__ __forceinline__ Work work_of(const CrossArgs &p, int b) {
   }
   return w;
 }
+// The pieces of work (work_of's) in falling order of their sequence's states, so
+// that those which end last are short, and without those that have no rows. A lane
+// has a sequence.
+struct Order {
+  int first, tiles, all;  // its first piece; query tiles with rows; pieces of all sequences
+};
+// For the whole warp; tiles_of(n): query tiles that n tokens of a sequence reach.
+template <typename F>
+__device__ __forceinline__ Order order_of(const CrossArgs &p, F tiles_of) {
+  Order o = {};
+  if (!p.sorted) return o;
+  const int lane = threadIdx.x & 31;
+  const bool on = lane < p.seqs;
+  int klen = !on ? 0 : p.klen ? p.klen[lane] : p.keys;
+  int qlen = !on ? 0 : p.qlen ? p.qlen[lane] : p.tokens;
+  const bool first = threadIdx.x < 32 && blockIdx.x == 0;
+  if (klen < 0 || klen > p.keys) {
+    if (first) set_err(p.err, HKV_ERR_BOUNDS);
+    klen = 0;
+  }
+  if (qlen < 0 || qlen > p.tokens) {
+    if (first) set_err(p.qerr, HKV_ERR_BOUNDS);
+    qlen = 0;
+  }
+  o.tiles = tiles_of(qlen);
+#pragma unroll 4
+  for (int i = 0; i < p.seqs; ++i) {
+    const int other = __shfl_sync(0xFFFFFFFFu, klen, i), tiles = __shfl_sync(0xFFFFFFFFu, o.tiles, i);
+    o.all += tiles;
+    if (other > klen || (other == klen && i < lane)) o.first += tiles;
+  }
+  o.first *= p.kv;
+  o.all *= p.kv;
+  return o;
+}
+// work_of's number of piece i, or -1
+__device__ __forceinline__ int piece_at(const CrossArgs &p, const Order &o, int i) {
+  if (!p.sorted) return i;
+  if (i >= o.all) return -1;
+  const int at = i - o.first;
+  const int s = __ffs(__ballot_sync(0xFFFFFFFFu, at >= 0 && at < o.tiles * p.kv)) - 1;
+  const int n = __shfl_sync(0xFFFFFFFFu, o.tiles, s), in = __shfl_sync(0xFFFFFFFFu, at, s);
+  return (s * p.kv + in / n) * p.tiles + p.tiles - n + in % n;
+}
 // a query row of a (sequence, key head): which head of the group, which token
 struct Row {
   int head, token;

@@ -128,7 +128,12 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
     tmem_alloc(&s_tmem, kCols);
     pdl_launch_dependents();
   }
-  const Work w = work_of(p, blockIdx.x);
+  const Order order = order_of(p, [&](int tokens) {
+    return tokens == 0 ? 0 : p.group == 1 ? (tokens + kRows - 1) / kRows : p.tiles;
+  });
+  const int piece = piece_at(p, order, blockIdx.x);
+  Work w = {};
+  if (piece >= 0) w = work_of(p, piece);
   const int all = p.group * p.tokens, r0 = w.tile * kRows;
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, r0, min(all, r0 + kRows)), lo + p.split_len);

@@ -79,10 +79,10 @@ template <int D, int TILES>
 __device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
   constexpr int kKeys = TcPlan<D, TILES>::kKeys;
   Item<TILES> x;
+  x = {};
+  if (index < 0) return x;
   x.w = work_of(p, index);
   x.lo = x.w.sp * p.split_len;
-  x.most = 0;
-  x.any = false;
   // the heads of a group side by side: query tiles of a CTA see the same keys, and
   // have rows or none together
   const int head_tiles = (p.group + p.box_heads - 1) / p.box_heads;
@@ -158,7 +158,11 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
     tmem_alloc(&s_tmem, TP::kCols);
     pdl_launch_dependents();
   }
-  Item<TILES> x = item_of<D, TILES>(p, blockIdx.x);
+  const Order order = order_of(p, [&](int tokens) {
+    const int token_tiles = (tokens + p.box_tokens - 1) / p.box_tokens;
+    return (token_tiles * ((p.group + p.box_heads - 1) / p.box_heads) + TILES - 1) / TILES;
+  });
+  Item<TILES> x = item_of<D, TILES>(p, piece_at(p, order, blockIdx.x));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -241,8 +245,11 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         else ok = false;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (item >= 0) x = item_of<D, TILES>(p, item);
-      } while (item >= 0 && !x.any);
+        if (item < 0) break;
+        const int piece = piece_at(p, order, item);
+        x = item_of<D, TILES>(p, piece);
+        if (x.any) item = piece;
+      } while (!x.any);
       if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
         ok = false;
         break;

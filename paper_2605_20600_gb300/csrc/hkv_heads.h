@@ -54,6 +54,7 @@ struct CrossArgs {
   int causal;
   int splits, split_len, tiles;       // key ranges; query tiles of a key head
   int box_tokens, box_heads;          // a query tile of the tcgen05 kernel
+  int sorted;                         // work by the sequences' lengths (Order)
   float *part;                        // [rows of (sequence, head, token)][splits][D + 4]
   float qscale;                       // log2(e) / sqrt(D)
 };
@@ -61,7 +62,7 @@ struct CrossArgs {
 struct CrossPlan {
   int rows;                           // queries of a CTA (256, 128: the tcgen05 kernel)
   int splits, split_len, tiles;
-  int box_tokens, box_heads;
+  int box_tokens, box_heads, sorted;
   size_t part_bytes;
 };
 CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, int dtype,

@@ -303,6 +303,7 @@ hkv_status hkv_cross_attention(const hkv_config *cfg, const hkv_states *states,
   a.tiles = pl.tiles;
   a.box_tokens = pl.box_tokens;
   a.box_heads = pl.box_heads;
+  a.sorted = pl.sorted && (a.klen || a.qlen);
   a.part = static_cast<float *>(workspace);
   a.qscale = (float)(1.4426950408889634 / sqrt((double)cfg->head_dim));
   return cuda_status(

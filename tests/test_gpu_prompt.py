@@ -418,6 +418,55 @@ def test_attention_over_states(case, ragged, causal):
     check_cross(q, k, v, o, lse, causal=causal, heads=range(0, heads, max(1, S * heads // 16)), **lens)
 
 
+@pytest.mark.parametrize("which", ["both", "queries", "states", "bad"])
+@pytest.mark.parametrize("dtype,out,D,S,heads,KV,T,N", [
+    ("bf16", "bf16", 64, 16, 20, 4, 300, 200), ("bf16", "bf16", 128, 32, 24, 6, 40, 100),
+    ("bf16", "bf16", 64, 31, 12, 12, 100, 90), ("bf16", "bf16", 64, 33, 12, 12, 100, 90),
+    ("fp32", "fp32", 64, 7, 11, 11, 300, 300), ("fp32", "fp32", 128, 9, 20, 4, 130, 257),
+    ("bf16", "fp32", 64, 5, 16, 16, 257, 600)])
+def test_more_work_than_the_device_holds_of_unequal_sequences(dtype, out, D, S, heads, KV, T, N, which):
+    """Up to 32 sequences are worked on by length; equal ones, empty ones, lengths that
+    are out of range and batches with one kind of lengths only."""
+    torch, H = mods()
+    q, k, v = qkv(torch, S, T, heads, KV, N, D, dtype)
+    rng = np.random.default_rng(S)
+    ql, kl = ([int(x) for x in rng.integers(1, most + 1, S)] for most in (T, N))
+    ql[0], kl[1], ql[2], kl[3], kl[4] = T, N, 0, 0, kl[1]
+    if which == "queries":
+        kl = None
+    if which == "states":
+        ql = None
+    tok_err, st_err = ints([0]), ints([0])
+    given = list(ql or []), list(kl or [])
+    if which == "bad":
+        given[0][0], given[1][1] = T + 1, -1
+    tok = H.make_tokens(T, ints(given[0]) if ql else None, None, tok_err)
+    st = H.make_states(k, v, ints(given[1]) if kl else None, st_err)
+    cfg = cfg_of(H, S, heads, D, dtype)
+    n = H.hkv_cross_workspace_size(cfg, st, tok)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    o = torch.full(q.shape, 3.0, dtype=torch.float32 if out == "fp32" else torch.bfloat16, device="cuda")
+    lse = torch.full((S, heads, T), 3.0, device="cuda")
+    for causal in (0, H.HKV_ATTN_CAUSAL):
+        o.fill_(3.0), lse.fill_(3.0)
+        H.hkv_cross_attention(cfg, st, tok, H.make_rows(q), H.make_rows(o), lse, ws, n, causal)
+        first = 0
+        if which == "bad":
+            assert int(tok_err) == int(st_err) == H.HKV_ERR_BOUNDS
+            assert (o[0] == 3.0).all() and (lse[0] == 3.0).all()
+            assert torch.isnan(o[1, :ql[1]]).all() and torch.isnan(lse[1, :, :ql[1]]).all()
+            assert (o[1, ql[1]:] == 3.0).all() and (lse[1, :, ql[1]:] == 3.0).all()
+            first = 2
+        check_cross(q[first:], k[first:], v[first:], o[first:], lse[first:], causal=bool(causal),
+                    qlens=ql and ql[first:], klens=kl and kl[first:],
+                    heads=range(0, heads, max(1, S * heads // 16)))
+        # the same rows whatever the batch
+        if which == "both":
+            a, b = run_cross(H, torch, q.flip(0), k.flip(0), v.flip(0), qlens=ql[::-1], klens=kl[::-1],
+                             causal=bool(causal), out_dtype=o.dtype)
+            assert torch.equal(a.flip(0), o) and torch.equal(b.flip(0), lse)
+
+
 def test_no_lse_and_strided_views():
     """Queries and outs by heads, states by tokens (slices of one projection), no lse."""
     torch, H = mods()
