@@ -66,6 +66,13 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
       : "memory");
 }
 
+// the same into L2
+__device__ __forceinline__ void tma_ahead(const CUtensorMap *map, int c, int row, int head, int seq) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(map), "r"(c),
+               "r"(row), "r"(head), "r"(seq)
+               : "memory");
+}
+
 // the query tiles of a CTA's work
 template <int TILES>
 struct Item {
@@ -74,6 +81,7 @@ struct Item {
   int head0[TILES], token0[TILES];   // heads within the group
   int n[TILES], most;                // key tiles
   bool any;                          // rows to write
+  bool none;                         // no work at all
 };
 template <int D, int TILES>
 __device__ __forceinline__ Item<TILES> item_of(const CrossArgs &p, int index) {
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   extern __shared__ unsigned char dyn_raw[];
   __shared__ __align__(16) uint4 s_answer;            // to the load warp: another CTA's work
   __shared__ uint64_t s_asked;
-  __shared__ int s_item[2];                           // the CTA's items, and whether they are
+  __shared__ Item<TILES> s_item[2];                   // the CTA's items, and whether they are
   __shared__ uint64_t s_nf[2], s_ne[2];               // there, and read by the other warps
   __shared__ uint64_t s_full[SLOTS], s_empty[SLOTS];  // slots of the ring
   __shared__ uint64_t s_s[TILES][2], s_p[TILES][2];   // S and W of a key tile are ready
@@ -176,27 +184,27 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   // The load warp finds the CTA's items, the work of CTAs that were not launched
   // yet; the others read them, k = 0, 1, ... behind the first, until there is none.
   auto next_item = [&](int k) {
-    int item = -1;
-    if (wait(&s_nf[k & 1], (k >> 1) & 1)) item = s_item[k & 1];
-    else ok = false;
+    if (!wait(&s_nf[k & 1], (k >> 1) & 1)) return ok = false;
+    x = s_item[k & 1];
     __syncwarp();
     if (lane == 0) mbar_arrive(&s_ne[k & 1]);
-    if (item >= 0) x = item_of<D, TILES>(p, item);
-    return item >= 0;
+    return !x.none;
   };
   if (warp == TILES * 4) {
     // loads: Q and the ring's slots, as far ahead as there is room, of the next
     // item too
     uint32_t slots = 0, queries[TILES] = {}, edges = 0;  // so far
     uint32_t asked = 0;
-    for (int k = 0, item = 0; item >= 0; ++k) {
+    bool ahead = false;  // the next item has been asked for
+    for (int k = 0; !x.none; ++k) {
       for (int j = 0; x.most > 0 && j <= x.most && ok; ++j, ++slots) {
         const uint32_t slot = slots % SLOTS;
         const int k0 = x.lo + j * kKeys, past = k0 - x.w.klen;
         if (slots >= SLOTS) ok = wait(&s_empty[slot], (slots / SLOTS - 1) & 1);
         if (!ok) break;
         unsigned char *dst = ring + slot * 2 * TP::kKV;
-        const bool edge = past > 0;  // V's tile is the sequence's last, and not a whole one
+        // V's tile ends behind the sequence (past the last one's states there are zeros)
+        const bool edge = past > 0 && x.w.klen < p.keys;
         if (lane == 0) {
           uint64_t *bar = edge ? &s_edge : &s_full[slot];
           mbar_arrive_expect_tx(bar, ((j < x.most) + (j > 0)) * TP::kKV);
@@ -224,6 +232,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           }
         }
         if (edge) {
+          if (lane == 0) next_cta_ask(&s_answer, &s_asked);
+          ahead = true;
           ok = ok && wait(&s_edge, edges++ & 1);
           if (!ok) break;
           for (int e = lane; e < past * (D / 8); e += 32) {
@@ -239,23 +249,33 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       // the next item that has rows to write; asked for only now, so that what is
       // left at the end goes to the CTA that is free first
       do {
-        if (lane == 0) next_cta_ask(&s_answer, &s_asked);
-        item = -1;
+        if (!ahead && lane == 0) next_cta_ask(&s_answer, &s_asked);
+        ahead = false;
+        int item = -1;
         if (wait(&s_asked, asked++ & 1)) item = next_cta(&s_answer);
         else ok = false;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (item < 0) break;
-        const int piece = piece_at(p, order, item);
-        x = item_of<D, TILES>(p, piece);
-        if (x.any) item = piece;
-      } while (!x.any);
+        if (item >= 0) x = item_of<D, TILES>(p, piece_at(p, order, item));
+        else x.none = true;
+      } while (!x.any && !x.none);
+#ifdef PFQ
+      if (lane == 0 && !x.none) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          if (x.n[t] == 0) continue;
+#pragma unroll
+          for (int c = 0; c < D; c += 64)
+            tma_ahead(&qmap, c, x.token0[t], x.w.kvh * p.group + x.head0[t], x.w.s);
+        }
+      }
+#endif
       if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
         ok = false;
         break;
       }
       if (lane == 0) {
-        s_item[k & 1] = item;
+        s_item[k & 1] = x;
         mbar_arrive(&s_nf[k & 1]);
       }
     }
@@ -366,7 +386,9 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       const int n = TILES == 2 && t ? x.n[TILES - 1] : x.n[0];
       const int first = TILES == 2 && t ? x.token0[TILES - 1] : x.token0[0];
       const int head0 = TILES == 2 && t ? x.head0[TILES - 1] : x.head0[0], token = first + token_in;
-      const int seen = min(keys_seen(p, x.w, token), x.lo + p.split_len);
+      const int seen = min(keys_seen(p, x.w, token) - x.lo, p.split_len);  // of the range
+      const int head = x.w.kvh * p.group + head0 + h;
+      const bool live = h < p.box_heads && head0 + h < p.group && token < x.w.qlen;
       float m = -INFINITY, l = 0.f;
       for (int i = 0; i < n && ok; ++i, ++steps) {
         const uint32_t b = steps & 1, mine_s = mine + b * kKeys;
@@ -380,7 +402,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
 #pragma unroll
         for (int c = 0; c < kKeys / 32; ++c) tmem_ld32(s[c], mine_s + c * 32);
         tmem_wait_ld();
-        const int left = seen - x.lo - i * kKeys;  // keys of the tile that count
+        const int left = seen - i * kKeys;  // keys of the tile that count
         if (left < kKeys) {
 #pragma unroll
           for (int j = 0; j < kKeys; ++j)
@@ -449,8 +471,6 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       // O is complete
       if (ok && n > 0) ok = wait(&s_v[t], (steps - 1) & 1);
       tc_fence_after();
-      const int head = x.w.kvh * p.group + head0 + h;
-      const bool live = h < p.box_heads && head0 + h < p.group && token < x.w.qlen;
       const bool wrong = x.w.bad || !ok, any = n > 0 && ok;
       const size_t row = ((size_t)x.w.s * p.heads + head) * p.tokens + token;
       auto o_read = [&] {  // the next item's products may overwrite O
