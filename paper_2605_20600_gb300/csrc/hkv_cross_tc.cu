@@ -2,7 +2,8 @@
 // bf16 outs, on tcgen05.
 //
 // A CTA works on TILES query tiles of one (sequence, key head) and a range of keys
-// in tiles of 64. A query tile is 128 tokens of a head, or all tokens of a few
+// in tiles of 64 (96 for heads of 64: the weights of half as many channels bound
+// them, and longer tiles wait less often). A query tile is 128 tokens of a head, or all tokens of a few
 // heads of the group, 128 rows at most. One warp loads Q, and K and V tiles into a
 // ring of slots (TMA); four warps a query tile, a thread per row, turn scores into
 // weights: S = Q K^T lies in TMEM in two buffers, a thread reads its row of S,
@@ -22,16 +23,19 @@
 //
 // What bounds it, heads of 128: the products, which keep the tensor pipe busy for
 // 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 322 us, 1705 TFLOP/s;
-// causal over 4288: 0.68, 230 us). On the way: products issued
+// causal over 4288: 0.68, 223 us). On the way: products issued
 // from divergent code, each operand's descriptor moved to uniform registers, 470;
 // from uniform code, K and V in one wait, 387; S in two buffers, so that products
 // and weights of a tile overlap, 341; the scores after the next behind a tile's
 // W V, one wait a tile, 322. Two threads a row: 365 (their agreement on a maximum
 // costs more than half of the exponentials); one warp for both tiles' products in
 // turn: 387; tiles of 128 keys leave no room in TMEM for a second S. Heads of 64
-// have half of the products: 306 us, bound by the weights (64 exponentials a row
-// and tile, 512 cycles of two tiles, and the chain around them).
+// have half of the products: 267 us (306 in tiles of 64 keys), bound by the weights
+// (96 exponentials a row and tile, and the chain around them). Short states: a
+// piece of work's chain, 8 x 4160 queries of 32 heads over 120: 111 us, 5 TB/s (145
+// with every warp working out what the next piece is, and 16-byte stores of outs).
 #include <cuda.h>
+#include <type_traits>
 
 #include "hkv_cross.cuh"
 #include "hkv_tcgen05.cuh"
@@ -51,6 +55,9 @@ struct TcPlan {
   static constexpr int kSlots = TILES * (D == 64 ? 3 : 2);
   // channels of a row that go out at a time, through a warp's piece of shared memory
   static constexpr int kOut = TILES == 2 ? 64 : 32;
+  // the outs by bulk copies: 8 x 4160 queries of 32 heads over 120 states, heads of
+  // 128, 119 -> 111 us; of 64, whose rows are one piece, 113.7 -> 114.5
+  static constexpr bool kCopyOut = D == 128 && TILES == 2;
   static constexpr int kBytes = 1024 + TILES * kQ + kSlots * 2 * kKV + TILES * 4 * 32 * kOut * 2;
   static constexpr int kParts = TILES == 1 ? 2 : 1;  // bf16 parts of a weight
   static constexpr int kCols = TILES * 256;         // TMEM: two buffers of S of each tile, then O of each
@@ -66,11 +73,13 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
       : "memory");
 }
 
-// the same into L2
-__device__ __forceinline__ void tma_ahead(const CUtensorMap *map, int c, int row, int head, int seq) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(map), "r"(c),
-               "r"(row), "r"(head), "r"(seq)
-               : "memory");
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, const void *from, int c, int row, int head,
+                                          int seq) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];\n"
+      "cp.async.bulk.commit_group;" ::"l"(map),
+      "r"(c), "r"(row), "r"(head), "r"(seq), "r"(smem_u32(from))
+      : "memory");
 }
 
 // the query tiles of a CTA's work
@@ -114,7 +123,8 @@ template <int D, int TILES>
 __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2)
     cross_tc_kernel(const __grid_constant__ CrossArgs p, const __grid_constant__ CUtensorMap qmap,
                     const __grid_constant__ CUtensorMap kmap,
-                    const __grid_constant__ CUtensorMap vmap) {
+                    const __grid_constant__ CUtensorMap vmap,
+                    const __grid_constant__ CUtensorMap omap) {
   using TP = TcPlan<D, TILES>;
   constexpr int PF = D + 4, SLOTS = TP::kSlots, kKeys = TP::kKeys;
   extern __shared__ unsigned char dyn_raw[];
@@ -259,17 +269,6 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         if (item >= 0) x = item_of<D, TILES>(p, piece_at(p, order, item));
         else x.none = true;
       } while (!x.any && !x.none);
-#ifdef PFQ
-      if (lane == 0 && !x.none) {
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          if (x.n[t] == 0) continue;
-#pragma unroll
-          for (int c = 0; c < D; c += 64)
-            tma_ahead(&qmap, c, x.token0[t], x.w.kvh * p.group + x.head0[t], x.w.s);
-        }
-      }
-#endif
       if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
         ok = false;
         break;
@@ -495,50 +494,75 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         if (any) o_read();
         if (live) *reinterpret_cast<float2 *>(part + D) = make_float2(wrong ? NAN : m, wrong ? 0.f : l);
       } else {
-        // kOut channels at a time to shared memory, then whole rows of them out
         const float inv = wrong ? NAN : l == 0.f ? 0.f : 1.f / l;
         __nv_bfloat16 *to =
             static_cast<__nv_bfloat16 *>(p.out) + x.w.s * p.os + token * p.ot + head * p.oh;
+        // kOut channels at a time to shared memory, then whole rows of them out
         constexpr int CH = TP::kOut, PPR = CH / 8;
         auto at = [](int rr, int c) {
           return rr * CH * 2 + ((c ^ (CH == 64 ? rr & 7 : (rr >> 1) & 3)) << 4);
         };
+        auto piece = [&](int c, unsigned char *place, auto at_) {  // 32 channels of the thread's row
+          uint32_t o[32] = {};
+          if (any) {
+            tmem_ld32(o, mine_o + c);
+            tmem_wait_ld();
+          }
+          if (any && c + 32 == D) o_read();
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              v[i] = pack2(__uint_as_float(o[e * 8 + 2 * i]) * inv,
+                           __uint_as_float(o[e * 8 + 2 * i + 1]) * inv);
+            *reinterpret_cast<uint4 *>(place + at_(e)) = make_uint4(v[0], v[1], v[2], v[3]);
+          }
+        };
+        auto copied = [&](auto left) {  // all but `left` of the warp's copies have left its place
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(decltype(left)::value) : "memory");
+          __syncwarp();
+        };
+        // Copies of 32 channels of 32 rows where the warp's rows are of one head and
+        // those without a token past the tensor's end, else row by row
+        if (TP::kCopyOut && p.box_heads == 1 &&
+            __all_sync(0xFFFFFFFFu, live || h > 0 || token >= p.tokens)) {
+          const bool some = __any_sync(0xFFFFFFFFu, live);
+          const int warp_token = __shfl_sync(0xFFFFFFFFu, token, 0);
 #pragma unroll 1
-        for (int c = 0; c < D; c += CH) {
-#pragma unroll
-          for (int c1 = 0; c1 < CH; c1 += 32) {
-            uint32_t o[32] = {};
-            if (any) {
-              tmem_ld32(o, mine_o + c + c1);
-              tmem_wait_ld();
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t v[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                v[i] = pack2(__uint_as_float(o[e * 8 + 2 * i]) * inv,
-                             __uint_as_float(o[e * 8 + 2 * i + 1]) * inv);
-              *reinterpret_cast<uint4 *>(rows + at(lane, c1 / 8 + e)) = make_uint4(v[0], v[1], v[2], v[3]);
-            }
+          for (int c = 0; c < D; c += 32) {
+            unsigned char *half = rows + (c & 32) * 64;
+            copied(std::integral_constant<int, 1>{});
+            piece(c, half, [&](int e) { return lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4); });
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && some) tma_store(&omap, half, c, warp_token, head, x.w.s);
           }
-          if (any && c + CH == D) o_read();
-          __syncwarp();
+        } else {
+          if (TP::kCopyOut) copied(std::integral_constant<int, 0>{});
+#pragma unroll 1
+          for (int c = 0; c < D; c += CH) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 32 / PPR) {
-            const int rr = i + lane / PPR, pc = lane % PPR;
-            const bool on = __shfl_sync(0xFFFFFFFFu, live, rr);
-            __nv_bfloat16 *row_at = reinterpret_cast<__nv_bfloat16 *>(
-                __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), rr));
-            if (on)
-              *reinterpret_cast<uint4 *>(row_at + c + pc * 8) =
-                  *reinterpret_cast<const uint4 *>(rows + at(rr, pc));
+            for (int c1 = 0; c1 < CH; c1 += 32)
+              piece(c + c1, rows, [&](int e) { return at(lane, c1 / 8 + e); });
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 32; i += 32 / PPR) {
+              const int rr = i + lane / PPR, pc = lane % PPR;
+              const bool on = __shfl_sync(0xFFFFFFFFu, live, rr);
+              __nv_bfloat16 *row_at = reinterpret_cast<__nv_bfloat16 *>(
+                  __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(to), rr));
+              if (on)
+                *reinterpret_cast<uint4 *>(row_at + c + pc * 8) =
+                    *reinterpret_cast<const uint4 *>(rows + at(rr, pc));
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
         if (live && p.lse) p.lse[row] = wrong ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       }
     } while (next_item(k++));
+    if (TP::kCopyOut && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     if (!ok && lane == 0) set_err(p.err, HKV_ERR_TIMEOUT);
   }
   tc_fence_before();
@@ -547,11 +571,11 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   if (warp == 0) tmem_free(tmem, TP::kCols);
 }
 
-// Rows as a tensor of [sequences][heads][tokens][D], read in boxes of 64
-// channels (128 bytes, 128-byte swizzle); rows past the last are zero
+// Rows as a tensor of [sequences][heads][tokens][D], in boxes of 64 channels (128
+// bytes, 128-byte swizzle) or 32; rows past the last are zero, and not written
 cudaError_t encode(CUtensorMap *map, const void *base, int D, int tokens, long long token_stride,
                    int heads, long long head_stride, int seqs, long long seq_stride, int box_tokens,
-                   int box_heads) {
+                   int box_heads, int box_channels = 64) {
   using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                               const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
                               CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -572,10 +596,11 @@ cudaError_t encode(CUtensorMap *map, const void *base, int D, int tokens, long l
   const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)seqs};
   const cuuint64_t strides[3] = {stride(token_stride, tokens), stride(head_stride, heads),
                                  stride(seq_stride, seqs)};
-  const cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, (cuuint32_t)box_heads, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)box_channels, (cuuint32_t)box_tokens, (cuuint32_t)box_heads, 1};
   const cuuint32_t step[4] = {1, 1, 1, 1};
   const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides,
-                       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       box_channels == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -585,13 +610,15 @@ cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
   using TP = TcPlan<D, TILES>;
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = allow_smem_of(cross_tc_kernel<D, TILES>, TP::kBytes, ready);
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, o;
   if (e == cudaSuccess)
     e = encode(&q, a.q, D, a.tokens, a.qt, a.heads, a.qh, a.seqs, a.qs, a.box_tokens, a.box_heads);
   if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
   if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
+  if (e == cudaSuccess)
+    e = encode(&o, a.out, D, a.tokens, a.ot, a.heads, a.oh, a.seqs, a.os, 32, 1, 32);
   if (e != cudaSuccess) return e;
-  return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v);
+  return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v, o);
 }
 
 }  // namespace
