@@ -467,6 +467,28 @@ def test_more_work_than_the_device_holds_of_unequal_sequences(dtype, out, D, S, 
             assert torch.equal(a.flip(0), o) and torch.equal(b.flip(0), lse)
 
 
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("S,T,heads,KV", [(2, 100, 3, 3), (2, 300, 3, 3), (1, 257, 4, 2), (2, 60, 6, 1)])
+def test_outs_between_other_rows(S, T, heads, KV, ragged):
+    """Views of outs leave the tokens, heads and sequences around them as they are."""
+    torch, H = mods()
+    D, N = 128, 90
+    q, k, v = qkv(torch, S, T, heads, KV, N, D, "bf16")
+    ql = [T - 37] + [T] * (S - 1) if ragged else None
+    want, wlse = run_cross(H, torch, q, k, v, qlens=ql)
+    check_cross(q, k, v, want, wlse, qlens=ql)
+    around = torch.full((S + 1, T + 5, heads + 2, D + 8), 3.0, dtype=q.dtype, device="cuda")
+    out = around[:S, 2:T + 2, 1:heads + 1, :D]
+    cfg = cfg_of(H, S, heads, D, "bf16")
+    tok, st = H.make_tokens(T, None if ql is None else ints(ql)), H.make_states(k, v)
+    n = H.hkv_cross_workspace_size(cfg, st, tok)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    H.hkv_cross_attention(cfg, st, tok, H.make_rows(q), H.make_rows(out), None, ws, n)
+    assert torch.equal(out, want)
+    out.fill_(3.0)
+    assert (around == 3.0).all()
+
+
 def test_no_lse_and_strided_views():
     """Queries and outs by heads, states by tokens (slices of one projection), no lse."""
     torch, H = mods()
