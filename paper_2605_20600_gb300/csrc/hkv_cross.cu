@@ -411,14 +411,14 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
   }
 }
 
-// Joins a query's ranges: W warps a query, each a run of its ranges in order. Two
-// dependent reads, 7 us for 40 queries of 147 ranges (with a warp a query the whole
-// call took 31 us instead of 25).
-constexpr int kJoinThreads = 256;
+// Joins a query's ranges: W warps a query, each a run of its ranges in order. What
+// bounds it: its launch, and a read of what has just been written. 5 queries of 8
+// heads in 147 ranges: the whole call takes 20.0 us, with eight warps a query that
+// read maxima and sums before the rows 21.6, with one 31.
 template <int D, typename O, int W>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(W == 16 ? 512 : 256)
     cross_join_kernel(const CrossArgs p, long long rows) {
-  constexpr int PF = D + 4, E = D / 32, ROWS = kJoinThreads / 32 / W;
+  constexpr int PF = D + 4, E = D / 32, ROWS = W == 16 ? 1 : 8 / W;
   __shared__ float s_acc[ROWS][W][D], s_ml[ROWS][W][2];
   pdl_wait();
   pdl_launch_dependents();
@@ -435,38 +435,36 @@ __global__ void __launch_bounds__(kJoinThreads)
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   bool bad = false;
-  // the ranges' maxima and sums, a lane each, 32 at a time; then their rows, a
-  // few on the way at a time
-  for (int k0 = 0; k0 < n; k0 += 32) {
-    const int here = min(32, n - k0);
+  // B ranges at a time: their rows, and their maxima and sums (a lane each)
+  constexpr int B = W == 16 ? 16 : 8;
+  for (int k0 = 0; k0 < n; k0 += B) {
+    const int here = min(B, n - k0);
+    float v[B][E];
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+      if (u < here) load_row<E>(first + (size_t)(k0 + u) * PF + lane * E, v[u]);
     float2 ml = make_float2(-INFINITY, 0.f);
     if (lane < here) ml = *reinterpret_cast<const float2 *>(first + (size_t)(k0 + lane) * PF + D);
     bad |= __any_sync(0xFFFFFFFFu, ml.x != ml.x && ml.y == 0.f);
     float top = ml.y != 0.f ? ml.x : -INFINITY;
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    for (int o = B / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    top = __shfl_sync(0xFFFFFFFFu, top, 0);
     const float mn = fmaxf(m, top), old = l == 0.f ? 0.f : ex2_approx(m - mn);
     const float f = ml.y == 0.f ? 0.f : ex2_approx(ml.x - mn);
     m = mn;
     float sum = ml.y * f;
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    l = l * old + sum;
+    for (int o = B / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    l = l * old + __shfl_sync(0xFFFFFFFFu, sum, 0);
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] *= old;
-    constexpr int B = W > 1 ? 16 : 8;
-    for (int j = 0; j < here; j += B) {
-      float v[B][E];
 #pragma unroll
-      for (int u = 0; u < B; ++u)
-        if (j + u < here) load_row<E>(first + (size_t)(k0 + j + u) * PF + lane * E, v[u]);
+    for (int u = 0; u < B; ++u) {
+      const float fu = __shfl_sync(0xFFFFFFFFu, f, u);
+      if (u < here && fu != 0.f) {
 #pragma unroll
-      for (int u = 0; u < B; ++u) {
-        const float fj = __shfl_sync(0xFFFFFFFFu, f, (j + u) & 31);
-        if (j + u < here && fj != 0.f) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] += v[u][e] * fj;
-        }
+        for (int e = 0; e < E; ++e) acc[e] += v[u][e] * fu;
       }
     }
   }
@@ -546,15 +544,17 @@ cudaError_t launch(const CrossArgs &a, const CrossPlan &pl, int dtype, int out_d
                                                           : launch_few<D, 16>(a, g, s);
   }
   if (e != cudaSuccess || a.splits == 1) return e;
-  // a warp a query, or eight where there are many ranges
   const long long queries = (long long)a.seqs * a.heads * a.tokens;
-  const bool many = a.splits > 16;
-  const int blocks = (int)(many ? queries : (queries + 7) / 8);
+  const int warps = a.splits <= 8 ? 1 : a.splits <= 16 ? 2 : 16;  // a query
+  const int blocks = (int)(warps == 16 ? queries : (queries * warps + 7) / 8);
+  auto join = [&](auto *kernel) {
+    return pdl_launch(kernel, blocks, warps == 16 ? 512 : 256, 0, s, a, queries);
+  };
   if (out_dtype == HKV_BF16)
-    return pdl_launch(many ? cross_join_kernel<D, bf16, 8> : cross_join_kernel<D, bf16, 1>, blocks,
-                      kJoinThreads, 0, s, a, queries);
-  return pdl_launch(many ? cross_join_kernel<D, float, 8> : cross_join_kernel<D, float, 1>, blocks,
-                    kJoinThreads, 0, s, a, queries);
+    return join(warps == 1 ? cross_join_kernel<D, bf16, 1>
+                : warps == 2 ? cross_join_kernel<D, bf16, 2> : cross_join_kernel<D, bf16, 16>);
+  return join(warps == 1 ? cross_join_kernel<D, float, 1>
+              : warps == 2 ? cross_join_kernel<D, float, 2> : cross_join_kernel<D, float, 16>);
 }
 
 }  // namespace
