@@ -585,17 +585,33 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
     pl.tiles = (int)((all + pl.rows - 1) / pl.rows);
   }
   const long long base = (long long)seqs * kv * pl.tiles;
-  // One round of CTAs, or (few query rows, whose partial results are small, and
-  // ranges of 512 keys) four, so that uneven ones even out; ranges long enough that
-  // joining them pays: a CTA takes about 3 us and 0.9 (16 rows) or 0.5 more for 64
-  // keys, and the join 2.5.
-  const long long least = pl.rows == 16 ? 192 : 256;
+  // Rounds of CTAs, whose ranges are long enough that joining them pays. Few query
+  // rows, whose partial results are small: one, or (ranges of 512 keys) four, so
+  // that uneven ones even out. More: none, one or two, by the times below (in us):
+  // two where the CTAs of one leave much of the device empty (fp32, 18 queries of 7 x
+  // 77 heads on 11 over up to 6401 states, 77 CTAs: 140 -> 67 us; 1200 of 20 heads
+  // over 8000, 100: 98 -> 87; four rounds 78 and 88).
   long long want = base < ctas ? ctas / base : 1;
-  if (want > keys / least) want = keys / least;
-  if (pl.rows == 16 && base < 4LL * ctas) {
-    long long four = (4LL * ctas + base - 1) / base;
-    if (four > keys / 512) four = keys / 512;
-    if (want < four) want = four;
+  if (pl.rows == 16) {
+    if (want > keys / 192) want = keys / 192;
+    if (base < 4LL * ctas) {
+      long long four = (4LL * ctas + base - 1) / base;
+      if (four > keys / 512) four = keys / 512;
+      if (want < four) want = four;
+    }
+  } else if (base < ctas) {
+    const double start = tc ? 4 : 5;  // of a CTA; of 64 keys more:
+    const double tile = !tc ? D / 64 * (dtype == HKV_FP32 ? 1.7 : 1.0) : pl.rows == 128 ? 0.5 : 0.8;
+    const double part = (double)seqs * heads * tokens * (D + 4) * 8 / 4e6;  // written and read
+    double least = start + keys / 64 * tile;
+    want = 1;
+    for (int rounds = 1; rounds <= 2; ++rounds) {
+      long long n = rounds * (long long)ctas / base;
+      if (n > keys / 256) n = keys / 256;
+      if (n < 2) continue;
+      const double us = rounds * (start + (double)keys / 64 / n * tile) + 2 + n * part;
+      if (us < least) least = us, want = n;
+    }
   }
   if (want > kMostSplits) want = kMostSplits;
   if (want < 1 || keys < 512) want = 1;

@@ -66,7 +66,7 @@ __device__ __forceinline__ Order order_of(const CrossArgs &p, F tiles_of) {
   const bool on = lane < p.seqs;
   int klen = !on ? 0 : p.klen ? p.klen[lane] : p.keys;
   int qlen = !on ? 0 : p.qlen ? p.qlen[lane] : p.tokens;
-  const bool first = threadIdx.x < 32 && blockIdx.x == 0;
+  const bool first = threadIdx.x < 32;  // of every CTA that is launched
   if (klen < 0 || klen > p.keys) {
     if (first) set_err(p.err, HKV_ERR_BOUNDS);
     klen = 0;

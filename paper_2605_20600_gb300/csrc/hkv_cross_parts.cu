@@ -15,10 +15,10 @@
 //          one before are made (two buffers of S, of the last parts and of O)
 //
 // What bounds it: the chain of loads, parts and products around each tile of keys;
-// the tensor pipe is busy for a third. 1024 fp32 queries and states, 32 heads of
-// 128: 140 us (123 TFLOP/s of the definition's products, 735 of bf16 ones; six
-// products of parts on mma.sync took 915); 257 padded queries over up to 777
-// states, 5 x 8 heads of 64: 28 us (83).
+// the tensor pipe is busy for 0.42. 1024 fp32 queries and states, 32 heads of 128:
+// 118 us (145 TFLOP/s of the definition's products, 873 of bf16 ones; six products
+// of parts on mma.sync took 915, Q loaded by the warps of K and V first 140); 257
+// padded queries over up to 777 states, 5 x 8 heads of 64: 22.5 us (28).
 #include "hkv_cross.cuh"
 #include "hkv_quant.cuh"
 #include "hkv_tcgen05.cuh"

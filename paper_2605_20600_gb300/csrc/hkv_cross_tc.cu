@@ -2,15 +2,15 @@
 // bf16 outs, on tcgen05.
 //
 // A CTA works on TILES query tiles of one (sequence, key head) and a range of keys
-// in tiles of 64 (96 for heads of 64: the weights of half as many channels bound
-// them, and longer tiles wait less often). A query tile is 128 tokens of a head, or all tokens of a few
-// heads of the group, 128 rows at most. One warp loads Q, and K and V tiles into a
-// ring of slots (TMA); four warps a query tile, a thread per row, turn scores into
-// weights: S = Q K^T lies in TMEM in two buffers, a thread reads its row of S,
-// writes the weights as bf16 over it, and they are the A operand of O += W V, which
-// stays in TMEM; a warp a query tile issues its products. A CTA that has issued the
-// loads of its work takes over that of a CTA which was not launched yet, so that
-// loads and first scores run beside the outs of the work before.
+// in tiles of 64 (96 for heads of 64, which the weights bound: longer tiles wait
+// less often). A query tile is 128 tokens of a head, or all tokens of a few heads of
+// the group, 128 rows at most. One warp loads Q, and K and V tiles into a ring of
+// slots (TMA); four warps a query tile, a thread per row, turn scores into weights:
+// S = Q K^T lies in TMEM in two buffers, a thread reads its row of S, writes the
+// weights as bf16 over it, and they are the A operand of O += W V, which stays in
+// TMEM; a warp a query tile issues its products. A CTA that has issued the loads of
+// its work takes over that of a CTA which was not launched yet, so that loads and
+// first scores run beside the outs of the work before.
 //
 // A row's reference maximum moves (and O and its sum are rescaled) only when a
 // tile's maximum is more than 2^8 above it, so that weights stay below 2^8. The
@@ -22,9 +22,9 @@
 // zero times what lies there could be NaN); scores past it are masked.
 //
 // What bounds it, heads of 128: the products, which keep the tensor pipe busy for
-// 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 322 us, 1705 TFLOP/s;
-// causal over 4288: 0.68, 223 us). On the way: products issued
-// from divergent code, each operand's descriptor moved to uniform registers, 470;
+// 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 318 us, 1729 TFLOP/s;
+// causal over 4288: 0.70, 222 us). On the way: products issued from divergent code,
+// each operand's descriptor moved to uniform registers, 470;
 // from uniform code, K and V in one wait, 387; S in two buffers, so that products
 // and weights of a tile overlap, 341; the scores after the next behind a tile's
 // W V, one wait a tile, 322. Two threads a row: 365 (their agreement on a maximum
@@ -610,12 +610,12 @@ cudaError_t launch(const CrossArgs &a, int grid, cudaStream_t s) {
   using TP = TcPlan<D, TILES>;
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = allow_smem_of(cross_tc_kernel<D, TILES>, TP::kBytes, ready);
-  CUtensorMap q, k, v, o;
+  CUtensorMap q, k, v, o = {};
   if (e == cudaSuccess)
     e = encode(&q, a.q, D, a.tokens, a.qt, a.heads, a.qh, a.seqs, a.qs, a.box_tokens, a.box_heads);
   if (e == cudaSuccess) e = encode(&k, a.k, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
   if (e == cudaSuccess) e = encode(&v, a.v, D, a.keys, a.kt, a.kv, a.kh, a.seqs, a.ks, TP::kKeys, 1);
-  if (e == cudaSuccess)
+  if (TP::kCopyOut && e == cudaSuccess)
     e = encode(&o, a.out, D, a.tokens, a.ot, a.heads, a.oh, a.seqs, a.os, 32, 1, 32);
   if (e != cudaSuccess) return e;
   return pdl_launch(cross_tc_kernel<D, TILES>, grid, TP::kThreads, TP::kBytes, s, a, q, k, v, o);
