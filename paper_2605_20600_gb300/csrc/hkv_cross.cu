@@ -11,7 +11,7 @@
 // What bounds them: DRAM. One bf16 query of 64 x 32 heads over 300 states of 128:
 // 59 us, 5.3 TB/s (tcgen05, with one of 128 rows in use, would take 64 keys a
 // microsecond and CTA); 8 key heads over 2000 states: 86 us, 6.1 TB/s; fp32, 32
-// heads over 300: 102 us, 6.2 TB/s (six products of parts on mma.sync: 400).
+// heads over 300: 98 us, 6.4 TB/s (six products of parts on mma.sync: 400).
 //
 // Precision of cross_kernel: queries, keys and values (bf16) enter as they are, the weights as
 // three bf16 parts for fp32 outs, which leaves nothing of them out, and as two,
@@ -297,15 +297,21 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
   }
   if (lo < hi) {
     int k0 = lo + warp * 32;
+#pragma unroll
+    for (int e = tid; e < R * PPR; e += kThreads) {
+      const int r = e / PPR, c = e % PPR;
+      const Row x = row_of(p, w.kvh, min(r, nq - 1));
+      const bool on = r < nq && x.token < w.qlen;
+      cp_async16_zfill(sq + e * 4, static_cast<const float *>(p.q) + w.s * p.qs +
+                                       (on ? x.token * p.qt + x.head * p.qh : 0) + c * 4, on);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
     if (k0 < hi) {
       load_rows(sk, K, k0);
       load_rows(sv, V, k0);
-    }
-    for (int e = tid; e < R * D; e += kThreads) {
-      const int r = e / D;
-      const Row x = row_of(p, w.kvh, min(r, nq - 1));
-      const bool on = r < nq && x.token < w.qlen;
-      sq[e] = on ? static_cast<const float *>(p.q)[w.s * p.qs + x.token * p.qt + x.head * p.qh + e % D] : 0.f;
+      asm volatile("cp.async.wait_group 2;" ::: "memory");
+    } else {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
     __syncthreads();
     for (; k0 < hi; k0 += kWarps * 32) {
@@ -347,8 +353,9 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
       // four channels a lane; heads of 64: lanes 16-31 take the odd keys
       constexpr int KS = 128 / D;
       const int first = lane / PPR, ch = lane % PPR;
+      const int most = min(32, hi - k0);
 #pragma unroll 4
-      for (int j = first; j < 32; j += KS) {
+      for (int j = first; j < most; j += KS) {
         const float4 vv = *reinterpret_cast<const float4 *>(sv + j * SM::kRow + ch * 16);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -540,8 +547,12 @@ cudaError_t launch(const CrossArgs &a, const CrossPlan &pl, int dtype, int out_d
   } else if (dtype == HKV_BF16) {
     e = out_dtype == HKV_BF16 ? launch_rows<D, bf16>(a, g, s) : launch_rows<D, float>(a, g, s);
   } else {
-    e = rows == 1 ? launch_few<D, 1>(a, g, s) : rows <= 4 ? launch_few<D, 4>(a, g, s)
-                                                          : launch_few<D, 16>(a, g, s);
+    // (arithmetic for no more rows than twice those there: 7 rows of 12 x 9 key heads
+    // of 64 over 253 states 14.2 -> 9.4 us, 6 of 17 x 8 of 128 over 333 37 -> 25.5)
+    e = rows == 1   ? launch_few<D, 1>(a, g, s)
+        : rows <= 4 ? launch_few<D, 4>(a, g, s)
+        : rows <= 8 ? launch_few<D, 8>(a, g, s)
+                    : launch_few<D, 16>(a, g, s);
   }
   if (e != cudaSuccess || a.splits == 1) return e;
   const long long queries = (long long)a.seqs * a.heads * a.tokens;
