@@ -26,6 +26,15 @@ namespace {
 constexpr int kStages = 2;
 using bf16 = __nv_bfloat16;
 
+// the CTA's work. SORTED: by the sequences' lengths (kernels of their own, since
+// the smallest wait for their instructions)
+template <bool SORTED>
+__device__ __forceinline__ Work few_work(const CrossArgs &p) {
+  if (!SORTED) return work_of(p, blockIdx.x);
+  const int piece = piece_at(p, order_of(p, [](int tokens) { return tokens > 0 ? 1 : 0; }), blockIdx.x);
+  return piece < 0 ? Work{} : work_of(p, piece);
+}
+
 template <int D, int W>
 struct CSmem {
   static constexpr int kStep = D == 64 ? 32 : 16;  // keys of a tile a warp
@@ -36,7 +45,7 @@ struct CSmem {
   static_assert(W * 16 * D * 4 <= kTiles, "the warps' outputs reuse the tiles");
 };
 
-template <int D, typename O, int W>
+template <int D, typename O, int W, bool SORTED>
 __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(const __grid_constant__ CrossArgs p) {
   using SM = CSmem<D, W>;
   constexpr int kKeys = SM::kKeys, KW = SM::kStep, NB = KW / 16, kThreads = W * 32;
@@ -47,7 +56,7 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  const Work w = work_of(p, blockIdx.x);
+  const Work w = few_work<SORTED>(p);
   const int nq = p.group * p.tokens;  // query rows of the (sequence, key head)
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);
@@ -259,7 +268,7 @@ struct FSmem {
   static constexpr int kTotal = kWarps * kWarp + R * D * 4 + kWarps * R * 32 * 4;
   static_assert(R * D * 4 <= kWarp, "a warp's outputs reuse its tiles");
 };
-template <int D, int R>
+template <int D, int R, bool SORTED>
 __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(const __grid_constant__ CrossArgs p) {
   using SM = FSmem<D, R>;
   constexpr int PF = D + 4, PPR = D / 4, kWarps = SM::kWarps, kThreads = kWarps * 32;
@@ -268,7 +277,7 @@ __global__ void __launch_bounds__(FSmem<D, R>::kWarps * 32) cross_few_kernel(con
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  const Work w = work_of(p, blockIdx.x);
+  const Work w = few_work<SORTED>(p);
   const int nq = p.group * p.tokens;
   const int lo = w.sp * p.split_len;
   const int hi = min(keys_of_rows(p, w, 0, nq), lo + p.split_len);
@@ -511,12 +520,12 @@ __global__ void __launch_bounds__(W == 16 ? 512 : 256)
   if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-template <int D, typename O, int W>
+template <int D, typename O, int W, bool SORTED>
 cudaError_t launch_warps(const CrossArgs &a, int grid, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(cross_kernel<D, O, W>, CSmem<D, W>::kTotal, ready);
+  const cudaError_t e = allow_smem_of(cross_kernel<D, O, W, SORTED>, CSmem<D, W>::kTotal, ready);
   if (e != cudaSuccess) return e;
-  return pdl_launch(cross_kernel<D, O, W>, grid, W * 32, CSmem<D, W>::kTotal, s, a);
+  return pdl_launch(cross_kernel<D, O, W, SORTED>, grid, W * 32, CSmem<D, W>::kTotal, s, a);
 }
 // Twelve warps an SM as CTAs of two, whose starts and ends lie apart more, as
 // soon as there are enough of them: one query of 64 x 32 heads over up to 300
@@ -524,16 +533,21 @@ cudaError_t launch_warps(const CrossArgs &a, int grid, cudaStream_t s) {
 // eight: 32 heads over 300 states take 6.5 us, with four 6.7; over 1000 12.6 and 16.
 template <int D, typename O>
 cudaError_t launch_rows(const CrossArgs &a, int grid, cudaStream_t s) {
-  if (grid >= 912) return launch_warps<D, O, 2>(a, grid, s);
-  if (grid <= 152 && a.split_len > 128) return launch_warps<D, O, 8>(a, grid, s);
-  return launch_warps<D, O, 4>(a, grid, s);
+  if (grid >= 912)
+    return a.sorted ? launch_warps<D, O, 2, true>(a, grid, s) : launch_warps<D, O, 2, false>(a, grid, s);
+  if (grid <= 152 && a.split_len > 128) return launch_warps<D, O, 8, false>(a, grid, s);
+  return a.sorted ? launch_warps<D, O, 4, true>(a, grid, s) : launch_warps<D, O, 4, false>(a, grid, s);
+}
+template <int D, int R, bool SORTED>
+cudaError_t launch_few_of(const CrossArgs &a, int grid, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem_of(cross_few_kernel<D, R, SORTED>, FSmem<D, R>::kTotal, ready);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(cross_few_kernel<D, R, SORTED>, grid, FSmem<D, R>::kWarps * 32, FSmem<D, R>::kTotal, s, a);
 }
 template <int D, int R>
 cudaError_t launch_few(const CrossArgs &a, int grid, cudaStream_t s) {
-  static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem_of(cross_few_kernel<D, R>, FSmem<D, R>::kTotal, ready);
-  if (e != cudaSuccess) return e;
-  return pdl_launch(cross_few_kernel<D, R>, grid, FSmem<D, R>::kWarps * 32, FSmem<D, R>::kTotal, s, a);
+  return a.sorted ? launch_few_of<D, R, true>(a, grid, s) : launch_few_of<D, R, false>(a, grid, s);
 }
 
 template <int D>
@@ -630,8 +644,10 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   pl.splits = (keys + pl.split_len - 1) / pl.split_len;
   // Where there are more CTAs than fit, by length: 16 x 577 padded queries of 20 heads
   // on 4 over up to 1025 states 35.6 -> 29.8 us; fp32, 16 x 257 over up to 777, 60 -> 49,
-  // but 0.3 more a CTA (542 over up to 33: 56 -> 58.5).
-  pl.sorted = pl.rows != 16 && seqs > 1 && seqs <= 32 && base > ctas && (tc || keys >= 256);
+  // one query of 21 x 12 heads over up to 2861 in ranges 28.5 -> 23.6; but 0.3 more a
+  // CTA (542 over up to 33: 56 -> 58.5).
+  pl.sorted = seqs > 1 && seqs <= 32 && base * pl.splits > ctas &&
+              (tc || keys >= (pl.rows == 16 ? 512 : 256));
   pl.part_bytes =
       pl.splits > 1 ? (size_t)seqs * heads * tokens * pl.splits * (D + 4) * sizeof(float) : 0;
   return pl;

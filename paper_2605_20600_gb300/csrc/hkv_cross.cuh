@@ -51,11 +51,11 @@ __device__ __forceinline__ Work work_of(const CrossArgs &p, int b) {
   }
   return w;
 }
-// The pieces of work (work_of's) in falling order of their sequence's states, so
-// that those which end last are short, and without those that have no rows. A lane
-// has a sequence.
+// The pieces of work (work_of's) of each range of keys in falling order of their
+// sequence's states, so that those which end last are short, and without those that
+// have no rows. A lane has a sequence.
 struct Order {
-  int first, tiles, all;  // its first piece; query tiles with rows; pieces of all sequences
+  int first, tiles, all;  // of a range: its first piece; query tiles with rows; all pieces
 };
 // For the whole warp; tiles_of(n): query tiles that n tokens of a sequence reach.
 template <typename F>
@@ -89,11 +89,13 @@ __device__ __forceinline__ Order order_of(const CrossArgs &p, F tiles_of) {
 // work_of's number of piece i, or -1
 __device__ __forceinline__ int piece_at(const CrossArgs &p, const Order &o, int i) {
   if (!p.sorted) return i;
+  const int per = p.tiles * p.kv * p.seqs, range = i / per;
+  i -= range * per;
   if (i >= o.all) return -1;
   const int at = i - o.first;
   const int s = __ffs(__ballot_sync(0xFFFFFFFFu, at >= 0 && at < o.tiles * p.kv)) - 1;
   const int n = __shfl_sync(0xFFFFFFFFu, o.tiles, s), in = __shfl_sync(0xFFFFFFFFu, at, s);
-  return (s * p.kv + in / n) * p.tiles + p.tiles - n + in % n;
+  return range * per + (s * p.kv + in / n) * p.tiles + p.tiles - n + in % n;
 }
 // a query row of a (sequence, key head): which head of the group, which token
 struct Row {

@@ -423,7 +423,11 @@ def test_attention_over_states(case, ragged, causal):
     ("bf16", "bf16", 64, 16, 20, 4, 300, 200), ("bf16", "bf16", 128, 32, 24, 6, 40, 100),
     ("bf16", "bf16", 64, 31, 12, 12, 100, 90), ("bf16", "bf16", 64, 33, 12, 12, 100, 90),
     ("fp32", "fp32", 64, 7, 11, 11, 300, 300), ("fp32", "fp32", 128, 9, 20, 4, 130, 257),
-    ("bf16", "fp32", 64, 5, 16, 16, 257, 600)])
+    ("bf16", "fp32", 64, 5, 16, 16, 257, 600),
+    # in ranges of keys
+    ("bf16", "fp32", 64, 21, 12, 12, 1, 1200), ("bf16", "bf16", 128, 32, 16, 8, 3, 1100),
+    ("fp32", "fp32", 128, 20, 24, 12, 3, 1100), ("fp32", "fp32", 64, 7, 22, 11, 18, 1600),
+    ("bf16", "bf16", 64, 10, 10, 10, 200, 4000)])
 def test_more_work_than_the_device_holds_of_unequal_sequences(dtype, out, D, S, heads, KV, T, N, which):
     """Up to 32 sequences are worked on by length; equal ones, empty ones, lengths that
     are out of range and batches with one kind of lengths only."""
