@@ -4,9 +4,10 @@
 // cross_kernel (here) takes up to 16 bf16 query rows of a (sequence, key head), the
 // heads of the group one after the other, and a range of keys on mma.sync
 // m16n8k16, 16 keys of a tile a warp (32 for heads of 64: as many bytes on their way;
-// single queries of 12 heads over up to 2861 states 30.4 -> 28.6 us); cross_few_kernel as many fp32 rows without
-// the tensor core; the ranges of one query are joined by a second kernel. More rows
-// are hkv_cross_tc.cu's and hkv_cross_parts.cu's.
+// single queries of 21 x 12 heads over up to 2861 states 30.4 -> 28.6 us);
+// cross_few_kernel as many fp32 rows without the tensor core; the ranges of one query
+// are joined by a second kernel. More rows are hkv_cross_tc.cu's and
+// hkv_cross_parts.cu's.
 //
 // What bounds them: DRAM. One bf16 query of 64 x 32 heads over 300 states of 128:
 // 59 us, 5.3 TB/s (tcgen05, with one of 128 rows in use, would take 64 keys a
