@@ -130,9 +130,11 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
   // two pieces; interleaved: of the pairs themselves, the first piece's first
   uint64_t c[2], sn[2], wa[2], wb[2], ba[2], bb[2];
   const bool shared = NORM != 0 && x.wh == 0;
-  // (the arithmetic below is a warp's, rows or none: 8 x 4288 padded tokens, on average
-  // half of them there, 213 us, 168 without that of the padding)
-  if (!__any_sync(0xFFFFFFFFu, on)) return;
+  // The arithmetic below is a warp's, rows or none: 8 x 4288 padded tokens, on average
+  // half of them there, 213 us, 168 without that of the padding. RMS norms ask behind
+  // their first loads, and few rows not at all (5 x 1001 of 18 heads 6.3 us, 6.8 with
+  // it); layer norms spill unless they ask here (8 x 4288 tokens 391 us against 296).
+  if (NORM == HKV_NORM_LAYER && !__any_sync(0xFFFFFFFFu, on)) return;
   for (int r0 = 0; r0 < most; r0 += U) {
     Raw ra[U], rb[U];
 #pragma unroll
@@ -142,6 +144,7 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
         rb[u] = *reinterpret_cast<const Raw *>(in + (r0 + u) * in_step + step);
       }
     if (r0 == 0) {
+      if (NORM == HKV_NORM_RMS && most >= 8 && !__any_sync(0xFFFFFFFFu, on)) return;
       if (shared && x.weight) {
         const T *w = static_cast<const T *>(x.weight) + ca;
         P::unpack(*reinterpret_cast<const Raw *>(w), wa);

@@ -242,6 +242,37 @@ def test_norms_with_the_rotation(case):
         assert np.array_equal(host(ins[i])[~live], host(parts[i])[~live])
 
 
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("dtype,D,HQ,KV", [("bf16", 64, 40, 8), ("fp32", 128, 24, 24)])
+def test_norms_of_long_padded_batches(dtype, D, HQ, KV, kind):
+    """Many rows a thread: tokens there are as in a full batch, those behind left alone."""
+    torch, H = mods()
+    S, T = 5, 900
+    cfg = cfg_of(H, S, HQ, D, dtype)
+    x = torch.randn(S, T, HQ + 2 * KV, D, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    rope, norm = H.hkv_make_rope(head_dim=D), H.make_norm(H.HKV_NORM_RMS if kind == "rms" else H.HKV_NORM_LAYER, 1e-5)
+    pos, parts = ints(np.arange(T)[None]), (x[:, :, :HQ], x[:, :, HQ:HQ + KV], x[:, :, HQ + KV:])
+    got = []
+    for lens in (None, [T, 0, 1, 450, T - 1]):
+        out = torch.full_like(x, 7.0)
+        outs = (out[:, :, :HQ], out[:, :, HQ:HQ + KV], out[:, :, HQ + KV:])
+        tok = H.make_tokens(T, None if lens is None else ints(lens), pos)
+        H.hkv_qk_norm_rope(cfg, norm, rope, tok, *(H.make_rows(p) for p in parts), *(H.make_rows(o) for o in outs))
+        got.append(out)
+    full, padded = got
+    live = torch.arange(T, device="cuda")[None] < ints(lens)[:, None]
+    assert torch.equal(padded[live], full[live]) and (padded[~live] == 7.0).all()
+    xin = host(x[3, 440:460, :HQ])
+    want = P.norm(xin, kind, float(np.float32(1e-5)), None, None)
+    tol = norm_error(xin, kind, float(np.float32(1e-5)), None) + 2 * U * np.abs(want)
+    freq = P.frequencies(D, (D // 2,))
+    a = np.broadcast_to(P.angles_of(np.arange(440, 460)[None, None], freq, (D // 2,))[0][:, None], (20, HQ, D // 2))
+    turned = rotation_error(want, a, "half", 1.0)
+    tol = rotation_error(tol, np.zeros(a.shape), "half", 1.0) / (10 * U) + turned
+    want = P.rotate(want, a, "half")
+    close(host(full[3, 440:460, :HQ]), want, tol + 2 * U * np.abs(want), dtype)
+
+
 def test_rows_of_extremes():
     """Zeros, infinities and NaN stay in their row; eps carries a row of zeros."""
     torch, H = mods()
