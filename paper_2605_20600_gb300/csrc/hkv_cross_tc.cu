@@ -524,10 +524,14 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           __syncwarp();
         };
         // Copies of 32 channels of 32 rows where the warp's rows are of one head and
-        // those without a token past the tensor's end, else row by row
-        if (TP::kCopyOut && p.box_heads == 1 &&
-            __all_sync(0xFFFFFFFFu, live || h > 0 || token >= p.tokens)) {
-          const bool some = __any_sync(0xFFFFFFFFu, live);
+        // those without a token past the tensor's end, else row by row. The halves of
+        // the warp's place take turns and all copies but the last are waited for, so
+        // who writes a half copies it too: a warp without rows writes none (the last
+        // copy of the work before may still read the second).
+        if (!__any_sync(0xFFFFFFFFu, live)) {
+          if (any) o_read();
+        } else if (TP::kCopyOut && p.box_heads == 1 &&
+                   __all_sync(0xFFFFFFFFu, live || h > 0 || token >= p.tokens)) {
           const int warp_token = __shfl_sync(0xFFFFFFFFu, token, 0);
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
@@ -536,7 +540,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
             piece(c, half, [&](int e) { return lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4); });
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0 && some) tma_store(&omap, half, c, warp_token, head, x.w.s);
+            if (lane == 0) tma_store(&omap, half, c, warp_token, head, x.w.s);
           }
         } else {
           if (TP::kCopyOut) copied(std::integral_constant<int, 0>{});
