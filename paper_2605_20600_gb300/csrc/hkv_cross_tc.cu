@@ -137,6 +137,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
   __shared__ uint64_t s_v[TILES];                     // O holds a key tile's products
   __shared__ uint64_t s_q[TILES], s_qe[TILES];        // Q is there; its last product is done
   __shared__ uint64_t s_oe[TILES];                    // O has been read
+  __shared__ int s_left[TILES * 4];                   // item that a warp did not wait for, or -1
   __shared__ uint64_t s_edge, s_drain;
   __shared__ uint32_t s_tmem;
   unsigned char *dyn = dyn_raw + ((1024u - (smem_u32(dyn_raw) & 1023u)) & 1023u);
@@ -148,6 +149,7 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       mbar_init(&s_nf[i], 1);
       mbar_init(&s_ne[i], TILES * 5);
     }
+    for (int i = 0; i < TILES * 4; ++i) s_left[i] = -1;
     mbar_init(&s_asked, 1);
     for (int i = 0; i < SLOTS; ++i) {
       mbar_init(&s_full[i], 1);
@@ -242,8 +244,8 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           }
         }
         if (edge) {
-          if (lane == 0) next_cta_ask(&s_answer, &s_asked);
-          ahead = true;
+          ahead = k < 2 || __all_sync(0xFFFFFFFFu, mbar_test_wait(&s_ne[k & 1], ((k >> 1) - 1) & 1));
+          if (ahead && lane == 0) next_cta_ask(&s_answer, &s_asked);
           ok = ok && wait(&s_edge, edges++ & 1);
           if (!ok) break;
           for (int e = lane; e < past * (D / 8); e += 32) {
@@ -256,8 +258,17 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
           if (lane == 0) mbar_arrive(&s_full[slot]);
         }
       }
-      // the next item that has rows to write; asked for only now, so that what is
-      // left at the end goes to the CTA that is free first
+      // The next item that has rows to write; asked for only now, so that what is
+      // left at the end goes to the CTA that is free first. What has been taken over
+      // nobody else does, so it is asked for only when there is room to hand it on
+      // (`ahead` has made sure). The other warps may take the limit before they read
+      // on, so this wait may take several.
+      bool room = ahead || k < 2;
+      for (int i = 0; i < 4 && !room; ++i) {
+        room = wait(&s_ne[k & 1], ((k >> 1) - 1) & 1);
+        ok = ok && room;
+      }
+      if (!room) break;
       do {
         if (!ahead && lane == 0) next_cta_ask(&s_answer, &s_asked);
         ahead = false;
@@ -269,10 +280,6 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
         if (item >= 0) x = item_of<D, TILES>(p, piece_at(p, order, item));
         else x.none = true;
       } while (!x.any && !x.none);
-      if (k >= 2 && !wait(&s_ne[k & 1], ((k >> 1) - 1) & 1)) {
-        ok = false;
-        break;
-      }
       if (lane == 0) {
         s_item[k & 1] = x;
         mbar_arrive(&s_nf[k & 1]);
@@ -567,12 +574,38 @@ __global__ void __launch_bounds__(TcPlan<D, TILES>::kThreads, TILES == 2 ? 1 : 2
       }
     } while (next_item(k++));
     if (TP::kCopyOut && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    if (!ok && lane == 0) set_err(p.err, HKV_ERR_TIMEOUT);
+    if (!ok && lane == 0) {
+      set_err(p.err, HKV_ERR_TIMEOUT);
+      if (!x.none) s_left[warp] = k - 1;
+    }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == 0) tmem_free(tmem, TP::kCols);
+  // Items that were handed on after a warp's wait for the next one had run out (two
+  // at most: there is no room for more until it reads them) get their NaN here, where
+  // the code costs the loop above nothing (in it: 112 -> 114 us for 8 x 4160 queries of
+  // 32 heads over 120 states).
+  if (warp < TILES * 4 && s_left[warp] >= 0) {
+    const int t = warp >> 2, r = tid & 127, h = r / p.box_tokens;
+    for (int k = s_left[warp]; mbar_test_wait(&s_nf[k & 1], (k >> 1) & 1); ++k) {
+      const Item<TILES> &y = s_item[k & 1];
+      if (y.none) break;
+      const int token = y.token0[t] + r - h * p.box_tokens, g = y.head0[t] + h, head = y.w.kvh * p.group + g;
+      if (h >= p.box_heads || g >= p.group || token >= y.w.qlen) continue;
+      const size_t row = ((size_t)y.w.s * p.heads + head) * p.tokens + token;
+      if (p.splits > 1) {
+        *reinterpret_cast<float2 *>(p.part + (row * p.splits + y.w.sp) * PF + D) = make_float2(NAN, 0.f);
+        continue;
+      }
+      __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(p.out) + y.w.s * p.os + token * p.ot + head * p.oh;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 8)
+        *reinterpret_cast<uint4 *>(to + c) = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+      if (p.lse) p.lse[row] = NAN;
+    }
+  }
 }
 
 // Rows as a tensor of [sequences][heads][tokens][D], in boxes of 64 channels (128
