@@ -93,6 +93,8 @@ template <typename T, int D, int NORM, bool PAIRS, int U>
 __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
     heads_kernel(const __grid_constant__ HeadsArgs a, uint32_t places) {
   constexpr int N = 4, G = D / (2 * N);
+  // pairs that do not turn go out as they were read: a NaN's bits too
+  constexpr bool kKeep = NORM == 0 && PAIRS && sizeof(T) == 2;
   using P = Piece<T>;
   using Raw = typename P::Raw;
   pdl_wait();
@@ -119,6 +121,7 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
   // the thread's two pieces; the channels behind R of a half layout two by two
   const bool apart = !PAIRS && N * g < R / 2;
   const int ca = apart ? N * g : 2 * N * g, step = apart ? R / 2 : N;
+  const int turning = PAIRS ? min(max(R / 2 - N * (int)g, 0), 4) : apart ? 4 : 0;  // of its 4 pairs
   const int hfirst = chunk * x.chunk + first, h1 = min(x.heads, (int)(chunk + 1) * x.chunk);
   const T *in = static_cast<const T *>(x.in) + s * x.is + t * x.it + hfirst * x.ih + ca;
   T *out = static_cast<T *>(x.out) + s * x.os + t * x.ot + hfirst * x.oh + ca;
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
     for (int u = 0; u < U; ++u) {
       if (r0 + u >= most) break;
       const bool live = r0 + u < rows;
-      if ((NORM == 0 || !x.norm) && R == 0) {  // a copy
+      if (NORM == 0 ? turning == 0 : !x.norm && R == 0) {  // a copy
         if (live) {
           *reinterpret_cast<Raw *>(out + (r0 + u) * out_step) = ra[u];
           *reinterpret_cast<Raw *>(out + (r0 + u) * out_step + step) = rb[u];
@@ -223,14 +226,19 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
       }
       if (!live) continue;
       if (PAIRS) {
-        if (R > 0) {
+        auto turned = [&](int k) {  // pair (x, y): c x - s y, s x + c y
+          uint64_t &v = k < 2 ? va[k & 1] : vb[k & 1];
+          const float cc = k & 1 ? high(c[k / 2]) : low(c[k / 2]);
+          const float ss = k & 1 ? high(sn[k / 2]) : low(sn[k / 2]);
+          v = pair_of(low(v) * cc - high(v) * ss, low(v) * ss + high(v) * cc);
+        };
+        if (kKeep || R == D) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {  // pairs (x, y): c x - s y, s x + c y
-            uint64_t &v = k < 2 ? va[k & 1] : vb[k & 1];
-            const float cc = k & 1 ? high(c[k / 2]) : low(c[k / 2]);
-            const float ss = k & 1 ? high(sn[k / 2]) : low(sn[k / 2]);
-            v = pair_of(low(v) * cc - high(v) * ss, low(v) * ss + high(v) * cc);
-          }
+          for (int k = 0; k < 4; ++k) turned(k);
+        } else {  // (the others not by a turn of zero: y may be infinite)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < turning) turned(k);
         }
       } else if (apart) {
 #pragma unroll
@@ -240,8 +248,16 @@ __global__ void __launch_bounds__(kHeadThreads, sizeof(T) == 4 ? 3 : 4)
           vb[k] = fma2(x0, sn[k], mul2(y0, c[k]));
         }
       }
-      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step) = P::pack(va);
-      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step + step) = P::pack(vb);
+      Raw pa = P::pack(va), pb = P::pack(vb);
+      if constexpr (kKeep) {
+        if (R < D) {
+          if (turning < 2) pa.y = ra[u].y;
+          if (turning < 3) pb.x = rb[u].x;
+          if (turning < 4) pb.y = rb[u].y;
+        }
+      }
+      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step) = pa;
+      *reinterpret_cast<Raw *>(out + (r0 + u) * out_step + step) = pb;
     }
   }
 }
@@ -266,8 +282,9 @@ __global__ void __launch_bounds__(kHeadThreads)
   const HeadSet &x = a.set[i];
   const T *in = static_cast<const T *>(x.in) + s * x.is + t * x.it + h * x.ih;
   float v[E];
+  T raw[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = Elem<T>::load1(in, lane + 32 * e);
+  for (int e = 0; e < E; ++e) raw[e] = in[lane + 32 * e], v[e] = Elem<T>::load1(raw, e);
   if (NORM != 0 && x.norm) {
     float mean = 0.f, sum = 0.f;
     if (NORM == HKV_NORM_LAYER) {
@@ -301,6 +318,10 @@ __global__ void __launch_bounds__(kHeadThreads)
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int ch = lane + 32 * e;
+    if (ch >= R && (NORM == 0 || !x.norm)) {  // as it was read: a NaN's bits too
+      out[ch] = raw[e];
+      continue;
+    }
     if (ch < R) {
       const bool second = ch >= R / 2;
       float c, sn;
