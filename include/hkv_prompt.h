@@ -192,14 +192,17 @@ size_t hkv_cross_workspace_size(const hkv_config *cfg, const hkv_states *states,
  * Scores and sums are fp32. The weights exp(score - a reference) are fp32 in
  * lse; their products with v take them in three bf16 parts for fp32 outs, and
  * for bf16 outs in two, or, for batches of many queries, rounded to bf16.
- * An infinite or NaN element of a query or of a state that counts shows in the
- * outputs that its products enter as a number that is not finite; with
- * HKV_ATTN_CAUSAL one of v may show in earlier queries too, whose weight of zero
- * it meets. What lies in rows from a length on shows nowhere. A sequence
- * whose number of states is out of range gets NaN, and HKV_ERR_BOUNDS in the
- * states' error word; queries whose products did not finish within the
- * kernel's limit of two seconds get NaN, with HKV_ERR_TIMEOUT. out must not
- * overlap q or the states. */
+ * A key whose score is -inf (an infinite element against one of the other sign,
+ * products below fp32's range) weighs nothing, and a query that has no other keys
+ * gets zeros and -inf. Any other infinite or NaN element of a query or of a state
+ * that counts shows in the outputs that its products enter as a number that is not
+ * finite (NaN also where the definition gives an infinity); with HKV_ATTN_CAUSAL one
+ * of v may show in earlier queries too, whose weight of zero it meets. A key whose
+ * products of finite elements lie above fp32's range shows so too, or weighs nothing.
+ * What lies in rows from a length on shows nowhere. A sequence whose number of
+ * states is out of range gets NaN, and HKV_ERR_BOUNDS in the states' error word;
+ * queries whose products did not finish within the kernel's limit of two seconds get
+ * NaN, with HKV_ERR_TIMEOUT. out must not overlap q or the states. */
 hkv_status hkv_cross_attention(const hkv_config *cfg, const hkv_states *states,
                                const hkv_tokens *tokens, const hkv_rows *q, const hkv_rows *out,
                                float *lse, void *workspace, size_t ws_bytes, int flags,

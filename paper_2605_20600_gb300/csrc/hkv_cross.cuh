@@ -22,6 +22,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// ... NaN where one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // what a CTA works on
 struct Work {
   int s, kvh, tile, sp;   // sequence, key head, query tile, key range

@@ -91,6 +91,30 @@ __device__ __forceinline__ int piece_of(int r, int c) {
   return (c >> 3) * ROWS * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
 }
 
+// Scores that are NaN or +inf are computed once more from the elements: the parts of
+// an infinite one have signs of their own, so that its products meet as inf - inf, and
+// where a product of finite ones overflows, those of their small parts may have done so
+// before it with the other sign. One thread's row and 64 keys, in TMEM at `at`, of
+// which `left` count. (A function, so that its code costs the loop nothing: with it
+// there 5 x 257 queries of 8 heads over 777 states take 28.7 us instead of 26.8.)
+template <int D>
+__device__ __noinline__ void plain_scores(const float *q, const float *k, long long kt, int left, uint32_t at) {
+#pragma unroll 1
+  for (int j = 0; j < kKeys; ++j) {
+    uint32_t bits;
+    tmem_ld1(bits, at + j);
+    tmem_wait_ld();
+    float sum = __uint_as_float(bits);
+    if (j < left && !(sum < INFINITY)) {
+      sum = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < D; ++c) sum = fmaf(q[c], k[j * kt + c], sum);
+    }
+    tmem_st1(at + j, __float_as_uint(sum));
+  }
+  tmem_wait_st();
+}
+
 template <int D, typename T>
 __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_constant__ CrossArgs p) {
   using SM = PartsSmem<D, T>;
@@ -279,23 +303,38 @@ __global__ void __launch_bounds__(kThreads, 1) cross_parts_kernel(const __grid_c
       if (!ok) break;
       tc_fence_after();
       uint32_t s[2][32];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) tmem_ld32(s[c], tmem + lanes + kS + b * 64 + c * 32);
-      tmem_wait_ld();
       const int left = seen - lo - i * kKeys;  // keys of the tile that count
-      if (left < kKeys) {
+      auto load_scores = [&] {
 #pragma unroll
-        for (int j = 0; j < kKeys; ++j)
-          if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
+        for (int c = 0; c < 2; ++c) tmem_ld32(s[c], tmem + lanes + kS + b * 64 + c * 32);
+        tmem_wait_ld();
+      };
+      load_scores();
+      float mx;
+      auto mask_and_max = [&] {
+        if (left < kKeys) {
+#pragma unroll
+          for (int j = 0; j < kKeys; ++j)
+            if (j >= left) s[j >> 5][j & 31] = 0xFF800000u;  // -inf
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kKeys; j += 8)
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            top[u] = max3_nan(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
+                              __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
+        mx = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * p.qscale;
+      };
+      mask_and_max();
+      if (NP > 1 && __any_sync(0xFFFFFFFFu, !(mx < INFINITY))) {
+        const Row x = row_of(p, w.kvh, min(r, all - 1));
+        plain_scores<D>(static_cast<const float *>(p.q) + w.s * p.qs + x.token * p.qt + x.head * p.qh,
+                        static_cast<const float *>(p.k) + w.s * p.ks + w.kvh * p.kh + (lo + i * kKeys) * p.kt,
+                        p.kt, left, tmem + lanes + kS + b * 64);
+        load_scores();
+        mask_and_max();
       }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int j = 0; j < kKeys; j += 8)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          top[u] = max3(top[u], __uint_as_float(s[j >> 5][(j & 31) + 2 * u]),
-                        __uint_as_float(s[j >> 5][(j & 31) + 2 * u + 1]));
-      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.qscale;
       // (the reference stays finite: scores of -inf weigh nothing against it)
       const float mn = fmaxf(m, mx), f = mn == m ? 1.f : ex2_approx(m - mn);
       m = mn;
