@@ -97,6 +97,7 @@ class hkv_rope(Structure):
 
 class hkv_rows(Structure):
     of = None   # (sequences, tokens, head_dim) of the rows, where make_rows knows them
+    on = None   # the device's number, -1 for the host, where it is known (as of the following)
     _fields_ = [
         ("data", c_void_p), ("seq_stride", c_int64), ("token_stride", c_int64),
         ("head_stride", c_int64), ("n_heads", c_int32), ("dtype", c_int32),
@@ -105,6 +106,7 @@ class hkv_rows(Structure):
 
 class hkv_tokens(Structure):
     of = None   # (sequences or None, axes, rows of positions), where make_tokens knows them
+    on = None
     _fields_ = [
         ("n_tokens", c_int32), ("reserved", c_int32), ("len", c_void_p), ("pos", c_void_p),
         ("pos_axis_stride", c_int64), ("pos_seq_stride", c_int64), ("err", c_void_p),
@@ -113,6 +115,7 @@ class hkv_tokens(Structure):
 
 class hkv_norm(Structure):
     of = None   # (dtype, head_dim, heads of q's and of k's weights or None), where make_norm knows them
+    on = None
     _fields_ = [
         ("kind", c_int32), ("eps", c_float), ("q_weight", c_void_p), ("q_bias", c_void_p),
         ("k_weight", c_void_p), ("k_bias", c_void_p), ("q_head_stride", c_int64),
@@ -122,6 +125,7 @@ class hkv_norm(Structure):
 
 class hkv_states(Structure):
     of = None   # (dtype, sequences, head_dim) of the states, where make_states knows them
+    on = None
     _fields_ = [
         ("k", c_void_p), ("v", c_void_p), ("len", c_void_p), ("err", c_void_p),
         ("seq_stride", c_int64), ("head_stride", c_int64), ("token_stride", c_int64),
@@ -452,6 +456,21 @@ def hkv_prefix_attention(cfg, prefix, q, out, lse, workspace, ws_bytes, stream=0
 _DTYPES = _PROMPT_DTYPES
 
 
+def _on(name, *given):
+    """The device's number (-1: the host) of the tensors among `given`, which
+    have to lie together; None without any."""
+    where = on = None
+    for x in given:
+        d = getattr(x, "device", None)   # an address has none
+        if d is None:
+            continue
+        if where is None:
+            where, on = d, x.get_device()
+        elif d != where:
+            raise HkvError(name, HKV_ERR_INVALID_ARG)
+    return on
+
+
 def hkv_make_rope(*, head_dim, rot_dim=None, layout=HKV_ROPE_HALF, sections=None, joint=False,
                   base=10000.0, scaling=HKV_ROPE_PLAIN, factor=1.0, original=1.0, low=1.0, high=32.0,
                   amplitude=1.0) -> hkv_rope:
@@ -479,13 +498,15 @@ def make_rows(x) -> hkv_rows:
     r = hkv_rows(y.data_ptr(), y.stride(0), y.stride(1), y.stride(2), y.shape[2], dtype)
     r.arrays = x
     r.of = (y.shape[0], y.shape[1], y.shape[3])
+    r.on = x.get_device()
     return r
 
 
 def make_tokens(n_tokens, length=None, pos=None, err=None) -> hkv_tokens:
     """hkv_tokens of n_tokens places a sequence; length: None, or contiguous
     int32 [sequences]; pos: None, or int32 positions of [axes][sequences or
-    1][n_tokens] or [sequences or 1][n_tokens], the last stride 1."""
+    1][n_tokens] or [sequences or 1][n_tokens], the last stride 1; all on the
+    device of the call's other views."""
     if length is not None and (str(length.dtype) != "torch.int32" or length.dim() != 1
                                or not length.is_contiguous()):
         raise HkvError("make_tokens", HKV_ERR_SHAPE)
@@ -497,11 +518,11 @@ def make_tokens(n_tokens, length=None, pos=None, err=None) -> hkv_tokens:
             raise HkvError("make_tokens", HKV_ERR_SHAPE)
         axes, rows = p.shape[0], p.shape[1]
         strides = (p.stride(0) if axes > 1 else 0, p.stride(1) if rows > 1 else 0)
-    if length is not None and pos is not None and length.device != pos.device:
-        raise HkvError("make_tokens", HKV_ERR_INVALID_ARG)
+    on = _on("make_tokens", length, pos, err)
     t = hkv_tokens(n_tokens, 0, _p(length), _p(pos), strides[0], strides[1], _p(err))
     t.arrays = (length, pos, err)
     t.of = (None if length is None else length.numel(), axes, rows)
+    t.on = on
     return t
 
 
@@ -523,6 +544,7 @@ def make_norm(kind, eps, q_weight=None, k_weight=None, q_bias=None, k_bias=None)
         raise HkvError("make_norm", HKV_ERR_SHAPE)
     n = hkv_norm(kind, eps, _p(q_weight), _p(q_bias), _p(k_weight), _p(k_bias), strides[0], strides[1])
     n.arrays = given
+    n.on = _on("make_norm", *given)
     if given:
         n.of = (_DTYPES[str(given[0].dtype)], given[0].shape[-1], heads[0], heads[1])
     return n
@@ -541,12 +563,12 @@ def make_states(k, v, length=None, err=None) -> hkv_states:
     if length is not None and (length.numel() != k.shape[0] or str(length.dtype) != "torch.int32"
                                or not length.is_contiguous()):
         raise HkvError("make_states", HKV_ERR_SHAPE)
-    if k.device != v.device or (length is not None and length.device != k.device):
-        raise HkvError("make_states", HKV_ERR_INVALID_ARG)
+    on = _on("make_states", k, v, length, err)
     s = hkv_states(k.data_ptr(), v.data_ptr(), _p(length), _p(err), k.stride(0), k.stride(1), k.stride(2),
                    k.shape[1], k.shape[2])
     s.arrays = (k, v, length, err)
     s.of = (dtype, k.shape[0], k.shape[3])
+    s.on = on
     return s
 
 
@@ -557,14 +579,18 @@ def _at(x):
     return None if x is None else _addr(x)
 
 
-def _fit(name, cfg, tokens, rope, rows) -> None:
-    """Refuses views whose known sizes are not the call's."""
+def _fit(name, cfg, tokens, rope, rows):
+    """Refuses views whose known sizes are not the call's. The number of their
+    device: None where it is not known, -1 for the host's or several."""
     seqs = cfg.n_seqs
     want = (seqs, tokens.n_tokens, cfg.head_dim)
-    ok = True
+    ok, on = True, tokens.on
     for r in rows:
-        if r is not None and r.of != want and r.of is not None:
-            ok = False
+        if r is not None:
+            if r.of != want and r.of is not None:
+                ok = False
+            if r.on != on and r.on is not None:
+                on = r.on if on is None else -1
     if tokens.of is not None:
         len_seqs, axes, pos_rows = tokens.of
         if len_seqs is not None and len_seqs != seqs:
@@ -573,10 +599,12 @@ def _fit(name, cfg, tokens, rope, rows) -> None:
             ok = False
     if not ok:
         raise HkvError(name, HKV_ERR_SHAPE)
+    return on
 
 
 def hkv_rope_rotate(cfg, rope, tokens, x, out, flags=0, stream=0) -> None:
-    _fit("rope_rotate", cfg, tokens, rope, (x, out))
+    if _fit("rope_rotate", cfg, tokens, rope, (x, out)) == -1:
+        raise HkvError("rope_rotate", HKV_ERR_INVALID_ARG)
     st = (_lib or lib()).hkv_rope_rotate(_addr(cfg), _addr(rope), _addr(tokens), _addr(x), _addr(out),
                                          flags, stream)
     if st != HKV_OK:
@@ -585,13 +613,17 @@ def hkv_rope_rotate(cfg, rope, tokens, x, out, flags=0, stream=0) -> None:
 
 def hkv_qk_norm_rope(cfg, norm, rope, tokens, q, k, v, q_out, k_out, v_out, stream=0) -> None:
     """norm and rope may be None, and pairs of q, k, v and their outs."""
-    _fit("qk_norm_rope", cfg, tokens, rope, (q, k, v, q_out, k_out, v_out))
+    on = _fit("qk_norm_rope", cfg, tokens, rope, (q, k, v, q_out, k_out, v_out))
     if norm is not None and norm.of is not None:
         dtype, dim, q_heads, k_heads = norm.of
         if dtype != cfg.dtype or dim != cfg.head_dim \
                 or (q is not None and q_heads is not None and q_heads != q.n_heads) \
                 or (k is not None and k_heads is not None and k_heads != k.n_heads):
             raise HkvError("qk_norm_rope", HKV_ERR_SHAPE)
+        if norm.on != on and norm.on is not None:
+            on = norm.on if on is None else -1
+    if on == -1:
+        raise HkvError("qk_norm_rope", HKV_ERR_INVALID_ARG)
     st = (_lib or lib()).hkv_qk_norm_rope(_addr(cfg), _at(norm), _at(rope), _addr(tokens), _at(q), _at(k),
                                           _at(v), _at(q_out), _at(k_out), _at(v_out), stream)
     if st != HKV_OK:
@@ -608,10 +640,37 @@ def hkv_cross_workspace_size(cfg, states, tokens) -> int:
     return int(lib().hkv_cross_workspace_size(_addr(cfg), _addr(states), _addr(tokens)))
 
 
+_float32 = None   # torch's, once a call has met it
+
+
 def hkv_cross_attention(cfg, states, tokens, q, out, lse, workspace, ws_bytes, flags=0, stream=0) -> None:
-    _fit("cross_attention", cfg, tokens, None, (q, out))
+    """lse: None, an address, or a contiguous fp32 tensor of [n_seqs][n_heads]
+    [n_tokens] elements at least; workspace: an address, or a tensor of ws_bytes
+    bytes at least."""
+    on = _fit("cross_attention", cfg, tokens, None, (q, out))
     if not _states_fit(cfg, states):
         raise HkvError("cross_attention", HKV_ERR_SHAPE)
+    if states.on != on and states.on is not None:
+        on = states.on if on is None else -1
+    global _float32
+    size = getattr(lse, "nbytes", None)
+    if size is not None:
+        if lse.dtype is not _float32:
+            if str(lse.dtype) != "torch.float32":
+                raise HkvError("cross_attention", HKV_ERR_SHAPE)
+            _float32 = lse.dtype
+        if size < 4 * cfg.n_seqs * cfg.n_heads * tokens.n_tokens or not lse.is_contiguous():
+            raise HkvError("cross_attention", HKV_ERR_SHAPE)
+        if lse.get_device() != on and on is not None:
+            on = -1
+    size = getattr(workspace, "nbytes", None)
+    if size is not None:
+        if size < ws_bytes:
+            raise HkvError("cross_attention", HKV_ERR_CAPACITY)
+        if workspace.get_device() != on and on is not None:
+            on = -1
+    if on == -1:
+        raise HkvError("cross_attention", HKV_ERR_INVALID_ARG)
     st = (_lib or lib()).hkv_cross_attention(_addr(cfg), _addr(states), _addr(tokens), _addr(q), _addr(out),
                                              _p(lse), _p(workspace), ws_bytes, flags, stream)
     if st != HKV_OK:
