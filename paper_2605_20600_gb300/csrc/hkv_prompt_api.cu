@@ -158,15 +158,15 @@ hkv_status hkv_make_rope(const hkv_rope_params *p, hkv_rope *rope) {
       (!(p->original > 0.0 && p->original < 1e30) || !(p->low >= 0.0 && p->low < p->high) ||
        !(p->high < 1e30)))
     return HKV_ERR_INVALID_ARG;
-  *rope = hkv_rope{};
-  rope->head_dim = p->head_dim;
-  rope->rot_dim = p->rot_dim;
-  rope->layout = p->layout;
-  rope->n_axes = p->n_axes;
-  rope->amplitude = (float)p->amplitude;
+  hkv_rope made = {};
+  made.head_dim = p->head_dim;
+  made.rot_dim = p->rot_dim;
+  made.layout = p->layout;
+  made.n_axes = p->n_axes;
+  made.amplitude = (float)p->amplitude;
   int pair = 0;
   for (int a = 0; a < p->n_axes; ++a) {
-    rope->section[a] = p->section[a];
+    made.section[a] = p->section[a];
     for (int i = 0; i < p->section[a]; ++i, ++pair) {
       const double d = p->joint ? p->rot_dim : 2.0 * p->section[a];
       double base = p->base;
@@ -178,10 +178,12 @@ hkv_status hkv_make_rope(const hkv_rope_params *p, hkv_rope *rope) {
         g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
         turns *= g + (1.0 - g) / p->factor;
       }
+      if (!(turns < HUGE_VAL)) return HKV_ERR_INVALID_ARG;  // of a base next to zero
       // a fraction of a turn below 1 - 2^-54, so that 2^64 times it fits
-      rope->turns[pair] = (uint64_t)ldexp(turns - floor(turns), 64);
+      made.turns[pair] = (uint64_t)ldexp(turns - floor(turns), 64);
     }
   }
+  *rope = made;
   return HKV_OK;
 }
 
