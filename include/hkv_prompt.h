@@ -12,8 +12,9 @@
  *     (x, y) -> A (x cos t - y sin t, x sin t + y cos t),
  * the other channels stay. With several axes every pair belongs to one of
  * them and turns by the token's position on it (row and column of an image
- * grid). An angle is taken modulo one turn in integers, f_i / 2 pi in 64 bits,
- * so that it is as exact at position 2^31 - 1 as at 1.
+ * grid). An angle is taken modulo one turn in integers, f_i / 2 pi in units of
+ * 2^-64: it is off by 2^-32 turns, and by 2^-51 of itself at any position up to
+ * 2^31 - 1 (the rounding of f_i in 64 bits).
  */
 #ifndef HKV_PROMPT_H
 #define HKV_PROMPT_H
@@ -37,7 +38,8 @@ enum {
   HKV_ROPE_LINEAR = 1, /* f / s */
   HKV_ROPE_BASE = 2,   /* base s^(d / (d - 2)) instead of base (d > 2) */
   HKV_ROPE_PARTS = 3   /* f (g + (1 - g) / s), g = (r - low) / (high - low)
-                        * within 0 .. 1, r = original f / 2 pi turns */
+                        * within 0 .. 1, r = original f / 2 pi turns: a ramp
+                        * over turns, not over the pairs' numbers */
 };
 
 /* flags of hkv_rope_rotate */
@@ -74,7 +76,9 @@ typedef struct {
 } hkv_rope_params;
 
 /* A rotation, made by hkv_make_rope: plain host data that calls copy.
- * turns[i] = f_i / 2 pi in units of 2^-64, modulo 1. */
+ * turns[i] = f_i / 2 pi in units of 2^-64, modulo 1; a caller whose model has
+ * other frequencies (a ramp over the pairs' numbers, a factor for each pair) makes
+ * a plain rotation and fills turns itself. */
 typedef struct {
   int32_t head_dim, rot_dim, layout, n_axes;
   int32_t section[3];
@@ -102,7 +106,8 @@ typedef struct {
  *        of places from len on are neither read nor written.
  *  pos   int32 (device) positions, for rotations: of token t of sequence s on
  *        axis a at a * pos_axis_stride + s * pos_seq_stride + t (a
- *        pos_seq_stride of 0: one row for all sequences); of either sign
+ *        pos_seq_stride of 0: one row for all sequences); of either sign; those
+ *        of places from len on are read too, and do not matter
  *  err   error word (a cache's), or NULL: a len outside its range sets
  *        HKV_ERR_BOUNDS there, and that sequence's outputs are left as they are
  */
@@ -191,7 +196,9 @@ size_t hkv_cross_workspace_size(const hkv_config *cfg, const hkv_states *states,
  * hkv_quant_attention and hkv_quant_step.
  * Scores and sums are fp32. The weights exp(score - a reference) are fp32 in
  * lse; their products with v take them in three bf16 parts for fp32 outs, and
- * for bf16 outs in two, or, for batches of many queries, rounded to bf16.
+ * for bf16 outs in two, or, where a key head has more than 128 query rows in the
+ * call (n_tokens times the query heads that read it), rounded to bf16: outs of a
+ * prompt as a whole and in pieces may differ by 2^-9 of the weights.
  * A key whose score is -inf (an infinite element against one of the other sign,
  * products below fp32's range) weighs nothing, and a query that has no other keys
  * gets zeros and -inf. Any other infinite or NaN element of a query or of a state

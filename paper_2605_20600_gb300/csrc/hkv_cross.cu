@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(W * 32, W == 8 ? 1 : 12 / W) cross_kernel(cons
 // channels (of 64: every second key) and all keys' weights.
 template <int D, int R>
 struct FSmem {
-  static constexpr int kWarps = D == 128 ? 2 : 4;               // three CTAs an SM
+  static constexpr int kWarps = D == 128 ? 2 : 4;               // three CTAs an SM (R = 16: two)
   static constexpr int kRow = D * 4 + 16, kTile = 32 * kRow;   // bytes
   static constexpr int kWarp = 2 * kTile;                       // K, V
   static constexpr int kTotal = kWarps * kWarp + R * D * 4 + kWarps * R * 32 * 4;
@@ -585,9 +585,10 @@ cudaError_t launch(const CrossArgs &a, const CrossPlan &pl, int dtype, int out_d
 
 }  // namespace
 
-// As many key ranges as fill the device twice over (2 CTAs an SM), each a whole
-// number of tiles. The 152 SMs are a constant here, so that the workspace a
-// caller allocated does not depend on the device of the call.
+// Key ranges for as many CTAs as the device holds at a time, once or several times
+// over, each a multiple of 64 keys (with tiles of 96, a range's last one is partly
+// empty). The 152 SMs are a constant here, so that the workspace a caller allocated
+// does not depend on the device of the call.
 CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, int dtype,
                      int out_dtype) {
   constexpr int kMostSplits = 456;
@@ -595,7 +596,8 @@ CrossPlan cross_plan(int seqs, int heads, int kv, int tokens, int keys, int D, i
   const long long all = (long long)(heads / kv) * tokens;
   const bool tc = all > 16 && out_dtype == HKV_BF16;
   pl.rows = all <= 16 ? 16 : tc && all > 128 ? 256 : 128;
-  // CTAs that the device holds at a time
+  // CTAs that the device holds at a time, three, two or one an SM (9 to 16 fp32 rows: two,
+  // counted as three here)
   const int ctas = pl.rows == 16 ? 456 : tc && pl.rows == 128 ? 304 : 152;
   // the tcgen05 kernel's query tiles: 128 tokens of a head, or all tokens of as
   // many heads of a group as fit 128 rows

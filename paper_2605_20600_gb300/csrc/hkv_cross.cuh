@@ -37,7 +37,7 @@ struct Work {
 };
 __device__ __forceinline__ Work work_of(const CrossArgs &p, int b) {
   Work w;
-  w.tile = p.tiles - 1 - b % p.tiles;  // causal: the longest rows of keys first
+  w.tile = p.tiles - 1 - b % p.tiles;  // causal: the longest rows of keys of a key head first
   b /= p.tiles;
   w.kvh = b % p.kv;
   b /= p.kv;

@@ -15,7 +15,9 @@
 //          one before are made (two buffers of S, of the last parts and of O)
 //
 // What bounds it: the chain of loads, parts and products around each tile of keys;
-// the tensor pipe is busy for 0.42. 1024 fp32 queries and states, 32 heads of 128:
+// the tensor pipe is busy for 0.42. Thirteen warps leave a thread 128 registers, too
+// few for warps 4-7 with heads of 128 (a row of O and 32 columns more): 428 bytes are
+// spilled (fp32; 52 with heads of 64). 1024 fp32 queries and states, 32 heads of 128:
 // 118 us (145 TFLOP/s of the definition's products, 873 of bf16 ones; six products
 // of parts on mma.sync took 915, Q loaded by the warps of K and V first 140); 257
 // padded queries over up to 777 states, 5 x 8 heads of 64: 22.5 us (28).

@@ -22,15 +22,16 @@
 // zero times what lies there could be NaN); scores past it are masked.
 //
 // What bounds it, heads of 128: the products, which keep the tensor pipe busy for
-// 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 318 us, 1729 TFLOP/s;
-// causal over 4288: 0.70, 222 us). On the way: products issued from divergent code,
+// 0.77 of the cycles (2 x 32 heads of 4096 queries and keys: 321 us, 1713 TFLOP/s;
+// causal over 4288: 0.70, 225 us: key heads come one after the other, so that the last
+// one's long tiles start late and end at 1.15 of the mean work of a CTA). On the way: products issued from divergent code,
 // each operand's descriptor moved to uniform registers, 470;
 // from uniform code, K and V in one wait, 387; S in two buffers, so that products
 // and weights of a tile overlap, 341; the scores after the next behind a tile's
 // W V, one wait a tile, 322. Two threads a row: 365 (their agreement on a maximum
 // costs more than half of the exponentials); one warp for both tiles' products in
 // turn: 387; tiles of 128 keys leave no room in TMEM for a second S. Heads of 64
-// have half of the products: 267 us (306 in tiles of 64 keys), bound by the weights
+// have half of the products: 269 us (306 in tiles of 64 keys), bound by the weights
 // (96 exponentials a row and tile, and the chain around them). Short states: a
 // piece of work's chain, 8 x 4160 queries of 32 heads over 120: 111 us, 5 TB/s (145
 // with every warp working out what the next piece is, and 16-byte stores of outs).
